@@ -262,6 +262,177 @@ int jb_max_seeds_per_call(void);
 const char* jb_status_string(int status);
 
 /* ---------------------------------------------------------------------------
+ * Writing answers with the perturbed model. A sample's score need not be a loss
+ * with a gradient: accuracy or a reward of what the model writes serves as well.
+ * The calls below are those that writing needs between two perturbations: a
+ * cache of keys and values in pages, attention of new tokens over it, and the
+ * draw of the next token from a given random word (the same words at +eps and
+ * -eps, so that the two scores differ by the weights alone).
+ *
+ * All arrays named d_* and all pointers in jb_pages and jb_kv are device memory,
+ * caller-owned; the structures themselves are host memory, copied during the
+ * call. Everything is enqueued on `stream`, and nothing is read back: lengths,
+ * page tables and page counts live on the device, so a whole generation step can
+ * be captured in a CUDA graph. Argument errors that the host can see are statuses,
+ * as above. What only the device can see (a row index out of range, too few free
+ * pages) never causes an access out of bounds; each call says what happens.
+ * ------------------------------------------------------------------------- */
+
+/* The pages of a cache: row r holds lens[r] tokens, token t in page
+ * table[r * row_pages + t / page_tokens] at place t % page_tokens. Entries past a
+ * row's last page are -1. refs[p] counts the entries that name page p (rows forked
+ * from one another share full pages); a page with refs 0 is free. An empty cache:
+ * table all -1, lens and refs all 0. The arrays are kept consistent by jb_cache_*.
+ *   page_tokens  a multiple of 16, at most 1024
+ *   n_rows       at most 65536;  row_pages * page_tokens below 2^31
+ */
+typedef struct {
+    int32_t* table; /* [n_rows][row_pages] */
+    int32_t* lens;  /* [n_rows] */
+    int32_t* refs;  /* [n_pages] */
+    int32_t n_rows;
+    int32_t row_pages;
+    int32_t n_pages;
+    int32_t page_tokens;
+} jb_pages;
+
+/* One layer's keys and values: page p at k (v) + p * page_stride elements, in it
+ * [heads][page_tokens][head_dim] (by_token = 0) or [page_tokens][heads][head_dim]
+ * (by_token = 1), without gaps.
+ *   dtype     JB_F32 or JB_BF16, of keys, values, queries and outputs alike
+ *   head_dim  at most 256, rows of a multiple of 16 bytes; k, v 16-byte aligned,
+ *             page_stride a multiple of 16 bytes and at least a page
+ */
+typedef struct {
+    void* k;
+    void* v;
+    uint64_t page_stride;
+    int32_t heads;
+    int32_t head_dim;
+    int32_t dtype;
+    int32_t by_token;
+} jb_kv;
+
+/*
+ * jb_cache_reserve -- room for new tokens: lens[d_rows[i]] += d_tokens[i], with free
+ * pages taken for it, the lowest ids first, in the order of the list (i, then the
+ * row's pages). The listed rows must differ. *d_status (one int32) receives
+ *    0   done
+ *   >0   that many free pages too few: nothing is changed
+ *   -1   a row index out of range or listed twice, a negative count, or a row that
+ *        would outgrow its table: nothing is changed
+ *   n    at most 16384 rows a call; 0 is a no-op that writes status 0.
+ */
+int jb_cache_reserve(const jb_pages* pages, const int32_t* d_rows, const int32_t* d_tokens, int n,
+                     int32_t* d_status, struct CUstream_st* stream);
+
+/*
+ * jb_cache_free -- the listed rows become empty; pages that no row names any more are
+ * free. Listing a row twice frees it once; an index out of range is skipped.
+ */
+int jb_cache_free(const jb_pages* pages, const int32_t* d_rows, int n, struct CUstream_st* stream);
+
+/*
+ * jb_cache_fork -- row d_children[i] becomes a copy of row d_parents[i], for all i at
+ * once (a row may be both: its state before the call is what is copied). Full pages
+ * are shared; the last page, if it is not full, is copied in every layer to a page
+ * that is free before the call (the lowest ids, in the order of the list): its valid
+ * tokens, the rest of that page is left as it is. The child's former pages are
+ * released. A pair with equal rows changes nothing. *d_status as for
+ * jb_cache_reserve: -1 for an index out of range or a child listed twice.
+ *   workspace  jb_cache_workspace(pages, n) bytes, 16-byte aligned, contents free
+ */
+int jb_cache_fork(const jb_pages* pages, const jb_kv* layers, int n_layers, const int32_t* d_parents,
+                  const int32_t* d_children, int n, int32_t* d_status, void* workspace,
+                  uint64_t workspace_bytes, struct CUstream_st* stream);
+
+/*
+ * jb_cache_compact -- moves pages so that the n_live pages in use are ids 0 ..
+ * n_live - 1: the i-th page in use at or above n_live goes to the i-th free page below
+ * it, in every layer. Tables and counts follow. *d_status receives n_live.
+ *   workspace  jb_cache_workspace(pages, 0) bytes
+ */
+int jb_cache_compact(const jb_pages* pages, const jb_kv* layers, int n_layers, int32_t* d_status,
+                     void* workspace, uint64_t workspace_bytes, struct CUstream_st* stream);
+
+/* Device bytes that jb_cache_fork of n pairs (n > 0) or jb_cache_compact (n = 0) works in. */
+uint64_t jb_cache_workspace(const jb_pages* pages, int n);
+
+/*
+ * jb_cache_write -- new keys and values to their places: token i, d_k[i][head][:] and
+ * d_v[i][head][:] of the layer's dtype, to position d_pos[i] of row d_rows[i] (room for
+ * it reserved before). A token whose row, position or page is out of range is skipped;
+ * two tokens with the same place race.
+ *   strides  in elements, multiples of 16 bytes: from token to token and head to head
+ */
+int jb_cache_write(const jb_pages* pages, const jb_kv* layer, const void* d_k, uint64_t k_token_stride,
+                   uint64_t k_head_stride, const void* d_v, uint64_t v_token_stride, uint64_t v_head_stride,
+                   const int32_t* d_rows, const int32_t* d_pos, int n, struct CUstream_st* stream);
+
+/* What jb_attend does to the scores, besides their scale. */
+typedef struct {
+    float scale;         /* x = scale q.k */
+    float softcap;       /* > 0: x = softcap tanh(x / softcap); 0: off */
+    int32_t window;      /* > 0: only the last `window` positions are seen; 0: all */
+    const float* slopes; /* device, one per query head: x += slope (t - pos); NULL: off */
+} jb_scores;
+
+/*
+ * jb_attend -- attention of n queries over the pages: query i, head a reads key head
+ * a / (q_heads / heads) of positions t <= d_pos[i] of row d_rows[i] (and
+ * t > d_pos[i] - window):
+ *   out = sum_t exp(x_t) v_t / sum_t exp(x_t)
+ * A new token's query comes with the position that its key was written to; the tokens
+ * of a prompt are queries of one row with consecutive positions. A query that sees
+ * nothing (position -1, or a row or position out of range) gets zeros; a position whose
+ * page is missing is not seen. What a page holds past the last position seen has no
+ * effect, NaN included. Results are bitwise repeatable.
+ * Scores, maxima and sums are fp32; fp32 caches are computed in fp32. With bf16 the
+ * products run on the tensor cores with fp32 sums, and a weight exp(x_t) enters them
+ * as the sum of two bf16 numbers (16 bits of it).
+ *   q_heads    a multiple of the layer's heads
+ *   strides    in elements, multiples of 16 bytes; pointers 16-byte aligned
+ *   workspace  jb_attend_workspace(...) bytes, 16-byte aligned, contents free
+ */
+int jb_attend(const jb_pages* pages, const jb_kv* layer, const jb_scores* scores, const void* d_q,
+              uint64_t q_row_stride, uint64_t q_head_stride, int q_heads, const int32_t* d_rows,
+              const int32_t* d_pos, int n, void* d_out, uint64_t out_row_stride, uint64_t out_head_stride,
+              void* workspace, uint64_t workspace_bytes, struct CUstream_st* stream);
+
+/* Device bytes that jb_attend works in, for any n. */
+uint64_t jb_attend_workspace(const jb_kv* layer, int q_heads);
+
+/* Per-row settings of jb_sample: device arrays of n entries, or NULL for the default.
+ * temperature (1): below 2^-64 or NaN, the row's largest logit is taken (the first one).
+ * top_k (0): <= 0 or at least the vocabulary keeps all. top_p (1): >= 1 or NaN keeps all.
+ * min_p (0): <= 0 or NaN keeps all, above 1 counts as 1. */
+typedef struct {
+    const float* temperature;
+    const int32_t* top_k;
+    const float* top_p;
+    const float* min_p;
+} jb_sampling;
+
+/*
+ * jb_sample -- the next token of each row from its logits and one random word:
+ *   L = max l;  y_j = (l_j - L) (1 / temperature);  w_j = rint(2^30 exp(y_j))
+ * Weights are integers, so sums of them are exact and the draw does not depend on the
+ * order in which they are added. Tokens are ordered by logit, equal ones by index; kept
+ * are the first top_k; of those the shortest run from the front whose weights reach
+ * ceil(top_p W), W their sum; of those the ones with w_j >= ceil(min_p 2^30). Then, with
+ * W the sum of the kept weights, the token is the first index whose running sum of kept
+ * weights exceeds floor(word W / 2^32), and its log-probability y - ln(W / 2^30).
+ * NaN logits are never drawn; logits of +inf share the draw among themselves. A row with
+ * nothing to draw (all -inf or NaN) gives token -1 and -inf.
+ *   d_logits   [n][vocab] of dtype, rows at row_stride elements; vocab at most 262144
+ *   d_words    n random 32-bit words
+ *   d_tokens, d_logprobs  n results each; d_logprobs may be NULL
+ */
+int jb_sample(const void* d_logits, uint64_t row_stride, int dtype, int n, int vocab,
+              const jb_sampling* sampling, const uint32_t* d_words, int32_t* d_tokens, float* d_logprobs,
+              struct CUstream_st* stream);
+
+/* ---------------------------------------------------------------------------
  * Test hooks (not on the hot path). Device buffers are caller-owned.
  * ------------------------------------------------------------------------- */
 

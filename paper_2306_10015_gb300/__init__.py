@@ -15,6 +15,14 @@ streams. The functions keep the C names:
 * ``jb_quantize_grad`` / ``jb_dequantize_grad``  the one-byte projected
   gradient (Section 3, Training Speed)
 
+and, for scores that are not losses, what writing an answer with the perturbed model needs:
+
+* ``jb_cache_reserve``, ``jb_cache_fork``, ``jb_cache_free``, ``jb_cache_compact``  the pages
+  of a key-value cache (``PageTable``, ``KVCache``)
+* ``jb_cache_write``  new keys and values to their places in the pages
+* ``jb_attend``  attention of new tokens over the pages
+* ``jb_sample``  the next token from its logits and a given random word
+
 There is no CPU fallback: if ``libjb.so`` is missing, loading it raises.
 """
 from __future__ import annotations
@@ -51,6 +59,28 @@ class jb_segment(ctypes.Structure):
 class jb_q4_segment(ctypes.Structure):
     _fields_ = [("codes", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("numel", ctypes.c_uint64),
                 ("flat_offset", ctypes.c_uint64)]
+
+
+class jb_pages(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("refs", ctypes.c_void_p),
+                ("n_rows", ctypes.c_int32), ("row_pages", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("page_tokens", ctypes.c_int32)]
+
+
+class jb_kv(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_stride", ctypes.c_uint64),
+                ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("by_token", ctypes.c_int32)]
+
+
+class jb_scores(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("window", ctypes.c_int32),
+                ("slopes", ctypes.c_void_p)]
+
+
+class jb_sampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p),
+                ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p)]
 
 
 class jb_seed(ctypes.Structure):
@@ -92,6 +122,18 @@ def lib() -> ctypes.CDLL:
             L.jb_max_seeds_per_call.argtypes = []
             L.jb_status_string.argtypes = [i32]
             L.jb_status_string.restype = ctypes.c_char_p
+            L.jb_cache_reserve.argtypes = [vp, vp, vp, i32, vp, vp]
+            L.jb_cache_free.argtypes = [vp, vp, i32, vp]
+            L.jb_cache_fork.argtypes = [vp, vp, i32, vp, vp, i32, vp, vp, u64, vp]
+            L.jb_cache_compact.argtypes = [vp, vp, i32, vp, vp, u64, vp]
+            L.jb_cache_write.argtypes = [vp, vp, vp, u64, u64, vp, u64, u64, vp, vp, i32, vp]
+            L.jb_attend.argtypes = [vp, vp, vp, vp, u64, u64, i32, vp, vp, i32, vp, u64, u64, vp,
+                                    u64, vp]
+            L.jb_sample.argtypes = [vp, u64, i32, i32, i32, vp, vp, vp, vp, vp]
+            L.jb_cache_workspace.argtypes = [vp, i32]
+            L.jb_cache_workspace.restype = u64
+            L.jb_attend_workspace.argtypes = [vp, i32]
+            L.jb_attend_workspace.restype = u64
             L.jb_debug_philox.argtypes = [jb_seed, u64, u64, vp, vp]
             L.jb_debug_philox_fold.argtypes = [jb_seed, u64, u64, vp, vp]
             L.jb_debug_gaussian.argtypes = [jb_seed, u64, u64, vp, vp]
@@ -99,6 +141,8 @@ def lib() -> ctypes.CDLL:
             for f in ("jb_perturb", "jb_perturb_with_grid", "jb_apply_updates",
                       "jb_apply_updates_with_grid", "jb_apply_updates_from", "jb_replay_updates",
                       "jb_checksum", "jb_checksum_with_grid", "jb_perturb_q4", "jb_q4_levels",
+                      "jb_cache_reserve", "jb_cache_free", "jb_cache_fork", "jb_cache_compact",
+                      "jb_cache_write", "jb_attend", "jb_sample",
                       "jb_quantize_grad", "jb_dequantize_grad",
                       "jb_max_seeds_per_call", "jb_debug_philox", "jb_debug_philox_fold",
                       "jb_debug_gaussian",
@@ -314,6 +358,248 @@ def jb_checksum(table: ParamTable, out, stream=None, grid_ctas: int = 0) -> None
     _check(rc)
 
 
+# --- writing answers ------------------------------------------------------------
+
+def _list32(t, what: str):
+    """A one-dimensional contiguous int32 CUDA tensor: its address and length."""
+    import torch
+    if t.dtype is not torch.int32 or not t.is_cuda or t.dim() != 1 or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous one-dimensional int32 CUDA tensor")
+    return t.data_ptr(), t.shape[0]
+
+
+def _two_lists(a, b, what: str):
+    pa, n = _list32(a, what)
+    pb, m = _list32(b, what)
+    if n != m:
+        raise ValueError(f"{what} must have the same length")
+    return pa, pb, n
+
+
+def _storage(dtype) -> int:
+    import torch
+    if dtype is torch.bfloat16:
+        return JB_BF16
+    if dtype is torch.float32:
+        return JB_F32
+    raise TypeError(f"tensors must be float32 or bfloat16, got {dtype}")
+
+
+class PageTable:
+    """The rows of a cache and their pages (jb_pages): ``table`` [rows, row_pages], ``lens`` [rows]
+    and ``refs`` [pages], int32 CUDA tensors that the jb_cache_* calls keep consistent. Holds
+    references to them. ``PageTable.empty`` makes them."""
+
+    def __init__(self, table, lens, refs, page_tokens: int):
+        import torch
+        for t, dim in ((table, 2), (lens, 1), (refs, 1)):
+            if t.dtype is not torch.int32 or not t.is_cuda or t.dim() != dim or not t.is_contiguous():
+                raise ValueError("table [rows, row_pages], lens [rows] and refs [pages] must be contiguous int32 CUDA tensors")
+        if lens.shape[0] != table.shape[0]:
+            raise ValueError("one length per row of the table")
+        if not 16 <= page_tokens <= 1024 or page_tokens % 16:
+            raise ValueError("page_tokens must be a multiple of 16, at most 1024")
+        self.table, self.lens, self.refs, self.page_tokens = table, lens, refs, int(page_tokens)
+        self.struct = jb_pages(table.data_ptr(), lens.data_ptr(), refs.data_ptr(), table.shape[0],
+                               table.shape[1], refs.shape[0], self.page_tokens)
+        self.ref = ctypes.byref(self.struct)
+
+    @classmethod
+    def empty(cls, n_rows: int, row_pages: int, n_pages: int, page_tokens: int, device="cuda") -> "PageTable":
+        import torch
+        return cls(torch.full((n_rows, row_pages), -1, dtype=torch.int32, device=device),
+                   torch.zeros(n_rows, dtype=torch.int32, device=device),
+                   torch.zeros(n_pages, dtype=torch.int32, device=device), page_tokens)
+
+
+class KVCache:
+    """Keys and values of a model's layers in pages: one tensor [pages, heads, page_tokens, head_dim]
+    a layer in ``keys`` and ``values``, float32 or bfloat16, whose pages are contiguous with heads
+    before tokens or (transposed view) tokens before heads. Holds references to the tensors."""
+
+    def __init__(self, pages: PageTable, keys: Sequence, values: Sequence):
+        self.pages, self.keys, self.values = pages, list(keys), list(values)
+        if not self.keys or len(self.keys) != len(self.values):
+            raise ValueError("one tensor of keys and one of values per layer")
+        first = self.keys[0]
+        self.dtype = _storage(first.dtype)
+        if first.dim() != 4:
+            raise ValueError("keys and values must be [pages, heads, page_tokens, head_dim]")
+        n_pages, heads, tokens, d = first.shape
+        if n_pages != pages.refs.shape[0] or tokens != pages.page_tokens:
+            raise ValueError("the tensors' pages differ from the table's")
+        inner = first.stride()[1:]
+        if inner == (tokens * d, d, 1):
+            by_token = 0
+        elif inner == (d, heads * d, 1):
+            by_token = 1
+        else:
+            raise ValueError("a page must be contiguous, by heads or by tokens")
+        for t in self.keys + self.values:
+            if t.shape != first.shape or t.dtype != first.dtype or t.stride() != first.stride() or not t.is_cuda:
+                raise ValueError("keys and values must be CUDA tensors of one shape, type and layout")
+        n = len(self.keys)
+        self.torch_dtype, self.heads, self.head_dim, self.n_layers = first.dtype, heads, d, n
+        self.layers = (jb_kv * n)()
+        for i, (k, v) in enumerate(zip(self.keys, self.values)):
+            self.layers[i] = jb_kv(k.data_ptr(), v.data_ptr(), first.stride(0), heads, d, self.dtype, by_token)
+        self.layer_refs = [ctypes.byref(self.layers, i * ctypes.sizeof(jb_kv)) for i in range(n)]
+        self.attend_bytes = int(lib().jb_attend_workspace(self.layer_refs[0], heads))
+
+
+def _new(stream, make, *args, **kwargs):
+    """make(...) on the call's stream: what the allocator hands out is ordered with that stream alone."""
+    import torch
+    if stream is None:
+        return make(*args, **kwargs)
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+        return make(*args, **kwargs)
+
+
+def _status_of(status, like, stream):
+    import torch
+    if status is None:
+        return _new(stream, torch.empty, 1, dtype=torch.int32, device=like.device)
+    if _list32(status, "status")[1] != 1:
+        raise ValueError("status must have one element")
+    return status
+
+
+def _scratch(nbytes: int, like, stream):
+    """Device bytes for one call."""
+    import torch
+    return _new(stream, torch.empty, nbytes, dtype=torch.uint8, device=like.device)
+
+
+def jb_cache_reserve(cache, rows, tokens, status=None, stream=None):
+    """Room for tokens[i] more tokens in row rows[i]; returns the status tensor (0: done, > 0:
+    that many pages too few, -1: bad list; then nothing is changed). `cache`: a KVCache or its
+    PageTable."""
+    pages = getattr(cache, "pages", cache)
+    pr, pt, n = _two_lists(rows, tokens, "rows and tokens")
+    status = _status_of(status, pages.refs, stream)
+    _check(lib().jb_cache_reserve(pages.ref, pr, pt, n, status.data_ptr(), _stream(stream)))
+    return status
+
+
+def jb_cache_free(cache, rows, stream=None) -> None:
+    """The rows become empty; pages that no other row names are free."""
+    pages = getattr(cache, "pages", cache)
+    pr, n = _list32(rows, "rows")
+    _check(lib().jb_cache_free(pages.ref, pr, n, _stream(stream)))
+
+
+def jb_cache_fork(cache: KVCache, parents, children, status=None, stream=None):
+    """Row children[i] becomes a copy of row parents[i] (all at once): full pages shared, the last
+    one copied in every layer. Returns the status tensor as jb_cache_reserve does."""
+    pages = cache.pages
+    pp, pc, n = _two_lists(parents, children, "parents and children")
+    status = _status_of(status, pages.refs, stream)
+    nbytes = 0 if n == 0 else 4 * (16 + 2 * n + n * pages.struct.row_pages)
+    ws = _scratch(max(nbytes, 16), pages.refs, stream)
+    _check(lib().jb_cache_fork(pages.ref, cache.layers, cache.n_layers, pp, pc, n, status.data_ptr(),
+                               ws.data_ptr(), nbytes, _stream(stream)))
+    return status
+
+
+def jb_cache_compact(cache: KVCache, status=None, stream=None):
+    """Moves the pages in use to the lowest ids; returns the status tensor: how many they are."""
+    pages = cache.pages
+    status = _status_of(status, pages.refs, stream)
+    nbytes = int(lib().jb_cache_workspace(pages.ref, 0))
+    ws = _scratch(max(nbytes, 16), pages.refs, stream)
+    _check(lib().jb_cache_compact(pages.ref, cache.layers, cache.n_layers, status.data_ptr(),
+                                  ws.data_ptr(), nbytes, _stream(stream)))
+    return status
+
+
+def _heads_of(t, heads: int, cache: KVCache, n: int, what: str):
+    """Strides of a [n, heads, head_dim] CUDA tensor whose rows are contiguous."""
+    if t.dtype is not cache.torch_dtype or not t.is_cuda:
+        raise ValueError(f"{what} must be CUDA tensors of the cache's type")
+    if t.dim() != 3 or t.shape != (n, heads, cache.head_dim):
+        raise ValueError(f"{what} must be [{n}, {heads}, {cache.head_dim}], got {tuple(t.shape)}")
+    a, b, c = t.stride()
+    if c != 1 and cache.head_dim > 1:
+        raise ValueError(f"{what} must be contiguous in their last dimension")
+    return a, b
+
+
+def jb_cache_write(cache: KVCache, layer: int, k, v, rows, pos, stream=None) -> None:
+    """Keys and values k[i], v[i] ([n, heads, head_dim]) of a layer to position pos[i] of row rows[i]."""
+    pr, pp, n = _two_lists(rows, pos, "rows and positions")
+    ka, kb = _heads_of(k, cache.heads, cache, n, "new keys")
+    va, vb = _heads_of(v, cache.heads, cache, n, "new values")
+    _check(lib().jb_cache_write(cache.pages.ref, cache.layer_refs[layer], k.data_ptr(), ka, kb, v.data_ptr(), va, vb,
+                                pr, pp, n, _stream(stream)))
+
+
+def jb_attend(cache: KVCache, layer: int, q, rows, pos, out=None, scale: Optional[float] = None,
+              softcap: float = 0.0, window: int = 0, slopes=None, stream=None):
+    """Attention of queries q [n, q_heads, head_dim] over positions <= pos[i] of row rows[i];
+    returns ``out``. Scores are scale q.k (default 1 / sqrt(head_dim)), capped by softcap tanh,
+    biased by slopes[head] (t - pos), limited to the last `window` positions."""
+    import torch
+    pr, pp, n = _two_lists(rows, pos, "rows and positions")
+    heads = q.shape[1] if q.dim() == 3 else 0
+    qa, qb = _heads_of(q, heads, cache, n, "queries")
+    if out is None:
+        out = _new(stream, torch.empty, (n, heads, cache.head_dim), dtype=q.dtype, device=q.device)
+    oa, ob = _heads_of(out, heads, cache, n, "outputs")
+    if slopes is not None and (slopes.dtype is not torch.float32 or not slopes.is_cuda or slopes.shape != (heads,)
+                               or not slopes.is_contiguous()):
+        raise ValueError("slopes must be a contiguous float32 CUDA tensor, one per query head")
+    ws = _scratch(cache.attend_bytes, q, stream)
+    scores = jb_scores(cache.head_dim ** -0.5 if scale is None else scale, softcap, window,
+                       None if slopes is None else slopes.data_ptr())
+    _check(lib().jb_attend(cache.pages.ref, cache.layer_refs[layer], ctypes.byref(scores), q.data_ptr(), qa, qb, heads,
+                           pr, pp, n, out.data_ptr(), oa, ob, ws.data_ptr(), cache.attend_bytes, _stream(stream)))
+    return out
+
+
+def _per_row(value, default, n: int, dtype, device, stream):
+    """A setting of jb_sample as the address of n entries (None where it is the default) and the
+    tensor that holds them."""
+    import torch
+    if not isinstance(value, torch.Tensor):
+        if value == default:
+            return None, None
+        value = _new(stream, torch.full, (n,), value, dtype=dtype, device=device)
+    if value.dtype is not dtype or not value.is_cuda or value.shape != (n,) or not value.is_contiguous():
+        raise ValueError(f"a setting per row must be a contiguous {dtype} CUDA tensor of {n} entries")
+    return value.data_ptr(), value
+
+
+def jb_sample(logits, words, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tokens=None, logprobs=None,
+              stream=None):
+    """The next token of each row of logits [n, vocab] from its random word (int32 or uint32 bits),
+    and its log-probability; returns (tokens int32, logprobs float32). Settings are numbers or one
+    per row (float32, top_k int32 CUDA tensors)."""
+    import torch
+    if logits.dim() != 2 or not logits.is_cuda or (logits.stride(1) != 1 and logits.shape[1] > 1):
+        raise ValueError("logits must be a CUDA tensor [n, vocab], contiguous in a row")
+    n, vocab = logits.shape
+    if words.dtype not in (torch.int32, torch.uint32) or not words.is_cuda or words.shape != (n,) or not words.is_contiguous():
+        raise ValueError("words must be a contiguous int32 or uint32 CUDA tensor, one per row")
+    dev = logits.device
+    t, t_ = _per_row(temperature, 1.0, n, torch.float32, dev, stream)
+    k, k_ = _per_row(top_k, 0, n, torch.int32, dev, stream)
+    p, p_ = _per_row(top_p, 1.0, n, torch.float32, dev, stream)
+    m, m_ = _per_row(min_p, 0.0, n, torch.float32, dev, stream)
+    if tokens is None:
+        tokens = _new(stream, torch.empty, n, dtype=torch.int32, device=dev)
+    elif _list32(tokens, "tokens")[1] != n:
+        raise ValueError("one token per row")
+    if logprobs is None:
+        logprobs = _new(stream, torch.empty, n, dtype=torch.float32, device=dev)
+    elif logprobs.dtype is not torch.float32 or not logprobs.is_cuda or logprobs.shape != (n,) or not logprobs.is_contiguous():
+        raise ValueError("logprobs must be a contiguous float32 CUDA tensor, one per row")
+    settings = jb_sampling(t, k, p, m)
+    _check(lib().jb_sample(logits.data_ptr(), logits.stride(0), _storage(logits.dtype), n, vocab, ctypes.byref(settings),
+                           words.data_ptr(), tokens.data_ptr(), logprobs.data_ptr(), _stream(stream)))
+    return tokens, logprobs
+
+
 def jb_quantize_grad(g: float, qscale: float = 1.0) -> int:
     out = ctypes.c_int8()
     _check(lib().jb_quantize_grad(float(g), float(qscale), ctypes.byref(out)))
@@ -360,7 +646,9 @@ __all__ = [
     "JB_OK", "JB_F32", "JB_BF16", "SEED_DTYPE", "JbError", "ParamTable", "jb_segment", "jb_seed",
     "lib", "seeds_array", "default_flat_offsets", "jb_perturb", "jb_apply_updates",
     "jb_apply_updates_from", "jb_replay_updates", "jb_checksum", "jb_perturb_q4", "jb_q4_levels",
-    "Q4Table", "jb_q4_segment",
+    "Q4Table", "jb_q4_segment", "PageTable", "KVCache", "jb_pages", "jb_kv", "jb_scores", "jb_sampling",
+    "jb_cache_reserve", "jb_cache_free", "jb_cache_fork", "jb_cache_compact", "jb_cache_write",
+    "jb_attend", "jb_sample",
     "jb_quantize_grad", "jb_dequantize_grad", "jb_max_seeds_per_call", "jb_status_string",
     "jb_debug_philox", "jb_debug_gaussian", "jb_debug_box_muller",
 ]

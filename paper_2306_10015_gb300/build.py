@@ -2,7 +2,7 @@
 
     python -m paper_2306_10015_gb300.build
 
-Two translation units compiled in parallel by nvcc, linked with the static
+Translation units compiled in parallel by nvcc, linked with the static
 CUDA runtime. No fast-math: the fp32 arithmetic of the kernels is written with
 explicit round-to-nearest intrinsics and must not be re-associated.
 """
@@ -20,8 +20,9 @@ OUT_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(OUT_DIR, "libjb.so")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
-SOURCES = ["jb_kernels.cu", "jb_q4.cu", "jb_capi.cpp"]
-HEADERS = ["jb_rng.cuh", "jb_internal.h", "jb_offgrid.h"]
+SOURCES = ["jb_kernels.cu", "jb_q4.cu", "jb_attend.cu", "jb_pages.cu", "jb_sample.cu", "jb_capi.cpp",
+           "jb_answer_capi.cpp"]
+HEADERS = ["jb_rng.cuh", "jb_internal.h", "jb_offgrid.h", "jb_answer.h", "jb_host.h"]
 
 
 def nvcc() -> str:

@@ -9,37 +9,22 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
-#include <new>
 #include <vector>
 
 #include "jb.h"
+#include "jb_host.h"
 #include "jb_internal.h"
-
-#define JB_EXPORT extern "C" __attribute__((visibility("default")))
 
 namespace {
 
 constexpr uint64_t kMaxIndex = 1ull << 62;  // global element indices stay below this
 
+using jb::cuda_status;
+using jb::guarded;
+using jb::range_fits;
 using jb::Seg;
 
 size_t elem_size(int dtype) { return dtype == JB_F32 ? 4 : 2; }
-
-// [p, p + n * es) fits in the address space (written so that n * es cannot wrap).
-bool range_fits(uint64_t p, uint64_t n, uint64_t es) { return n <= (UINT64_MAX - p) / es; }
-
-// Runs an entry point's body; a host allocation failure (or any other C++
-// exception) becomes a status instead of crossing the C interface.
-template <typename F>
-int guarded(F&& body) noexcept {
-    try {
-        return body();
-    } catch (const std::bad_alloc&) {
-        return JB_ERR_NO_MEMORY;
-    } catch (...) {
-        return JB_ERR_INVALID_ARG;
-    }
-}
 
 // Checks the segment table; drops empty segments. Overlap in memory or in
 // global index is an argument error.
@@ -152,16 +137,6 @@ double dequantize(int8_t q, double qscale) {
     if (m > 127) m = 127;
     const double v = std::expm1(static_cast<double>(m) / qscale);
     return q < 0 ? -v : v;
-}
-
-// libjb links the CUDA runtime statically: its last-error state is its own, so the
-// errors of a caller's runtime (torch's, say) are neither seen nor cleared here. A
-// failed call of this library's is cleared from that state (cudaGetLastError) so that
-// it cannot be reported again by a later, unrelated call.
-int cuda_status(cudaError_t e) {
-    if (e == cudaSuccess) return JB_OK;
-    (void)cudaGetLastError();
-    return JB_ERR_CUDA;
 }
 
 int perturb_impl(const jb_segment* segs, int n_segs, int dtype, jb_seed seed, float eps,
@@ -453,7 +428,7 @@ JB_EXPORT const char* jb_status_string(int status) {
         case JB_OK: return "ok";
         case JB_ERR_INVALID_ARG: return "invalid argument";
         case JB_ERR_UNSUPPORTED_DTYPE: return "unsupported dtype (use JB_F32 or JB_BF16)";
-        case JB_ERR_MISALIGNED: return "segment pointer not aligned to its element size";
+        case JB_ERR_MISALIGNED: return "pointer or stride not aligned as the call needs";
         case JB_ERR_DUPLICATE_SEED: return "duplicate (machine_id, step, sample_id) seed";
         case JB_ERR_CUDA: return "CUDA runtime or launch error";
         case JB_ERR_RANGE: return "update coefficient not finite in fp32";

@@ -1,0 +1,281 @@
+"""jb_attend against the definition in 64 bits, where it can go wrong: lengths around groups and pages,
+empty and invalid queries, heads that share keys, head sizes between the kernels', both layouts, what
+unseen places hold, strides, streams, offsets past 32 bits.
+
+Tolerances. With A = sum_t p_t |v_t| (p the exact weights) and S = max_t scale sum_e |q_e k_e|:
+* a score is a sum of d products in fp32 and a few roundings: off by at most (d + 16) 2^-23 S (and as
+  much again for the cap and the bias, whose operands are below S' = S + bias), which moves every
+  weight by that factor, twice (numerator and sum);
+* the exponential is good to 2^-21, weights enter bf16 products with 2^-16, the sums of T terms lose at
+  most T 2^-23;
+* a bf16 result is rounded once, 2^-9 of it (2^-8 allows for the tie).
+"""
+import math
+
+import pytest
+import torch
+
+import paper_2306_10015_gb300 as jb
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def make(dtype, lens, heads, d, page, layout="hnd", spare=2, seed=0, fill=math.nan, layers=1, std=1.0):
+    """A cache whose rows hold lens tokens in shuffled pages; every place no token has holds `fill`."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    lens = torch.tensor(lens)
+    need = -(-lens // page)
+    n_pages, row_pages = int(need.sum()) + spare, max(1, int(need.max())) + 1
+    ids = torch.randperm(n_pages, generator=torch.Generator().manual_seed(seed)).int()
+    table = torch.full((len(lens), row_pages), -1, dtype=torch.int32)
+    at = 0
+    for i, k in enumerate(need.tolist()):
+        table[i, :k] = ids[at:at + k]
+        at += k
+    refs = torch.zeros(n_pages, dtype=torch.int32)
+    refs[ids[:at].long()] = 1
+    shape = (n_pages, heads, page, d) if layout == "hnd" else (n_pages, page, heads, d)
+    pools = []
+    for _ in range(2 * layers):
+        x = torch.randn(shape, generator=g, device="cuda") * std
+        x = x.to(DT[dtype])
+        x = x if layout == "hnd" else x.transpose(1, 2)
+        held = torch.zeros(n_pages, page, dtype=torch.bool)
+        for i, n in enumerate(lens.tolist()):
+            for j in range(0, n, page):
+                held[table[i, j // page], :min(page, n - j)] = True
+        x.masked_fill_(~held.cuda()[:, None, :, None], fill)
+        pools.append(x)
+    pages = jb.PageTable(table.cuda(), lens.int().cuda(), refs.cuda(), page)
+    return jb.KVCache(pages, pools[:layers], pools[layers:])
+
+
+def reference(cache, layer, q, rows, pos, scale=None, softcap=0.0, window=0, slopes=None):
+    """(result, tolerance) of every element in 64 bits."""
+    n, qh, d = q.shape
+    g = qh // cache.heads
+    scale = d ** -0.5 if scale is None else scale
+    page = cache.pages.page_tokens
+    out = torch.zeros(n, qh, d, dtype=torch.float64, device="cuda")
+    tol = torch.zeros_like(out)
+    table = cache.pages.table.cpu()
+    for i, (r, last) in enumerate(zip(rows.tolist(), pos.tolist())):
+        if not 0 <= r < table.shape[0] or not 0 <= last < table.shape[1] * page:
+            continue
+        t = torch.arange(max(0, last - window + 1) if window else 0, last + 1)
+        ids = table[r, t // page].long()
+        t, ids = t[ids >= 0], ids[ids >= 0]
+        if len(t) == 0:
+            continue
+        k = cache.keys[layer][ids.cuda(), :, (t % page).cuda()].double().repeat_interleave(g, 1)     # [T, qh, d]
+        v = cache.values[layer][ids.cuda(), :, (t % page).cuda()].double().repeat_interleave(g, 1)
+        prod = q[i].double()[None] * k * scale
+        x, size = prod.sum(-1), prod.abs().sum(-1).amax(0)
+        if softcap:
+            x = softcap * torch.tanh(x / softcap)
+            size = size + softcap
+        if slopes is not None:
+            x = x + slopes.double()[None] * (t.cuda() - last).double()[:, None]
+            size = size + slopes.double() * float(last - t[0])
+        p = torch.softmax(x, 0)
+        out[i] = torch.einsum("th,thd->hd", p, v)
+        a = torch.einsum("th,thd->hd", p, v.abs())
+        rel = 2 * (2 * (d + 16) * 2.0**-23 * size + 2.0**-21) + len(t) * 2.0**-23
+        if q.dtype == torch.bfloat16:
+            rel = rel + 2.0**-16
+        tol[i] = a * rel[:, None] + (2.0**-8 * out[i].abs() if q.dtype == torch.bfloat16 else 0) + 1e-38
+    return out, tol
+
+
+def check(cache, layer, q, rows, pos, **kw):
+    got = jb.jb_attend(cache, layer, q, rows, pos, **kw)
+    want, tol = reference(cache, layer, q, rows, pos, **{k: v for k, v in kw.items() if k not in ("out", "stream")})
+    torch.cuda.synchronize()
+    err = (got.double() - want).abs()
+    assert torch.isfinite(got).all()
+    worst = (err / tol.clamp(min=1e-300)).amax() if err.numel() else 0.0
+    assert (err <= tol).all(), f"worst error over tolerance {worst:.3g}"
+    return got
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def query(n, heads, d, dtype, seed=1, std=2.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(n, heads, d, generator=g, device="cuda") * std).to(DT[dtype])
+
+
+LENS = [1, 0, 15, 16, 17, 31, 33, 47, 48, 49, 63, 64, 65, 127, 128, 129, 255, 257, 700]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("page,layout", [(16, "hnd"), (48, "nhd"), (128, "hnd"), (64, "nhd")])
+def test_lengths_around_groups_and_pages(dtype, page, layout):
+    cache = make(dtype, LENS, 3, 64, page, layout)
+    check(cache, 0, query(len(LENS), 3, 64, dtype), i32(range(len(LENS))), cache.pages.lens - 1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [8, 16, 40, 64, 72, 80, 96, 120, 128, 136, 192, 256])
+@pytest.mark.parametrize("group", [1, 3])
+def test_head_sizes(dtype, d, group):
+    lens = [5, 130, 64]
+    cache = make(dtype, lens, 2, d, 32)
+    check(cache, 0, query(3, 2 * group, d, dtype), i32(range(3)), cache.pages.lens - 1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("heads,group", [(1, 1), (4, 2), (2, 4), (1, 5), (2, 7), (1, 8), (3, 9), (1, 16), (1, 27), (1, 64)])
+@pytest.mark.parametrize("layout", ["hnd", "nhd"])
+def test_shared_heads(dtype, heads, group, layout):
+    lens = [3, 200, 77]
+    cache = make(dtype, lens, heads, 128, 16, layout)
+    check(cache, 0, query(3, heads * group, 128, dtype), i32(range(3)), cache.pages.lens - 1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("window", [0, 1, 2, 15, 16, 17, 64, 100, 5000])
+@pytest.mark.parametrize("softcap,bias", [(0.0, False), (20.0, False), (0.0, True), (5.0, True)])
+def test_windows_caps_and_biases(dtype, window, softcap, bias):
+    lens = [1, 16, 65, 0, 333]
+    cache = make(dtype, lens, 2, 64, 16)
+    slopes = 2.0 ** -torch.arange(1, 7, device="cuda").float() if bias else None
+    check(cache, 0, query(5, 6, 64, dtype, std=4.0), i32(range(5)), cache.pages.lens - 1, window=window, softcap=softcap, slopes=slopes)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_prompt_tokens_are_queries_of_one_row(dtype):
+    cache = make(dtype, [150, 40], 2, 64, 16)
+    rows, pos = i32([0] * 150 + [1] * 40), i32(list(range(150)) + list(range(40)))
+    check(cache, 0, query(190, 4, 64, dtype), rows, pos)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_queries_that_see_nothing(dtype):
+    cache = make(dtype, [40, 20, 7], 2, 64, 16)
+    cap = cache.pages.struct.row_pages * 16
+    rows, pos = i32([0, -1, 3, 1, 2, 0, 1 << 30, 1]), i32([-1, 5, 5, cap, 6, -2147483648, 3, 2147483647])
+    q = query(8, 2, 64, dtype)
+    out = torch.full_like(q, math.nan)
+    got = check(cache, 0, q, rows, pos, out=out)
+    assert got is out and (got[[0, 1, 2, 3, 5, 6, 7]] == 0).all() and (got[4] != 0).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_missing_pages_are_not_seen(dtype):
+    """An entry of -1 inside a row, and positions past the row's pages (within its table's row)."""
+    cache = make(dtype, [160, 33], 2, 64, 16)
+    cache.pages.table[0, 3] = -1
+    cache.pages.table[0, 7:9] = -1
+    check(cache, 0, query(3, 2, 64, dtype), i32([0, 0, 0]), i32([159, 100, 170]), scale=0.3)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("heads,n", [(1, 1), (2, 3)])
+def test_long_rows_are_split_and_joined(dtype, heads, n):
+    lens = [50_001, 1, 16_384][:n]
+    cache = make(dtype, lens, heads, 128, 64, std=0.5)
+    check(cache, 0, query(n, heads * 2, 128, dtype), i32(range(n)), cache.pages.lens - 1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_rows(dtype):
+    g = torch.Generator().manual_seed(5)
+    lens = torch.randint(0, 90, (700,), generator=g).tolist()
+    cache = make(dtype, lens, 2, 64, 16)
+    check(cache, 0, query(700, 2, 64, dtype), i32(range(700)), cache.pages.lens - 1)
+
+
+def test_more_queries_than_one_launch_takes():
+    cache = make("bf16", [33], 1, 64, 16)
+    n = 16_384 + 77
+    q = query(3, 1, 64, "bf16")[torch.arange(n, device="cuda") % 3].contiguous()
+    pos = (torch.arange(n, device="cuda") % 33).int()
+    got = jb.jb_attend(cache, 0, q, torch.zeros(n, dtype=torch.int32, device="cuda"), pos)
+    want, tol = reference(cache, 0, q[:99], i32([0] * 99), pos[:99])
+    assert ((got[:99].double() - want).abs() <= tol).all()
+    again = torch.arange(n, device="cuda") % 99  # the same queries, cut at other places
+    assert ((got - got[:99][again]).double().abs() <= 2 * tol[again]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_scores_and_dominant_tokens(dtype):
+    """Maxima that rise along the row, by far more than the exponential's range."""
+    cache = make(dtype, [300], 1, 64, 16, std=1.0)
+    k = cache.keys[0]
+    table = cache.pages.table[0].cpu()
+    for t in (20, 150, 299):
+        k[int(table[t // 16]), 0, t % 16] *= 20.0 + t
+    check(cache, 0, query(1, 2, 64, dtype, std=6.0), i32([0]), i32([299]))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_strided_queries_and_outputs_and_interleaved_pages(dtype):
+    lens = [70, 9]
+    base = make(dtype, lens, 2, 64, 16)
+    both = torch.stack([base.keys[0], base.values[0]], 1)  # [pages, 2, heads, tokens, d]
+    cache = jb.KVCache(base.pages, [both[:, 0]], [both[:, 1]])
+    qkv = query(2, 8, 64, dtype)
+    q = qkv[:, 2:6]
+    out = torch.zeros(2, 9, 64, dtype=q.dtype, device="cuda")
+    check(cache, 0, q, i32([0, 1]), base.pages.lens - 1, out=out[:, 1:5])
+    assert (out[:, 0] == 0).all() and (out[:, 5:] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_results_repeat_and_streams_are_kept(dtype):
+    lens = [4000, 3, 900, 0, 2500]
+    cache = make(dtype, lens, 4, 128, 16)
+    q, rows, pos = query(5, 8, 128, dtype), i32(range(5)), cache.pages.lens - 1
+    first = jb.jb_attend(cache, 0, q, rows, pos)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        a = jb.jb_attend(cache, 0, q, rows, pos)
+    b = jb.jb_attend(cache, 0, q, rows, pos, stream=s)
+    c = jb.jb_attend(cache, 0, q, rows, pos, stream=s.cuda_stream)
+    s.synchronize()
+    for x in (a, b, c):
+        assert torch.equal(first, x)
+
+
+def test_in_a_graph_lengths_may_change():
+    cache = make("bf16", [500, 40], 2, 64, 16)
+    q, rows, pos = query(2, 4, 64, "bf16"), i32([0, 1]), i32([10, 10])
+    out = torch.empty_like(q)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        jb.jb_attend(cache, 0, q, rows, pos, out=out)
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        jb.jb_attend(cache, 0, q, rows, pos, out=out)
+    for p in ([499, 39], [0, -1], [250, 17]):
+        pos.copy_(i32(p))
+        graph.replay()
+        want, tol = reference(cache, 0, q, rows, pos)
+        torch.cuda.synchronize()
+        assert ((out.double() - want).abs() <= tol).all()
+
+
+def test_offsets_past_32_bits():
+    """Pages whose elements lie beyond 2^32 elements of their tensor."""
+    heads, d, page = 32, 128, 16
+    n_pages = (1 << 32) // (heads * d * page) + 40
+    k = torch.empty(n_pages, heads, page, d, dtype=torch.bfloat16, device="cuda")
+    v = torch.empty_like(k)
+    k[-30:].normal_()
+    v[-30:].normal_()
+    table = torch.full((2, 9), -1, dtype=torch.int32)
+    table[0, :8] = torch.arange(n_pages - 8, n_pages)
+    table[1, :3] = torch.tensor([n_pages - 20, n_pages - 11, n_pages - 30])
+    pages = jb.PageTable(table.cuda(), i32([128, 41]), torch.zeros(n_pages, dtype=torch.int32, device="cuda"), page)
+    cache = jb.KVCache(pages, [k], [v])
+    check(cache, 0, query(2, 32, 128, "bf16"), i32([0, 1]), i32([127, 40]))
+    new = query(2, 64, 128, "bf16", seed=9)
+    jb.jb_cache_write(cache, 0, new[:, :32], new[:, 32:], i32([0, 1]), i32([100, 47]))
+    assert torch.equal(k[n_pages - 8 + 6, :, 4], new[0, :32]) and torch.equal(v[n_pages - 30, :, 15], new[1, 32:])
