@@ -2,8 +2,13 @@
 //
 // Weights are integers (w = rint(2^30 exp(y))), so a sum of them is the same in every order and the
 // token is a function of the logits' bits, the settings and the word alone. What is kept is a prefix
-// of the order (logit descending, index ascending); its end is found by descending through the digits
-// of the logits' ordered keys with a histogram of counts and weights for each digit.
+// of the order (logit descending, index ascending). Its end is found without sorting: a histogram over
+// y of counts and weights gives the bin that holds the end, the bin's tokens are collected and ranked.
+// A bin with too many tokens is cut again, by key and at last by index, until they fit.
+//
+// A row is one cluster of CTAs that read it from L2 in each of their few passes (a batch of logits is
+// smaller than L2); histograms and sums are joined through distributed shared memory.
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
 #include "jb_answer.h"
@@ -11,9 +16,13 @@
 namespace jb {
 namespace {
 
+namespace cg = cooperative_groups;
+
 constexpr unsigned kAll = 0xFFFFFFFFu;
-constexpr int kThreads = 1024;
-constexpr int kWarps = kThreads / 32;
+constexpr int kBins = 2048;
+constexpr int kMaxCluster = 8;
+constexpr int kMaxSlice = 65536;       // tokens of one CTA: sums of halves of their weights fit 32 bits
+constexpr float kReach = 21.5f;        // weights round to 0 below y = -31 ln 2 = -21.49
 constexpr float kOne = 1073741824.0f;  // 2^30, the weight of the largest logit
 typedef unsigned long long u64;
 
@@ -33,21 +42,41 @@ struct Row {
     uint32_t top;   // key of the largest logit
     float high;     // the largest logit
     float inverse;  // 1 / temperature
-    u64 cut;        // least weight (min_p)
 
     __device__ float scaled(uint32_t key) const { return key == top ? 0.0f : (logit_of(key) - high) * inverse; }
-    __device__ u64 weight(uint32_t key) const {
-        if (key <= kNothing) return 0;
-        return static_cast<u64>(__float2ll_rn(expf(scaled(key)) * kOne));
+    __device__ uint32_t weight(uint32_t key) const {
+        return key <= kNothing ? 0 : __float2uint_rn(expf(scaled(key)) * kOne);
     }
 };
 
 template <typename T>
-__device__ __forceinline__ uint32_t load_key(const T* row, int j);
+__device__ __forceinline__ uint32_t load_key(const T* p);
 template <>
-__device__ __forceinline__ uint32_t load_key<float>(const float* row, int j) { return key_of(row[j]); }
+__device__ __forceinline__ uint32_t load_key<float>(const float* p) { return key_of(*p); }
 template <>
-__device__ __forceinline__ uint32_t load_key<__nv_bfloat16>(const __nv_bfloat16* row, int j) { return key_of(__bfloat162float(row[j])); }
+__device__ __forceinline__ uint32_t load_key<__nv_bfloat16>(const __nv_bfloat16* p) { return key_of(__bfloat162float(*p)); }
+
+// Eight tokens at a time. Past the end: key 0, which weighs nothing.
+constexpr int kUnit = 8;
+template <typename T>
+__device__ __forceinline__ void load_unit(const T* row, int j, int vocab, bool wide, uint32_t (&key)[kUnit]) {
+    if (wide && j + kUnit <= vocab) {
+        if constexpr (sizeof(T) == 2) {
+            const uint4 v = *reinterpret_cast<const uint4*>(row + j);
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i) key[i] = key_of(__uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16));
+        } else {
+            const float4 a = *reinterpret_cast<const float4*>(row + j), b = *reinterpret_cast<const float4*>(row + j + 4);
+            const float f[kUnit] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i) key[i] = key_of(f[i]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kUnit; ++i) key[i] = j + i < vocab ? load_key(row + j + i) : 0;
+    }
+}
 
 template <typename V>
 __device__ __forceinline__ V warp_inclusive(V v) {
@@ -60,181 +89,426 @@ __device__ __forceinline__ V warp_inclusive(V v) {
     return v;
 }
 
-// Exclusive prefix over the CTA's threads and the total.
-template <typename V>
+// Exclusive prefix over the CTA's threads and the total. sums: a word for each of kWarps warps.
+template <int kWarps, typename V>
 __device__ __forceinline__ V block_exclusive(V v, V* sums, V& total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const V in = warp_inclusive(v);
     if (lane == 31) sums[warp] = in;
     __syncthreads();
-    const V all = warp_inclusive(sums[lane]);
+    const V all = warp_inclusive(lane < kWarps ? sums[lane] : V(0));
     const V before = __shfl_sync(kAll, all, warp == 0 ? 0 : warp - 1);
     total = __shfl_sync(kAll, all, 31);
     __syncthreads();
     return in - v + (warp == 0 ? V(0) : before);
 }
 
-// The end of what is kept: keys above `key`, and of the tokens with that key the first `ties`.
-struct End {
-    uint32_t key;
-    int ties;
-    u64 mass;  // weight of what is kept
+// A token's place in the order as a number: larger comes first.
+__device__ __forceinline__ u64 place_of(uint32_t key, uint32_t index) { return static_cast<u64>(key) << 32 | ~index; }
+
+// The tokens that a histogram is taken of, places from `first` down to `last`, and its bins.
+enum Bins { kByScore, kByKey, kByIndex };
+struct Among {
+    u64 first, last;
+    Bins bins;
+    uint32_t key;  // the largest key (kByKey)
+    int shift;     // bits of key or index within a bin
 };
 
+// Where a histogram's running count or weight reaches its goal.
+struct Crossing {
+    int bin;     // -1: nowhere
+    int count;   // tokens in the bins before (of all bins, if nowhere)
+    u64 mass;    // their weight
+    u64 goal;
+};
+
+// What a prefix of the order has to reach: tokens, a weight, or a share of all weights.
+enum Kind { kTokens, kWeight, kShare };
+struct Goal {
+    Kind kind;
+    u64 value;
+    double share;
+};
+
+__device__ __forceinline__ u64 share_of(double share, u64 mass) {
+    return max(1ull, static_cast<u64>(ceil(fmax(share, 0.0) * static_cast<double>(mass))));
+}
+
+template <int kThreads>
 struct Shared {
-    int count[256];
-    u64 mass[256];
-    u64 sums[kWarps];
-    int counts[kWarps];
-    uint32_t key;
-    int above;
-    u64 mass_above;
-    int found;
+    uint32_t count[kBins], low[kBins], high[kBins];  // tokens, and their weights' halves
+    u64 list[kThreads], order[kThreads];             // tokens of the bin; in the first CTA, in order
+    u64 sums[32];
+    int counts[32];
+    u64 best;
+    int total_count, listed;
+    u64 total_mass;
+    uint32_t least, most;  // keys of the bin's tokens
+    Crossing crossing;
+    u64 cut, cut_mass;
 };
 
-// The end of the shortest prefix of the order, within `within`, that has `goal` tokens (by_mass
-// false) or weighs `goal` (by_mass true). Tokens of weight 0 are not counted: they are never drawn.
-template <typename T>
-__device__ End descend(const T* row, int vocab, const Row& r, const End& within, bool by_mass, u64 goal, Shared& sh) {
-    uint32_t prefix = 0;
-    int above = 0;
-    u64 mass_above = 0;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (threadIdx.x < 256) {
-            sh.count[threadIdx.x] = 0;
-            sh.mass[threadIdx.x] = 0;
+template <typename T, int kThreads>
+struct Draw {
+    static constexpr int kWarps = kThreads / 32;
+    const T* row;
+    int vocab, rank, ctas, from, to;  // units of this warp
+    bool wide;
+    Row r;
+    Shared<kThreads>& sh;
+    cg::cluster_group cluster;
+
+    __device__ __forceinline__ Shared<kThreads>& of(int cta) { return *cluster.map_shared_rank(&sh, cta); }
+
+    // f(key, index) for the warp's tokens, a thread's indices ascending.
+    template <typename F>
+    __device__ __forceinline__ void each(F f) {
+        for (int u = from + static_cast<int>(threadIdx.x & 31); u < to; u += 32) {
+            uint32_t key[kUnit];
+            load_unit(row, u * kUnit, vocab, wide, key);
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i) f(key[i], u * kUnit + i);
         }
-        __syncthreads();
-        for (int j = threadIdx.x; j < vocab; j += kThreads) {
-            const uint32_t key = load_key(row, j);
-            if (key < within.key || (shift < 24 && (key ^ prefix) >> (shift + 8) != 0)) continue;
-            const u64 w = r.weight(key);
-            if (w == 0) continue;
-            atomicAdd(&sh.count[key >> shift & 255], 1);
-            atomicAdd(&sh.mass[key >> shift & 255], w);
-        }
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            int digit = 255;
-            for (; digit > 0; --digit) {
-                const bool last = by_mass ? mass_above + sh.mass[digit] >= goal
-                                          : static_cast<u64>(above) + sh.count[digit] >= goal;
-                if (last) break;
-                above += sh.count[digit];
-                mass_above += sh.mass[digit];
-            }
-            sh.key = prefix | static_cast<uint32_t>(digit) << shift;
-            sh.above = above;
-            sh.mass_above = mass_above;
-        }
-        __syncthreads();
-        prefix = sh.key;
-        above = sh.above;
-        mass_above = sh.mass_above;
-        __syncthreads();
     }
-    End e;
-    e.key = prefix;
-    const u64 w = r.weight(prefix);
-    int most = prefix == within.key ? within.ties : 0x7FFFFFFF;  // tokens with this key
-    // sh.count holds the last digit's histogram: tokens with exactly this key
-    most = min(most, sh.count[prefix & 255]);
-    const u64 wanted = by_mass ? (w == 0 ? 0 : (goal - min(goal, mass_above) + w - 1) / w) : goal - min(goal, static_cast<u64>(above));
-    e.ties = static_cast<int>(min(static_cast<u64>(most), wanted));
-    e.mass = mass_above + w * e.ties;
-    __syncthreads();
-    return e;
+
+    // Bin of a token; -1 if it is not among them or weighs nothing.
+    __device__ __forceinline__ int bin_of(const Among& a, uint32_t key, int index) const {
+        if (key <= kNothing) return -1;
+        const u64 place = place_of(key, index);
+        if (place > a.first || place < a.last) return -1;
+        if (a.bins == kByScore) return min(kBins - 1, static_cast<int>(r.scaled(key) * (-kBins / kReach)));
+        return a.bins == kByKey ? static_cast<int>((a.key - key) >> a.shift) : index >> a.shift;
+    }
+
+    __device__ Crossing find(const Among& a, bool counts, bool masses, const Goal& g) {
+        for (int i = threadIdx.x; i < kBins; i += kThreads) sh.count[i] = sh.low[i] = sh.high[i] = 0;
+        __syncthreads();
+        each([&](uint32_t key, int index) {
+            const int b = bin_of(a, key, index);
+            if (b < 0) return;
+            const uint32_t w = r.weight(key);
+            if (w == 0) return;
+            if (counts) atomicAdd(&sh.count[b], 1u);
+            if (masses) {
+                atomicAdd(&sh.low[b], w & 0xFFFFu);
+                atomicAdd(&sh.high[b], w >> 16);
+            }
+        });
+        cluster.sync();
+        // each CTA joins a section of the bins, a thread a few in a row
+        constexpr int kMost = kBins / kThreads;
+        const int section = kBins / ctas, share = (section + kThreads - 1) / kThreads;
+        const int begin = static_cast<int>(threadIdx.x) * share;
+        const int first = rank * section + begin;
+        int count[kMost];
+        u64 mass[kMost];
+        int n = 0;
+        u64 m = 0;
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+            count[i] = 0;
+            mass[i] = 0;
+            if (i < share && begin + i < section) {
+                for (int c = 0; c < ctas; ++c) {
+                    if (counts) count[i] += of(c).count[first + i];
+                    if (masses) mass[i] += of(c).low[first + i] + (static_cast<u64>(of(c).high[first + i]) << 16);
+                }
+            }
+            n += count[i];
+            m += mass[i];
+        }
+        int total_count;
+        u64 total_mass;
+        int before = block_exclusive<kWarps>(n, sh.counts, total_count);
+        u64 mass_before = block_exclusive<kWarps>(m, sh.sums, total_mass);
+        if (threadIdx.x == 0) {
+            sh.total_count = total_count;
+            sh.total_mass = total_mass;
+        }
+        cluster.sync();
+        int all_count = 0;
+        u64 all_mass = 0;
+        for (int c = 0; c < ctas; ++c) {
+            if (c < rank) {
+                before += of(c).total_count;
+                mass_before += of(c).total_mass;
+            }
+            all_count += of(c).total_count;
+            all_mass += of(c).total_mass;
+        }
+        const bool tokens = g.kind == kTokens;
+        const u64 goal = g.kind == kShare ? share_of(g.share, all_mass) : g.value;
+        const auto tell = [&](const Crossing& x) {
+            for (int c = 0; c < ctas; ++c) of(c).crossing = x;
+        };
+        if ((tokens ? static_cast<u64>(all_count) : all_mass) < goal) {
+            if (rank == 0 && threadIdx.x == 0) tell({-1, all_count, all_mass, goal});
+        } else {
+#pragma unroll
+            for (int i = 0; i < kMost; ++i) {
+                const u64 x = tokens ? static_cast<u64>(before) : mass_before;
+                const u64 y = x + (tokens ? static_cast<u64>(count[i]) : mass[i]);
+                if (x < goal && y >= goal) tell({first + i, before, mass_before, goal});
+                before += count[i];
+                mass_before += mass[i];
+            }
+        }
+        cluster.sync();
+        return sh.crossing;
+    }
+
+    // The bin's tokens: their number, or more than kThreads if they do not fit the first CTA's list.
+    __device__ int collect(const Among& a, int bin) {
+        if (threadIdx.x == 0) {
+            sh.listed = 0;
+            sh.least = 0xFFFFFFFFu;
+            sh.most = 0;
+        }
+        __syncthreads();
+        uint32_t least = 0xFFFFFFFFu, most = 0;
+        each([&](uint32_t key, int index) {
+            if (bin_of(a, key, index) != bin || r.weight(key) == 0) return;
+            least = min(least, key);
+            most = max(most, key);
+            if (*static_cast<volatile int*>(&sh.listed) > kThreads) return;  // too many in any case
+            const int at = atomicAdd(&sh.listed, 1);
+            if (at < kThreads) sh.list[at] = place_of(key, index);
+        });
+        least = __reduce_min_sync(kAll, least);
+        most = __reduce_max_sync(kAll, most);
+        if ((threadIdx.x & 31) == 0) {
+            atomicMin(&sh.least, least);
+            atomicMax(&sh.most, most);
+        }
+        cluster.sync();
+        int n = 0;
+        for (int c = 0; c < ctas; ++c) n += min(of(c).listed, kThreads + 1);
+        return n;
+    }
+
+    // Ranks the n listed tokens and tells every CTA the place of the one that reaches the goal, `count`
+    // tokens of weight `mass` being before them.
+    __device__ void choose(int n, bool tokens, u64 goal, u64 count, u64 mass) {
+        if (rank == 0) {
+            const int i = threadIdx.x;
+            u64 place = 0;
+            if (i < n) {
+                int at = i, c = 0;
+                while (at >= of(c).listed) at -= of(c++).listed;
+                place = of(c).list[at];
+                sh.order[i] = place;
+            }
+            __syncthreads();
+            int before = 0;
+            for (int j = 0; j < n; ++j) before += sh.order[j] > place ? 1 : 0;
+            __syncthreads();
+            if (i < n) sh.order[before] = place;
+            __syncthreads();
+            place = i < n ? sh.order[i] : 0;
+            const u64 w = i < n ? r.weight(static_cast<uint32_t>(place >> 32)) : 0;
+            u64 all;
+            const u64 x = block_exclusive<kWarps>(w, sh.sums, all);
+            const bool here = tokens ? count + i + 1 == goal : mass + x < goal && mass + x + w >= goal;
+            if (i < n && here) {
+                for (int c = 0; c < ctas; ++c) {
+                    of(c).cut = place;
+                    of(c).cut_mass = mass + x + w;
+                }
+            }
+        }
+        cluster.sync();
+    }
+
+    // The last place of the shortest prefix of the order that reaches the goal, among the places from
+    // `last` on, and the prefix's weight. Place 0 if all together do not reach it.
+    __device__ void end_of(u64 last, bool masses, Goal g, u64& place, u64& weight) {
+        Among a = {~0ull, last, kByScore, 0, 0};
+        const bool tokens = g.kind == kTokens;
+        u64 count = 0, mass = 0;  // of what is before `a`
+        // by score; by key at most three times (32 bits, 11 at a time); by index, 128 to a bin: those fit
+        for (int round = 0; round < 5; ++round) {
+            const Crossing x = find(a, tokens, masses, g);
+            if (g.kind == kShare) g = {kWeight, x.goal, 0.0};
+            count += x.count;
+            mass += x.mass;
+            if (x.bin < 0) break;
+            const int n = collect(a, x.bin);
+            if (n <= kThreads) {
+                choose(n, tokens, tokens ? count - x.count + g.value : mass - x.mass + g.value, count, mass);
+                place = sh.cut;
+                weight = sh.cut_mass;
+                return;
+            }
+            uint32_t least = 0xFFFFFFFFu, most = 0;
+            for (int c = 0; c < ctas; ++c) {
+                least = min(least, of(c).least);
+                most = max(most, of(c).most);
+            }
+            cluster.sync();  // read by all before it is set anew
+            g.value -= tokens ? static_cast<u64>(x.count) : x.mass;
+            a.first = min(a.first, place_of(most, 0));
+            a.last = max(a.last, place_of(least, 0xFFFFFFFFu));
+            a.key = most;
+            a.bins = least == most ? kByIndex : kByKey;
+            a.shift = least == most ? 7 : max(0, 21 - __clz(most - least));
+        }
+        place = 0;
+        weight = mass;
+    }
+
+    __device__ void run(const Sample& p, int i) {
+        // the largest logit, the first of equal ones
+        uint32_t top = 0;
+        int first = 0;
+        each([&](uint32_t key, int index) {
+            if (key > top) {
+                top = key;
+                first = index;
+            }
+        });
+        u64 best = place_of(top, first);
+#pragma unroll
+        for (int d = 16; d > 0; d /= 2) best = max(best, __shfl_xor_sync(kAll, best, d));
+        if ((threadIdx.x & 31) == 0) sh.sums[threadIdx.x >> 5] = best;
+        __syncthreads();
+        for (int w = 0; w < kWarps; ++w) best = max(best, sh.sums[w]);
+        if (threadIdx.x == 0) sh.best = best;
+        cluster.sync();
+        for (int c = 0; c < ctas; ++c) best = max(best, of(c).best);
+
+        r.top = static_cast<uint32_t>(best >> 32);
+        r.high = logit_of(r.top);
+        const float temperature = p.temperature == nullptr ? 1.0f : p.temperature[i];
+        const int top_k = p.top_k == nullptr ? 0 : p.top_k[i];
+        const bool greedy = !(temperature >= 0x1p-64f) || top_k == 1;
+        if (greedy || r.top <= kNothing) {
+            if (rank == 0 && threadIdx.x == 0) {
+                const bool none = r.top <= kNothing;
+                p.tokens[i] = none ? -1 : static_cast<int>(~static_cast<uint32_t>(best));
+                if (p.logprobs != nullptr) p.logprobs[i] = none ? -INFINITY : 0.0f;
+            }
+            cluster.sync();  // until every CTA has read the others' memory
+            return;
+        }
+        r.inverse = __frcp_rn(temperature);
+        const float min_p = p.min_p == nullptr ? 0.0f : p.min_p[i];
+        const double top_p = p.top_p == nullptr ? 1.0 : static_cast<double>(p.top_p[i]);
+        const uint32_t least = min_p > 0.0f ? static_cast<uint32_t>(ceil(fmin(static_cast<double>(min_p), 1.0) * 1073741824.0)) : 0;
+        u64 last = 0, mass = 0;
+        const bool counted = top_k > 0 && top_k < vocab, nucleus = top_p < 1.0;
+        if (counted) end_of(0, nucleus, {kTokens, static_cast<u64>(top_k), 0.0}, last, mass);
+        if (nucleus)
+            end_of(last, true, counted ? Goal{kWeight, share_of(top_p, mass), 0.0} : Goal{kShare, 0, top_p}, last, mass);
+
+        const auto kept = [&](uint32_t key, int index) -> uint32_t {
+            if (key <= kNothing || place_of(key, index) < last) return 0;
+            const uint32_t w = r.weight(key);
+            return w >= least ? w : 0;
+        };
+        const int lane = threadIdx.x & 31;
+        u64 sum = 0;
+        each([&](uint32_t key, int index) { sum += kept(key, index); });
+#pragma unroll
+        for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(kAll, sum, d);
+        u64 here;
+        // one thread a warp counts: its prefix is the warp's
+        u64 before = block_exclusive<kWarps>(lane == 0 ? sum : 0, sh.sums, here);
+        before = __shfl_sync(kAll, before, 0);
+        if (threadIdx.x == 0) sh.total_mass = here;
+        cluster.sync();
+        u64 all = 0;
+        for (int c = 0; c < ctas; ++c) {
+            const u64 v = of(c).total_mass;
+            if (c < rank) before += v;
+            all += v;
+        }
+        const u64 aim = __umul64hi(static_cast<u64>(p.words[i]) << 32, all);
+        if (aim >= before && aim < before + sum) {  // the warp that has the token
+            u64 run = before;
+            for (int u = from; u < to; u += 32) {
+                uint32_t key[kUnit];
+                u64 mine = 0;
+                if (u + lane < to) {
+                    load_unit(row, (u + lane) * kUnit, vocab, wide, key);
+#pragma unroll
+                    for (int k = 0; k < kUnit; ++k) mine += kept(key[k], (u + lane) * kUnit + k);
+                }
+                const u64 in = run + warp_inclusive(mine);
+                if (aim >= in - mine && aim < in) {
+                    u64 x = in - mine;
+#pragma unroll
+                    for (int k = 0; k < kUnit; ++k) {
+                        const u64 w = kept(key[k], (u + lane) * kUnit + k);
+                        if (aim >= x && aim < x + w) {
+                            p.tokens[i] = (u + lane) * kUnit + k;
+                            if (p.logprobs != nullptr)
+                                p.logprobs[i] = r.scaled(key[k]) - logf(static_cast<float>(all) * (1.0f / kOne));
+                        }
+                        x += w;
+                    }
+                }
+                run = __shfl_sync(kAll, in, 31);
+                if (run > aim) break;
+            }
+        }
+        cluster.sync();  // until every CTA has read the others' memory
+    }
+};
+
+__host__ __device__ constexpr int units_per_warp(int vocab, int warps) {
+    return ((vocab + kUnit - 1) / kUnit + warps - 1) / warps;
+}
+
+template <typename T, int kThreads>
+__global__ void __launch_bounds__(kThreads) sample_kernel(Sample p) {
+    __shared__ Shared<kThreads> sh;
+    const cg::cluster_group cluster = cg::this_cluster();
+    const int ctas = cluster.num_blocks(), rank = cluster.block_rank(), i = blockIdx.x / ctas;
+    const T* row = reinterpret_cast<const T*>(p.logits) + static_cast<uint64_t>(i) * p.row_stride;
+    // a warp's tokens are consecutive, and so are the warps': indices ascend with (CTA, warp)
+    constexpr int kWarps = kThreads / 32;
+    const int units = (p.vocab + kUnit - 1) / kUnit, per = units_per_warp(p.vocab, ctas * kWarps);
+    const int from = min((rank * kWarps + static_cast<int>(threadIdx.x >> 5)) * per, units);
+    const bool wide = reinterpret_cast<uint64_t>(row) % 16 == 0;
+    Draw<T, kThreads> draw = {row, p.vocab, rank, ctas, from, min(from + per, units), wide, {}, sh, cluster};
+    draw.run(p, i);
+}
+
+template <typename T, int kThreads>
+cudaError_t launch(const Sample& p, int ctas, cudaStream_t s) {
+    cudaLaunchAttribute cluster;
+    cluster.id = cudaLaunchAttributeClusterDimension;
+    cluster.val.clusterDim.x = ctas;
+    cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+    cudaLaunchConfig_t c = {};
+    c.gridDim = dim3(static_cast<unsigned>(p.n) * ctas);
+    c.blockDim = dim3(kThreads);
+    c.stream = s;
+    c.attrs = &cluster;
+    c.numAttrs = 1;
+    return cudaLaunchKernelEx(&c, sample_kernel<T, kThreads>, p);
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) sample_kernel(Sample p) {
-    __shared__ Shared sh;
-    const int i = blockIdx.x;
-    const T* row = reinterpret_cast<const T*>(p.logits) + static_cast<uint64_t>(i) * p.row_stride;
-
-    uint32_t top = 0;
-    for (int j = threadIdx.x; j < p.vocab; j += kThreads) top = max(top, load_key(row, j));
-    top = __reduce_max_sync(kAll, top);
-    if ((threadIdx.x & 31) == 0) sh.counts[threadIdx.x >> 5] = static_cast<int>(top);
-    __syncthreads();
-    top = __reduce_max_sync(kAll, static_cast<uint32_t>(sh.counts[threadIdx.x & 31]));
-    __syncthreads();
-    if (top <= kNothing) {
-        if (threadIdx.x == 0) {
-            p.tokens[i] = -1;
-            if (p.logprobs != nullptr) p.logprobs[i] = -INFINITY;
-        }
-        return;
-    }
-    const float temperature = p.temperature == nullptr ? 1.0f : p.temperature[i];
-    const bool greedy = !(temperature >= 0x1p-64f);
-    Row r;
-    r.top = top;
-    r.high = logit_of(top);
-    r.inverse = greedy ? 1.0f : __frcp_rn(temperature);
-    const float min_p = p.min_p == nullptr ? 0.0f : p.min_p[i];
-    r.cut = min_p > 0.0f ? static_cast<u64>(ceil(fmin(static_cast<double>(min_p), 1.0) * 1073741824.0)) : 0;
-    const int top_k = greedy ? 1 : p.top_k == nullptr ? 0 : p.top_k[i];
-    const double top_p = p.top_p == nullptr ? 1.0 : static_cast<double>(p.top_p[i]);
-
-    // everything that has a weight
-    End end = {kNothing + 1, 0x7FFFFFFF, 0};
-    if (top_k > 0 && top_k < p.vocab) {
-        end = descend(row, p.vocab, r, end, false, static_cast<u64>(top_k), sh);
-    } else {
-        u64 sum = 0;
-        for (int j = threadIdx.x; j < p.vocab; j += kThreads) sum += r.weight(load_key(row, j));
-        block_exclusive(sum, sh.sums, end.mass);
-    }
-    if (top_p < 1.0) {
-        const u64 goal = max(1ull, static_cast<u64>(ceil(fmax(top_p, 0.0) * static_cast<double>(end.mass))));
-        end = descend(row, p.vocab, r, end, true, goal, sh);
-    }
-    // weights of what is kept, in the order of the indices
-    const auto kept = [&](uint32_t key, int tie) -> u64 {
-        if (key < end.key || (key == end.key && tie >= end.ties)) return 0;
-        const u64 w = r.weight(key);
-        return w >= r.cut ? w : 0;
+cudaError_t launch_t(const Sample& p, cudaStream_t s) {
+    // few tokens: CTAs of 256 threads, more of which fit an SM
+    const bool small = p.vocab <= 8192;
+    const int threads = small ? 256 : 1024, tokens = threads * kUnit, room = 152 * (small ? 6 : 2);
+    int ctas = 1;
+    // as many CTAs as run at once and have a unit for every thread; more where a slice would be too long
+    const auto more = [&](int c) {
+        return units_per_warp(p.vocab, c * threads / 32) * (threads / 32) * kUnit > kMaxSlice ||
+               (2ll * c * p.n <= room && p.vocab > c * tokens);
     };
-    u64 all = 0;
-    int ties = 0;
-    for (int first = 0; first < p.vocab; first += kThreads) {
-        const int j = first + threadIdx.x;
-        const uint32_t key = j < p.vocab ? load_key(row, j) : 0;
-        int here;
-        const int tie = ties + block_exclusive(key == end.key ? 1 : 0, sh.counts, here);
-        u64 sum;
-        block_exclusive(kept(key, tie), sh.sums, sum);
-        all += sum;
-        ties += here;
-    }
-    const u64 aim = __umul64hi(static_cast<u64>(p.words[i]) << 32, all);
-    u64 run = 0;
-    ties = 0;
-    for (int first = 0; first < p.vocab; first += kThreads) {
-        const int j = first + threadIdx.x;
-        const uint32_t key = j < p.vocab ? load_key(row, j) : 0;
-        int here;
-        const int tie = ties + block_exclusive(key == end.key ? 1 : 0, sh.counts, here);
-        u64 sum;
-        const u64 w = kept(key, tie);
-        const u64 before = run + block_exclusive(w, sh.sums, sum);
-        if (w > 0 && before <= aim && aim < before + w) {
-            p.tokens[i] = j;
-            if (p.logprobs != nullptr) p.logprobs[i] = r.scaled(key) - logf(static_cast<float>(all) * (1.0f / kOne));
-        }
-        run += sum;
-        ties += here;
-        if (run > aim) break;
-    }
+    while (ctas < kMaxCluster && more(ctas)) ctas *= 2;
+    return small ? launch<T, 256>(p, ctas, s) : launch<T, 1024>(p, ctas, s);
 }
 
 }  // namespace
 
 cudaError_t launch_sample(const Sample& p, cudaStream_t s) {
-    if (p.bf16) sample_kernel<__nv_bfloat16><<<p.n, kThreads, 0, s>>>(p);
-    else sample_kernel<float><<<p.n, kThreads, 0, s>>>(p);
-    return cudaGetLastError();
+    return p.bf16 ? launch_t<__nv_bfloat16>(p, s) : launch_t<float>(p, s);
 }
 
 }  // namespace jb
