@@ -8,6 +8,8 @@
 //
 // Softmax is kept with a running maximum, so that one pass is enough:
 //   m' = max(m, max_t x_t), s' = s e^(m - m') + sum e^(x_t - m'), o' likewise.
+#include <atomic>
+
 #include <cuda_bf16.h>
 
 #include "jb_answer.h"
@@ -84,6 +86,13 @@ struct Stretch {
     Span span;
 };
 
+// a / b; 64-bit division only where it is needed.
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+    return ((a | b) >> 32) == 0 ? static_cast<long long>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)) : a / b;
+}
+
+static_assert(kMaxListed <= kThreads * kThreads, "a thread's run of queries is searched by one thread each");
+
 // Deals the line of tiles out. All threads of a CTA go through it together.
 struct Dealer {
     long long next, end, total;
@@ -93,51 +102,47 @@ struct Dealer {
     Span span;
 
     __device__ static long long bound(long long total, int ctas, int cta) {
-        return total / ctas * cta + total % ctas * cta / ctas;
+        const long long each = quotient(total, ctas);
+        return each * cta + quotient((total - each * ctas) * cta, ctas);
     }
 
-    // sums: kThreads + 1 words of shared memory.
-    __device__ void start(const Params& p, long long* sums) {
+    // sums: kThreads + 1 words of shared memory, found: two.
+    __device__ void start(const Params& p, long long* sums, long long* found) {
         const int n = p.a.n, pairs = p.a.heads * p.blocks;
         const int per = (n + kThreads - 1) / kThreads;
-        // tiles of each thread's run of queries, then of the queries of the run that matters
+        // tiles of each thread's run of queries
+        const int mine_from = static_cast<int>(threadIdx.x) * per, mine_to = min(n, mine_from + per);
         long long mine = 0;
-        for (int i = threadIdx.x * per; i < min(n, (static_cast<int>(threadIdx.x) + 1) * per); ++i) mine += span_of(p, i).tiles();
+        for (int i = mine_from; i < mine_to; ++i) mine += span_of(p, i).tiles();
         scan(mine, sums);
         total = sums[kThreads] * pairs;
-        // a stretch below four tiles is not worth its join
-        const long long most = max(1ll, total / 4);
-        ctas = static_cast<int>(min(static_cast<long long>(gridDim.x), most));
+        ctas = static_cast<int>(min(static_cast<long long>(gridDim.x), max(1ll, total)));
         if (static_cast<int>(blockIdx.x) >= ctas || total == 0) {
             next = end = 0;
             return;
         }
         next = bound(total, ctas, blockIdx.x);
         end = bound(total, ctas, blockIdx.x + 1);
-        const long long goal = next / pairs;  // tiles of whole queries are multiples of `pairs`
-        int run = 0;
-        while (sums[run + 1] <= goal) ++run;
-        const long long before = sums[run];
+        // the run with the tile `next`, then the query: tiles before a query are multiples of `pairs`
+        const long long goal = quotient(next, pairs);
+        if (sums[threadIdx.x] <= goal && goal < sums[threadIdx.x + 1]) {
+            found[0] = mine_from;
+            found[1] = sums[threadIdx.x];
+        }
         __syncthreads();
-        long long base = before;
-        int found = run * per;
-        for (int first = run * per; first < min(n, (run + 1) * per); first += kThreads) {
-            const int i = first + threadIdx.x;
-            scan(i < min(n, (run + 1) * per) ? span_of(p, i).tiles() : 0, sums);
-            if (base + sums[kThreads] > goal) {
-                int k = 0;
-                while (base + sums[k + 1] <= goal) ++k;
-                found = first + k;
-                base += sums[k];
-                __syncthreads();
-                break;
+        if (per > 1) {  // at most kThreads queries (of kMaxListed) are a run
+            const long long base = found[1];
+            const int i = static_cast<int>(found[0]) + threadIdx.x;
+            scan(static_cast<int>(threadIdx.x) < per && i < n ? span_of(p, i).tiles() : 0, sums);
+            if (base + sums[threadIdx.x] <= goal && goal < base + sums[threadIdx.x + 1]) {
+                found[0] = i;
+                found[1] = base + sums[threadIdx.x];
             }
-            base += sums[kThreads];
             __syncthreads();
         }
-        query = found;
+        query = static_cast<int>(found[0]);
         span = span_of(p, query);
-        at = next - base * pairs;
+        at = next - found[1] * pairs;
     }
 
     // sums[i] = sum of v over threads before i, sums[kThreads] = of all.
@@ -169,10 +174,10 @@ struct Dealer {
         s.query = query;
         s.span = span;
         s.tiles = span.tiles();
-        const int pair = static_cast<int>(at / s.tiles);
+        const int pair = static_cast<int>(quotient(at, s.tiles));
         s.head = pair / p.blocks;
         s.block = pair % p.blocks;
-        s.from = static_cast<int>(at % s.tiles);
+        s.from = static_cast<int>(at - static_cast<long long>(pair) * s.tiles);
         s.to = static_cast<int>(min(static_cast<long long>(s.tiles), s.from + (end - next)));
         next += s.to - s.from;
         at += s.to - s.from;
@@ -187,16 +192,16 @@ __device__ __forceinline__ void store_out<float>(float* to, float v) { *to = v; 
 template <>
 __device__ __forceinline__ void store_out<__nv_bfloat16>(__nv_bfloat16* to, float v) { *to = __float2bfloat16_rn(v); }
 
-// Joins the warps' results in shared memory. part: [kWarps][kHeads][D]; top, sum: [kWarps][kHeads].
-// Then either the result itself or a slot of the workspace.
-template <typename T, int D>
-__device__ __forceinline__ void finish(const Params& p, const Stretch& s, int heads_here, const float* part, const float* top,
-                                       const float* sum, float* ws) {
+// Adds up the warps' results, kPart elements of each head from `first` on, and stores the result itself
+// or its part of a slot of the workspace. part: [kWarps][kHeads][kPart]; top, sum: [kWarps][kHeads].
+template <typename T, int D, int kPart>
+__device__ __forceinline__ void finish(const Params& p, const Stretch& s, int heads_here, int first, const float* part,
+                                       const float* top, const float* sum) {
     const int d = p.a.head_dim;
     const bool whole = s.from == 0 && s.to == s.tiles;
-    float* slot = ws + static_cast<size_t>(slot_floats(D)) * (2 * blockIdx.x + (s.from == 0 ? 1 : 0));
-    for (int u = threadIdx.x; u < heads_here * D; u += kThreads) {
-        const int h = u / D, e = u % D;
+    float* slot = p.a.ws + static_cast<size_t>(slot_floats(D)) * (2 * blockIdx.x + (s.from == 0 ? 1 : 0));
+    for (int u = threadIdx.x; u < heads_here * kPart; u += kThreads) {
+        const int h = u / kPart, e = first + u % kPart;
         float m = kLowest;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) m = fmaxf(m, top[w * kHeads + h]);
@@ -204,7 +209,7 @@ __device__ __forceinline__ void finish(const Params& p, const Stretch& s, int he
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
             const float c = exp2_approx(top[w * kHeads + h] - m);
-            o = fmaf(c, part[(w * kHeads + h) * D + e], o);
+            o = fmaf(c, part[w * kHeads * kPart + u], o);
             l = fmaf(c, sum[w * kHeads + h], l);
         }
         if (whole) {
@@ -277,31 +282,117 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 
 __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
-// bf16. A warp holds the scores of 8 query heads x 16 tokens. With r = lane / 4 and c = lane % 4 the
-// fragments of mma.m16n8k16 need no shared memory:
-//   Q K^T: lane (r, c) loads 16 bytes of key token r, elements 32 s + 8 c .. + 7; the order of the
-//     products' inner index is free as long as the queries use the same.
+// 16 bytes from global to shared memory, asynchronously; zeros if not `real`.
+__device__ __forceinline__ void copy_async(uint32_t to, const void* from, bool real) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(real ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void wait_copies() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
+}
+__device__ __forceinline__ uint4 load_shared(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+
+// bf16. A warp holds the scores of 8 query heads x 16 tokens. With r = lane / 4 and c = lane % 4 every
+// lane's part of the fragments of mma.m16n8k16 is 16 bytes at a time from one row of the page:
+//   Q K^T: lane (r, c) takes key token r, elements 32 s + 8 c .. + 7; the order of the products' inner
+//     index is free as long as the queries use the same.
 //   P V: the scores' fragment is the next product's first operand (tokens 2c, 2c + 1 of each eight);
-//     lane (r, c) loads elements 8 r .. 8 r + 7 of those four tokens' values, and byte permutes pair
+//     lane (r, c) takes elements 8 r .. 8 r + 7 of those four tokens' values, and byte permutes pair
 //     them up. The output's columns come out in the order of r and are written back accordingly.
+// So each lane copies what it will use itself, kStages groups ahead, into places of its own in shared
+// memory: no bank conflicts, and nothing to wait for but its own copies.
 // The 16-row operand has 8 query heads; for P its other 8 rows hold what rounding P to bf16 drops, so
 // that the weights enter with 16 bits at no cost.
+template <int D>
+struct Bf16Shape {
+    static constexpr int kS = D / 32, kV = D / 64, kPieces = 2 * kS + 4 * kV;
+    static constexpr int kStages = D == 64 ? 4 : 3;
+    static constexpr int kPart = D / 2;  // elements of the output that the warps add up at a time
+    static constexpr int kCtas = D == 64 ? 3 : D == 128 ? 2 : 1;  // on an SM
+    static constexpr int kRing = kWarps * kStages * kPieces * 512;
+    static constexpr int kShared = kRing + kWarps * kHeads * kPart * 4;
+};
+
 template <int D, bool kExtra>
-__global__ void __launch_bounds__(kThreads) attend_bf16_kernel(const __grid_constant__ Params p) {
-    constexpr int kS = D / 32, kV = D / 64;
-    __shared__ long long sums[kThreads + 1];
-    __shared__ float part[kWarps * kHeads * D];
+__global__ void __launch_bounds__(kThreads, Bf16Shape<D>::kCtas) attend_bf16_kernel(const __grid_constant__ Params p) {
+    using Shape = Bf16Shape<D>;
+    using T = __nv_bfloat16;
+    constexpr int kS = Shape::kS, kV = Shape::kV, kStages = Shape::kStages, kPart = Shape::kPart;
+    constexpr uint32_t kStageBytes = Shape::kPieces * 512;
+    extern __shared__ __align__(16) char dynamic[];
+    float* part = reinterpret_cast<float*>(dynamic + Shape::kRing);
+    __shared__ long long sums[kThreads + 1], found[2];
     __shared__ float top[kWarps * kHeads], sum[kWarps * kHeads];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
     const int d = p.a.head_dim;
-    using T = __nv_bfloat16;
+    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(dynamic)) + warp * kStages * kStageBytes + lane * 16;
+
+    // Copies of a stretch's groups: what is next to be asked for, and which of the stages hold a group
+    // whose page is missing.
+    struct Feed {
+        const int* table;
+        const T *k, *v;      // of the key head, at this lane's first element
+        int group, stop, page, lo, pos;
+        uint32_t missing;
+    } feed = {};
+    const auto ahead = [&] { feed.page = feed.group < feed.stop ? feed.table[feed.group / p.page_groups] : -1; };
+    const auto open = [&](const Stretch& s) {
+        feed.table = p.pages.table + static_cast<size_t>(s.span.row) * p.pages.row_pages;
+        feed.k = reinterpret_cast<const T*>(p.a.k) + s.head * p.a.head_stride + r * p.a.token_stride + 8 * c;
+        feed.v = reinterpret_cast<const T*>(p.a.v) + s.head * p.a.head_stride + 2 * c * p.a.token_stride + 8 * r;
+        feed.group = s.span.first + s.from * kTile + warp;
+        feed.stop = min(s.span.last + 1, s.span.first + s.to * kTile);
+        feed.lo = s.span.lo;
+        feed.pos = s.span.pos;
+        feed.missing = 0;
+        ahead();
+    };
+    const auto ask = [&](int stage) {
+        if (feed.group < feed.stop) {
+            const bool real = feed.page >= 0 && feed.page < p.pages.n_pages;
+            feed.missing = (feed.missing & ~(1u << stage)) | (real ? 0u : 1u << stage);
+            if (real) {
+                const uint64_t at = feed.page * p.a.page_stride + feed.group % p.page_groups * kGroup * p.a.token_stride;
+                const uint32_t to = ring + stage * kStageBytes;
+                const T* kp = feed.k + at;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < kS; ++i)
+                        copy_async(to + (t * kS + i) * 512, kp + t * 8 * p.a.token_stride + 32 * i, 32 * i + 8 * c < d);
+                const T* vp = feed.v + at;
+                const int token = feed.group * kGroup + 2 * c;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const int off = (t & 1) + (t >> 1) * 8;
+                    // a value that is not seen must not reach the sum, whatever it holds
+                    const bool seen = token + off >= feed.lo && token + off <= feed.pos;
+#pragma unroll
+                    for (int i = 0; i < kV; ++i)
+                        copy_async(to + (2 * kS + t * kV + i) * 512, vp + off * p.a.token_stride + 64 * i, seen && 64 * i + 8 * r < d);
+                }
+            }
+            feed.group += kTile;
+            ahead();
+        }
+        commit_copies();
+    };
 
     Dealer deal;
-    deal.start(p, sums);
-    Stretch s;
-    bool any = false;
-    while (deal.take(p, s)) {
-        any = true;
+    deal.start(p, sums, found);
+    Stretch s, after;
+    bool any = deal.take(p, s), more = any;
+    if (more) {
+        open(s);
+#pragma unroll
+        for (int i = 0; i < kStages; ++i) ask(i);
+    }
+    while (more) {
         const int heads_here = min(kHeads, p.a.group - s.block * kHeads);
         const int head0 = s.head * p.a.group + s.block * kHeads;
         uint4 q[kS];
@@ -315,75 +406,73 @@ __global__ void __launch_bounds__(kThreads) attend_bf16_kernel(const __grid_cons
 #pragma unroll
         for (int j = 0; j < 8 * kV; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
         float m = kLowest, l = 0.0f;
-        const int* table = p.pages.table + static_cast<size_t>(s.span.row) * p.pages.row_pages;
-        const int stop = min(s.span.last + 1, s.span.first + s.to * kTile);
+        const int stop = feed.stop;
+        int stage = 0;
         for (int g = s.span.first + s.from * kTile + warp; g < stop; g += kTile) {
-            const int page = table[g / p.page_groups];
-            if (page < 0 || page >= p.pages.n_pages) continue;
-            const uint64_t at = page * p.a.page_stride + s.head * p.a.head_stride + g % p.page_groups * kGroup * p.a.token_stride;
-            const T* kp = reinterpret_cast<const T*>(p.a.k) + at;
-            const T* vp = reinterpret_cast<const T*>(p.a.v) + at;
-            uint4 kf[2][kS], vf[4][kV];
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
+            wait_copies<kStages - 1>();
+            const uint32_t at = ring + stage * kStageBytes;
+            if (!(feed.missing >> stage & 1u)) {
+                float x[2][4] = {};
 #pragma unroll
                 for (int i = 0; i < kS; ++i)
-                    kf[t][i] = 32 * i + 8 * c < d ? load_stream(kp + (8 * t + r) * p.a.token_stride + 32 * i + 8 * c) : make_uint4(0, 0, 0, 0);
-            const int t0 = g * kGroup + 2 * c;  // this lane's tokens: t0, t0 + 1, t0 + 8, t0 + 9
-            const bool edge = g * kGroup < s.span.lo || g * kGroup + kGroup - 1 > s.span.pos;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const int off = 2 * c + (t & 1) + (t >> 1) * 8, token = g * kGroup + off;
-                // a value that is not seen must not reach the sum, whatever it holds
-                const bool seen = !edge || (token >= s.span.lo && token <= s.span.pos);
+                    for (int t = 0; t < 2; ++t) {
+                        const uint4 k = load_shared(at + (t * kS + i) * 512);
+                        mma(x[t], q[i].x, 0, q[i].y, 0, k.x, k.y);
+                        mma(x[t], q[i].z, 0, q[i].w, 0, k.z, k.w);
+                    }
+                const int t0 = g * kGroup + 2 * c;  // this lane's tokens: t0, t0 + 1, t0 + 8, t0 + 9
+                const bool edge = g * kGroup < s.span.lo || g * kGroup + kGroup - 1 > s.span.pos;
+                float y[4];
 #pragma unroll
-                for (int i = 0; i < kV; ++i)
-                    vf[t][i] = seen && 64 * i + 8 * r < d ? load_stream(vp + off * p.a.token_stride + 64 * i + 8 * r) : make_uint4(0, 0, 0, 0);
-            }
-            float x[2][4] = {};
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int i = 0; i < kS; ++i) {
-                    mma(x[t], q[i].x, 0, q[i].y, 0, kf[t][i].x, kf[t][i].y);
-                    mma(x[t], q[i].z, 0, q[i].w, 0, kf[t][i].z, kf[t][i].w);
+                for (int t = 0; t < 4; ++t) {
+                    const int token = t0 + (t & 1) + (t >> 1) * 8;
+                    y[t] = score<kExtra>(p, x[t >> 1][t & 1], slope, token - s.span.pos);
+                    if (edge && (token < s.span.lo || token > s.span.pos)) y[t] = -INFINITY;
                 }
-            float y[4];  // t0, t0 + 1, t0 + 8, t0 + 9
+                float high = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
+                high = fmaxf(high, __shfl_xor_sync(kAll, high, 1));
+                high = fmaxf(high, __shfl_xor_sync(kAll, high, 2));
+                if (__any_sync(kAll, high > m)) {
+                    const float next = fmaxf(m, high), k = exp2_approx(m - next);
+                    m = next;
+                    l *= k;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const int token = t0 + (t & 1) + (t >> 1) * 8;
-                y[t] = score<kExtra>(p, x[t >> 1][t & 1], slope, token - s.span.pos);
-                if (edge && (token < s.span.lo || token > s.span.pos)) y[t] = -INFINITY;
-            }
-            float high = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
-            high = fmaxf(high, __shfl_xor_sync(kAll, high, 1));
-            high = fmaxf(high, __shfl_xor_sync(kAll, high, 2));
-            if (__any_sync(kAll, high > m)) {
-                const float next = fmaxf(m, high), k = exp2_approx(m - next);
-                m = next;
-                l *= k;
+                    for (int j = 0; j < 8 * kV; ++j)
 #pragma unroll
-                for (int j = 0; j < 8 * kV; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[j][e] *= k;
-            }
-            float w[4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                w[t] = exp2_approx(y[t] - m);
-                l += w[t];
-            }
-            const uint32_t a0 = pack_bf16(w[0], w[1]), a2 = pack_bf16(w[2], w[3]);
-            const uint32_t a1 = pack_bf16(w[0] - __uint_as_float(a0 << 16), w[1] - __uint_as_float(a0 & 0xFFFF0000u));
-            const uint32_t a3 = pack_bf16(w[2] - __uint_as_float(a2 << 16), w[3] - __uint_as_float(a2 & 0xFFFF0000u));
-#pragma unroll
-            for (int i = 0; i < kV; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const uint32_t pick = j & 1 ? 0x7632u : 0x5410u;
-                    mma(acc[8 * i + j], a0, a1, a2, a3, __byte_perm(word(vf[0][i], j / 2), word(vf[1][i], j / 2), pick),
-                        __byte_perm(word(vf[2][i], j / 2), word(vf[3][i], j / 2), pick));
+                        for (int e = 0; e < 4; ++e) acc[j][e] *= k;
                 }
+                float w[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    w[t] = exp2_approx(y[t] - m);
+                    l += w[t];
+                }
+                const uint32_t a0 = pack_bf16(w[0], w[1]), a2 = pack_bf16(w[2], w[3]);
+                const uint32_t a1 = pack_bf16(w[0] - __uint_as_float(a0 << 16), w[1] - __uint_as_float(a0 & 0xFFFF0000u));
+                const uint32_t a3 = pack_bf16(w[2] - __uint_as_float(a2 << 16), w[3] - __uint_as_float(a2 & 0xFFFF0000u));
+#pragma unroll
+                for (int i = 0; i < kV; ++i) {
+                    uint4 v[4];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) v[t] = load_shared(at + (2 * kS + t * kV + i) * 512);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const uint32_t pick = j & 1 ? 0x7632u : 0x5410u;
+                        mma(acc[8 * i + j], a0, a1, a2, a3, __byte_perm(word(v[0], j / 2), word(v[1], j / 2), pick),
+                            __byte_perm(word(v[2], j / 2), word(v[3], j / 2), pick));
+                    }
+                }
+            }
+            ask(stage);
+            stage = stage == kStages - 1 ? 0 : stage + 1;
+        }
+        // the next stretch's copies run while this one is added up
+        more = deal.take(p, after);
+        if (more) {
+            open(after);
+#pragma unroll
+            for (int i = 0; i < kStages; ++i) ask(i);
         }
         l += __shfl_xor_sync(kAll, l, 1);
         l += __shfl_xor_sync(kAll, l, 2);
@@ -391,19 +480,26 @@ __global__ void __launch_bounds__(kThreads) attend_bf16_kernel(const __grid_cons
             top[warp * kHeads + r] = m;
             sum[warp * kHeads + r] = l;
         }
-        if (r < heads_here) {
-            float* to = part + (warp * kHeads + r) * D;
 #pragma unroll
-            for (int i = 0; i < kV; ++i)
+        for (int h = 0; h < D / kPart; ++h) {
+            if (r < heads_here) {
+                float* to = part + (warp * kHeads + r) * kPart;
+                // fragment 8 i + j, columns 2c and 2c + 1: elements 64 i + 16 c + j and + 8
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    to[64 * i + 16 * c + j] = acc[8 * i + j][0] + acc[8 * i + j][2];
-                    to[64 * i + 16 * c + 8 + j] = acc[8 * i + j][1] + acc[8 * i + j][3];
+                for (int j = 0; j < 8 * kV; ++j) {
+                    const int e = 64 * (j / 8) + 16 * c + j % 8;
+                    if (kPart >= 64 ? 64 * (j / 8) / kPart == h : e / kPart == h) {
+                        to[e - h * kPart] = acc[j][0] + acc[j][2];
+                        to[e - h * kPart + 8] = acc[j][1] + acc[j][3];
+                    }
                 }
+            }
+            __syncthreads();
+            finish<T, D, kPart>(p, s, heads_here, h * kPart, part, top, sum);
+            __syncthreads();
         }
-        __syncthreads();
-        finish<T, D>(p, s, heads_here, part, top, sum, p.a.ws);
-        __syncthreads();
+        if (!more) break;
+        s = after;
     }
     note_unfinished(p, deal, s, any, D);
     write_rest<T>(p);
@@ -416,7 +512,7 @@ __global__ void __launch_bounds__(kThreads) attend_bf16_kernel(const __grid_cons
 template <int D, int kH>
 __global__ void __launch_bounds__(kThreads) attend_f32_kernel(const __grid_constant__ Params p) {
     constexpr int kS = D / 16, kV = (D + 127) / 128;
-    __shared__ long long sums[kThreads + 1];
+    __shared__ long long sums[kThreads + 1], found[2];
     __shared__ __align__(16) float part[kWarps * kHeads * D];
     __shared__ __align__(16) float queries[kH * D];
     __shared__ float top[kWarps * kHeads], sum[kWarps * kHeads];
@@ -424,7 +520,7 @@ __global__ void __launch_bounds__(kThreads) attend_f32_kernel(const __grid_const
     const int d = p.a.head_dim;
 
     Dealer deal;
-    deal.start(p, sums);
+    deal.start(p, sums, found);
     Stretch s;
     bool any = false;
     while (deal.take(p, s)) {
@@ -548,7 +644,7 @@ __global__ void __launch_bounds__(kThreads) attend_f32_kernel(const __grid_const
                         make_float4(acc[h][i][0], acc[h][i][1], acc[h][i][2], acc[h][i][3]);
         }
         __syncthreads();
-        finish<float, D>(p, s, heads_here, part, top, sum, p.a.ws);
+        finish<float, D, D>(p, s, heads_here, 0, part, top, sum);
         __syncthreads();
     }
     note_unfinished(p, deal, s, any, D);
@@ -581,15 +677,31 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
     }
 }
 
-template <typename Kernel>
-cudaError_t launch_both(Kernel kernel, void (*join)(Params), const Params& p, cudaStream_t s) {
+// SMs of a device and CTAs of a kernel on one, asked for once.
+constexpr int kDevices = 64;
+template <auto kKernel>
+cudaError_t resident(int shared, int& ctas) {
+    static std::atomic<int> known[kDevices];
     int device = 0, sms = 0, each = 0;
     cudaError_t e = cudaGetDevice(&device);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, kernel, kThreads, 0);
     if (e != cudaSuccess) return e;
-    const int ctas = sms * each < kMaxCtas ? sms * each : kMaxCtas;
-    kernel<<<ctas, kThreads, 0, s>>>(p);
+    ctas = device < kDevices ? known[device].load(std::memory_order_relaxed) : 0;
+    if (ctas > 0) return cudaSuccess;
+    if (shared > 48 * 1024) e = cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, kKernel, kThreads, shared);
+    if (e != cudaSuccess) return e;
+    ctas = sms * each < kMaxCtas ? sms * each : kMaxCtas;
+    if (device < kDevices) known[device].store(ctas, std::memory_order_relaxed);
+    return cudaSuccess;
+}
+
+template <auto kKernel>
+cudaError_t launch_both(int shared, void (*join)(Params), const Params& p, cudaStream_t s) {
+    int ctas = 0;
+    cudaError_t e = resident<kKernel>(shared, ctas);
+    if (e != cudaSuccess) return e;
+    kKernel<<<ctas, kThreads, shared, s>>>(p);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     join<<<ctas, kThreads, 0, s>>>(p);
@@ -599,15 +711,16 @@ cudaError_t launch_both(Kernel kernel, void (*join)(Params), const Params& p, cu
 template <int D>
 cudaError_t launch_d(const Params& p, cudaStream_t s) {
     if (p.a.bf16) {
-        const bool extra = p.a.softcap > 0.0f || p.a.slopes != nullptr;
-        return extra ? launch_both(attend_bf16_kernel<D, true>, join_kernel<__nv_bfloat16, D>, p, s)
-                     : launch_both(attend_bf16_kernel<D, false>, join_kernel<__nv_bfloat16, D>, p, s);
+        constexpr int shared = Bf16Shape<D>::kShared;
+        return p.a.softcap > 0.0f || p.a.slopes != nullptr
+                   ? launch_both<attend_bf16_kernel<D, true>>(shared, join_kernel<__nv_bfloat16, D>, p, s)
+                   : launch_both<attend_bf16_kernel<D, false>>(shared, join_kernel<__nv_bfloat16, D>, p, s);
     }
     const int g = p.a.group;
-    return g == 1   ? launch_both(attend_f32_kernel<D, 1>, join_kernel<float, D>, p, s)
-           : g == 2 ? launch_both(attend_f32_kernel<D, 2>, join_kernel<float, D>, p, s)
-           : g <= 4 ? launch_both(attend_f32_kernel<D, 4>, join_kernel<float, D>, p, s)
-                    : launch_both(attend_f32_kernel<D, 8>, join_kernel<float, D>, p, s);
+    return g == 1   ? launch_both<attend_f32_kernel<D, 1>>(0, join_kernel<float, D>, p, s)
+           : g == 2 ? launch_both<attend_f32_kernel<D, 2>>(0, join_kernel<float, D>, p, s)
+           : g <= 4 ? launch_both<attend_f32_kernel<D, 4>>(0, join_kernel<float, D>, p, s)
+                    : launch_both<attend_f32_kernel<D, 8>>(0, join_kernel<float, D>, p, s);
 }
 
 int padded(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
