@@ -280,8 +280,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return r;
 }
 
-__device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
-
 // 16 bytes from global to shared memory, asynchronously; zeros if not `real`.
 __device__ __forceinline__ void copy_async(uint32_t to, const void* from, bool real) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(real ? 16 : 0) : "memory");
@@ -291,30 +289,31 @@ template <int kLeft>
 __device__ __forceinline__ void wait_copies() {
     asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
 }
-__device__ __forceinline__ uint4 load_shared(uint32_t at) {
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
-    return v;
+// Four 8 x 8 matrices of 16-bit elements; lane l gives the address of row l % 8 of matrix l / 8.
+__device__ __forceinline__ void load_matrices(uint32_t (&m)[4], uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(m[0]), "=r"(m[1]), "=r"(m[2]), "=r"(m[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void load_transposed(uint32_t (&m)[4], uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(m[0]), "=r"(m[1]), "=r"(m[2]), "=r"(m[3]) : "r"(at) : "memory");
 }
 
-// bf16. A warp holds the scores of 8 query heads x 16 tokens. With r = lane / 4 and c = lane % 4 every
-// lane's part of the fragments of mma.m16n8k16 is 16 bytes at a time from one row of the page:
-//   Q K^T: lane (r, c) takes key token r, elements 32 s + 8 c .. + 7; the order of the products' inner
-//     index is free as long as the queries use the same.
-//   P V: the scores' fragment is the next product's first operand (tokens 2c, 2c + 1 of each eight);
-//     lane (r, c) takes elements 8 r .. 8 r + 7 of those four tokens' values, and byte permutes pair
-//     them up. The output's columns come out in the order of r and are written back accordingly.
-// So each lane copies what it will use itself, kStages groups ahead, into places of its own in shared
-// memory: no bank conflicts, and nothing to wait for but its own copies.
+// bf16, mma.m16n8k16 with 8 query heads x 16 tokens a warp. Each warp copies its own groups, whole rows at a
+// time, kStages ahead into a ring of its own, so that warps never wait for one another; 16-byte pieces of row t
+// are stored at column (piece ^ t % 8), which makes the reads of 8 rows free of bank conflicts.
 // The 16-row operand has 8 query heads; for P its other 8 rows hold what rounding P to bf16 drops, so
 // that the weights enter with 16 bits at no cost.
 template <int D>
 struct Bf16Shape {
-    static constexpr int kS = D / 32, kV = D / 64, kPieces = 2 * kS + 4 * kV;
-    static constexpr int kStages = D == 64 ? 4 : 3;
+    static constexpr int kS = D / 16;                  // steps of the scores' inner product
+    static constexpr int kPieces = D / 8;              // of a row
+    static constexpr int kRows = 32 / kPieces;         // that the warp copies at a time
+    static constexpr int kGroupBytes = kGroup * D * 2; // keys, and as much for the values
+    static constexpr int kStages = D == 64 ? 4 : 2;
     static constexpr int kPart = D / 2;  // elements of the output that the warps add up at a time
     static constexpr int kCtas = D == 64 ? 3 : D == 128 ? 2 : 1;  // on an SM
-    static constexpr int kRing = kWarps * kStages * kPieces * 512;
+    static constexpr int kRing = kWarps * kStages * 2 * kGroupBytes;
     static constexpr int kShared = kRing + kWarps * kHeads * kPart * 4;
 };
 
@@ -322,29 +321,32 @@ template <int D, bool kExtra>
 __global__ void __launch_bounds__(kThreads, Bf16Shape<D>::kCtas) attend_bf16_kernel(const __grid_constant__ Params p) {
     using Shape = Bf16Shape<D>;
     using T = __nv_bfloat16;
-    constexpr int kS = Shape::kS, kV = Shape::kV, kStages = Shape::kStages, kPart = Shape::kPart;
-    constexpr uint32_t kStageBytes = Shape::kPieces * 512;
-    extern __shared__ __align__(16) char dynamic[];
+    constexpr int kS = Shape::kS, kPieces = Shape::kPieces, kRows = Shape::kRows, kStages = Shape::kStages, kPart = Shape::kPart;
+    constexpr uint32_t kGroupBytes = Shape::kGroupBytes, kStageBytes = 2 * kGroupBytes, kRowBytes = D * 2;
+    extern __shared__ __align__(128) char dynamic[];
     float* part = reinterpret_cast<float*>(dynamic + Shape::kRing);
     __shared__ long long sums[kThreads + 1], found[2];
     __shared__ float top[kWarps * kHeads], sum[kWarps * kHeads];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
     const int d = p.a.head_dim;
-    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(dynamic)) + warp * kStages * kStageBytes + lane * 16;
+    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(dynamic)) + warp * kStages * kStageBytes;
+    // this lane's row and piece of a copy, and of the matrices that it addresses
+    const int row = lane / kPieces, piece = lane % kPieces;
+    const uint32_t k_row = ring + (8 * (lane >> 4) + (lane & 7)) * kRowBytes, k_piece = (lane >> 3) & 1;
+    const uint32_t v_row = ring + kGroupBytes + (8 * ((lane >> 3) & 1) + (lane & 7)) * kRowBytes, v_piece = lane >> 4;
 
     // Copies of a stretch's groups: what is next to be asked for, and which of the stages hold a group
     // whose page is missing.
     struct Feed {
         const int* table;
-        const T *k, *v;      // of the key head, at this lane's first element
+        uint64_t at;         // the key head's, this lane's row and piece, in elements
         int group, stop, page, lo, pos;
         uint32_t missing;
     } feed = {};
     const auto ahead = [&] { feed.page = feed.group < feed.stop ? feed.table[feed.group / p.page_groups] : -1; };
     const auto open = [&](const Stretch& s) {
         feed.table = p.pages.table + static_cast<size_t>(s.span.row) * p.pages.row_pages;
-        feed.k = reinterpret_cast<const T*>(p.a.k) + s.head * p.a.head_stride + r * p.a.token_stride + 8 * c;
-        feed.v = reinterpret_cast<const T*>(p.a.v) + s.head * p.a.head_stride + 2 * c * p.a.token_stride + 8 * r;
+        feed.at = s.head * p.a.head_stride + row * p.a.token_stride + 8 * piece;
         feed.group = s.span.first + s.from * kTile + warp;
         feed.stop = min(s.span.last + 1, s.span.first + s.to * kTile);
         feed.lo = s.span.lo;
@@ -357,24 +359,18 @@ __global__ void __launch_bounds__(kThreads, Bf16Shape<D>::kCtas) attend_bf16_ker
             const bool real = feed.page >= 0 && feed.page < p.pages.n_pages;
             feed.missing = (feed.missing & ~(1u << stage)) | (real ? 0u : 1u << stage);
             if (real) {
-                const uint64_t at = feed.page * p.a.page_stride + feed.group % p.page_groups * kGroup * p.a.token_stride;
-                const uint32_t to = ring + stage * kStageBytes;
-                const T* kp = feed.k + at;
+                const uint64_t at = feed.at + feed.page * p.a.page_stride + feed.group % p.page_groups * kGroup * p.a.token_stride;
+                const T* kp = reinterpret_cast<const T*>(p.a.k) + at;
+                const T* vp = reinterpret_cast<const T*>(p.a.v) + at;
+                const uint32_t to = ring + stage * kStageBytes + row * kRowBytes;
+                const int token = feed.group * kGroup + row;
+                const bool inside = 8 * piece < d;
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int i = 0; i < kS; ++i)
-                        copy_async(to + (t * kS + i) * 512, kp + t * 8 * p.a.token_stride + 32 * i, 32 * i + 8 * c < d);
-                const T* vp = feed.v + at;
-                const int token = feed.group * kGroup + 2 * c;
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int off = (t & 1) + (t >> 1) * 8;
+                for (int j = 0; j < kGroup; j += kRows) {
+                    const uint32_t place = to + j * kRowBytes + ((piece ^ ((row + j) & 7)) << 4);
+                    copy_async(place, kp + j * p.a.token_stride, inside);
                     // a value that is not seen must not reach the sum, whatever it holds
-                    const bool seen = token + off >= feed.lo && token + off <= feed.pos;
-#pragma unroll
-                    for (int i = 0; i < kV; ++i)
-                        copy_async(to + (2 * kS + t * kV + i) * 512, vp + off * p.a.token_stride + 64 * i, seen && 64 * i + 8 * r < d);
+                    copy_async(place + kGroupBytes, vp + j * p.a.token_stride, inside && token + j >= feed.lo && token + j <= feed.pos);
                 }
             }
             feed.group += kTile;
@@ -395,32 +391,34 @@ __global__ void __launch_bounds__(kThreads, Bf16Shape<D>::kCtas) attend_bf16_ker
     while (more) {
         const int heads_here = min(kHeads, p.a.group - s.block * kHeads);
         const int head0 = s.head * p.a.group + s.block * kHeads;
-        uint4 q[kS];
-        const T* qp = reinterpret_cast<const T*>(p.a.q) + s.query * p.a.q_row + (head0 + r) * p.a.q_head;
+        uint32_t q[kS][2];
+        const T* qp = reinterpret_cast<const T*>(p.a.q) + s.query * p.a.q_row + (head0 + r) * p.a.q_head + 2 * c;
 #pragma unroll
         for (int i = 0; i < kS; ++i)
-            q[i] = r < heads_here && 32 * i + 8 * c < d ? *reinterpret_cast<const uint4*>(qp + 32 * i + 8 * c) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                q[i][h] = r < heads_here && 16 * i + 8 * h < d ? *reinterpret_cast<const uint32_t*>(qp + 16 * i + 8 * h) : 0;
         const float slope = kExtra && p.a.slopes != nullptr && r < heads_here ? p.a.slopes[head0 + r] : 0.0f;
 
-        float acc[8 * kV][4];
+        float acc[kPieces][4];
 #pragma unroll
-        for (int j = 0; j < 8 * kV; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
+        for (int j = 0; j < kPieces; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
         float m = kLowest, l = 0.0f;
         const int stop = feed.stop;
         int stage = 0;
         for (int g = s.span.first + s.from * kTile + warp; g < stop; g += kTile) {
             wait_copies<kStages - 1>();
-            const uint32_t at = ring + stage * kStageBytes;
+            __syncwarp();
+            const uint32_t at = stage * kStageBytes;
             if (!(feed.missing >> stage & 1u)) {
                 float x[2][4] = {};
 #pragma unroll
-                for (int i = 0; i < kS; ++i)
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        const uint4 k = load_shared(at + (t * kS + i) * 512);
-                        mma(x[t], q[i].x, 0, q[i].y, 0, k.x, k.y);
-                        mma(x[t], q[i].z, 0, q[i].w, 0, k.z, k.w);
-                    }
+                for (int i = 0; i < kS; ++i) {
+                    uint32_t k[4];
+                    load_matrices(k, k_row + at + (((2 * i + k_piece) ^ (lane & 7)) << 4));
+                    mma(x[0], q[i][0], 0, q[i][1], 0, k[0], k[1]);
+                    mma(x[1], q[i][0], 0, q[i][1], 0, k[2], k[3]);
+                }
                 const int t0 = g * kGroup + 2 * c;  // this lane's tokens: t0, t0 + 1, t0 + 8, t0 + 9
                 const bool edge = g * kGroup < s.span.lo || g * kGroup + kGroup - 1 > s.span.pos;
                 float y[4];
@@ -438,7 +436,7 @@ __global__ void __launch_bounds__(kThreads, Bf16Shape<D>::kCtas) attend_bf16_ker
                     m = next;
                     l *= k;
 #pragma unroll
-                    for (int j = 0; j < 8 * kV; ++j)
+                    for (int j = 0; j < kPieces; ++j)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) acc[j][e] *= k;
                 }
@@ -452,18 +450,14 @@ __global__ void __launch_bounds__(kThreads, Bf16Shape<D>::kCtas) attend_bf16_ker
                 const uint32_t a1 = pack_bf16(w[0] - __uint_as_float(a0 << 16), w[1] - __uint_as_float(a0 & 0xFFFF0000u));
                 const uint32_t a3 = pack_bf16(w[2] - __uint_as_float(a2 << 16), w[3] - __uint_as_float(a2 & 0xFFFF0000u));
 #pragma unroll
-                for (int i = 0; i < kV; ++i) {
-                    uint4 v[4];
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) v[t] = load_shared(at + (2 * kS + t * kV + i) * 512);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const uint32_t pick = j & 1 ? 0x7632u : 0x5410u;
-                        mma(acc[8 * i + j], a0, a1, a2, a3, __byte_perm(word(v[0], j / 2), word(v[1], j / 2), pick),
-                            __byte_perm(word(v[2], j / 2), word(v[3], j / 2), pick));
-                    }
+                for (int j = 0; j < kPieces; j += 2) {
+                    uint32_t v[4];
+                    load_transposed(v, v_row + at + (((j + v_piece) ^ (lane & 7)) << 4));
+                    mma(acc[j], a0, a1, a2, a3, v[0], v[1]);
+                    mma(acc[j + 1], a0, a1, a2, a3, v[2], v[3]);
                 }
             }
+            __syncwarp();
             ask(stage);
             stage = stage == kStages - 1 ? 0 : stage + 1;
         }
@@ -484,14 +478,10 @@ __global__ void __launch_bounds__(kThreads, Bf16Shape<D>::kCtas) attend_bf16_ker
         for (int h = 0; h < D / kPart; ++h) {
             if (r < heads_here) {
                 float* to = part + (warp * kHeads + r) * kPart;
-                // fragment 8 i + j, columns 2c and 2c + 1: elements 64 i + 16 c + j and + 8
 #pragma unroll
-                for (int j = 0; j < 8 * kV; ++j) {
-                    const int e = 64 * (j / 8) + 16 * c + j % 8;
-                    if (kPart >= 64 ? 64 * (j / 8) / kPart == h : e / kPart == h) {
-                        to[e - h * kPart] = acc[j][0] + acc[j][2];
-                        to[e - h * kPart + 8] = acc[j][1] + acc[j][3];
-                    }
+                for (int j = 0; j < kPart / 8; ++j) {
+                    const float(&x)[4] = acc[h * (kPart / 8) + j];
+                    *reinterpret_cast<float2*>(to + 8 * j + 2 * c) = make_float2(x[0] + x[2], x[1] + x[3]);
                 }
             }
             __syncthreads();
