@@ -444,7 +444,14 @@ class KVCache:
         for i, (k, v) in enumerate(zip(self.keys, self.values)):
             self.layers[i] = jb_kv(k.data_ptr(), v.data_ptr(), first.stride(0), heads, d, self.dtype, by_token)
         self.layer_refs = [ctypes.byref(self.layers, i * ctypes.sizeof(jb_kv)) for i in range(n)]
-        self.attend_bytes = int(lib().jb_attend_workspace(self.layer_refs[0], heads))
+        self._attend_bytes = {}
+
+    def attend_workspace(self, q_heads: int) -> int:
+        """Device bytes that attention of so many query heads works in."""
+        nbytes = self._attend_bytes.get(q_heads)
+        if nbytes is None:
+            nbytes = self._attend_bytes[q_heads] = int(lib().jb_attend_workspace(self.layer_refs[0], q_heads))
+        return nbytes
 
 
 def _new(stream, make, *args, **kwargs):
@@ -549,11 +556,12 @@ def jb_attend(cache: KVCache, layer: int, q, rows, pos, out=None, scale: Optiona
     if slopes is not None and (slopes.dtype is not torch.float32 or not slopes.is_cuda or slopes.shape != (heads,)
                                or not slopes.is_contiguous()):
         raise ValueError("slopes must be a contiguous float32 CUDA tensor, one per query head")
-    ws = _scratch(cache.attend_bytes, q, stream)
+    nbytes = cache.attend_workspace(heads)
+    ws = _scratch(max(nbytes, 16), q, stream)
     scores = jb_scores(cache.head_dim ** -0.5 if scale is None else scale, softcap, window,
                        None if slopes is None else slopes.data_ptr())
     _check(lib().jb_attend(cache.pages.ref, cache.layer_refs[layer], ctypes.byref(scores), q.data_ptr(), qa, qb, heads,
-                           pr, pp, n, out.data_ptr(), oa, ob, ws.data_ptr(), cache.attend_bytes, _stream(stream)))
+                           pr, pp, n, out.data_ptr(), oa, ob, ws.data_ptr(), nbytes, _stream(stream)))
     return out
 
 

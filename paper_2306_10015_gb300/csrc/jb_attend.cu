@@ -3,8 +3,9 @@
 // A query reads each key and value of its row once and does 4 g operations per element with g
 // query heads to a key head, so the bytes bound it: the kernels stream pages from HBM and keep all
 // state in registers. Work is cut evenly whatever the rows' lengths: the 16-token groups of all
-// (query, key head) pairs are one line, every CTA takes an equal stretch of it, and pairs that
-// cross a boundary are joined by a second kernel from partial (maximum, sum, weighted values).
+// (query, key head) pairs are one line, every warp takes an equal stretch of it and works alone, and
+// pairs that cross a boundary are joined by a second kernel from partial (maximum, sum, weighted
+// values).
 //
 // Softmax is kept with a running maximum, so that one pass is enough:
 //   m' = max(m, max_t x_t), s' = s e^(m - m') + sum e^(x_t - m'), o' likewise.
@@ -18,12 +19,10 @@ namespace jb {
 namespace {
 
 constexpr unsigned kAll = 0xFFFFFFFFu;
-constexpr int kGroup = 16;       // tokens a warp takes at a time; pages hold a multiple of it
+constexpr int kGroup = 16;         // tokens a warp takes at a time; pages hold a multiple of it
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
-constexpr int kTile = kWarps;    // groups that a CTA takes at a time: one a warp
-constexpr int kHeads = 8;        // query heads of one key head that are worked on together
-constexpr int kMaxCtas = 1024;   // of the persistent grid; the workspace has two slots for each
+constexpr int kMaxWorkers = 2048;  // warps of the persistent grid; the workspace has two slots for each
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.0e38f;
 
@@ -33,56 +32,46 @@ __device__ __forceinline__ float exp2_approx(float x) {
     return y;
 }
 
-// Cached pages are read once: no place in L1 for them.
-__device__ __forceinline__ uint4 load_stream(const void* p) {
-    uint4 v;
-    asm("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-        : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-        : "l"(p));
-    return v;
-}
-
 struct Params {
     Pages pages;
     Attend a;
-    int blocks;        // blocks of kHeads query heads to a key head
+    int blocks;        // blocks of query heads to a key head
     int page_groups;   // groups in a page
 };
 
-// The partial result of a stretch: o[kHeads][D], m[kHeads], s[kHeads].
-__host__ __device__ constexpr int slot_floats(int d) { return kHeads * (d + 2); }
+// Partial results of a stretch: o[heads][D], m[heads], s[heads], for the query heads that are worked on
+// together.
+__host__ __device__ constexpr int slot_floats(int heads, int d) { return heads * (d + 2); }
 
-// Which pair a CTA started and did not finish: joined from slot 1 of the CTA and slot 0 of the
-// `parts` - 1 that follow.
-struct Unfinished {
-    int query, head, block, parts;
+// Part `index` of a pair that is cut into `parts` stretches, the first of them worker `first`'s; parts = 0:
+// none. The first stretch is in its worker's slot 1, the others in their workers' slots 0.
+struct Cut {
+    int query, head, block, first, parts, index;
 };
 
-// Groups that query i reads: [first, last] of them, none if last < first.
+// Groups that query i reads: [first, first + groups), of tokens lo to pos.
 struct Span {
-    int row, lo, pos, first, last;
-    __device__ int tiles() const { return (last - first + kTile) / kTile; }
+    int row, lo, pos, first, groups;
 };
 
 __device__ __forceinline__ Span span_of(const Params& p, int i) {
     Span s;
     s.row = p.a.rows[i];
     s.pos = p.a.pos[i];
-    s.lo = s.first = 0;
-    s.last = -1;
+    s.lo = s.first = s.groups = 0;
     if (s.row < 0 || s.row >= p.pages.n_rows || s.pos < 0 || s.pos >= p.pages.row_pages * p.pages.page_tokens) {
         s.pos = -1;
         return s;
     }
     if (p.a.window > 0) s.lo = max(0, s.pos - p.a.window + 1);
     s.first = s.lo / kGroup;
-    s.last = s.pos / kGroup;
+    s.groups = s.pos / kGroup - s.first + 1;
     return s;
 }
 
-// A stretch of one (query, key head, block of query heads): tiles [from, to) of `tiles`.
+// Groups [from, to) of a (query, key head, block of query heads).
 struct Stretch {
-    int query, head, block, from, to, tiles;
+    int query, head, block, from, to;
     Span span;
 };
 
@@ -91,58 +80,73 @@ __device__ __forceinline__ long long quotient(long long a, long long b) {
     return ((a | b) >> 32) == 0 ? static_cast<long long>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)) : a / b;
 }
 
-static_assert(kMaxListed <= kThreads * kThreads, "a thread's run of queries is searched by one thread each");
+static_assert(kMaxListed <= kThreads * kThreads, "a thread's run of queries");
 
-// Deals the line of tiles out. All threads of a CTA go through it together.
+// Deals the line of groups out to the warps.
 struct Dealer {
     long long next, end, total;
-    int ctas;
+    int workers, worker;
     int query;
-    long long at;         // tiles of the query before `next`
+    long long at;         // groups of the query before `next`
     Span span;
 
-    __device__ static long long bound(long long total, int ctas, int cta) {
-        const long long each = quotient(total, ctas);
-        return each * cta + quotient((total - each * ctas) * cta, ctas);
+    __device__ long long bound(int w) const {
+        const long long each = quotient(total, workers);
+        return each * w + quotient((total - each * workers) * w, workers);
     }
 
-    // sums: kThreads + 1 words of shared memory, found: two.
-    __device__ void start(const Params& p, long long* sums, long long* found) {
-        const int n = p.a.n, pairs = p.a.heads * p.blocks;
+    // The CTA together. sums: kThreads + 1 words of shared memory; runs: kWarps.
+    __device__ void start(const Params& p, long long* sums, int* runs) {
+        const int n = p.a.n, pairs = p.a.heads * p.blocks, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         const int per = (n + kThreads - 1) / kThreads;
-        // tiles of each thread's run of queries
-        const int mine_from = static_cast<int>(threadIdx.x) * per, mine_to = min(n, mine_from + per);
+        // groups of each thread's run of queries
         long long mine = 0;
-        for (int i = mine_from; i < mine_to; ++i) mine += span_of(p, i).tiles();
+        for (int k = 0; k < per; ++k) {
+            const int i = static_cast<int>(threadIdx.x) * per + k;
+            if (i < n) mine += span_of(p, i).groups;
+        }
         scan(mine, sums);
         total = sums[kThreads] * pairs;
-        ctas = static_cast<int>(min(static_cast<long long>(gridDim.x), max(1ll, total)));
-        if (static_cast<int>(blockIdx.x) >= ctas || total == 0) {
-            next = end = 0;
-            return;
-        }
-        next = bound(total, ctas, blockIdx.x);
-        end = bound(total, ctas, blockIdx.x + 1);
-        // the run with the tile `next`, then the query: tiles before a query are multiples of `pairs`
-        const long long goal = quotient(next, pairs);
-        if (sums[threadIdx.x] <= goal && goal < sums[threadIdx.x + 1]) {
-            found[0] = mine_from;
-            found[1] = sums[threadIdx.x];
+        // neighbours on the line are on different SMs, so that few stretches use all of them
+        worker = warp * gridDim.x + blockIdx.x;
+        workers = static_cast<int>(min(static_cast<long long>(gridDim.x) * kWarps, max(1ll, total)));
+        next = end = 0;
+        if (total == 0) return;
+        // the runs with the warps' first groups: groups before a query are multiples of `pairs`
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            const int other = w * gridDim.x + blockIdx.x;
+            const long long goal = other < workers ? quotient(bound(other), pairs) : -1;
+            if (sums[threadIdx.x] <= goal && goal < sums[threadIdx.x + 1]) runs[w] = threadIdx.x;
         }
         __syncthreads();
-        if (per > 1) {  // at most kThreads queries (of kMaxListed) are a run
-            const long long base = found[1];
-            const int i = static_cast<int>(found[0]) + threadIdx.x;
-            scan(static_cast<int>(threadIdx.x) < per && i < n ? span_of(p, i).tiles() : 0, sums);
-            if (base + sums[threadIdx.x] <= goal && goal < base + sums[threadIdx.x + 1]) {
-                found[0] = i;
-                found[1] = base + sums[threadIdx.x];
+        if (worker >= workers) return;
+        next = bound(worker);
+        end = bound(worker + 1);
+        const long long goal = quotient(next, pairs);
+        long long base = sums[runs[warp]];
+        query = runs[warp] * per;
+        for (int k = 0; k < per; k += 32) {  // and the query within the run
+            const int i = query + lane;
+            const int g = k + lane < per && i < n ? span_of(p, i).groups : 0;
+            int in = g;
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) {
+                const int o = __shfl_up_sync(kAll, in, d);
+                if (lane >= d) in += o;
             }
-            __syncthreads();
+            const unsigned past = __ballot_sync(kAll, base + in > goal);
+            if (past != 0) {
+                const int l = __ffs(past) - 1;
+                base += __shfl_sync(kAll, in - g, l);
+                query += l;
+                break;
+            }
+            base += __shfl_sync(kAll, in, 31);
+            query += 32;
         }
-        query = static_cast<int>(found[0]);
         span = span_of(p, query);
-        at = next - found[1] * pairs;
+        at = next - base * pairs;
     }
 
     // sums[i] = sum of v over threads before i, sums[kThreads] = of all.
@@ -166,22 +170,40 @@ struct Dealer {
     __device__ bool take(const Params& p, Stretch& s) {
         if (next >= end) return false;
         const long long pairs = p.a.heads * p.blocks;
-        while (span.tiles() == 0 || at >= span.tiles() * pairs) {
-            at -= span.tiles() * pairs;
+        while (at >= span.groups * pairs) {
+            at -= span.groups * pairs;
             ++query;
             span = span_of(p, query);
         }
         s.query = query;
         s.span = span;
-        s.tiles = span.tiles();
-        const int pair = static_cast<int>(quotient(at, s.tiles));
+        const int pair = static_cast<int>(quotient(at, span.groups));
         s.head = pair / p.blocks;
         s.block = pair % p.blocks;
-        s.from = static_cast<int>(at - static_cast<long long>(pair) * s.tiles);
-        s.to = static_cast<int>(min(static_cast<long long>(s.tiles), s.from + (end - next)));
+        s.from = static_cast<int>(at - static_cast<long long>(pair) * span.groups);
+        s.to = static_cast<int>(min(static_cast<long long>(span.groups), s.from + (end - next)));
         next += s.to - s.from;
         at += s.to - s.from;
         return true;
+    }
+
+    // The worker with group x of the line.
+    __device__ int owner(long long x) const {
+        int w = static_cast<int>(quotient(x * workers, total));
+        while (bound(w) > x) --w;
+        while (bound(w + 1) <= x) ++w;
+        return w;
+    }
+
+    // How the last stretch taken is cut off at its end, if it is.
+    __device__ Cut cut(bool any, const Stretch& s) const {
+        Cut c = {0, 0, 0, 0, 0, 0};
+        if (!any || s.to == s.span.groups) return c;
+        const long long begin = next - s.to;
+        c = {s.query, s.head, s.block, owner(begin), 0, 0};
+        c.parts = owner(begin + s.span.groups - 1) - c.first + 1;
+        c.index = worker - c.first;
+        return c;
     }
 };
 
@@ -192,65 +214,109 @@ __device__ __forceinline__ void store_out<float>(float* to, float v) { *to = v; 
 template <>
 __device__ __forceinline__ void store_out<__nv_bfloat16>(__nv_bfloat16* to, float v) { *to = __float2bfloat16_rn(v); }
 
-// Adds up the warps' results, kPart elements of each head from `first` on, and stores the result itself
-// or its part of a slot of the workspace. part: [kWarps][kHeads][kPart]; top, sum: [kWarps][kHeads].
-template <typename T, int D, int kPart>
-__device__ __forceinline__ void finish(const Params& p, const Stretch& s, int heads_here, int first, const float* part,
-                                       const float* top, const float* sum) {
-    const int d = p.a.head_dim;
-    const bool whole = s.from == 0 && s.to == s.tiles;
-    float* slot = p.a.ws + static_cast<size_t>(slot_floats(D)) * (2 * blockIdx.x + (s.from == 0 ? 1 : 0));
-    for (int u = threadIdx.x; u < heads_here * kPart; u += kThreads) {
-        const int h = u / kPart, e = first + u % kPart;
-        float m = kLowest;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) m = fmaxf(m, top[w * kHeads + h]);
-        float o = 0.0f, l = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            const float c = exp2_approx(top[w * kHeads + h] - m);
-            o = fmaf(c, part[w * kHeads * kPart + u], o);
-            l = fmaf(c, sum[w * kHeads + h], l);
-        }
-        if (whole) {
-            const int head = (s.head * p.a.group) + s.block * kHeads + h;
-            if (e < d)
-                store_out(reinterpret_cast<T*>(p.a.out) + s.query * p.a.out_row + head * p.a.out_head + e, l > 0.0f ? o / l : 0.0f);
-        } else {
-            slot[h * D + e] = o;
-            if (e == 0) {
-                slot[kHeads * D + h] = m;
-                slot[kHeads * D + kHeads + h] = l;
-            }
-        }
-    }
+__device__ __forceinline__ float* slot_of(const Params& p, int heads, int d, int worker, bool first) {
+    return p.a.ws + static_cast<size_t>(slot_floats(heads, d)) * (2 * worker + (first ? 1 : 0));
 }
 
-// Which pair the CTA leaves for the second kernel, and zeros for the queries that see nothing.
+__device__ __forceinline__ Cut* cuts_of(const Params& p, int heads, int d) {
+    return reinterpret_cast<Cut*>(p.a.ws + static_cast<size_t>(slot_floats(heads, d)) * 2 * kMaxWorkers);
+}
+
+// Zeros for the queries that see nothing.
 template <typename T>
-__device__ __forceinline__ void write_rest(const Params& p) {
+__device__ __forceinline__ void write_zeros(const Params& p) {
     const int d = p.a.head_dim, heads = p.a.heads * p.a.group;
     for (int i = blockIdx.x; i < p.a.n; i += gridDim.x) {
-        if (span_of(p, i).pos >= 0) continue;
+        if (span_of(p, i).groups > 0) continue;
         for (int u = threadIdx.x; u < heads * d; u += kThreads)
             store_out(reinterpret_cast<T*>(p.a.out) + i * p.a.out_row + u / d * p.a.out_head + u % d, 0.0f);
     }
 }
 
-__device__ __forceinline__ Unfinished* unfinished(const Params& p, int d_padded) {
-    return reinterpret_cast<Unfinished*>(p.a.ws + static_cast<size_t>(slot_floats(d_padded)) * 2 * kMaxCtas);
+// 16 bytes from global to shared memory, asynchronously; zeros if not `real`.
+__device__ __forceinline__ void copy_async(uint32_t to, const void* from, bool real) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(real ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void wait_copies() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
+}
+__device__ __forceinline__ void prefetch(const void* p) { asm volatile("prefetch.global.L1 [%0];" ::"l"(p)); }
 
-__device__ __forceinline__ void note_unfinished(const Params& p, const Dealer& deal, const Stretch& s, bool any, int d_padded) {
-    if (threadIdx.x != 0) return;
-    Unfinished u = {0, 0, 0, 0};
-    if (any && s.from == 0 && s.to < s.tiles) {
-        const long long stop = deal.next - s.to + s.tiles;  // where the pair ends on the line
-        u = {s.query, s.head, s.block, 1};
-        while (Dealer::bound(deal.total, deal.ctas, blockIdx.x + u.parts) < stop) ++u.parts;
+// A warp copies its groups, whole rows at a time, kStages ahead into a ring of its own, so that warps
+// never wait for one another. 16-byte pieces of row t are stored at column (piece ^ t % 8): reads of one
+// column of 8 rows, and of one row, are free of bank conflicts.
+template <typename T, int D>
+struct Feed {
+    static constexpr int kStages = D * sizeof(T) > 512 ? 1 : 2;           // groups that a warp copies ahead
+    static constexpr int kPieces = D * static_cast<int>(sizeof(T)) / 16;  // of a row
+    static constexpr int kLanes = kPieces < 32 ? kPieces : 32;            // of them that copy one row
+    static constexpr int kRows = 32 / kLanes;                             // rows that the warp copies at a time
+    static constexpr uint32_t kRowBytes = D * sizeof(T);
+    static constexpr uint32_t kGroupBytes = kGroup * kRowBytes;           // keys, and as much for the values
+    static constexpr uint32_t kStageBytes = 2 * kGroupBytes;
+    static constexpr int kRing = kStages * kStageBytes;
+    static constexpr int kElems = 16 / sizeof(T);
+
+    uint32_t ring;       // shared address of the warp's ring
+    const int* table;
+    uint64_t at;         // the key head's, this lane's row and piece, in elements
+    int group, stop, page, lo, pos;
+    uint32_t missing;    // stages that hold a group whose page is missing
+
+    __device__ void ahead(const Params& p) { page = group < stop ? table[group / p.page_groups] : -1; }
+
+    __device__ void open(const Params& p, const Stretch& s) {
+        const int lane = threadIdx.x & 31;
+        table = p.pages.table + static_cast<size_t>(s.span.row) * p.pages.row_pages;
+        at = s.head * p.a.head_stride + lane / kLanes * p.a.token_stride + kElems * (lane % kLanes);
+        group = s.span.first + s.from;
+        stop = s.span.first + s.to;
+        lo = s.span.lo;
+        pos = s.span.pos;
+        missing = 0;
+        ahead(p);
+#pragma unroll
+        for (int i = 0; i < kStages; ++i) ask(p, i);
     }
-    unfinished(p, d_padded)[blockIdx.x] = u;
-}
+
+    __device__ __forceinline__ void ask(const Params& p, int stage) {
+        const int row = (threadIdx.x & 31) / kLanes, piece = threadIdx.x % kLanes;
+        if (group < stop) {
+            const bool real = page >= 0 && page < p.pages.n_pages;
+            missing = (missing & ~(1u << stage)) | (real ? 0u : 1u << stage);
+            if (real) {
+                const uint64_t from = at + page * p.a.page_stride + group % p.page_groups * kGroup * p.a.token_stride;
+                const T* kp = reinterpret_cast<const T*>(p.a.k) + from;
+                const T* vp = reinterpret_cast<const T*>(p.a.v) + from;
+                const uint32_t to = ring + stage * kStageBytes + row * kRowBytes;
+                const int token = group * kGroup + row;
+#pragma unroll
+                for (int j = 0; j < kGroup; j += kRows)
+#pragma unroll
+                    for (int i = 0; i < kPieces; i += kLanes) {
+                        const bool inside = kElems * (piece + i) < p.a.head_dim;
+                        const uint32_t place = to + j * kRowBytes + (((piece + i) ^ ((row + j) & 7)) << 4);
+                        copy_async(place, kp + j * p.a.token_stride + kElems * i, inside);
+                        // a value that is not seen must not reach the sum, whatever it holds
+                        copy_async(place + kGroupBytes, vp + j * p.a.token_stride + kElems * i,
+                                   inside && token + j >= lo && token + j <= pos);
+                    }
+            }
+            ++group;
+            ahead(p);
+        }
+        commit_copies();
+    }
+
+    // Waits for the group in `stage`; false if its page is missing.
+    __device__ __forceinline__ bool ready(int stage) {
+        wait_copies<kStages - 1>();
+        __syncwarp();
+        return !(missing >> stage & 1u);
+    }
+};
 
 // The score as the softmax takes it, in units of ln 2.
 template <bool kExtra>
@@ -279,16 +345,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
+// What rounding (lo, hi) to bf16 as `packed` drops.
+__device__ __forceinline__ uint32_t pack_rest(float lo, float hi, uint32_t packed) {
+    return pack_bf16(lo - __uint_as_float(packed << 16), hi - __uint_as_float(packed & 0xFFFF0000u));
+}
 
-// 16 bytes from global to shared memory, asynchronously; zeros if not `real`.
-__device__ __forceinline__ void copy_async(uint32_t to, const void* from, bool real) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(real ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int kLeft>
-__device__ __forceinline__ void wait_copies() {
-    asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
-}
 // Four 8 x 8 matrices of 16-bit elements; lane l gives the address of row l % 8 of matrix l / 8.
 __device__ __forceinline__ void load_matrices(uint32_t (&m)[4], uint32_t at) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -299,232 +360,216 @@ __device__ __forceinline__ void load_transposed(uint32_t (&m)[4], uint32_t at) {
                  : "=r"(m[0]), "=r"(m[1]), "=r"(m[2]), "=r"(m[3]) : "r"(at) : "memory");
 }
 
-// bf16, mma.m16n8k16 with 8 query heads x 16 tokens a warp. Each warp copies its own groups, whole rows at a
-// time, kStages ahead into a ring of its own, so that warps never wait for one another; 16-byte pieces of row t
-// are stored at column (piece ^ t % 8), which makes the reads of 8 rows free of bank conflicts.
-// The 16-row operand has 8 query heads; for P its other 8 rows hold what rounding P to bf16 drops, so
-// that the weights enter with 16 bits at no cost.
-template <int D>
-struct Bf16Shape {
-    static constexpr int kS = D / 16;                  // steps of the scores' inner product
-    static constexpr int kPieces = D / 8;              // of a row
-    static constexpr int kRows = 32 / kPieces;         // that the warp copies at a time
-    static constexpr int kGroupBytes = kGroup * D * 2; // keys, and as much for the values
-    static constexpr int kStages = D == 64 ? 4 : 2;
-    static constexpr int kPart = D / 2;  // elements of the output that the warps add up at a time
-    static constexpr int kCtas = D == 64 ? 3 : D == 128 ? 2 : 1;  // on an SM
-    static constexpr int kRing = kWarps * kStages * 2 * kGroupBytes;
-    static constexpr int kShared = kRing + kWarps * kHeads * kPart * 4;
-};
+// bf16, mma.m16n8k16: a warp multiplies up to 16 query heads (rows) by 16 tokens. With r = lane / 4 and
+// c = lane % 4 a lane holds the scores of rows r and r + 8, tokens 2c and 2c + 1 of each eight, which is
+// also how the weights enter the second product.
+// Weights enter it with 16 bits, as two bf16 numbers. With up to 8 query heads to a key head (kH = 8) the
+// other 8 rows hold what rounding drops, at no cost; with more, a second product adds it.
+template <int D, int kH>
+constexpr int kBf16Ctas = D == 64 ? 3 : D == 128 ? 2 : 1;  // on an SM
 
-template <int D, bool kExtra>
-__global__ void __launch_bounds__(kThreads, Bf16Shape<D>::kCtas) attend_bf16_kernel(const __grid_constant__ Params p) {
-    using Shape = Bf16Shape<D>;
+template <int D, int kH, bool kExtra>
+__global__ void __launch_bounds__(kThreads, kBf16Ctas<D, kH>) attend_bf16_kernel(const __grid_constant__ Params p) {
     using T = __nv_bfloat16;
-    constexpr int kS = Shape::kS, kPieces = Shape::kPieces, kRows = Shape::kRows, kStages = Shape::kStages, kPart = Shape::kPart;
-    constexpr uint32_t kGroupBytes = Shape::kGroupBytes, kStageBytes = 2 * kGroupBytes, kRowBytes = D * 2;
+    constexpr int kS = D / 16, kPieces = D / 8, kR = kH / 8;
     extern __shared__ __align__(128) char dynamic[];
-    float* part = reinterpret_cast<float*>(dynamic + Shape::kRing);
-    __shared__ long long sums[kThreads + 1], found[2];
-    __shared__ float top[kWarps * kHeads], sum[kWarps * kHeads];
+    __shared__ long long sums[kThreads + 1];
+    __shared__ int runs[kWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
     const int d = p.a.head_dim;
-    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(dynamic)) + warp * kStages * kStageBytes;
-    // this lane's row and piece of a copy, and of the matrices that it addresses
-    const int row = lane / kPieces, piece = lane % kPieces;
-    const uint32_t k_row = ring + (8 * (lane >> 4) + (lane & 7)) * kRowBytes, k_piece = (lane >> 3) & 1;
-    const uint32_t v_row = ring + kGroupBytes + (8 * ((lane >> 3) & 1) + (lane & 7)) * kRowBytes, v_piece = lane >> 4;
-
-    // Copies of a stretch's groups: what is next to be asked for, and which of the stages hold a group
-    // whose page is missing.
-    struct Feed {
-        const int* table;
-        uint64_t at;         // the key head's, this lane's row and piece, in elements
-        int group, stop, page, lo, pos;
-        uint32_t missing;
-    } feed = {};
-    const auto ahead = [&] { feed.page = feed.group < feed.stop ? feed.table[feed.group / p.page_groups] : -1; };
-    const auto open = [&](const Stretch& s) {
-        feed.table = p.pages.table + static_cast<size_t>(s.span.row) * p.pages.row_pages;
-        feed.at = s.head * p.a.head_stride + row * p.a.token_stride + 8 * piece;
-        feed.group = s.span.first + s.from * kTile + warp;
-        feed.stop = min(s.span.last + 1, s.span.first + s.to * kTile);
-        feed.lo = s.span.lo;
-        feed.pos = s.span.pos;
-        feed.missing = 0;
-        ahead();
-    };
-    const auto ask = [&](int stage) {
-        if (feed.group < feed.stop) {
-            const bool real = feed.page >= 0 && feed.page < p.pages.n_pages;
-            feed.missing = (feed.missing & ~(1u << stage)) | (real ? 0u : 1u << stage);
-            if (real) {
-                const uint64_t at = feed.at + feed.page * p.a.page_stride + feed.group % p.page_groups * kGroup * p.a.token_stride;
-                const T* kp = reinterpret_cast<const T*>(p.a.k) + at;
-                const T* vp = reinterpret_cast<const T*>(p.a.v) + at;
-                const uint32_t to = ring + stage * kStageBytes + row * kRowBytes;
-                const int token = feed.group * kGroup + row;
-                const bool inside = 8 * piece < d;
-#pragma unroll
-                for (int j = 0; j < kGroup; j += kRows) {
-                    const uint32_t place = to + j * kRowBytes + ((piece ^ ((row + j) & 7)) << 4);
-                    copy_async(place, kp + j * p.a.token_stride, inside);
-                    // a value that is not seen must not reach the sum, whatever it holds
-                    copy_async(place + kGroupBytes, vp + j * p.a.token_stride, inside && token + j >= feed.lo && token + j <= feed.pos);
-                }
-            }
-            feed.group += kTile;
-            ahead();
-        }
-        commit_copies();
-    };
+    Feed<T, D> feed;
+    feed.ring = static_cast<uint32_t>(__cvta_generic_to_shared(dynamic)) + warp * Feed<T, D>::kRing;
+    // this lane's row and piece of the matrices that it addresses
+    const uint32_t k_row = feed.ring + (8 * (lane >> 4) + (lane & 7)) * Feed<T, D>::kRowBytes, k_piece = (lane >> 3) & 1;
+    const uint32_t v_row = feed.ring + Feed<T, D>::kGroupBytes + (8 * ((lane >> 3) & 1) + (lane & 7)) * Feed<T, D>::kRowBytes, v_piece = lane >> 4;
 
     Dealer deal;
-    deal.start(p, sums, found);
+    deal.start(p, sums, runs);
     Stretch s, after;
     bool any = deal.take(p, s), more = any;
-    if (more) {
-        open(s);
-#pragma unroll
-        for (int i = 0; i < kStages; ++i) ask(i);
-    }
+    if (more) feed.open(p, s);
     while (more) {
-        const int heads_here = min(kHeads, p.a.group - s.block * kHeads);
-        const int head0 = s.head * p.a.group + s.block * kHeads;
-        uint32_t q[kS][2];
+        const int heads_here = min(kH, p.a.group - s.block * kH);
+        const int head0 = s.head * p.a.group + s.block * kH;
+        uint32_t q[kS][2 * kR];  // rows r and r + 8, elements 16 i + 2c and + 8
+        float slope[kR];
         const T* qp = reinterpret_cast<const T*>(p.a.q) + s.query * p.a.q_row + (head0 + r) * p.a.q_head + 2 * c;
 #pragma unroll
-        for (int i = 0; i < kS; ++i)
+        for (int h = 0; h < kR; ++h) {
+            const bool real = r + 8 * h < heads_here;
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                q[i][h] = r < heads_here && 16 * i + 8 * h < d ? *reinterpret_cast<const uint32_t*>(qp + 16 * i + 8 * h) : 0;
-        const float slope = kExtra && p.a.slopes != nullptr && r < heads_here ? p.a.slopes[head0 + r] : 0.0f;
-
-        float acc[kPieces][4];
+            for (int i = 0; i < 2 * kS; ++i)
+                q[i / 2][(i & 1) * kR + h] = real && 8 * i < d ? *reinterpret_cast<const uint32_t*>(qp + 8 * h * p.a.q_head + 8 * i) : 0;
+            slope[h] = kExtra && p.a.slopes != nullptr && real ? p.a.slopes[head0 + r + 8 * h] : 0.0f;
+        }
+        float acc[kPieces][4], m[kR], l[kR];
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
-        float m = kLowest, l = 0.0f;
-        const int stop = feed.stop;
+#pragma unroll
+        for (int h = 0; h < kR; ++h) {
+            m[h] = kLowest;
+            l[h] = 0.0f;
+        }
         int stage = 0;
-        for (int g = s.span.first + s.from * kTile + warp; g < stop; g += kTile) {
-            wait_copies<kStages - 1>();
-            __syncwarp();
-            const uint32_t at = stage * kStageBytes;
-            if (!(feed.missing >> stage & 1u)) {
+        for (int g = s.span.first + s.from; g < s.span.first + s.to; ++g) {
+            if (feed.ready(stage)) {
+                const uint32_t at = stage * Feed<T, D>::kStageBytes;
                 float x[2][4] = {};
 #pragma unroll
                 for (int i = 0; i < kS; ++i) {
                     uint32_t k[4];
                     load_matrices(k, k_row + at + (((2 * i + k_piece) ^ (lane & 7)) << 4));
-                    mma(x[0], q[i][0], 0, q[i][1], 0, k[0], k[1]);
-                    mma(x[1], q[i][0], 0, q[i][1], 0, k[2], k[3]);
+                    mma(x[0], q[i][0], kR == 2 ? q[i][1] : 0, q[i][kR], kR == 2 ? q[i][3] : 0, k[0], k[1]);
+                    mma(x[1], q[i][0], kR == 2 ? q[i][1] : 0, q[i][kR], kR == 2 ? q[i][3] : 0, k[2], k[3]);
                 }
                 const int t0 = g * kGroup + 2 * c;  // this lane's tokens: t0, t0 + 1, t0 + 8, t0 + 9
                 const bool edge = g * kGroup < s.span.lo || g * kGroup + kGroup - 1 > s.span.pos;
-                float y[4];
+                float y[kR][4];
+                bool rises = false;
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int token = t0 + (t & 1) + (t >> 1) * 8;
-                    y[t] = score<kExtra>(p, x[t >> 1][t & 1], slope, token - s.span.pos);
-                    if (edge && (token < s.span.lo || token > s.span.pos)) y[t] = -INFINITY;
+                for (int h = 0; h < kR; ++h) {
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        const int token = t0 + (t & 1) + (t >> 1) * 8;
+                        y[h][t] = score<kExtra>(p, x[t >> 1][2 * h + (t & 1)], slope[h], token - s.span.pos);
+                        if (edge && (token < s.span.lo || token > s.span.pos)) y[h][t] = -INFINITY;
+                    }
+                    float high = fmaxf(fmaxf(y[h][0], y[h][1]), fmaxf(y[h][2], y[h][3]));
+                    high = fmaxf(high, __shfl_xor_sync(kAll, high, 1));
+                    high = fmaxf(high, __shfl_xor_sync(kAll, high, 2));
+                    x[0][h] = fmaxf(m[h], high);
+                    rises = rises || high > m[h];
                 }
-                float high = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]));
-                high = fmaxf(high, __shfl_xor_sync(kAll, high, 1));
-                high = fmaxf(high, __shfl_xor_sync(kAll, high, 2));
-                if (__any_sync(kAll, high > m)) {
-                    const float next = fmaxf(m, high), k = exp2_approx(m - next);
-                    m = next;
-                    l *= k;
+                if (__any_sync(kAll, rises)) {
+                    float k[kR];
+#pragma unroll
+                    for (int h = 0; h < kR; ++h) {
+                        k[h] = exp2_approx(m[h] - x[0][h]);
+                        m[h] = x[0][h];
+                        l[h] *= k[h];
+                    }
 #pragma unroll
                     for (int j = 0; j < kPieces; ++j)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[j][e] *= k;
+                        for (int e = 0; e < 4; ++e) acc[j][e] *= k[kR == 2 ? e / 2 : 0];
                 }
-                float w[4];
+                uint32_t high_part[kR][2], rest[kR][2];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    w[t] = exp2_approx(y[t] - m);
-                    l += w[t];
+                for (int h = 0; h < kR; ++h) {
+                    float w[4];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        w[t] = exp2_approx(y[h][t] - m[h]);
+                        l[h] += w[t];
+                    }
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        high_part[h][t] = pack_bf16(w[2 * t], w[2 * t + 1]);
+                        rest[h][t] = pack_rest(w[2 * t], w[2 * t + 1], high_part[h][t]);
+                    }
                 }
-                const uint32_t a0 = pack_bf16(w[0], w[1]), a2 = pack_bf16(w[2], w[3]);
-                const uint32_t a1 = pack_bf16(w[0] - __uint_as_float(a0 << 16), w[1] - __uint_as_float(a0 & 0xFFFF0000u));
-                const uint32_t a3 = pack_bf16(w[2] - __uint_as_float(a2 << 16), w[3] - __uint_as_float(a2 & 0xFFFF0000u));
 #pragma unroll
                 for (int j = 0; j < kPieces; j += 2) {
                     uint32_t v[4];
                     load_transposed(v, v_row + at + (((j + v_piece) ^ (lane & 7)) << 4));
-                    mma(acc[j], a0, a1, a2, a3, v[0], v[1]);
-                    mma(acc[j + 1], a0, a1, a2, a3, v[2], v[3]);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        if constexpr (kR == 1) {
+                            mma(acc[j + i], high_part[0][0], rest[0][0], high_part[0][1], rest[0][1], v[2 * i], v[2 * i + 1]);
+                        } else {
+                            mma(acc[j + i], high_part[0][0], high_part[kR - 1][0], high_part[0][1], high_part[kR - 1][1], v[2 * i], v[2 * i + 1]);
+                            mma(acc[j + i], rest[0][0], rest[kR - 1][0], rest[0][1], rest[kR - 1][1], v[2 * i], v[2 * i + 1]);
+                        }
+                    }
                 }
             }
             __syncwarp();
-            ask(stage);
-            stage = stage == kStages - 1 ? 0 : stage + 1;
+            feed.ask(p, stage);
+            stage = stage == Feed<T, D>::kStages - 1 ? 0 : stage + 1;
         }
-        // the next stretch's copies run while this one is added up
+        // the next stretch's copies run while this one is finished
         more = deal.take(p, after);
         if (more) {
-            open(after);
-#pragma unroll
-            for (int i = 0; i < kStages; ++i) ask(i);
+            feed.open(p, after);
+            if (c < D / 64 && r < p.a.group)
+                prefetch(reinterpret_cast<const T*>(p.a.q) + after.query * p.a.q_row +
+                         (after.head * p.a.group + min(after.block * kH + r, p.a.group - 1)) * p.a.q_head + min(64 * c, d - 8));
         }
-        l += __shfl_xor_sync(kAll, l, 1);
-        l += __shfl_xor_sync(kAll, l, 2);
-        if (c == 0) {
-            top[warp * kHeads + r] = m;
-            sum[warp * kHeads + r] = l;
-        }
+        const bool whole = s.from == 0 && s.to == s.span.groups;
+        float* slot = slot_of(p, kH, D, deal.worker, s.from == 0);
 #pragma unroll
-        for (int h = 0; h < D / kPart; ++h) {
-            if (r < heads_here) {
-                float* to = part + (warp * kHeads + r) * kPart;
+        for (int h = 0; h < kR; ++h) {
+            l[h] += __shfl_xor_sync(kAll, l[h], 1);
+            l[h] += __shfl_xor_sync(kAll, l[h], 2);
+            if (r + 8 * h >= heads_here) continue;
+            const float inverse = l[h] > 0.0f ? 1.0f / l[h] : 0.0f;
+            T* out = reinterpret_cast<T*>(p.a.out) + s.query * p.a.out_row + (head0 + r + 8 * h) * p.a.out_head + 2 * c;
 #pragma unroll
-                for (int j = 0; j < kPart / 8; ++j) {
-                    const float(&x)[4] = acc[h * (kPart / 8) + j];
-                    *reinterpret_cast<float2*>(to + 8 * j + 2 * c) = make_float2(x[0] + x[2], x[1] + x[3]);
-                }
+            for (int j = 0; j < kPieces; ++j) {
+                // rows r and r + 8 are two query heads, or two parts of one
+                const float o0 = kR == 2 ? acc[j][2 * h] : acc[j][0] + acc[j][2];
+                const float o1 = kR == 2 ? acc[j][2 * h + 1] : acc[j][1] + acc[j][3];
+                if (!whole)
+                    *reinterpret_cast<float2*>(slot + (r + 8 * h) * D + 8 * j + 2 * c) = make_float2(o0, o1);
+                else if (8 * j < d)
+                    *reinterpret_cast<uint32_t*>(out + 8 * j) = pack_bf16(o0 * inverse, o1 * inverse);
             }
-            __syncthreads();
-            finish<T, D, kPart>(p, s, heads_here, h * kPart, part, top, sum);
-            __syncthreads();
+            if (!whole && c == 0) {
+                slot[kH * D + r + 8 * h] = m[h];
+                slot[kH * D + kH + r + 8 * h] = l[h];
+            }
         }
         if (!more) break;
         s = after;
     }
-    note_unfinished(p, deal, s, any, D);
-    write_rest<T>(p);
+    if (lane == 0) cuts_of(p, kH, D)[warp * gridDim.x + blockIdx.x] = deal.cut(any, s);
+    write_zeros<T>(p);
 }
 
-// fp32, on the FMA units. kH query heads at a time. For the scores lane (r, c) takes key token r,
-// elements 16 s + 4 c .. + 3, against the queries in shared memory, and the quad adds up; for the
-// values a lane takes elements 4 lane .. + 3 of every token, with the weights from the lanes that
-// hold them.
+// fp32, on the FMA units, kH query heads at a time. For the scores a lane takes token lane % 16 and half of
+// its elements against the queries in shared memory; for the values it takes four (eight) elements of
+// every token, with the weights from shared memory.
+template <int D>
+constexpr int kF32Ctas = D == 64 ? 3 : 1;  // on an SM
+constexpr int kF32Heads = 8;               // of a slot
+
 template <int D, int kH>
-__global__ void __launch_bounds__(kThreads) attend_f32_kernel(const __grid_constant__ Params p) {
-    constexpr int kS = D / 16, kV = (D + 127) / 128;
-    __shared__ long long sums[kThreads + 1], found[2];
-    __shared__ __align__(16) float part[kWarps * kHeads * D];
-    __shared__ __align__(16) float queries[kH * D];
-    __shared__ float top[kWarps * kHeads], sum[kWarps * kHeads];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
+struct F32Shape {
+    static constexpr int kQueries = kH * D * 4, kWeights = kGroup * kH * 4;
+    static constexpr int kWarpBytes = Feed<float, D>::kRing + kQueries + kWeights;
+};
+
+template <int D, int kH>
+__global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const __grid_constant__ Params p) {
+    using T = float;
+    using Shape = F32Shape<D, kH>;
+    constexpr int kPieces = D / 4, kV = (D + 127) / 128;  // pieces of the values that a lane takes
+    extern __shared__ __align__(128) char dynamic[];
+    __shared__ long long sums[kThreads + 1];
+    __shared__ int runs[kWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, token = lane & 15, half = lane >> 4;
     const int d = p.a.head_dim;
+    char* mine = dynamic + warp * Shape::kWarpBytes;
+    float* queries = reinterpret_cast<float*>(mine + Feed<float, D>::kRing);
+    float* weights = queries + kH * D;
+    Feed<float, D> feed;
+    feed.ring = static_cast<uint32_t>(__cvta_generic_to_shared(mine));
 
     Dealer deal;
-    deal.start(p, sums, found);
-    Stretch s;
-    bool any = false;
-    while (deal.take(p, s)) {
-        any = true;
-        const int heads_here = min(kHeads, p.a.group - s.block * kHeads);
-        const int head0 = s.head * p.a.group + s.block * kHeads;
-        for (int u = threadIdx.x; u < kH * D; u += kThreads) {
-            const int h = u / D, e = u % D;
-            queries[u] = h < heads_here && e < d
-                             ? reinterpret_cast<const float*>(p.a.q)[s.query * p.a.q_row + (head0 + h) * p.a.q_head + e]
-                             : 0.0f;
-        }
-        __syncthreads();
+    deal.start(p, sums, runs);
+    Stretch s, after;
+    bool any = deal.take(p, s), more = any;
+    if (more) feed.open(p, s);
+    while (more) {
+        const int heads_here = min(kH, p.a.group - s.block * kH);
+        const int head0 = s.head * p.a.group + s.block * kH;
         float slope[kH], m[kH], l[kH], acc[kH][kV][4];
+        for (int u = lane; u < kH * kPieces; u += 32) {
+            const int h = u / kPieces, e = u % kPieces * 4;
+            *reinterpret_cast<float4*>(queries + 4 * u) =
+                h < heads_here && e < d ? *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.a.q) + s.query * p.a.q_row + (head0 + h) * p.a.q_head + e)
+                                        : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        }
 #pragma unroll
         for (int h = 0; h < kH; ++h) {
             slope[h] = p.a.slopes != nullptr && h < heads_here ? p.a.slopes[head0 + h] : 0.0f;
@@ -533,137 +578,162 @@ __global__ void __launch_bounds__(kThreads) attend_f32_kernel(const __grid_const
 #pragma unroll
             for (int i = 0; i < kV; ++i) acc[h][i][0] = acc[h][i][1] = acc[h][i][2] = acc[h][i][3] = 0.0f;
         }
-        const int* table = p.pages.table + static_cast<size_t>(s.span.row) * p.pages.row_pages;
-        const int stop = min(s.span.last + 1, s.span.first + s.to * kTile);
-        for (int g = s.span.first + s.from * kTile + warp; g < stop; g += kTile) {
-            const int page = table[g / p.page_groups];
-            if (page < 0 || page >= p.pages.n_pages) continue;
-            const uint64_t at = page * p.a.page_stride + s.head * p.a.head_stride + g % p.page_groups * kGroup * p.a.token_stride;
-            const float* kp = reinterpret_cast<const float*>(p.a.k) + at;
-            const float* vp = reinterpret_cast<const float*>(p.a.v) + at;
-            float x[2][kH] = {};
+        __syncwarp();
+        int stage = 0;
+        for (int g = s.span.first + s.from; g < s.span.first + s.to; ++g) {
+            if (feed.ready(stage)) {
+                const char* keys = mine + stage * Feed<float, D>::kStageBytes + token * Feed<float, D>::kRowBytes;
+                const char* values = mine + stage * Feed<float, D>::kStageBytes + Feed<float, D>::kGroupBytes;
+                float x[kH] = {};
+#pragma unroll 4
+                for (int i = 0; i < kPieces; i += 2) {
+                    const float4 k = *reinterpret_cast<const float4*>(keys + (((i + half) ^ (token & 7)) << 4));
 #pragma unroll
-            for (int i = 0; i < kS; ++i) {
-                if (16 * i + 4 * c >= d) break;
-                float4 kf[2];
+                    for (int h = 0; h < kH; ++h) {
+                        const float4 q = *reinterpret_cast<const float4*>(queries + h * D + 4 * (i + half));
+                        x[h] = fmaf(q.w, k.w, fmaf(q.z, k.z, fmaf(q.y, k.y, fmaf(q.x, k.x, x[h]))));
+                    }
+                }
+                const int t = g * kGroup + token;
+                const bool unseen = t < s.span.lo || t > s.span.pos;
+                float high[kH];
+                bool rises = false;
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const uint4 v = load_stream(kp + (8 * t + r) * p.a.token_stride + 16 * i + 4 * c);
-                    kf[t] = make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
+                for (int h = 0; h < kH; ++h) {
+                    float y = (x[h] + __shfl_xor_sync(kAll, x[h], 16)) * p.a.scale;
+                    if (p.a.softcap > 0.0f) y = p.a.softcap * tanhf(y / p.a.softcap);
+                    y = fmaf(slope[h], static_cast<float>(t - s.span.pos), y);
+                    x[h] = unseen ? -INFINITY : y;
+                    high[h] = x[h];
+#pragma unroll
+                    for (int w = 1; w < 16; w *= 2) high[h] = fmaxf(high[h], __shfl_xor_sync(kAll, high[h], w));
+                    rises = rises || high[h] > m[h];
+                }
+                if (rises) {  // the lanes agree
+#pragma unroll
+                    for (int h = 0; h < kH; ++h) {
+                        const float top = fmaxf(m[h], high[h]), k = exp2_approx((m[h] - top) * kLog2e);
+                        m[h] = top;
+                        l[h] *= k;
+#pragma unroll
+                        for (int i = 0; i < kV; ++i)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[h][i][e] *= k;
+                    }
                 }
 #pragma unroll
                 for (int h = 0; h < kH; ++h) {
-                    const float4 q = *reinterpret_cast<const float4*>(queries + h * D + 16 * i + 4 * c);
-#pragma unroll
-                    for (int t = 0; t < 2; ++t)
-                        x[t][h] = fmaf(q.w, kf[t].w, fmaf(q.z, kf[t].z, fmaf(q.y, kf[t].y, fmaf(q.x, kf[t].x, x[t][h]))));
+                    x[h] = exp2_approx((x[h] - m[h]) * kLog2e);
+                    l[h] += x[h];
+                    if (half == 0) weights[token * kH + h] = x[h];
                 }
-            }
-            const bool edge = g * kGroup < s.span.lo || g * kGroup + kGroup - 1 > s.span.pos;
-            float w[2][kH];
-#pragma unroll
-            for (int h = 0; h < kH; ++h) {
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    float y = x[t][h];
-                    y += __shfl_xor_sync(kAll, y, 1);
-                    y += __shfl_xor_sync(kAll, y, 2);
-                    const int token = g * kGroup + 8 * t + r;
-                    y *= p.a.scale;
-                    if (p.a.softcap > 0.0f) y = p.a.softcap * tanhf(y / p.a.softcap);
-                    y = fmaf(slope[h], static_cast<float>(token - s.span.pos), y);
-                    if (edge && (token < s.span.lo || token > s.span.pos)) y = -INFINITY;
-                    w[t][h] = y;
-                }
-                float high = fmaxf(w[0][h], w[1][h]);
-                high = fmaxf(high, __shfl_xor_sync(kAll, high, 4));
-                high = fmaxf(high, __shfl_xor_sync(kAll, high, 8));
-                high = fmaxf(high, __shfl_xor_sync(kAll, high, 16));
-                if (high > m[h]) {
-                    const float k = exp2_approx((m[h] - high) * kLog2e);
-                    m[h] = high;
-                    l[h] *= k;
+                __syncwarp();
+#pragma unroll 4
+                for (int u = 0; u < kGroup; ++u) {
+                    float4 v[kV];
 #pragma unroll
                     for (int i = 0; i < kV; ++i)
+                        v[i] = *reinterpret_cast<const float4*>(values + u * Feed<float, D>::kRowBytes + (((lane % kPieces + 32 * i) ^ (u & 7)) << 4));
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[h][i][e] *= k;
-                }
+                    for (int h = 0; h < kH; ++h) {
+                        const float w = weights[u * kH + h];
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    w[t][h] = exp2_approx((w[t][h] - m[h]) * kLog2e);
-                    l[h] += w[t][h];
-                }
-            }
-#pragma unroll
-            for (int t = 0; t < kGroup; ++t) {
-                const int token = g * kGroup + t;
-                if (edge && (token < s.span.lo || token > s.span.pos)) continue;  // the warp agrees
-                float4 v[kV];
-#pragma unroll
-                for (int i = 0; i < kV; ++i) {
-                    uint4 u = make_uint4(0, 0, 0, 0);
-                    if (128 * i + 4 * lane < d) u = load_stream(vp + t * p.a.token_stride + 128 * i + 4 * lane);
-                    v[i] = make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w));
-                }
-#pragma unroll
-                for (int h = 0; h < kH; ++h) {
-                    const float weight = __shfl_sync(kAll, w[t >> 3][h], (t & 7) * 4);
-#pragma unroll
-                    for (int i = 0; i < kV; ++i) {
-                        acc[h][i][0] = fmaf(weight, v[i].x, acc[h][i][0]);
-                        acc[h][i][1] = fmaf(weight, v[i].y, acc[h][i][1]);
-                        acc[h][i][2] = fmaf(weight, v[i].z, acc[h][i][2]);
-                        acc[h][i][3] = fmaf(weight, v[i].w, acc[h][i][3]);
+                        for (int i = 0; i < kV; ++i) {
+                            acc[h][i][0] = fmaf(w, v[i].x, acc[h][i][0]);
+                            acc[h][i][1] = fmaf(w, v[i].y, acc[h][i][1]);
+                            acc[h][i][2] = fmaf(w, v[i].z, acc[h][i][2]);
+                            acc[h][i][3] = fmaf(w, v[i].w, acc[h][i][3]);
+                        }
                     }
                 }
             }
+            __syncwarp();
+            feed.ask(p, stage);
+            stage = stage == Feed<T, D>::kStages - 1 ? 0 : stage + 1;
         }
+        more = deal.take(p, after);
+        if (more) feed.open(p, after);
+        const bool whole = s.from == 0 && s.to == s.span.groups;
+        float* slot = slot_of(p, kF32Heads, D, deal.worker, s.from == 0);
 #pragma unroll
         for (int h = 0; h < kH; ++h) {
-            l[h] += __shfl_xor_sync(kAll, l[h], 4);
-            l[h] += __shfl_xor_sync(kAll, l[h], 8);
-            l[h] += __shfl_xor_sync(kAll, l[h], 16);
-            if (lane == 0) {
-                top[warp * kHeads + h] = m[h] * kLog2e;
-                sum[warp * kHeads + h] = l[h];
-            }
 #pragma unroll
-            for (int i = 0; i < kV; ++i)
-                if (128 * i + 4 * lane < D)
-                    *reinterpret_cast<float4*>(part + (warp * kHeads + h) * D + 128 * i + 4 * lane) =
-                        make_float4(acc[h][i][0], acc[h][i][1], acc[h][i][2], acc[h][i][3]);
+            for (int w = 1; w < 16; w *= 2) l[h] += __shfl_xor_sync(kAll, l[h], w);
+            if (h >= heads_here) continue;
+            const float inverse = l[h] > 0.0f ? 1.0f / l[h] : 0.0f;
+            float* out = reinterpret_cast<float*>(p.a.out) + s.query * p.a.out_row + (head0 + h) * p.a.out_head;
+#pragma unroll
+            for (int i = 0; i < kV; ++i) {
+                const int e = 4 * lane + 128 * i;
+                if (e >= D) continue;
+                if (!whole)
+                    *reinterpret_cast<float4*>(slot + h * D + e) = make_float4(acc[h][i][0], acc[h][i][1], acc[h][i][2], acc[h][i][3]);
+                else if (e < d)
+                    *reinterpret_cast<float4*>(out + e) =
+                        make_float4(acc[h][i][0] * inverse, acc[h][i][1] * inverse, acc[h][i][2] * inverse, acc[h][i][3] * inverse);
+            }
+            if (!whole && lane == 0) {
+                slot[kF32Heads * D + h] = m[h] * kLog2e;
+                slot[kF32Heads * D + kF32Heads + h] = l[h];
+            }
         }
-        __syncthreads();
-        finish<float, D, D>(p, s, heads_here, 0, part, top, sum);
-        __syncthreads();
+        if (!more) break;
+        s = after;
+        __syncwarp();
     }
-    note_unfinished(p, deal, s, any, D);
-    write_rest<float>(p);
+    if (lane == 0) cuts_of(p, kF32Heads, D)[warp * gridDim.x + blockIdx.x] = deal.cut(any, s);
+    write_zeros<float>(p);
 }
 
-// Joins a pair's partial results; one CTA for each CTA that left one, in the order of the line.
-template <typename T, int D>
+// Joins the parts of cut pairs in the order of the line. Every worker whose last stretch is cut off has a
+// CTA here; those of one pair share its elements: all by one, or an 8th or a 64th each. With fewer
+// elements than threads, groups of threads take every so many parts and are added up at the end.
+template <typename T, int D, int kH>
 __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ Params p) {
-    const Unfinished u = unfinished(p, D)[blockIdx.x];
-    if (u.parts == 0) return;
-    const int heads_here = min(kHeads, p.a.group - u.block * kHeads), d = p.a.head_dim;
-    const auto slot = [&](int i) {
-        return p.a.ws + static_cast<size_t>(slot_floats(D)) * (2 * (blockIdx.x + i) + (i == 0 ? 1 : 0));
-    };
-    for (int e = threadIdx.x; e < heads_here * D; e += kThreads) {
-        const int h = e / D;
-        float m = kLowest;
-        for (int i = 0; i < u.parts; ++i) m = fmaxf(m, slot(i)[kHeads * D + h]);
-        float o = 0.0f, l = 0.0f;
-        for (int i = 0; i < u.parts; ++i) {
-            const float* f = slot(i);
-            const float c = exp2_approx(f[kHeads * D + h] - m);
-            o = fmaf(c, f[e], o);
-            l = fmaf(c, f[kHeads * D + kHeads + h], l);
+    const Cut u = cuts_of(p, kH, D)[blockIdx.x];
+    const int slices = u.parts > 64 ? 64 : u.parts > 8 ? 8 : 1;
+    if (u.parts == 0 || u.index >= slices) return;
+    __shared__ float4 sums[kThreads];
+    __shared__ float2 stats[kThreads];
+    const int heads_here = min(kH, p.a.group - u.block * kH), d = p.a.head_dim;
+    const int quads = kH * D / 4 / slices, lanes = min(quads, kThreads), teams = kThreads / lanes;
+    const int lane = threadIdx.x % lanes, team = threadIdx.x / lanes;
+    for (int first = u.index * quads; first < (u.index + 1) * quads; first += lanes) {
+        const int e = 4 * (first + lane), h = e / D;
+        float m = kLowest, l = 0.0f;
+        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (h < heads_here) {
+#pragma unroll 4
+            for (int i = team; i < u.parts; i += teams) {
+                const float* f = slot_of(p, kH, D, u.first + i, i == 0);
+                const float mi = f[kH * D + h], li = f[kH * D + kH + h];
+                const float4 x = *reinterpret_cast<const float4*>(f + e);
+                const float high = fmaxf(m, mi), a = exp2_approx(m - high), b = exp2_approx(mi - high);
+                m = high;
+                l = fmaf(b, li, a * l);
+                o = make_float4(fmaf(b, x.x, a * o.x), fmaf(b, x.y, a * o.y), fmaf(b, x.z, a * o.z), fmaf(b, x.w, a * o.w));
+            }
         }
-        if (e % D < d)
-            store_out(reinterpret_cast<T*>(p.a.out) + u.query * p.a.out_row + (u.head * p.a.group + u.block * kHeads + h) * p.a.out_head + e % D,
-                      l > 0.0f ? o / l : 0.0f);
+        sums[threadIdx.x] = o;
+        stats[threadIdx.x] = make_float2(m, l);
+        __syncthreads();
+        if (team == 0 && h < heads_here && e % D < d) {
+            for (int i = 1; i < teams; ++i) {
+                const float4 x = sums[i * lanes + lane];
+                const float2 t = stats[i * lanes + lane];
+                const float high = fmaxf(m, t.x), a = exp2_approx(m - high), b = exp2_approx(t.x - high);
+                m = high;
+                l = fmaf(b, t.y, a * l);
+                o = make_float4(fmaf(b, x.x, a * o.x), fmaf(b, x.y, a * o.y), fmaf(b, x.z, a * o.z), fmaf(b, x.w, a * o.w));
+            }
+            const float inverse = l > 0.0f ? 1.0f / l : 0.0f;
+            T* out = reinterpret_cast<T*>(p.a.out) + u.query * p.a.out_row + (u.head * p.a.group + u.block * kH + h) * p.a.out_head + e % D;
+            store_out(out, o.x * inverse);
+            store_out(out + 1, o.y * inverse);
+            store_out(out + 2, o.z * inverse);
+            store_out(out + 3, o.w * inverse);
+        }
+        __syncthreads();
     }
 }
 
@@ -681,48 +751,57 @@ cudaError_t resident(int shared, int& ctas) {
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
     if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, kKernel, kThreads, shared);
     if (e != cudaSuccess) return e;
-    ctas = sms * each < kMaxCtas ? sms * each : kMaxCtas;
+    ctas = sms * each < kMaxWorkers / kWarps ? sms * each : kMaxWorkers / kWarps;
+    if (ctas < 1) return cudaErrorInvalidConfiguration;
     if (device < kDevices) known[device].store(ctas, std::memory_order_relaxed);
     return cudaSuccess;
 }
 
-template <auto kKernel>
-cudaError_t launch_both(int shared, void (*join)(Params), const Params& p, cudaStream_t s) {
+template <auto kKernel, auto kJoin>
+cudaError_t launch_both(int shared, const Params& p, cudaStream_t s) {
     int ctas = 0;
     cudaError_t e = resident<kKernel>(shared, ctas);
     if (e != cudaSuccess) return e;
     kKernel<<<ctas, kThreads, shared, s>>>(p);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
-    join<<<ctas, kThreads, 0, s>>>(p);
+    kJoin<<<ctas * kWarps, kThreads, 0, s>>>(p);
     return cudaGetLastError();
+}
+
+template <int D, int kH>
+cudaError_t launch_bf16(Params p, cudaStream_t s) {
+    constexpr int shared = kWarps * Feed<__nv_bfloat16, D>::kRing;
+    p.blocks = (p.a.group + kH - 1) / kH;
+    return p.a.softcap > 0.0f || p.a.slopes != nullptr
+               ? launch_both<attend_bf16_kernel<D, kH, true>, join_kernel<__nv_bfloat16, D, kH>>(shared, p, s)
+               : launch_both<attend_bf16_kernel<D, kH, false>, join_kernel<__nv_bfloat16, D, kH>>(shared, p, s);
+}
+
+template <int D, int kH>
+cudaError_t launch_f32(Params p, cudaStream_t s) {
+    p.blocks = (p.a.group + kH - 1) / kH;
+    return launch_both<attend_f32_kernel<D, kH>, join_kernel<float, D, kF32Heads>>(kWarps * F32Shape<D, kH>::kWarpBytes, p, s);
 }
 
 template <int D>
 cudaError_t launch_d(const Params& p, cudaStream_t s) {
-    if (p.a.bf16) {
-        constexpr int shared = Bf16Shape<D>::kShared;
-        return p.a.softcap > 0.0f || p.a.slopes != nullptr
-                   ? launch_both<attend_bf16_kernel<D, true>>(shared, join_kernel<__nv_bfloat16, D>, p, s)
-                   : launch_both<attend_bf16_kernel<D, false>>(shared, join_kernel<__nv_bfloat16, D>, p, s);
-    }
     const int g = p.a.group;
-    return g == 1   ? launch_both<attend_f32_kernel<D, 1>>(0, join_kernel<float, D>, p, s)
-           : g == 2 ? launch_both<attend_f32_kernel<D, 2>>(0, join_kernel<float, D>, p, s)
-           : g <= 4 ? launch_both<attend_f32_kernel<D, 4>>(0, join_kernel<float, D>, p, s)
-                    : launch_both<attend_f32_kernel<D, 8>>(0, join_kernel<float, D>, p, s);
+    if (p.a.bf16) return g <= 8 ? launch_bf16<D, 8>(p, s) : launch_bf16<D, 16>(p, s);
+    return g == 1 ? launch_f32<D, 1>(p, s) : g == 2 ? launch_f32<D, 2>(p, s) : g <= 4 ? launch_f32<D, 4>(p, s) : launch_f32<D, 8>(p, s);
 }
 
 int padded(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 
 }  // namespace
 
-uint64_t attend_workspace(int, int, int, int head_dim) {
-    return kMaxCtas * (2ull * slot_floats(padded(head_dim)) * sizeof(float) + sizeof(Unfinished));
+uint64_t attend_workspace(int bf16, int, int group, int head_dim) {
+    const int heads = bf16 && group > 8 ? 16 : 8;
+    return kMaxWorkers * (2ull * slot_floats(heads, padded(head_dim)) * sizeof(float) + sizeof(Cut));
 }
 
 cudaError_t launch_attend(const Pages& pages, const Attend& a, cudaStream_t s) {
-    const Params p = {pages, a, (a.group + kHeads - 1) / kHeads, pages.page_tokens / kGroup};
+    const Params p = {pages, a, 1, pages.page_tokens / kGroup};
     switch (padded(a.head_dim)) {
         case 64: return launch_d<64>(p, s);
         case 128: return launch_d<128>(p, s);
