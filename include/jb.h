@@ -392,7 +392,9 @@ typedef struct {
  * as the sum of two bf16 numbers (16 bits of it).
  *   q_heads    a multiple of the layer's heads
  *   strides    in elements, multiples of 16 bytes; pointers 16-byte aligned
- *   workspace  jb_attend_workspace(...) bytes, 16-byte aligned, contents free
+ *   workspace  jb_attend_workspace(...) bytes, 16-byte aligned, the first 65536 of them
+ *              zero before its first use; every call leaves it ready for the next one on
+ *              the stream. Calls that may run at the same time need one each.
  */
 int jb_attend(const jb_pages* pages, const jb_kv* layer, const jb_scores* scores, const void* d_q,
               uint64_t q_row_stride, uint64_t q_head_stride, int q_heads, const int32_t* d_rows,

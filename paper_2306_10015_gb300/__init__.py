@@ -43,6 +43,7 @@ JB_F32, JB_BF16 = 0, 1
 SEED_DTYPE = np.dtype([("machine_id", "<u8"), ("step", "<u4"), ("sample_id", "<u4")])
 
 FLAT_ALIGN = 8
+ATTEND_ZEROS = 65536  # bytes of a workspace of jb_attend that are zero between calls
 
 
 class JbError(RuntimeError):
@@ -444,14 +445,27 @@ class KVCache:
         for i, (k, v) in enumerate(zip(self.keys, self.values)):
             self.layers[i] = jb_kv(k.data_ptr(), v.data_ptr(), first.stride(0), heads, d, self.dtype, by_token)
         self.layer_refs = [ctypes.byref(self.layers, i * ctypes.sizeof(jb_kv)) for i in range(n)]
-        self._attend_bytes = {}
+        self._workspaces = {}
 
-    def attend_workspace(self, q_heads: int) -> int:
-        """Device bytes that attention of so many query heads works in."""
-        nbytes = self._attend_bytes.get(q_heads)
-        if nbytes is None:
-            nbytes = self._attend_bytes[q_heads] = int(lib().jb_attend_workspace(self.layer_refs[0], q_heads))
-        return nbytes
+    def new_workspace(self, q_heads: int, stream=None):
+        """A workspace for jb_attend with so many query heads: a uint8 tensor, ready for use on the stream."""
+        import torch
+        nbytes = int(lib().jb_attend_workspace(self.layer_refs[0], q_heads))
+        ws = _new(stream, torch.empty, max(nbytes, ATTEND_ZEROS), dtype=torch.uint8, device=self.keys[0].device)
+        _new(stream, ws[:ATTEND_ZEROS].zero_)
+        return ws
+
+    def _workspace(self, q_heads: int, stream):
+        # one for each stream, and a new one for each call that a graph captures: the graph may be
+        # replayed on another stream
+        import torch
+        if _new(stream, torch.cuda.is_current_stream_capturing):
+            return self.new_workspace(q_heads, stream)
+        key = _stream(stream).value, q_heads
+        ws = self._workspaces.get(key)
+        if ws is None:
+            ws = self._workspaces[key] = self.new_workspace(q_heads, stream)
+        return ws
 
 
 def _new(stream, make, *args, **kwargs):
@@ -542,10 +556,12 @@ def jb_cache_write(cache: KVCache, layer: int, k, v, rows, pos, stream=None) -> 
 
 
 def jb_attend(cache: KVCache, layer: int, q, rows, pos, out=None, scale: Optional[float] = None,
-              softcap: float = 0.0, window: int = 0, slopes=None, stream=None):
+              softcap: float = 0.0, window: int = 0, slopes=None, workspace=None, stream=None):
     """Attention of queries q [n, q_heads, head_dim] over positions <= pos[i] of row rows[i];
     returns ``out``. Scores are scale q.k (default 1 / sqrt(head_dim)), capped by softcap tanh,
-    biased by slopes[head] (t - pos), limited to the last `window` positions."""
+    biased by slopes[head] (t - pos), limited to the last `window` positions. ``workspace``: by default
+    one that the cache keeps for the stream; ``cache.new_workspace`` makes others, for instance one for
+    all the calls that a CUDA graph captures (by default each gets its own there)."""
     import torch
     pr, pp, n = _two_lists(rows, pos, "rows and positions")
     heads = q.shape[1] if q.dim() == 3 else 0
@@ -556,12 +572,11 @@ def jb_attend(cache: KVCache, layer: int, q, rows, pos, out=None, scale: Optiona
     if slopes is not None and (slopes.dtype is not torch.float32 or not slopes.is_cuda or slopes.shape != (heads,)
                                or not slopes.is_contiguous()):
         raise ValueError("slopes must be a contiguous float32 CUDA tensor, one per query head")
-    nbytes = cache.attend_workspace(heads)
-    ws = _scratch(max(nbytes, 16), q, stream)
+    ws = cache._workspace(heads, stream) if workspace is None else workspace
     scores = jb_scores(cache.head_dim ** -0.5 if scale is None else scale, softcap, window,
                        None if slopes is None else slopes.data_ptr())
     _check(lib().jb_attend(cache.pages.ref, cache.layer_refs[layer], ctypes.byref(scores), q.data_ptr(), qa, qb, heads,
-                           pr, pp, n, out.data_ptr(), oa, ob, ws.data_ptr(), nbytes, _stream(stream)))
+                           pr, pp, n, out.data_ptr(), oa, ob, ws.data_ptr(), ws.shape[0], _stream(stream)))
     return out
 
 

@@ -22,7 +22,7 @@ LIB = os.path.join(OUT_DIR, "libjb.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["jb_kernels.cu", "jb_q4.cu", "jb_attend.cu", "jb_pages.cu", "jb_sample.cu", "jb_capi.cpp",
            "jb_answer_capi.cpp"]
-HEADERS = ["jb_rng.cuh", "jb_internal.h", "jb_offgrid.h", "jb_answer.h", "jb_host.h"]
+HEADERS = ["jb_rng.cuh", "jb_internal.h", "jb_offgrid.h", "jb_answer.h", "jb_host.h", "jb_launch.cuh"]
 
 
 def nvcc() -> str:

@@ -3,9 +3,9 @@
 // A query reads each key and value of its row once and does 4 g operations per element with g
 // query heads to a key head, so the bytes bound it: the kernels stream pages from HBM and keep all
 // state in registers. Work is cut evenly whatever the rows' lengths: the 16-token groups of all
-// (query, key head) pairs are one line, every warp takes an equal stretch of it and works alone, and
-// pairs that cross a boundary are joined by a second kernel from partial (maximum, sum, weighted
-// values).
+// (query, key head) pairs are one line, every warp takes an equal stretch of it and works alone. A pair
+// that crosses a boundary is joined from partial (maximum, sum, weighted values) by the warp that
+// finishes last, eight parts at a time.
 //
 // Softmax is kept with a running maximum, so that one pass is enough:
 //   m' = max(m, max_t x_t), s' = s e^(m - m') + sum e^(x_t - m'), o' likewise.
@@ -14,6 +14,7 @@
 #include <cuda_bf16.h>
 
 #include "jb_answer.h"
+#include "jb_launch.cuh"
 
 namespace jb {
 namespace {
@@ -23,6 +24,8 @@ constexpr int kGroup = 16;         // tokens a warp takes at a time; pages hold 
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kMaxWorkers = 2048;  // warps of the persistent grid; the workspace has two slots for each
+constexpr int kRadix = 8;          // parts of a pair that are joined at a time
+constexpr int kLevels = 4;         // kRadix^kLevels >= kMaxWorkers
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.0e38f;
 
@@ -42,12 +45,6 @@ struct Params {
 // Partial results of a stretch: o[heads][D], m[heads], s[heads], for the query heads that are worked on
 // together.
 __host__ __device__ constexpr int slot_floats(int heads, int d) { return heads * (d + 2); }
-
-// Part `index` of a pair that is cut into `parts` stretches, the first of them worker `first`'s; parts = 0:
-// none. The first stretch is in its worker's slot 1, the others in their workers' slots 0.
-struct Cut {
-    int query, head, block, first, parts, index;
-};
 
 // Groups that query i reads: [first, first + groups), of tokens lo to pos.
 struct Span {
@@ -72,6 +69,7 @@ __device__ __forceinline__ Span span_of(const Params& p, int i) {
 // Groups [from, to) of a (query, key head, block of query heads).
 struct Stretch {
     int query, head, block, from, to;
+    long long begin;  // where the pair starts on the line
     Span span;
 };
 
@@ -82,18 +80,31 @@ __device__ __forceinline__ long long quotient(long long a, long long b) {
 
 static_assert(kMaxListed <= kThreads * kThreads, "a thread's run of queries");
 
-// Deals the line of groups out to the warps.
-struct Dealer {
-    long long next, end, total;
-    int workers, worker;
-    int query;
-    long long at;         // groups of the query before `next`
-    Span span;
+// The line of groups, and which warp has which of them.
+struct Line {
+    long long total;
+    int workers;
 
     __device__ long long bound(int w) const {
         const long long each = quotient(total, workers);
         return each * w + quotient((total - each * workers) * w, workers);
     }
+    __device__ int owner(long long x) const {
+        int w = static_cast<int>(quotient(x * workers, total));
+        while (bound(w) > x) --w;
+        while (bound(w + 1) <= x) ++w;
+        return w;
+    }
+};
+
+// Deals the line out.
+struct Dealer {
+    long long next, end;
+    Line line;
+    int worker;
+    int query;
+    long long at;         // groups of the query before `next`
+    Span span;
 
     // The CTA together. sums: kThreads + 1 words of shared memory; runs: kWarps.
     __device__ void start(const Params& p, long long* sums, int* runs) {
@@ -106,23 +117,23 @@ struct Dealer {
             if (i < n) mine += span_of(p, i).groups;
         }
         scan(mine, sums);
-        total = sums[kThreads] * pairs;
+        line.total = sums[kThreads] * pairs;
         // neighbours on the line are on different SMs, so that few stretches use all of them
         worker = warp * gridDim.x + blockIdx.x;
-        workers = static_cast<int>(min(static_cast<long long>(gridDim.x) * kWarps, max(1ll, total)));
+        line.workers = static_cast<int>(min(static_cast<long long>(gridDim.x) * kWarps, max(1ll, line.total)));
         next = end = 0;
-        if (total == 0) return;
+        if (line.total == 0) return;
         // the runs with the warps' first groups: groups before a query are multiples of `pairs`
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
             const int other = w * gridDim.x + blockIdx.x;
-            const long long goal = other < workers ? quotient(bound(other), pairs) : -1;
+            const long long goal = other < line.workers ? quotient(line.bound(other), pairs) : -1;
             if (sums[threadIdx.x] <= goal && goal < sums[threadIdx.x + 1]) runs[w] = threadIdx.x;
         }
         __syncthreads();
-        if (worker >= workers) return;
-        next = bound(worker);
-        end = bound(worker + 1);
+        if (worker >= line.workers) return;
+        next = line.bound(worker);
+        end = line.bound(worker + 1);
         const long long goal = quotient(next, pairs);
         long long base = sums[runs[warp]];
         query = runs[warp] * per;
@@ -182,28 +193,10 @@ struct Dealer {
         s.block = pair % p.blocks;
         s.from = static_cast<int>(at - static_cast<long long>(pair) * span.groups);
         s.to = static_cast<int>(min(static_cast<long long>(span.groups), s.from + (end - next)));
+        s.begin = next - s.from;
         next += s.to - s.from;
         at += s.to - s.from;
         return true;
-    }
-
-    // The worker with group x of the line.
-    __device__ int owner(long long x) const {
-        int w = static_cast<int>(quotient(x * workers, total));
-        while (bound(w) > x) --w;
-        while (bound(w + 1) <= x) ++w;
-        return w;
-    }
-
-    // How the last stretch taken is cut off at its end, if it is.
-    __device__ Cut cut(bool any, const Stretch& s) const {
-        Cut c = {0, 0, 0, 0, 0, 0};
-        if (!any || s.to == s.span.groups) return c;
-        const long long begin = next - s.to;
-        c = {s.query, s.head, s.block, owner(begin), 0, 0};
-        c.parts = owner(begin + s.span.groups - 1) - c.first + 1;
-        c.index = worker - c.first;
-        return c;
     }
 };
 
@@ -214,12 +207,14 @@ __device__ __forceinline__ void store_out<float>(float* to, float v) { *to = v; 
 template <>
 __device__ __forceinline__ void store_out<__nv_bfloat16>(__nv_bfloat16* to, float v) { *to = __float2bfloat16_rn(v); }
 
-__device__ __forceinline__ float* slot_of(const Params& p, int heads, int d, int worker, bool first) {
-    return p.a.ws + static_cast<size_t>(slot_floats(heads, d)) * (2 * worker + (first ? 1 : 0));
-}
-
-__device__ __forceinline__ Cut* cuts_of(const Params& p, int heads, int d) {
-    return reinterpret_cast<Cut*>(p.a.ws + static_cast<size_t>(slot_floats(heads, d)) * 2 * kMaxWorkers);
+// The workspace: a counter for each slot and level, zero between calls, then the slots. Part 0 of a pair
+// is in its worker's slot 1, the others in their workers' slots 0, so that a worker's end of one pair
+// and start of the next do not meet.
+__host__ __device__ constexpr size_t counters() { return static_cast<size_t>(kLevels) * 2 * kMaxWorkers; }
+static_assert(counters() * 4 == 65536, "what jb.h says of the workspace");
+__device__ __forceinline__ int slot_index(int first, int part) { return 2 * (first + part) + (part == 0 ? 1 : 0); }
+__device__ __forceinline__ float* slot_of(const Params& p, int heads, int d, int index) {
+    return p.a.ws + counters() + static_cast<size_t>(slot_floats(heads, d)) * index;
 }
 
 // Zeros for the queries that see nothing.
@@ -230,6 +225,83 @@ __device__ __forceinline__ void write_zeros(const Params& p) {
         if (span_of(p, i).groups > 0) continue;
         for (int u = threadIdx.x; u < heads * d; u += kThreads)
             store_out(reinterpret_cast<T*>(p.a.out) + i * p.a.out_row + u / d * p.a.out_head + u % d, 0.0f);
+    }
+}
+
+// A stretch's part is in its slot. The warp that hands in the last of eight parts joins them, and so on
+// up to the whole pair, which it stores. The order of the sums is that of the line, whoever joins.
+template <typename T, int D, int kH>
+__device__ __noinline__ void hand_in(const Params& p, Line line, int worker, long long begin, int groups, int query, int head, int block) {
+    const int lane = threadIdx.x & 31;
+    const int heads_here = min(kH, p.a.group - block * kH), d = p.a.head_dim;
+    const int first = line.owner(begin);
+    int index = worker - first, count = line.owner(begin + groups - 1) - first + 1;
+    int* counter = reinterpret_cast<int*>(p.a.ws);
+    for (int reach = 1;; reach *= kRadix, counter += 2 * kMaxWorkers) {  // a part stands for `reach` stretches
+        const int team = index / kRadix, members = min(kRadix, count - team * kRadix);
+        const int base = slot_index(first, team * kRadix * reach);
+        if (members > 1) {
+            __threadfence();
+            __syncwarp();
+            int before = 0;
+            if (lane == 0) before = atomicAdd(&counter[base], 1);
+            before = __shfl_sync(kAll, before, 0);
+            if (before + 1 < members) return;
+            if (lane == 0) counter[base] = 0;
+            __threadfence();
+            const auto slot = [&](int i) { return slot_of(p, kH, D, slot_index(first, (team * kRadix + i) * reach)); };
+            // lane h: head h's maximum and sum
+            float m = kLowest, l = 0.0f;
+            if (lane < heads_here) {
+                float mi[kRadix], li[kRadix];
+#pragma unroll
+                for (int i = 0; i < kRadix; ++i) {
+                    mi[i] = i < members ? __ldcg(slot(i) + kH * D + lane) : kLowest;
+                    li[i] = i < members ? __ldcg(slot(i) + kH * D + kH + lane) : 0.0f;
+                }
+#pragma unroll
+                for (int i = 0; i < kRadix; ++i) m = fmaxf(m, mi[i]);
+#pragma unroll
+                for (int i = 0; i < kRadix; ++i) l = fmaf(exp2_approx(mi[i] - m), li[i], l);
+            }
+            const bool last = count <= kRadix;
+            const float inverse = l > 0.0f ? 1.0f / l : 0.0f;
+            for (int from = 0; from < heads_here * D; from += 128) {
+                const int e = from + 4 * lane, h = min(e / D, heads_here - 1);
+                const float top = __shfl_sync(kAll, m, h), scale = __shfl_sync(kAll, inverse, h);
+                if (e >= heads_here * D) continue;
+                float4 x[kRadix];
+                float f[kRadix];
+#pragma unroll
+                for (int i = 0; i < kRadix; ++i) {
+                    x[i] = i < members ? __ldcg(reinterpret_cast<const float4*>(slot(i) + e)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    f[i] = i < members ? __ldcg(slot(i) + kH * D + h) : kLowest;
+                }
+                float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                for (int i = 0; i < kRadix; ++i) {
+                    const float k = exp2_approx(f[i] - top);
+                    o = make_float4(fmaf(k, x[i].x, o.x), fmaf(k, x[i].y, o.y), fmaf(k, x[i].z, o.z), fmaf(k, x[i].w, o.w));
+                }
+                if (!last) {
+                    *reinterpret_cast<float4*>(slot(0) + e) = o;
+                } else if (e % D < d) {
+                    T* out = reinterpret_cast<T*>(p.a.out) + query * p.a.out_row + (head * p.a.group + block * kH + h) * p.a.out_head + e % D;
+                    store_out(out, o.x * scale);
+                    store_out(out + 1, o.y * scale);
+                    store_out(out + 2, o.z * scale);
+                    store_out(out + 3, o.w * scale);
+                }
+            }
+            if (last) return;
+            __syncwarp();  // the parts' maxima are read until here
+            if (lane < heads_here) {
+                slot(0)[kH * D + lane] = m;
+                slot(0)[kH * D + kH + lane] = l;
+            }
+        }
+        index = team;
+        count = (count + kRadix - 1) / kRadix;
     }
 }
 
@@ -383,10 +455,12 @@ __global__ void __launch_bounds__(kThreads, kBf16Ctas<D, kH>) attend_bf16_kernel
     const uint32_t k_row = feed.ring + (8 * (lane >> 4) + (lane & 7)) * Feed<T, D>::kRowBytes, k_piece = (lane >> 3) & 1;
     const uint32_t v_row = feed.ring + Feed<T, D>::kGroupBytes + (8 * ((lane >> 3) & 1) + (lane & 7)) * Feed<T, D>::kRowBytes, v_piece = lane >> 4;
 
+    after_previous();
+    let_next_start();
     Dealer deal;
     deal.start(p, sums, runs);
     Stretch s, after;
-    bool any = deal.take(p, s), more = any;
+    bool more = deal.take(p, s);
     if (more) feed.open(p, s);
     while (more) {
         const int heads_here = min(kH, p.a.group - s.block * kH);
@@ -496,7 +570,7 @@ __global__ void __launch_bounds__(kThreads, kBf16Ctas<D, kH>) attend_bf16_kernel
                          (after.head * p.a.group + min(after.block * kH + r, p.a.group - 1)) * p.a.q_head + min(64 * c, d - 8));
         }
         const bool whole = s.from == 0 && s.to == s.span.groups;
-        float* slot = slot_of(p, kH, D, deal.worker, s.from == 0);
+        float* slot = slot_of(p, kH, D, 2 * deal.worker + (s.from == 0 ? 1 : 0));
 #pragma unroll
         for (int h = 0; h < kR; ++h) {
             l[h] += __shfl_xor_sync(kAll, l[h], 1);
@@ -519,10 +593,10 @@ __global__ void __launch_bounds__(kThreads, kBf16Ctas<D, kH>) attend_bf16_kernel
                 slot[kH * D + kH + r + 8 * h] = l[h];
             }
         }
+        if (!whole) hand_in<T, D, kH>(p, deal.line, deal.worker, s.begin, s.span.groups, s.query, s.head, s.block);
         if (!more) break;
         s = after;
     }
-    if (lane == 0) cuts_of(p, kH, D)[warp * gridDim.x + blockIdx.x] = deal.cut(any, s);
     write_zeros<T>(p);
 }
 
@@ -555,10 +629,12 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const
     Feed<float, D> feed;
     feed.ring = static_cast<uint32_t>(__cvta_generic_to_shared(mine));
 
+    after_previous();
+    let_next_start();
     Dealer deal;
     deal.start(p, sums, runs);
     Stretch s, after;
-    bool any = deal.take(p, s), more = any;
+    bool more = deal.take(p, s);
     if (more) feed.open(p, s);
     while (more) {
         const int heads_here = min(kH, p.a.group - s.block * kH);
@@ -654,7 +730,7 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const
         more = deal.take(p, after);
         if (more) feed.open(p, after);
         const bool whole = s.from == 0 && s.to == s.span.groups;
-        float* slot = slot_of(p, kF32Heads, D, deal.worker, s.from == 0);
+        float* slot = slot_of(p, kF32Heads, D, 2 * deal.worker + (s.from == 0 ? 1 : 0));
 #pragma unroll
         for (int h = 0; h < kH; ++h) {
 #pragma unroll
@@ -677,64 +753,12 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const
                 slot[kF32Heads * D + kF32Heads + h] = l[h];
             }
         }
+        if (!whole) hand_in<T, D, kF32Heads>(p, deal.line, deal.worker, s.begin, s.span.groups, s.query, s.head, s.block);
         if (!more) break;
         s = after;
         __syncwarp();
     }
-    if (lane == 0) cuts_of(p, kF32Heads, D)[warp * gridDim.x + blockIdx.x] = deal.cut(any, s);
     write_zeros<float>(p);
-}
-
-// Joins the parts of cut pairs in the order of the line. Every worker whose last stretch is cut off has a
-// CTA here; those of one pair share its elements: all by one, or an 8th or a 64th each. With fewer
-// elements than threads, groups of threads take every so many parts and are added up at the end.
-template <typename T, int D, int kH>
-__global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ Params p) {
-    const Cut u = cuts_of(p, kH, D)[blockIdx.x];
-    const int slices = u.parts > 64 ? 64 : u.parts > 8 ? 8 : 1;
-    if (u.parts == 0 || u.index >= slices) return;
-    __shared__ float4 sums[kThreads];
-    __shared__ float2 stats[kThreads];
-    const int heads_here = min(kH, p.a.group - u.block * kH), d = p.a.head_dim;
-    const int quads = kH * D / 4 / slices, lanes = min(quads, kThreads), teams = kThreads / lanes;
-    const int lane = threadIdx.x % lanes, team = threadIdx.x / lanes;
-    for (int first = u.index * quads; first < (u.index + 1) * quads; first += lanes) {
-        const int e = 4 * (first + lane), h = e / D;
-        float m = kLowest, l = 0.0f;
-        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (h < heads_here) {
-#pragma unroll 4
-            for (int i = team; i < u.parts; i += teams) {
-                const float* f = slot_of(p, kH, D, u.first + i, i == 0);
-                const float mi = f[kH * D + h], li = f[kH * D + kH + h];
-                const float4 x = *reinterpret_cast<const float4*>(f + e);
-                const float high = fmaxf(m, mi), a = exp2_approx(m - high), b = exp2_approx(mi - high);
-                m = high;
-                l = fmaf(b, li, a * l);
-                o = make_float4(fmaf(b, x.x, a * o.x), fmaf(b, x.y, a * o.y), fmaf(b, x.z, a * o.z), fmaf(b, x.w, a * o.w));
-            }
-        }
-        sums[threadIdx.x] = o;
-        stats[threadIdx.x] = make_float2(m, l);
-        __syncthreads();
-        if (team == 0 && h < heads_here && e % D < d) {
-            for (int i = 1; i < teams; ++i) {
-                const float4 x = sums[i * lanes + lane];
-                const float2 t = stats[i * lanes + lane];
-                const float high = fmaxf(m, t.x), a = exp2_approx(m - high), b = exp2_approx(t.x - high);
-                m = high;
-                l = fmaf(b, t.y, a * l);
-                o = make_float4(fmaf(b, x.x, a * o.x), fmaf(b, x.y, a * o.y), fmaf(b, x.z, a * o.z), fmaf(b, x.w, a * o.w));
-            }
-            const float inverse = l > 0.0f ? 1.0f / l : 0.0f;
-            T* out = reinterpret_cast<T*>(p.a.out) + u.query * p.a.out_row + (u.head * p.a.group + u.block * kH + h) * p.a.out_head + e % D;
-            store_out(out, o.x * inverse);
-            store_out(out + 1, o.y * inverse);
-            store_out(out + 2, o.z * inverse);
-            store_out(out + 3, o.w * inverse);
-        }
-        __syncthreads();
-    }
 }
 
 // SMs of a device and CTAs of a kernel on one, asked for once.
@@ -757,16 +781,11 @@ cudaError_t resident(int shared, int& ctas) {
     return cudaSuccess;
 }
 
-template <auto kKernel, auto kJoin>
-cudaError_t launch_both(int shared, const Params& p, cudaStream_t s) {
+template <auto kKernel>
+cudaError_t launch_resident(int shared, const Params& p, cudaStream_t s) {
     int ctas = 0;
-    cudaError_t e = resident<kKernel>(shared, ctas);
-    if (e != cudaSuccess) return e;
-    kKernel<<<ctas, kThreads, shared, s>>>(p);
-    e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
-    kJoin<<<ctas * kWarps, kThreads, 0, s>>>(p);
-    return cudaGetLastError();
+    const cudaError_t e = resident<kKernel>(shared, ctas);
+    return e != cudaSuccess ? e : launch(kKernel, ctas, kThreads, shared, 0, s, p);
 }
 
 template <int D, int kH>
@@ -774,14 +793,14 @@ cudaError_t launch_bf16(Params p, cudaStream_t s) {
     constexpr int shared = kWarps * Feed<__nv_bfloat16, D>::kRing;
     p.blocks = (p.a.group + kH - 1) / kH;
     return p.a.softcap > 0.0f || p.a.slopes != nullptr
-               ? launch_both<attend_bf16_kernel<D, kH, true>, join_kernel<__nv_bfloat16, D, kH>>(shared, p, s)
-               : launch_both<attend_bf16_kernel<D, kH, false>, join_kernel<__nv_bfloat16, D, kH>>(shared, p, s);
+               ? launch_resident<attend_bf16_kernel<D, kH, true>>(shared, p, s)
+               : launch_resident<attend_bf16_kernel<D, kH, false>>(shared, p, s);
 }
 
 template <int D, int kH>
 cudaError_t launch_f32(Params p, cudaStream_t s) {
     p.blocks = (p.a.group + kH - 1) / kH;
-    return launch_both<attend_f32_kernel<D, kH>, join_kernel<float, D, kF32Heads>>(kWarps * F32Shape<D, kH>::kWarpBytes, p, s);
+    return launch_resident<attend_f32_kernel<D, kH>>(kWarps * F32Shape<D, kH>::kWarpBytes, p, s);
 }
 
 template <int D>
@@ -797,7 +816,7 @@ int padded(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 
 
 uint64_t attend_workspace(int bf16, int, int group, int head_dim) {
     const int heads = bf16 && group > 8 ? 16 : 8;
-    return kMaxWorkers * (2ull * slot_floats(heads, padded(head_dim)) * sizeof(float) + sizeof(Cut));
+    return sizeof(float) * (counters() + 2ull * kMaxWorkers * slot_floats(heads, padded(head_dim)));
 }
 
 cudaError_t launch_attend(const Pages& pages, const Attend& a, cudaStream_t s) {
