@@ -24,8 +24,8 @@ constexpr int kGroup = 16;         // tokens a warp takes at a time; pages hold 
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kMaxWorkers = 2048;  // warps of the persistent grid; the workspace has two slots for each
-constexpr int kRadix = 8;          // parts of a pair that are joined at a time
-constexpr int kLevels = 4;         // kRadix^kLevels >= kMaxWorkers
+constexpr int kLevels = 4;         // of joining eight parts of a pair at a time: 8^4 >= kMaxWorkers
+constexpr int kLeast = 4;          // groups of a stretch, where that leaves one to each CTA
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.0e38f;
 
@@ -80,20 +80,15 @@ __device__ __forceinline__ long long quotient(long long a, long long b) {
 
 static_assert(kMaxListed <= kThreads * kThreads, "a thread's run of queries");
 
-// The line of groups, and which warp has which of them.
+// The line of groups, and which warp has which of them: `each`, and the first `extra` warps one more.
 struct Line {
-    long long total;
-    int workers;
+    long long total, each;
+    int workers, extra;
 
-    __device__ long long bound(int w) const {
-        const long long each = quotient(total, workers);
-        return each * w + quotient((total - each * workers) * w, workers);
-    }
+    __device__ long long bound(int w) const { return each * w + min(w, extra); }
     __device__ int owner(long long x) const {
-        int w = static_cast<int>(quotient(x * workers, total));
-        while (bound(w) > x) --w;
-        while (bound(w + 1) <= x) ++w;
-        return w;
+        const long long longer = (each + 1) * extra;
+        return x < longer ? static_cast<int>(quotient(x, each + 1)) : extra + static_cast<int>(quotient(x - longer, each));
     }
 };
 
@@ -106,8 +101,8 @@ struct Dealer {
     long long at;         // groups of the query before `next`
     Span span;
 
-    // The CTA together. sums: kThreads + 1 words of shared memory; runs: kWarps.
-    __device__ void start(const Params& p, long long* sums, int* runs) {
+    // The CTA together. sums: kThreads + 1 words of shared memory.
+    __device__ void start(const Params& p, long long* sums) {
         const int n = p.a.n, pairs = p.a.heads * p.blocks, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         const int per = (n + kThreads - 1) / kThreads;
         // groups of each thread's run of queries
@@ -120,24 +115,27 @@ struct Dealer {
         line.total = sums[kThreads] * pairs;
         // neighbours on the line are on different SMs, so that few stretches use all of them
         worker = warp * gridDim.x + blockIdx.x;
-        line.workers = static_cast<int>(min(static_cast<long long>(gridDim.x) * kWarps, max(1ll, line.total)));
+        // few groups: one to a warp on every SM, then kLeast before the next warps get some (one row of 2048
+        // tokens, 32 heads: 16.9 us with one group a warp, 13.4 with four)
+        line.workers = static_cast<int>(min(static_cast<long long>(gridDim.x) * kWarps,
+                                            max(min(max(1ll, line.total), static_cast<long long>(gridDim.x)), line.total / kLeast)));
         next = end = 0;
-        if (line.total == 0) return;
-        // the runs with the warps' first groups: groups before a query are multiples of `pairs`
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            const int other = w * gridDim.x + blockIdx.x;
-            const long long goal = other < line.workers ? quotient(line.bound(other), pairs) : -1;
-            if (sums[threadIdx.x] <= goal && goal < sums[threadIdx.x + 1]) runs[w] = threadIdx.x;
-        }
-        __syncthreads();
-        if (worker >= line.workers) return;
+        if (worker >= line.workers || line.total == 0) return;
+        line.each = quotient(line.total, line.workers);
+        line.extra = static_cast<int>(line.total - line.each * line.workers);
         next = line.bound(worker);
         end = line.bound(worker + 1);
+        // the run with the warp's first group: groups before a query are multiples of `pairs`
         const long long goal = quotient(next, pairs);
-        long long base = sums[runs[warp]];
-        query = runs[warp] * per;
-        for (int k = 0; k < per; k += 32) {  // and the query within the run
+        int run = 0;
+#pragma unroll
+        for (int k = 0; k < kThreads; k += 32) {
+            const unsigned here = __ballot_sync(kAll, sums[k + lane] <= goal && goal < sums[k + lane + 1]);
+            if (here != 0) run = k + __ffs(here) - 1;
+        }
+        long long base = sums[run];
+        query = run * per;
+        for (int k = 0; per > 1 && k < per; k += 32) {  // and the query within the run
             const int i = query + lane;
             const int g = k + lane < per && i < n ? span_of(p, i).groups : 0;
             int in = g;
@@ -228,73 +226,81 @@ __device__ __forceinline__ void write_zeros(const Params& p) {
     }
 }
 
-// A stretch's part is in its slot. The warp that hands in the last of eight parts joins them, and so on
-// up to the whole pair, which it stores. The order of the sums is that of the line, whoever joins.
-template <typename T, int D, int kH>
-__device__ __noinline__ void hand_in(const Params& p, Line line, int worker, long long begin, int groups, int query, int head, int block) {
+// A stretch's part is in its slot. The warp that hands in the last of kRadix parts joins them, and so on
+// up to the whole pair, which it stores. The order of the sums is that of the line, whoever joins. A
+// join is a chain of waits on L2, so its loads are issued together, kDeep float4 of each part at a time.
+template <typename T, int D, int kH, int kRadix, int kDeep>
+__device__ __forceinline__ void join_up(const Params& p, int first, int index, int count, int query, int head, int block) {
     const int lane = threadIdx.x & 31;
     const int heads_here = min(kH, p.a.group - block * kH), d = p.a.head_dim;
-    const int first = line.owner(begin);
-    int index = worker - first, count = line.owner(begin + groups - 1) - first + 1;
     int* counter = reinterpret_cast<int*>(p.a.ws);
     for (int reach = 1;; reach *= kRadix, counter += 2 * kMaxWorkers) {  // a part stands for `reach` stretches
         const int team = index / kRadix, members = min(kRadix, count - team * kRadix);
-        const int base = slot_index(first, team * kRadix * reach);
         if (members > 1) {
-            __threadfence();
+            const int base = slot_index(first, team * kRadix * reach);
             __syncwarp();
             int before = 0;
-            if (lane == 0) before = atomicAdd(&counter[base], 1);
+            if (lane == 0) {
+                __threadfence();
+                before = atomicAdd(&counter[base], 1);
+                __threadfence();
+            }
             before = __shfl_sync(kAll, before, 0);
             if (before + 1 < members) return;
             if (lane == 0) counter[base] = 0;
-            __threadfence();
-            const auto slot = [&](int i) { return slot_of(p, kH, D, slot_index(first, (team * kRadix + i) * reach)); };
-            // lane h: head h's maximum and sum
-            float m = kLowest, l = 0.0f;
-            if (lane < heads_here) {
-                float mi[kRadix], li[kRadix];
-#pragma unroll
-                for (int i = 0; i < kRadix; ++i) {
-                    mi[i] = i < members ? __ldcg(slot(i) + kH * D + lane) : kLowest;
-                    li[i] = i < members ? __ldcg(slot(i) + kH * D + kH + lane) : 0.0f;
-                }
-#pragma unroll
-                for (int i = 0; i < kRadix; ++i) m = fmaxf(m, mi[i]);
-#pragma unroll
-                for (int i = 0; i < kRadix; ++i) l = fmaf(exp2_approx(mi[i] - m), li[i], l);
-            }
             const bool last = count <= kRadix;
-            const float inverse = l > 0.0f ? 1.0f / l : 0.0f;
-            for (int from = 0; from < heads_here * D; from += 128) {
-                const int e = from + 4 * lane, h = min(e / D, heads_here - 1);
-                const float top = __shfl_sync(kAll, m, h), scale = __shfl_sync(kAll, inverse, h);
-                if (e >= heads_here * D) continue;
-                float4 x[kRadix];
-                float f[kRadix];
+            const auto slot = [&](int i) { return slot_of(p, kH, D, slot_index(first, (team * kRadix + i) * reach)); };
+            // lane h: head h's maxima and sums
+            float f[kRadix], li[kRadix], m = kLowest, l = 0.0f, inverse = 0.0f;
 #pragma unroll
-                for (int i = 0; i < kRadix; ++i) {
-                    x[i] = i < members ? __ldcg(reinterpret_cast<const float4*>(slot(i) + e)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    f[i] = i < members ? __ldcg(slot(i) + kH * D + h) : kLowest;
-                }
-                float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            for (int i = 0; i < kRadix; ++i) {
+                const bool real = i < members && lane < heads_here;
+                f[i] = real ? __ldcg(slot(i) + kH * D + lane) : kLowest;
+                li[i] = real ? __ldcg(slot(i) + kH * D + kH + lane) : 0.0f;
+            }
+            for (int from = 0; from < heads_here * D; from += 128 * kDeep) {
+                float4 x[kDeep][kRadix];
 #pragma unroll
-                for (int i = 0; i < kRadix; ++i) {
-                    const float k = exp2_approx(f[i] - top);
-                    o = make_float4(fmaf(k, x[i].x, o.x), fmaf(k, x[i].y, o.y), fmaf(k, x[i].z, o.z), fmaf(k, x[i].w, o.w));
+                for (int j = 0; j < kDeep; ++j) {
+                    const int e = from + 128 * j + 4 * lane;
+#pragma unroll
+                    for (int i = 0; i < kRadix; ++i)
+                        x[j][i] = i < members && e < heads_here * D ? __ldcg(reinterpret_cast<const float4*>(slot(i) + e))
+                                                                    : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                 }
-                if (!last) {
-                    *reinterpret_cast<float4*>(slot(0) + e) = o;
-                } else if (e % D < d) {
-                    T* out = reinterpret_cast<T*>(p.a.out) + query * p.a.out_row + (head * p.a.group + block * kH + h) * p.a.out_head + e % D;
-                    store_out(out, o.x * scale);
-                    store_out(out + 1, o.y * scale);
-                    store_out(out + 2, o.z * scale);
-                    store_out(out + 3, o.w * scale);
+                if (from == 0) {
+#pragma unroll
+                    for (int i = 0; i < kRadix; ++i) m = fmaxf(m, f[i]);
+#pragma unroll
+                    for (int i = 0; i < kRadix; ++i) {
+                        f[i] = exp2_approx(f[i] - m);
+                        l = fmaf(f[i], li[i], l);
+                    }
+                    inverse = l > 0.0f ? 1.0f / l : 0.0f;
+                }
+#pragma unroll
+                for (int j = 0; j < kDeep; ++j) {
+                    const int e = from + 128 * j + 4 * lane, h = min(e / D, heads_here - 1);
+                    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                    for (int i = 0; i < kRadix; ++i) {
+                        const float k = __shfl_sync(kAll, f[i], h);
+                        o = make_float4(fmaf(k, x[j][i].x, o.x), fmaf(k, x[j][i].y, o.y), fmaf(k, x[j][i].z, o.z), fmaf(k, x[j][i].w, o.w));
+                    }
+                    const float scale = __shfl_sync(kAll, inverse, h);
+                    if (e >= heads_here * D) continue;
+                    if (!last) {
+                        *reinterpret_cast<float4*>(slot(0) + e) = o;
+                    } else if (e % D < d) {
+                        T* out = reinterpret_cast<T*>(p.a.out) + query * p.a.out_row + (head * p.a.group + block * kH + h) * p.a.out_head + e % D;
+                        store_out(out, o.x * scale);
+                        store_out(out + 1, o.y * scale);
+                        store_out(out + 2, o.z * scale);
+                        store_out(out + 3, o.w * scale);
+                    }
                 }
             }
             if (last) return;
-            __syncwarp();  // the parts' maxima are read until here
             if (lane < heads_here) {
                 slot(0)[kH * D + lane] = m;
                 slot(0)[kH * D + kH + lane] = l;
@@ -302,6 +308,30 @@ __device__ __noinline__ void hand_in(const Params& p, Line line, int worker, lon
         }
         index = team;
         count = (count + kRadix - 1) / kRadix;
+    }
+}
+
+// A warp has at most two pairs that are cut: its first and its last. They are noted here, and handed in
+// when the warp has nothing else to do (and the registers of its products are free).
+struct Noted {
+    int query, head, block, first, count;
+};
+
+__device__ __forceinline__ void note(Noted& to, const Dealer& deal, const Stretch& s) {
+    const int first = deal.line.owner(s.begin), last = deal.line.owner(s.begin + s.span.groups - 1);
+    if ((threadIdx.x & 31) == 0) to = {s.query, s.head, s.block, first, last - first + 1};
+}
+
+template <typename T, int D, int kH>
+__device__ __forceinline__ void hand_in(const Params& p, const Noted* noted, int n, int worker) {
+    __syncwarp();
+    for (int i = 0; i < n; ++i) {
+        const Noted c = noted[i];
+        // parts of one float4 a lane are joined 16 at a time, longer ones 8 at a time
+        if (min(kH, p.a.group - c.block * kH) * D <= 128)
+            join_up<T, D, kH, 16, 1>(p, c.first, worker - c.first, c.count, c.query, c.head, c.block);
+        else
+            join_up<T, D, kH, 8, D == 64 ? 2 : 4>(p, c.first, worker - c.first, c.count, c.query, c.head, c.block);
     }
 }
 
@@ -446,7 +476,7 @@ __global__ void __launch_bounds__(kThreads, kBf16Ctas<D, kH>) attend_bf16_kernel
     constexpr int kS = D / 16, kPieces = D / 8, kR = kH / 8;
     extern __shared__ __align__(128) char dynamic[];
     __shared__ long long sums[kThreads + 1];
-    __shared__ int runs[kWarps];
+    __shared__ Noted noted[kWarps][2];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
     const int d = p.a.head_dim;
     Feed<T, D> feed;
@@ -458,9 +488,10 @@ __global__ void __launch_bounds__(kThreads, kBf16Ctas<D, kH>) attend_bf16_kernel
     after_previous();
     let_next_start();
     Dealer deal;
-    deal.start(p, sums, runs);
+    deal.start(p, sums);
     Stretch s, after;
     bool more = deal.take(p, s);
+    int cuts = 0;
     if (more) feed.open(p, s);
     while (more) {
         const int heads_here = min(kH, p.a.group - s.block * kH);
@@ -593,10 +624,11 @@ __global__ void __launch_bounds__(kThreads, kBf16Ctas<D, kH>) attend_bf16_kernel
                 slot[kH * D + kH + r + 8 * h] = l[h];
             }
         }
-        if (!whole) hand_in<T, D, kH>(p, deal.line, deal.worker, s.begin, s.span.groups, s.query, s.head, s.block);
+        if (!whole) note(noted[warp][cuts++], deal, s);
         if (!more) break;
         s = after;
     }
+    hand_in<T, D, kH>(p, noted[warp], cuts, deal.worker);
     write_zeros<T>(p);
 }
 
@@ -620,7 +652,7 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const
     constexpr int kPieces = D / 4, kV = (D + 127) / 128;  // pieces of the values that a lane takes
     extern __shared__ __align__(128) char dynamic[];
     __shared__ long long sums[kThreads + 1];
-    __shared__ int runs[kWarps];
+    __shared__ Noted noted[kWarps][2];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, token = lane & 15, half = lane >> 4;
     const int d = p.a.head_dim;
     char* mine = dynamic + warp * Shape::kWarpBytes;
@@ -632,9 +664,10 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const
     after_previous();
     let_next_start();
     Dealer deal;
-    deal.start(p, sums, runs);
+    deal.start(p, sums);
     Stretch s, after;
     bool more = deal.take(p, s);
+    int cuts = 0;
     if (more) feed.open(p, s);
     while (more) {
         const int heads_here = min(kH, p.a.group - s.block * kH);
@@ -753,12 +786,13 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const
                 slot[kF32Heads * D + kF32Heads + h] = l[h];
             }
         }
-        if (!whole) hand_in<T, D, kF32Heads>(p, deal.line, deal.worker, s.begin, s.span.groups, s.query, s.head, s.block);
+        if (!whole) note(noted[warp][cuts++], deal, s);
         if (!more) break;
         s = after;
         __syncwarp();
     }
-    write_zeros<float>(p);
+    hand_in<T, D, kF32Heads>(p, noted[warp], cuts, deal.worker);
+    write_zeros<T>(p);
 }
 
 // SMs of a device and CTAs of a kernel on one, asked for once.
