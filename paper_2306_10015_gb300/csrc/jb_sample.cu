@@ -12,6 +12,7 @@
 #include <cuda_bf16.h>
 
 #include "jb_answer.h"
+#include "jb_launch.cuh"
 
 namespace jb {
 namespace {
@@ -19,9 +20,11 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr unsigned kAll = 0xFFFFFFFFu;
-constexpr int kBins = 2048;
+constexpr int kIndexBins = 1024;       // bins of an index, 2^18 tokens at most
 constexpr int kMaxCluster = 8;
 constexpr int kMaxSlice = 65536;       // tokens of one CTA: sums of halves of their weights fit 32 bits
+constexpr int kLarge = 512;            // threads of a CTA, 256 for small vocabularies
+constexpr int kSmallVocab = 8192;
 constexpr float kReach = 21.5f;        // weights round to 0 below y = -31 ln 2 = -21.49
 constexpr float kOne = 1073741824.0f;  // 2^30, the weight of the largest logit
 typedef unsigned long long u64;
@@ -38,45 +41,40 @@ __device__ __forceinline__ float logit_of(uint32_t key) {
     return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
 }
 
-struct Row {
-    uint32_t top;   // key of the largest logit
-    float high;     // the largest logit
-    float inverse;  // 1 / temperature
-
-    __device__ float scaled(uint32_t key) const { return key == top ? 0.0f : (logit_of(key) - high) * inverse; }
-    __device__ uint32_t weight(uint32_t key) const {
-        return key <= kNothing ? 0 : __float2uint_rn(expf(scaled(key)) * kOne);
-    }
-};
-
-template <typename T>
-__device__ __forceinline__ uint32_t load_key(const T* p);
-template <>
-__device__ __forceinline__ uint32_t load_key<float>(const float* p) { return key_of(*p); }
-template <>
-__device__ __forceinline__ uint32_t load_key<__nv_bfloat16>(const __nv_bfloat16* p) { return key_of(__bfloat162float(*p)); }
-
-// Eight tokens at a time. Past the end: key 0, which weighs nothing.
+// Eight logits at a time; NaN past the end. In a row whose largest logit is +inf those stand for 0 and all
+// others for -inf.
 constexpr int kUnit = 8;
 template <typename T>
-__device__ __forceinline__ void load_unit(const T* row, int j, int vocab, bool wide, uint32_t (&key)[kUnit]) {
+__device__ __forceinline__ void load_unit(const T* row, int j, int vocab, bool wide, bool infinite, float (&x)[kUnit]) {
     if (wide && j + kUnit <= vocab) {
         if constexpr (sizeof(T) == 2) {
             const uint4 v = *reinterpret_cast<const uint4*>(row + j);
             const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int i = 0; i < kUnit; ++i) key[i] = key_of(__uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16));
+            for (int i = 0; i < kUnit; ++i) x[i] = __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
         } else {
             const float4 a = *reinterpret_cast<const float4*>(row + j), b = *reinterpret_cast<const float4*>(row + j + 4);
-            const float f[kUnit] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-            for (int i = 0; i < kUnit; ++i) key[i] = key_of(f[i]);
+            x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < kUnit; ++i) key[i] = j + i < vocab ? load_key(row + j + i) : 0;
+        for (int i = 0; i < kUnit; ++i) x[i] = j + i < vocab ? static_cast<float>(row[j + i]) : NAN;
+    }
+    if (infinite) {
+#pragma unroll
+        for (int i = 0; i < kUnit; ++i) x[i] = x[i] == INFINITY ? 0.0f : -INFINITY;
     }
 }
+
+struct Row {
+    float top;      // the largest logit
+    float inverse;  // 1 / temperature
+
+    // NaN stays NaN, and weighs 0
+    __device__ float scaled(float x) const { return (x - top) * inverse; }
+    __device__ static uint32_t weight_of(float y) { return __float2uint_rn(expf(y) * kOne); }
+    __device__ uint32_t weight(float x) const { return weight_of(scaled(x)); }
+};
 
 template <typename V>
 __device__ __forceinline__ V warp_inclusive(V v) {
@@ -103,6 +101,12 @@ __device__ __forceinline__ V block_exclusive(V v, V* sums, V& total) {
     return in - v + (warp == 0 ? V(0) : before);
 }
 
+// Adds to to[at] in shared memory without a branch.
+__device__ __forceinline__ void add_if(bool really, uint32_t* to, uint32_t at, uint32_t v) {
+    const uint32_t p = static_cast<uint32_t>(__cvta_generic_to_shared(to)) + 4 * at;
+    asm volatile("{.reg .pred p; setp.ne.u32 p, %2, 0; @p red.shared.add.u32 [%0], %1;}" ::"r"(p), "r"(v), "r"(really ? 1 : 0) : "memory");
+}
+
 // A token's place in the order as a number: larger comes first.
 __device__ __forceinline__ u64 place_of(uint32_t key, uint32_t index) { return static_cast<u64>(key) << 32 | ~index; }
 
@@ -111,6 +115,7 @@ enum Bins { kByScore, kByKey, kByIndex };
 struct Among {
     u64 first, last;
     Bins bins;
+    float scale;   // bins for each unit of y (kByScore)
     uint32_t key;  // the largest key (kByKey)
     int shift;     // bits of key or index within a bin
 };
@@ -137,65 +142,121 @@ __device__ __forceinline__ u64 share_of(double share, u64 mass) {
 
 template <int kThreads>
 struct Shared {
+    static constexpr int kBins = 4 * kThreads;
     uint32_t count[kBins], low[kBins], high[kBins];  // tokens, and their weights' halves
     u64 list[kThreads], order[kThreads];             // tokens of the bin; in the first CTA, in order
     u64 sums[32];
     int counts[32];
-    u64 best;
-    int total_count, listed;
-    u64 total_mass;
-    uint32_t least, most;  // keys of the bin's tokens
+    float top;
+    int total_count, listed, index;
+    u64 total_mass, beyond;                          // beyond: weight of what no bin holds
+    uint32_t least, most;                            // keys of the bin's tokens
     Crossing crossing;
     u64 cut, cut_mass;
 };
 
 template <typename T, int kThreads>
 struct Draw {
-    static constexpr int kWarps = kThreads / 32;
+    static constexpr int kWarps = kThreads / 32, kBins = Shared<kThreads>::kBins;
+    static_assert(kBins >= kIndexBins);
     const T* row;
     int vocab, rank, ctas, from, to;  // units of this warp
-    bool wide;
+    bool wide, infinite;
     Row r;
     Shared<kThreads>& sh;
     cg::cluster_group cluster;
 
     __device__ __forceinline__ Shared<kThreads>& of(int cta) { return *cluster.map_shared_rank(&sh, cta); }
 
-    // f(key, index) for the warp's tokens, a thread's indices ascending.
+    __device__ __forceinline__ void sync() {
+        if (ctas > 1) cluster.sync();
+        else __syncthreads();
+    }
+
+    // f(logits, first index) for the warp's units, a thread's indices ascending.
     template <typename F>
-    __device__ __forceinline__ void each(F f) {
+    __device__ __forceinline__ void each_unit(F f) {
         for (int u = from + static_cast<int>(threadIdx.x & 31); u < to; u += 32) {
-            uint32_t key[kUnit];
-            load_unit(row, u * kUnit, vocab, wide, key);
-#pragma unroll
-            for (int i = 0; i < kUnit; ++i) f(key[i], u * kUnit + i);
+            float x[kUnit];
+            load_unit(row, u * kUnit, vocab, wide, infinite, x);
+            f(x, u * kUnit);
+        }
+    }
+    // f(logit, index) for the set bits of a unit's mask. Few are: they are loaded again, one by one.
+    template <typename F>
+    __device__ __forceinline__ void each_set(unsigned mask, int j, F f) {
+        for (; mask != 0; mask &= mask - 1) {
+            const int at = j + __ffs(mask) - 1;
+            float x = static_cast<float>(row[at]);
+            if (infinite) x = x == INFINITY ? 0.0f : -INFINITY;
+            f(x, at);
         }
     }
 
-    // Bin of a token; -1 if it is not among them or weighs nothing.
-    __device__ __forceinline__ int bin_of(const Among& a, uint32_t key, int index) const {
-        if (key <= kNothing) return -1;
+    // Bin of a token; -1 if it is not among them.
+    __device__ __forceinline__ int bin_of(const Among& a, float x, int index) const {
+        const uint32_t key = key_of(x);
         const u64 place = place_of(key, index);
-        if (place > a.first || place < a.last) return -1;
-        if (a.bins == kByScore) return min(kBins - 1, static_cast<int>(r.scaled(key) * (-kBins / kReach)));
+        if (key <= kNothing || place > a.first || place < a.last) return -1;
+        if (a.bins == kByScore) return static_cast<int>(fminf(r.scaled(x) * a.scale, static_cast<float>(kBins)));
         return a.bins == kByKey ? static_cast<int>((a.key - key) >> a.shift) : index >> a.shift;
+    }
+    // The unit's tokens that may be among them (no NaN).
+    __device__ __forceinline__ unsigned near(const Among& a, const float (&x)[kUnit]) const {
+        const float least = a.last == 0 ? -INFINITY : logit_of(static_cast<uint32_t>(a.last >> 32));
+        unsigned mask = 0;
+#pragma unroll
+        for (int i = 0; i < kUnit; ++i) mask |= x[i] >= least ? 1u << i : 0u;
+        return mask;
+    }
+
+    // Counts of the bins need no weights: a token without weight only follows all others.
+    template <bool kCounts, bool kMasses>
+    __device__ __forceinline__ void fill(const Among& a) {
+        u64 beyond = 0;
+        each_unit([&](const float (&x)[kUnit], int j) {
+            if (a.bins == kByScore && a.last == 0) {  // all tokens
+#pragma unroll
+                for (int i = 0; i < kUnit; ++i) {
+                    const float y = r.scaled(x[i]), b = y * a.scale;
+                    const bool binned = b < static_cast<float>(kBins);  // NaN is in no bin
+                    const uint32_t at = static_cast<uint32_t>(b);
+                    if constexpr (kCounts) add_if(binned, &sh.count[0], at, 1);
+                    if constexpr (kMasses) {
+                        const uint32_t w = Row::weight_of(y);
+                        add_if(binned, &sh.low[0], at, w & 0xFFFFu);
+                        add_if(binned, &sh.high[0], at, w >> 16);
+                        beyond += binned ? 0 : w;
+                    }
+                }
+            } else {
+                each_set(near(a, x), j, [&](float v, int index) {
+                    const int b = bin_of(a, v, index);
+                    const bool binned = b >= 0 && b < kBins;
+                    if constexpr (kCounts) add_if(binned, &sh.count[0], b, 1);
+                    if constexpr (kMasses) {
+                        const uint32_t w = r.weight(v);
+                        add_if(binned, &sh.low[0], b, w & 0xFFFFu);
+                        add_if(binned, &sh.high[0], b, w >> 16);
+                    }
+                });
+            }
+        });
+        if constexpr (kMasses) {
+#pragma unroll
+            for (int d = 16; d > 0; d /= 2) beyond += __shfl_xor_sync(kAll, beyond, d);
+            if ((threadIdx.x & 31) == 0 && beyond > 0) atomicAdd(&sh.beyond, beyond);
+        }
     }
 
     __device__ Crossing find(const Among& a, bool counts, bool masses, const Goal& g) {
         for (int i = threadIdx.x; i < kBins; i += kThreads) sh.count[i] = sh.low[i] = sh.high[i] = 0;
+        if (threadIdx.x == 0) sh.beyond = 0;
         __syncthreads();
-        each([&](uint32_t key, int index) {
-            const int b = bin_of(a, key, index);
-            if (b < 0) return;
-            const uint32_t w = r.weight(key);
-            if (w == 0) return;
-            if (counts) atomicAdd(&sh.count[b], 1u);
-            if (masses) {
-                atomicAdd(&sh.low[b], w & 0xFFFFu);
-                atomicAdd(&sh.high[b], w >> 16);
-            }
-        });
-        cluster.sync();
+        if (counts && masses) fill<true, true>(a);
+        else if (masses) fill<false, true>(a);
+        else fill<true, false>(a);
+        sync();
         // each CTA joins a section of the bins, a thread a few in a row
         constexpr int kMost = kBins / kThreads;
         const int section = kBins / ctas, share = (section + kThreads - 1) / kThreads;
@@ -218,31 +279,33 @@ struct Draw {
             n += count[i];
             m += mass[i];
         }
-        int total_count;
-        u64 total_mass;
-        int before = block_exclusive<kWarps>(n, sh.counts, total_count);
-        u64 mass_before = block_exclusive<kWarps>(m, sh.sums, total_mass);
+        int total_count = 0, before = 0;
+        u64 total_mass = 0, mass_before = 0;
+        if (counts) before = block_exclusive<kWarps>(n, sh.counts, total_count);
+        if (masses) mass_before = block_exclusive<kWarps>(m, sh.sums, total_mass);
         if (threadIdx.x == 0) {
             sh.total_count = total_count;
             sh.total_mass = total_mass;
         }
-        cluster.sync();
+        sync();
         int all_count = 0;
-        u64 all_mass = 0;
+        u64 binned = 0, all_mass = 0;
         for (int c = 0; c < ctas; ++c) {
             if (c < rank) {
                 before += of(c).total_count;
                 mass_before += of(c).total_mass;
             }
             all_count += of(c).total_count;
-            all_mass += of(c).total_mass;
+            binned += of(c).total_mass;
+            all_mass += of(c).beyond;
         }
+        all_mass += binned;
         const bool tokens = g.kind == kTokens;
         const u64 goal = g.kind == kShare ? share_of(g.share, all_mass) : g.value;
         const auto tell = [&](const Crossing& x) {
             for (int c = 0; c < ctas; ++c) of(c).crossing = x;
         };
-        if ((tokens ? static_cast<u64>(all_count) : all_mass) < goal) {
+        if ((tokens ? static_cast<u64>(all_count) : binned) < goal) {
             if (rank == 0 && threadIdx.x == 0) tell({-1, all_count, all_mass, goal});
         } else {
 #pragma unroll
@@ -254,7 +317,7 @@ struct Draw {
                 mass_before += mass[i];
             }
         }
-        cluster.sync();
+        sync();
         return sh.crossing;
     }
 
@@ -267,13 +330,27 @@ struct Draw {
         }
         __syncthreads();
         uint32_t least = 0xFFFFFFFFu, most = 0;
-        each([&](uint32_t key, int index) {
-            if (bin_of(a, key, index) != bin || r.weight(key) == 0) return;
-            least = min(least, key);
-            most = max(most, key);
-            if (*static_cast<volatile int*>(&sh.listed) > kThreads) return;  // too many in any case
-            const int at = atomicAdd(&sh.listed, 1);
-            if (at < kThreads) sh.list[at] = place_of(key, index);
+        each_unit([&](const float (&x)[kUnit], int j) {
+            unsigned mask = 0;
+            if (a.bins == kByScore) {  // the bin's edges, in the same arithmetic
+                const float from = static_cast<float>(bin), to = static_cast<float>(bin + 1);
+#pragma unroll
+                for (int i = 0; i < kUnit; ++i) {
+                    const float b = r.scaled(x[i]) * a.scale;
+                    mask |= b >= from && b < to ? 1u << i : 0u;
+                }
+            } else {
+                mask = near(a, x);
+            }
+            each_set(mask, j, [&](float v, int index) {
+                if (bin_of(a, v, index) != bin) return;
+                const uint32_t key = key_of(v);
+                least = min(least, key);
+                most = max(most, key);
+                if (*static_cast<volatile int*>(&sh.listed) > kThreads) return;  // too many in any case
+                const int at = atomicAdd(&sh.listed, 1);
+                if (at < kThreads) sh.list[at] = place_of(key, index);
+            });
         });
         least = __reduce_min_sync(kAll, least);
         most = __reduce_max_sync(kAll, most);
@@ -281,7 +358,7 @@ struct Draw {
             atomicMin(&sh.least, least);
             atomicMax(&sh.most, most);
         }
-        cluster.sync();
+        sync();
         int n = 0;
         for (int c = 0; c < ctas; ++c) n += min(of(c).listed, kThreads + 1);
         return n;
@@ -306,7 +383,7 @@ struct Draw {
             if (i < n) sh.order[before] = place;
             __syncthreads();
             place = i < n ? sh.order[i] : 0;
-            const u64 w = i < n ? r.weight(static_cast<uint32_t>(place >> 32)) : 0;
+            const u64 w = i < n ? r.weight(logit_of(static_cast<uint32_t>(place >> 32))) : 0;
             u64 all;
             const u64 x = block_exclusive<kWarps>(w, sh.sums, all);
             const bool here = tokens ? count + i + 1 == goal : mass + x < goal && mass + x + w >= goal;
@@ -317,19 +394,26 @@ struct Draw {
                 }
             }
         }
-        cluster.sync();
+        sync();
     }
 
     // The last place of the shortest prefix of the order that reaches the goal, among the places from
-    // `last` on, and the prefix's weight. Place 0 if all together do not reach it.
-    __device__ void end_of(u64 last, bool masses, Goal g, u64& place, u64& weight) {
-        Among a = {~0ull, last, kByScore, 0, 0};
+    // `last` on, and the prefix's weight. Place 0 if all together do not reach it. `reach`: the goal is
+    // expected within this much below the largest y.
+    __device__ void end_of(u64 last, float reach, bool masses, Goal g, u64& place, u64& weight) {
+        Among a = {~0ull, last, kByScore, -kBins / reach, 0, 0};
         const bool tokens = g.kind == kTokens;
         u64 count = 0, mass = 0;  // of what is before `a`
-        // by score; by key at most three times (32 bits, 11 at a time); by index, 128 to a bin: those fit
-        for (int round = 0; round < 5; ++round) {
+        // by score, twice if it was not within reach; by key at most four times (32 bits, 10 at a time); by
+        // index, 256 to a bin: those fit
+        for (int round = 0; round < 7; ++round) {
             const Crossing x = find(a, tokens, masses, g);
             if (g.kind == kShare) g = {kWeight, x.goal, 0.0};
+            if (x.bin < 0 && a.bins == kByScore && reach < kReach) {
+                reach = kReach;
+                a.scale = -kBins / reach;
+                continue;
+            }
             count += x.count;
             mass += x.mass;
             if (x.bin < 0) break;
@@ -345,70 +429,103 @@ struct Draw {
                 least = min(least, of(c).least);
                 most = max(most, of(c).most);
             }
-            cluster.sync();  // read by all before it is set anew
+            sync();  // read by all before it is set anew
             g.value -= tokens ? static_cast<u64>(x.count) : x.mass;
             a.first = min(a.first, place_of(most, 0));
             a.last = max(a.last, place_of(least, 0xFFFFFFFFu));
             a.key = most;
             a.bins = least == most ? kByIndex : kByKey;
-            a.shift = least == most ? 7 : max(0, 21 - __clz(most - least));
+            a.shift = least == most ? 8 : max(0, 22 - __clz(most - least));
         }
         place = 0;
         weight = mass;
     }
 
-    __device__ void run(const Sample& p, int i) {
-        // the largest logit, the first of equal ones
-        uint32_t top = 0;
-        int first = 0;
-        each([&](uint32_t key, int index) {
-            if (key > top) {
-                top = key;
-                first = index;
-            }
-        });
-        u64 best = place_of(top, first);
+    // Of the unit's tokens, which may be kept: at or above x, and with y at or above y.
+    __device__ __forceinline__ unsigned candidates(const float(&x)[kUnit], float least_x, float least_y) const {
+        unsigned mask = 0;
 #pragma unroll
-        for (int d = 16; d > 0; d /= 2) best = max(best, __shfl_xor_sync(kAll, best, d));
-        if ((threadIdx.x & 31) == 0) sh.sums[threadIdx.x >> 5] = best;
-        __syncthreads();
-        for (int w = 0; w < kWarps; ++w) best = max(best, sh.sums[w]);
-        if (threadIdx.x == 0) sh.best = best;
-        cluster.sync();
-        for (int c = 0; c < ctas; ++c) best = max(best, of(c).best);
+        for (int i = 0; i < kUnit; ++i) mask |= x[i] >= least_x && r.scaled(x[i]) >= least_y ? 1u << i : 0u;
+        return mask;
+    }
 
-        r.top = static_cast<uint32_t>(best >> 32);
-        r.high = logit_of(r.top);
+    __device__ void run(const Sample& p, int i) {
+        float top = -INFINITY;
+        each_unit([&](const float (&x)[kUnit], int) {
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i) top = fmaxf(top, x[i]);  // NaN is passed over
+        });
+#pragma unroll
+        for (int d = 16; d > 0; d /= 2) top = fmaxf(top, __shfl_xor_sync(kAll, top, d));
+        if ((threadIdx.x & 31) == 0) sh.counts[threadIdx.x >> 5] = __float_as_int(top);
+        if (threadIdx.x == 0) sh.index = 0x7FFFFFFF;
+        __syncthreads();
+        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, __int_as_float(sh.counts[w]));
+        if (threadIdx.x == 0) sh.top = top;
+        sync();
+        for (int c = 0; c < ctas; ++c) top = fmaxf(top, of(c).top);
+
         const float temperature = p.temperature == nullptr ? 1.0f : p.temperature[i];
         const int top_k = p.top_k == nullptr ? 0 : p.top_k[i];
-        const bool greedy = !(temperature >= 0x1p-64f) || top_k == 1;
-        if (greedy || r.top <= kNothing) {
+        const bool none = top == -INFINITY;
+        if (none || !(temperature >= 0x1p-64f) || top_k == 1) {  // the first of the largest
+            int first = 0x7FFFFFFF;
+            each_unit([&](const float (&x)[kUnit], int j) {
+#pragma unroll
+                for (int i = 0; i < kUnit; ++i) first = min(first, x[i] == top ? j + i : 0x7FFFFFFF);
+            });
+            first = __reduce_min_sync(kAll, first);
+            if ((threadIdx.x & 31) == 0) atomicMin(&sh.index, first);
+            sync();
             if (rank == 0 && threadIdx.x == 0) {
-                const bool none = r.top <= kNothing;
-                p.tokens[i] = none ? -1 : static_cast<int>(~static_cast<uint32_t>(best));
+                for (int c = 0; c < ctas; ++c) first = min(first, of(c).index);
+                p.tokens[i] = none ? -1 : first;
                 if (p.logprobs != nullptr) p.logprobs[i] = none ? -INFINITY : 0.0f;
             }
-            cluster.sync();  // until every CTA has read the others' memory
+            sync();  // until every CTA's memory has been read
             return;
         }
+        infinite = top == INFINITY;
+        r.top = infinite ? 0.0f : top;
         r.inverse = __frcp_rn(temperature);
         const float min_p = p.min_p == nullptr ? 0.0f : p.min_p[i];
-        const double top_p = p.top_p == nullptr ? 1.0 : static_cast<double>(p.top_p[i]);
+        const float top_p = p.top_p == nullptr ? 1.0f : p.top_p[i];
         const uint32_t least = min_p > 0.0f ? static_cast<uint32_t>(ceil(fmin(static_cast<double>(min_p), 1.0) * 1073741824.0)) : 0;
         u64 last = 0, mass = 0;
-        const bool counted = top_k > 0 && top_k < vocab, nucleus = top_p < 1.0;
-        if (counted) end_of(0, nucleus, {kTokens, static_cast<u64>(top_k), 0.0}, last, mass);
-        if (nucleus)
-            end_of(last, true, counted ? Goal{kWeight, share_of(top_p, mass), 0.0} : Goal{kShare, 0, top_p}, last, mass);
+        const bool counted = top_k > 0 && top_k < vocab, nucleus = top_p < 1.0f;
+        if (counted) end_of(0, kReach, nucleus, {kTokens, static_cast<u64>(top_k), 0.0}, last, mass);
+        if (nucleus) {
+            // tokens more than ln(vocab / (1 - p)) below the largest together weigh less than 1 - p of it; 0.1
+            // for roundings, which are larger where weights are below five units
+            float reach = logf(static_cast<float>(vocab) / (1.0f - fmaxf(top_p, 0.0f))) + 0.1f;
+            if (!(reach < 19.0f)) reach = kReach;
+            const double share = static_cast<double>(top_p);
+            end_of(last, reach, true, counted ? Goal{kWeight, share_of(share, mass), 0.0} : Goal{kShare, 0, share}, last, mass);
+        }
 
-        const auto kept = [&](uint32_t key, int index) -> uint32_t {
-            if (key <= kNothing || place_of(key, index) < last) return 0;
-            const uint32_t w = r.weight(key);
+        // what is kept; few tokens are where something is cut off, and only those are weighed
+        const float least_x = last == 0 ? -INFINITY : logit_of(static_cast<uint32_t>(last >> 32));
+        const int last_index = static_cast<int>(~static_cast<uint32_t>(last));
+        const float least_y = least > 0 ? logf(fminf(min_p, 1.0f)) - 0.01f : -INFINITY;
+        const bool cut = last != 0 || least > 0;
+        const auto kept = [&](float x, int index) -> uint32_t {
+            if (x == least_x && index > last_index && last != 0) return 0;
+            const uint32_t w = r.weight(x);
             return w >= least ? w : 0;
+        };
+        const auto weigh = [&](const float(&x)[kUnit], int j) -> u64 {
+            u64 sum = 0;
+            if (cut) {
+                each_set(candidates(x, least_x, least_y), j, [&](float v, int at) { sum += kept(v, at); });
+            } else {
+#pragma unroll
+                for (int k = 0; k < kUnit; ++k) sum += r.weight(x[k]);
+            }
+            return sum;
         };
         const int lane = threadIdx.x & 31;
         u64 sum = 0;
-        each([&](uint32_t key, int index) { sum += kept(key, index); });
+        each_unit([&](const float(&x)[kUnit], int j) { sum += weigh(x, j); });
 #pragma unroll
         for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(kAll, sum, d);
         u64 here;
@@ -416,7 +533,7 @@ struct Draw {
         u64 before = block_exclusive<kWarps>(lane == 0 ? sum : 0, sh.sums, here);
         before = __shfl_sync(kAll, before, 0);
         if (threadIdx.x == 0) sh.total_mass = here;
-        cluster.sync();
+        sync();
         u64 all = 0;
         for (int c = 0; c < ctas; ++c) {
             const u64 v = of(c).total_mass;
@@ -427,32 +544,30 @@ struct Draw {
         if (aim >= before && aim < before + sum) {  // the warp that has the token
             u64 run = before;
             for (int u = from; u < to; u += 32) {
-                uint32_t key[kUnit];
+                float x[kUnit];
                 u64 mine = 0;
                 if (u + lane < to) {
-                    load_unit(row, (u + lane) * kUnit, vocab, wide, key);
-#pragma unroll
-                    for (int k = 0; k < kUnit; ++k) mine += kept(key[k], (u + lane) * kUnit + k);
+                    load_unit(row, (u + lane) * kUnit, vocab, wide, infinite, x);
+                    mine = weigh(x, (u + lane) * kUnit);
                 }
                 const u64 in = run + warp_inclusive(mine);
                 if (aim >= in - mine && aim < in) {
-                    u64 x = in - mine;
+                    u64 sofar = in - mine;
 #pragma unroll
                     for (int k = 0; k < kUnit; ++k) {
-                        const u64 w = kept(key[k], (u + lane) * kUnit + k);
-                        if (aim >= x && aim < x + w) {
+                        const u64 w = x[k] >= least_x ? kept(x[k], (u + lane) * kUnit + k) : 0;
+                        if (aim >= sofar && aim < sofar + w) {
                             p.tokens[i] = (u + lane) * kUnit + k;
-                            if (p.logprobs != nullptr)
-                                p.logprobs[i] = r.scaled(key[k]) - logf(static_cast<float>(all) * (1.0f / kOne));
+                            if (p.logprobs != nullptr) p.logprobs[i] = r.scaled(x[k]) - logf(static_cast<float>(all) * (1.0f / kOne));
                         }
-                        x += w;
+                        sofar += w;
                     }
                 }
                 run = __shfl_sync(kAll, in, 31);
                 if (run > aim) break;
             }
         }
-        cluster.sync();  // until every CTA has read the others' memory
+        sync();  // until every CTA has read the others' memory
     }
 };
 
@@ -463,6 +578,8 @@ __host__ __device__ constexpr int units_per_warp(int vocab, int warps) {
 template <typename T, int kThreads>
 __global__ void __launch_bounds__(kThreads) sample_kernel(Sample p) {
     __shared__ Shared<kThreads> sh;
+    after_previous();
+    let_next_start();
     const cg::cluster_group cluster = cg::this_cluster();
     const int ctas = cluster.num_blocks(), rank = cluster.block_rank(), i = blockIdx.x / ctas;
     const T* row = reinterpret_cast<const T*>(p.logits) + static_cast<uint64_t>(i) * p.row_stride;
@@ -471,30 +588,15 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(Sample p) {
     const int units = (p.vocab + kUnit - 1) / kUnit, per = units_per_warp(p.vocab, ctas * kWarps);
     const int from = min((rank * kWarps + static_cast<int>(threadIdx.x >> 5)) * per, units);
     const bool wide = reinterpret_cast<uint64_t>(row) % 16 == 0;
-    Draw<T, kThreads> draw = {row, p.vocab, rank, ctas, from, min(from + per, units), wide, {}, sh, cluster};
+    Draw<T, kThreads> draw = {row, p.vocab, rank, ctas, from, min(from + per, units), wide, false, {}, sh, cluster};
     draw.run(p, i);
-}
-
-template <typename T, int kThreads>
-cudaError_t launch(const Sample& p, int ctas, cudaStream_t s) {
-    cudaLaunchAttribute cluster;
-    cluster.id = cudaLaunchAttributeClusterDimension;
-    cluster.val.clusterDim.x = ctas;
-    cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
-    cudaLaunchConfig_t c = {};
-    c.gridDim = dim3(static_cast<unsigned>(p.n) * ctas);
-    c.blockDim = dim3(kThreads);
-    c.stream = s;
-    c.attrs = &cluster;
-    c.numAttrs = 1;
-    return cudaLaunchKernelEx(&c, sample_kernel<T, kThreads>, p);
 }
 
 template <typename T>
 cudaError_t launch_t(const Sample& p, cudaStream_t s) {
     // few tokens: CTAs of 256 threads, more of which fit an SM
-    const bool small = p.vocab <= 8192;
-    const int threads = small ? 256 : 1024, tokens = threads * kUnit, room = 152 * (small ? 6 : 2);
+    const bool small = p.vocab <= kSmallVocab;
+    const int threads = small ? 256 : kLarge, tokens = threads * kUnit, room = 152 * (small ? 6 : 2048 / kLarge);
     int ctas = 1;
     // as many CTAs as run at once and have a unit for every thread; more where a slice would be too long
     const auto more = [&](int c) {
@@ -502,7 +604,7 @@ cudaError_t launch_t(const Sample& p, cudaStream_t s) {
                (2ll * c * p.n <= room && p.vocab > c * tokens);
     };
     while (ctas < kMaxCluster && more(ctas)) ctas *= 2;
-    return small ? launch<T, 256>(p, ctas, s) : launch<T, 1024>(p, ctas, s);
+    return launch(small ? sample_kernel<T, 256> : sample_kernel<T, kLarge>, static_cast<unsigned>(p.n) * ctas, threads, 0, ctas, s, p);
 }
 
 }  // namespace
