@@ -22,6 +22,8 @@ namespace cg = cooperative_groups;
 constexpr unsigned kAll = 0xFFFFFFFFu;
 constexpr int kIndexBins = 1024;       // bins of an index, 2^18 tokens at most
 constexpr int kMaxCluster = 8;
+constexpr int kSms = 152;
+constexpr int kResident = 1024;        // threads on an SM: 64 registers each; 1536 and 2048 are slower
 constexpr int kMaxSlice = 65536;       // tokens of one CTA: sums of halves of their weights fit 32 bits
 constexpr int kLarge = 512;            // threads of a CTA, 256 for small vocabularies
 constexpr int kSmallVocab = 8192;
@@ -225,7 +227,7 @@ struct Draw {
                     if constexpr (kMasses) {
                         const uint32_t w = Row::weight_of(y);
                         add_if(binned, &sh.low[0], at, w & 0xFFFFu);
-                        add_if(binned, &sh.high[0], at, w >> 16);
+                        add_if(binned && w >> 16 != 0, &sh.high[0], at, w >> 16);  // few
                         beyond += binned ? 0 : w;
                     }
                 }
@@ -247,6 +249,19 @@ struct Draw {
             for (int d = 16; d > 0; d /= 2) beyond += __shfl_xor_sync(kAll, beyond, d);
             if ((threadIdx.x & 31) == 0 && beyond > 0) atomicAdd(&sh.beyond, beyond);
         }
+    }
+
+    // The sum of v over the cluster's CTAs, one a lane; adds those of lanes below `rank` to `before`.
+    template <typename V>
+    __device__ __forceinline__ static V sum_to(V v, int rank, V& before) {
+        V in = v;
+#pragma unroll
+        for (int d = 1; d < kMaxCluster; d *= 2) {
+            const V o = __shfl_up_sync(kAll, in, d);
+            if (static_cast<int>(threadIdx.x & 31) >= d) in += o;
+        }
+        before += rank > 0 ? __shfl_sync(kAll, in, rank > 0 ? rank - 1 : 0) : V(0);
+        return __shfl_sync(kAll, in, kMaxCluster - 1);
     }
 
     __device__ Crossing find(const Among& a, bool counts, bool masses, const Goal& g) {
@@ -288,18 +303,14 @@ struct Draw {
             sh.total_mass = total_mass;
         }
         sync();
-        int all_count = 0;
-        u64 binned = 0, all_mass = 0;
-        for (int c = 0; c < ctas; ++c) {
-            if (c < rank) {
-                before += of(c).total_count;
-                mass_before += of(c).total_mass;
-            }
-            all_count += of(c).total_count;
-            binned += of(c).total_mass;
-            all_mass += of(c).beyond;
-        }
-        all_mass += binned;
+        // a lane reads a CTA's totals
+        const int lane = threadIdx.x & 31;
+        const Shared<kThreads>& other = of(min(lane, ctas - 1));
+        const bool real = lane < ctas;
+        const int all_count = counts ? sum_to(real ? other.total_count : 0, rank, before) : 0;
+        const u64 binned = masses ? sum_to(real ? other.total_mass : 0, rank, mass_before) : 0;
+        u64 none = 0;
+        const u64 all_mass = masses ? binned + sum_to(real ? other.beyond : 0, 0, none) : 0;
         const bool tokens = g.kind == kTokens;
         const u64 goal = g.kind == kShare ? share_of(g.share, all_mass) : g.value;
         const auto tell = [&](const Crossing& x) {
@@ -359,9 +370,8 @@ struct Draw {
             atomicMax(&sh.most, most);
         }
         sync();
-        int n = 0;
-        for (int c = 0; c < ctas; ++c) n += min(of(c).listed, kThreads + 1);
-        return n;
+        const int lane = threadIdx.x & 31;
+        return __reduce_add_sync(kAll, lane < ctas ? min(of(min(lane, ctas - 1)).listed, kThreads + 1) : 0);
     }
 
     // Ranks the n listed tokens and tells every CTA the place of the one that reaches the goal, `count`
@@ -449,24 +459,35 @@ struct Draw {
         return mask;
     }
 
+    __device__ __forceinline__ static float max_of(float v) {
+#pragma unroll
+        for (int d = 16; d > 0; d /= 2) v = fmaxf(v, __shfl_xor_sync(kAll, v, d));
+        return v;
+    }
+
     __device__ void run(const Sample& p, int i) {
+        const float temperature = p.temperature == nullptr ? 1.0f : p.temperature[i];
+        const int top_k = p.top_k == nullptr ? 0 : p.top_k[i];
+        const float min_p = p.min_p == nullptr ? 0.0f : p.min_p[i];
+        const float top_p = p.top_p == nullptr ? 1.0f : p.top_p[i];
+        const uint32_t random = p.words[i];
         float top = -INFINITY;
         each_unit([&](const float (&x)[kUnit], int) {
 #pragma unroll
             for (int i = 0; i < kUnit; ++i) top = fmaxf(top, x[i]);  // NaN is passed over
         });
-#pragma unroll
-        for (int d = 16; d > 0; d /= 2) top = fmaxf(top, __shfl_xor_sync(kAll, top, d));
+        top = max_of(top);
         if ((threadIdx.x & 31) == 0) sh.counts[threadIdx.x >> 5] = __float_as_int(top);
         if (threadIdx.x == 0) sh.index = 0x7FFFFFFF;
         __syncthreads();
-        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, __int_as_float(sh.counts[w]));
-        if (threadIdx.x == 0) sh.top = top;
-        sync();
-        for (int c = 0; c < ctas; ++c) top = fmaxf(top, of(c).top);
+        const int lane = threadIdx.x & 31;
+        top = max_of(lane < kWarps ? __int_as_float(sh.counts[lane]) : -INFINITY);
+        if (ctas > 1) {
+            if (threadIdx.x == 0) sh.top = top;
+            sync();
+            top = max_of(of(min(lane, ctas - 1)).top);
+        }
 
-        const float temperature = p.temperature == nullptr ? 1.0f : p.temperature[i];
-        const int top_k = p.top_k == nullptr ? 0 : p.top_k[i];
         const bool none = top == -INFINITY;
         if (none || !(temperature >= 0x1p-64f) || top_k == 1) {  // the first of the largest
             int first = 0x7FFFFFFF;
@@ -488,8 +509,6 @@ struct Draw {
         infinite = top == INFINITY;
         r.top = infinite ? 0.0f : top;
         r.inverse = __frcp_rn(temperature);
-        const float min_p = p.min_p == nullptr ? 0.0f : p.min_p[i];
-        const float top_p = p.top_p == nullptr ? 1.0f : p.top_p[i];
         const uint32_t least = min_p > 0.0f ? static_cast<uint32_t>(ceil(fmin(static_cast<double>(min_p), 1.0) * 1073741824.0)) : 0;
         u64 last = 0, mass = 0;
         const bool counted = top_k > 0 && top_k < vocab, nucleus = top_p < 1.0f;
@@ -523,7 +542,6 @@ struct Draw {
             }
             return sum;
         };
-        const int lane = threadIdx.x & 31;
         u64 sum = 0;
         each_unit([&](const float(&x)[kUnit], int j) { sum += weigh(x, j); });
 #pragma unroll
@@ -534,13 +552,8 @@ struct Draw {
         before = __shfl_sync(kAll, before, 0);
         if (threadIdx.x == 0) sh.total_mass = here;
         sync();
-        u64 all = 0;
-        for (int c = 0; c < ctas; ++c) {
-            const u64 v = of(c).total_mass;
-            if (c < rank) before += v;
-            all += v;
-        }
-        const u64 aim = __umul64hi(static_cast<u64>(p.words[i]) << 32, all);
+        const u64 all = sum_to(lane < ctas ? of(min(lane, ctas - 1)).total_mass : 0, rank, before);
+        const u64 aim = __umul64hi(static_cast<u64>(random) << 32, all);
         if (aim >= before && aim < before + sum) {  // the warp that has the token
             u64 run = before;
             for (int u = from; u < to; u += 32) {
@@ -576,7 +589,7 @@ __host__ __device__ constexpr int units_per_warp(int vocab, int warps) {
 }
 
 template <typename T, int kThreads>
-__global__ void __launch_bounds__(kThreads) sample_kernel(Sample p) {
+__global__ void __launch_bounds__(kThreads, kResident / kThreads) sample_kernel(Sample p) {
     __shared__ Shared<kThreads> sh;
     after_previous();
     let_next_start();
@@ -596,7 +609,7 @@ template <typename T>
 cudaError_t launch_t(const Sample& p, cudaStream_t s) {
     // few tokens: CTAs of 256 threads, more of which fit an SM
     const bool small = p.vocab <= kSmallVocab;
-    const int threads = small ? 256 : kLarge, tokens = threads * kUnit, room = 152 * (small ? 6 : 2048 / kLarge);
+    const int threads = small ? 256 : kLarge, tokens = threads * kUnit, room = kSms * (kResident / threads);
     int ctas = 1;
     // as many CTAs as run at once and have a unit for every thread; more where a slice would be too long
     const auto more = [&](int c) {
