@@ -516,7 +516,7 @@ def jb_cache_fork(cache: KVCache, parents, children, status=None, stream=None):
     pages = cache.pages
     pp, pc, n = _two_lists(parents, children, "parents and children")
     status = _status_of(status, pages.refs, stream)
-    nbytes = 0 if n == 0 else 4 * (16 + 2 * n + n * pages.struct.row_pages)
+    nbytes = 0 if n == 0 else int(lib().jb_cache_workspace(pages.ref, n))
     ws = _scratch(max(nbytes, 16), pages.refs, stream)
     _check(lib().jb_cache_fork(pages.ref, cache.layers, cache.n_layers, pp, pc, n, status.data_ptr(),
                                ws.data_ptr(), nbytes, _stream(stream)))

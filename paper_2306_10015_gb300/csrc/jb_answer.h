@@ -36,17 +36,14 @@ cudaError_t launch_reserve(const Pages& p, const int* rows, const int* tokens, i
 cudaError_t launch_free(const Pages& p, const int* rows, int n, cudaStream_t s);
 cudaError_t launch_fork_plan(const Pages& p, const int* parents, const int* children, int n, int* status, int* ws,
                              cudaStream_t s);
-cudaError_t launch_fork_copy(const Pages& p, const Pools& pools, const int* parents, int n, const int* ws,
-                             cudaStream_t s);
-cudaError_t launch_fork_rows(const Pages& p, const int* parents, const int* children, int n, int* ws, cudaStream_t s);
+cudaError_t launch_fork_copy(const Pages& p, const Pools& pools, int n, const int* ws, cudaStream_t s);
 cudaError_t launch_compact_plan(const Pages& p, int* status, int* ws, cudaStream_t s);
-cudaError_t launch_compact_copy(const Pages& p, const Pools& pools, const int* ws, cudaStream_t s);
-cudaError_t launch_compact_table(const Pages& p, const int* ws, cudaStream_t s);
+cudaError_t launch_compact_move(const Pages& p, const Pools& pools, bool table, const int* ws, cudaStream_t s);
 
 // Words of the workspaces, in 4-byte units.
 constexpr int kHeaderWords = 16;
 inline uint64_t fork_words(const Pages& p, int n) {
-    return kHeaderWords + 2ull * n + static_cast<uint64_t>(n) * p.row_pages;
+    return kHeaderWords + 3ull * n + static_cast<uint64_t>(n) * p.row_pages;
 }
 inline uint64_t compact_words(const Pages& p) {  // moves (from, to), new ids
     return kHeaderWords + 2ull * (p.n_pages / 2 + 1) + p.n_pages;
@@ -60,7 +57,10 @@ struct Write {
     uint64_t page_stride, to_head, to_token;  // bytes
     const int* rows;
     const int* pos;
-    int n, heads, head_vecs;     // 16-byte vectors of a head
+    int n, heads;
+    uint32_t head_vecs;          // 16-byte vectors of a head
+    uint64_t magic;              // 2^32 / head_vecs rounded up: v magic >> 32 is v / head_vecs below 2^20, the
+                                 // limit of a token's vectors
 };
 cudaError_t launch_write(const Pages& p, const Write& w, cudaStream_t s);
 

@@ -77,7 +77,7 @@ int for_pools(const jb_kv* layers, int n, F f) {
             pools.base[pools.n++] = static_cast<char*>(layers[i].k);
             pools.base[pools.n++] = static_cast<char*>(layers[i].v);
         }
-        const int rc = cuda_status(f(pools));
+        const int rc = cuda_status(f(pools, first == 0));
         if (rc != JB_OK) return rc;
     }
     return JB_OK;
@@ -144,10 +144,7 @@ JB_EXPORT int jb_cache_fork(const jb_pages* pages, const jb_kv* layers, int n_la
         JB_TRY(check_workspace(workspace, workspace_bytes, 4 * jb::fork_words(p, n)));
         int* ws = static_cast<int*>(workspace);
         JB_TRY(cuda_status(jb::launch_fork_plan(p, d_parents, d_children, n, d_status, ws, stream)));
-        JB_TRY(for_pools(layers, n_layers, [&](const jb::Pools& pools) {
-            return jb::launch_fork_copy(p, pools, d_parents, n, ws, stream);
-        }));
-        return cuda_status(jb::launch_fork_rows(p, d_parents, d_children, n, ws, stream));
+        return for_pools(layers, n_layers, [&](const jb::Pools& pools, bool) { return jb::launch_fork_copy(p, pools, n, ws, stream); });
     });
 }
 
@@ -161,10 +158,9 @@ JB_EXPORT int jb_cache_compact(const jb_pages* pages, const jb_kv* layers, int n
         JB_TRY(check_workspace(workspace, workspace_bytes, 4 * jb::compact_words(p)));
         int* ws = static_cast<int*>(workspace);
         JB_TRY(cuda_status(jb::launch_compact_plan(p, d_status, ws, stream)));
-        JB_TRY(for_pools(layers, n_layers, [&](const jb::Pools& pools) {
-            return jb::launch_compact_copy(p, pools, ws, stream);
-        }));
-        return cuda_status(jb::launch_compact_table(p, ws, stream));
+        return for_pools(layers, n_layers, [&](const jb::Pools& pools, bool first) {
+            return jb::launch_compact_move(p, pools, first, ws, stream);
+        });
     });
 }
 
@@ -199,7 +195,8 @@ JB_EXPORT int jb_cache_write(const jb_pages* pages, const jb_kv* layer, const vo
         w.pos = d_pos;
         w.n = n;
         w.heads = layer->heads;
-        w.head_vecs = static_cast<int>(layer->head_dim * es / 16);
+        w.head_vecs = static_cast<uint32_t>(layer->head_dim * es / 16);
+        w.magic = ((1ull << 32) + w.head_vecs - 1) / w.head_vecs;
         return cuda_status(jb::launch_write(p, w, stream));
     });
 }

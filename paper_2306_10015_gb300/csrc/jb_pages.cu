@@ -7,6 +7,7 @@
 #include <cooperative_groups.h>
 
 #include "jb_answer.h"
+#include "jb_launch.cuh"
 
 namespace jb {
 namespace {
@@ -83,32 +84,52 @@ __device__ __forceinline__ int row_len(const Pages& p, int row) {
     return min(max(p.lens[row], 0), p.row_pages * p.page_tokens);
 }
 
-// The cluster's slice of the pages, and the free pages before it and in all.
-struct Slice {
-    int lo, hi, before, total;
+// The plan's CTAs, in step.
+struct Team {
+    cg::cluster_group cluster;
+    int ctas, rank;
+
+    __device__ Team() : cluster(cg::this_cluster()), ctas(cluster.num_blocks()), rank(cluster.block_rank()) {}
+    __device__ void sync() const {
+        if (ctas > 1) cluster.sync();
+        else __syncthreads();
+    }
+    // The sum of v over the CTAs, and over those before this one. word: one of shared memory, not used for
+    // anything else.
+    __device__ int sum(int v, int* word, int& before) const {
+        if (threadIdx.x == 0) *word = v;
+        sync();
+        int all = 0;
+        before = 0;
+        for (int c = 0; c < ctas; ++c) {
+            const int x = *cluster.map_shared_rank(word, c);
+            if (c < rank) before += x;
+            all += x;
+        }
+        return all;
+    }
 };
 
-// `mine`: a word of shared memory that the other CTAs read. Ends with the CTAs in step.
+// The team's slice of the pages, and the flagged ones before it, in it and in all.
+struct Slice {
+    int lo, hi, before, here, total;
+};
+
 template <typename Flag>
-__device__ __forceinline__ Slice count_pages(int n_pages, int* sums, int* mine, Flag flag) {
-    const cg::cluster_group cluster = cg::this_cluster();
-    const int ctas = cluster.num_blocks(), rank = cluster.block_rank();
-    const int per = (n_pages + ctas - 1) / ctas;
-    Slice s;
-    s.lo = min(rank * per, n_pages);
-    s.hi = min(s.lo + per, n_pages);
+__device__ __forceinline__ int count_pages(int lo, int hi, int* sums, Flag flag) {
     int n = 0;
-    for (int i = s.lo + threadIdx.x; i < s.hi; i += kPlanThreads) n += flag(i) ? 1 : 0;
-    n = block_sum(n, sums);
-    if (threadIdx.x == 0) *mine = n;
-    cluster.sync();
-    s.before = s.total = 0;
-    for (int c = 0; c < ctas; ++c) {
-        const int v = *cluster.map_shared_rank(mine, c);
-        if (c < rank) s.before += v;
-        s.total += v;
-    }
-    cluster.sync();
+    for (int i = lo + static_cast<int>(threadIdx.x); i < hi; i += kPlanThreads) n += flag(i) ? 1 : 0;
+    return block_sum(n, sums);
+}
+
+template <typename Flag>
+__device__ __forceinline__ Slice slice_of(const Team& team, int n_pages, int* sums, int* word, Flag flag) {
+    const int per = (n_pages + team.ctas - 1) / team.ctas;
+    Slice s;
+    s.lo = min(team.rank * per, n_pages);
+    s.hi = min(s.lo + per, n_pages);
+    s.here = count_pages(s.lo, s.hi, sums, flag);
+    s.total = team.sum(s.here, word, s.before);
     return s;
 }
 
@@ -140,7 +161,9 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(Pages p, const in
     __shared__ int free_here;
     int* base = dynamic;
     unsigned* seen = reinterpret_cast<unsigned*>(dynamic + n);
-    const cg::cluster_group cluster = cg::this_cluster();
+    after_previous();
+    let_next_start();
+    const Team team;
 
     // every CTA works the list out for itself
     clear_seen(seen, p.n_rows);
@@ -168,10 +191,10 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(Pages p, const in
         need_all = min(need_all + total, 0x3FFFFFFF);
     }
     bad = __syncthreads_or(bad);
-    const Slice s = count_pages(p.n_pages, sums, &free_here, [&](int i) { return p.refs[i] == 0; });
-    const bool first_thread = cluster.block_rank() == 0 && threadIdx.x == 0;
+    const Slice s = slice_of(team, p.n_pages, sums, &free_here, [&](int i) { return p.refs[i] == 0; });
     if (bad || need_all > s.total) {
-        if (first_thread) *status = bad ? -1 : need_all - s.total;
+        if (team.rank == 0 && threadIdx.x == 0) *status = bad ? -1 : need_all - s.total;
+        team.sync();  // until every CTA's memory has been read
         return;
     }
     ranked(s.lo, s.hi, s.before, need_all, sums, [&](int page) { return p.refs[page] == 0; },
@@ -182,8 +205,8 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(Pages p, const in
                p.table[static_cast<size_t>(row) * p.row_pages + at] = page;
                p.refs[page] = 1;
            });
-    cluster.sync();  // the lengths are read until here
-    if (cluster.block_rank() == 0) {
+    team.sync();  // the lengths are read until here
+    if (team.rank == 0) {
         for (int i = threadIdx.x; i < n; i += kPlanThreads) p.lens[rows[i]] = row_len(p, rows[i]) + tokens[i];
         if (threadIdx.x == 0) *status = 0;
     }
@@ -191,19 +214,22 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(Pages p, const in
 
 // One CTA a row. Entries are taken out one by one, so a row listed twice is released once.
 __global__ void __launch_bounds__(256) free_kernel(Pages p, const int* rows) {
+    after_previous();
+    let_next_start();
     const int row = rows[blockIdx.x];
     if (row < 0 || row >= p.n_rows) return;
     int* entry = p.table + static_cast<size_t>(row) * p.row_pages;
-    for (int j = threadIdx.x; j < p.row_pages; j += 256) {
-        if (entry[j] < 0) continue;
+    const int pages = pages_of(row_len(p, row), p.page_tokens);
+    __syncthreads();  // the length is read until here
+    for (int j = threadIdx.x; j < pages; j += 256) {
         const int page = atomicExch(&entry[j], -1);
         if (page >= 0 && page < p.n_pages) atomicSub(&p.refs[page], 1);
     }
     if (threadIdx.x == 0) p.lens[row] = 0;
 }
 
-// Workspace of a fork: header, fresh[n] (the page that takes the last tokens, or -1), len[n] (tokens
-// of the parent, or -1: nothing to do), stage[n][row_pages] (the parents' entries).
+// Workspace of a fork: header, from[n] and to[n] (the pages of the last tokens, -1: nothing to copy), len[n]
+// (tokens of the parent, -1: nothing to do), stage[n][row_pages] (the parents' entries).
 __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(Pages p, const int* parents, const int* children,
                                                                  int n, int* status, int* ws) {
     extern __shared__ int dynamic[];
@@ -211,9 +237,13 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(Pages p, const 
     __shared__ int free_here;
     int* base = dynamic;
     unsigned* seen = reinterpret_cast<unsigned*>(dynamic + n);
-    const cg::cluster_group cluster = cg::this_cluster();
-    int* fresh = ws + kHeaderWords;
-    int* len = fresh + n;
+    after_previous();
+    let_next_start();
+    const Team team;
+    int* from = ws + kHeaderWords;
+    int* to = from + n;
+    int* len = to + n;
+    int* stage = len + n;
 
     clear_seen(seen, p.n_rows);
     __syncthreads();
@@ -233,22 +263,55 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(Pages p, const 
         need_all += total;
     }
     bad = __syncthreads_or(bad);
-    const Slice s = count_pages(p.n_pages, sums, &free_here, [&](int i) { return p.refs[i] == 0; });
+    const Slice s = slice_of(team, p.n_pages, sums, &free_here, [&](int i) { return p.refs[i] == 0; });
     const bool go = !bad && need_all <= s.total;
-    if (cluster.block_rank() == 0) {
+    if (team.rank == 0) {
         for (int i = threadIdx.x; i < n; i += kPlanThreads) {
-            const bool moves = go && parents[i] != children[i];
-            len[i] = moves ? row_len(p, parents[i]) : -1;
-            if (!(moves && len[i] % p.page_tokens != 0)) fresh[i] = -1;
+            const int a = parents[i];
+            const bool moves = go && a != children[i];
+            const int tokens = moves ? row_len(p, a) : -1;
+            len[i] = tokens;
+            from[i] = moves && tokens % p.page_tokens != 0 ? p.table[static_cast<size_t>(a) * p.row_pages + tokens / p.page_tokens] : -1;
         }
         if (threadIdx.x == 0) *status = bad ? -1 : max(need_all - s.total, 0);
     }
-    if (!go) return;
+    if (!go) {
+        team.sync();  // until every CTA's memory has been read
+        return;
+    }
     ranked(s.lo, s.hi, s.before, need_all, sums, [&](int page) { return p.refs[page] == 0; },
            [&](int page, int rank) {
-               fresh[owner_of(base, n, rank)] = page;
+               to[owner_of(base, n, rank)] = page;
                p.refs[page] = 1;
            });
+    team.sync();
+    // The parents' entries are set aside before any row is written: a parent may be a child too. A warp takes a
+    // pair at a time.
+    const int lane = threadIdx.x & 31, warp = team.rank * kPlanWarps + static_cast<int>(threadIdx.x >> 5), warps = team.ctas * kPlanWarps;
+    for (int i = warp; i < n; i += warps) {
+        const int full = len[i] < 0 ? 0 : len[i] / p.page_tokens;
+        const int* entry = p.table + static_cast<size_t>(parents[i]) * p.row_pages;
+        for (int j = lane; j < full; j += 32) {
+            const int page = entry[j];
+            stage[static_cast<size_t>(i) * p.row_pages + j] = page;
+            if (page >= 0 && page < p.n_pages) atomicAdd(&p.refs[page], 1);
+        }
+    }
+    team.sync();
+    for (int i = warp; i < n; i += warps) {
+        const int tokens = len[i];
+        if (tokens < 0) continue;
+        const int child = children[i], full = tokens / p.page_tokens, pages = pages_of(tokens, p.page_tokens);
+        const int had = pages_of(row_len(p, child), p.page_tokens);
+        int* entry = p.table + static_cast<size_t>(child) * p.row_pages;
+        __syncwarp();  // the length is read until here
+        for (int j = lane; j < max(pages, had); j += 32) {
+            const int old = j < had ? entry[j] : -1;
+            if (old >= 0 && old < p.n_pages) atomicSub(&p.refs[old], 1);
+            entry[j] = j < full ? stage[static_cast<size_t>(i) * p.row_pages + j] : j < pages ? to[i] : -1;
+        }
+        if (lane == 0) p.lens[child] = tokens;
+    }
 }
 
 // A run of 16-byte vectors, four in flight a thread.
@@ -270,147 +333,135 @@ struct Ends {
     char* second;
 };
 
-// One CTA for a pair's last page in one pool: the valid tokens of each slab.
-__global__ void __launch_bounds__(256) fork_copy_kernel(Pages p, const __grid_constant__ Pools pools,
-                                                        const int* parents, int n, const int* ws) {
-    const int i = blockIdx.x / pools.n, pool = blockIdx.x % pools.n;
-    const int to = ws[kHeaderWords + i], len = ws[kHeaderWords + n + i];
-    if (to < 0) return;
-    const int from = p.table[static_cast<size_t>(parents[i]) * p.row_pages + len / p.page_tokens];
+// `splits` CTAs for a pair's last page in one pool: the valid tokens of each slab.
+__global__ void __launch_bounds__(256) fork_copy_kernel(Pages p, const __grid_constant__ Pools pools, int n, int splits,
+                                                        const int* ws) {
+    after_previous();
+    let_next_start();
+    const int split = blockIdx.x % splits, unit = blockIdx.x / splits, i = unit / pools.n, pool = unit % pools.n;
+    const int from = ws[kHeaderWords + i], to = ws[kHeaderWords + n + i], len = ws[kHeaderWords + 2 * n + i];
     if (from < 0 || from >= p.n_pages) return;
     const uint32_t run = (len % p.page_tokens) * pools.row_vecs, whole = p.page_tokens * pools.row_vecs;
     const char* src = pools.base[pool] + from * pools.stride;
     char* dst = pools.base[pool] + to * pools.stride;
-    copy_vectors(threadIdx.x, run * pools.slabs, 256, [&](uint32_t v) {
+    copy_vectors(split * 256 + threadIdx.x, run * pools.slabs, splits * 256, [&](uint32_t v) {
         const uint64_t at = 16ull * (v / run * whole + v % run);
         return Ends{src + at, dst + at};
     });
-}
-
-// The parents' entries are set aside before any row is written: a parent may be a child too.
-__global__ void __launch_bounds__(256) fork_stage_kernel(Pages p, const int* parents, int n, int* ws) {
-    const int i = blockIdx.x, len = ws[kHeaderWords + n + i];
-    if (len < 0) return;
-    const int full = len / p.page_tokens;
-    const int* entry = p.table + static_cast<size_t>(parents[i]) * p.row_pages;
-    int* stage = ws + kHeaderWords + 2 * n + static_cast<size_t>(i) * p.row_pages;
-    for (int j = threadIdx.x; j < full; j += 256) {
-        const int page = entry[j];
-        stage[j] = page;
-        if (page >= 0 && page < p.n_pages) atomicAdd(&p.refs[page], 1);
-    }
-}
-
-__global__ void __launch_bounds__(256) fork_rows_kernel(Pages p, const int* children, int n, const int* ws) {
-    const int i = blockIdx.x, len = ws[kHeaderWords + n + i];
-    if (len < 0) return;
-    const int full = len / p.page_tokens, fresh = ws[kHeaderWords + i], child = children[i];
-    int* entry = p.table + static_cast<size_t>(child) * p.row_pages;
-    const int* stage = ws + kHeaderWords + 2 * n + static_cast<size_t>(i) * p.row_pages;
-    for (int j = threadIdx.x; j < p.row_pages; j += 256) {
-        const int old = entry[j];
-        if (old >= 0 && old < p.n_pages) atomicSub(&p.refs[old], 1);
-        const int now = j < full ? stage[j] : j == full ? fresh : -1;
-        if (now != old) entry[j] = now;
-    }
-    if (threadIdx.x == 0) p.lens[child] = len;
 }
 
 // Workspace of a compaction: header (moves, pages in use), from[n_pages / 2 + 1], to[...], the new id
 // of each page that moves.
 __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(Pages p, int* status, int* ws) {
     __shared__ int sums[kPlanWarps];
-    __shared__ int used_here, holes_here, movers_here;
-    const cg::cluster_group cluster = cg::this_cluster();
+    __shared__ int used_here, low_here;
+    after_previous();
+    let_next_start();
+    const Team team;
     int* from = ws + kHeaderWords;
     int* to = from + p.n_pages / 2 + 1;
     int* moved = to + p.n_pages / 2 + 1;
     const auto used = [&](int page) { return p.refs[page] > 0; };
-    const int n_live = count_pages(p.n_pages, sums, &used_here, used).total;
-    const auto hole = [&](int page) { return page < n_live && !used(page); };
-    const auto mover = [&](int page) { return page >= n_live && used(page); };
-    const Slice h = count_pages(p.n_pages, sums, &holes_here, hole);
-    const Slice m = count_pages(p.n_pages, sums, &movers_here, mover);
-    ranked(h.lo, h.hi, h.before, h.total, sums, hole, [&](int page, int rank) { to[rank] = page; });
-    ranked(m.lo, m.hi, m.before, m.total, sums, mover, [&](int page, int rank) { from[rank] = page; });
-    cluster.sync();  // both lists are whole
-    const int step = cluster.num_blocks() * kPlanThreads;
-    for (int i = cluster.block_rank() * kPlanThreads + threadIdx.x; i < m.total; i += step) {
+    const Slice s = slice_of(team, p.n_pages, sums, &used_here, used);
+    const int n_live = s.total;
+    // pages in use below n_live: of the slices on both sides they are known
+    const int low = s.hi <= n_live ? s.here : s.lo >= n_live ? 0 : count_pages(s.lo, n_live, sums, used);
+    int before;
+    const int low_all = team.sum(low, &low_here, before);
+    const int moves = n_live - low_all;
+    // the first page's rank among the holes, and of the first page from n_live on among the movers
+    ranked(s.lo, min(s.hi, n_live), s.lo - s.before, moves, sums, [&](int page) { return !used(page); },
+           [&](int page, int rank) { to[rank] = page; });
+    const int start = max(s.lo, n_live);
+    ranked(start, s.hi, s.before + low - low_all, moves, sums, used, [&](int page, int rank) { from[rank] = page; });
+    team.sync();  // both lists are whole
+    const int step = team.ctas * kPlanThreads;
+    for (int i = team.rank * kPlanThreads + static_cast<int>(threadIdx.x); i < moves; i += step) {
         moved[from[i]] = to[i];
         p.refs[to[i]] = p.refs[from[i]];
         p.refs[from[i]] = 0;
     }
-    if (cluster.block_rank() == 0 && threadIdx.x == 0) {
-        ws[0] = m.total;
+    if (team.rank == 0 && threadIdx.x == 0) {
+        ws[0] = moves;
         ws[1] = n_live;
         if (status != nullptr) *status = n_live;
     }
 }
 
-__global__ void __launch_bounds__(256) compact_copy_kernel(Pages p, const __grid_constant__ Pools pools, const int* ws) {
+// The first table_ctas CTAs put the new ids into the table, the others move pages, 16 KB at a time.
+constexpr int kChunk = 4 * 256;  // 16-byte vectors
+__global__ void __launch_bounds__(256) compact_move_kernel(Pages p, const __grid_constant__ Pools pools, int table_ctas, const int* ws) {
+    after_previous();
+    let_next_start();
+    const int moves = ws[0], n_live = ws[1];
+    if (moves == 0) return;
     const int* from = ws + kHeaderWords;
     const int* to = from + p.n_pages / 2 + 1;
-    const uint32_t vecs = pools.slabs * p.page_tokens * pools.row_vecs;
-    const uint64_t units = static_cast<uint64_t>(ws[0]) * pools.n;
-    for (uint64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const uint32_t i = static_cast<uint32_t>(u / pools.n), pool = static_cast<uint32_t>(u % pools.n);
+    const int* moved = to + p.n_pages / 2 + 1;
+    if (static_cast<int>(blockIdx.x) < table_ctas) {
+        const size_t n = static_cast<size_t>(p.n_rows) * p.row_pages, step = table_ctas * 256ull;
+        for (size_t i = blockIdx.x * 256ull + threadIdx.x; i < n; i += step) {
+            const int page = p.table[i];
+            if (page >= n_live && page < p.n_pages) p.table[i] = moved[page];
+        }
+        return;
+    }
+    const uint32_t vecs = pools.slabs * p.page_tokens * pools.row_vecs, chunks = (vecs + kChunk - 1) / kChunk;
+    const uint64_t units = static_cast<uint64_t>(moves) * pools.n * chunks;
+    for (uint64_t u = blockIdx.x - table_ctas; u < units; u += gridDim.x - table_ctas) {
+        const uint64_t page = u / chunks;
+        const uint32_t first = static_cast<uint32_t>(u - page * chunks) * kChunk + threadIdx.x;
+        const uint32_t i = static_cast<uint32_t>(page / pools.n), pool = static_cast<uint32_t>(page - static_cast<uint64_t>(i) * pools.n);
         const char* src = pools.base[pool] + from[i] * pools.stride;
         char* dst = pools.base[pool] + to[i] * pools.stride;
-        copy_vectors(threadIdx.x, vecs, 256, [&](uint32_t v) { return Ends{src + 16ull * v, dst + 16ull * v}; });
+        uint4 x[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (first + k * 256 < vecs) x[k] = __ldcs(reinterpret_cast<const uint4*>(src) + first + k * 256);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (first + k * 256 < vecs) __stcs(reinterpret_cast<uint4*>(dst) + first + k * 256, x[k]);
     }
 }
 
-__global__ void __launch_bounds__(256) compact_table_kernel(Pages p, const int* ws) {
-    const int n_live = ws[1];
-    if (ws[0] == 0) return;
-    const int* moved = ws + kHeaderWords + 2 * (p.n_pages / 2 + 1);
-    const size_t n = static_cast<size_t>(p.n_rows) * p.row_pages;
-    for (size_t i = static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<size_t>(gridDim.x) * 256) {
-        const int page = p.table[i];
-        if (page >= n_live && page < p.n_pages) p.table[i] = moved[page];
+// A warp takes kVecs vectors a lane of a token's keys (blockIdx.y even) or values.
+constexpr int kVecs = 4;
+__global__ void __launch_bounds__(256) write_kernel(Pages p, const __grid_constant__ Write w) {
+    after_previous();
+    let_next_start();
+    const int i = blockIdx.x * 8 + static_cast<int>(threadIdx.x >> 5), which = blockIdx.y & 1;
+    if (i >= w.n) return;
+    const int row = w.rows[i], pos = w.pos[i];
+    if (row < 0 || row >= p.n_rows || pos < 0 || pos / p.page_tokens >= p.row_pages) return;
+    const int page = p.table[static_cast<size_t>(row) * p.row_pages + pos / p.page_tokens];
+    if (page < 0 || page >= p.n_pages) return;
+    const char* src = w.from[which] + i * w.token_stride[which];
+    char* dst = w.to[which] + page * w.page_stride + pos % p.page_tokens * w.to_token;
+    const uint32_t first = (blockIdx.y >> 1) * 32 * kVecs + (threadIdx.x & 31), vecs = w.heads * w.head_vecs;
+    uint4 x[kVecs];
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+        const uint32_t v = first + 32 * k, head = static_cast<uint32_t>(v * w.magic >> 32);
+        if (v < vecs) x[k] = *reinterpret_cast<const uint4*>(src + head * w.head_stride[which] + 16 * (v - head * w.head_vecs));
+    }
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+        const uint32_t v = first + 32 * k, head = static_cast<uint32_t>(v * w.magic >> 32);
+        if (v < vecs) *reinterpret_cast<uint4*>(dst + head * w.to_head + 16 * (v - head * w.head_vecs)) = x[k];
     }
 }
 
-// One thread a 16-byte vector: the keys' vectors first, then the values'.
-__global__ void __launch_bounds__(256) write_kernel(Pages p, const Write w) {
-    const uint32_t token_vecs = w.heads * w.head_vecs;
-    const uint64_t each = static_cast<uint64_t>(w.n) * token_vecs;
-    for (uint64_t u = blockIdx.x * 256ull + threadIdx.x; u < 2 * each; u += gridDim.x * 256ull) {
-        const int which = u >= each;
-        const uint64_t at = u - (which ? each : 0);
-        const int i = static_cast<int>(at / token_vecs);
-        const uint32_t in = static_cast<uint32_t>(at % token_vecs), head = in / w.head_vecs, vec = in % w.head_vecs;
-        const int row = w.rows[i], pos = w.pos[i];
-        if (row < 0 || row >= p.n_rows || pos < 0 || pos / p.page_tokens >= p.row_pages) continue;
-        const int page = p.table[static_cast<size_t>(row) * p.row_pages + pos / p.page_tokens];
-        if (page < 0 || page >= p.n_pages) continue;
-        const char* src = w.from[which] + i * w.token_stride[which] + head * w.head_stride[which] + 16ull * vec;
-        char* dst = w.to[which] + page * w.page_stride + head * w.to_head + (pos % p.page_tokens) * w.to_token + 16ull * vec;
-        *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(src);
-    }
-}
-
-// Ranking the free pages of a small cache takes one CTA; eight share larger ones.
-constexpr int kOneCtaPages = 16384;
+// A small plan takes one CTA; eight share larger ones. work: pages to rank and entries to write.
+constexpr uint64_t kOneCta = 16384;
 
 template <typename... Params, typename... Args>
-cudaError_t launch_plan(void (*kernel)(Params...), int n_pages, size_t shared, cudaStream_t s, Args... args) {
+cudaError_t launch_plan(void (*kernel)(Params...), uint64_t work, size_t shared, cudaStream_t s, const Args&... args) {
     if (shared > 48 * 1024) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(shared));
         if (e != cudaSuccess) return e;
     }
-    cudaLaunchAttribute cluster;
-    cluster.id = cudaLaunchAttributeClusterDimension;
-    cluster.val.clusterDim.x = n_pages <= kOneCtaPages ? 1 : 8;
-    cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
-    cudaLaunchConfig_t c = {};
-    c.gridDim = dim3(cluster.val.clusterDim.x);
-    c.blockDim = dim3(kPlanThreads);
-    c.dynamicSmemBytes = shared;
-    c.stream = s;
-    c.attrs = &cluster;
-    c.numAttrs = 1;
-    return cudaLaunchKernelEx(&c, kernel, static_cast<Params>(args)...);
+    const unsigned ctas = work <= kOneCta ? 1 : 8;
+    return launch(kernel, ctas, kPlanThreads, shared, ctas, s, args...);
 }
 
 size_t plan_shared(const Pages& p, int n) { return 4ull * n + 4ull * ((p.n_rows + 31) / 32); }
@@ -422,49 +473,43 @@ cudaError_t launch_reserve(const Pages& p, const int* rows, const int* tokens, i
 }
 
 cudaError_t launch_free(const Pages& p, const int* rows, int n, cudaStream_t s) {
-    free_kernel<<<n, 256, 0, s>>>(p, rows);
-    return cudaGetLastError();
+    return launch(free_kernel, n, 256, 0, 0, s, p, rows);
 }
 
 cudaError_t launch_fork_plan(const Pages& p, const int* parents, const int* children, int n, int* status, int* ws,
                              cudaStream_t s) {
-    return launch_plan(fork_plan_kernel, p.n_pages, plan_shared(p, n), s, p, parents, children, n, status, ws);
+    return launch_plan(fork_plan_kernel, p.n_pages + static_cast<uint64_t>(n) * p.row_pages, plan_shared(p, n), s, p, parents,
+                       children, n, status, ws);
 }
 
-cudaError_t launch_fork_copy(const Pages& p, const Pools& pools, const int* parents, int n, const int* ws,
-                             cudaStream_t s) {
-    fork_copy_kernel<<<n * pools.n, 256, 0, s>>>(p, pools, parents, n, ws);
-    return cudaGetLastError();
-}
-
-cudaError_t launch_fork_rows(const Pages& p, const int* parents, const int* children, int n, int* ws, cudaStream_t s) {
-    fork_stage_kernel<<<n, 256, 0, s>>>(p, parents, n, ws);
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
-    fork_rows_kernel<<<n, 256, 0, s>>>(p, children, n, ws);
-    return cudaGetLastError();
+cudaError_t launch_fork_copy(const Pages& p, const Pools& pools, int n, const int* ws, cudaStream_t s) {
+    // few pages are shared out further, so that every SM has some
+    const int units = n * static_cast<int>(pools.n), splits = units >= 2048 ? 1 : units >= 512 ? 4 : 8;
+    return launch(fork_copy_kernel, static_cast<unsigned>(units) * splits, 256, 0, 0, s, p, pools, n, splits, ws);
 }
 
 cudaError_t launch_compact_plan(const Pages& p, int* status, int* ws, cudaStream_t s) {
     return launch_plan(compact_plan_kernel, p.n_pages, 0, s, p, status, ws);
 }
 
-cudaError_t launch_compact_copy(const Pages& p, const Pools& pools, const int* ws, cudaStream_t s) {
-    compact_copy_kernel<<<152 * 8, 256, 0, s>>>(p, pools, ws);
-    return cudaGetLastError();
-}
-
-cudaError_t launch_compact_table(const Pages& p, const int* ws, cudaStream_t s) {
-    const uint64_t n = static_cast<uint64_t>(p.n_rows) * p.row_pages;
-    const uint64_t blocks = (n + 255) / 256;
-    compact_table_kernel<<<static_cast<unsigned>(blocks < 1216 ? blocks : 1216), 256, 0, s>>>(p, ws);
-    return cudaGetLastError();
+cudaError_t launch_compact_move(const Pages& p, const Pools& pools, bool table, const int* ws, cudaStream_t s) {
+    const uint64_t blocks = (static_cast<uint64_t>(p.n_rows) * p.row_pages + 255) / 256;
+    const int table_ctas = table ? static_cast<int>(blocks < 152 ? blocks : 152) : 0;
+    return launch(compact_move_kernel, 152 * 8 + table_ctas, 256, 0, 0, s, p, pools, table_ctas, ws);
 }
 
 cudaError_t launch_write(const Pages& p, const Write& w, cudaStream_t s) {
-    const uint64_t n = 2ull * w.n * w.heads * w.head_vecs, blocks = (n + 255) / 256;
-    write_kernel<<<static_cast<unsigned>(blocks < 65536 ? blocks : 65536), 256, 0, s>>>(p, w);
-    return cudaGetLastError();
+    const unsigned vecs = w.heads * w.head_vecs, parts = (vecs + 32 * kVecs - 1) / (32 * kVecs);
+    cudaLaunchConfig_t c = {};
+    cudaLaunchAttribute a;
+    a.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    a.val.programmaticStreamSerializationAllowed = 1;
+    c.gridDim = dim3((w.n + 7u) / 8u, 2 * parts);
+    c.blockDim = dim3(256);
+    c.stream = s;
+    c.attrs = &a;
+    c.numAttrs = 1;
+    return cudaLaunchKernelEx(&c, write_kernel, p, w);
 }
 
 }  // namespace jb
