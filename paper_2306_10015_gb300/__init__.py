@@ -361,12 +361,22 @@ def jb_checksum(table: ParamTable, out, stream=None, grid_ctas: int = 0) -> None
 
 # --- writing answers ------------------------------------------------------------
 
+torch = None  # imported by the first call that needs it: the rest of the package works without
+
+
+def _need_torch():
+    global torch
+    import torch as module
+    torch = module
+
+
 def _list32(t, what: str):
     """A one-dimensional contiguous int32 CUDA tensor: its address and length."""
-    import torch
+    if torch is None:
+        _need_torch()
     if t.dtype is not torch.int32 or not t.is_cuda or t.dim() != 1 or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous one-dimensional int32 CUDA tensor")
-    return t.data_ptr(), t.shape[0]
+    return t.data_ptr(), t.numel()
 
 
 def _two_lists(a, b, what: str):
@@ -378,7 +388,6 @@ def _two_lists(a, b, what: str):
 
 
 def _storage(dtype) -> int:
-    import torch
     if dtype is torch.bfloat16:
         return JB_BF16
     if dtype is torch.float32:
@@ -392,7 +401,7 @@ class PageTable:
     references to them. ``PageTable.empty`` makes them."""
 
     def __init__(self, table, lens, refs, page_tokens: int):
-        import torch
+        _need_torch()
         for t, dim in ((table, 2), (lens, 1), (refs, 1)):
             if t.dtype is not torch.int32 or not t.is_cuda or t.dim() != dim or not t.is_contiguous():
                 raise ValueError("table [rows, row_pages], lens [rows] and refs [pages] must be contiguous int32 CUDA tensors")
@@ -407,7 +416,7 @@ class PageTable:
 
     @classmethod
     def empty(cls, n_rows: int, row_pages: int, n_pages: int, page_tokens: int, device="cuda") -> "PageTable":
-        import torch
+        _need_torch()
         return cls(torch.full((n_rows, row_pages), -1, dtype=torch.int32, device=device),
                    torch.zeros(n_rows, dtype=torch.int32, device=device),
                    torch.zeros(n_pages, dtype=torch.int32, device=device), page_tokens)
@@ -449,28 +458,27 @@ class KVCache:
 
     def new_workspace(self, q_heads: int, stream=None):
         """A workspace for jb_attend with so many query heads: a uint8 tensor, ready for use on the stream."""
-        import torch
         nbytes = int(lib().jb_attend_workspace(self.layer_refs[0], q_heads))
         ws = _new(stream, torch.empty, max(nbytes, ATTEND_ZEROS), dtype=torch.uint8, device=self.keys[0].device)
         _new(stream, ws[:ATTEND_ZEROS].zero_)
         return ws
 
-    def _workspace(self, q_heads: int, stream):
+    def _workspace(self, q_heads: int, stream, handle):
         # one for each stream, and a new one for each call that a graph captures: the graph may be
         # replayed on another stream
-        import torch
         if _new(stream, torch.cuda.is_current_stream_capturing):
-            return self.new_workspace(q_heads, stream)
-        key = _stream(stream).value, q_heads
-        ws = self._workspaces.get(key)
-        if ws is None:
-            ws = self._workspaces[key] = self.new_workspace(q_heads, stream)
-        return ws
+            ws = self.new_workspace(q_heads, stream)
+            return ws.data_ptr(), ws.numel(), ws
+        key = handle.value, q_heads
+        found = self._workspaces.get(key)
+        if found is None:
+            ws = self.new_workspace(q_heads, stream)
+            found = self._workspaces[key] = ws.data_ptr(), ws.numel(), ws
+        return found
 
 
 def _new(stream, make, *args, **kwargs):
     """make(...) on the call's stream: what the allocator hands out is ordered with that stream alone."""
-    import torch
     if stream is None:
         return make(*args, **kwargs)
     with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
@@ -478,7 +486,6 @@ def _new(stream, make, *args, **kwargs):
 
 
 def _status_of(status, like, stream):
-    import torch
     if status is None:
         return _new(stream, torch.empty, 1, dtype=torch.int32, device=like.device)
     if _list32(status, "status")[1] != 1:
@@ -488,7 +495,6 @@ def _status_of(status, like, stream):
 
 def _scratch(nbytes: int, like, stream):
     """Device bytes for one call."""
-    import torch
     return _new(stream, torch.empty, nbytes, dtype=torch.uint8, device=like.device)
 
 
@@ -562,7 +568,6 @@ def jb_attend(cache: KVCache, layer: int, q, rows, pos, out=None, scale: Optiona
     biased by slopes[head] (t - pos), limited to the last `window` positions. ``workspace``: by default
     one that the cache keeps for the stream; ``cache.new_workspace`` makes others, for instance one for
     all the calls that a CUDA graph captures (by default each gets its own there)."""
-    import torch
     pr, pp, n = _two_lists(rows, pos, "rows and positions")
     heads = q.shape[1] if q.dim() == 3 else 0
     qa, qb = _heads_of(q, heads, cache, n, "queries")
@@ -572,18 +577,21 @@ def jb_attend(cache: KVCache, layer: int, q, rows, pos, out=None, scale: Optiona
     if slopes is not None and (slopes.dtype is not torch.float32 or not slopes.is_cuda or slopes.shape != (heads,)
                                or not slopes.is_contiguous()):
         raise ValueError("slopes must be a contiguous float32 CUDA tensor, one per query head")
-    ws = cache._workspace(heads, stream) if workspace is None else workspace
+    handle = _stream(stream)
+    if workspace is None:
+        ws, nbytes, held = cache._workspace(heads, stream, handle)
+    else:
+        ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     scores = jb_scores(cache.head_dim ** -0.5 if scale is None else scale, softcap, window,
                        None if slopes is None else slopes.data_ptr())
     _check(lib().jb_attend(cache.pages.ref, cache.layer_refs[layer], ctypes.byref(scores), q.data_ptr(), qa, qb, heads,
-                           pr, pp, n, out.data_ptr(), oa, ob, ws.data_ptr(), ws.shape[0], _stream(stream)))
+                           pr, pp, n, out.data_ptr(), oa, ob, ws, nbytes, handle))
     return out
 
 
 def _per_row(value, default, n: int, dtype, device, stream):
     """A setting of jb_sample as the address of n entries (None where it is the default) and the
     tensor that holds them."""
-    import torch
     if not isinstance(value, torch.Tensor):
         if value == default:
             return None, None
@@ -598,7 +606,8 @@ def jb_sample(logits, words, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tok
     """The next token of each row of logits [n, vocab] from its random word (int32 or uint32 bits),
     and its log-probability; returns (tokens int32, logprobs float32). Settings are numbers or one
     per row (float32, top_k int32 CUDA tensors)."""
-    import torch
+    if torch is None:
+        _need_torch()
     if logits.dim() != 2 or not logits.is_cuda or (logits.stride(1) != 1 and logits.shape[1] > 1):
         raise ValueError("logits must be a CUDA tensor [n, vocab], contiguous in a row")
     n, vocab = logits.shape
