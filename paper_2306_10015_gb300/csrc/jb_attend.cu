@@ -351,7 +351,7 @@ __device__ __forceinline__ void prefetch(const void* p) { asm volatile("prefetch
 // column of 8 rows, and of one row, are free of bank conflicts.
 template <typename T, int D>
 struct Feed {
-    static constexpr int kStages = D * sizeof(T) > 512 ? 1 : 2;           // groups that a warp copies ahead
+    static constexpr int kStages = sizeof(T) == 4 && D >= 128 ? 1 : 2;    // groups that a warp copies ahead
     static constexpr int kPieces = D * static_cast<int>(sizeof(T)) / 16;  // of a row
     static constexpr int kLanes = kPieces < 32 ? kPieces : 32;            // of them that copy one row
     static constexpr int kRows = 32 / kLanes;                             // rows that the warp copies at a time
@@ -636,7 +636,7 @@ __global__ void __launch_bounds__(kThreads, kBf16Ctas<D, kH>) attend_bf16_kernel
 // its elements against the queries in shared memory; for the values it takes four (eight) elements of
 // every token, with the weights from shared memory.
 template <int D>
-constexpr int kF32Ctas = D == 64 ? 3 : 1;  // on an SM
+constexpr int kF32Ctas = D == 64 ? 3 : D == 128 ? 2 : 1;  // on an SM
 constexpr int kF32Heads = 8;               // of a slot
 
 template <int D, int kH>
@@ -672,7 +672,8 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const
     while (more) {
         const int heads_here = min(kH, p.a.group - s.block * kH);
         const int head0 = s.head * p.a.group + s.block * kH;
-        float slope[kH], m[kH], l[kH], acc[kH][kV][4];
+        float slope[kH], m[kH], l[kH];
+        float2 acc[kH][kV][2];
         for (int u = lane; u < kH * kPieces; u += 32) {
             const int h = u / kPieces, e = u % kPieces * 4;
             *reinterpret_cast<float4*>(queries + 4 * u) =
@@ -685,7 +686,7 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const
             m[h] = kLowest;
             l[h] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < kV; ++i) acc[h][i][0] = acc[h][i][1] = acc[h][i][2] = acc[h][i][3] = 0.0f;
+            for (int i = 0; i < kV; ++i) acc[h][i][0] = acc[h][i][1] = make_float2(0.0f, 0.0f);
         }
         __syncwarp();
         int stage = 0;
@@ -693,16 +694,22 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const
             if (feed.ready(stage)) {
                 const char* keys = mine + stage * Feed<float, D>::kStageBytes + token * Feed<float, D>::kRowBytes;
                 const char* values = mine + stage * Feed<float, D>::kStageBytes + Feed<float, D>::kGroupBytes;
-                float x[kH] = {};
-#pragma unroll 4
+                float2 sums2[kH];
+#pragma unroll
+                for (int h = 0; h < kH; ++h) sums2[h] = make_float2(0.0f, 0.0f);
+#pragma unroll 8
                 for (int i = 0; i < kPieces; i += 2) {
                     const float4 k = *reinterpret_cast<const float4*>(keys + (((i + half) ^ (token & 7)) << 4));
 #pragma unroll
                     for (int h = 0; h < kH; ++h) {
                         const float4 q = *reinterpret_cast<const float4*>(queries + h * D + 4 * (i + half));
-                        x[h] = fmaf(q.w, k.w, fmaf(q.z, k.z, fmaf(q.y, k.y, fmaf(q.x, k.x, x[h]))));
+                        sums2[h] = __ffma2_rn(make_float2(q.x, q.y), make_float2(k.x, k.y), sums2[h]);
+                        sums2[h] = __ffma2_rn(make_float2(q.z, q.w), make_float2(k.z, k.w), sums2[h]);
                     }
                 }
+                float x[kH];
+#pragma unroll
+                for (int h = 0; h < kH; ++h) x[h] = sums2[h].x + sums2[h].y;
                 const int t = g * kGroup + token;
                 const bool unseen = t < s.span.lo || t > s.span.pos;
                 float high[kH];
@@ -727,7 +734,7 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const
 #pragma unroll
                         for (int i = 0; i < kV; ++i)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[h][i][e] *= k;
+                            for (int e = 0; e < 2; ++e) acc[h][i][e] = __fmul2_rn(acc[h][i][e], make_float2(k, k));
                     }
                 }
 #pragma unroll
@@ -737,21 +744,27 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const
                     if (half == 0) weights[token * kH + h] = x[h];
                 }
                 __syncwarp();
-#pragma unroll 4
+#pragma unroll 8
                 for (int u = 0; u < kGroup; ++u) {
                     float4 v[kV];
 #pragma unroll
                     for (int i = 0; i < kV; ++i)
                         v[i] = *reinterpret_cast<const float4*>(values + u * Feed<float, D>::kRowBytes + (((lane % kPieces + 32 * i) ^ (u & 7)) << 4));
+                    float w[kH];
+                    if constexpr (kH >= 4) {
+#pragma unroll
+                        for (int h = 0; h < kH; h += 4) *reinterpret_cast<float4*>(w + h) = *reinterpret_cast<const float4*>(weights + u * kH + h);
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < kH; ++h) w[h] = weights[u * kH + h];
+                    }
 #pragma unroll
                     for (int h = 0; h < kH; ++h) {
-                        const float w = weights[u * kH + h];
+                        const float2 pair = make_float2(w[h], w[h]);
 #pragma unroll
                         for (int i = 0; i < kV; ++i) {
-                            acc[h][i][0] = fmaf(w, v[i].x, acc[h][i][0]);
-                            acc[h][i][1] = fmaf(w, v[i].y, acc[h][i][1]);
-                            acc[h][i][2] = fmaf(w, v[i].z, acc[h][i][2]);
-                            acc[h][i][3] = fmaf(w, v[i].w, acc[h][i][3]);
+                            acc[h][i][0] = __ffma2_rn(pair, make_float2(v[i].x, v[i].y), acc[h][i][0]);
+                            acc[h][i][1] = __ffma2_rn(pair, make_float2(v[i].z, v[i].w), acc[h][i][1]);
                         }
                     }
                 }
@@ -776,10 +789,10 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const
                 const int e = 4 * lane + 128 * i;
                 if (e >= D) continue;
                 if (!whole)
-                    *reinterpret_cast<float4*>(slot + h * D + e) = make_float4(acc[h][i][0], acc[h][i][1], acc[h][i][2], acc[h][i][3]);
+                    *reinterpret_cast<float4*>(slot + h * D + e) = make_float4(acc[h][i][0].x, acc[h][i][0].y, acc[h][i][1].x, acc[h][i][1].y);
                 else if (e < d)
                     *reinterpret_cast<float4*>(out + e) =
-                        make_float4(acc[h][i][0] * inverse, acc[h][i][1] * inverse, acc[h][i][2] * inverse, acc[h][i][3] * inverse);
+                        make_float4(acc[h][i][0].x * inverse, acc[h][i][0].y * inverse, acc[h][i][1].x * inverse, acc[h][i][1].y * inverse);
             }
             if (!whole && lane == 0) {
                 slot[kF32Heads * D + h] = m[h] * kLog2e;
