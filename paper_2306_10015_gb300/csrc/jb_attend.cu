@@ -40,6 +40,7 @@ struct Params {
     Attend a;
     int blocks;        // blocks of query heads to a key head
     int page_groups;   // groups in a page
+    float cap_in, cap_out;  // softcap: 2 scale / (cap ln 2) of the score's exponent, cap / ln 2
 };
 
 // Partial results of a stretch: o[heads][D], m[heads], s[heads], for the query heads that are worked on
@@ -420,19 +421,19 @@ struct Feed {
     }
 };
 
-// The score as the softmax takes it, in units of ln 2.
+// The score as the softmax takes it, in units of ln 2, as is the slope.
 template <bool kExtra>
 __device__ __forceinline__ float score(const Params& p, float dot, float slope, int back) {
     if constexpr (!kExtra) {
         return dot * (p.a.scale * kLog2e);
     } else {
-        float x = dot * p.a.scale;
+        float x = dot * (p.a.scale * kLog2e);
         if (p.a.softcap > 0.0f) {
             // tanh(y) = 1 - 2 / (1 + e^2y): absolute error of a few 2^-24 of the cap
-            const float e = exp2_approx(x / p.a.softcap * (2.0f * kLog2e));
-            x = p.a.softcap * (1.0f - __fdividef(2.0f, 1.0f + e));
+            const float e = exp2_approx(dot * p.cap_in);
+            x = fmaf(-2.0f * p.cap_out, __fdividef(1.0f, 1.0f + e), p.cap_out);
         }
-        return fmaf(slope, static_cast<float>(back), x) * kLog2e;
+        return fmaf(slope, static_cast<float>(back), x);
     }
 }
 
@@ -505,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, kBf16Ctas<D, kH>) attend_bf16_kernel
 #pragma unroll
             for (int i = 0; i < 2 * kS; ++i)
                 q[i / 2][(i & 1) * kR + h] = real && 8 * i < d ? *reinterpret_cast<const uint32_t*>(qp + 8 * h * p.a.q_head + 8 * i) : 0;
-            slope[h] = kExtra && p.a.slopes != nullptr && real ? p.a.slopes[head0 + r + 8 * h] : 0.0f;
+            slope[h] = kExtra && p.a.slopes != nullptr && real ? p.a.slopes[head0 + r + 8 * h] * kLog2e : 0.0f;
         }
         float acc[kPieces][4], m[kR], l[kR];
 #pragma unroll
@@ -867,7 +868,8 @@ uint64_t attend_workspace(int bf16, int, int group, int head_dim) {
 }
 
 cudaError_t launch_attend(const Pages& pages, const Attend& a, cudaStream_t s) {
-    const Params p = {pages, a, 1, pages.page_tokens / kGroup};
+    const float cap = a.softcap > 0.0f ? a.softcap : 1.0f;
+    const Params p = {pages, a, 1, pages.page_tokens / kGroup, 2.0f * a.scale / cap * kLog2e, cap * kLog2e};
     switch (padded(a.head_dim)) {
         case 64: return launch_d<64>(p, s);
         case 128: return launch_d<128>(p, s);

@@ -103,11 +103,18 @@ __device__ __forceinline__ V block_exclusive(V v, V* sums, V& total) {
     return in - v + (warp == 0 ? V(0) : before);
 }
 
-// Adds to to[at] in shared memory without a branch.
-__device__ __forceinline__ void add_if(bool really, uint32_t* to, uint32_t at, uint32_t v) {
-    const uint32_t p = static_cast<uint32_t>(__cvta_generic_to_shared(to)) + 4 * at;
-    asm volatile("{.reg .pred p; setp.ne.u32 p, %2, 0; @p red.shared.add.u32 [%0], %1;}" ::"r"(p), "r"(v), "r"(really ? 1 : 0) : "memory");
+// Adds to to[at] in shared memory if b < limit, without a branch.
+__device__ __forceinline__ void add_below(float b, float limit, uint32_t to, uint32_t v) {
+    asm volatile("{.reg .pred p; setp.lt.f32 p, %0, %1; @p red.shared.add.u32 [%2], %3;}" ::"f"(b), "f"(limit), "r"(to), "r"(v) : "memory");
 }
+// The halves of a weight; few have an upper one.
+__device__ __forceinline__ void add_halves_below(float b, float limit, uint32_t low, uint32_t high, uint32_t w) {
+    asm volatile(
+        "{.reg .pred p, q; setp.lt.f32 p, %0, %1; setp.ne.and.u32 q, %5, 0, p;"
+        "@p red.shared.add.u32 [%2], %4; @q red.shared.add.u32 [%3], %5;}" ::"f"(b), "f"(limit), "r"(low), "r"(high), "r"(w & 0xFFFFu), "r"(w >> 16)
+        : "memory");
+}
+__device__ __forceinline__ uint32_t shared_address(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 
 // A token's place in the order as a number: larger comes first.
 __device__ __forceinline__ u64 place_of(uint32_t key, uint32_t index) { return static_cast<u64>(key) << 32 | ~index; }
@@ -151,7 +158,7 @@ struct Shared {
     int counts[32];
     float top;
     int total_count, listed, index;
-    u64 total_mass, beyond;                          // beyond: weight of what no bin holds
+    u64 total_mass, all;                             // of the bins; of all tokens
     uint32_t least, most;                            // keys of the bin's tokens
     Crossing crossing;
     u64 cut, cut_mass;
@@ -215,39 +222,36 @@ struct Draw {
     // Counts of the bins need no weights: a token without weight only follows all others.
     template <bool kCounts, bool kMasses>
     __device__ __forceinline__ void fill(const Among& a) {
-        u64 beyond = 0;
+        constexpr float kLimit = static_cast<float>(kBins);
+        const uint32_t counts = shared_address(sh.count), lows = shared_address(sh.low), highs = shared_address(sh.high);
+        u64 all = 0;
         each_unit([&](const float (&x)[kUnit], int j) {
             if (a.bins == kByScore && a.last == 0) {  // all tokens
 #pragma unroll
                 for (int i = 0; i < kUnit; ++i) {
-                    const float y = r.scaled(x[i]), b = y * a.scale;
-                    const bool binned = b < static_cast<float>(kBins);  // NaN is in no bin
-                    const uint32_t at = static_cast<uint32_t>(b);
-                    if constexpr (kCounts) add_if(binned, &sh.count[0], at, 1);
+                    const float y = r.scaled(x[i]), b = y * a.scale;  // NaN is in no bin
+                    const uint32_t at = 4 * static_cast<uint32_t>(b);
+                    if constexpr (kCounts) add_below(b, kLimit, counts + at, 1);
                     if constexpr (kMasses) {
                         const uint32_t w = Row::weight_of(y);
-                        add_if(binned, &sh.low[0], at, w & 0xFFFFu);
-                        add_if(binned && w >> 16 != 0, &sh.high[0], at, w >> 16);  // few
-                        beyond += binned ? 0 : w;
+                        add_halves_below(b, kLimit, lows + at, highs + at, w);
+                        all += w;
                     }
                 }
             } else {
                 each_set(near(a, x), j, [&](float v, int index) {
-                    const int b = bin_of(a, v, index);
-                    const bool binned = b >= 0 && b < kBins;
-                    if constexpr (kCounts) add_if(binned, &sh.count[0], b, 1);
-                    if constexpr (kMasses) {
-                        const uint32_t w = r.weight(v);
-                        add_if(binned, &sh.low[0], b, w & 0xFFFFu);
-                        add_if(binned, &sh.high[0], b, w >> 16);
-                    }
+                    const int bin = bin_of(a, v, index);
+                    const float b = bin < 0 ? kLimit : static_cast<float>(bin);
+                    const uint32_t at = 4u * static_cast<uint32_t>(bin);
+                    if constexpr (kCounts) add_below(b, kLimit, counts + at, 1);
+                    if constexpr (kMasses) add_halves_below(b, kLimit, lows + at, highs + at, r.weight(v));
                 });
             }
         });
         if constexpr (kMasses) {
 #pragma unroll
-            for (int d = 16; d > 0; d /= 2) beyond += __shfl_xor_sync(kAll, beyond, d);
-            if ((threadIdx.x & 31) == 0 && beyond > 0) atomicAdd(&sh.beyond, beyond);
+            for (int d = 16; d > 0; d /= 2) all += __shfl_xor_sync(kAll, all, d);
+            if ((threadIdx.x & 31) == 0 && all > 0) atomicAdd(&sh.all, all);
         }
     }
 
@@ -266,7 +270,7 @@ struct Draw {
 
     __device__ Crossing find(const Among& a, bool counts, bool masses, const Goal& g) {
         for (int i = threadIdx.x; i < kBins; i += kThreads) sh.count[i] = sh.low[i] = sh.high[i] = 0;
-        if (threadIdx.x == 0) sh.beyond = 0;
+        if (threadIdx.x == 0) sh.all = 0;
         __syncthreads();
         if (counts && masses) fill<true, true>(a);
         else if (masses) fill<false, true>(a);
@@ -310,7 +314,7 @@ struct Draw {
         const int all_count = counts ? sum_to(real ? other.total_count : 0, rank, before) : 0;
         const u64 binned = masses ? sum_to(real ? other.total_mass : 0, rank, mass_before) : 0;
         u64 none = 0;
-        const u64 all_mass = masses ? binned + sum_to(real ? other.beyond : 0, 0, none) : 0;
+        const u64 all_mass = g.kind == kShare ? sum_to(real ? other.all : 0, 0, none) : binned;
         const bool tokens = g.kind == kTokens;
         const u64 goal = g.kind == kShare ? share_of(g.share, all_mass) : g.value;
         const auto tell = [&](const Crossing& x) {
@@ -455,7 +459,11 @@ struct Draw {
     __device__ __forceinline__ unsigned candidates(const float(&x)[kUnit], float least_x, float least_y) const {
         unsigned mask = 0;
 #pragma unroll
-        for (int i = 0; i < kUnit; ++i) mask |= x[i] >= least_x && r.scaled(x[i]) >= least_y ? 1u << i : 0u;
+        for (int i = 0; i < kUnit; ++i) mask |= x[i] >= least_x ? 1u << i : 0u;
+        if (least_y > -INFINITY) {
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i) mask &= r.scaled(x[i]) >= least_y ? ~0u : ~(1u << i);
+        }
         return mask;
     }
 
