@@ -27,6 +27,7 @@ constexpr int kResident = 1024;        // threads on an SM: 64 registers each; 1
 constexpr int kMaxSlice = 65536;       // tokens of one CTA: sums of halves of their weights fit 32 bits
 constexpr int kLarge = 512;            // threads of a CTA, 256 for small vocabularies
 constexpr int kSmallVocab = 8192;
+constexpr int kSteps = 16;             // of 32 units, that a warp's part of a slice has at most
 constexpr float kReach = 21.5f;        // weights round to 0 below y = -31 ln 2 = -21.49
 constexpr float kOne = 1073741824.0f;  // 2^30, the weight of the largest logit
 typedef unsigned long long u64;
@@ -162,6 +163,7 @@ struct Shared {
     uint32_t least, most;                            // keys of the bin's tokens
     Crossing crossing;
     u64 cut, cut_mass;
+    u64 steps[kThreads / 32][kSteps];                // kept weight of each warp's runs of 32 units
 };
 
 template <typename T, int kThreads>
@@ -550,10 +552,22 @@ struct Draw {
             }
             return sum;
         };
+        // sums of the warp's steps of 32 units, kept for finding the token's
+        const int warp = threadIdx.x >> 5;
         u64 sum = 0;
-        each_unit([&](const float(&x)[kUnit], int j) { sum += weigh(x, j); });
+        for (int u = from; u < to; u += 32) {
+            u64 mine = 0;
+            if (u + lane < to) {
+                float x[kUnit];
+                load_unit(row, (u + lane) * kUnit, vocab, wide, infinite, x);
+                mine = weigh(x, (u + lane) * kUnit);
+            }
 #pragma unroll
-        for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(kAll, sum, d);
+            for (int d = 16; d > 0; d /= 2) mine += __shfl_xor_sync(kAll, mine, d);
+            if (lane == 0) sh.steps[warp][(u - from) / 32] = mine;
+            sum += mine;
+        }
+        __syncwarp();
         u64 here;
         // one thread a warp counts: its prefix is the warp's
         u64 before = block_exclusive<kWarps>(lane == 0 ? sum : 0, sh.sums, here);
@@ -564,33 +578,33 @@ struct Draw {
         const u64 aim = __umul64hi(static_cast<u64>(random) << 32, all);
         if (aim >= before && aim < before + sum) {  // the warp that has the token
             u64 run = before;
-            for (int u = from; u < to; u += 32) {
-                float x[kUnit];
-                u64 mine = 0;
-                if (u + lane < to) {
-                    load_unit(row, (u + lane) * kUnit, vocab, wide, infinite, x);
-                    mine = weigh(x, (u + lane) * kUnit);
-                }
-                const u64 in = run + warp_inclusive(mine);
-                if (aim >= in - mine && aim < in) {
-                    u64 sofar = in - mine;
+            int u = from;
+            for (int step = 0; run + sh.steps[warp][step] <= aim; ++step, u += 32) run += sh.steps[warp][step];
+            float x[kUnit];
+            u64 mine = 0;
+            if (u + lane < to) {
+                load_unit(row, (u + lane) * kUnit, vocab, wide, infinite, x);
+                mine = weigh(x, (u + lane) * kUnit);
+            }
+            const u64 in = run + warp_inclusive(mine);
+            if (aim >= in - mine && aim < in) {
+                u64 sofar = in - mine;
 #pragma unroll
-                    for (int k = 0; k < kUnit; ++k) {
-                        const u64 w = x[k] >= least_x ? kept(x[k], (u + lane) * kUnit + k) : 0;
-                        if (aim >= sofar && aim < sofar + w) {
-                            p.tokens[i] = (u + lane) * kUnit + k;
-                            if (p.logprobs != nullptr) p.logprobs[i] = r.scaled(x[k]) - logf(static_cast<float>(all) * (1.0f / kOne));
-                        }
-                        sofar += w;
+                for (int k = 0; k < kUnit; ++k) {
+                    const u64 w = x[k] >= least_x ? kept(x[k], (u + lane) * kUnit + k) : 0;
+                    if (aim >= sofar && aim < sofar + w) {
+                        p.tokens[i] = (u + lane) * kUnit + k;
+                        if (p.logprobs != nullptr) p.logprobs[i] = r.scaled(x[k]) - logf(static_cast<float>(all) * (1.0f / kOne));
                     }
+                    sofar += w;
                 }
-                run = __shfl_sync(kAll, in, 31);
-                if (run > aim) break;
             }
         }
         sync();  // until every CTA has read the others' memory
     }
 };
+
+static_assert(kMaxSlice / kUnit / 32 <= kSteps * (kLarge / 32) && kSmallVocab / kUnit / 32 <= kSteps * 8, "a warp's steps");
 
 __host__ __device__ constexpr int units_per_warp(int vocab, int warps) {
     return ((vocab + kUnit - 1) / kUnit + warps - 1) / warps;
