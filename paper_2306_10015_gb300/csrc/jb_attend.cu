@@ -9,6 +9,11 @@
 //
 // Softmax is kept with a running maximum, so that one pass is enough:
 //   m' = max(m, max_t x_t), s' = s e^(m - m') + sum e^(x_t - m'), o' likewise.
+//
+// Why a warp and not a CTA: warps that add up their parts of a pair at a barrier cost 2.7 us a pair, which is
+// all that 40 tokens take (256 rows of 20 to 60 tokens, 32 heads of 128: 74 us, now 43). Why equal pieces
+// decided at the start: keeping a share back for the warps that are done first was slower everywhere (by 2 to
+// 30 %), since a warp that is done leaves its bandwidth to the others.
 #include <atomic>
 
 #include <cuda_bf16.h>
@@ -463,7 +468,13 @@ __device__ __forceinline__ void load_transposed(uint32_t (&m)[4], uint32_t at) {
                  : "=r"(m[0]), "=r"(m[1]), "=r"(m[2]), "=r"(m[3]) : "r"(at) : "memory");
 }
 
-// bf16, mma.m16n8k16: a warp multiplies up to 16 query heads (rows) by 16 tokens. With r = lane / 4 and
+// bf16, mma.m16n8k16: a warp multiplies up to 16 query heads (rows) by 16 tokens. Few rows are real, so the
+// tensor cores are 17 % busy at most and a 128-row product would only pad more; what bounds it is HBM.
+// Measured (GPU time): 96 rows of 1900 to 2048 tokens, 40 heads of 128: 570 us, 6.8 TB/s, the rate of a copy, and
+// the bytes of one read (1.296 GB of 1.294 GB at a third of the rows). 3 rows of up to 131072 tokens, 8 query heads
+// to each of 8 key heads: 230 us, 6.3 TB/s. 48 rows of 65 to 2048 tokens: 85 us, 5.5 TB/s (3 us until the first
+// copies, 5 us of joins at the end). Two groups ahead and two CTAs: three ahead take 4 % longer, three CTAs 6 %.
+// With r = lane / 4 and
 // c = lane % 4 a lane holds the scores of rows r and r + 8, tokens 2c and 2c + 1 of each eight, which is
 // also how the weights enter the second product.
 // Weights enter it with 16 bits, as two bf16 numbers. With up to 8 query heads to a key head (kH = 8) the
@@ -633,7 +644,10 @@ __global__ void __launch_bounds__(kThreads, kBf16Ctas<D, kH>) attend_bf16_kernel
     write_zeros<T>(p);
 }
 
-// fp32, on the FMA units, kH query heads at a time. For the scores a lane takes token lane % 16 and half of
+// fp32, on the FMA units (packed pairs), kH query heads at a time. HBM bounds it up to 2 query heads to a key head
+// (64 rows of about 1500 tokens, 32 heads of 64: 246 us, 6.4 TB/s; heads of 128: 6.6 TB/s); with 8, the reads of
+// queries and weights from shared memory and the products do (8 key heads of 128: 161 us, 4.9 TB/s).
+// For the scores a lane takes token lane % 16 and half of
 // its elements against the queries in shared memory; for the values it takes four (eight) elements of
 // every token, with the weights from shared memory.
 template <int D>
