@@ -62,7 +62,7 @@
  * tensors). The library copies the host arrays it is given (segments, seeds,
  * codes) during the call, keeps no pointer to them, allocates no device
  * memory and holds no state between calls other than a per-device cache of
- * the SM count. Work is enqueued on `stream` (a cudaStream_t; NULL is the
+ * the SM count and of how many CTAs of a kernel run at once. Work is enqueued on `stream` (a cudaStream_t; NULL is the
  * legacy default stream) and the call returns without waiting for it. Calls on
  * different streams that touch the same parameters race.
  *

@@ -22,27 +22,29 @@ constexpr int kPlanThreads = 1024;
 constexpr int kPlanWarps = kPlanThreads / 32;
 constexpr unsigned kAll = 0xFFFFFFFFu;
 
-__device__ __forceinline__ int warp_inclusive(int v) {
+template <typename V>
+__device__ __forceinline__ V warp_inclusive(V v) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
-        const int o = __shfl_up_sync(kAll, v, d);
+        const V o = __shfl_up_sync(kAll, v, d);
         if (lane >= d) v += o;
     }
     return v;
 }
 
 // Exclusive prefix of v over the CTA's threads; `total` is the sum. sums: kPlanWarps words.
-__device__ __forceinline__ int block_exclusive(int v, int* sums, int& total) {
+template <typename V>
+__device__ __forceinline__ V block_exclusive(V v, V* sums, V& total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int in = warp_inclusive(v);
+    const V in = warp_inclusive(v);
     if (lane == 31) sums[warp] = in;
     __syncthreads();
-    const int all = warp_inclusive(lane < kPlanWarps ? sums[lane] : 0);
-    const int before = __shfl_sync(kAll, all, warp == 0 ? 0 : warp - 1);
+    const V all = warp_inclusive(lane < kPlanWarps ? sums[lane] : V(0));
+    const V before = __shfl_sync(kAll, all, warp == 0 ? 0 : warp - 1);
     total = __shfl_sync(kAll, all, 31);
     __syncthreads();
-    return in - v + (warp == 0 ? 0 : before);
+    return in - v + (warp == 0 ? V(0) : before);
 }
 
 __device__ __forceinline__ int block_sum(int v, int* sums) {
@@ -162,6 +164,7 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(Pages p, const in
                                                                int* status) {
     extern __shared__ int dynamic[];
     __shared__ int sums[kPlanWarps];
+    __shared__ long long wide_sums[kPlanWarps];
     __shared__ int free_here;
     int* base = dynamic;
     unsigned* seen = reinterpret_cast<unsigned*>(dynamic + n);
@@ -172,11 +175,11 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(Pages p, const in
     // every CTA works the list out for itself
     clear_seen(seen, p.n_rows);
     __syncthreads();
-    int need_all = 0;
+    long long need_all = 0;  // rows of 2^27 pages may be asked for
     bool bad = false;
     for (int first = 0; first < n; first += kPlanThreads) {
         const int i = first + threadIdx.x;
-        int need = 0;
+        long long need = 0;
         if (i < n) {
             const int row = rows[i], more = tokens[i];
             if (row < 0 || row >= p.n_rows || more < 0 || seen_before(seen, row)) {
@@ -188,20 +191,19 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(Pages p, const in
                 else need = pages_of(want, p.page_tokens) - pages_of(len, p.page_tokens);
             }
         }
-        int total;
-        const int at = need_all + block_exclusive(need, sums, total);
-        if (i < n) base[i] = at;
-        // more than all pages: the exact number no longer matters, but it must not wrap
-        need_all = min(need_all + total, 0x3FFFFFFF);
+        long long total;
+        const long long at = need_all + block_exclusive(need, wide_sums, total);
+        if (i < n) base[i] = static_cast<int>(min(at, 0x7FFFFFFFll));  // looked at if all are fewer than the pages
+        need_all += total;
     }
     bad = __syncthreads_or(bad);
     const Slice s = slice_of(team, p.n_pages, sums, &free_here, [&](int i) { return p.refs[i] == 0; });
     if (bad || need_all > s.total) {
-        if (team.rank == 0 && threadIdx.x == 0) *status = bad ? -1 : need_all - s.total;
+        if (team.rank == 0 && threadIdx.x == 0) *status = bad ? -1 : static_cast<int>(min(need_all - s.total, 0x7FFFFFFFll));
         team.sync();  // until every CTA's memory has been read
         return;
     }
-    ranked(s.lo, s.hi, s.before, need_all, sums, [&](int page) { return p.refs[page] == 0; },
+    ranked(s.lo, s.hi, s.before, static_cast<int>(need_all), sums, [&](int page) { return p.refs[page] == 0; },
            [&](int page, int rank) {
                const int i = owner_of(base, n, rank);
                const int row = rows[i];

@@ -143,16 +143,9 @@ struct Crossing {
     u64 goal;
 };
 
-// What a prefix of the order has to reach: tokens, a weight, or a share of all weights.
-enum Kind { kTokens, kWeight, kShare };
-struct Goal {
-    Kind kind;
-    u64 value;
-    double share;
-};
-
-__device__ __forceinline__ u64 share_of(double share, u64 mass) {
-    return max(1ull, static_cast<u64>(ceil(fmax(share, 0.0) * static_cast<double>(mass))));
+// The weight that a share of top_p of a weight is.
+__device__ __forceinline__ u64 share_of(float top_p, u64 mass) {
+    return max(1ull, static_cast<u64>(ceil(fmax(static_cast<double>(top_p), 0.0) * static_cast<double>(mass))));
 }
 
 template <int kThreads>
@@ -169,6 +162,14 @@ struct Shared {
     Crossing crossing;
     u64 cut, cut_mass;
     u64 steps[kThreads / 32][kSteps];                // kept weight of each warp's runs of 32 units
+};
+
+// A row's settings.
+struct Settings {
+    const Sample& p;
+    int row, top_k;
+    float top_p;
+    uint32_t least, random;  // the least weight (min_p), the word
 };
 
 template <typename T, int kThreads>
@@ -275,13 +276,13 @@ struct Draw {
         return __shfl_sync(kAll, in, kMaxCluster - 1);
     }
 
-    __device__ Crossing find(const Among& a, bool counts, bool masses, const Goal& g) {
+    // Where the tokens' number (kCounts) or else their weight reaches `goal` (0: a share of top_p of all weights).
+    template <bool kCounts, bool kMasses>
+    __device__ Crossing find(const Among& a, u64 goal, float top_p) {
         for (int i = threadIdx.x; i < kBins; i += kThreads) sh.count[i] = sh.low[i] = sh.high[i] = 0;
         if (threadIdx.x == 0) sh.all = 0;
         __syncthreads();
-        if (counts && masses) fill<true, true>(a);
-        else if (masses) fill<false, true>(a);
-        else fill<true, false>(a);
+        fill<kCounts, kMasses>(a);
         sync();
         // each CTA joins a section of the bins, a thread a few in a row
         constexpr int kMost = kBins / kThreads;
@@ -298,8 +299,8 @@ struct Draw {
             mass[i] = 0;
             if (i < share && begin + i < section) {
                 for (int c = 0; c < ctas; ++c) {
-                    if (counts) count[i] += of(c).count[first + i];
-                    if (masses) mass[i] += of(c).low[first + i] + (static_cast<u64>(of(c).high[first + i]) << 16);
+                    if constexpr (kCounts) count[i] += of(c).count[first + i];
+                    if constexpr (kMasses) mass[i] += of(c).low[first + i] + (static_cast<u64>(of(c).high[first + i]) << 16);
                 }
             }
             n += count[i];
@@ -307,8 +308,8 @@ struct Draw {
         }
         int total_count = 0, before = 0;
         u64 total_mass = 0, mass_before = 0;
-        if (counts) before = block_exclusive<kWarps>(n, sh.counts, total_count);
-        if (masses) mass_before = block_exclusive<kWarps>(m, sh.sums, total_mass);
+        if constexpr (kCounts) before = block_exclusive<kWarps>(n, sh.counts, total_count);
+        if constexpr (kMasses) mass_before = block_exclusive<kWarps>(m, sh.sums, total_mass);
         if (threadIdx.x == 0) {
             sh.total_count = total_count;
             sh.total_mass = total_mass;
@@ -318,22 +319,20 @@ struct Draw {
         const int lane = threadIdx.x & 31;
         const Shared<kThreads>& other = of(min(lane, ctas - 1));
         const bool real = lane < ctas;
-        const int all_count = counts ? sum_to(real ? other.total_count : 0, rank, before) : 0;
-        const u64 binned = masses ? sum_to(real ? other.total_mass : 0, rank, mass_before) : 0;
+        const int all_count = kCounts ? sum_to(real ? other.total_count : 0, rank, before) : 0;
+        const u64 binned = kMasses ? sum_to(real ? other.total_mass : 0, rank, mass_before) : 0;
         u64 none = 0;
-        const u64 all_mass = g.kind == kShare ? sum_to(real ? other.all : 0, 0, none) : binned;
-        const bool tokens = g.kind == kTokens;
-        const u64 goal = g.kind == kShare ? share_of(g.share, all_mass) : g.value;
+        if (goal == 0) goal = share_of(top_p, sum_to(real ? other.all : 0, 0, none));
         const auto tell = [&](const Crossing& x) {
             for (int c = 0; c < ctas; ++c) of(c).crossing = x;
         };
-        if ((tokens ? static_cast<u64>(all_count) : binned) < goal) {
-            if (rank == 0 && threadIdx.x == 0) tell({-1, all_count, all_mass, goal});
+        if ((kCounts ? static_cast<u64>(all_count) : binned) < goal) {
+            if (rank == 0 && threadIdx.x == 0) tell({-1, all_count, binned, goal});
         } else {
 #pragma unroll
             for (int i = 0; i < kMost; ++i) {
-                const u64 x = tokens ? static_cast<u64>(before) : mass_before;
-                const u64 y = x + (tokens ? static_cast<u64>(count[i]) : mass[i]);
+                const u64 x = kCounts ? static_cast<u64>(before) : mass_before;
+                const u64 y = x + (kCounts ? static_cast<u64>(count[i]) : mass[i]);
                 if (x < goal && y >= goal) tell({first + i, before, mass_before, goal});
                 before += count[i];
                 mass_before += mass[i];
@@ -343,8 +342,9 @@ struct Draw {
         return sh.crossing;
     }
 
-    // The bin's tokens: their number, or more than kThreads if they do not fit the first CTA's list.
-    __device__ int collect(const Among& a, int bin) {
+    // The bin's tokens (with all_before, and those of the bins before, by score): their number, or more than
+    // kThreads if they do not fit the first CTA's list.
+    __device__ int collect(const Among& a, int bin, bool all_before) {
         if (threadIdx.x == 0) {
             sh.listed = 0;
             sh.least = 0xFFFFFFFFu;
@@ -355,7 +355,7 @@ struct Draw {
         each_unit([&](const float (&x)[kUnit], int j) {
             unsigned mask = 0;
             if (a.bins == kByScore) {  // the bin's edges, in the same arithmetic
-                const float from = static_cast<float>(bin), to = static_cast<float>(bin + 1);
+                const float from = all_before ? 0.0f : static_cast<float>(bin), to = static_cast<float>(bin + 1);
 #pragma unroll
                 for (int i = 0; i < kUnit; ++i) {
                     const float b = r.scaled(x[i]) * a.scale;
@@ -365,7 +365,8 @@ struct Draw {
                 mask = near(a, x);
             }
             each_set(mask, j, [&](float v, int index) {
-                if (bin_of(a, v, index) != bin) return;
+                const int b = bin_of(a, v, index);
+                if (b != bin && !(all_before && b >= 0 && b < bin)) return;
                 const uint32_t key = key_of(v);
                 least = min(least, key);
                 most = max(most, key);
@@ -385,25 +386,31 @@ struct Draw {
         return __reduce_add_sync(kAll, lane < ctas ? min(of(min(lane, ctas - 1)).listed, kThreads + 1) : 0);
     }
 
+    // The first CTA: the place of the thread's token in the order of the n that are listed; 0 past them.
+    __device__ __forceinline__ u64 ranked(int n) {
+        const int i = threadIdx.x;
+        u64 place = 0;
+        if (i < n) {
+            int at = i, c = 0;
+            while (at >= of(c).listed) at -= of(c++).listed;
+            place = of(c).list[at];
+            sh.order[i] = place;
+        }
+        __syncthreads();
+        int before = 0;
+        for (int j = 0; j < n; ++j) before += sh.order[j] > place ? 1 : 0;
+        __syncthreads();
+        if (i < n) sh.order[before] = place;
+        __syncthreads();
+        return i < n ? sh.order[i] : 0;
+    }
+
     // Ranks the n listed tokens and tells every CTA the place of the one that reaches the goal, `count`
     // tokens of weight `mass` being before them.
     __device__ void choose(int n, bool tokens, u64 goal, u64 count, u64 mass) {
         if (rank == 0) {
             const int i = threadIdx.x;
-            u64 place = 0;
-            if (i < n) {
-                int at = i, c = 0;
-                while (at >= of(c).listed) at -= of(c++).listed;
-                place = of(c).list[at];
-                sh.order[i] = place;
-            }
-            __syncthreads();
-            int before = 0;
-            for (int j = 0; j < n; ++j) before += sh.order[j] > place ? 1 : 0;
-            __syncthreads();
-            if (i < n) sh.order[before] = place;
-            __syncthreads();
-            place = i < n ? sh.order[i] : 0;
+            const u64 place = ranked(n);
             const u64 w = i < n ? r.weight(logit_of(static_cast<uint32_t>(place >> 32))) : 0;
             u64 all;
             const u64 x = block_exclusive<kWarps>(w, sh.sums, all);
@@ -418,48 +425,103 @@ struct Draw {
         sync();
     }
 
-    // The last place of the shortest prefix of the order that reaches the goal, among the places from
-    // `last` on, and the prefix's weight. Place 0 if all together do not reach it. `reach`: the goal is
-    // expected within this much below the largest y.
-    __device__ void end_of(u64 last, float reach, bool masses, Goal g, u64& place, u64& weight) {
+    // The whole draw by the first CTA, where everything that is kept is among the n listed tokens: the first
+    // top_k, and of those what reaches `goal` (0: a share of top_p of them).
+    __device__ void draw_listed(const Settings& t, int n, int top_k, u64 goal) {
+        const int i = threadIdx.x;
+        const u64 place = ranked(n);
+        const float x = i < n ? logit_of(static_cast<uint32_t>(place >> 32)) : -INFINITY;
+        const uint32_t w = i < min(n, top_k) ? r.weight(x) : 0, index = ~static_cast<uint32_t>(place);
+        u64 mass, total;
+        const u64 before = block_exclusive<kWarps>(static_cast<u64>(w), sh.sums, mass);
+        if (goal == 0 && t.top_p < 1.0f) goal = share_of(t.top_p, mass);
+        const bool in = goal == 0 || before < goal;
+        const uint32_t kept = in && w >= t.least ? w : 0;
+        block_exclusive<kWarps>(static_cast<u64>(kept), sh.sums, total);
+        sh.list[i] = static_cast<u64>(index) << 32 | kept;  // of this CTA: all have been read
+        __syncthreads();
+        u64 run = 0;  // of kept tokens with a lower index
+        for (int j = 0; j < n; ++j) {
+            const u64 other = sh.list[j];
+            if (static_cast<uint32_t>(other >> 32) < index) run += static_cast<uint32_t>(other);
+        }
+        const u64 aim = __umul64hi(static_cast<u64>(t.random) << 32, total);
+        if (kept > 0 && run <= aim && aim < run + kept) {
+            t.p.tokens[t.row] = static_cast<int>(index);
+            if (t.p.logprobs != nullptr) t.p.logprobs[t.row] = r.scaled(x) - logf(static_cast<float>(total) * (1.0f / kOne));
+        }
+    }
+
+    // The end of what is kept by the number of tokens or else by weight: `last` is the place of its last token (0:
+    // nothing is cut off), `mass` its weight; both tell of an earlier end before. True if the draw is done.
+    template <bool kTokens>
+    __device__ __forceinline__ bool cut_off(const Settings& t, bool nucleus, bool counted, u64& last, u64& mass) {
+        // tokens more than ln(vocab / (1 - p)) below the largest together weigh less than 1 - p of it; 0.1
+        // for roundings, which are larger where weights are below five units
+        float reach = kTokens ? kReach : logf(static_cast<float>(vocab) / (1.0f - fmaxf(t.top_p, 0.0f))) + 0.1f;
+        if (!(reach < 19.0f)) reach = kReach;
+        u64 goal = kTokens ? static_cast<u64>(t.top_k) : counted ? share_of(t.top_p, mass) : 0;  // 0: known with the weights
         Among a = {~0ull, last, kByScore, -kBins / reach, 0, 0};
-        const bool tokens = g.kind == kTokens;
-        u64 count = 0, mass = 0;  // of what is before `a`
-        // by score, twice if it was not within reach; by key at most four times (32 bits, 10 at a time); by
-        // index, 256 to a bin: those fit
-        for (int round = 0; round < 7; ++round) {
-            const Crossing x = find(a, tokens, masses, g);
-            if (g.kind == kShare) g = {kWeight, x.goal, 0.0};
-            if (x.bin < 0 && a.bins == kByScore && reach < kReach) {
-                reach = kReach;
-                a.scale = -kBins / reach;
-                continue;
+        // where few are kept one list holds them all, ties apart, and the first CTA does the rest
+        bool whole = kTokens ? t.top_k <= kThreads / 2 : !counted;
+        int count = 0;  // of tokens before `a`, and their weight; `last` stays if the goal is not reached
+        mass = 0;
+        // by score, twice if it was not within reach or the list was not enough; by key at most four times (32
+        // bits, 10 at a time); by index, 256 to a bin: those fit
+        for (int round = 0; round < 8; ++round) {
+            const u64 left = goal == 0 ? 0 : goal - (kTokens ? count : mass);
+            Crossing x;
+            if (kTokens && (whole || !nucleus)) x = find<kTokens, !kTokens>(a, left, t.top_p);
+            else x = find<kTokens, true>(a, left, t.top_p);
+            if (goal == 0) goal = x.goal;
+            if (x.bin < 0) {
+                if (a.bins == kByScore && reach < kReach) {
+                    reach = kReach;
+                    a.scale = -kBins / reach;
+                    continue;
+                }
+                if (kTokens && whole && nucleus) {  // all are kept, and now their weight is wanted
+                    whole = false;
+                    continue;
+                }
+                mass += x.mass;
+                break;
+            }
+            // tokens before the bin weigh at least as much each as one on its upper edge: are they few?
+            if (!kTokens) whole = whole && static_cast<float>(x.mass) <= kThreads / 2 * kOne * expf(static_cast<float>(x.bin) / a.scale);
+            int n = collect(a, x.bin, whole);
+            if (whole) {
+                if (n <= kThreads) {
+                    if (rank == 0) draw_listed(t, n, kTokens ? t.top_k : vocab, kTokens ? 0 : goal);
+                    sync();  // until every CTA's memory has been read
+                    return true;
+                }
+                sync();
+                whole = false;
+                if (kTokens) continue;
+                n = collect(a, x.bin, false);
             }
             count += x.count;
             mass += x.mass;
-            if (x.bin < 0) break;
-            const int n = collect(a, x.bin);
             if (n <= kThreads) {
-                choose(n, tokens, tokens ? count - x.count + g.value : mass - x.mass + g.value, count, mass);
-                place = sh.cut;
-                weight = sh.cut_mass;
-                return;
+                choose(n, kTokens, goal, count, mass);
+                last = sh.cut;
+                mass = sh.cut_mass;
+                break;
             }
-            uint32_t least = 0xFFFFFFFFu, most = 0;
+            uint32_t lowest = 0xFFFFFFFFu, highest = 0;
             for (int c = 0; c < ctas; ++c) {
-                least = min(least, of(c).least);
-                most = max(most, of(c).most);
+                lowest = min(lowest, of(c).least);
+                highest = max(highest, of(c).most);
             }
             sync();  // read by all before it is set anew
-            g.value -= tokens ? static_cast<u64>(x.count) : x.mass;
-            a.first = min(a.first, place_of(most, 0));
-            a.last = max(a.last, place_of(least, 0xFFFFFFFFu));
-            a.key = most;
-            a.bins = least == most ? kByIndex : kByKey;
-            a.shift = least == most ? 8 : max(0, 22 - __clz(most - least));
+            a.first = min(a.first, place_of(highest, 0));
+            a.last = max(a.last, place_of(lowest, 0xFFFFFFFFu));
+            a.key = highest;
+            a.bins = lowest == highest ? kByIndex : kByKey;
+            a.shift = lowest == highest ? 8 : max(0, 22 - __clz(highest - lowest));
         }
-        place = 0;
-        weight = mass;
+        return false;
     }
 
     // Of the unit's tokens, which may be kept: at or above x, and with y at or above y.
@@ -527,15 +589,10 @@ struct Draw {
         const uint32_t least = min_p > 0.0f ? static_cast<uint32_t>(ceil(fmin(static_cast<double>(min_p), 1.0) * 1073741824.0)) : 0;
         u64 last = 0, mass = 0;
         const bool counted = top_k > 0 && top_k < vocab, nucleus = top_p < 1.0f;
-        if (counted) end_of(0, kReach, nucleus, {kTokens, static_cast<u64>(top_k), 0.0}, last, mass);
-        if (nucleus) {
-            // tokens more than ln(vocab / (1 - p)) below the largest together weigh less than 1 - p of it; 0.1
-            // for roundings, which are larger where weights are below five units
-            float reach = logf(static_cast<float>(vocab) / (1.0f - fmaxf(top_p, 0.0f))) + 0.1f;
-            if (!(reach < 19.0f)) reach = kReach;
-            const double share = static_cast<double>(top_p);
-            end_of(last, reach, true, counted ? Goal{kWeight, share_of(share, mass), 0.0} : Goal{kShare, 0, share}, last, mass);
-        }
+        // the end of what is kept, first by top_k and then, among that, by top_p
+        const Settings settings = {p, i, top_k, top_p, least, random};
+        if (counted && cut_off<true>(settings, nucleus, counted, last, mass)) return;
+        if (nucleus && cut_off<false>(settings, nucleus, counted, last, mass)) return;
 
         // what is kept; few tokens are where something is cut off, and only those are weighed
         const float least_x = last == 0 ? -INFINITY : logit_of(static_cast<uint32_t>(last >> 32));

@@ -244,6 +244,18 @@ def test_many_pages(n_pages):
     assert torch.equal(now[kept], rows[kept])
 
 
+def test_more_pages_asked_for_than_32_bits_count():
+    """Rows whose tables are long: the number that is missing is exact, or the largest there is."""
+    n, row_pages = 3, 1 << 27                              # 1.6 GB of table, rows of 2^31 - 16 tokens
+    pages = jb.PageTable(torch.full((n, row_pages - 1), -1, dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda"),
+                         torch.zeros(100, dtype=torch.int32, device="cuda"), 16)
+    most = 16 * (row_pages - 1)
+    assert jb.jb_cache_reserve(pages, i32([0, 1]), i32([most, 17])).item() == row_pages - 1 + 2 - 100
+    assert jb.jb_cache_reserve(pages, i32([0, 1, 2]), i32([most, most, most])).item() == 3 * (row_pages - 1) - 100
+    assert jb.jb_cache_reserve(pages, i32([0, 1]), i32([most, most + 1])).item() == -1
+    assert pages.lens.tolist() == [0, 0, 0] and (pages.refs == 0).all()
+
+
 def test_many_listed_rows():
     """As many rows as one call takes, forked from one another."""
     n = 16_384

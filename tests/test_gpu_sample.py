@@ -103,6 +103,19 @@ def test_vocabularies(dtype, V):
     check(x, top_p=0.97, min_p=0.003)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,V", [(1, 50_272), (5, 3001), (300, 9001)])
+@pytest.mark.parametrize("std", [1.0, 6.0, 30.0])
+def test_few_and_many_kept(dtype, n, V, std):
+    """Nuclei of a few tokens and of most of them, and top-k around what one list holds."""
+    x = logits_of(n, V, dtype, seed=3, std=std)
+    check(x, top_p=0.9)
+    check(x, top_p=0.999, min_p=0.01)
+    check(x, top_k=127, top_p=0.9)
+    check(x, top_k=128, min_p=0.02)
+    check(x, top_k=257, top_p=0.7)
+
+
 @pytest.mark.parametrize("n", [1, 2, 7, 63, 152, 153, 300, 1000])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_rows(n, dtype):
