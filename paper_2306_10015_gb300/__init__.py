@@ -413,6 +413,14 @@ class PageTable:
         self.struct = jb_pages(table.data_ptr(), lens.data_ptr(), refs.data_ptr(), table.shape[0],
                                table.shape[1], refs.shape[0], self.page_tokens)
         self.ref = ctypes.byref(self.struct)
+        self._bytes = {}
+
+    def workspace(self, n: int) -> int:
+        """Device bytes that jb_cache_fork of n pairs works in, or jb_cache_compact (n = 0)."""
+        nbytes = self._bytes.get(n)
+        if nbytes is None:
+            nbytes = self._bytes[n] = max(16, int(lib().jb_cache_workspace(self.ref, n)))
+        return nbytes
 
     @classmethod
     def empty(cls, n_rows: int, row_pages: int, n_pages: int, page_tokens: int, device="cuda") -> "PageTable":
@@ -420,6 +428,26 @@ class PageTable:
         return cls(torch.full((n_rows, row_pages), -1, dtype=torch.int32, device=device),
                    torch.zeros(n_rows, dtype=torch.int32, device=device),
                    torch.zeros(n_pages, dtype=torch.int32, device=device), page_tokens)
+
+
+class _Workspaces:
+    """Device bytes that calls work in: kept for each stream, and new for each call that a graph captures, since
+    the graph may be replayed on another stream."""
+
+    def __init__(self):
+        self.kept = {}
+
+    def get(self, key, nbytes: int, stream, handle, make):
+        """Address and bytes of at least `nbytes`, made by make(nbytes), and what holds them."""
+        if _new(stream, torch.cuda.is_current_stream_capturing):
+            ws = make(nbytes)
+            return ws.data_ptr(), nbytes, ws
+        key = key, handle.value
+        found = self.kept.get(key)
+        if found is None or found[1] < nbytes:
+            ws = make(nbytes)
+            found = self.kept[key] = ws.data_ptr(), nbytes, ws
+        return found
 
 
 class KVCache:
@@ -454,27 +482,28 @@ class KVCache:
         for i, (k, v) in enumerate(zip(self.keys, self.values)):
             self.layers[i] = jb_kv(k.data_ptr(), v.data_ptr(), first.stride(0), heads, d, self.dtype, by_token)
         self.layer_refs = [ctypes.byref(self.layers, i * ctypes.sizeof(jb_kv)) for i in range(n)]
-        self._workspaces = {}
+        self._workspaces, self._attend_bytes = _Workspaces(), {}
 
     def new_workspace(self, q_heads: int, stream=None):
         """A workspace for jb_attend with so many query heads: a uint8 tensor, ready for use on the stream."""
-        nbytes = int(lib().jb_attend_workspace(self.layer_refs[0], q_heads))
-        ws = _new(stream, torch.empty, max(nbytes, ATTEND_ZEROS), dtype=torch.uint8, device=self.keys[0].device)
+        return self._zeroed(max(int(lib().jb_attend_workspace(self.layer_refs[0], q_heads)), ATTEND_ZEROS), stream)
+
+    def _zeroed(self, nbytes, stream):
+        ws = _new(stream, torch.empty, nbytes, dtype=torch.uint8, device=self.keys[0].device)
         _new(stream, ws[:ATTEND_ZEROS].zero_)
         return ws
 
-    def _workspace(self, q_heads: int, stream, handle):
-        # one for each stream, and a new one for each call that a graph captures: the graph may be
-        # replayed on another stream
-        if _new(stream, torch.cuda.is_current_stream_capturing):
-            ws = self.new_workspace(q_heads, stream)
-            return ws.data_ptr(), ws.numel(), ws
-        key = handle.value, q_heads
-        found = self._workspaces.get(key)
-        if found is None:
-            ws = self.new_workspace(q_heads, stream)
-            found = self._workspaces[key] = ws.data_ptr(), ws.numel(), ws
-        return found
+    def _attend_workspace(self, q_heads: int, stream, handle):
+        nbytes = self._attend_bytes.get(q_heads)
+        if nbytes is None:
+            nbytes = max(int(lib().jb_attend_workspace(self.layer_refs[0], q_heads)), ATTEND_ZEROS)
+            self._attend_bytes[q_heads] = nbytes
+        return self._workspaces.get("attend", nbytes, stream, handle, lambda size: self._zeroed(size, stream))
+
+    def _pages_workspace(self, n: int, stream, handle):
+        nbytes = self.pages.workspace(n)
+        return self._workspaces.get("pages", nbytes, stream, handle,
+                                    lambda size: _new(stream, torch.empty, size, dtype=torch.uint8, device=self.keys[0].device))
 
 
 def _new(stream, make, *args, **kwargs):
@@ -491,11 +520,6 @@ def _status_of(status, like, stream):
     if _list32(status, "status")[1] != 1:
         raise ValueError("status must have one element")
     return status
-
-
-def _scratch(nbytes: int, like, stream):
-    """Device bytes for one call."""
-    return _new(stream, torch.empty, nbytes, dtype=torch.uint8, device=like.device)
 
 
 def jb_cache_reserve(cache, rows, tokens, status=None, stream=None):
@@ -522,10 +546,9 @@ def jb_cache_fork(cache: KVCache, parents, children, status=None, stream=None):
     pages = cache.pages
     pp, pc, n = _two_lists(parents, children, "parents and children")
     status = _status_of(status, pages.refs, stream)
-    nbytes = 0 if n == 0 else int(lib().jb_cache_workspace(pages.ref, n))
-    ws = _scratch(max(nbytes, 16), pages.refs, stream)
-    _check(lib().jb_cache_fork(pages.ref, cache.layers, cache.n_layers, pp, pc, n, status.data_ptr(),
-                               ws.data_ptr(), nbytes, _stream(stream)))
+    handle = _stream(stream)
+    ws, nbytes, held = cache._pages_workspace(n, stream, handle)
+    _check(lib().jb_cache_fork(pages.ref, cache.layers, cache.n_layers, pp, pc, n, status.data_ptr(), ws, nbytes, handle))
     return status
 
 
@@ -533,10 +556,9 @@ def jb_cache_compact(cache: KVCache, status=None, stream=None):
     """Moves the pages in use to the lowest ids; returns the status tensor: how many they are."""
     pages = cache.pages
     status = _status_of(status, pages.refs, stream)
-    nbytes = int(lib().jb_cache_workspace(pages.ref, 0))
-    ws = _scratch(max(nbytes, 16), pages.refs, stream)
-    _check(lib().jb_cache_compact(pages.ref, cache.layers, cache.n_layers, status.data_ptr(),
-                                  ws.data_ptr(), nbytes, _stream(stream)))
+    handle = _stream(stream)
+    ws, nbytes, held = cache._pages_workspace(0, stream, handle)
+    _check(lib().jb_cache_compact(pages.ref, cache.layers, cache.n_layers, status.data_ptr(), ws, nbytes, handle))
     return status
 
 
@@ -579,7 +601,7 @@ def jb_attend(cache: KVCache, layer: int, q, rows, pos, out=None, scale: Optiona
         raise ValueError("slopes must be a contiguous float32 CUDA tensor, one per query head")
     handle = _stream(stream)
     if workspace is None:
-        ws, nbytes, held = cache._workspace(heads, stream, handle)
+        ws, nbytes, held = cache._attend_workspace(heads, stream, handle)
     else:
         ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     scores = jb_scores(cache.head_dim ** -0.5 if scale is None else scale, softcap, window,
@@ -589,15 +611,15 @@ def jb_attend(cache: KVCache, layer: int, q, rows, pos, out=None, scale: Optiona
     return out
 
 
-def _per_row(value, default, n: int, dtype, device, stream):
-    """A setting of jb_sample as the address of n entries (None where it is the default) and the
-    tensor that holds them."""
-    if not isinstance(value, torch.Tensor):
+def _per_row(value, default, words, dtype, stream):
+    """A setting of jb_sample as the address of its entries (None where it is the default) and the tensor
+    that holds them, one for each of the words."""
+    if type(value) is not torch.Tensor and not isinstance(value, torch.Tensor):
         if value == default:
             return None, None
-        value = _new(stream, torch.full, (n,), value, dtype=dtype, device=device)
-    if value.dtype is not dtype or not value.is_cuda or value.shape != (n,) or not value.is_contiguous():
-        raise ValueError(f"a setting per row must be a contiguous {dtype} CUDA tensor of {n} entries")
+        value = _new(stream, torch.full, words.shape, value, dtype=dtype, device=words.device)
+    if value.dtype is not dtype or not value.is_cuda or value.shape != words.shape or not value.is_contiguous():
+        raise ValueError(f"a setting per row must be a contiguous {dtype} CUDA tensor of one entry per word")
     return value.data_ptr(), value
 
 
@@ -608,26 +630,30 @@ def jb_sample(logits, words, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tok
     per row (float32, top_k int32 CUDA tensors)."""
     if torch is None:
         _need_torch()
-    if logits.dim() != 2 or not logits.is_cuda or (logits.stride(1) != 1 and logits.shape[1] > 1):
-        raise ValueError("logits must be a CUDA tensor [n, vocab], contiguous in a row")
+    i32, f32 = torch.int32, torch.float32
+    if logits.dim() != 2 or not logits.is_cuda:
+        raise ValueError("logits must be a CUDA tensor [n, vocab]")
     n, vocab = logits.shape
-    if words.dtype not in (torch.int32, torch.uint32) or not words.is_cuda or words.shape != (n,) or not words.is_contiguous():
+    pitch, step = logits.stride()
+    if step != 1 and vocab > 1:
+        raise ValueError("logits must be contiguous in a row")
+    if (words.dtype is not i32 and words.dtype is not torch.uint32) or not words.is_cuda or words.dim() != 1 or words.numel() != n \
+            or not words.is_contiguous():
         raise ValueError("words must be a contiguous int32 or uint32 CUDA tensor, one per row")
-    dev = logits.device
-    t, t_ = _per_row(temperature, 1.0, n, torch.float32, dev, stream)
-    k, k_ = _per_row(top_k, 0, n, torch.int32, dev, stream)
-    p, p_ = _per_row(top_p, 1.0, n, torch.float32, dev, stream)
-    m, m_ = _per_row(min_p, 0.0, n, torch.float32, dev, stream)
+    t, t_ = _per_row(temperature, 1.0, words, f32, stream)
+    k, k_ = _per_row(top_k, 0, words, i32, stream)
+    p, p_ = _per_row(top_p, 1.0, words, f32, stream)
+    m, m_ = _per_row(min_p, 0.0, words, f32, stream)
     if tokens is None:
-        tokens = _new(stream, torch.empty, n, dtype=torch.int32, device=dev)
+        tokens = _new(stream, torch.empty_like, words, dtype=i32)
     elif _list32(tokens, "tokens")[1] != n:
         raise ValueError("one token per row")
     if logprobs is None:
-        logprobs = _new(stream, torch.empty, n, dtype=torch.float32, device=dev)
-    elif logprobs.dtype is not torch.float32 or not logprobs.is_cuda or logprobs.shape != (n,) or not logprobs.is_contiguous():
+        logprobs = _new(stream, torch.empty_like, words, dtype=f32)
+    elif logprobs.dtype is not f32 or not logprobs.is_cuda or logprobs.shape != words.shape or not logprobs.is_contiguous():
         raise ValueError("logprobs must be a contiguous float32 CUDA tensor, one per row")
     settings = jb_sampling(t, k, p, m)
-    _check(lib().jb_sample(logits.data_ptr(), logits.stride(0), _storage(logits.dtype), n, vocab, ctypes.byref(settings),
+    _check(lib().jb_sample(logits.data_ptr(), pitch, _storage(logits.dtype), n, vocab, ctypes.byref(settings),
                            words.data_ptr(), tokens.data_ptr(), logprobs.data_ptr(), _stream(stream)))
     return tokens, logprobs
 
