@@ -372,7 +372,7 @@ int jb_cache_write(const jb_pages* pages, const jb_kv* layer, const void* d_k, u
 /* What jb_attend does to the scores, besides their scale. */
 typedef struct {
     float scale;         /* x = scale q.k */
-    float softcap;       /* > 0: x = softcap tanh(x / softcap); 0: off */
+    float softcap;       /* > 0: x = softcap tanh(x / softcap), at most 1e30 and scale / softcap finite; 0: off */
     int32_t window;      /* > 0: only the last `window` positions are seen; 0: all */
     const float* slopes; /* device, one per query head: x += slope (t - pos); NULL: off */
 } jb_scores;

@@ -78,7 +78,7 @@ struct Attend {
     float scale, softcap;
     int window, n, heads, group, head_dim, bf16;
 };
-uint64_t attend_workspace(int bf16, int heads, int group, int head_dim);
+uint64_t attend_workspace(int bf16, int group, int head_dim);
 cudaError_t launch_attend(const Pages& p, const Attend& a, cudaStream_t s);
 
 struct Sample {

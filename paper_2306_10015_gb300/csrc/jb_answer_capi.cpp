@@ -204,7 +204,7 @@ JB_EXPORT int jb_cache_write(const jb_pages* pages, const jb_kv* layer, const vo
 JB_EXPORT uint64_t jb_attend_workspace(const jb_kv* layer, int q_heads) {
     if (layer == nullptr || layer->heads < 1 || q_heads < layer->heads || layer->head_dim < 1 || layer->head_dim > jb::kMaxHeadDim)
         return 0;
-    return jb::attend_workspace(layer->dtype == JB_BF16, layer->heads, q_heads / layer->heads, layer->head_dim);
+    return jb::attend_workspace(layer->dtype == JB_BF16, q_heads / layer->heads, layer->head_dim);
 }
 
 JB_EXPORT int jb_attend(const jb_pages* pages, const jb_kv* layer, const jb_scores* scores, const void* d_q,
@@ -218,6 +218,8 @@ JB_EXPORT int jb_attend(const jb_pages* pages, const jb_kv* layer, const jb_scor
         JB_TRY(check_layer(*layer, p));
         if (q_heads < 1 || q_heads > 65536 || q_heads % layer->heads != 0) return static_cast<int>(JB_ERR_INVALID_ARG);
         if (!std::isfinite(scores->scale) || !std::isfinite(scores->softcap) || scores->softcap < 0.0f || scores->window < 0)
+            return static_cast<int>(JB_ERR_INVALID_ARG);
+        if (scores->softcap > 0.0f && (scores->softcap > 1e30f || !std::isfinite(scores->scale / scores->softcap)))
             return static_cast<int>(JB_ERR_INVALID_ARG);
         JB_TRY(check_list(d_rows, d_pos, n, INT32_MAX));
         if (n == 0) return static_cast<int>(JB_OK);

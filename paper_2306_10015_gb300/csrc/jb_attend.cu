@@ -45,7 +45,7 @@ struct Params {
     Attend a;
     int blocks;        // blocks of query heads to a key head
     int page_groups;   // groups in a page
-    float cap_in, cap_out;  // softcap: 2 scale / (cap ln 2) of the score's exponent, cap / ln 2
+    float cap_in, cap_out;  // softcap: scale / cap, cap / ln 2
 };
 
 // Partial results of a stretch: o[heads][D], m[heads], s[heads], for the query heads that are worked on
@@ -434,9 +434,13 @@ __device__ __forceinline__ float score(const Params& p, float dot, float slope, 
     } else {
         float x = dot * (p.a.scale * kLog2e);
         if (p.a.softcap > 0.0f) {
-            // tanh(y) = 1 - 2 / (1 + e^2y): absolute error of a few 2^-24 of the cap
-            const float e = exp2_approx(dot * p.cap_in);
-            x = fmaf(-2.0f * p.cap_out, __fdividef(1.0f, 1.0f + e), p.cap_out);
+            // tanh(y) = 1 - 2 / (1 + e^2y), to a few 2^-24; near 0 that is not enough of a small y, and
+            // tanh(y) / y = 1 - y^2/3 + 2 y^4/15 - 17 y^6/315 is good to 6e-8 below 1/5
+            const float y = dot * p.cap_in, y2 = y * y;
+            const float e = exp2_approx(y * (2.0f * kLog2e));
+            const float large = fmaf(-2.0f * p.cap_out, __fdividef(1.0f, 1.0f + e), p.cap_out);
+            const float small = x * fmaf(y2, fmaf(y2, fmaf(y2, -17.0f / 315.0f, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
+            x = fabsf(y) < 0.2f ? small : large;
         }
         return fmaf(slope, static_cast<float>(back), x);
     }
@@ -876,14 +880,14 @@ int padded(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 
 
 }  // namespace
 
-uint64_t attend_workspace(int bf16, int, int group, int head_dim) {
+uint64_t attend_workspace(int bf16, int group, int head_dim) {
     const int heads = bf16 && group > 8 ? 16 : 8;
     return sizeof(float) * (counters() + 2ull * kMaxWorkers * slot_floats(heads, padded(head_dim)));
 }
 
 cudaError_t launch_attend(const Pages& pages, const Attend& a, cudaStream_t s) {
     const float cap = a.softcap > 0.0f ? a.softcap : 1.0f;
-    const Params p = {pages, a, 1, pages.page_tokens / kGroup, 2.0f * a.scale / cap * kLog2e, cap * kLog2e};
+    const Params p = {pages, a, 1, pages.page_tokens / kGroup, a.scale / cap, cap * kLog2e};
     switch (padded(a.head_dim)) {
         case 64: return launch_d<64>(p, s);
         case 128: return launch_d<128>(p, s);

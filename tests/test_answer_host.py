@@ -114,7 +114,7 @@ def test_bad_attention(jb):
                    (dict(rows=0), INV), (dict(pos=0), INV), (dict(qp=FAKE + 2), MIS), (dict(out=FAKE + 8), MIS), (dict(qa=260), MIS), (dict(ob=4), MIS),
                    (dict(ws=0), INV), (dict(ws=FAKE + 8), MIS), (dict(size=16), INV), (dict(qa=1 << 50), INV),
                    (dict(scores=s(nan, 0.0, 0, None)), INV), (dict(scores=s(inf, 0.0, 0, None)), INV), (dict(scores=s(1.0, -1.0, 0, None)), INV),
-                   (dict(scores=s(1.0, nan, 0, None)), INV), (dict(scores=s(1.0, 0.0, -1, None)), INV), (dict(scores=s(1.0, 0.0, 0, FAKE + 2)), MIS)):
+                   (dict(scores=s(1.0, nan, 0, None)), INV), (dict(scores=s(1.0, 2e30, 0, None)), INV), (dict(scores=s(1.0, 1e-40, 0, None)), INV), (dict(scores=s(1.0, 0.0, -1, None)), INV), (dict(scores=s(1.0, 0.0, 0, FAKE + 2)), MIS)):
         assert attend(jb, q, kv, **kw) == rc, kw
     assert jb.lib().jb_attend(q, None, C.byref(s(1.0, 0.0, 0, None)), p(FAKE), 256, 64, 4, p(FAKE), p(FAKE), 1, p(FAKE), 256, 64, p(FAKE), 1 << 40, None) == INV
     assert jb.lib().jb_attend_workspace(None, 4) == 0 and jb.lib().jb_attend_workspace(C.byref(kv), 1) == 0

@@ -147,6 +147,25 @@ def test_windows_caps_and_biases(dtype, window, softcap, bias):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cap", [1e-3, 0.25, 7.0, 50.0, 3e3, 1e7, 1e25])
+def test_caps_keep_small_scores(dtype, cap):
+    """Whatever the cap, tanh is good to a few parts in 2^20 of itself: the score moves by no more than that of
+    its own size (here 2^-19 of the largest score after the cap), not of the cap's."""
+    cache = make(dtype, [200], 2, 64, 16)
+    q, rows, pos = query(1, 2, 64, dtype, std=3.0), i32([0]), i32([199])
+    got = jb.jb_attend(cache, 0, q, rows, pos, softcap=cap)
+    ids = cache.pages.table[0, torch.arange(200, device="cuda") // 16].long()
+    k, v = (x[0][ids, :, torch.arange(200, device="cuda") % 16].double() for x in (cache.keys, cache.values))
+    prod = q[0].double()[None] * k / 8.0
+    x = cap * torch.tanh(prod.sum(-1) / cap)
+    p = torch.softmax(x, 0)
+    want, size = torch.einsum("th,thd->hd", p, v), torch.einsum("th,thd->hd", p, v.abs())
+    rel = 2 * (80 * 2.0**-23 * prod.abs().sum(-1).amax(0) + 2.0**-19 * x.abs().amax(0) + 2.0**-21) + 200 * 2.0**-23
+    tol = size * (rel[:, None] + (2.0**-16 if dtype == "bf16" else 0)) + (2.0**-8 * want.abs() if dtype == "bf16" else 0)
+    assert ((got[0].double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_prompt_tokens_are_queries_of_one_row(dtype):
     cache = make(dtype, [150, 40], 2, 64, 16)
     rows, pos = i32([0] * 150 + [1] * 40), i32(list(range(150)) + list(range(40)))
