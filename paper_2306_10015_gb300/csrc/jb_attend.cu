@@ -352,9 +352,12 @@ __device__ __forceinline__ void wait_copies() {
 }
 __device__ __forceinline__ void prefetch(const void* p) { asm volatile("prefetch.global.L1 [%0];" ::"l"(p)); }
 
-// A warp copies its groups, whole rows at a time, kStages ahead into a ring of its own, so that warps
-// never wait for one another. 16-byte pieces of row t are stored at column (piece ^ t % 8): reads of one
-// column of 8 rows, and of one row, are free of bank conflicts.
+// The stretches whose copies are under way, in the order of the line; a ring for each warp.
+constexpr int kQueue = 4;
+
+// A warp copies its groups, whole rows at a time, kStages ahead into a ring of its own, across the ends of
+// stretches, so that it waits neither for other warps nor between pairs. 16-byte pieces of row t are stored at
+// column (piece ^ t % 8): reads of one column of 8 rows, and of one row, are free of bank conflicts.
 template <typename T, int D>
 struct Feed {
     static constexpr int kStages = sizeof(T) == 4 && D >= 128 ? 1 : 2;    // groups that a warp copies ahead
@@ -366,8 +369,11 @@ struct Feed {
     static constexpr uint32_t kStageBytes = 2 * kGroupBytes;
     static constexpr int kRing = kStages * kStageBytes;
     static constexpr int kElems = 16 / sizeof(T);
+    static_assert(kStages + 1 < kQueue);
 
     uint32_t ring;       // shared address of the warp's ring
+    Stretch* queue;
+    int queued;          // stretches put there so far
     const int* table;
     uint64_t at;         // the key head's, this lane's row and piece, in elements
     int group, stop, page, lo, pos;
@@ -375,21 +381,39 @@ struct Feed {
 
     __device__ void ahead(const Params& p) { page = group < stop ? table[group / p.page_groups] : -1; }
 
-    __device__ void open(const Params& p, const Stretch& s) {
+    // Goes on to the dealer's next stretch, whose first page it looks up.
+    __device__ void next(const Params& p, Dealer& deal, int heads_together) {
+        Stretch s;
+        if (!deal.take(p, s)) {
+            group = stop = 0;
+            return;
+        }
         const int lane = threadIdx.x & 31;
+        if (lane == 0) queue[queued % kQueue] = s;
+        ++queued;
         table = p.pages.table + static_cast<size_t>(s.span.row) * p.pages.row_pages;
         at = s.head * p.a.head_stride + lane / kLanes * p.a.token_stride + kElems * (lane % kLanes);
         group = s.span.first + s.from;
         stop = s.span.first + s.to;
         lo = s.span.lo;
         pos = s.span.pos;
-        missing = 0;
         ahead(p);
-#pragma unroll
-        for (int i = 0; i < kStages; ++i) ask(p, i);
+        // the queries that will be wanted: 128 bytes a lane
+        constexpr int kLines = static_cast<int>(D * sizeof(T) / 128);
+        const int h = min(s.block * heads_together + lane / kLines, p.a.group - 1), e = lane % kLines * static_cast<int>(128 / sizeof(T));
+        if (lane / kLines < heads_together && e < p.a.head_dim)
+            prefetch(reinterpret_cast<const T*>(p.a.q) + s.query * p.a.q_row + (s.head * p.a.group + h) * p.a.q_head + e);
     }
 
-    __device__ __forceinline__ void ask(const Params& p, int stage) {
+    __device__ void start(const Params& p, Dealer& deal, int heads_together) {
+        queued = 0;
+        missing = 0;
+        next(p, deal, heads_together);
+#pragma unroll
+        for (int i = 0; i < kStages; ++i) ask(p, i, deal, heads_together);
+    }
+
+    __device__ __forceinline__ void ask(const Params& p, int stage, Dealer& deal, int heads_together) {
         const int row = (threadIdx.x & 31) / kLanes, piece = threadIdx.x % kLanes;
         if (group < stop) {
             const bool real = page >= 0 && page < p.pages.n_pages;
@@ -412,8 +436,8 @@ struct Feed {
                                    inside && token + j >= lo && token + j <= pos);
                     }
             }
-            ++group;
-            ahead(p);
+            if (++group < stop) ahead(p);
+            else next(p, deal, heads_together);
         }
         commit_copies();
     }
@@ -493,6 +517,7 @@ __global__ void __launch_bounds__(kThreads, kBf16Ctas<D, kH>) attend_bf16_kernel
     extern __shared__ __align__(128) char dynamic[];
     __shared__ long long sums[kThreads + 1];
     __shared__ Noted noted[kWarps][2];
+    __shared__ Stretch queue[kWarps][kQueue];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
     const int d = p.a.head_dim;
     Feed<T, D> feed;
@@ -503,13 +528,14 @@ __global__ void __launch_bounds__(kThreads, kBf16Ctas<D, kH>) attend_bf16_kernel
 
     after_previous();
     let_next_start();
+    feed.queue = queue[warp];
     Dealer deal;
     deal.start(p, sums);
-    Stretch s, after;
-    bool more = deal.take(p, s);
-    int cuts = 0;
-    if (more) feed.open(p, s);
-    while (more) {
+    feed.start(p, deal, kH);
+    int cuts = 0, stage = 0;
+    for (int done = 0; done < feed.queued; ++done) {
+        __syncwarp();
+        const Stretch s = queue[warp][done % kQueue];
         const int heads_here = min(kH, p.a.group - s.block * kH);
         const int head0 = s.head * p.a.group + s.block * kH;
         uint32_t q[kS][2 * kR];  // rows r and r + 8, elements 16 i + 2c and + 8
@@ -531,7 +557,6 @@ __global__ void __launch_bounds__(kThreads, kBf16Ctas<D, kH>) attend_bf16_kernel
             m[h] = kLowest;
             l[h] = 0.0f;
         }
-        int stage = 0;
         for (int g = s.span.first + s.from; g < s.span.first + s.to; ++g) {
             if (feed.ready(stage)) {
                 const uint32_t at = stage * Feed<T, D>::kStageBytes;
@@ -605,17 +630,10 @@ __global__ void __launch_bounds__(kThreads, kBf16Ctas<D, kH>) attend_bf16_kernel
                 }
             }
             __syncwarp();
-            feed.ask(p, stage);
+            feed.ask(p, stage, deal, kH);
             stage = stage == Feed<T, D>::kStages - 1 ? 0 : stage + 1;
         }
-        // the next stretch's copies run while this one is finished
-        more = deal.take(p, after);
-        if (more) {
-            feed.open(p, after);
-            if (c < D / 64 && r < p.a.group)
-                prefetch(reinterpret_cast<const T*>(p.a.q) + after.query * p.a.q_row +
-                         (after.head * p.a.group + min(after.block * kH + r, p.a.group - 1)) * p.a.q_head + min(64 * c, d - 8));
-        }
+        // the next stretches' copies run while this one is finished
         const bool whole = s.from == 0 && s.to == s.span.groups;
         float* slot = slot_of(p, kH, D, 2 * deal.worker + (s.from == 0 ? 1 : 0));
 #pragma unroll
@@ -641,8 +659,6 @@ __global__ void __launch_bounds__(kThreads, kBf16Ctas<D, kH>) attend_bf16_kernel
             }
         }
         if (!whole) note(noted[warp][cuts++], deal, s);
-        if (!more) break;
-        s = after;
     }
     hand_in<T, D, kH>(p, noted[warp], cuts, deal.worker);
     write_zeros<T>(p);
@@ -672,6 +688,7 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const
     extern __shared__ __align__(128) char dynamic[];
     __shared__ long long sums[kThreads + 1];
     __shared__ Noted noted[kWarps][2];
+    __shared__ Stretch queue[kWarps][kQueue];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, token = lane & 15, half = lane >> 4;
     const int d = p.a.head_dim;
     char* mine = dynamic + warp * Shape::kWarpBytes;
@@ -682,13 +699,14 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const
 
     after_previous();
     let_next_start();
+    feed.queue = queue[warp];
     Dealer deal;
     deal.start(p, sums);
-    Stretch s, after;
-    bool more = deal.take(p, s);
-    int cuts = 0;
-    if (more) feed.open(p, s);
-    while (more) {
+    feed.start(p, deal, kH);
+    int cuts = 0, stage = 0;
+    for (int done = 0; done < feed.queued; ++done) {
+        __syncwarp();
+        const Stretch s = queue[warp][done % kQueue];
         const int heads_here = min(kH, p.a.group - s.block * kH);
         const int head0 = s.head * p.a.group + s.block * kH;
         float slope[kH], m[kH], l[kH];
@@ -708,7 +726,6 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const
             for (int i = 0; i < kV; ++i) acc[h][i][0] = acc[h][i][1] = make_float2(0.0f, 0.0f);
         }
         __syncwarp();
-        int stage = 0;
         for (int g = s.span.first + s.from; g < s.span.first + s.to; ++g) {
             if (feed.ready(stage)) {
                 const char* keys = mine + stage * Feed<float, D>::kStageBytes + token * Feed<float, D>::kRowBytes;
@@ -789,11 +806,9 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const
                 }
             }
             __syncwarp();
-            feed.ask(p, stage);
+            feed.ask(p, stage, deal, kH);
             stage = stage == Feed<T, D>::kStages - 1 ? 0 : stage + 1;
         }
-        more = deal.take(p, after);
-        if (more) feed.open(p, after);
         const bool whole = s.from == 0 && s.to == s.span.groups;
         float* slot = slot_of(p, kF32Heads, D, 2 * deal.worker + (s.from == 0 ? 1 : 0));
 #pragma unroll
@@ -819,8 +834,6 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const
             }
         }
         if (!whole) note(noted[warp][cuts++], deal, s);
-        if (!more) break;
-        s = after;
         __syncwarp();
     }
     hand_in<T, D, kF32Heads>(p, noted[warp], cuts, deal.worker);
