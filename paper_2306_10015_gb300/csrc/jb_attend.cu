@@ -428,12 +428,11 @@ struct Feed {
                 for (int j = 0; j < kGroup; j += kRows)
 #pragma unroll
                     for (int i = 0; i < kPieces; i += kLanes) {
-                        const bool inside = kElems * (piece + i) < p.a.head_dim;
+                        // what is not seen is not read: a value must not reach the sum, whatever it holds
+                        const bool seen = kElems * (piece + i) < p.a.head_dim && token + j >= lo && token + j <= pos;
                         const uint32_t place = to + j * kRowBytes + (((piece + i) ^ ((row + j) & 7)) << 4);
-                        copy_async(place, kp + j * p.a.token_stride + kElems * i, inside);
-                        // a value that is not seen must not reach the sum, whatever it holds
-                        copy_async(place + kGroupBytes, vp + j * p.a.token_stride + kElems * i,
-                                   inside && token + j >= lo && token + j <= pos);
+                        copy_async(place, kp + j * p.a.token_stride + kElems * i, seen);
+                        copy_async(place + kGroupBytes, vp + j * p.a.token_stride + kElems * i, seen);
                     }
             }
             if (++group < stop) ahead(p);
