@@ -5,7 +5,7 @@
 // state in registers. Work is cut evenly whatever the rows' lengths: the 16-token groups of all
 // (query, key head) pairs are one line, every warp takes an equal stretch of it and works alone. A pair
 // that crosses a boundary is joined from partial (maximum, sum, weighted values) by the warp that
-// finishes last, eight parts at a time.
+// finishes last, 8 or 16 parts at a time.
 //
 // Softmax is kept with a running maximum, so that one pass is enough:
 //   m' = max(m, max_t x_t), s' = s e^(m - m') + sum e^(x_t - m'), o' likewise.
@@ -13,7 +13,8 @@
 // Why a warp and not a CTA: warps that add up their parts of a pair at a barrier cost 2.7 us a pair, which is
 // all that 40 tokens take (256 rows of 20 to 60 tokens, 32 heads of 128: 74 us, now 43). Why equal pieces
 // decided at the start: keeping a share back for the warps that are done first was slower everywhere (by 2 to
-// 30 %), since a warp that is done leaves its bandwidth to the others.
+// 30 %), and so were twice as many CTAs as run at once (1 to 20 %): a warp that is done leaves its bandwidth to
+// the others, and every further piece costs a start and a join.
 #include <atomic>
 
 #include <cuda_bf16.h>
@@ -29,7 +30,7 @@ constexpr int kGroup = 16;         // tokens a warp takes at a time; pages hold 
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kMaxWorkers = 2048;  // warps of the persistent grid; the workspace has two slots for each
-constexpr int kLevels = 4;         // of joining eight parts of a pair at a time: 8^4 >= kMaxWorkers
+constexpr int kLevels = 4;         // of joining 8 or 16 parts of a pair at a time: 8^4 >= kMaxWorkers
 constexpr int kLeast = 4;          // groups of a stretch, where that leaves one to each CTA
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -3.0e38f;
@@ -252,6 +253,7 @@ __device__ __forceinline__ void join_up(const Params& p, int first, int index, i
                 __threadfence();
             }
             before = __shfl_sync(kAll, before, 0);
+            __syncwarp();  // every lane reads what lane 0 may read now
             if (before + 1 < members) return;
             if (lane == 0) counter[base] = 0;
             const bool last = count <= kRadix;
@@ -499,8 +501,8 @@ __device__ __forceinline__ void load_transposed(uint32_t (&m)[4], uint32_t at) {
 // tensor cores are 17 % busy at most and a 128-row product would only pad more; what bounds it is HBM.
 // Measured (GPU time): 96 rows of 1900 to 2048 tokens, 40 heads of 128: 570 us, 6.8 TB/s, the rate of a copy, and
 // the bytes of one read (1.296 GB of 1.294 GB at a third of the rows). 3 rows of up to 131072 tokens, 8 query heads
-// to each of 8 key heads: 230 us, 6.3 TB/s. 48 rows of 65 to 2048 tokens: 85 us, 5.5 TB/s (3 us until the first
-// copies, 5 us of joins at the end). Two groups ahead and two CTAs: three ahead take 4 % longer, three CTAs 6 %.
+// to each of 8 key heads: 230 us, 6.3 TB/s. 48 rows of 65 to 2048 tokens: 81 us, 5.7 TB/s (3 us until the first
+// copies, 5 us of joins at the end; 85 us where copies stopped at the end of each pair). Two groups ahead and two CTAs: three ahead take 4 % longer, three CTAs 6 %.
 // With r = lane / 4 and
 // c = lane % 4 a lane holds the scores of rows r and r + 8, tokens 2c and 2c + 1 of each eight, which is
 // also how the weights enter the second product.
@@ -665,7 +667,7 @@ __global__ void __launch_bounds__(kThreads, kBf16Ctas<D, kH>) attend_bf16_kernel
 
 // fp32, on the FMA units (packed pairs), kH query heads at a time. HBM bounds it up to 2 query heads to a key head
 // (64 rows of about 1500 tokens, 32 heads of 64: 246 us, 6.4 TB/s; heads of 128: 6.6 TB/s); with 8, the reads of
-// queries and weights from shared memory and the products do (8 key heads of 128: 161 us, 4.9 TB/s).
+// queries and weights from shared memory and the products do (8 key heads of 128: 160 us, 4.9 TB/s).
 // For the scores a lane takes token lane % 16 and half of
 // its elements against the queries in shared memory; for the values it takes four (eight) elements of
 // every token, with the weights from shared memory.

@@ -6,7 +6,7 @@
 // data runs after it over the whole GPU, and HBM bounds it. Small caches are bound by launches, which is why
 // a plan also writes the tables.
 // Measured (GPU time): 24 prompts forked to 8 answers each in 24 layers, 1.1 GB written: 194 us (a prompt's page
-// is read from HBM once); 3000 pages of 131 KB freed, moved and reserved: 272 us, 5.9 TB/s; the same with 35
+// is read from HBM once); 3000 pages of 131 KB freed, moved and reserved: 248 us, 6.5 TB/s; the same with 35
 // pages: 15 us; 8191 new tokens of 3 KB keys and values each: 17 us, 5.9 TB/s; 64 new tokens: 2.6 us.
 #include <cooperative_groups.h>
 

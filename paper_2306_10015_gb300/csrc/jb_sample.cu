@@ -10,9 +10,10 @@
 // smaller than L2); histograms and sums are joined through distributed shared memory.
 //
 // What bounds it is not the bytes: for few rows a chain of a dozen barriers (one fp32 row of 50272 tokens: 8 us
-// without filters, 15 with top-k, 18 with top-p, 27 with all), for many the instructions, about 90 for each
-// token (256 bf16 rows: 20 us without filters, 38 with top-k, 66 with top-p: 15 of them the exponentials and
-// shared-memory additions of the histogram, 9 the sum of what is kept, 7 the search for the bin's tokens).
+// without filters, 14 with top-k or with all filters, 18 with top-p), for many the instructions, about 90 for each
+// token (256 bf16 rows: 20 us without filters, 33 with top-k, 67 with top-p: 15 of them the exponentials and
+// shared-memory additions of the histogram, 9 the sum of what is kept, 7 the search for the bin's tokens; 45
+// where top-p keeps few tokens, whose list serves the rest of the draw).
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
