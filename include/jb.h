@@ -391,7 +391,8 @@ typedef struct {
  * products run on the tensor cores with fp32 sums, and a weight exp(x_t) enters them
  * as the sum of two bf16 numbers (16 bits of it).
  *   q_heads    a multiple of the layer's heads
- *   strides    in elements, multiples of 16 bytes; pointers 16-byte aligned
+ *   strides    in elements, multiples of 16 bytes, those of d_out at least head_dim where
+ *              there are several queries or heads; pointers 16-byte aligned
  *   workspace  jb_attend_workspace(...) bytes, 16-byte aligned, the first 65536 of them
  *              zero before its first use; every call leaves it ready for the next one on
  *              the stream. Calls that may run at the same time need one each.

@@ -603,6 +603,8 @@ def jb_attend(cache: KVCache, layer: int, q, rows, pos, out=None, scale: Optiona
     if workspace is None:
         ws, nbytes, held = cache._attend_workspace(heads, stream, handle)
     else:
+        if not workspace.is_cuda or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous CUDA tensor")
         ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     scores = jb_scores(cache.head_dim ** -0.5 if scale is None else scale, softcap, window,
                        None if slopes is None else slopes.data_ptr())

@@ -228,6 +228,9 @@ JB_EXPORT int jb_attend(const jb_pages* pages, const jb_kv* layer, const jb_scor
         const uint64_t es = size_of(layer->dtype);
         JB_TRY(check_strides(q_row_stride, q_head_stride, es));
         JB_TRY(check_strides(out_row_stride, out_head_stride, es));
+        // outputs that share bytes would hold whichever was written last
+        if ((n > 1 && out_row_stride < static_cast<uint64_t>(layer->head_dim)) || (q_heads > 1 && out_head_stride < static_cast<uint64_t>(layer->head_dim)))
+            return static_cast<int>(JB_ERR_INVALID_ARG);
         JB_TRY(check_workspace(workspace, workspace_bytes, jb_attend_workspace(layer, q_heads)));
         jb::Attend a;
         a.k = static_cast<const char*>(layer->k);
@@ -248,12 +251,12 @@ JB_EXPORT int jb_attend(const jb_pages* pages, const jb_kv* layer, const jb_scor
         a.group = q_heads / layer->heads;
         a.head_dim = layer->head_dim;
         a.bf16 = layer->dtype == JB_BF16;
-        for (int first = 0; first < n; first += jb::kMaxListed) {
-            a.q = static_cast<const char*>(d_q) + first * q_row_stride * es;
-            a.out = static_cast<char*>(d_out) + first * out_row_stride * es;
+        for (int64_t first = 0; first < n; first += jb::kMaxListed) {
+            a.q = static_cast<const char*>(d_q) + static_cast<uint64_t>(first) * q_row_stride * es;
+            a.out = static_cast<char*>(d_out) + static_cast<uint64_t>(first) * out_row_stride * es;
             a.rows = d_rows + first;
             a.pos = d_pos + first;
-            a.n = n - first < jb::kMaxListed ? n - first : jb::kMaxListed;
+            a.n = static_cast<int>(n - first < jb::kMaxListed ? n - first : jb::kMaxListed);
             JB_TRY(cuda_status(jb::launch_attend(p, a, stream)));
         }
         return static_cast<int>(JB_OK);

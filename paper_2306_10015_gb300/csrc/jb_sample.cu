@@ -702,6 +702,7 @@ cudaError_t launch_t(const Sample& p, cudaStream_t s) {
                (2ll * c * p.n <= room && p.vocab > c * tokens);
     };
     while (ctas < kMaxCluster && more(ctas)) ctas *= 2;
+    if (static_cast<long long>(p.n) * ctas > 0x7FFFFFFFll) return cudaErrorInvalidValue;
     return launch(small ? sample_kernel<T, 256> : sample_kernel<T, kLarge>, static_cast<unsigned>(p.n) * ctas, threads, 0, ctas, s, p);
 }
 

@@ -143,3 +143,9 @@ def test_python_refuses_tensors_that_are_not_on_the_gpu(jb):
         jb.jb_cache_free(None, z)
     with pytest.raises(ValueError):
         jb.jb_cache_reserve(None, z, z)
+
+
+def test_outputs_that_overlap_are_refused(jb):
+    q, kv = C.byref(pages(jb)), layer(jb)
+    for kw in (dict(n=2, oa=0), dict(n=2, oa=56), dict(ob=0), dict(ob=56, oa=64)):
+        assert attend(jb, q, kv, **kw) == INV, kw

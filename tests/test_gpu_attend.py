@@ -298,3 +298,15 @@ def test_offsets_past_32_bits():
     new = query(2, 64, 128, "bf16", seed=9)
     jb.jb_cache_write(cache, 0, new[:, :32], new[:, 32:], i32([0, 1]), i32([100, 47]))
     assert torch.equal(k[n_pages - 8 + 6, :, 4], new[0, :32]) and torch.equal(v[n_pages - 30, :, 15], new[1, 32:])
+
+
+def test_workspace_on_the_host_is_refused():
+    pages = jb.PageTable.empty(1, 2, 2, 16)
+    kv = torch.zeros(2, 1, 16, 64, dtype=torch.bfloat16, device="cuda")
+    cache = jb.KVCache(pages, [kv], [kv.clone()])
+    at = torch.zeros(1, dtype=torch.int32, device="cuda")
+    q = torch.zeros(1, 1, 64, dtype=torch.bfloat16, device="cuda")
+    size = cache.new_workspace(1).numel()
+    for ws in (torch.zeros(size, dtype=torch.uint8), torch.zeros(2 * size, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError):
+            jb.jb_attend(cache, 0, q, at, at, workspace=ws)
