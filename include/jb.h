@@ -389,7 +389,8 @@ typedef struct {
  * effect, NaN included. Results are bitwise repeatable.
  * Scores, maxima and sums are fp32; fp32 caches are computed in fp32. With bf16 the
  * products run on the tensor cores with fp32 sums, and a weight exp(x_t) enters them
- * as the sum of two bf16 numbers (16 bits of it).
+ * as the sum of two bf16 numbers (16 bits of it), so that an infinite value that is seen
+ * gives an infinity or NaN.
  *   q_heads    a multiple of the layer's heads
  *   strides    in elements, multiples of 16 bytes, those of d_out at least head_dim where
  *              there are several queries or heads; pointers 16-byte aligned

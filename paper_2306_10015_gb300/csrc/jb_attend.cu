@@ -502,10 +502,10 @@ __device__ __forceinline__ void load_transposed(uint32_t (&m)[4], uint32_t at) {
 // Measured (GPU time): 96 rows of 1900 to 2048 tokens, 40 heads of 128: 570 us, 6.8 TB/s, the rate of a copy, and
 // the bytes of one read (1.296 GB of 1.294 GB at a third of the rows). 3 rows of up to 131072 tokens, 8 query heads
 // to each of 8 key heads: 230 us, 6.3 TB/s. 48 rows of 65 to 2048 tokens: 81 us, 5.7 TB/s (3 us until the first
-// copies, 5 us of joins at the end; 85 us where copies stopped at the end of each pair). Two groups ahead and two CTAs: three ahead take 4 % longer, three CTAs 6 %.
-// With r = lane / 4 and
-// c = lane % 4 a lane holds the scores of rows r and r + 8, tokens 2c and 2c + 1 of each eight, which is
-// also how the weights enter the second product.
+// copies, 5 us of joins at the end; 85 us where copies stopped at the end of each pair). Two groups ahead and two
+// CTAs: three ahead take 4 % longer, three CTAs 6 %.
+// With r = lane / 4 and c = lane % 4 a lane holds the scores of rows r and r + 8, tokens 2c and 2c + 1 of each
+// eight, which is also how the weights enter the second product.
 // Weights enter it with 16 bits, as two bf16 numbers. With up to 8 query heads to a key head (kH = 8) the
 // other 8 rows hold what rounding drops, at no cost; with more, a second product adds it.
 template <int D, int kH>
