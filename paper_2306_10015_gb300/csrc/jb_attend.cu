@@ -667,12 +667,14 @@ __global__ void __launch_bounds__(kThreads, kBf16Ctas<D, kH>) attend_bf16_kernel
 
 // fp32, on the FMA units (packed pairs), kH query heads at a time. HBM bounds it up to 2 query heads to a key head
 // (64 rows of about 1500 tokens, 32 heads of 64: 246 us, 6.4 TB/s; heads of 128: 6.6 TB/s); with 8, the reads of
-// queries and weights from shared memory and the products do (8 key heads of 128: 160 us, 4.9 TB/s).
-// For the scores a lane takes token lane % 16 and half of
-// its elements against the queries in shared memory; for the values it takes four (eight) elements of
-// every token, with the weights from shared memory.
-template <int D>
-constexpr int kF32Ctas = D == 64 ? 3 : D == 128 ? 2 : 1;  // on an SM
+// queries and weights from shared memory and the products do (8 key heads of 128: 144 us, 5.5 TB/s).
+// For the scores a lane takes token lane % 16 and half of its elements against the queries in shared memory, or,
+// with 8 query heads, two tokens and a quarter, which halves the reads of queries (144 us, 147 without). The parts
+// are added up so that each half of the warp has half of the heads, and caps, maxima and exponentials are worked out
+// once (147 us, 160 where both halves did all; 64 rows of 8 key heads of 64: 98 us, 117). For the values a lane takes four (eight) elements of every token,
+// with the weights from shared memory.
+template <int D, int kH>
+constexpr int kF32Ctas = D == 64 ? (kH == 8 ? 2 : 3) : D == 128 ? 2 : 1;  // on an SM; three for 8 heads of 64 spill
 constexpr int kF32Heads = 8;               // of a slot
 
 template <int D, int kH>
@@ -682,10 +684,13 @@ struct F32Shape {
 };
 
 template <int D, int kH>
-__global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(kThreads, kF32Ctas<D, kH>) attend_f32_kernel(const __grid_constant__ Params p) {
     using T = float;
     using Shape = F32Shape<D, kH>;
     constexpr int kPieces = D / 4, kV = (D + 127) / 128;  // pieces of the values that a lane takes
+    constexpr int kMine = kH > 1 ? kH / 2 : 1;            // heads whose softmax a lane works on
+    constexpr int kT = kH == 8 ? 2 : 1;                   // tokens whose scores a lane adds a part of
+    constexpr int kApart = kGroup / kT;                   // from one to the next
     extern __shared__ __align__(128) char dynamic[];
     __shared__ long long sums[kThreads + 1];
     __shared__ Noted noted[kWarps][2];
@@ -710,8 +715,9 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const
         const Stretch s = queue[warp][done % kQueue];
         const int heads_here = min(kH, p.a.group - s.block * kH);
         const int head0 = s.head * p.a.group + s.block * kH;
-        float slope[kH], m[kH], l[kH];
+        float slope[kMine], m[kMine], l[kMine];  // of heads first, first + 1, ..
         float2 acc[kH][kV][2];
+        const int first = kH > 1 ? half * kMine : 0;
         for (int u = lane; u < kH * kPieces; u += 32) {
             const int h = u / kPieces, e = u % kPieces * 4;
             *reinterpret_cast<float4*>(queries + 4 * u) =
@@ -719,66 +725,91 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const
                                         : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         }
 #pragma unroll
-        for (int h = 0; h < kH; ++h) {
-            slope[h] = p.a.slopes != nullptr && h < heads_here ? p.a.slopes[head0 + h] : 0.0f;
+        for (int h = 0; h < kMine; ++h) {
+            slope[h] = p.a.slopes != nullptr && first + h < heads_here ? p.a.slopes[head0 + first + h] * kLog2e : 0.0f;
             m[h] = kLowest;
             l[h] = 0.0f;
+        }
+#pragma unroll
+        for (int h = 0; h < kH; ++h)
 #pragma unroll
             for (int i = 0; i < kV; ++i) acc[h][i][0] = acc[h][i][1] = make_float2(0.0f, 0.0f);
-        }
         __syncwarp();
         for (int g = s.span.first + s.from; g < s.span.first + s.to; ++g) {
             if (feed.ready(stage)) {
-                const char* keys = mine + stage * Feed<float, D>::kStageBytes + token * Feed<float, D>::kRowBytes;
+                const int part = lane / kApart;  // pieces part, part + 2 kT, .. of tokens lane % kApart and (kT = 2) 8 on
+                const char* keys = mine + stage * Feed<float, D>::kStageBytes + lane % kApart * Feed<float, D>::kRowBytes;
                 const char* values = mine + stage * Feed<float, D>::kStageBytes + Feed<float, D>::kGroupBytes;
-                float2 sums2[kH];
+                float2 sums2[kH][kT];
 #pragma unroll
-                for (int h = 0; h < kH; ++h) sums2[h] = make_float2(0.0f, 0.0f);
-#pragma unroll 8
-                for (int i = 0; i < kPieces; i += 2) {
-                    const float4 k = *reinterpret_cast<const float4*>(keys + (((i + half) ^ (token & 7)) << 4));
+                for (int h = 0; h < kH; ++h)
+#pragma unroll
+                    for (int u = 0; u < kT; ++u) sums2[h][u] = make_float2(0.0f, 0.0f);
+#pragma unroll 8 / kT
+                for (int i = 0; i < kPieces; i += 2 * kT) {
+                    float4 k[kT];
+#pragma unroll
+                    for (int u = 0; u < kT; ++u)
+                        k[u] = *reinterpret_cast<const float4*>(keys + u * kApart * Feed<float, D>::kRowBytes + (((i + part) ^ (lane & 7)) << 4));
 #pragma unroll
                     for (int h = 0; h < kH; ++h) {
-                        const float4 q = *reinterpret_cast<const float4*>(queries + h * D + 4 * (i + half));
-                        sums2[h] = __ffma2_rn(make_float2(q.x, q.y), make_float2(k.x, k.y), sums2[h]);
-                        sums2[h] = __ffma2_rn(make_float2(q.z, q.w), make_float2(k.z, k.w), sums2[h]);
+                        const float4 q = *reinterpret_cast<const float4*>(queries + h * D + 4 * (i + part));
+#pragma unroll
+                        for (int u = 0; u < kT; ++u) {
+                            sums2[h][u] = __ffma2_rn(make_float2(q.x, q.y), make_float2(k[u].x, k[u].y), sums2[h][u]);
+                            sums2[h][u] = __ffma2_rn(make_float2(q.z, q.w), make_float2(k[u].z, k[u].w), sums2[h][u]);
+                        }
                     }
                 }
-                float x[kH];
-#pragma unroll
-                for (int h = 0; h < kH; ++h) x[h] = sums2[h].x + sums2[h].y;
                 const int t = g * kGroup + token;
                 const bool unseen = t < s.span.lo || t > s.span.pos;
-                float high[kH];
+                // lanes 16 (and 8) apart hold the parts of a score: the halves get the other's for their own heads, and
+                // the lanes of a half for their own token
+                const auto part_of = [&](int h, int u) { return sums2[h][u].x + sums2[h][u].y; };
+                float x[kMine], high[kMine];
                 bool rises = false;
 #pragma unroll
-                for (int h = 0; h < kH; ++h) {
-                    float y = (x[h] + __shfl_xor_sync(kAll, x[h], 16)) * p.a.scale;
-                    if (p.a.softcap > 0.0f) y = p.a.softcap * tanhf(y / p.a.softcap);
-                    y = fmaf(slope[h], static_cast<float>(t - s.span.pos), y);
-                    x[h] = unseen ? -INFINITY : y;
+                for (int h = 0; h < kMine; ++h) {
+                    float mine_of[kT];
+#pragma unroll
+                    for (int u = 0; u < kT; ++u) {
+                        const float low = part_of(h, u), up = part_of(kH - kMine + h, u);
+                        mine_of[u] = (half == 0 ? low : up) + __shfl_xor_sync(kAll, half == 0 ? up : low, 16);
+                    }
+                    float dot = mine_of[0];
+                    if constexpr (kT == 2) {
+                        const bool second = lane & 8;
+                        dot = (second ? mine_of[1] : mine_of[0]) + __shfl_xor_sync(kAll, second ? mine_of[0] : mine_of[1], 8);
+                    }
+                    x[h] = unseen ? -INFINITY : score<true>(p, dot, slope[h], t - s.span.pos);
                     high[h] = x[h];
 #pragma unroll
                     for (int w = 1; w < 16; w *= 2) high[h] = fmaxf(high[h], __shfl_xor_sync(kAll, high[h], w));
                     rises = rises || high[h] > m[h];
                 }
-                if (rises) {  // the lanes agree
+                if (__any_sync(kAll, rises)) {
+                    float k[kMine];
+#pragma unroll
+                    for (int h = 0; h < kMine; ++h) {
+                        const float top = fmaxf(m[h], high[h]);
+                        k[h] = exp2_approx(m[h] - top);
+                        m[h] = top;
+                        l[h] *= k[h];
+                    }
 #pragma unroll
                     for (int h = 0; h < kH; ++h) {
-                        const float top = fmaxf(m[h], high[h]), k = exp2_approx((m[h] - top) * kLog2e);
-                        m[h] = top;
-                        l[h] *= k;
+                        const float kh = __shfl_sync(kAll, k[h % kMine], 16 * (h / kMine));
 #pragma unroll
                         for (int i = 0; i < kV; ++i)
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) acc[h][i][e] = __fmul2_rn(acc[h][i][e], make_float2(k, k));
+                            for (int e = 0; e < 2; ++e) acc[h][i][e] = __fmul2_rn(acc[h][i][e], make_float2(kh, kh));
                     }
                 }
 #pragma unroll
-                for (int h = 0; h < kH; ++h) {
-                    x[h] = exp2_approx((x[h] - m[h]) * kLog2e);
+                for (int h = 0; h < kMine; ++h) {
+                    x[h] = exp2_approx(x[h] - m[h]);
                     l[h] += x[h];
-                    if (half == 0) weights[token * kH + h] = x[h];
+                    if (kH > 1 || half == 0) weights[token * kH + first + h] = x[h];
                 }
                 __syncwarp();
 #pragma unroll 8
@@ -813,11 +844,14 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const
         const bool whole = s.from == 0 && s.to == s.span.groups;
         float* slot = slot_of(p, kF32Heads, D, 2 * deal.worker + (s.from == 0 ? 1 : 0));
 #pragma unroll
-        for (int h = 0; h < kH; ++h) {
+        for (int h = 0; h < kMine; ++h)
 #pragma unroll
             for (int w = 1; w < 16; w *= 2) l[h] += __shfl_xor_sync(kAll, l[h], w);
+#pragma unroll
+        for (int h = 0; h < kH; ++h) {
+            const float mh = __shfl_sync(kAll, m[h % kMine], 16 * (h / kMine)), lh = __shfl_sync(kAll, l[h % kMine], 16 * (h / kMine));
             if (h >= heads_here) continue;
-            const float inverse = l[h] > 0.0f ? 1.0f / l[h] : 0.0f;
+            const float inverse = lh > 0.0f ? 1.0f / lh : 0.0f;
             float* out = reinterpret_cast<float*>(p.a.out) + s.query * p.a.out_row + (head0 + h) * p.a.out_head;
 #pragma unroll
             for (int i = 0; i < kV; ++i) {
@@ -830,8 +864,8 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D>) attend_f32_kernel(const
                         make_float4(acc[h][i][0].x * inverse, acc[h][i][0].y * inverse, acc[h][i][1].x * inverse, acc[h][i][1].y * inverse);
             }
             if (!whole && lane == 0) {
-                slot[kF32Heads * D + h] = m[h] * kLog2e;
-                slot[kF32Heads * D + kF32Heads + h] = l[h];
+                slot[kF32Heads * D + h] = mh;
+                slot[kF32Heads * D + kF32Heads + h] = lh;
             }
         }
         if (!whole) note(noted[warp][cuts++], deal, s);
