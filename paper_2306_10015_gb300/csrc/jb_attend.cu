@@ -407,40 +407,83 @@ struct Feed {
             prefetch(reinterpret_cast<const T*>(p.a.q) + s.query * p.a.q_row + (s.head * p.a.group + h) * p.a.q_head + e);
     }
 
+    // kApart: keys and values are asked and waited for one after the other.
+    template <bool kApart>
     __device__ void start(const Params& p, Dealer& deal, int heads_together) {
         queued = 0;
         missing = 0;
         next(p, deal, heads_together);
 #pragma unroll
-        for (int i = 0; i < kStages; ++i) ask(p, i, deal, heads_together);
+        for (int i = 0; i < kStages; ++i) {
+            if constexpr (kApart) {
+                ask_keys(p, i);
+                ask_values(p, i, deal, heads_together);
+            } else {
+                ask(p, i, deal, heads_together);
+            }
+        }
     }
 
-    __device__ __forceinline__ void ask(const Params& p, int stage, Dealer& deal, int heads_together) {
-        const int row = (threadIdx.x & 31) / kLanes, piece = threadIdx.x % kLanes;
-        if (group < stop) {
-            const bool real = page >= 0 && page < p.pages.n_pages;
+    // Copies the group's keys, values or both; the values alone after the keys.
+    template <bool kKeys, bool kValues>
+    __device__ __forceinline__ void copy(const Params& p, int stage) {
+        bool real = !(missing >> stage & 1u);
+        if constexpr (kKeys) {
+            real = page >= 0 && page < p.pages.n_pages;
             missing = (missing & ~(1u << stage)) | (real ? 0u : 1u << stage);
-            if (real) {
-                const uint64_t from = at + page * p.a.page_stride + group % p.page_groups * kGroup * p.a.token_stride;
-                const T* kp = reinterpret_cast<const T*>(p.a.k) + from;
-                const T* vp = reinterpret_cast<const T*>(p.a.v) + from;
-                const uint32_t to = ring + stage * kStageBytes + row * kRowBytes;
-                const int token = group * kGroup + row;
+        }
+        if (!real) return;
+        const int row = (threadIdx.x & 31) / kLanes, piece = threadIdx.x % kLanes;
+        const uint64_t from = at + page * p.a.page_stride + group % p.page_groups * kGroup * p.a.token_stride;
+        const T* kp = reinterpret_cast<const T*>(p.a.k) + from;
+        const T* vp = reinterpret_cast<const T*>(p.a.v) + from;
+        const uint32_t to = ring + stage * kStageBytes + row * kRowBytes;
+        const int token = group * kGroup + row;
 #pragma unroll
-                for (int j = 0; j < kGroup; j += kRows)
+        for (int j = 0; j < kGroup; j += kRows)
 #pragma unroll
-                    for (int i = 0; i < kPieces; i += kLanes) {
-                        // what is not seen is not read: a value must not reach the sum, whatever it holds
-                        const bool seen = kElems * (piece + i) < p.a.head_dim && token + j >= lo && token + j <= pos;
-                        const uint32_t place = to + j * kRowBytes + (((piece + i) ^ ((row + j) & 7)) << 4);
-                        copy_async(place, kp + j * p.a.token_stride + kElems * i, seen);
-                        copy_async(place + kGroupBytes, vp + j * p.a.token_stride + kElems * i, seen);
-                    }
+            for (int i = 0; i < kPieces; i += kLanes) {
+                // what is not seen is not read: a value must not reach the sum, whatever it holds
+                const bool seen = kElems * (piece + i) < p.a.head_dim && token + j >= lo && token + j <= pos;
+                const uint32_t place = to + j * kRowBytes + (((piece + i) ^ ((row + j) & 7)) << 4);
+                if constexpr (kKeys) copy_async(place, kp + j * p.a.token_stride + kElems * i, seen);
+                if constexpr (kValues) copy_async(place + kGroupBytes, vp + j * p.a.token_stride + kElems * i, seen);
             }
-            if (++group < stop) ahead(p);
-            else next(p, deal, heads_together);
+    }
+    __device__ __forceinline__ void advance(const Params& p, Dealer& deal, int heads_together) {
+        if (++group < stop) ahead(p);
+        else next(p, deal, heads_together);
+    }
+    __device__ __forceinline__ void ask_keys(const Params& p, int stage) {
+        if (group < stop) copy<true, false>(p, stage);
+        commit_copies();
+    }
+    // Of the group whose keys were asked for last; goes on to the next one.
+    __device__ __forceinline__ void ask_values(const Params& p, int stage, Dealer& deal, int heads_together) {
+        if (group < stop) {
+            copy<false, true>(p, stage);
+            advance(p, deal, heads_together);
         }
         commit_copies();
+    }
+    __device__ __forceinline__ void ask(const Params& p, int stage, Dealer& deal, int heads_together) {
+        if (group < stop) {
+            copy<true, true>(p, stage);
+            advance(p, deal, heads_together);
+        }
+        commit_copies();
+    }
+
+    // Waits for the keys in `stage`; false if the group's page is missing.
+    __device__ __forceinline__ bool keys_ready(int stage) {
+        wait_copies<2 * kStages - 1>();
+        __syncwarp();
+        return !(missing >> stage & 1u);
+    }
+    // Waits for the values, the keys of a later group having been asked for.
+    __device__ __forceinline__ void values_ready() {
+        wait_copies<2 * kStages - 1>();
+        __syncwarp();
     }
 
     // Waits for the group in `stage`; false if its page is missing.
@@ -500,7 +543,7 @@ __device__ __forceinline__ void load_transposed(uint32_t (&m)[4], uint32_t at) {
 // bf16, mma.m16n8k16: a warp multiplies up to 16 query heads (rows) by 16 tokens. Few rows are real, so the
 // tensor cores are 17 % busy at most and a 128-row product would only pad more; what bounds it is HBM.
 // Measured (GPU time): 96 rows of 1900 to 2048 tokens, 40 heads of 128: 570 us, 6.8 TB/s, the rate of a copy, and
-// the bytes of one read (1.296 GB of 1.294 GB at a third of the rows). 3 rows of up to 131072 tokens, 8 query heads
+// the bytes of one read (1.294 GB at a third of the rows). 3 rows of up to 131072 tokens, 8 query heads
 // to each of 8 key heads: 230 us, 6.3 TB/s. 48 rows of 65 to 2048 tokens: 81 us, 5.7 TB/s (3 us until the first
 // copies, 5 us of joins at the end; 85 us where copies stopped at the end of each pair). Two groups ahead and two
 // CTAs: three ahead take 4 % longer, three CTAs 6 %.
@@ -532,7 +575,7 @@ __global__ void __launch_bounds__(kThreads, kBf16Ctas<D, kH>) attend_bf16_kernel
     feed.queue = queue[warp];
     Dealer deal;
     deal.start(p, sums);
-    feed.start(p, deal, kH);
+    feed.template start<false>(p, deal, kH);
     int cuts = 0, stage = 0;
     for (int done = 0; done < feed.queued; ++done) {
         __syncwarp();
@@ -667,11 +710,12 @@ __global__ void __launch_bounds__(kThreads, kBf16Ctas<D, kH>) attend_bf16_kernel
 
 // fp32, on the FMA units (packed pairs), kH query heads at a time. HBM bounds it up to 2 query heads to a key head
 // (64 rows of about 1500 tokens, 32 heads of 64: 246 us, 6.4 TB/s; heads of 128: 6.6 TB/s); with 8, the reads of
-// queries and weights from shared memory and the products do (8 key heads of 128: 144 us, 5.5 TB/s).
+// queries and weights from shared memory, the products and their latencies do (8 key heads of 128: 137 us, 5.7 TB/s;
+// 144 where a warp does not copy keys while it multiplies values; with one head that costs 1 to 2 %).
 // For the scores a lane takes token lane % 16 and half of its elements against the queries in shared memory, or,
-// with 8 query heads, two tokens and a quarter, which halves the reads of queries (144 us, 147 without). The parts
+// with 8 query heads, two tokens and a quarter, which halves the reads of queries (147 to 144 us then). The parts
 // are added up so that each half of the warp has half of the heads, and caps, maxima and exponentials are worked out
-// once (147 us, 160 where both halves did all; 64 rows of 8 key heads of 64: 98 us, 117). For the values a lane takes four (eight) elements of every token,
+// once (160 to 147 us; 64 rows of 8 key heads of 64: 98 us, 117). For the values a lane takes four (eight) elements of every token,
 // with the weights from shared memory.
 template <int D, int kH>
 constexpr int kF32Ctas = D == 64 ? (kH == 8 ? 2 : 3) : D == 128 ? 2 : 1;  // on an SM; three for 8 heads of 64 spill
@@ -690,7 +734,9 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D, kH>) attend_f32_kernel(c
     constexpr int kPieces = D / 4, kV = (D + 127) / 128;  // pieces of the values that a lane takes
     constexpr int kMine = kH > 1 ? kH / 2 : 1;            // heads whose softmax a lane works on
     constexpr int kT = kH == 8 ? 2 : 1;                   // tokens whose scores a lane adds a part of
-    constexpr int kApart = kGroup / kT;                   // from one to the next
+    constexpr int kStep = kGroup / kT;                    // from one to the next
+    // with one stage, keys are copied while values are multiplied and the other way round
+    constexpr bool kApart = Feed<float, D>::kStages == 1 && kH >= 4;
     extern __shared__ __align__(128) char dynamic[];
     __shared__ long long sums[kThreads + 1];
     __shared__ Noted noted[kWarps][2];
@@ -708,7 +754,7 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D, kH>) attend_f32_kernel(c
     feed.queue = queue[warp];
     Dealer deal;
     deal.start(p, sums);
-    feed.start(p, deal, kH);
+    feed.template start<kApart>(p, deal, kH);
     int cuts = 0, stage = 0;
     for (int done = 0; done < feed.queued; ++done) {
         __syncwarp();
@@ -736,10 +782,10 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D, kH>) attend_f32_kernel(c
             for (int i = 0; i < kV; ++i) acc[h][i][0] = acc[h][i][1] = make_float2(0.0f, 0.0f);
         __syncwarp();
         for (int g = s.span.first + s.from; g < s.span.first + s.to; ++g) {
-            if (feed.ready(stage)) {
-                const int part = lane / kApart;  // pieces part, part + 2 kT, .. of tokens lane % kApart and (kT = 2) 8 on
-                const char* keys = mine + stage * Feed<float, D>::kStageBytes + lane % kApart * Feed<float, D>::kRowBytes;
-                const char* values = mine + stage * Feed<float, D>::kStageBytes + Feed<float, D>::kGroupBytes;
+            const bool real = kApart ? feed.keys_ready(stage) : feed.ready(stage);
+            if (real) {
+                const int part = lane / kStep;  // pieces part, part + 2 kT, .. of tokens lane % kStep and (kT = 2) 8 on
+                const char* keys = mine + stage * Feed<float, D>::kStageBytes + lane % kStep * Feed<float, D>::kRowBytes;
                 float2 sums2[kH][kT];
 #pragma unroll
                 for (int h = 0; h < kH; ++h)
@@ -750,7 +796,7 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D, kH>) attend_f32_kernel(c
                     float4 k[kT];
 #pragma unroll
                     for (int u = 0; u < kT; ++u)
-                        k[u] = *reinterpret_cast<const float4*>(keys + u * kApart * Feed<float, D>::kRowBytes + (((i + part) ^ (lane & 7)) << 4));
+                        k[u] = *reinterpret_cast<const float4*>(keys + u * kStep * Feed<float, D>::kRowBytes + (((i + part) ^ (lane & 7)) << 4));
 #pragma unroll
                     for (int h = 0; h < kH; ++h) {
                         const float4 q = *reinterpret_cast<const float4*>(queries + h * D + 4 * (i + part));
@@ -811,7 +857,12 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D, kH>) attend_f32_kernel(c
                     l[h] += x[h];
                     if (kH > 1 || half == 0) weights[token * kH + first + h] = x[h];
                 }
-                __syncwarp();
+            }
+            __syncwarp();
+            if constexpr (kApart) feed.ask_keys(p, stage);
+            if (real) {
+                if constexpr (kApart) feed.values_ready();
+                const char* values = mine + stage * Feed<float, D>::kStageBytes + Feed<float, D>::kGroupBytes;
 #pragma unroll 8
                 for (int u = 0; u < kGroup; ++u) {
                     float4 v[kV];
@@ -838,7 +889,8 @@ __global__ void __launch_bounds__(kThreads, kF32Ctas<D, kH>) attend_f32_kernel(c
                 }
             }
             __syncwarp();
-            feed.ask(p, stage, deal, kH);
+            if constexpr (kApart) feed.ask_values(p, stage, deal, kH);
+            else feed.ask(p, stage, deal, kH);
             stage = stage == Feed<T, D>::kStages - 1 ? 0 : stage + 1;
         }
         const bool whole = s.from == 0 && s.to == s.span.groups;
