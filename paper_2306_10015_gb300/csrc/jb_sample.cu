@@ -525,7 +525,8 @@ struct Draw {
         return false;
     }
 
-    // Of the unit's tokens, which may be kept: at or above x, and with y at or above y.
+    // Of the unit's tokens, which may be kept: at or above x, and with y at or above y. It only saves weighing: none that
+    // is kept may be left out.
     __device__ __forceinline__ unsigned candidates(const float(&x)[kUnit], float least_x, float least_y) const {
         unsigned mask = 0;
 #pragma unroll
@@ -598,7 +599,8 @@ struct Draw {
         // what is kept; few tokens are where something is cut off, and only those are weighed
         const float least_x = last == 0 ? -INFINITY : logit_of(static_cast<uint32_t>(last >> 32));
         const int last_index = static_cast<int>(~static_cast<uint32_t>(last));
-        const float least_y = least > 0 ? logf(fminf(min_p, 1.0f)) - 0.01f : -INFINITY;
+        // a weight is rounded to the least one from half a unit below it on; 0.01 for the roundings of y, logf and expf
+        const float least_y = least > 0 ? logf((static_cast<float>(least) - 0.5f) * (1.0f / kOne)) - 0.01f : -INFINITY;
         const bool cut = last != 0 || least > 0;
         const auto kept = [&](float x, int index) -> uint32_t {
             if (x == least_x && index > last_index && last != 0) return 0;

@@ -197,3 +197,30 @@ def test_rows_repeat_whatever_is_beside_them(dtype):
     for i in (0, 1, 151, 399):
         one, l1 = jb.jb_sample(x[i:i + 1], w[i:i + 1], top_p=0.9, top_k=300)
         assert one.item() == all_[i].item() and l1.item() == lp[i].item()
+
+
+# For each min_p the tail's y, on both sides of where a weight reaches the least that is kept: ln((least - 1/2) / 2^30), since
+# weights are rounded (least = ceil(min_p 2^30) = 1, 2, 11, 43).
+SMALL_MIN_P = [(2.0**-30, -21.7, -20.6), (1.8e-9, -20.6, -19.9), (1e-8, -18.5, -18.38), (4e-8, -17.06, -17.03)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,V", [(1, 50_272), (40, 5003), (200, 20_001)])
+@pytest.mark.parametrize("min_p,low,high", SMALL_MIN_P)
+@pytest.mark.parametrize("f", [dict(), dict(top_k=3000), dict(top_k=900, top_p=1 - 2.0**-24)], ids=str)
+def test_min_p_keeps_weights_that_round_up_to_the_least(dtype, n, V, min_p, low, high, f):
+    """One likely token before a tail whose weights are a few units: the words are spread over the tail's share of
+    the draw, so that a token which is left out, or counted in one place alone, moves the tokens after it."""
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = low + (high - low) * torch.rand(n, V, generator=g, device="cuda")
+    x[:, 0] = 0.0
+    x = x.to(dtype)
+    w = torch.round(torch.exp(x[0].float()) * 2.0**30)
+    w[w < math.ceil(float(np.float32(min_p)) * 2**30)] = 0
+    k = min(f.get("top_k", V), V)
+    share = float(w.sort(descending=True)[0][1:k].sum()) / 2.0**30
+    words = [(1 << 32) - 1 - int(i / n * share * 2.0**32) for i in range(n)]
+    words = torch.from_numpy(np.array(words, dtype=np.uint64).astype(np.uint32).view(np.int32)).cuda()
+    got = check(x, words=words, min_p=min_p, **f)
+    if k == V and share > 0:
+        assert (got > 0).any()
