@@ -145,10 +145,10 @@ struct Dealer {
         for (int k = 0; per > 1 && k < per; k += 32) {  // and the query within the run
             const int i = query + lane;
             const int g = k + lane < per && i < n ? span_of(p, i).groups : 0;
-            int in = g;
+            long long in = g;  // a query may have 2^27
 #pragma unroll
             for (int d = 1; d < 32; d *= 2) {
-                const int o = __shfl_up_sync(kAll, in, d);
+                const long long o = __shfl_up_sync(kAll, in, d);
                 if (lane >= d) in += o;
             }
             const unsigned past = __ballot_sync(kAll, base + in > goal);

@@ -310,3 +310,22 @@ def test_workspace_on_the_host_is_refused():
     for ws in (torch.zeros(size, dtype=torch.uint8), torch.zeros(2 * size, dtype=torch.uint8, device="cuda")[::2]):
         with pytest.raises(ValueError):
             jb.jb_attend(cache, 0, q, at, at, workspace=ws)
+
+
+def test_groups_of_a_run_of_queries_pass_32_bits():
+    """17 queries in a row at the end of a row of 2^31 - 1024 tokens: a thread's run of them has more than 2^31 groups
+    of 16. All pages but the last are missing, so no key is copied for the others. The wanted values are those of a
+    row that has this page alone."""
+    page, row_pages, n = 1024, (1 << 21) - 1, 17 * 128
+    kv = torch.randn(2, 1, 1, page, 64, device="cuda").to(torch.bfloat16)
+    table = torch.full((1, row_pages), -1, dtype=torch.int32, device="cuda")
+    table[0, -1] = 0
+    cache = jb.KVCache(jb.PageTable(table, i32([row_pages * page]), i32([1]), page), [kv[0]], [kv[1]])
+    short = jb.KVCache(jb.PageTable(i32([[0]]), i32([page]), i32([1]), page), [kv[0]], [kv[1]])
+    q, rows = query(n, 1, 64, "bf16"), torch.zeros(n, dtype=torch.int32, device="cuda")
+    at = torch.full((n,), -1, dtype=torch.int32)
+    at[17 * 40:17 * 41] = page - 1 - 3 * torch.arange(17, dtype=torch.int32)
+    first = (row_pages - 1) * page
+    got = jb.jb_attend(cache, 0, q, rows, torch.where(at >= 0, at + first, -1).int().cuda())
+    want, tol = reference(short, 0, q, rows, at.cuda())
+    assert ((got.double() - want).abs() <= tol).all() and (got[17 * 40:17 * 41] != 0).any() and (got[:17 * 40] == 0).all()
