@@ -392,8 +392,8 @@ typedef struct {
  * as the sum of two bf16 numbers (16 bits of it), so that an infinite value that is seen
  * gives an infinity or NaN.
  *   q_heads    a multiple of the layer's heads
- *   strides    in elements, multiples of 16 bytes, those of d_out at least head_dim where
- *              there are several queries or heads; pointers 16-byte aligned
+ *   strides    in elements, multiples of 16 bytes; pointers 16-byte aligned. No two
+ *              outputs (query, head) may share bytes: JB_ERR_INVALID_ARG
  *   workspace  jb_attend_workspace(...) bytes, 16-byte aligned, the first 65536 of them
  *              zero before its first use; every call leaves it ready for the next one on
  *              the stream. Calls that may run at the same time need one each.

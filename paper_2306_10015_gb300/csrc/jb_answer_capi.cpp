@@ -93,6 +93,21 @@ int check_strides(uint64_t a, uint64_t b, uint64_t es) {
     return a * es % 16 == 0 && b * es % 16 == 0 ? JB_OK : JB_ERR_MISALIGNED;
 }
 
+// Whether two of `na` x `nb` runs of `len` elements at i * sa + j * sb share some: those of (i, j) and (i2, j2) do if
+// (i - i2) sa and (j2 - j) sb are less than `len` apart. Counts are below 2^31, one of them at most 2^16, and strides at
+// most 2^48, so that no product with the smaller count wraps.
+bool outputs_overlap(uint64_t na, uint64_t sa, uint64_t nb, uint64_t sb, uint64_t len) {
+    if ((na > 1 && sa < len) || (nb > 1 && sb < len)) return true;
+    if (na < 2 || nb < 2) return false;
+    if (na < nb) return outputs_overlap(nb, sb, na, sa, len);
+    if (sa >= (nb - 1) * sb + len || sb / sa >= na) return false;  // one within the other, as a row holds its heads
+    for (uint64_t j = 1; j < nb; ++j) {                            // the two i's nearest to j
+        const uint64_t i = j * sb / sa, past = j * sb % sa;
+        if ((i < na && past < len) || (i + 1 < na && sa - past < len)) return true;
+    }
+    return false;
+}
+
 #define JB_TRY(x)                     \
     do {                              \
         const int rc_ = (x);          \
@@ -229,8 +244,7 @@ JB_EXPORT int jb_attend(const jb_pages* pages, const jb_kv* layer, const jb_scor
         JB_TRY(check_strides(q_row_stride, q_head_stride, es));
         JB_TRY(check_strides(out_row_stride, out_head_stride, es));
         // outputs that share bytes would hold whichever was written last
-        if ((n > 1 && out_row_stride < static_cast<uint64_t>(layer->head_dim)) || (q_heads > 1 && out_head_stride < static_cast<uint64_t>(layer->head_dim)))
-            return static_cast<int>(JB_ERR_INVALID_ARG);
+        if (outputs_overlap(n, out_row_stride, q_heads, out_head_stride, layer->head_dim)) return static_cast<int>(JB_ERR_INVALID_ARG);
         JB_TRY(check_workspace(workspace, workspace_bytes, jb_attend_workspace(layer, q_heads)));
         jb::Attend a;
         a.k = static_cast<const char*>(layer->k);

@@ -149,3 +149,27 @@ def test_outputs_that_overlap_are_refused(jb):
     q, kv = C.byref(pages(jb)), layer(jb)
     for kw in (dict(n=2, oa=0), dict(n=2, oa=56), dict(ob=0), dict(ob=56, oa=64)):
         assert attend(jb, q, kv, **kw) == INV, kw
+
+
+def test_outputs_that_share_bytes_are_refused_in_any_order(jb):
+    """Every small pair of strides against the places that the outputs take. A workspace off its grid ends the calls
+    whose outputs are apart before anything is launched."""
+    q, kv = C.byref(pages(jb)), layer(jb, head_dim=8, page_stride=2 * 8 * 16)
+    apart = 0
+    for n in (1, 2, 3, 5):
+        for heads in (2, 4, 6):
+            for oa in range(0, 88, 8):
+                for ob in range(0, 88, 8):
+                    places = [i * oa + h * ob + e for i in range(n) for h in range(heads) for e in range(8)]
+                    rc = MIS if len(set(places)) == len(places) else INV
+                    apart += rc == MIS
+                    assert attend(jb, q, kv, n=n, heads=heads, oa=oa, ob=ob, ws=FAKE + 8) == rc, (n, heads, oa, ob)
+    assert apart > 400
+
+
+def test_outputs_of_long_strides(jb):
+    q, kv, far = C.byref(pages(jb)), layer(jb, head_dim=8, page_stride=2 * 8 * 16), 1 << 48
+    for n, heads, oa, ob, rc in ((2, 65536, far, 8, MIS), (2, 65536, 65536 * 8, 8, MIS), (2, 65536, 65535 * 8, 8, INV), (2147483647, 65536, far, far, INV),
+                                 (2147483647, 2, 8, far, MIS), (2147483647, 65536, far - 8, far, MIS), (3, 65536, far, far - 8, MIS),
+                                 (2147483647, 2, 8, 8 * 2147483647, MIS), (2147483647, 2, 8, 8 * 2147483646, INV)):
+        assert attend(jb, q, kv, n=n, heads=heads, oa=oa, ob=ob, ws=FAKE + 8) == rc, (n, heads, oa, ob)
