@@ -269,8 +269,8 @@ const char* jb_status_string(int status);
  * draw of the next token from a given random word (the same words at +eps and
  * -eps, so that the two scores differ by the weights alone).
  *
- * All arrays named d_* and all pointers in jb_pages and jb_kv are device memory,
- * caller-owned; the structures themselves are host memory, copied during the
+ * All arrays named d_* and all pointers in jb_pages and jb_kv are memory of the
+ * current device, caller-owned; the structures themselves are host memory, copied during the
  * call. Everything is enqueued on `stream`, and nothing is read back: lengths,
  * page tables and page counts live on the device, so a whole generation step can
  * be captured in a CUDA graph. Argument errors that the host can see are statuses,

@@ -162,14 +162,15 @@ def _check(rc: int) -> None:
         raise JbError(rc, jb_status_string(rc))
 
 
-def _stream(stream) -> ctypes.c_void_p:
+def _stream(stream, device=None) -> ctypes.c_void_p:
+    """The stream's handle; of None the current one's, on the current device, which a caller that knows it gives."""
     if stream is None:
         import torch
         # the current stream's handle without a Stream object around it (0.1 us, not 3); the
         # function is not part of torch's public interface, so it may be missing
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         if raw is not None and torch.cuda.is_initialized():
-            return ctypes.c_void_p(raw(torch.cuda.current_device()))
+            return ctypes.c_void_p(raw(torch.cuda.current_device() if device is None else device))
         return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
     if isinstance(stream, int):
         return ctypes.c_void_p(stream)
@@ -370,21 +371,30 @@ def _need_torch():
     torch = module
 
 
-def _list32(t, what: str):
-    """A one-dimensional contiguous int32 CUDA tensor: its address and length."""
+# The tensors of a call are on one device, and that is the current one: a kernel of another device would take their
+# addresses for its own memory's. `device` is the number of the cache's or, of jb_sample, of the logits'.
+
+def _list32(t, what: str, device: int):
+    """A one-dimensional contiguous int32 tensor on the call's device: its address and length."""
     if torch is None:
         _need_torch()
-    if t.dtype is not torch.int32 or not t.is_cuda or t.dim() != 1 or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous one-dimensional int32 CUDA tensor")
+    if t.dtype is not torch.int32 or t.get_device() != device or t.dim() != 1 or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous one-dimensional int32 tensor on the call's CUDA device")
     return t.data_ptr(), t.numel()
 
 
-def _two_lists(a, b, what: str):
-    pa, n = _list32(a, what)
-    pb, m = _list32(b, what)
+def _two_lists(a, b, what: str, device: int):
+    pa, n = _list32(a, what, device)
+    pb, m = _list32(b, what, device)
     if n != m:
         raise ValueError(f"{what} must have the same length")
     return pa, pb, n
+
+
+def _stream_on(device: int, stream) -> ctypes.c_void_p:
+    if torch.cuda.current_device() != device:
+        raise ValueError(f"the tensors are on CUDA device {device}, which is not the current device")
+    return _stream(stream, device)
 
 
 def _storage(dtype) -> int:
@@ -405,11 +415,14 @@ class PageTable:
         for t, dim in ((table, 2), (lens, 1), (refs, 1)):
             if t.dtype is not torch.int32 or not t.is_cuda or t.dim() != dim or not t.is_contiguous():
                 raise ValueError("table [rows, row_pages], lens [rows] and refs [pages] must be contiguous int32 CUDA tensors")
+        if lens.get_device() != table.get_device() or refs.get_device() != table.get_device():
+            raise ValueError("table, lens and refs must be on one CUDA device")
         if lens.shape[0] != table.shape[0]:
             raise ValueError("one length per row of the table")
         if not 16 <= page_tokens <= 1024 or page_tokens % 16:
             raise ValueError("page_tokens must be a multiple of 16, at most 1024")
         self.table, self.lens, self.refs, self.page_tokens = table, lens, refs, int(page_tokens)
+        self.device = table.get_device()
         self.struct = jb_pages(table.data_ptr(), lens.data_ptr(), refs.data_ptr(), table.shape[0],
                                table.shape[1], refs.shape[0], self.page_tokens)
         self.ref = ctypes.byref(self.struct)
@@ -476,8 +489,10 @@ class KVCache:
         for t in self.keys + self.values:
             if t.shape != first.shape or t.dtype != first.dtype or t.stride() != first.stride() or not t.is_cuda:
                 raise ValueError("keys and values must be CUDA tensors of one shape, type and layout")
+            if t.get_device() != pages.device:
+                raise ValueError("keys and values must be on the page table's device")
         n = len(self.keys)
-        self.torch_dtype, self.heads, self.head_dim, self.n_layers = first.dtype, heads, d, n
+        self.torch_dtype, self.heads, self.head_dim, self.n_layers, self.device = first.dtype, heads, d, n, pages.device
         self.layers = (jb_kv * n)()
         for i, (k, v) in enumerate(zip(self.keys, self.values)):
             self.layers[i] = jb_kv(k.data_ptr(), v.data_ptr(), first.stride(0), heads, d, self.dtype, by_token)
@@ -514,10 +529,10 @@ def _new(stream, make, *args, **kwargs):
         return make(*args, **kwargs)
 
 
-def _status_of(status, like, stream):
+def _status_of(status, pages, stream):
     if status is None:
-        return _new(stream, torch.empty, 1, dtype=torch.int32, device=like.device)
-    if _list32(status, "status")[1] != 1:
+        return _new(stream, torch.empty, 1, dtype=torch.int32, device=pages.refs.device)
+    if _list32(status, "status", pages.device)[1] != 1:
         raise ValueError("status must have one element")
     return status
 
@@ -527,26 +542,28 @@ def jb_cache_reserve(cache, rows, tokens, status=None, stream=None):
     that many pages too few, -1: bad list; then nothing is changed). `cache`: a KVCache or its
     PageTable."""
     pages = getattr(cache, "pages", cache)
-    pr, pt, n = _two_lists(rows, tokens, "rows and tokens")
-    status = _status_of(status, pages.refs, stream)
-    _check(lib().jb_cache_reserve(pages.ref, pr, pt, n, status.data_ptr(), _stream(stream)))
+    device = getattr(pages, "device", None)
+    pr, pt, n = _two_lists(rows, tokens, "rows and tokens", device)
+    status = _status_of(status, pages, stream)
+    _check(lib().jb_cache_reserve(pages.ref, pr, pt, n, status.data_ptr(), _stream_on(device, stream)))
     return status
 
 
 def jb_cache_free(cache, rows, stream=None) -> None:
     """The rows become empty; pages that no other row names are free."""
     pages = getattr(cache, "pages", cache)
-    pr, n = _list32(rows, "rows")
-    _check(lib().jb_cache_free(pages.ref, pr, n, _stream(stream)))
+    device = getattr(pages, "device", None)
+    pr, n = _list32(rows, "rows", device)
+    _check(lib().jb_cache_free(pages.ref, pr, n, _stream_on(device, stream)))
 
 
 def jb_cache_fork(cache: KVCache, parents, children, status=None, stream=None):
     """Row children[i] becomes a copy of row parents[i] (all at once): full pages shared, the last
     one copied in every layer. Returns the status tensor as jb_cache_reserve does."""
     pages = cache.pages
-    pp, pc, n = _two_lists(parents, children, "parents and children")
-    status = _status_of(status, pages.refs, stream)
-    handle = _stream(stream)
+    pp, pc, n = _two_lists(parents, children, "parents and children", cache.device)
+    status = _status_of(status, pages, stream)
+    handle = _stream_on(cache.device, stream)
     ws, nbytes, held = cache._pages_workspace(n, stream, handle)
     _check(lib().jb_cache_fork(pages.ref, cache.layers, cache.n_layers, pp, pc, n, status.data_ptr(), ws, nbytes, handle))
     return status
@@ -555,8 +572,8 @@ def jb_cache_fork(cache: KVCache, parents, children, status=None, stream=None):
 def jb_cache_compact(cache: KVCache, status=None, stream=None):
     """Moves the pages in use to the lowest ids; returns the status tensor: how many they are."""
     pages = cache.pages
-    status = _status_of(status, pages.refs, stream)
-    handle = _stream(stream)
+    status = _status_of(status, pages, stream)
+    handle = _stream_on(cache.device, stream)
     ws, nbytes, held = cache._pages_workspace(0, stream, handle)
     _check(lib().jb_cache_compact(pages.ref, cache.layers, cache.n_layers, status.data_ptr(), ws, nbytes, handle))
     return status
@@ -564,8 +581,8 @@ def jb_cache_compact(cache: KVCache, status=None, stream=None):
 
 def _heads_of(t, heads: int, cache: KVCache, n: int, what: str):
     """Strides of a [n, heads, head_dim] CUDA tensor whose rows are contiguous."""
-    if t.dtype is not cache.torch_dtype or not t.is_cuda:
-        raise ValueError(f"{what} must be CUDA tensors of the cache's type")
+    if t.dtype is not cache.torch_dtype or t.get_device() != cache.device:
+        raise ValueError(f"{what} must be tensors of the cache's type on its CUDA device")
     if t.dim() != 3 or t.shape != (n, heads, cache.head_dim):
         raise ValueError(f"{what} must be [{n}, {heads}, {cache.head_dim}], got {tuple(t.shape)}")
     a, b, c = t.stride()
@@ -576,11 +593,11 @@ def _heads_of(t, heads: int, cache: KVCache, n: int, what: str):
 
 def jb_cache_write(cache: KVCache, layer: int, k, v, rows, pos, stream=None) -> None:
     """Keys and values k[i], v[i] ([n, heads, head_dim]) of a layer to position pos[i] of row rows[i]."""
-    pr, pp, n = _two_lists(rows, pos, "rows and positions")
+    pr, pp, n = _two_lists(rows, pos, "rows and positions", cache.device)
     ka, kb = _heads_of(k, cache.heads, cache, n, "new keys")
     va, vb = _heads_of(v, cache.heads, cache, n, "new values")
     _check(lib().jb_cache_write(cache.pages.ref, cache.layer_refs[layer], k.data_ptr(), ka, kb, v.data_ptr(), va, vb,
-                                pr, pp, n, _stream(stream)))
+                                pr, pp, n, _stream_on(cache.device, stream)))
 
 
 def jb_attend(cache: KVCache, layer: int, q, rows, pos, out=None, scale: Optional[float] = None,
@@ -590,21 +607,21 @@ def jb_attend(cache: KVCache, layer: int, q, rows, pos, out=None, scale: Optiona
     biased by slopes[head] (t - pos), limited to the last `window` positions. ``workspace``: by default
     one that the cache keeps for the stream; ``cache.new_workspace`` makes others, for instance one for
     all the calls that a CUDA graph captures (by default each gets its own there)."""
-    pr, pp, n = _two_lists(rows, pos, "rows and positions")
+    pr, pp, n = _two_lists(rows, pos, "rows and positions", cache.device)
     heads = q.shape[1] if q.dim() == 3 else 0
     qa, qb = _heads_of(q, heads, cache, n, "queries")
     if out is None:
         out = _new(stream, torch.empty, (n, heads, cache.head_dim), dtype=q.dtype, device=q.device)
     oa, ob = _heads_of(out, heads, cache, n, "outputs")
-    if slopes is not None and (slopes.dtype is not torch.float32 or not slopes.is_cuda or slopes.shape != (heads,)
-                               or not slopes.is_contiguous()):
-        raise ValueError("slopes must be a contiguous float32 CUDA tensor, one per query head")
-    handle = _stream(stream)
+    if slopes is not None and (slopes.dtype is not torch.float32 or slopes.get_device() != cache.device
+                               or slopes.shape != (heads,) or not slopes.is_contiguous()):
+        raise ValueError("slopes must be a contiguous float32 tensor on the cache's CUDA device, one per query head")
+    handle = _stream_on(cache.device, stream)
     if workspace is None:
         ws, nbytes, held = cache._attend_workspace(heads, stream, handle)
     else:
-        if not workspace.is_cuda or not workspace.is_contiguous():
-            raise ValueError("workspace must be a contiguous CUDA tensor")
+        if workspace.get_device() != cache.device or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on the cache's CUDA device")
         ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     scores = jb_scores(cache.head_dim ** -0.5 if scale is None else scale, softcap, window,
                        None if slopes is None else slopes.data_ptr())
@@ -613,15 +630,15 @@ def jb_attend(cache: KVCache, layer: int, q, rows, pos, out=None, scale: Optiona
     return out
 
 
-def _per_row(value, default, words, dtype, stream):
+def _per_row(value, default, words, dtype, stream, device):
     """A setting of jb_sample as the address of its entries (None where it is the default) and the tensor
     that holds them, one for each of the words."""
     if type(value) is not torch.Tensor and not isinstance(value, torch.Tensor):
         if value == default:
             return None, None
         value = _new(stream, torch.full, words.shape, value, dtype=dtype, device=words.device)
-    if value.dtype is not dtype or not value.is_cuda or value.shape != words.shape or not value.is_contiguous():
-        raise ValueError(f"a setting per row must be a contiguous {dtype} CUDA tensor of one entry per word")
+    if value.dtype is not dtype or value.get_device() != device or value.shape != words.shape or not value.is_contiguous():
+        raise ValueError(f"a setting per row must be a contiguous {dtype} tensor of one entry per word on the logits' CUDA device")
     return value.data_ptr(), value
 
 
@@ -633,30 +650,31 @@ def jb_sample(logits, words, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tok
     if torch is None:
         _need_torch()
     i32, f32 = torch.int32, torch.float32
-    if logits.dim() != 2 or not logits.is_cuda:
+    device = logits.get_device()
+    if logits.dim() != 2 or device < 0:
         raise ValueError("logits must be a CUDA tensor [n, vocab]")
     n, vocab = logits.shape
     pitch, step = logits.stride()
     if step != 1 and vocab > 1:
         raise ValueError("logits must be contiguous in a row")
-    if (words.dtype is not i32 and words.dtype is not torch.uint32) or not words.is_cuda or words.dim() != 1 or words.numel() != n \
-            or not words.is_contiguous():
-        raise ValueError("words must be a contiguous int32 or uint32 CUDA tensor, one per row")
-    t, t_ = _per_row(temperature, 1.0, words, f32, stream)
-    k, k_ = _per_row(top_k, 0, words, i32, stream)
-    p, p_ = _per_row(top_p, 1.0, words, f32, stream)
-    m, m_ = _per_row(min_p, 0.0, words, f32, stream)
+    if (words.dtype is not i32 and words.dtype is not torch.uint32) or words.get_device() != device or words.dim() != 1 \
+            or words.numel() != n or not words.is_contiguous():
+        raise ValueError("words must be a contiguous int32 or uint32 tensor on the logits' CUDA device, one per row")
+    t, t_ = _per_row(temperature, 1.0, words, f32, stream, device)
+    k, k_ = _per_row(top_k, 0, words, i32, stream, device)
+    p, p_ = _per_row(top_p, 1.0, words, f32, stream, device)
+    m, m_ = _per_row(min_p, 0.0, words, f32, stream, device)
     if tokens is None:
         tokens = _new(stream, torch.empty_like, words, dtype=i32)
-    elif _list32(tokens, "tokens")[1] != n:
+    elif _list32(tokens, "tokens", device)[1] != n:
         raise ValueError("one token per row")
     if logprobs is None:
         logprobs = _new(stream, torch.empty_like, words, dtype=f32)
-    elif logprobs.dtype is not f32 or not logprobs.is_cuda or logprobs.shape != words.shape or not logprobs.is_contiguous():
-        raise ValueError("logprobs must be a contiguous float32 CUDA tensor, one per row")
+    elif logprobs.dtype is not f32 or logprobs.get_device() != device or logprobs.shape != words.shape or not logprobs.is_contiguous():
+        raise ValueError("logprobs must be a contiguous float32 tensor on the logits' CUDA device, one per row")
     settings = jb_sampling(t, k, p, m)
     _check(lib().jb_sample(logits.data_ptr(), pitch, _storage(logits.dtype), n, vocab, ctypes.byref(settings),
-                           words.data_ptr(), tokens.data_ptr(), logprobs.data_ptr(), _stream(stream)))
+                           words.data_ptr(), tokens.data_ptr(), logprobs.data_ptr(), _stream_on(device, stream)))
     return tokens, logprobs
 
 

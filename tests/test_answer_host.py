@@ -173,3 +173,104 @@ def test_outputs_of_long_strides(jb):
                                  (2147483647, 2, 8, far, MIS), (2147483647, 65536, far - 8, far, MIS), (3, 65536, far, far - 8, MIS),
                                  (2147483647, 2, 8, 8 * 2147483647, MIS), (2147483647, 2, 8, 8 * 2147483646, INV)):
         assert attend(jb, q, kv, n=n, heads=heads, oa=oa, ob=ob, ws=FAKE + 8) == rc, (n, heads, oa, ob)
+
+
+def on_device(index, *tensors):
+    """The tensors as if they were on that CUDA device."""
+    import torch
+
+    class There(torch.Tensor):
+        where = index
+        is_cuda = property(lambda self: True)
+
+        def get_device(self):
+            return self.where
+
+    return [t.as_subclass(There) for t in tensors]
+
+
+class Launches:
+    """A library that counts its calls."""
+
+    def __init__(self):
+        self.calls = 0
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls += 1
+            return 0
+        return call
+
+
+def a_call(jb, name, lists, cache_on):
+    """The call's arguments; `lists` maps an argument's place to its device, 0 by default."""
+    import torch
+    i32, f32 = torch.int32, torch.float32
+    table, lens, refs = on_device(cache_on, torch.zeros(2, 3, dtype=i32), torch.zeros(2, dtype=i32), torch.zeros(6, dtype=i32))
+    k, v = on_device(cache_on, torch.zeros(6, 2, 16, 64), torch.zeros(6, 2, 16, 64))
+    cache = jb.KVCache(jb.PageTable(table, lens, refs, 16), [k], [v])
+    new = lambda *shape, dtype=i32: torch.zeros(shape, dtype=dtype)  # noqa: E731
+    args = dict(jb_cache_reserve=dict(rows=new(2), tokens=new(2), status=new(1)), jb_cache_free=dict(rows=new(2)),
+                jb_cache_fork=dict(parents=new(2), children=new(2), status=new(1)), jb_cache_compact=dict(status=new(1)),
+                jb_cache_write=dict(k=new(2, 2, 64, dtype=f32), v=new(2, 2, 64, dtype=f32), rows=new(2), pos=new(2)),
+                jb_attend=dict(q=new(2, 4, 64, dtype=f32), rows=new(2), pos=new(2), out=new(2, 4, 64, dtype=f32), slopes=new(4, dtype=f32),
+                               workspace=new(1 << 20)),
+                jb_sample=dict(logits=new(2, 9, dtype=f32), words=new(2), temperature=new(2, dtype=f32), top_k=new(2), top_p=new(2, dtype=f32),
+                               min_p=new(2, dtype=f32), tokens=new(2), logprobs=new(2, dtype=f32)))[name]
+    args = {a: on_device(lists.get(a, lists.get("all", 0)), t)[0] for a, t in args.items()}
+    first = {"jb_sample": (), "jb_attend": (cache, 0), "jb_cache_write": (cache, 0)}.get(name, (cache,))
+    return first, args
+
+
+CALLS = dict(jb_cache_reserve=3, jb_cache_free=1, jb_cache_fork=3, jb_cache_compact=1, jb_cache_write=4, jb_attend=6, jb_sample=8)
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_tensors_of_another_device_are_refused(jb, name, monkeypatch):
+    import torch
+    current = [0]
+    library = Launches()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    _, args = a_call(jb, name, {}, 0)
+    assert len(args) == CALLS[name]
+    for one in args:                                                     # one argument elsewhere
+        first, args = a_call(jb, name, {one: 1}, 0)
+        with monkeypatch.context() as m:
+            m.setattr(jb, "lib", lambda: library)
+            with pytest.raises(ValueError, match="device"):
+                getattr(jb, name)(*first, **args, stream=1)
+    for current[0], lists, cache_on in ((0, 1, 1), (1, 0, 0), (0, 1, 0), (1, 1, 0)):
+        if name == "jb_sample" and current[0] == lists:
+            continue                                                     # it has no cache
+        first, args = a_call(jb, name, {"all": lists}, cache_on)
+        with monkeypatch.context() as m:
+            m.setattr(jb, "lib", lambda: library)
+            with pytest.raises(ValueError, match="device"):
+                getattr(jb, name)(*first, **args, stream=1)
+    assert library.calls == 0
+
+
+@pytest.mark.parametrize("name", ["jb_cache_reserve", "jb_cache_free", "jb_cache_write", "jb_attend", "jb_sample"])
+@pytest.mark.parametrize("device", [0, 3])
+def test_tensors_of_the_current_device_are_taken(jb, name, device, monkeypatch):
+    import torch
+    library = Launches()
+    first, args = a_call(jb, name, {"all": device}, device)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: device)
+    monkeypatch.setattr(jb, "lib", lambda: library)
+    getattr(jb, name)(*first, **args, stream=1)
+    assert library.calls == 1
+
+
+def test_a_cache_is_on_one_device(jb):
+    import torch
+    i32 = torch.int32
+    whole = lambda a, b, c: jb.PageTable(*on_device(a, torch.zeros(2, 3, dtype=i32)), *on_device(b, torch.zeros(2, dtype=i32)),  # noqa: E731
+                                         *on_device(c, torch.zeros(6, dtype=i32)), 16)
+    for where in ((0, 0, 1), (0, 1, 0), (1, 0, 0)):
+        with pytest.raises(ValueError, match="device"):
+            whole(*where)
+    kv = lambda at: on_device(at, torch.zeros(6, 2, 16, 64))  # noqa: E731
+    for where in ((0, 1), (1, 0), (1, 1)):
+        with pytest.raises(ValueError, match="device"):
+            jb.KVCache(whole(0, 0, 0), kv(where[0]), kv(where[1]))
