@@ -149,7 +149,7 @@ __device__ __forceinline__ bool seen_before(unsigned* seen, int row) {
     return (atomicOr(&seen[row >> 5], bit) & bit) != 0;
 }
 
-// Dynamic shared memory of the plans: base[n + 1], then a bit for each row.
+// Dynamic shared memory of the plans: base[n], then a bit for each row.
 __device__ __forceinline__ int owner_of(const int* base, int n, int rank) {
     int lo = 0, hi = n - 1;  // the last i with base[i] <= rank
     while (lo < hi) {
@@ -458,25 +458,27 @@ __global__ void __launch_bounds__(256) write_kernel(Pages p, const __grid_consta
     }
 }
 
+// Dynamic shared memory of a plan, and the most that one takes.
+constexpr size_t plan_shared(int n_rows, int n) { return 4ull * n + 4ull * ((n_rows + 31) / 32); }
+constexpr int kMostShared = static_cast<int>(plan_shared(kMaxRows, kMaxListed));
+
 // A small plan takes one CTA; eight share larger ones. work: pages to rank and entries to write.
 constexpr uint64_t kOneCta = 16384;
 
 template <typename... Params, typename... Args>
 cudaError_t launch_plan(void (*kernel)(Params...), uint64_t work, size_t shared, cudaStream_t s, const Args&... args) {
-    if (shared > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(shared));
+    if (shared > 48 * 1024) {  // the limit is the kernel's, not the call's: every host thread sets the same one
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
         if (e != cudaSuccess) return e;
     }
     const unsigned ctas = work <= kOneCta ? 1 : 8;
     return launch(kernel, ctas, kPlanThreads, shared, ctas, s, args...);
 }
 
-size_t plan_shared(const Pages& p, int n) { return 4ull * n + 4ull * ((p.n_rows + 31) / 32); }
-
 }  // namespace
 
 cudaError_t launch_reserve(const Pages& p, const int* rows, const int* tokens, int n, int* status, cudaStream_t s) {
-    return launch_plan(reserve_kernel, p.n_pages, plan_shared(p, n), s, p, rows, tokens, n, status);
+    return launch_plan(reserve_kernel, p.n_pages, plan_shared(p.n_rows, n), s, p, rows, tokens, n, status);
 }
 
 cudaError_t launch_free(const Pages& p, const int* rows, int n, cudaStream_t s) {
@@ -485,7 +487,7 @@ cudaError_t launch_free(const Pages& p, const int* rows, int n, cudaStream_t s) 
 
 cudaError_t launch_fork_plan(const Pages& p, const int* parents, const int* children, int n, int* status, int* ws,
                              cudaStream_t s) {
-    return launch_plan(fork_plan_kernel, p.n_pages + static_cast<uint64_t>(n) * p.row_pages, plan_shared(p, n), s, p, parents,
+    return launch_plan(fork_plan_kernel, p.n_pages + static_cast<uint64_t>(n) * p.row_pages, plan_shared(p.n_rows, n), s, p, parents,
                        children, n, status, ws);
 }
 

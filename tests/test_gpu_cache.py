@@ -1,6 +1,7 @@
 """The pages of a cache against a plain model of them: rows as lists of page ids, counts, and what
 every place of every page holds. All values are compared exactly."""
 import random
+import threading
 
 import pytest
 import torch
@@ -341,3 +342,31 @@ def test_a_generation_step_in_a_graph():
     for r in range(2):
         ids = b.pages.table[r, :3].long()
         assert b.pools[1][ids].transpose(1, 2).reshape(48, 3, 8)[:40, 0, 0].tolist() == [float(i) for i in range(40)]
+
+
+def test_long_and_longer_lists_at_the_same_time():
+    """Host threads whose lists need different amounts of shared memory, above what a launch has by default: each call
+    is legal by itself, and so they are side by side."""
+    n_rows = 40_000
+
+    def work(n, rounds, errors):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                pages = jb.PageTable.empty(n_rows, 1, 64, 16)
+                rows, none, status = torch.arange(n, dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda"), i32([7])
+                stream.synchronize()
+                for _ in range(rounds):
+                    jb.jb_cache_reserve(pages, rows, none, status=status)
+                stream.synchronize()
+                assert status.item() == 0
+        except Exception as e:  # noqa: BLE001
+            errors.append(e)
+
+    errors = []
+    threads = [threading.Thread(target=work, args=(n, 3000, errors)) for n in 2 * (12_300, 13_500, 14_700, 16_384)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors[0]
