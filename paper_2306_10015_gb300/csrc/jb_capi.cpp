@@ -428,7 +428,7 @@ JB_EXPORT const char* jb_status_string(int status) {
         case JB_OK: return "ok";
         case JB_ERR_INVALID_ARG: return "invalid argument";
         case JB_ERR_UNSUPPORTED_DTYPE: return "unsupported dtype (use JB_F32 or JB_BF16)";
-        case JB_ERR_MISALIGNED: return "pointer or stride not aligned as the call needs";
+        case JB_ERR_MISALIGNED: return "segment pointer not aligned to its element size, or another pointer or stride not as the call needs";
         case JB_ERR_DUPLICATE_SEED: return "duplicate (machine_id, step, sample_id) seed";
         case JB_ERR_CUDA: return "CUDA runtime or launch error";
         case JB_ERR_RANGE: return "update coefficient not finite in fp32";

@@ -274,3 +274,8 @@ def test_a_cache_is_on_one_device(jb):
     for where in ((0, 1), (1, 0), (1, 1)):
         with pytest.raises(ValueError, match="device"):
             jb.KVCache(whole(0, 0, 0), kv(where[0]), kv(where[1]))
+
+
+def test_the_text_of_a_misaligned_argument_tells_of_segments(jb):
+    text = jb.jb_status_string(MIS)
+    assert "segment pointer not aligned to its element size" in text and "stride" in text
