@@ -329,3 +329,82 @@ def test_groups_of_a_run_of_queries_pass_32_bits():
     got = jb.jb_attend(cache, 0, q, rows, torch.where(at >= 0, at + first, -1).int().cuda())
     want, tol = reference(short, 0, q, rows, at.cuda())
     assert ((got.double() - want).abs() <= tol).all() and (got[17 * 40:17 * 41] != 0).any() and (got[:17 * 40] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_two_streams_at_the_same_time(dtype):
+    """Calls whose rows are split, on one cache from two streams without waiting in between: each stream has its own
+    parts to join."""
+    cache = make(dtype, [9000, 5, 3000], 2, 128, 16)
+    rows, pos = i32([0, 1, 2]), cache.pages.lens - 1
+    queries = [query(3, 4, 128, dtype, seed=s) for s in range(20, 26)]
+    want = [check(cache, 0, q, rows, pos) for q in queries]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [jb.jb_attend(cache, 0, queries[i % 6], rows, pos, stream=streams[i % 2]) for i in range(120)]
+    torch.cuda.synchronize()
+    for i, x in enumerate(got):
+        assert torch.equal(x, want[i % 6])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_kept_workspaces_grow(dtype):
+    """Few query heads, then more of them (a larger workspace on the same stream), and few again."""
+    cache = make(dtype, [6000, 700], 2, 128, 16)
+    rows, pos = i32([0, 1]), cache.pages.lens - 1
+    first = {}
+    for group in (1, 16, 1, 2, 16, 9, 1):
+        got = check(cache, 0, query(2, 2 * group, 128, dtype), rows, pos)
+        assert torch.equal(first.setdefault(group, got), got)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("length", [40, 5000])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_values_that_are_not_finite_and_seen(dtype, length, bad):
+    """They reach their own element of the heads that read them, and nothing else; in fp32 an infinity stays one. The
+    token's weight is made large, so that it is not lost in the sum."""
+    cache = make(dtype, [length], 2, 64, 16)
+    q, rows, pos = query(1, 6, 64, dtype), i32([0]), i32([length - 1])
+    t = length // 2
+    page = int(cache.pages.table[0, t // 16])
+    cache.keys[0][page, 1, t % 16] = q[0, 3:].mean(0)
+    want, tol = reference(cache, 0, q, rows, pos)
+    cache.values[0][page, 1, t % 16, 17] = bad
+    got = jb.jb_attend(cache, 0, q, rows, pos)
+    hit = torch.zeros(1, 6, 64, dtype=torch.bool, device="cuda")
+    hit[0, 3:, 17] = True
+    assert not torch.isfinite(got[hit]).any()
+    if dtype == "f32" and not math.isnan(bad):
+        assert (got[hit] == bad).all()
+    assert ((got.double() - want).abs() <= tol)[~torch.isnan(want) & ~hit].all() and torch.isfinite(got[~hit]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("length", [40, 5000])
+def test_keys_that_are_not_finite_and_seen(dtype, length):
+    """A score of +inf or NaN gives NaN, one of -inf leaves its token out, and where all are -inf nothing is seen."""
+    cache = make(dtype, [length], 2, 64, 16)
+    q, rows, pos = query(1, 4, 64, dtype), i32([0]), i32([length - 1])
+    q[0, 2:, 5] = q[0, 2:, 5].abs() + 0.5
+    t = length // 3
+    page = int(cache.pages.table[0, t // 16])
+    clean, tol = reference(cache, 0, q, rows, pos)
+    for bad in (math.nan, math.inf):
+        cache.keys[0][page, 1, t % 16, 5] = bad
+        got = jb.jb_attend(cache, 0, q, rows, pos)
+        assert torch.isnan(got[0, 2:]).all() and ((got.double() - clean).abs() <= tol)[0, :2].all()
+    cache.keys[0][page, 1, t % 16, 5] = -math.inf
+    got = jb.jb_attend(cache, 0, q, rows, pos)[0, 2:].double()
+    others = torch.arange(length, device="cuda")
+    others = others[others != t]
+    ids = cache.pages.table[0, others // 16].long()
+    k, v = (x[0][ids, 1, others % 16].double() for x in (cache.keys, cache.values))
+    prod = q[0, 2:].double()[:, None] * k / 8.0
+    p = torch.softmax(prod.sum(-1), -1)
+    size = prod.abs().sum(-1).amax(1, keepdim=True)
+    rel = 2 * (2 * 80 * 2.0**-23 * size + 2.0**-21) + length * 2.0**-23 + (2.0**-16 if dtype == "bf16" else 0)
+    assert ((got - p @ v).abs() <= (p @ v.abs()) * rel + (2.0**-8 * (p @ v).abs() if dtype == "bf16" else 0)).all()
+    cache.keys[0][:, 1, :, 5] = -math.inf
+    got = jb.jb_attend(cache, 0, q, rows, pos)
+    assert (got[0, 2:] == 0).all() and ((got.double() - clean).abs() <= tol)[0, :2].all()

@@ -370,3 +370,39 @@ def test_long_and_longer_lists_at_the_same_time():
     for t in threads:
         t.join()
     assert not errors, errors[0]
+
+
+def test_forks_of_unlike_length_and_two_caches_at_the_same_time():
+    """A kept workspace that has to grow between calls, and forks, frees and compactions of two caches from two
+    streams without waiting in between."""
+    caches = [Both(n_rows=64, row_pages=4, n_pages=200, layers=2) for _ in range(2)]
+    for b in caches:
+        b.reserve([0, 1, 2], [37, 20, 50])
+        b.fork([0], [3])
+        b.fork([0, 1, 2] * 15, list(range(4, 49)))
+        b.free(list(range(4, 30)))
+        b.compact()
+        b.fork([1, 2], [50, 51])
+    lists = [(i32([0, 1, 2]), i32([10, 11, 12])), (i32([2] * 20), i32(list(range(10, 30))))]
+    gone = i32(list(range(10, 20)))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for turn in range(6):
+        for b, s in zip(caches, streams):
+            jb.jb_cache_fork(b.cache, *lists[turn % 2], stream=s)
+            jb.jb_cache_free(b.cache, gone, stream=s)
+            jb.jb_cache_compact(b.cache, stream=s)
+    torch.cuda.synchronize()
+    for b in caches:
+        for turn in range(6):
+            status, copies = b.model.fork(*[x.tolist() for x in lists[turn % 2]])
+            for a, c, n in copies:
+                for x in b.want:
+                    x[c, :, :n] = x[a, :, :n]
+            b.model.free(list(range(10, 20)))
+            _, moves = b.model.compact()
+            for x in b.want:
+                if moves:
+                    a, c = zip(*moves)
+                    x[list(c)] = x[list(a)]
+        b.same()
