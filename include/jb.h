@@ -92,7 +92,7 @@ typedef enum {
     JB_OK = 0,
     JB_ERR_INVALID_ARG = -1,      /* NULL pointer, negative count, bad scalar, overlap */
     JB_ERR_UNSUPPORTED_DTYPE = -2,
-    JB_ERR_MISALIGNED = -3,       /* segment pointer not aligned to its element size */
+    JB_ERR_MISALIGNED = -3,       /* segment pointer not aligned to its element size; calls say what else they need */
     JB_ERR_DUPLICATE_SEED = -4,   /* two pairs with the same (machine_id, step, sample_id) */
     JB_ERR_CUDA = -5,             /* a CUDA runtime call or launch failed */
     JB_ERR_RANGE = -6,            /* a coefficient -lr deq(q) / denom is not finite in fp32 */
@@ -383,11 +383,13 @@ typedef struct {
  * t > d_pos[i] - window):
  *   out = sum_t exp(x_t) v_t / sum_t exp(x_t)
  * A new token's query comes with the position that its key was written to; the tokens
- * of a prompt are queries of one row with consecutive positions. A query that sees
+ * of a prompt are queries of one row with consecutive positions, each of which reads the
+ * row for itself: long prompts are slow. A query that sees
  * nothing (position -1, or a row or position out of range) gets zeros; a position whose
- * page is missing is not seen. What a page holds past the last position seen has no
- * effect, NaN included. Results are bitwise repeatable.
- * Scores, maxima and sums are fp32; fp32 caches are computed in fp32. With bf16 the
+ * page is missing is not seen, nor is one whose score is -inf. What a page holds past the
+ * last position seen has no effect, NaN included. Results are bitwise repeatable.
+ * Scores, maxima and sums are fp32 (scores beyond 2e38 in size count as infinite); fp32
+ * caches are computed in fp32. With bf16 the
  * products run on the tensor cores with fp32 sums, and a weight exp(x_t) enters them
  * as the sum of two bf16 numbers (16 bits of it), so that an infinite value that is seen
  * gives an infinity or NaN.

@@ -23,6 +23,9 @@ and, for scores that are not losses, what writing an answer with the perturbed m
 * ``jb_attend``  attention of new tokens over the pages
 * ``jb_sample``  the next token from its logits and a given random word
 
+Their tensors are on one device, the current one. No gradients flow through any call here: results
+of tensors that require them carry none.
+
 There is no CPU fallback: if ``libjb.so`` is missing, loading it raises.
 """
 from __future__ import annotations
@@ -604,7 +607,8 @@ def jb_attend(cache: KVCache, layer: int, q, rows, pos, out=None, scale: Optiona
               softcap: float = 0.0, window: int = 0, slopes=None, workspace=None, stream=None):
     """Attention of queries q [n, q_heads, head_dim] over positions <= pos[i] of row rows[i];
     returns ``out``. Scores are scale q.k (default 1 / sqrt(head_dim)), capped by softcap tanh,
-    biased by slopes[head] (t - pos), limited to the last `window` positions. ``workspace``: by default
+    biased by slopes[head] (t - pos), limited to the last `window` positions. The tokens of a prompt may be
+    queries of one row, but each reads the row for itself: long prompts are slow. ``workspace``: by default
     one that the cache keeps for the stream; ``cache.new_workspace`` makes others, for instance one for
     all the calls that a CUDA graph captures (by default each gets its own there)."""
     pr, pp, n = _two_lists(rows, pos, "rows and positions", cache.device)

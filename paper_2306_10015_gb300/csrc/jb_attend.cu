@@ -15,6 +15,10 @@
 // decided at the start: keeping a share back for the warps that are done first was slower everywhere (by 2 to
 // 30 %), and so were twice as many CTAs as run at once (1 to 20 %): a warp that is done leaves its bandwidth to
 // the others, and every further piece costs a start and a join.
+//
+// What it is not made for: the tokens of a prompt, each of which streams its row's keys and values for itself (one
+// of 2048 bf16 tokens, 32 heads of 128: 5.1 ms), and groups of more than 8 (fp32) or 16 (bf16) query heads, which
+// read them once for each block of so many heads (16 fp32 heads of 256: 2.2 times the floor).
 #include <atomic>
 
 #include <cuda_bf16.h>
@@ -552,7 +556,7 @@ __device__ __forceinline__ void load_transposed(uint32_t (&m)[4], uint32_t at) {
 // Weights enter it with 16 bits, as two bf16 numbers. With up to 8 query heads to a key head (kH = 8) the
 // other 8 rows hold what rounding drops, at no cost; with more, a second product adds it.
 template <int D, int kH>
-constexpr int kBf16Ctas = D == 64 ? 3 : D == 128 ? 2 : 1;  // on an SM
+constexpr int kBf16Ctas = D == 64 ? 3 : D == 128 ? 2 : 1;  // on an SM; heads of 256 spill 32 to 164 bytes at 255 registers
 
 template <int D, int kH, bool kExtra>
 __global__ void __launch_bounds__(kThreads, kBf16Ctas<D, kH>) attend_bf16_kernel(const __grid_constant__ Params p) {

@@ -29,7 +29,7 @@ constexpr unsigned kAll = 0xFFFFFFFFu;
 constexpr int kIndexBins = 1024;       // bins of an index, 2^18 tokens at most
 constexpr int kMaxCluster = 8;
 constexpr int kSms = 152;
-constexpr int kResident = 1024;        // threads on an SM: 64 registers each; 1536 and 2048 are slower
+constexpr int kResident = 1024;        // threads on an SM: 64 registers each (4 bytes spilled); 1536 and 2048 are slower
 constexpr int kMaxSlice = 65536;       // tokens of one CTA: sums of halves of their weights fit 32 bits
 constexpr int kLarge = 512;            // threads of a CTA, 256 for small vocabularies
 constexpr int kSmallVocab = 8192;
