@@ -439,6 +439,115 @@ int jb_sample(const void* d_logits, uint64_t row_stride, int dtype, int n, int v
               struct CUstream_st* stream);
 
 /* ---------------------------------------------------------------------------
+ * Drafted tokens. Several tokens of an answer can be checked in one pass over the weights
+ * and the cache: a tree of guesses is written behind its row's tokens (jb_cache_reserve,
+ * jb_cache_append), attended to at once (jb_attend_tree), and of it the path that the model
+ * writes itself is kept (jb_cache_keep). With random words given by position the answers
+ * are those of one token at a time. A chain is a tree: the tokens of a prompt can be written
+ * 256 at a time in this way.
+ * ------------------------------------------------------------------------- */
+
+/* Trees of drafted tokens: the nodes of tree i are starts[i] .. starts[i + 1] - 1 of a list of
+ * n_nodes, at most 256, and they are the last tokens of row rows[i], in that order.
+ * parents[] counts within the tree: the node that a node follows, before it in the list, or
+ * -1 for one that follows the row's tokens before the tree. Device arrays; `starts` ascends,
+ * and no row is listed twice. At most 16384 trees. */
+typedef struct {
+    const int32_t* rows;    /* [n] */
+    const int32_t* starts;  /* [n + 1] */
+    const int32_t* parents; /* [n_nodes] */
+    int32_t n;
+    int32_t n_nodes;
+} jb_trees;
+
+/* How queries and keys are turned by their positions. Pair j of the first `dims` elements of a
+ * head (even, at most head_dim; the others stay) is turned by t steps[j] mod 2^64 parts of
+ * 2^-64 of a full turn at position t: exact at any position. Pairs are (j, j + dims / 2), or
+ * neighbours (2 j, 2 j + 1) with interleaved != 0. For the usual powers steps[j] is
+ * 2^64 base^(-2 j / dims) / (2 pi). */
+typedef struct {
+    const uint64_t* steps; /* device, [dims / 2], 8-byte aligned */
+    int32_t dims;
+    int32_t interleaved;
+} jb_rotation;
+
+/*
+ * jb_cache_append -- jb_cache_write with the rotation on the way: the key of token i is turned
+ * by its position d_turns[i] and written, with its value, to position d_pos[i] of row
+ * d_rows[i]; its queries are turned alike and written to d_q_out. d_turns differs from d_pos
+ * for a tree's nodes (their places follow one another, their positions go by depth) and for a
+ * text whose beginning the cache no longer holds; NULL: as d_pos. The rotation is computed in
+ * fp32 from an angle exact to 2^-24 of itself, and rounded once.
+ * A token whose row, position or page is out of range is not written (its queries are turned);
+ * two tokens with the same place race.
+ *   q_heads    any number of query heads, 0: none (d_q and d_q_out are not looked at)
+ *   strides    in elements, multiples of 16 bytes; pointers 16-byte aligned
+ *   d_q_out    d_q itself with its strides, or apart from all that is read. What shares bytes
+ *              otherwise, or cannot be told not to, is refused: JB_ERR_INVALID_ARG
+ */
+int jb_cache_append(const jb_pages* pages, const jb_kv* layer, const jb_rotation* rotation, const void* d_q,
+                    uint64_t q_token_stride, uint64_t q_head_stride, int q_heads, void* d_q_out,
+                    uint64_t out_token_stride, uint64_t out_head_stride, const void* d_k, uint64_t k_token_stride,
+                    uint64_t k_head_stride, const void* d_v, uint64_t v_token_stride, uint64_t v_head_stride,
+                    const int32_t* d_rows, const int32_t* d_pos, const int32_t* d_turns, int n, struct CUstream_st* stream);
+
+/*
+ * jb_attend_tree -- attention of the nodes of trees, as jb_attend's: node j of tree i (query
+ * starts[i] + j) sees its row's tokens before the tree, its ancestors and itself. For windows
+ * and slopes a node's position is that of the token that it would be in a chain: tokens
+ * before the tree plus its depth.
+ * A node whose chain of parents is not valid (an index not below its own, or below -1) gets
+ * zeros, and so do the nodes of a tree whose row is out of range, holds fewer tokens than the
+ * tree, or that has more than 256 nodes. Queries of no tree are left as they are.
+ * Accuracy, missing pages, infinite scores and what unseen places hold: as jb_attend.
+ *   q_heads    a multiple of the layer's heads
+ *   strides    in elements, multiples of 16 bytes; pointers 16-byte aligned. Outputs share bytes
+ *              neither with one another nor with queries: JB_ERR_INVALID_ARG
+ *   workspace  jb_attend_tree_workspace(...) bytes, 16-byte aligned, contents free. Calls that
+ *              may run at the same time need one each.
+ */
+int jb_attend_tree(const jb_pages* pages, const jb_kv* layer, const jb_scores* scores, const jb_trees* trees, const void* d_q,
+                   uint64_t q_row_stride, uint64_t q_head_stride, int q_heads, void* d_out, uint64_t out_row_stride,
+                   uint64_t out_head_stride, void* workspace, uint64_t workspace_bytes, struct CUstream_st* stream);
+
+/* Device bytes that jb_attend_tree works in, whatever the trees. */
+uint64_t jb_attend_tree_workspace(const jb_kv* layer);
+
+/*
+ * jb_cache_keep -- of each tree the path from its root to node d_leaves[i] stays (-1: nothing
+ * does): the path's keys and values move, in every layer, to the places behind the tokens
+ * before the tree, the row ends with them, and pages behind are given back. *d_status receives
+ *    0   done
+ *   -1   a tree that is not valid (see jb_attend_tree) or whose row is listed twice, a leaf out
+ *        of range or without a valid path, or a token that would move from a missing page or to
+ *        one that is missing or that other rows name too: nothing is changed
+ *   workspace  jb_cache_keep_workspace(trees) bytes, 16-byte aligned, contents free
+ */
+int jb_cache_keep(const jb_pages* pages, const jb_kv* layers, int n_layers, const jb_trees* trees, const int32_t* d_leaves,
+                  int32_t* d_status, void* workspace, uint64_t workspace_bytes, struct CUstream_st* stream);
+
+/* Device bytes that jb_cache_keep works in. */
+uint64_t jb_cache_keep_workspace(const jb_trees* trees);
+
+/*
+ * jb_q4_matmul -- products of n rows with a matrix of 4-bit weights, as they are between two
+ * calls of jb_perturb_q4: y_i[o] = sum_k x_i[k] level[code] scale + bias[o], the weight of
+ * output o and input k being element o in_features + k of the tensor.
+ *   weights       numel = out_features in_features; its flat_offset is not looked at
+ *   in_features   a multiple of 64 (a block's scale belongs to one output), at most 65536
+ *   dtype         JB_F32 or JB_BF16, of x, bias and y alike; sums are fp32. Levels enter bf16
+ *                 products with 11 bits and fp32 products with 24, and so does x (bf16: all its bits)
+ *   d_x           [n][in_features], 16-byte aligned, rows x_row_stride elements apart (a multiple
+ *                 of 16 bytes)
+ *   d_bias        [out_features], or NULL
+ *   d_y           [n][out_features], rows y_row_stride elements apart; shares no byte with what is
+ *                 read: JB_ERR_INVALID_ARG
+ * Made for few rows: the weights are read once for each 64 of them at most.
+ */
+int jb_q4_matmul(const jb_q4_segment* weights, int out_features, int in_features, int dtype, const void* d_x, uint64_t x_row_stride,
+                 int n, const void* d_bias, void* d_y, uint64_t y_row_stride, struct CUstream_st* stream);
+
+/* ---------------------------------------------------------------------------
  * Test hooks (not on the hot path). Device buffers are caller-owned.
  * ------------------------------------------------------------------------- */
 

@@ -22,6 +22,9 @@ and, for scores that are not losses, what writing an answer with the perturbed m
 * ``jb_cache_write``  new keys and values to their places in the pages
 * ``jb_attend``  attention of new tokens over the pages
 * ``jb_sample``  the next token from its logits and a given random word
+* ``jb_cache_append``, ``jb_attend_tree``, ``jb_cache_keep``  trees of drafted tokens (``DraftTrees``): written with
+  their positions' rotation (``Rotation``), attended to at once, and one path of them kept
+* ``jb_q4_matmul``  products with the 4-bit weights that ``jb_perturb_q4`` perturbs
 
 Their tensors are on one device, the current one. No gradients flow through any call here: results
 of tensors that require them carry none.
@@ -87,6 +90,15 @@ class jb_sampling(ctypes.Structure):
                 ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p)]
 
 
+class jb_trees(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_void_p), ("starts", ctypes.c_void_p), ("parents", ctypes.c_void_p),
+                ("n", ctypes.c_int32), ("n_nodes", ctypes.c_int32)]
+
+
+class jb_rotation(ctypes.Structure):
+    _fields_ = [("steps", ctypes.c_void_p), ("dims", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
 class jb_seed(ctypes.Structure):
     _fields_ = [("machine_id", ctypes.c_uint64), ("step", ctypes.c_uint32),
                 ("sample_id", ctypes.c_uint32)]
@@ -138,6 +150,15 @@ def lib() -> ctypes.CDLL:
             L.jb_cache_workspace.restype = u64
             L.jb_attend_workspace.argtypes = [vp, i32]
             L.jb_attend_workspace.restype = u64
+            L.jb_cache_append.argtypes = [vp, vp, vp, vp, u64, u64, i32, vp, u64, u64, vp, u64, u64, vp, u64, u64, vp, vp,
+                                          vp, i32, vp]
+            L.jb_attend_tree.argtypes = [vp, vp, vp, vp, vp, u64, u64, i32, vp, u64, u64, vp, u64, vp]
+            L.jb_cache_keep.argtypes = [vp, vp, i32, vp, vp, vp, vp, u64, vp]
+            L.jb_q4_matmul.argtypes = [vp, i32, i32, i32, vp, u64, i32, vp, vp, u64, vp]
+            L.jb_attend_tree_workspace.argtypes = [vp]
+            L.jb_attend_tree_workspace.restype = u64
+            L.jb_cache_keep_workspace.argtypes = [vp]
+            L.jb_cache_keep_workspace.restype = u64
             L.jb_debug_philox.argtypes = [jb_seed, u64, u64, vp, vp]
             L.jb_debug_philox_fold.argtypes = [jb_seed, u64, u64, vp, vp]
             L.jb_debug_gaussian.argtypes = [jb_seed, u64, u64, vp, vp]
@@ -146,7 +167,8 @@ def lib() -> ctypes.CDLL:
                       "jb_apply_updates_with_grid", "jb_apply_updates_from", "jb_replay_updates",
                       "jb_checksum", "jb_checksum_with_grid", "jb_perturb_q4", "jb_q4_levels",
                       "jb_cache_reserve", "jb_cache_free", "jb_cache_fork", "jb_cache_compact",
-                      "jb_cache_write", "jb_attend", "jb_sample",
+                      "jb_cache_write", "jb_attend", "jb_sample", "jb_cache_append",
+                      "jb_attend_tree", "jb_cache_keep", "jb_q4_matmul",
                       "jb_quantize_grad", "jb_dequantize_grad",
                       "jb_max_seeds_per_call", "jb_debug_philox", "jb_debug_philox_fold",
                       "jb_debug_gaussian",
@@ -519,9 +541,21 @@ class KVCache:
         return self._workspaces.get("attend", nbytes, stream, handle, lambda size: self._zeroed(size, stream))
 
     def _pages_workspace(self, n: int, stream, handle):
-        nbytes = self.pages.workspace(n)
-        return self._workspaces.get("pages", nbytes, stream, handle,
+        return self._plain_workspace("pages", self.pages.workspace(n), stream, handle)
+
+    def _plain_workspace(self, key, nbytes: int, stream, handle):
+        return self._workspaces.get(key, nbytes, stream, handle,
                                     lambda size: _new(stream, torch.empty, size, dtype=torch.uint8, device=self.keys[0].device))
+
+    def new_tree_workspace(self, stream=None):
+        """A workspace for jb_attend_tree, whatever the trees: a uint8 tensor."""
+        return _new(stream, torch.empty, self._tree_workspace_bytes(), dtype=torch.uint8, device=self.keys[0].device)
+
+    def _tree_workspace_bytes(self) -> int:
+        nbytes = self._attend_bytes.get("tree")
+        if nbytes is None:
+            nbytes = self._attend_bytes["tree"] = max(16, int(lib().jb_attend_tree_workspace(self.layer_refs[0])))
+        return nbytes
 
 
 def _new(stream, make, *args, **kwargs):
@@ -634,6 +668,178 @@ def jb_attend(cache: KVCache, layer: int, q, rows, pos, out=None, scale: Optiona
     return out
 
 
+class DraftTrees:
+    """Trees of drafted tokens (jb_trees), int32 CUDA tensors: nodes starts[i] .. starts[i + 1] - 1 of a list are the last
+    tokens of row rows[i], and parents[j] is the node of the same tree that node j follows, counted from the tree's
+    first, or -1. At most 256 nodes a tree. Holds references to the tensors."""
+
+    def __init__(self, rows, starts, parents):
+        if torch is None:
+            _need_torch()
+        device = rows.get_device()
+        if device < 0:
+            raise ValueError("rows must be a CUDA tensor")
+        pr, n = _list32(rows, "rows", device)
+        ps, m = _list32(starts, "starts", device)
+        pp, n_nodes = _list32(parents, "parents", device)
+        if m != n + 1:
+            raise ValueError("starts must have one entry more than rows")
+        self.rows, self.starts, self.parents, self.n, self.n_nodes, self.device = rows, starts, parents, n, n_nodes, device
+        self.struct = jb_trees(pr, ps, pp, n, n_nodes)
+        self.ref = ctypes.byref(self.struct)
+
+
+class Rotation:
+    """How jb_cache_append turns queries and keys (jb_rotation): pair j of the first 2 len(steps) elements of a head by
+    steps[j] 2^-64 of a full turn per position, steps an int64 CUDA tensor of 64-bit words. Pairs are (j, j + len(steps)),
+    or neighbours if `interleaved`. ``Rotation.powers`` and ``Rotation.of`` make the steps. Holds a reference to them."""
+
+    def __init__(self, steps, interleaved: bool = False):
+        if torch is None:
+            _need_torch()
+        if steps.dtype is not torch.int64 or steps.get_device() < 0 or steps.dim() != 1 or not steps.is_contiguous():
+            raise ValueError("steps must be a contiguous one-dimensional int64 CUDA tensor")
+        self.steps, self.interleaved, self.dims, self.device = steps, bool(interleaved), 2 * steps.numel(), steps.get_device()
+        self.struct = jb_rotation(steps.data_ptr(), self.dims, int(self.interleaved))
+        self.ref = ctypes.byref(self.struct)
+
+    @staticmethod
+    def steps_of(frequencies) -> np.ndarray:
+        """Steps of frequencies in radians per position, as int64."""
+        turns = np.asarray(frequencies, dtype=np.float64) / (2 * np.pi)
+        if not np.isfinite(turns).all():
+            raise ValueError("frequencies must be finite")
+        return np.mod(turns * 2.0**64, 2.0**64).astype(np.uint64).view(np.int64)
+
+    @classmethod
+    def of(cls, frequencies, interleaved: bool = False, device="cuda") -> "Rotation":
+        """The rotation with these frequencies, in radians per position, one for each pair."""
+        _need_torch()
+        return cls(torch.from_numpy(cls.steps_of(frequencies)).to(device), interleaved)
+
+    @classmethod
+    def powers(cls, dims: int, base: float = 10000.0, interleaved: bool = False, device="cuda") -> "Rotation":
+        """Frequencies base^(-2 j / dims)."""
+        if dims < 2 or dims % 2:
+            raise ValueError("dims must be even")
+        return cls.of(np.float64(base) ** (-np.arange(0, dims, 2) / dims), interleaved, device)
+
+
+def jb_cache_append(cache: KVCache, layer: int, q, k, v, rows, pos, rotation: Rotation, turns=None, q_out=None, stream=None):
+    """jb_cache_write with the rotation on the way: keys k[i] of a layer, turned by position turns[i] (default pos[i]), and
+    values v[i] to position pos[i] of row rows[i]. Queries q [n, q_heads, head_dim] are turned alike; returns ``q_out``,
+    which may be q itself. q None: no queries, and None is returned."""
+    device = cache.device
+    pr, pp, n = _two_lists(rows, pos, "rows and positions", device)
+    if rotation.device != device:
+        raise ValueError("the rotation's steps must be on the cache's CUDA device")
+    pt = None
+    if turns is not None:
+        pt, m = _list32(turns, "turns", device)
+        if m != n:
+            raise ValueError("one turn per token")
+    ka, kb = _heads_of(k, cache.heads, cache, n, "new keys")
+    va, vb = _heads_of(v, cache.heads, cache, n, "new values")
+    heads = qa = qb = oa = ob = 0
+    pq = po = None
+    if q is None:
+        if q_out is not None:
+            raise ValueError("q_out without queries")
+    else:
+        heads = q.shape[1] if q.dim() == 3 else 0
+        qa, qb = _heads_of(q, heads, cache, n, "queries")
+        if q_out is None:
+            q_out = _new(stream, torch.empty, (n, heads, cache.head_dim), dtype=q.dtype, device=q.device)
+        oa, ob = _heads_of(q_out, heads, cache, n, "turned queries")
+        pq, po = q.data_ptr(), q_out.data_ptr()
+    _check(lib().jb_cache_append(cache.pages.ref, cache.layer_refs[layer], rotation.ref, pq, qa, qb, heads, po, oa, ob,
+                                 k.data_ptr(), ka, kb, v.data_ptr(), va, vb, pr, pp, pt, n, _stream_on(device, stream)))
+    return q_out
+
+
+def _trees_on(trees: DraftTrees, cache: KVCache) -> None:
+    if trees.device != cache.device:
+        raise ValueError("the trees must be on the cache's CUDA device")
+
+
+def jb_attend_tree(cache: KVCache, layer: int, q, trees: DraftTrees, out=None, scale: Optional[float] = None,
+                   softcap: float = 0.0, window: int = 0, slopes=None, workspace=None, stream=None):
+    """Attention of the nodes of trees: query q[j] ([n_nodes, q_heads, head_dim]) of node j sees its row's tokens before
+    the tree, its ancestors and itself; returns ``out``. Scores as in jb_attend, positions by depth. Outputs of nodes of
+    no tree are left as they are. ``workspace``: by default one that the cache keeps for the stream;
+    ``cache.new_tree_workspace`` makes others."""
+    _trees_on(trees, cache)
+    n = trees.n_nodes
+    heads = q.shape[1] if q.dim() == 3 else 0
+    qa, qb = _heads_of(q, heads, cache, n, "queries")
+    if out is None:
+        out = _new(stream, torch.empty, (n, heads, cache.head_dim), dtype=q.dtype, device=q.device)
+    oa, ob = _heads_of(out, heads, cache, n, "outputs")
+    if slopes is not None and (slopes.dtype is not torch.float32 or slopes.get_device() != cache.device
+                               or slopes.shape != (heads,) or not slopes.is_contiguous()):
+        raise ValueError("slopes must be a contiguous float32 tensor on the cache's CUDA device, one per query head")
+    handle = _stream_on(cache.device, stream)
+    if workspace is None:
+        ws, nbytes, held = cache._plain_workspace("tree", cache._tree_workspace_bytes(), stream, handle)
+    else:
+        if workspace.get_device() != cache.device or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on the cache's CUDA device")
+        ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    scores = jb_scores(cache.head_dim ** -0.5 if scale is None else scale, softcap, window,
+                       None if slopes is None else slopes.data_ptr())
+    _check(lib().jb_attend_tree(cache.pages.ref, cache.layer_refs[layer], ctypes.byref(scores), trees.ref, q.data_ptr(), qa, qb,
+                                heads, out.data_ptr(), oa, ob, ws, nbytes, handle))
+    return out
+
+
+def jb_cache_keep(cache: KVCache, trees: DraftTrees, leaves, status=None, stream=None):
+    """Of each tree the path from its root to node leaves[i] stays (-1: nothing does): its tokens move, in every layer,
+    behind the row's tokens before the tree, the row ends with them, and the pages behind are free. Returns the status
+    tensor: 0, or -1 where something is not valid and nothing is changed."""
+    pages = cache.pages
+    _trees_on(trees, cache)
+    pl, n = _list32(leaves, "leaves", cache.device)
+    if n != trees.n:
+        raise ValueError("one leaf per tree")
+    status = _status_of(status, pages, stream)
+    handle = _stream_on(cache.device, stream)
+    nbytes = max(16, int(lib().jb_cache_keep_workspace(trees.ref)))
+    ws, nbytes, held = cache._plain_workspace("keep", nbytes, stream, handle)
+    _check(lib().jb_cache_keep(pages.ref, cache.layers, cache.n_layers, trees.ref, pl, status.data_ptr(), ws, nbytes, handle))
+    return status
+
+
+def jb_q4_matmul(table: "Q4Table", index: int, x, out_features: int, bias=None, out=None, stream=None):
+    """Products of x [n, in_features] with tensor `index` of the table, a matrix [out_features, in_features] of 4-bit weights,
+    plus bias; returns ``out`` [n, out_features]. float32 or bfloat16; in_features a multiple of 64."""
+    if torch is None:
+        _need_torch()
+    device = x.get_device()
+    if x.dim() != 2 or device < 0:
+        raise ValueError("x must be a CUDA tensor [n, in_features]")
+    n, inner = x.shape
+    dtype = _storage(x.dtype)
+    codes, scale, _ = table.tensors[index]
+    if codes.get_device() != device or scale.get_device() != device:
+        raise ValueError("the weights must be on x's CUDA device")
+    if codes.dtype is not torch.uint8 or scale.dtype is not torch.float32 or not codes.is_contiguous() or not scale.is_contiguous():
+        raise ValueError("the weights must be contiguous uint8 codes and float32 scales")
+    if x.stride(1) != 1 and inner > 1:
+        raise ValueError("x must be contiguous in a row")
+    if bias is not None and (bias.dtype is not x.dtype or bias.get_device() != device or bias.shape != (out_features,)
+                             or (out_features > 1 and bias.stride(0) != 1)):
+        raise ValueError("bias must be a contiguous tensor of x's type on its CUDA device, one entry per output")
+    if out is None:
+        out = _new(stream, torch.empty, (n, out_features), dtype=x.dtype, device=x.device)
+    elif out.dtype is not x.dtype or out.get_device() != device or out.shape != (n, out_features) \
+            or (out.stride(1) != 1 and out_features > 1):
+        raise ValueError("out must be [n, out_features] of x's type on its CUDA device, contiguous in a row")
+    segment = ctypes.byref(table.segments, index % table.n_segments * ctypes.sizeof(jb_q4_segment))
+    _check(lib().jb_q4_matmul(segment, out_features, inner, dtype, x.data_ptr(), x.stride(0), n,
+                              None if bias is None else bias.data_ptr(), out.data_ptr(), out.stride(0), _stream_on(device, stream)))
+    return out
+
+
 def _per_row(value, default, words, dtype, stream, device):
     """A setting of jb_sample as the address of its entries (None where it is the default) and the tensor
     that holds them, one for each of the words."""
@@ -730,7 +936,8 @@ __all__ = [
     "jb_apply_updates_from", "jb_replay_updates", "jb_checksum", "jb_perturb_q4", "jb_q4_levels",
     "Q4Table", "jb_q4_segment", "PageTable", "KVCache", "jb_pages", "jb_kv", "jb_scores", "jb_sampling",
     "jb_cache_reserve", "jb_cache_free", "jb_cache_fork", "jb_cache_compact", "jb_cache_write",
-    "jb_attend", "jb_sample",
+    "jb_attend", "jb_sample", "jb_trees", "jb_rotation", "DraftTrees", "Rotation", "jb_cache_append", "jb_attend_tree",
+    "jb_cache_keep", "jb_q4_matmul",
     "jb_quantize_grad", "jb_dequantize_grad", "jb_max_seeds_per_call", "jb_status_string",
     "jb_debug_philox", "jb_debug_gaussian", "jb_debug_box_muller",
 ]

@@ -25,6 +25,7 @@
 
 #include "jb_answer.h"
 #include "jb_launch.cuh"
+#include "jb_scores.cuh"
 
 namespace jb {
 namespace {
@@ -36,14 +37,6 @@ constexpr int kThreads = 32 * kWarps;
 constexpr int kMaxWorkers = 2048;  // warps of the persistent grid; the workspace has two slots for each
 constexpr int kLevels = 4;         // of joining 8 or 16 parts of a pair at a time: 8^4 >= kMaxWorkers
 constexpr int kLeast = 4;          // groups of a stretch, where that leaves one to each CTA
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLowest = -3.0e38f;
-
-__device__ __forceinline__ float exp2_approx(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 
 struct Params {
     Pages pages;
@@ -497,26 +490,6 @@ struct Feed {
         return !(missing >> stage & 1u);
     }
 };
-
-// The score as the softmax takes it, in units of ln 2, as is the slope.
-template <bool kExtra>
-__device__ __forceinline__ float score(const Params& p, float dot, float slope, int back) {
-    if constexpr (!kExtra) {
-        return dot * (p.a.scale * kLog2e);
-    } else {
-        float x = dot * (p.a.scale * kLog2e);
-        if (p.a.softcap > 0.0f) {
-            // tanh(y) = 1 - 2 / (1 + e^2y), to a few 2^-24; near 0 that is not enough of a small y, and
-            // tanh(y) / y = 1 - y^2/3 + 2 y^4/15 - 17 y^6/315 is good to 6e-8 below 1/5
-            const float y = dot * p.cap_in, y2 = y * y;
-            const float e = exp2_approx(y * (2.0f * kLog2e));
-            const float large = fmaf(-2.0f * p.cap_out, __fdividef(1.0f, 1.0f + e), p.cap_out);
-            const float small = x * fmaf(y2, fmaf(y2, fmaf(y2, -17.0f / 315.0f, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
-            x = fabsf(y) < 0.2f ? small : large;
-        }
-        return fmaf(slope, static_cast<float>(back), x);
-    }
-}
 
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"

@@ -1,0 +1,36 @@
+// jb_scores.cuh -- what attention does to a score, for the kernels of jb_attend.cu and jb_tree.cu.
+#pragma once
+#include <cuda_runtime.h>
+
+namespace jb {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLowest = -3.0e38f;
+
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// The score as the softmax takes it, in units of ln 2, as is the slope. p.cap_in is scale / cap, p.cap_out cap / ln 2.
+template <bool kExtra, typename P>
+__device__ __forceinline__ float score(const P& p, float dot, float slope, int back) {
+    if constexpr (!kExtra) {
+        return dot * (p.a.scale * kLog2e);
+    } else {
+        float x = dot * (p.a.scale * kLog2e);
+        if (p.a.softcap > 0.0f) {
+            // tanh(y) = 1 - 2 / (1 + e^2y), to a few 2^-24; near 0 that is not enough of a small y, and
+            // tanh(y) / y = 1 - y^2/3 + 2 y^4/15 - 17 y^6/315 is good to 6e-8 below 1/5
+            const float y = dot * p.cap_in, y2 = y * y;
+            const float e = exp2_approx(y * (2.0f * kLog2e));
+            const float large = fmaf(-2.0f * p.cap_out, __fdividef(1.0f, 1.0f + e), p.cap_out);
+            const float small = x * fmaf(y2, fmaf(y2, fmaf(y2, -17.0f / 315.0f, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
+            x = fabsf(y) < 0.2f ? small : large;
+        }
+        return fmaf(slope, static_cast<float>(back), x);
+    }
+}
+
+}  // namespace jb

@@ -1,0 +1,328 @@
+// jb_tree.cuh -- what the kernels of jb_tree.cu share: which queries and positions a tree has, who sees whom, how the
+// work is dealt out, and how parts of one row's attention are joined.
+//
+// The rows of a block are (node, query head of the key head) pairs, nodes first: row r is node r / group. Tiles of
+// positions of all (tree, key head, block of rows) are one line, and every CTA of a persistent grid takes an equal
+// stretch of it, whatever the rows' lengths. Blocks that a boundary cuts leave (weighted values, maximum, sum) in the
+// workspace, which join_kernel adds up in the order of the line: results do not depend on which CTA was first.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include "jb_draft.h"
+#include "jb_launch.cuh"
+#include "jb_scores.cuh"
+
+namespace jb {
+namespace {
+
+constexpr int kGroup = 16;          // pages hold a multiple of so many tokens
+constexpr int kMaskWords = kMaxNodes / 32;
+constexpr int kMaxCtas = 640;       // of the persistent grids; the workspace has two slots for each
+
+struct TreeParams {
+    Pages pages;
+    Trees trees;
+    TreeAttend a;
+    int page_groups;        // groups in a page
+    float cap_in, cap_out;  // softcap: scale / cap, cap / ln 2
+};
+
+// Tree i: its queries, its row's positions that some node sees, [lo, len), the nodes' among them [base, len), and their
+// tiles. tiles == 0: a tree without nodes or one that is not valid, whose queries get zeros.
+struct Span {
+    int row, first, nodes, base, len, lo, first_tile, tiles, blocks;
+};
+
+template <int kRows, int kTile>
+__device__ __forceinline__ Span span_of(const TreeParams& p, int i) {
+    Span s;
+    s.row = p.trees.rows[i];
+    const long long from = p.trees.starts[i], to = p.trees.starts[i + 1];
+    const bool listed = from >= 0 && from < to && to <= p.trees.n_nodes;
+    s.first = listed ? static_cast<int>(from) : 0;
+    s.nodes = listed ? static_cast<int>(to - from) : 0;
+    s.base = s.len = s.lo = s.first_tile = s.tiles = s.blocks = 0;
+    if (!listed || s.nodes > kMaxNodes || s.row < 0 || s.row >= p.pages.n_rows) return s;
+    const int len = p.pages.lens[s.row];
+    if (len < s.nodes || len > p.pages.row_pages * p.pages.page_tokens) return s;
+    s.len = len;
+    s.base = len - s.nodes;
+    if (p.a.window > 0) s.lo = max(0, s.base - p.a.window + 1);  // what a root sees
+    s.first_tile = s.lo / kTile;
+    s.tiles = (s.len - 1) / kTile + 1 - s.first_tile;
+    s.blocks = (s.nodes * p.a.group + kRows - 1) / kRows;  // group is at most 65536
+    return s;
+}
+
+// Tiles [from, to) of a block of rows of a tree's key head.
+struct Piece {
+    int tree, head, block, from, to;
+    long long begin;  // where the block's tiles start on the line
+    Span span;
+};
+
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+    return ((a | b) >> 32) == 0 ? static_cast<long long>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)) : a / b;
+}
+
+// The line, and which CTA has which of it: `each` tiles, and the first `extra` CTAs one more.
+struct Line {
+    long long total, each;
+    int workers, extra;
+
+    __device__ long long bound(int w) const { return each * w + min(w, extra); }
+    __device__ int owner(long long x) const {
+        const long long longer = (each + 1) * extra;
+        return x < longer ? static_cast<int>(quotient(x, each + 1)) : extra + static_cast<int>(quotient(x - longer, each));
+    }
+};
+
+// Sum of v over the threads before this one, and over all. sums: kThreads / 32 words.
+template <int kThreads>
+__device__ __forceinline__ long long before_thread(long long v, long long* sums, long long& total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    long long in = v;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const long long o = __shfl_up_sync(0xFFFFFFFFu, in, d);
+        if (lane >= d) in += o;
+    }
+    if (lane == 31) sums[warp] = in;
+    __syncthreads();
+    long long base = 0;
+    total = 0;
+    for (int w = 0; w < kThreads / 32; ++w) {
+        if (w < warp) base += sums[w];
+        total += sums[w];
+    }
+    __syncthreads();
+    return base + in - v;
+}
+
+// Deals a CTA's stretch of the line out in pieces.
+template <int kRows, int kTile, int kThreads>
+struct Dealer {
+    long long next, end, at;  // at: tiles of the tree before `next`
+    Line line;
+    int tree;
+    Span span;
+
+    // The CTA together; kThreads of them. False: the CTA has nothing to do. found: two words of shared memory.
+    __device__ bool start(const TreeParams& p, int worker, int ctas, long long* sums, long long* found) {
+        long long total = 0;
+        for (int first = 0; first < p.trees.n; first += kThreads) {
+            long long here;
+            before_thread<kThreads>(tiles_of(p, first + static_cast<int>(threadIdx.x)), sums, here);
+            total += here;
+        }
+        line.total = total;
+        line.workers = static_cast<int>(min(static_cast<long long>(ctas), max(1ll, total)));
+        line.each = quotient(total, line.workers);
+        line.extra = static_cast<int>(total - line.each * line.workers);
+        next = end = 0;
+        if (worker >= line.workers || total == 0) return false;
+        next = line.bound(worker);
+        end = line.bound(worker + 1);
+        seek(p, next, sums, found);
+        return true;
+    }
+    static __device__ long long tiles_of(const TreeParams& p, int i) {
+        if (i >= p.trees.n) return 0;
+        const Span s = span_of<kRows, kTile>(p, i);
+        return static_cast<long long>(s.tiles) * s.blocks * p.a.heads;
+    }
+    // The tree with tile x of the line. The CTA together.
+    __device__ void seek(const TreeParams& p, long long x, long long* sums, long long* found) {
+        long long base = 0;
+        for (int first = 0; first < p.trees.n; first += kThreads) {
+            const int i = first + static_cast<int>(threadIdx.x);
+            const long long mine = tiles_of(p, i);
+            long long here;
+            const long long before = base + before_thread<kThreads>(mine, sums, here);
+            if (before <= x && x < before + mine) {
+                found[0] = i;
+                found[1] = before;
+            }
+            base += here;
+            if (x < base) break;  // the same for all threads
+        }
+        __syncthreads();
+        tree = static_cast<int>(found[0]);
+        at = x - found[1];
+        span = span_of<kRows, kTile>(p, tree);
+        __syncthreads();
+    }
+    __device__ bool take(const TreeParams& p, Piece& s) {
+        if (next >= end) return false;
+        while (at >= static_cast<long long>(span.tiles) * span.blocks * p.a.heads) {
+            at -= static_cast<long long>(span.tiles) * span.blocks * p.a.heads;
+            ++tree;
+            span = span_of<kRows, kTile>(p, tree);
+        }
+        s.tree = tree;
+        s.span = span;
+        const int pair = static_cast<int>(quotient(at, span.tiles));
+        s.head = pair / span.blocks;
+        s.block = pair - s.head * span.blocks;
+        s.from = static_cast<int>(at - static_cast<long long>(pair) * span.tiles);
+        s.to = static_cast<int>(min(static_cast<long long>(span.tiles), s.from + (end - next)));
+        s.begin = next - s.from;
+        next += s.to - s.from;
+        at += s.to - s.from;
+        return true;
+    }
+};
+
+// Who sees whom in a tree: depth of each node (-1: its chain of parents is not valid, and it sees nothing), and of its
+// ancestors and itself those within the window, as bits.
+struct Nodes {
+    unsigned mask[kMaxNodes][kMaskWords];
+    int depth[kMaxNodes];
+    short jump[kMaxNodes];
+};
+
+// kThreads threads together, `rank` among them; any(x): a barrier of them, true if x is in one of them. The chains are
+// walked by doubling: after round r a node has the ancestors up to 2^r steps away.
+template <int kThreads, typename Any>
+__device__ __forceinline__ void fill_nodes(const TreeParams& p, const Span& s, Nodes& t, int rank, Any any) {
+    constexpr int kBad = 1 << 20, kEach = (kMaxNodes + kThreads - 1) / kThreads;
+    bool more = false;
+    any(false);  // nobody reads the last tree's any more
+    for (int j = rank; j < s.nodes; j += kThreads) {
+        const int up = p.trees.parents[s.first + j];
+        const bool inner = up >= 0 && up < j;
+        t.jump[j] = static_cast<short>(inner ? up : -1);
+        t.depth[j] = inner ? 1 : up == -1 ? 0 : kBad;
+        for (int w = 0; w < kMaskWords; ++w) t.mask[j][w] = w == j >> 5 ? 1u << (j & 31) : 0;
+        more = more || inner;
+    }
+    while (any(more)) {  // at most 8 rounds: a chain has at most 255 steps
+        unsigned mask[kEach][kMaskWords];
+        int depth[kEach], jump[kEach];
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int j = rank + e * kThreads, up = j < s.nodes ? t.jump[j] : -1;
+            jump[e] = up;
+            if (up < 0) continue;
+            depth[e] = min(t.depth[j] + t.depth[up], kBad);
+            jump[e] = t.jump[up];
+            for (int w = 0; w < kMaskWords; ++w) mask[e][w] = t.mask[j][w] | t.mask[up][w];
+        }
+        any(false);
+        more = false;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int j = rank + e * kThreads;
+            if (j >= s.nodes || t.jump[j] < 0) continue;
+            t.depth[j] = depth[e];
+            t.jump[j] = static_cast<short>(jump[e]);
+            for (int w = 0; w < kMaskWords; ++w) t.mask[j][w] = mask[e][w];
+            more = more || jump[e] >= 0;
+        }
+    }
+    for (int j = rank; j < s.nodes; j += kThreads) {
+        const bool valid = t.depth[j] < kBad;
+        const int from = valid && p.a.window > 0 ? t.depth[j] - p.a.window : -1;  // ancestors up to this depth are not seen
+        if (valid && from < 0) continue;
+        for (int w = 0; w < kMaskWords; ++w) {
+            unsigned keep = 0;
+            for (unsigned m = valid ? t.mask[j][w] : 0; m != 0; m &= m - 1)
+                if (t.depth[32 * w + __ffs(m) - 1] > from) keep |= m & -m;
+            t.mask[j][w] = keep;
+        }
+    }
+    any(false);
+    for (int j = rank; j < s.nodes; j += kThreads)
+        if (t.depth[j] >= kBad) t.depth[j] = -1;
+    any(false);
+}
+
+// Bits of the 32 positions from t on that lie in [lo, hi).
+__device__ __forceinline__ unsigned between(int t, int lo, int hi) {
+    const int a = max(lo - t, 0), b = min(hi - t, 32);
+    if (a >= b) return 0;
+    return (b == 32 ? 0xFFFFFFFFu : (1u << b) - 1u) & ~((1u << a) - 1u);
+}
+
+// Which of the 32 positions from t on a node of this depth and mask sees.
+__device__ __forceinline__ unsigned seen_of(const TreeParams& p, const Span& s, int depth, const unsigned* mask, int t) {
+    if (depth < 0) return 0;
+    const int lo = p.a.window > 0 ? max(0, min(s.base, s.base + depth - p.a.window + 1)) : 0;
+    unsigned bits = between(t, lo, s.base);
+    const int off = t - s.base;
+    if (off <= -32 || off >= kMaxNodes) return bits;
+    if (off < 0) return bits | mask[0] << -off;
+    const int w = off >> 5;
+    return bits | __funnelshift_r(mask[w], w + 1 < kMaskWords ? mask[w + 1] : 0u, off & 31);
+}
+
+template <typename T>
+__device__ __forceinline__ void store_out(T* to, float v);
+template <>
+__device__ __forceinline__ void store_out<float>(float* to, float v) { *to = v; }
+template <>
+__device__ __forceinline__ void store_out<__nv_bfloat16>(__nv_bfloat16* to, float v) { *to = __float2bfloat16_rn(v); }
+
+// Zeros for the queries of trees that are not valid.
+template <typename T, int kRows, int kTile, int kThreads>
+__device__ __forceinline__ void write_zeros(const TreeParams& p) {
+    const int d = p.a.head_dim;
+    const long long values = static_cast<long long>(p.a.heads) * p.a.group * d;
+    for (int i = blockIdx.x; i < p.trees.n; i += gridDim.x) {
+        const Span s = span_of<kRows, kTile>(p, i);
+        if (s.tiles > 0) continue;
+        for (int j = 0; j < s.nodes; ++j)
+            for (long long u = threadIdx.x; u < values; u += kThreads)
+                store_out(reinterpret_cast<T*>(p.a.out) + (s.first + j) * p.a.out_row + u / d * p.a.out_head + u % d, 0.0f);
+    }
+}
+
+// Partial results: o[rows][D], m[rows], l[rows]. The first part of a block is in its CTA's slot 1, the others in their
+// CTAs' slots 0, so that the end of one block and the start of the next do not meet.
+__host__ __device__ constexpr size_t slot_floats(int rows, int d) { return static_cast<size_t>(rows) * (d + 2); }
+template <int kRows, int D>
+__device__ __forceinline__ float* slot_of(const TreeParams& p, int worker, bool first) {
+    return p.a.ws + slot_floats(kRows, D) * (2 * static_cast<size_t>(worker) + (first ? 1 : 0));
+}
+
+// CTA (b - 1, slice) joins a slice of the rows of the block that boundary b is the first to cut.
+template <typename T, int D, int kRows, int kTile>
+__global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ TreeParams p, int ctas) {
+    constexpr int kThreads = 128, kQuads = D / 4, kAt = kThreads / kQuads;  // rows at a time
+    __shared__ long long sums[kThreads / 32], found[2];
+    after_previous();
+    let_next_start();
+    Dealer<kRows, kTile, kThreads> deal;
+    const int b = blockIdx.x + 1;
+    if (!deal.start(p, b, ctas, sums, found)) return;
+    const long long x = deal.next;
+    Piece s;
+    deal.take(p, s);
+    if (s.begin == x || s.begin < deal.line.bound(b - 1)) return;  // no cut, or an earlier boundary's
+    const int last = deal.line.owner(s.begin + s.span.tiles - 1), quad = threadIdx.x % kQuads;
+    const int row = blockIdx.y * kAt + threadIdx.x / kQuads, all = s.block * kRows + row;
+    if (threadIdx.x >= kAt * kQuads || row >= kRows || all >= s.span.nodes * p.a.group) return;
+    float m = kLowest, l = 0.0f;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int w = b - 1; w <= last; ++w) {
+        const float* slot = slot_of<kRows, D>(p, w, w == b - 1);
+        const float mw = __ldcg(slot + kRows * D + row), lw = __ldcg(slot + kRows * D + kRows + row);
+        const float4 ow = __ldcg(reinterpret_cast<const float4*>(slot + row * D) + quad);
+        const float top = fmaxf(m, mw), f = exp2_approx(m - top), g = exp2_approx(mw - top);
+        l = fmaf(g, lw, l * f);
+        o = make_float4(fmaf(g, ow.x, o.x * f), fmaf(g, ow.y, o.y * f), fmaf(g, ow.z, o.z * f), fmaf(g, ow.w, o.w * f));
+        m = top;
+    }
+    if (4 * quad >= p.a.head_dim) return;
+    const float inverse = l > 0.0f ? 1.0f / l : 0.0f;
+    const int node = all / p.a.group, h = all - node * p.a.group;
+    T* out = reinterpret_cast<T*>(p.a.out) + (s.span.first + node) * p.a.out_row + (s.head * p.a.group + h) * p.a.out_head + 4 * quad;
+    store_out(out, o.x * inverse);
+    store_out(out + 1, o.y * inverse);
+    store_out(out + 2, o.z * inverse);
+    store_out(out + 3, o.w * inverse);
+}
+
+}  // namespace
+}  // namespace jb

@@ -1,0 +1,185 @@
+"""jb_q4_matmul against the definition in 64 bits.
+
+Tolerance with A = sum_k |x_k w_k|: a term is a product of a level and an input. In bf16 a level enters with half a step of
+fp16, 2^-12, and inputs keep their 8 bits unless they are 2^-28 of the largest of their row and smaller (2^-40 of that one,
+covered below); in fp32 both enter with 2^-24 and their product drops less than 2^-23. The sum of K terms and the
+products with scales lose at most (K / 16 + 70) 2^-23 of A in any order of blocks and lanes (16 terms a step of a tensor
+core, whose sums may truncate: 2^-22 a step), and a result is rounded once: 2^-8 of it for bf16 with the tie.
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2306_10015_gb300 as jb
+from test_gpu_attend import DT
+
+pytestmark = pytest.mark.gpu
+
+
+def weights(out, inner, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    codes = torch.randint(0, 256, (out * inner // 2,), dtype=torch.uint8, device="cuda", generator=g)
+    scale = torch.rand(out * inner // 64, device="cuda", generator=g) + 0.1
+    return jb.Q4Table([(codes, scale, out * inner)])
+
+
+def dense(table, index, out, inner):
+    codes, scale, n = table.tensors[index]
+    c = torch.stack([codes & 15, codes >> 4], -1).view(-1)[:n].long()
+    w = torch.from_numpy(jb.jb_q4_levels().astype(np.float64)).cuda()[c] * scale.double().repeat_interleave(64)[:n]
+    return w.view(out, inner)
+
+
+def bound(x, w, bias, want):
+    a = x.double().abs() @ w.abs().T + (0 if bias is None else bias.double().abs())
+    rel = (x.shape[1] / 16 + 70) * 2.0**-22
+    if x.dtype == torch.bfloat16:
+        return a * (rel + 2.0**-12) + 2.0**-8 * want.abs() + 1e-38
+    return a * (rel + 3 * 2.0**-23) + 1e-38
+
+
+def check(dtype, n, out, inner, bias=True, x=None, table=None, **kw):
+    g = torch.Generator(device="cuda").manual_seed(n + out)
+    table = weights(out, inner) if table is None else table
+    x = torch.randn(n, inner, device="cuda", generator=g).to(DT[dtype]) if x is None else x
+    b = torch.randn(out, device="cuda", generator=g).to(DT[dtype]) if bias else None
+    got = jb.jb_q4_matmul(table, 0, x, out, bias=b, **kw)
+    w = dense(table, 0, out, inner)
+    want = x.double() @ w.T + (0 if b is None else b.double())
+    err, tol = (got.double() - want).abs(), bound(x, w, b, want)
+    assert got.shape == (n, out) and torch.isfinite(got).all()
+    assert (err <= tol).all(), f"worst error over tolerance {(err / tol).amax():.3g}"
+    return got
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 2, 3, 4, 5, 7, 8, 9, 16, 17, 31, 33, 64, 65, 130])
+@pytest.mark.parametrize("out,inner", [(100, 256), (33, 1088)])
+def test_numbers_of_rows(dtype, n, out, inner):
+    check(dtype, n, out, inner)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 6, 20])
+@pytest.mark.parametrize("out", [1, 7, 15, 16, 17, 31, 64, 300, 2501])
+@pytest.mark.parametrize("inner", [64, 128, 192, 448, 512, 576, 1024])
+def test_shapes(dtype, n, out, inner):
+    check(dtype, n, out, inner, bias=out % 2 == 0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 9, 40])
+@pytest.mark.parametrize("out,inner", [(40, 20480), (5, 65536), (17, 8256), (20000, 128)])
+def test_long_and_wide(dtype, n, out, inner):
+    check(dtype, n, out, inner)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_every_level(dtype):
+    """A weight at a time: y is x level scale, each code in each place of a block."""
+    table = weights(64, 64)
+    codes, scale, _ = table.tensors[0]
+    x = torch.zeros(1, 64, device="cuda", dtype=DT[dtype])
+    w = dense(table, 0, 64, 64)
+    for k in range(64):
+        x.zero_()
+        x[0, k] = 1.5
+        got = jb.jb_q4_matmul(table, 0, x, 64)[0].double()
+        want = 1.5 * w[:, k]
+        assert ((got - want).abs() <= want.abs() * (2.0**-8 + 2.0**-11 if dtype == "bf16" else 2.0**-21)).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_inputs_of_all_sizes(dtype):
+    """Inputs from 1e-38 to 1e37, rows of their own sizes, outliers beside small values, zeros."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn(9, 1024, device="cuda", generator=g)
+    x *= torch.tensor([1e-38, 1e-30, 1e-10, 1e-3, 1.0, 1e10, 1e30, 1e35, 0.0], device="cuda")[:, None]
+    x[:, ::97] *= 100.0
+    x[4, ::5] *= 1e-6
+    check(dtype, 9, 50, 1024, bias=False, x=x.to(DT[dtype]))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_not_finite_inputs(dtype):
+    """They make their own rows' results infinite or NaN, as the sums have it, and no others'."""
+    table = weights(40, 576)
+    x = torch.randn(5, 576, device="cuda").to(DT[dtype])
+    clean = jb.jb_q4_matmul(table, 0, x, 40)
+    x[1, 500], x[3, 70] = float("inf"), float("nan")
+    got = jb.jb_q4_matmul(table, 0, x, 40)
+    assert torch.equal(got[[0, 2, 4]], clean[[0, 2, 4]])
+    want = x.double() @ dense(table, 0, 40, 576).T
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isinf(got), torch.isinf(want))
+    assert (torch.sign(got[1]) == torch.sign(want[1]).to(got.dtype))[~torch.isnan(got[1])].all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_strides_outputs_and_later_tensors(dtype):
+    """Rows inside wider ones; a matrix that starts 8 bytes off a 16-byte boundary; the second of a table."""
+    g = torch.Generator(device="cuda").manual_seed(4)
+    out, inner = 70, 320
+    codes = torch.randint(0, 256, (out * inner // 2 + 8,), dtype=torch.uint8, device="cuda", generator=g)
+    scale = torch.rand(out * inner // 64 + 3, device="cuda", generator=g)
+    a = weights(10, 64)
+    table = jb.Q4Table([a.tensors[0], (codes[8:], scale[3:], out * inner)])
+    x = torch.randn(6, 400, device="cuda", generator=g).to(DT[dtype])[:, 40:360]
+    y = torch.full((6, out + 9), 4.0, dtype=DT[dtype], device="cuda")
+    got = jb.jb_q4_matmul(table, 1, x, out, out=y[:, 4:4 + out])
+    assert (y[:, :4] == 4).all() and (y[:, 4 + out:] == 4).all() and got.data_ptr() == y[:, 4:].data_ptr()
+    w = dense(table, 1, out, inner)
+    want = x.double() @ w.T
+    assert ((got.double() - want).abs() <= bound(x, w, None, want)).all()
+    assert torch.equal(jb.jb_q4_matmul(table, -1, x, out), got)
+    assert jb.jb_q4_matmul(table, 1, x[:0], out).shape == (0, out)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_repeatable_streams_and_graphs(dtype):
+    table = weights(3000, 2048)
+    x = torch.randn(12, 2048, device="cuda").to(DT[dtype])
+    want = check(dtype, 12, 3000, 2048, bias=False, x=x, table=table)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    a, b = jb.jb_q4_matmul(table, 0, x, 3000), jb.jb_q4_matmul(table, 0, x, 3000, stream=stream)
+    torch.cuda.synchronize()
+    assert torch.equal(a, want) and torch.equal(b, want)
+    out = torch.empty_like(want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        jb.jb_q4_matmul(table, 0, x, 3000, out=out)
+    for scale in (1.0, 3.0):
+        x.mul_(scale)
+        graph.replay()
+        assert torch.equal(out, jb.jb_q4_matmul(table, 0, x, 3000))
+
+
+def test_between_two_perturbations():
+    """The weights are read when the product runs: perturbed codes and scales enter, and theta + eps z - 2 eps z + eps z."""
+    table = weights(96, 640)
+    x = torch.randn(3, 640, device="cuda")
+    for eps in (1e-2, -2e-2, 1e-2):
+        jb.jb_perturb_q4(table, (5, 1, 0), eps)
+        got = jb.jb_q4_matmul(table, 0, x, 96)
+        w = dense(table, 0, 96, 640)
+        want = x.double() @ w.T
+        assert ((got.double() - want).abs() <= bound(x, w, None, want)).all()
+
+
+def test_large_matrices():
+    """More than 2^31 weights: offsets past 32 bits."""
+    out, inner = 33000, 65536
+    codes = torch.zeros(out * inner // 2, dtype=torch.uint8, device="cuda")
+    scale = torch.zeros(out * inner // 64, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    tail = 40 * inner
+    codes[-tail // 2:] = torch.randint(0, 256, (tail // 2,), dtype=torch.uint8, device="cuda", generator=g)
+    scale[-tail // 64:] = torch.rand(tail // 64, device="cuda", generator=g)
+    table = jb.Q4Table([(codes, scale, out * inner)])
+    for dtype in ("f32", "bf16"):
+        x = torch.randn(2, inner, device="cuda", generator=g).to(DT[dtype])
+        got = jb.jb_q4_matmul(table, 0, x, out)
+        w = dense(jb.Q4Table([(codes[-tail // 2:], scale[-tail // 64:], tail)]), 0, 40, inner)
+        want = x.double() @ w.T
+        assert (got[:, :-40] == 0).all()
+        assert ((got[:, -40:].double() - want).abs() <= bound(x, w, None, want)).all()
