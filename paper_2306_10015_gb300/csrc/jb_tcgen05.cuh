@@ -1,0 +1,124 @@
+// jb_tcgen05.cuh -- mbarriers, asynchronous copies and the fifth generation's tensor-core instructions as functions.
+#pragma once
+#include <cstdint>
+
+#include <cuda_runtime.h>
+
+namespace jb {
+
+__device__ __forceinline__ uint32_t shared_address(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+
+// --- mbarriers ---------------------------------------------------------------------------
+
+__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void barriers_initialized() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
+__device__ __forceinline__ void barrier_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0;
+}
+// Waits for the phase of this parity to end. A wait of over about two seconds gives up and sets *failed, and so does one
+// that finds it set: then all roles of the CTA leave their loops.
+constexpr long long kPatience = 4000000000ll;  // cycles
+__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, volatile int* failed) {
+    if (barrier_try(bar, parity)) return true;
+    const long long start = clock64();
+    for (;;) {
+        if (barrier_try(bar, parity)) return true;
+        if (*failed) return false;
+        if (clock64() - start > kPatience) {
+            *failed = 1;
+            return false;
+        }
+    }
+}
+
+// --- copies ------------------------------------------------------------------------------
+
+// 16 bytes from global to shared memory, asynchronously; zeros if not `real`.
+__device__ __forceinline__ void copy_async16(uint32_t to, const void* from, bool real) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(real ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void copies_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
+}
+// What this thread wrote to shared memory becomes visible to the tensor cores' reads.
+__device__ __forceinline__ void shared_to_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// --- tensor memory and products ------------------------------------------------------------
+
+__device__ __forceinline__ void tmem_alloc(uint32_t to, uint32_t columns) {  // a warp
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(to), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free(uint32_t at, uint32_t columns) {  // the same warp
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns) : "memory");
+}
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_loads() { __syncwarp(); asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_stores() { __syncwarp(); asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// An arrival at `bar` when all products that this thread has issued are done.
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// A tile in shared memory with rows of 128 bytes, 16-byte pieces of row r at (piece ^ r % 8), 1024-byte aligned. `leading`:
+// bytes from one 64-element panel to the next where the panels' direction is not the product's (unused otherwise).
+__device__ __forceinline__ uint64_t tile_descriptor(uint32_t at, uint32_t leading) {
+    constexpr uint64_t kVersion = 1ull << 46, kSwizzle128 = 2ull << 61, kEightRows = static_cast<uint64_t>(1024 >> 4) << 32;
+    return kSwizzle128 | kVersion | kEightRows | static_cast<uint64_t>((leading >> 4) & 0x3FFF) << 16 | ((at >> 4) & 0x3FFF);
+}
+
+// bf16 products with fp32 sums, M = 128: N columns; `across`: B's rows in memory are its product's summed index.
+__host__ __device__ constexpr uint32_t product_descriptor(int n, bool across) {
+    return 1u << 4 | 1u << 7 | 1u << 10 | (across ? 1u << 16 : 0u) | static_cast<uint32_t>(n >> 3) << 17 | (128u >> 4) << 24;
+}
+// D = A B (+ D): A and B in shared memory; 16 summed elements.
+__device__ __forceinline__ void tc_product(uint32_t d, uint64_t a, uint64_t b, uint32_t how, bool add) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(how),
+        "r"(static_cast<uint32_t>(add))
+        : "memory");
+}
+// The same with A in tensor memory, two elements a column.
+__device__ __forceinline__ void tc_product_from_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t how, bool add) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(how),
+        "r"(static_cast<uint32_t>(add))
+        : "memory");
+}
+
+// 32 columns of a warp's 32 lanes: lane l has its row's.
+// These are the whole warp's: lanes that took another way have to be back.
+__device__ __forceinline__ void tmem_load32(uint32_t at, uint32_t* x) {
+    __syncwarp();
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, "
+        "%20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7]), "=r"(x[8]), "=r"(x[9]), "=r"(x[10]),
+          "=r"(x[11]), "=r"(x[12]), "=r"(x[13]), "=r"(x[14]), "=r"(x[15]), "=r"(x[16]), "=r"(x[17]), "=r"(x[18]), "=r"(x[19]), "=r"(x[20]),
+          "=r"(x[21]), "=r"(x[22]), "=r"(x[23]), "=r"(x[24]), "=r"(x[25]), "=r"(x[26]), "=r"(x[27]), "=r"(x[28]), "=r"(x[29]), "=r"(x[30]), "=r"(x[31])
+        : "r"(at));
+}
+__device__ __forceinline__ void tmem_store32(uint32_t at, const uint32_t* x) {
+    __syncwarp();
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, "
+        "%20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(at),
+        "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]), "r"(x[8]), "r"(x[9]), "r"(x[10]), "r"(x[11]),
+        "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15]), "r"(x[16]), "r"(x[17]), "r"(x[18]), "r"(x[19]), "r"(x[20]), "r"(x[21]), "r"(x[22]),
+        "r"(x[23]), "r"(x[24]), "r"(x[25]), "r"(x[26]), "r"(x[27]), "r"(x[28]), "r"(x[29]), "r"(x[30]), "r"(x[31])
+        : "memory");
+}
+
+}  // namespace jb

@@ -15,11 +15,6 @@ constexpr int kRows = 16;   // rows of a block
 constexpr int kTile = 32;   // positions of a tile
 
 __device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
-__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
-    const uint2 v = *reinterpret_cast<const uint2*>(p);
-    return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xFFFF0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xFFFF0000u));
-}
-
 template <int D>
 struct Shared {
     float q[kRows][D];
@@ -200,17 +195,7 @@ cudaError_t launch_d(const TreeParams& p, cudaStream_t s) {
     cudaError_t e = resident<tree_kernel<T, D>>(kThreads, shared, ctas);
     if (e != cudaSuccess) return e;
     e = launch(tree_kernel<T, D>, ctas, kThreads, shared, 0, s, p);
-    if (e != cudaSuccess || ctas == 1) return e;
-    cudaLaunchConfig_t c = {};
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    c.gridDim = dim3(ctas - 1, slices);
-    c.blockDim = dim3(128);
-    c.stream = s;
-    c.attrs = &attr;
-    c.numAttrs = 1;
-    return cudaLaunchKernelEx(&c, join_kernel<T, D, kRows, kTile>, p, ctas);
+    return e != cudaSuccess || ctas == 1 ? e : launch_join<T, D, kRows, kTile>(p, ctas, slices, s);
 }
 
 template <typename T>
@@ -221,14 +206,14 @@ cudaError_t launch_t(const TreeParams& p, cudaStream_t s) {
 }  // namespace
 
 uint64_t tree_workspace(int bf16, int head_dim) {
-    (void)bf16;
+    if (bf16) return tree_workspace_bf16(head_dim);
     return sizeof(float) * 2ull * kMaxCtas * slot_floats(kRows, head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256);
 }
 
 cudaError_t launch_tree(const Pages& pages, const Trees& trees, const TreeAttend& a, cudaStream_t s) {
     const float cap = a.softcap > 0.0f ? a.softcap : 1.0f;
     const TreeParams p = {pages, trees, a, pages.page_tokens / kGroup, a.scale / cap, cap * kLog2e};
-    return a.bf16 ? launch_t<__nv_bfloat16>(p, s) : launch_t<float>(p, s);
+    return a.bf16 ? launch_tree_bf16(p, s) : launch_t<float>(p, s);
 }
 
 }  // namespace jb

@@ -19,6 +19,9 @@ namespace {
 constexpr int kGroup = 16;          // pages hold a multiple of so many tokens
 constexpr int kMaskWords = kMaxNodes / 32;
 constexpr int kMaxCtas = 640;       // of the persistent grids; the workspace has two slots for each
+constexpr int kMaxTcCtas = 160;     // of those with a CTA on an SM
+
+}  // namespace
 
 struct TreeParams {
     Pages pages;
@@ -27,6 +30,11 @@ struct TreeParams {
     int page_groups;        // groups in a page
     float cap_in, cap_out;  // softcap: scale / cap, cap / ln 2
 };
+
+uint64_t tree_workspace_bf16(int head_dim);
+cudaError_t launch_tree_bf16(const TreeParams& p, cudaStream_t s);
+
+namespace {
 
 // Tree i: its queries, its row's positions that some node sees, [lo, len), the nodes' among them [base, len), and their
 // tiles. tiles == 0: a tree without nodes or one that is not valid, whose queries get zeros.
@@ -322,6 +330,20 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ TreeP
     store_out(out + 1, o.y * inverse);
     store_out(out + 2, o.z * inverse);
     store_out(out + 3, o.w * inverse);
+}
+
+template <typename T, int D, int kRows, int kTile>
+cudaError_t launch_join(const TreeParams& p, int ctas, int slices, cudaStream_t s) {
+    cudaLaunchConfig_t c = {};
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    c.gridDim = dim3(ctas - 1, slices);
+    c.blockDim = dim3(128);
+    c.stream = s;
+    c.attrs = &attr;
+    c.numAttrs = 1;
+    return cudaLaunchKernelEx(&c, join_kernel<T, D, kRows, kTile>, p, ctas);
 }
 
 }  // namespace
