@@ -13,22 +13,26 @@ __device__ __forceinline__ float exp2_approx(float x) {
     return y;
 }
 
-// The score as the softmax takes it, in units of ln 2, as is the slope. p.cap_in is scale / cap, p.cap_out cap / ln 2.
+// scale q.k under the cap, in units of ln 2. p.cap_in is scale / cap, p.cap_out cap / ln 2.
+template <typename P>
+__device__ __forceinline__ float capped(const P& p, float dot) {
+    const float x = dot * (p.a.scale * kLog2e);
+    // tanh(y) = 1 - 2 / (1 + e^2y), to a few 2^-24; near 0 that is not enough of a small y, and
+    // tanh(y) / y = 1 - y^2/3 + 2 y^4/15 - 17 y^6/315 is good to 6e-8 below 1/5
+    const float y = dot * p.cap_in, y2 = y * y;
+    const float e = exp2_approx(y * (2.0f * kLog2e));
+    const float large = fmaf(-2.0f * p.cap_out, __fdividef(1.0f, 1.0f + e), p.cap_out);
+    const float small = x * fmaf(y2, fmaf(y2, fmaf(y2, -17.0f / 315.0f, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
+    return fabsf(y) < 0.2f ? small : large;
+}
+
+// The score as the softmax takes it, in units of ln 2, as is the slope.
 template <bool kExtra, typename P>
 __device__ __forceinline__ float score(const P& p, float dot, float slope, int back) {
     if constexpr (!kExtra) {
         return dot * (p.a.scale * kLog2e);
     } else {
-        float x = dot * (p.a.scale * kLog2e);
-        if (p.a.softcap > 0.0f) {
-            // tanh(y) = 1 - 2 / (1 + e^2y), to a few 2^-24; near 0 that is not enough of a small y, and
-            // tanh(y) / y = 1 - y^2/3 + 2 y^4/15 - 17 y^6/315 is good to 6e-8 below 1/5
-            const float y = dot * p.cap_in, y2 = y * y;
-            const float e = exp2_approx(y * (2.0f * kLog2e));
-            const float large = fmaf(-2.0f * p.cap_out, __fdividef(1.0f, 1.0f + e), p.cap_out);
-            const float small = x * fmaf(y2, fmaf(y2, fmaf(y2, -17.0f / 315.0f, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
-            x = fabsf(y) < 0.2f ? small : large;
-        }
+        const float x = p.a.softcap > 0.0f ? capped(p, dot) : dot * (p.a.scale * kLog2e);
         return fmaf(slope, static_cast<float>(back), x);
     }
 }

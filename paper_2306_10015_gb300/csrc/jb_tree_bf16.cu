@@ -6,11 +6,19 @@
 // with the maximum m of the softmax kept as it was until a row exceeds it by 2^8; only then is O multiplied. Weights enter
 // the second product as two bf16 numbers, 16 bits of them.
 //
-// Roles of a CTA, one on an SM: two warps copy keys and values (cp.async, whole rows, any page size and layout) into a
-// ring of swizzled tiles; one thread issues the products; four warps, a thread a row, take scores from tensor memory and put
-// weights in their place, so that of three score tiles one is being multiplied, one worked on and one its values' operand.
+// Roles of a CTA, one on an SM: a warp copies keys and values (TMA, boxes of a page's tokens, any page size and layout)
+// into swizzled tiles; two warps copy queries and look after values that some rows do not see; one thread issues the
+// products; eight warps take scores from tensor memory and put weights in their place, so that of three score tiles one is
+// being multiplied, one worked on and one its values' operand. A row has two threads, each with half of a tile's positions
+// and half of the sums; they exchange the maximum.
+//
+// Loops are kept short, not unrolled: a warp that runs alone through code that is longer than its instruction cache waits
+// for instructions (64 positions of a thread unrolled: 8000 cycles a tile). Nor is cp.async for keys and values: a warp
+// issued one in 170 cycles, 10000 for a tile's.
 #include <atomic>
+#include <numeric>
 
+#include <cuda.h>
 #include <cuda_bf16.h>
 
 #include "jb_tcgen05.cuh"
@@ -23,30 +31,41 @@ using T = __nv_bfloat16;
 
 constexpr unsigned kAll = 0xFFFFFFFFu;
 constexpr int kRows = 128;
-constexpr int kSoftmaxWarps = 4, kCopyWarps = 2;
-constexpr int kThreads = 256;        // a warp more than have a role: registers are dealt out to four warps at a time
+constexpr int kSoftmaxWarps = 8, kHelpWarps = 2;
+constexpr int kThreads = 32 * (kSoftmaxWarps + 2 + kHelpWarps);
+constexpr int kHelpThreads = 32 * kHelpWarps;
 constexpr int kScoreTiles = 3;
 constexpr uint32_t kColumns = 512;   // of tensor memory
 constexpr float kSlack = 8.0f;       // how far a row may exceed its maximum before sums are scaled, in powers of two
 
+// What a score goes through on its way to the softmax.
+enum Scores { kPlain, kCapped, kBiased };  // a positive scale alone; a cap; a bias, with or without a cap, or any scale
+
 template <int D>
 struct Shape {
     static constexpr int kTile = D == 256 ? 64 : 128;
-    static constexpr int kSlots = D == 64 ? 8 : D == 128 ? 5 : 4;
-    static constexpr int kDepth = kSlots - 2;  // tiles that are copied before the first of them is waited for
+    static constexpr int kSlots = D == 64 ? 8 : 4;
+    static constexpr int kQueries = D == 256 ? 1 : 2;  // blocks of queries that there is room for
     static constexpr uint32_t kTileBytes = kTile * D * 2, kQueryBytes = kRows * D * 2;
     static constexpr uint32_t kPanel = kTile * 128, kQueryPanel = kRows * 128;  // 64 elements of all rows
     static constexpr uint32_t kSums = kScoreTiles * kTile;                      // column of O
-    static constexpr int kShared = 1024 + kQueryBytes + kSlots * kTileBytes;
-    static_assert(kSums + D <= kColumns);
+    static constexpr int kShared = 1024 + kQueries * kQueryBytes + kSlots * kTileBytes;
+    static_assert(kSums + D <= kColumns && kSlots % 2 == 0);  // even: values are always in odd slots
+};
+
+struct TcParams {
+    TreeParams t;
+    CUtensorMap keys, values;  // [pages][heads][tokens][elements]
+    int box;                   // groups of a box, which lie in one page
 };
 
 struct Control {
-    unsigned long long full[8], empty[8], scores[kScoreTiles], weights[kScoreTiles], queries, sums, drained;
+    unsigned long long full[8], clean[8], empty[8], edges[8], scores[kScoreTiles], weights[kScoreTiles], queries[2], queries_read[2], sums, drained;
     uint32_t tmem;
     int failed;
-    int not_finite;       // a value that some rows see and others do not was not finite, in some tile so far
-    unsigned missing[8];  // groups of a tile whose page is missing; copies are at most five tiles ahead of the softmax
+    int not_finite;          // a value that some rows see and others do not was not finite, in some tile so far
+    unsigned missing[8];     // groups of a tile whose page is missing; copies are at most five tiles ahead of the softmax
+    float high[2][2][kRows]; // maxima of tiles, by the tile's parity and the half of its positions
 };
 
 // Whether some of the positions [t, t + n) are seen by some nodes and not by others.
@@ -60,92 +79,161 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return r;
 }
 
+// Keys and values of the blocks' tiles, in the order in which they are needed. Lane i copies box i of a tile: `box` groups of
+// 64 elements.
 template <int D>
-__device__ void copy_role(const TreeParams& p, Dealer<kRows, Shape<D>::kTile, kThreads> deal, Control& c, uint32_t ring) {
+__device__ void copy_role(const TcParams& tc, Dealer<kRows, Shape<D>::kTile, kThreads> deal, Control& c, uint32_t ring) {
     using S = Shape<D>;
-    constexpr int kTile = S::kTile, kGroups = kTile / kGroup, kPieces = D / 8, kStep = 32 * kCopyWarps / kPieces, kSteps = kTile / kStep;
-    const int u = threadIdx.x - 32 * (kSoftmaxWarps + 1), lane = u & 31, piece = u % kPieces, row0 = u / kPieces;
-    const int d = p.a.head_dim, pieces = (d + 15) / 16 * 2;  // products take 16 elements: the last piece may be zeros
-    // where this thread's piece of row row0 is in a tile; rows further on are a multiple of 8 rows or 4 rows away
-    const uint32_t panel = static_cast<uint32_t>(piece >> 3) * S::kPanel;
-    uint32_t next = 0, signalled = 0;
-    const auto slot_at = [&](uint32_t i) { return ring + i % S::kSlots * S::kTileBytes; };
-    const auto place = [&](uint32_t i, int row) { return slot_at(i) + panel + row * 128 + (((piece & 7) ^ (row & 7)) << 4); };
-    uint32_t edges = 0;  // bit i % 32: tile i holds values that some rows do not see
-    const auto signal = [&]() {  // tile `signalled` has arrived
-        const uint32_t i = signalled++;
-        if (edges >> (i % 32) & 1u) {
-            edges &= ~(1u << (i % 32));
-            // a value that is not finite must not meet a weight of zero: it is taken out here and added at the end to
-            // the rows that see it
-            bool bad = false;
-            if (piece < pieces)
-                for (int k = 0; k < kSteps; ++k) {
-                    const uint32_t at = place(i, row0 + k * kStep);
-                    uint32_t w[4], any = 0;
-                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t mask = ((w[e] & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((w[e] & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
-                        w[e] &= ~mask;
-                        any |= mask;
-                    }
-                    if (any == 0) continue;
-                    bad = true;
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
-                }
-            if (bad) *static_cast<volatile int*>(&c.not_finite) = 1;
-        }
-        shared_to_async_proxy();
-        __syncwarp();
-        if (lane == 0) barrier_arrive(shared_address(&c.full[i % S::kSlots]));
-    };
+    constexpr int kGroups = S::kTile / kGroup, kPanels = D / 64;
+    const TreeParams& p = tc.t;
+    const int lane = threadIdx.x & 31, panel = lane % kPanels, group = lane / kPanels * tc.box;  // group: of the tile
+    const bool mine = group < kGroups && 64 * panel < p.a.head_dim;
+    const uint32_t box_bytes = tc.box * kGroup * 128;
+    uint32_t copies = 0, tiles = 0, edges = 0;
     Piece s;
-    uint32_t tiles = 0;
     while (deal.take(p, s)) {
         const int* table = p.pages.table + static_cast<size_t>(s.span.row) * p.pages.row_pages;
-        // lane g: page and place of the tile's group g
         const auto look_up = [&](int tile) {
-            const int group = tile * kGroups + lane;
-            return lane < kGroups && group * kGroup < s.span.len ? table[group / p.page_groups] : -1;
+            const int g = tile * kGroups + group;
+            return mine && g * kGroup < s.span.len ? table[g / p.page_groups] : -1;
         };
         const int stop = s.span.first_tile + s.to;
         int page = look_up(s.span.first_tile + s.from);
         for (int tile = s.span.first_tile + s.from; tile < stop; ++tile, ++tiles) {
-            const int t0 = tile * kTile, group = tile * kGroups + lane;
             const bool real = page >= 0 && page < p.pages.n_pages;
-            const unsigned missing = ~__ballot_sync(kAll, real) & ((1u << kGroups) - 1u);
-            const long long at = real ? static_cast<long long>(page * p.a.page_stride + group % p.page_groups * (kGroup * p.a.token_stride)) : 0;
-            if (u == 0) *static_cast<volatile unsigned*>(&c.missing[tiles % 8]) = missing;
+            const int y = (tile * kGroups + group) % p.page_groups * kGroup, w = page;
+            const unsigned boxes = __ballot_sync(kAll, real);
+            unsigned missing = 0;  // groups, from the boxes of the first panel
+            for (int g = 0; g < kGroups; ++g)
+                if (!(boxes >> (g / tc.box * kPanels) & 1u)) missing |= 1u << g;
+            if (lane == 0) *static_cast<volatile unsigned*>(&c.missing[tiles % 8]) = missing;
             if (tile + 1 < stop) page = look_up(tile + 1);
-            const bool edge = edge_of(p, s.span, t0, kTile);
-#pragma unroll
+            const uint32_t bytes = __popc(boxes) * box_bytes;
+#pragma unroll 1
             for (int kind = 0; kind < 2; ++kind) {
-                const uint32_t i = next++;
-                if (!__all_sync(kAll, barrier_wait(shared_address(&c.empty[i % S::kSlots]), (i / S::kSlots & 1) ^ 1, &c.failed))) {
-                    copies_wait<0>();
+                const uint32_t i = copies++, slot = i % S::kSlots, at = ring + slot * S::kTileBytes;
+                if (!__all_sync(kAll, barrier_wait(shared_address(&c.empty[slot]), (i / S::kSlots & 1) ^ 1, &c.failed))) {
+                    int late = 0;  // what is under way arrives first
+                    for (uint32_t k = i < S::kSlots ? 0 : i - S::kSlots; k < i; ++k) barrier_wait(shared_address(&c.full[k % S::kSlots]), k / S::kSlots & 1, &late);
                     return;
                 }
-                const T* from = reinterpret_cast<const T*>(kind == 0 ? p.a.k : p.a.v) + s.head * p.a.head_stride + 8 * piece;
-#pragma unroll
-                for (int k = 0; k < kSteps; ++k) {
-                    constexpr int kPerGroup = kGroup / kStep > 0 ? kGroup / kStep : 1;
-                    const int row = row0 + k * kStep, t = t0 + row;
-                    const long long base = __shfl_sync(kAll, at, k / kPerGroup);
-                    const bool seen = !(missing >> (k / kPerGroup) & 1u) && t >= s.span.lo && t < s.span.len && 8 * piece < d;
-                    if (piece < pieces) copy_async16(place(i, row), from + base + (row % kGroup) * p.a.token_stride, seen);
+                if (kind == 1 && missing != 0) {  // what tiles before left there is no number to meet a weight of zero
+                    for (int g = 0; g < kGroups; ++g)
+                        if (missing >> g & 1u)
+                            for (int u = lane; u < kPanels * kGroup * 8; u += 32)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + u / (kGroup * 8) * S::kPanel + g * (kGroup * 128) + u % (kGroup * 8) * 16), "r"(0)
+                                             : "memory");
+                    shared_to_async_proxy();
                 }
-                copies_commit();
-                if (kind == 1 && edge) edges |= 1u << (i % 32);
-                if (next > S::kDepth) {
-                    copies_wait<S::kDepth>();
-                    signal();
+                __syncwarp();
+                if (lane == 0) {
+                    barrier_arrive_bytes(shared_address(&c.full[slot]), bytes);
+                    if (kind == 1) {
+                        if (edge_of(p, s.span, tile * S::kTile, S::kTile)) barrier_arrive(shared_address(&c.edges[edges++ % 8]));
+                        else barrier_arrive_count(shared_address(&c.clean[slot]), kHelpWarps);
+                    }
                 }
+                __syncwarp();
+                if (real) copy_box(at + panel * S::kPanel + group * (kGroup * 128), kind == 0 ? &tc.keys : &tc.values, 64 * panel, y, s.head, w, shared_address(&c.full[slot]));
             }
         }
     }
-    copies_wait<0>();
-    while (signalled < next) signal();
+}
+
+// Queries of the block, by all helpers. Rows that are not real stay what they were: their results go nowhere.
+template <int D>
+__device__ void copy_queries(const TreeParams& p, const Piece& s, uint32_t to) {
+    using S = Shape<D>;
+    constexpr int kPieces = D / 8, kStep = kHelpThreads / kPieces;
+    const int u = threadIdx.x - 32 * (kSoftmaxWarps + 2), piece = u % kPieces, row0 = u / kPieces, rows = s.span.nodes * p.a.group;
+    const int rows_here = min(kRows, rows - s.block * kRows);
+    int all = s.block * kRows + row0, node = all / p.a.group, h = all - node * p.a.group;
+    const T* from = reinterpret_cast<const T*>(p.a.q) + s.span.first * p.a.q_row + static_cast<uint64_t>(s.head) * p.a.group * p.a.q_head + 8 * piece;
+    const bool held = 8 * piece < p.a.head_dim;
+    constexpr int kAhead = 8;
+    static_assert(kRows % (kAhead * kStep) == 0);
+#pragma unroll 1
+    for (int row = row0; row < rows_here; row += kAhead * kStep) {
+        uint4 x[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            x[k] = held && all < rows ? *reinterpret_cast<const uint4*>(from + node * p.a.q_row + h * p.a.q_head) : make_uint4(0, 0, 0, 0);
+            all += kStep;
+            for (h += kStep; h >= p.a.group; h -= p.a.group) ++node;
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int r = row + k * kStep;
+            const uint32_t at = to + static_cast<uint32_t>(piece >> 3) * S::kQueryPanel + r * 128 + (((piece & 7) ^ (r & 7)) << 4);
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x[k].x), "r"(x[k].y), "r"(x[k].z), "r"(x[k].w) : "memory");
+        }
+    }
+}
+
+// A value that is not finite must not meet a weight of zero: it is taken out here and added at the end to the rows that see
+// it. So are the rows outside [lo, hi), which nobody sees. True if there was one inside.
+template <int D>
+__device__ bool clean_values(uint32_t tile, int lo, int hi) {
+    using S = Shape<D>;
+    const int u = threadIdx.x - 32 * (kSoftmaxWarps + 2);
+    bool bad = false;
+#pragma unroll 2
+    for (int i = u; i < S::kTile * (D / 8); i += kHelpThreads) {
+        const uint32_t at = tile + i * 16;
+        const int row = i / 8 % S::kTile;
+        uint32_t w[4], any = 0;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
+        const bool inside = row >= lo && row < hi;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t mask = ((w[e] & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((w[e] & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+            any |= mask;
+            w[e] = inside ? w[e] & ~mask : 0;
+        }
+        if (any != 0 || !inside) asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+        bad = bad || (any != 0 && inside);
+    }
+    return bad;
+}
+
+template <int D>
+__device__ void help_role(const TreeParams& p, Dealer<kRows, Shape<D>::kTile, kThreads> deal, Control& c, uint32_t queries, uint32_t ring) {
+    using S = Shape<D>;
+    const int lane = threadIdx.x & 31;
+    uint32_t blocks = 0, tiles = 0, edges = 0;
+    const auto tell = [&](unsigned long long* bar) {
+        shared_to_async_proxy();
+        __syncwarp();
+        if (lane == 0) barrier_arrive(shared_address(bar));
+    };
+    const auto block = [&](const Piece& s) {
+        const uint32_t b = blocks % S::kQueries;
+        if (!__all_sync(kAll, barrier_wait(shared_address(&c.queries_read[b]), (blocks / S::kQueries & 1) ^ 1, &c.failed))) return false;
+        ++blocks;
+        copy_queries<D>(p, s, queries + b * S::kQueryBytes);
+        tell(&c.queries[b]);
+        return true;
+    };
+    Piece s, next;
+    bool more = deal.take(p, s);
+    if (more && !block(s)) return;
+    while (more) {
+        more = deal.take(p, next);
+        if (S::kQueries > 1 && more && !block(next)) return;
+        for (int tile = s.span.first_tile + s.from; tile < s.span.first_tile + s.to; ++tile, ++tiles) {
+            if (!edge_of(p, s.span, tile * S::kTile, S::kTile)) continue;
+            const uint32_t i = 2 * tiles + 1, slot = i % S::kSlots, e = edges++;
+            // first that its copy has begun: the slot's own phase may be any before that
+            if (!__all_sync(kAll, barrier_wait(shared_address(&c.edges[e % 8]), e / 8 & 1, &c.failed))) return;
+            if (!__all_sync(kAll, barrier_wait(shared_address(&c.full[slot]), i / S::kSlots & 1, &c.failed))) return;
+            if (clean_values<D>(ring + slot * S::kTileBytes, s.span.lo - tile * S::kTile, s.span.len - tile * S::kTile))
+                *static_cast<volatile int*>(&c.not_finite) = 1;
+            tell(&c.clean[slot]);
+        }
+        // with room for one block of queries the next can come only when this one has been read to its end
+        if (S::kQueries == 1 && more && !block(next)) return;
+        s = next;
+    }
 }
 
 template <int D>
@@ -157,127 +245,125 @@ __device__ void product_role(const TreeParams& p, Dealer<kRows, Shape<D>::kTile,
     const uint32_t values = product_descriptor(16 * steps, true);
     const uint32_t tmem = c.tmem;
     uint32_t tiles = 0, blocks = 0;  // so far
-    const auto scores_of = [&](uint32_t tile) {
-        const uint32_t i = 2 * tile;
+    const auto scores_of = [&](uint32_t tile, bool last) {
+        const uint32_t i = 2 * tile, b = blocks % S::kQueries;
         if (!barrier_wait(shared_address(&c.full[i % S::kSlots]), i / S::kSlots & 1, &c.failed)) return false;
         tc_fence_after();
-        const uint32_t k = ring + i % S::kSlots * S::kTileBytes;
+        const uint32_t k = ring + i % S::kSlots * S::kTileBytes, q = queries + b * S::kQueryBytes;
+#pragma unroll 2
         for (int e = 0; e < steps; ++e)
-            tc_product(tmem + tile % kScoreTiles * kTile, tile_descriptor(queries + e / 4 * S::kQueryPanel + e % 4 * 32, 16),
+            tc_product(tmem + tile % kScoreTiles * kTile, tile_descriptor(q + e / 4 * S::kQueryPanel + e % 4 * 32, 16),
                        tile_descriptor(k + e / 4 * S::kPanel + e % 4 * 32, 16), kScores, e > 0);
         tc_commit(shared_address(&c.empty[i % S::kSlots]));
         tc_commit(shared_address(&c.scores[tile % kScoreTiles]));
+        if (last) tc_commit(shared_address(&c.queries_read[b]));
         return true;
     };
     Piece s;
-    while (deal.take(p, s)) {
+    for (; deal.take(p, s); ++blocks) {
         const uint32_t n = s.to - s.from;
-        if (!barrier_wait(shared_address(&c.queries), blocks++ & 1, &c.failed)) return;
+        if (!barrier_wait(shared_address(&c.queries[blocks % S::kQueries]), blocks / S::kQueries & 1, &c.failed)) return;
         tc_fence_after();
-        if (!scores_of(tiles)) return;
-        if (n > 1 && !scores_of(tiles + 1)) return;
+        if (!scores_of(tiles, n == 1)) return;
+        if (n > 1 && !scores_of(tiles + 1, n == 2)) return;
         for (uint32_t j = 0; j < n; ++j, ++tiles) {
             const uint32_t i = 2 * tiles + 1, buffer = tiles % kScoreTiles;
             if (!barrier_wait(shared_address(&c.weights[buffer]), tiles / kScoreTiles & 1, &c.failed)) return;
             if (!barrier_wait(shared_address(&c.full[i % S::kSlots]), i / S::kSlots & 1, &c.failed)) return;
+            if (!barrier_wait(shared_address(&c.clean[i % S::kSlots]), i / S::kSlots & 1, &c.failed)) return;
             tc_fence_after();
             const uint32_t v = ring + i % S::kSlots * S::kTileBytes, w = tmem + buffer * kTile;
-#pragma unroll
+#pragma unroll 1
             for (int half = 0; half < 2; ++half)  // the weights' upper and lower bits
+#pragma unroll 2
                 for (int e = 0; e < kTile / 16; ++e)
-                    tc_product_from_tmem(tmem + S::kSums, w + half * (kTile / 2) + 8 * e, tile_descriptor(v + e * 2048, S::kPanel), values,
+                    tc_product_from_tmem(tmem + S::kSums, w + e / 2 * 32 + half * 16 + e % 2 * 8, tile_descriptor(v + e * 2048, S::kPanel), values,
                                          j > 0 || half > 0 || e > 0);
             tc_commit(shared_address(&c.empty[i % S::kSlots]));
             tc_commit(shared_address(&c.sums));
-            if (j + 2 < n && !scores_of(tiles + 2)) return;
+            if (j + 2 < n && !scores_of(tiles + 2, j + 3 == n)) return;
         }
     }
 }
 
-template <int D, bool kExtra>
-__device__ void softmax_role(const TreeParams& p, Dealer<kRows, Shape<D>::kTile, kThreads> deal, Control& c, Nodes& nodes, uint32_t queries) {
+// A barrier of `threads` threads, true if x is in one of them.
+template <int kThreadsHere>
+__device__ __forceinline__ bool any_of(uint32_t id, bool x) {
+    uint32_t any;
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.or.pred p, %2, %3, q;\n selp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(any) : "r"(static_cast<uint32_t>(x)), "r"(id), "n"(kThreadsHere) : "memory");
+    return any != 0;
+}
+__device__ __forceinline__ void pair_barrier(uint32_t id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
+
+template <int D, Scores kScores>
+__device__ void softmax_role(const TreeParams& p, Dealer<kRows, Shape<D>::kTile, kThreads> deal, Control& c, Nodes& nodes) {
     using S = Shape<D>;
-    constexpr int kTile = S::kTile, kPieces = D / 8;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, d = p.a.head_dim;
-    const uint32_t tmem = c.tmem + (static_cast<uint32_t>(32 * warp) << 16);
-    const float factor = p.a.scale * kLog2e;  // positive unless kExtra
+    constexpr int kTile = S::kTile, kMine = kTile / 2;  // positions of a thread
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = warp >> 2, row = threadIdx.x & 127, d = p.a.head_dim;
+    const uint32_t pair = 2 + (warp & 3);  // barrier of the two warps with the same rows
+    const uint32_t tmem = c.tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16);
+    const float by = kScores == kPlain ? p.a.scale * kLog2e : 1.0f;
     uint32_t tiles = 0;
     int tree = -1;
     bool ok = true;  // a wait that gives up leaves the loops as they are: other warps may wait for this one
     Piece s;
     while (deal.take(p, s)) {
         if (s.tree != tree)
-            fill_nodes<32 * kSoftmaxWarps>(p, s.span, nodes, threadIdx.x, [](bool x) {
-                uint32_t any;
-                asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.or.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}"
-                             : "=r"(any) : "r"(static_cast<uint32_t>(x)), "n"(32 * kSoftmaxWarps) : "memory");
-                return any != 0;
-            });
+            fill_nodes<32 * kSoftmaxWarps>(p, s.span, nodes, threadIdx.x, [](bool x) { return any_of<32 * kSoftmaxWarps>(1, x); });
         tree = s.tree;
-        const int rows = s.span.nodes * p.a.group, all = s.block * kRows + threadIdx.x;
-        const bool real = all < rows, idle = s.block * kRows + 32 * warp >= rows;  // idle: none of the warp's rows is real
+        const int rows = s.span.nodes * p.a.group, all = s.block * kRows + row;
+        const bool real = all < rows, idle = s.block * kRows + 32 * (warp & 3) >= rows;  // idle: none of the warp's rows is real
         const int node = real ? all / p.a.group : 0, h = real ? all - node * p.a.group : 0, depth = real ? nodes.depth[node] : -1;
-        {   // the warp's queries
-            const T* mine = reinterpret_cast<const T*>(p.a.q) + (s.span.first + node) * p.a.q_row + (s.head * p.a.group + h) * p.a.q_head;
-            constexpr int kLanes = kPieces < 32 ? kPieces : 32, kAtOnce = 32 / kLanes;
-            const int piece = lane % kLanes;
-            const unsigned valid = __ballot_sync(kAll, real);
-            if (!idle)
-#pragma unroll 4
-                for (int k = 0; k < 32; k += kAtOnce) {
-                    const int r = k + lane / kLanes, row = 32 * warp + r;
-                    const T* from = reinterpret_cast<const T*>(__shfl_sync(kAll, reinterpret_cast<unsigned long long>(mine), r));
-                    copy_async16(queries + (piece >> 3) * S::kQueryPanel + row * 128 + (((piece & 7) ^ (row & 7)) << 4), from + 8 * piece,
-                                 (valid >> r & 1u) && 8 * piece < d);
-                }
-            copies_commit();
-            copies_wait<0>();
-            shared_to_async_proxy();
-            __syncwarp();
-            if (lane == 0) barrier_arrive(shared_address(&c.queries));
-        }
-        const float slope = kExtra && real && p.a.slopes != nullptr ? p.a.slopes[s.head * p.a.group + h] * kLog2e : 0.0f;
+        const float slope = kScores == kBiased && real && p.a.slopes != nullptr ? p.a.slopes[s.head * p.a.group + h] * kLog2e : 0.0f;
         float m = kLowest, offset = 0.0f, l = 0.0f;  // offset: what is subtracted from scores, in powers of two; 0 before one is seen
         for (int tile = s.span.first_tile + s.from; tile < s.span.first_tile + s.to; ++tile, ++tiles) {
-            const int t0 = tile * kTile;
-            const uint32_t buffer = tiles % kScoreTiles, at = tmem + buffer * kTile;
+            const int t0 = tile * kTile + half * kMine;
+            const uint32_t buffer = tiles % kScoreTiles, at = tmem + buffer * kTile + half * kMine;
             ok = barrier_wait(shared_address(&c.scores[buffer]), tiles / kScoreTiles & 1, &c.failed) && ok;
             tc_fence_after();
             if (!idle) {
-                uint32_t raw[kTile];
+                const unsigned missing = *static_cast<volatile unsigned*>(&c.missing[tiles % 8]) >> (half * kMine / kGroup);
+                const bool edge = missing != 0 || edge_of(p, s.span, tile * kTile, kTile);
+                float high = kLowest;
+                if (kScores == kPlain && !edge) {
+#pragma unroll 1
+                    for (int k = 0; k < kMine; k += 32) {
+                        uint32_t raw[32];
+                        tmem_load32(at + k, raw);
+                        tc_wait_loads();
 #pragma unroll
-                for (int k = 0; k < kTile; k += 32) tmem_load32(at + k, raw + k);
-                tc_wait_loads();
-                const unsigned missing = *static_cast<volatile unsigned*>(&c.missing[tiles % 8]);
-                const bool edge = missing != 0 || edge_of(p, s.span, t0, kTile);
-                if (kExtra || edge) {
+                        for (int e = 0; e < 32; ++e) high = fmaxf(high, __uint_as_float(raw[e]));
+                    }
+                } else {
+#pragma unroll 1
+                    for (int k = 0; k < kMine; k += 16) {
+                        uint32_t raw[16];
+                        tmem_load16(at + k, raw);
+                        unsigned seen = edge && !(missing >> (k / kGroup) & 1u) ? seen_of(p, s.span, depth, nodes.mask[node], t0 + k) : edge ? 0 : kAll;
+                        tc_wait_loads();
 #pragma unroll
-                    for (int k = 0; k < kTile; k += 32) {
-                        unsigned seen = kAll;
-                        if (edge) {
-                            seen = seen_of(p, s.span, depth, nodes.mask[node], t0 + k);
-                            if (missing >> (k / kGroup) & 1u) seen &= 0xFFFF0000u;
-                            if (missing >> (k / kGroup + 1) & 1u) seen &= 0x0000FFFFu;
-                        }
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            float x = __uint_as_float(raw[k + e]);
+                        for (int e = 0; e < 16; ++e) {
+                            float x = __uint_as_float(raw[e]);
                             const bool sees = seen >> e & 1u;
-                            if constexpr (kExtra) {
+                            if constexpr (kScores == kCapped) x = capped(p, x);
+                            if constexpr (kScores == kBiased) {
                                 const int t = t0 + k + e;
                                 int back = t - s.span.base - depth;
                                 if (edge && sees && t >= s.span.base) back = nodes.depth[t - s.span.base] - depth;
                                 x = score<true>(p, x, slope, back);
                             }
-                            raw[k + e] = __float_as_uint(sees ? x : -INFINITY);
+                            if (!sees) x = -INFINITY;
+                            raw[e] = __float_as_uint(x);
+                            high = fmaxf(high, x);
                         }
+                        tmem_store16(at + k, raw);
                     }
+                    tc_wait_stores();
                 }
-                float high = kLowest;
-#pragma unroll
-                for (int k = 0; k < kTile; ++k) high = fmaxf(high, __uint_as_float(raw[k]));
-                const float by = kExtra ? 1.0f : factor;
-                const bool first = tile == s.span.first_tile + s.from;
+                c.high[tiles & 1][half][row] = high;
+                pair_barrier(pair);
+                high = fmaxf(high, c.high[tiles & 1][half ^ 1][row]);
                 const bool rises = high > m && (m == kLowest || (high - m) * by > kSlack);
                 if (__any_sync(kAll, rises)) {
                     float k = 1.0f;
@@ -288,11 +374,11 @@ __device__ void softmax_role(const TreeParams& p, Dealer<kRows, Shape<D>::kTile,
                         offset = top;
                         l *= k;
                     }
-                    if (!first) {
+                    if (tile != s.span.first_tile + s.from) {
                         ok = barrier_wait(shared_address(&c.sums), (tiles - 1) & 1, &c.failed) && ok;
                         tc_fence_after();
-#pragma unroll
-                        for (int e = 0; e < D; e += 32) {
+#pragma unroll 1
+                        for (int e = half * (D / 2); e < (half + 1) * (D / 2); e += 32) {
                             uint32_t o[32];
                             tmem_load32(tmem + S::kSums + e, o);
                             tc_wait_loads();
@@ -302,24 +388,26 @@ __device__ void softmax_role(const TreeParams& p, Dealer<kRows, Shape<D>::kTile,
                         }
                     }
                 }
-                float part[4] = {};
+                float2 part[2] = {};
+                const float2 by2 = make_float2(by, by), less = make_float2(-offset, -offset);
+#pragma unroll 1
+                for (int k = 0; k < kMine; k += 32) {
+                    uint32_t raw[32], w[32];  // upper bits of 32 weights, then lower bits
+                    tmem_load32(at + k, raw);
+                    tc_wait_loads();
 #pragma unroll
-                for (int k = 0; k < kTile; k += 64) {
-                    uint32_t upper[32], lower[32];
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const float x0 = __uint_as_float(raw[k + 2 * e]), x1 = __uint_as_float(raw[k + 2 * e + 1]);
-                        const float w0 = exp2_approx(kExtra ? x0 - offset : fmaf(x0, by, -offset));
-                        const float w1 = exp2_approx(kExtra ? x1 - offset : fmaf(x1, by, -offset));
-                        part[e & 1] += w0;
-                        part[2 + (e & 1)] += w1;
-                        upper[e] = pack_bf16(w0, w1);
-                        lower[e] = pack_bf16(w0 - __uint_as_float(upper[e] << 16), w1 - __uint_as_float(upper[e] & 0xFFFF0000u));
+                    for (int e = 0; e < 16; ++e) {
+                        float2 x = __ffma2_rn(make_float2(__uint_as_float(raw[2 * e]), __uint_as_float(raw[2 * e + 1])), by2, less);
+                        x.x = exp2_approx(x.x);
+                        x.y = exp2_approx(x.y);
+                        part[e & 1] = __fadd2_rn(part[e & 1], x);
+                        w[e] = pack_bf16(x.x, x.y);
+                        const float2 rest = __fadd2_rn(x, make_float2(-__uint_as_float(w[e] << 16), -__uint_as_float(w[e] & 0xFFFF0000u)));
+                        w[16 + e] = pack_bf16(rest.x, rest.y);
                     }
-                    tmem_store32(at + k / 2, upper);
-                    tmem_store32(at + kTile / 2 + k / 2, lower);
+                    tmem_store32(at + k, w);
                 }
-                l += (part[0] + part[1]) + (part[2] + part[3]);
+                l += (part[0].x + part[0].y) + (part[1].x + part[1].y);
                 tc_wait_stores();
             }
             // The product of the tile before this one is done before this one's may start: so its weights' place is free
@@ -329,20 +417,26 @@ __device__ void softmax_role(const TreeParams& p, Dealer<kRows, Shape<D>::kTile,
             __syncwarp();
             if (lane == 0) barrier_arrive(shared_address(&c.weights[buffer]));
         }
+        if (!idle) {  // the row's sum of weights; this tile's place of maxima was last read a tile ago
+            c.high[tiles & 1][half][row] = l;
+            pair_barrier(pair);
+            l += c.high[tiles & 1][half ^ 1][row];
+            pair_barrier(pair);
+        }
         ok = barrier_wait(shared_address(&c.sums), (tiles - 1) & 1, &c.failed) && ok;
         tc_fence_after();
         if (idle) continue;
         const bool whole = s.from == 0 && s.to == s.span.tiles;
         float* slot = slot_of<kRows, D>(p, blockIdx.x, s.from == 0);
-        if (!whole && real) {
-            slot[kRows * D + threadIdx.x] = m == kLowest || depth < 0 ? kLowest : offset;
-            slot[kRows * D + kRows + threadIdx.x] = depth < 0 ? 0.0f : l;
+        if (!whole && real && half == 0) {
+            slot[kRows * D + row] = m == kLowest || depth < 0 ? kLowest : offset;
+            slot[kRows * D + kRows + row] = depth < 0 ? 0.0f : l;
         }
         const float inverse = l > 0.0f ? 1.0f / l : 0.0f;
         const bool mend = *static_cast<volatile int*>(&c.not_finite) != 0;
         T* out = reinterpret_cast<T*>(p.a.out) + (s.span.first + node) * p.a.out_row + (s.head * p.a.group + h) * p.a.out_head;
-#pragma unroll
-        for (int e = 0; e < D; e += 32) {
+#pragma unroll 1
+        for (int e = half * (D / 2); e < (half + 1) * (D / 2); e += 32) {
             uint32_t o[32];
             tmem_load32(tmem + S::kSums + e, o);
             tc_wait_loads();  // every lane's loads, also of lanes whose row is not real
@@ -370,8 +464,8 @@ __device__ void softmax_role(const TreeParams& p, Dealer<kRows, Shape<D>::kTile,
                 if (e + i >= d) continue;
                 const auto x = [&](int k) { return !ok ? NAN : depth < 0 ? 0.0f : __uint_as_float(o[i + k]); };
                 if (!whole) {
-                    *reinterpret_cast<float4*>(slot + threadIdx.x * D + e + i) = make_float4(x(0), x(1), x(2), x(3));
-                    *reinterpret_cast<float4*>(slot + threadIdx.x * D + e + i + 4) = make_float4(x(4), x(5), x(6), x(7));
+                    *reinterpret_cast<float4*>(slot + row * D + e + i) = make_float4(x(0), x(1), x(2), x(3));
+                    *reinterpret_cast<float4*>(slot + row * D + e + i + 4) = make_float4(x(4), x(5), x(6), x(7));
                 } else {
                     *reinterpret_cast<uint4*>(out + e + i) = make_uint4(pack_bf16(x(0) * inverse, x(1) * inverse), pack_bf16(x(2) * inverse, x(3) * inverse),
                                                                         pack_bf16(x(4) * inverse, x(5) * inverse), pack_bf16(x(6) * inverse, x(7) * inverse));
@@ -382,25 +476,31 @@ __device__ void softmax_role(const TreeParams& p, Dealer<kRows, Shape<D>::kTile,
     }
 }
 
-template <int D, bool kExtra>
-__global__ void __launch_bounds__(kThreads, 1) tree_bf16_kernel(const __grid_constant__ TreeParams p) {
+template <int D, Scores kScores>
+__global__ void __launch_bounds__(kThreads, 1) tree_bf16_kernel(const __grid_constant__ TcParams tc) {
     using S = Shape<D>;
+    const TreeParams& p = tc.t;
     extern __shared__ char dynamic[];
     __shared__ Control c;
     __shared__ Nodes nodes;
     __shared__ long long sums[kThreads / 32], found[2];
     const int warp = threadIdx.x >> 5;
-    const uint32_t queries = (shared_address(dynamic) + 1023) & ~1023u, ring = queries + S::kQueryBytes;
+    const uint32_t queries = (shared_address(dynamic) + 1023) & ~1023u, ring = queries + S::kQueries * S::kQueryBytes;
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kSlots; ++i) {
-            barrier_init(shared_address(&c.full[i]), kCopyWarps);
+            barrier_init(shared_address(&c.full[i]), 1);
+            barrier_init(shared_address(&c.clean[i]), kHelpWarps);
             barrier_init(shared_address(&c.empty[i]), 1);
         }
+        for (int i = 0; i < 8; ++i) barrier_init(shared_address(&c.edges[i]), 1);
         for (int i = 0; i < kScoreTiles; ++i) {
             barrier_init(shared_address(&c.scores[i]), 1);
             barrier_init(shared_address(&c.weights[i]), kSoftmaxWarps);
         }
-        barrier_init(shared_address(&c.queries), kSoftmaxWarps);
+        for (int i = 0; i < S::kQueries; ++i) {
+            barrier_init(shared_address(&c.queries[i]), kHelpWarps);
+            barrier_init(shared_address(&c.queries_read[i]), 1);
+        }
         barrier_init(shared_address(&c.sums), 1);
         barrier_init(shared_address(&c.drained), 1);
         c.failed = c.not_finite = 0;
@@ -415,7 +515,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_bf16_kernel(const __grid_con
     Dealer<kRows, S::kTile, kThreads> deal;
     if (deal.start(p, blockIdx.x, gridDim.x, sums, found)) {
         if (warp < kSoftmaxWarps) {
-            softmax_role<D, kExtra>(p, deal, c, nodes, queries);
+            softmax_role<D, kScores>(p, deal, c, nodes);
         } else if (warp == kSoftmaxWarps) {
             if ((threadIdx.x & 31) == 0) {
                 product_role<D>(p, deal, c, queries, ring);
@@ -426,8 +526,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_bf16_kernel(const __grid_con
                 }
             }
             __syncwarp();
-        } else if (warp <= kSoftmaxWarps + kCopyWarps) {
-            copy_role<D>(p, deal, c, ring);
+        } else if (warp == kSoftmaxWarps + 1) {
+            copy_role<D>(tc, deal, c, ring);
+        } else {
+            help_role<D>(p, deal, c, queries, ring);
         }
     }
     tc_fence_before();
@@ -455,19 +557,56 @@ cudaError_t resident(int shared, int& ctas) {
     return cudaSuccess;
 }
 
-template <int D, bool kExtra>
-cudaError_t launch_extra(const TreeParams& p, cudaStream_t s) {
+using Encode = decltype(&cuTensorMapEncodeTiled);
+
+// The driver's function that describes a tensor to the copies, asked for once.
+cudaError_t encoder(Encode& encode) {
+    static std::atomic<void*> known;
+    void* f = known.load(std::memory_order_acquire);
+    if (f == nullptr) {
+        cudaDriverEntryPointQueryResult found;
+        const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found);
+        if (e != cudaSuccess) return e;
+        if (found != cudaDriverEntryPointSuccess || f == nullptr) return cudaErrorNotSupported;
+        known.store(f, std::memory_order_release);
+    }
+    encode = reinterpret_cast<Encode>(f);
+    return cudaSuccess;
+}
+
+cudaError_t describe(CUtensorMap& map, const TreeParams& p, const char* pool, int box) {
+    Encode encode = nullptr;
+    const cudaError_t e = encoder(encode);
+    if (e != cudaSuccess) return e;
+    const cuuint64_t page = static_cast<cuuint64_t>(p.a.heads) * p.a.head_dim * p.pages.page_tokens;
+    const cuuint64_t dims[4] = {static_cast<cuuint64_t>(p.a.head_dim), static_cast<cuuint64_t>(p.pages.page_tokens), static_cast<cuuint64_t>(p.a.heads),
+                                static_cast<cuuint64_t>(p.pages.n_pages)};
+    const cuuint64_t strides[3] = {p.a.token_stride * sizeof(T), p.a.head_stride * sizeof(T), (p.pages.n_pages > 1 ? p.a.page_stride : page) * sizeof(T)};
+    const cuuint32_t boxes[4] = {64, static_cast<cuuint32_t>(box * kGroup), 1, 1}, steps[4] = {1, 1, 1, 1};
+    const CUresult r = encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<char*>(pool), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+template <int D, Scores kScores>
+cudaError_t launch_scores(const TreeParams& p, cudaStream_t s) {
     constexpr int slices = kRows / (128 / (D / 4));
     int ctas = 0;
-    cudaError_t e = resident<tree_bf16_kernel<D, kExtra>>(Shape<D>::kShared, ctas);
+    cudaError_t e = resident<tree_bf16_kernel<D, kScores>>(Shape<D>::kShared, ctas);
     if (e != cudaSuccess) return e;
-    e = launch(tree_bf16_kernel<D, kExtra>, ctas, kThreads, Shape<D>::kShared, 0, s, p);
+    TcParams tc;
+    tc.t = p;
+    tc.box = std::gcd(p.page_groups, Shape<D>::kTile / kGroup);
+    e = describe(tc.keys, p, p.a.k, tc.box);
+    if (e == cudaSuccess) e = describe(tc.values, p, p.a.v, tc.box);
+    if (e == cudaSuccess) e = launch(tree_bf16_kernel<D, kScores>, ctas, kThreads, Shape<D>::kShared, 0, s, tc);
     return e != cudaSuccess || ctas == 1 ? e : launch_join<T, D, kRows, Shape<D>::kTile>(p, ctas, slices, s);
 }
 
 template <int D>
 cudaError_t launch_d(const TreeParams& p, cudaStream_t s) {
-    return p.a.softcap > 0.0f || p.a.slopes != nullptr || !(p.a.scale > 0.0f) ? launch_extra<D, true>(p, s) : launch_extra<D, false>(p, s);
+    if (p.a.slopes != nullptr || (p.a.softcap == 0.0f && !(p.a.scale > 0.0f))) return launch_scores<D, kBiased>(p, s);
+    return p.a.softcap > 0.0f ? launch_scores<D, kCapped>(p, s) : launch_scores<D, kPlain>(p, s);
 }
 
 }  // namespace
