@@ -26,6 +26,23 @@ __device__ __forceinline__ float capped(const P& p, float dot) {
     return fabsf(y) < 0.2f ? small : large;
 }
 
+// The same of two scores where |scale q.k / cap| is below kSmallCap: tanh(y) / y up to y^12, good to 5e-8 there (the next term
+// of the series is 0.0015 y^14).
+constexpr float kSmallCap = 0.45f;
+template <typename P>
+__device__ __forceinline__ float2 capped_small(const P& p, float2 dot) {
+    const auto both = [](float x) { return make_float2(x, x); };
+    const float2 x = __fmul2_rn(dot, both(p.a.scale * kLog2e)), y = __fmul2_rn(dot, both(p.cap_in)), y2 = __fmul2_rn(y, y);
+    float2 t = both(21844.0f / 6081075.0f);
+    t = __ffma2_rn(t, y2, both(-1382.0f / 155925.0f));
+    t = __ffma2_rn(t, y2, both(62.0f / 2835.0f));
+    t = __ffma2_rn(t, y2, both(-17.0f / 315.0f));
+    t = __ffma2_rn(t, y2, both(2.0f / 15.0f));
+    t = __ffma2_rn(t, y2, both(-1.0f / 3.0f));
+    t = __ffma2_rn(t, y2, both(1.0f));
+    return __fmul2_rn(x, t);
+}
+
 // The score as the softmax takes it, in units of ln 2, as is the slope.
 template <bool kExtra, typename P>
 __device__ __forceinline__ float score(const P& p, float dot, float slope, int back) {

@@ -40,6 +40,13 @@ __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, vola
     }
 }
 
+// True in one lane of a converged warp: what it alone does keeps its operands the same for the whole warp.
+__device__ __forceinline__ bool elected() {
+    uint32_t e;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xFFFFFFFF;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(e));
+    return e != 0;
+}
+
 // --- copies ------------------------------------------------------------------------------
 
 // Announces a copy's bytes at the barrier and arrives there; the phase ends when they have come, too.
@@ -76,33 +83,31 @@ __device__ __forceinline__ void tc_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
-// A tile in shared memory with rows of 128 bytes, 16-byte pieces of row r at (piece ^ r % 8), 1024-byte aligned. `leading`:
-// bytes from one 64-element panel to the next where the panels' direction is not the product's (unused otherwise).
-__device__ __forceinline__ uint64_t tile_descriptor(uint32_t at, uint32_t leading) {
-    constexpr uint64_t kVersion = 1ull << 46, kSwizzle128 = 2ull << 61, kEightRows = static_cast<uint64_t>(1024 >> 4) << 32;
-    return kSwizzle128 | kVersion | kEightRows | static_cast<uint64_t>((leading >> 4) & 0x3FFF) << 16 | ((at >> 4) & 0x3FFF);
-}
+// A tile in shared memory with rows of 128 bytes, 16-byte pieces of row r at (piece ^ r % 8), 1024-byte aligned: the lower
+// word of its descriptor, to which bytes / 16 can be added; the upper word is the same for all. `leading`: bytes from one
+// 64-element panel to the next where the panels' direction is not the product's (unused otherwise).
+__device__ __forceinline__ uint32_t tile_descriptor(uint32_t at, uint32_t leading) { return (leading >> 4) << 16 | at >> 4; }
+constexpr uint32_t kTileDescriptor = (1024u >> 4) | 1u << 14 | 2u << 29;  // eight rows, version, swizzle of 128 bytes
 
 // bf16 products with fp32 sums, M = 128: N columns; `across`: B's rows in memory are its product's summed index.
 __host__ __device__ constexpr uint32_t product_descriptor(int n, bool across) {
     return 1u << 4 | 1u << 7 | 1u << 10 | (across ? 1u << 16 : 0u) | static_cast<uint32_t>(n >> 3) << 17 | (128u >> 4) << 24;
 }
 // D = A B (+ D): A and B in shared memory; 16 summed elements.
-__device__ __forceinline__ void tc_product(uint32_t d, uint64_t a, uint64_t b, uint32_t how, bool add) {
+__device__ __forceinline__ void tc_product(uint32_t d, uint32_t a, uint32_t b, uint32_t how, bool add) {
     asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(how),
-        "r"(static_cast<uint32_t>(add))
+        "{\n .reg .pred p;\n .reg .b64 a, b;\n setp.ne.b32 p, %5, 0;\n mov.b64 a, {%1, %4};\n mov.b64 b, {%2, %4};\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n}" ::"r"(d), "r"(a), "r"(b), "r"(how), "r"(kTileDescriptor), "r"(static_cast<uint32_t>(add))
         : "memory");
 }
 // The same with A in tensor memory, two elements a column.
-__device__ __forceinline__ void tc_product_from_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t how, bool add) {
+__device__ __forceinline__ void tc_product_from_tmem(uint32_t d, uint32_t a, uint32_t b, uint32_t how, bool add) {
     asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(how),
-        "r"(static_cast<uint32_t>(add))
+        "{\n .reg .pred p;\n .reg .b64 b;\n setp.ne.b32 p, %5, 0;\n mov.b64 b, {%2, %4};\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n}" ::"r"(d), "r"(a), "r"(b), "r"(how), "r"(kTileDescriptor), "r"(static_cast<uint32_t>(add))
         : "memory");
 }
 
-// 32 columns of a warp's 32 lanes: lane l has its row's.
 // These are the whole warp's: lanes that took another way have to be back.
 __device__ __forceinline__ void tmem_load32(uint32_t at, uint32_t* x) {
     __syncwarp();

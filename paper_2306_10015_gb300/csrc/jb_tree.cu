@@ -13,6 +13,7 @@ namespace {
 constexpr int kThreads = 128;
 constexpr int kRows = 16;   // rows of a block
 constexpr int kTile = 32;   // positions of a tile
+using C = Cut<kRows, kTile, 1>;
 
 __device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
 template <int D>
@@ -36,10 +37,11 @@ __global__ void __launch_bounds__(kThreads) tree_kernel(const __grid_constant__ 
     const int d = p.a.head_dim;
     after_previous();
     let_next_start();
-    Dealer<kRows, kTile, kThreads> deal;
+    Dealer<C, kThreads> deal;
     const bool work = deal.start(p, blockIdx.x, gridDim.x, sh.sums, sh.found);
     int tree = -1;
     Piece s;
+    Note cut = {-1, 0, 0, 0};
     while (work && deal.take(p, s)) {
         if (s.tree != tree) fill_nodes<kThreads>(p, s.span, sh.nodes, threadIdx.x, [](bool x) { return __syncthreads_or(x); });
         tree = s.tree;
@@ -139,7 +141,8 @@ __global__ void __launch_bounds__(kThreads) tree_kernel(const __grid_constant__ 
             }
         }
         const bool whole = s.from == 0 && s.to == s.span.tiles;
-        float* slot = slot_of<kRows, D>(p, blockIdx.x, s.from == 0);
+        float* slot = slot_of<C, D>(p, gridDim.x, blockIdx.x, s.from == 0);
+        if (s.from == 0 && !whole) cut = {s.tree, s.head, s.block, deal.last_of(s)};
         __syncthreads();
         if (c == 0) {
             sh.factor[r] = l > 0.0f ? 1.0f / l : 0.0f;
@@ -165,7 +168,8 @@ __global__ void __launch_bounds__(kThreads) tree_kernel(const __grid_constant__ 
             }
         }
     }
-    write_zeros<T, kRows, kTile, kThreads>(p);
+    if (threadIdx.x == 0) take_note(p, cut);
+    write_zeros<T, C, kThreads>(p);
 }
 
 // SMs of a device and CTAs of a kernel on one, asked for once.
@@ -190,12 +194,12 @@ cudaError_t resident(int threads, int shared, int& ctas) {
 
 template <typename T, int D>
 cudaError_t launch_d(const TreeParams& p, cudaStream_t s) {
-    constexpr int shared = sizeof(Shared<D>), slices = kRows / (kThreads / (D / 4));
+    constexpr int shared = sizeof(Shared<D>);
     int ctas = 0;
     cudaError_t e = resident<tree_kernel<T, D>>(kThreads, shared, ctas);
     if (e != cudaSuccess) return e;
     e = launch(tree_kernel<T, D>, ctas, kThreads, shared, 0, s, p);
-    return e != cudaSuccess || ctas == 1 ? e : launch_join<T, D, kRows, kTile>(p, ctas, slices, s);
+    return e != cudaSuccess || ctas == 1 ? e : launch_join<T, D, C>(p, ctas, s);
 }
 
 template <typename T>
@@ -207,7 +211,7 @@ cudaError_t launch_t(const TreeParams& p, cudaStream_t s) {
 
 uint64_t tree_workspace(int bf16, int head_dim) {
     if (bf16) return tree_workspace_bf16(head_dim);
-    return sizeof(float) * 2ull * kMaxCtas * slot_floats(kRows, head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256);
+    return sizeof(float) * workspace_floats(kMaxCtas, kRows, head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256);
 }
 
 cudaError_t launch_tree(const Pages& pages, const Trees& trees, const TreeAttend& a, cudaStream_t s) {

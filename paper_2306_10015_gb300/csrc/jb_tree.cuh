@@ -2,9 +2,10 @@
 // work is dealt out, and how parts of one row's attention are joined.
 //
 // The rows of a block are (node, query head of the key head) pairs, nodes first: row r is node r / group. Tiles of
-// positions of all (tree, key head, block of rows) are one line, and every CTA of a persistent grid takes an equal
-// stretch of it, whatever the rows' lengths. Blocks that a boundary cuts leave (weighted values, maximum, sum) in the
-// workspace, which join_kernel adds up in the order of the line: results do not depend on which CTA was first.
+// positions of all (tree, key head, block of rows) are one line, with kCost more for each block, and every CTA of a
+// persistent grid takes an equal stretch of it, whatever the rows' lengths. Blocks that a boundary cuts leave (weighted
+// values, maximum, sum) in the workspace, which join_kernel adds up in the order of the line: results do not depend on
+// which CTA was first.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -19,7 +20,6 @@ namespace {
 constexpr int kGroup = 16;          // pages hold a multiple of so many tokens
 constexpr int kMaskWords = kMaxNodes / 32;
 constexpr int kMaxCtas = 640;       // of the persistent grids; the workspace has two slots for each
-constexpr int kMaxTcCtas = 160;     // of those with a CTA on an SM
 
 }  // namespace
 
@@ -42,7 +42,13 @@ struct Span {
     int row, first, nodes, base, len, lo, first_tile, tiles, blocks;
 };
 
-template <int kRows, int kTile>
+// kRows rows of a block, kTile positions of a tile, the cost of a block in tiles.
+template <int kRows_, int kTile_, int kCost_>
+struct Cut {
+    static constexpr int kRows = kRows_, kTile = kTile_, kCost = kCost_;
+};
+
+template <typename C>
 __device__ __forceinline__ Span span_of(const TreeParams& p, int i) {
     Span s;
     s.row = p.trees.rows[i];
@@ -57,16 +63,16 @@ __device__ __forceinline__ Span span_of(const TreeParams& p, int i) {
     s.len = len;
     s.base = len - s.nodes;
     if (p.a.window > 0) s.lo = max(0, s.base - p.a.window + 1);  // what a root sees
-    s.first_tile = s.lo / kTile;
-    s.tiles = (s.len - 1) / kTile + 1 - s.first_tile;
-    s.blocks = (s.nodes * p.a.group + kRows - 1) / kRows;  // group is at most 65536
+    s.first_tile = s.lo / C::kTile;
+    s.tiles = (s.len - 1) / C::kTile + 1 - s.first_tile;
+    s.blocks = (s.nodes * p.a.group + C::kRows - 1) / C::kRows;  // group is at most 65536
     return s;
 }
 
-// Tiles [from, to) of a block of rows of a tree's key head.
+// Tiles [from, to) of a block of rows of a tree's key head, at least one.
 struct Piece {
     int tree, head, block, from, to;
-    long long begin;  // where the block's tiles start on the line
+    long long begin;  // where the block starts on the line
     Span span;
 };
 
@@ -109,77 +115,85 @@ __device__ __forceinline__ long long before_thread(long long v, long long* sums,
 }
 
 // Deals a CTA's stretch of the line out in pieces.
-template <int kRows, int kTile, int kThreads>
+template <typename C, int kThreads>
 struct Dealer {
-    long long next, end, at;  // at: tiles of the tree before `next`
+    long long next, end, at;  // at: the tree's part of the line before `next`
     Line line;
     int tree;
     Span span;
 
+    // What a tree takes of the line.
+    static __device__ long long cost_of(const TreeParams& p, const Span& s) {
+        return s.tiles == 0 ? 0 : static_cast<long long>(s.tiles + C::kCost) * s.blocks * p.a.heads;
+    }
+    static __device__ long long cost_of(const TreeParams& p, int i) { return i < p.trees.n ? cost_of(p, span_of<C>(p, i)) : 0; }
+
     // The CTA together; kThreads of them. False: the CTA has nothing to do. found: two words of shared memory.
     __device__ bool start(const TreeParams& p, int worker, int ctas, long long* sums, long long* found) {
-        long long total = 0;
+        long long total = 0, here = 0, mine = 0, before = 0;
+        const bool few = p.trees.n <= kThreads;
         for (int first = 0; first < p.trees.n; first += kThreads) {
-            long long here;
-            before_thread<kThreads>(tiles_of(p, first + static_cast<int>(threadIdx.x)), sums, here);
+            mine = cost_of(p, first + static_cast<int>(threadIdx.x));
+            before = before_thread<kThreads>(mine, sums, here);
             total += here;
         }
         line.total = total;
-        line.workers = static_cast<int>(min(static_cast<long long>(ctas), max(1ll, total)));
+        line.workers = static_cast<int>(min(static_cast<long long>(ctas), max(1ll, total / (C::kCost + 1))));
         line.each = quotient(total, line.workers);
         line.extra = static_cast<int>(total - line.each * line.workers);
         next = end = 0;
         if (worker >= line.workers || total == 0) return false;
         next = line.bound(worker);
         end = line.bound(worker + 1);
-        seek(p, next, sums, found);
-        return true;
-    }
-    static __device__ long long tiles_of(const TreeParams& p, int i) {
-        if (i >= p.trees.n) return 0;
-        const Span s = span_of<kRows, kTile>(p, i);
-        return static_cast<long long>(s.tiles) * s.blocks * p.a.heads;
-    }
-    // The tree with tile x of the line. The CTA together.
-    __device__ void seek(const TreeParams& p, long long x, long long* sums, long long* found) {
-        long long base = 0;
-        for (int first = 0; first < p.trees.n; first += kThreads) {
-            const int i = first + static_cast<int>(threadIdx.x);
-            const long long mine = tiles_of(p, i);
-            long long here;
-            const long long before = base + before_thread<kThreads>(mine, sums, here);
-            if (before <= x && x < before + mine) {
+        // the tree with the place `next`
+        const auto look = [&](int i) {
+            if (before <= next && next < before + mine) {
                 found[0] = i;
                 found[1] = before;
             }
-            base += here;
-            if (x < base) break;  // the same for all threads
+        };
+        if (few) {
+            look(threadIdx.x);
+        } else {
+            long long base = 0;
+            for (int first = 0; base <= next; first += kThreads, base += here) {
+                mine = cost_of(p, first + static_cast<int>(threadIdx.x));
+                before = base + before_thread<kThreads>(mine, sums, here);
+                look(first + threadIdx.x);
+            }
         }
         __syncthreads();
         tree = static_cast<int>(found[0]);
-        at = x - found[1];
-        span = span_of<kRows, kTile>(p, tree);
-        __syncthreads();
-    }
-    __device__ bool take(const TreeParams& p, Piece& s) {
-        if (next >= end) return false;
-        while (at >= static_cast<long long>(span.tiles) * span.blocks * p.a.heads) {
-            at -= static_cast<long long>(span.tiles) * span.blocks * p.a.heads;
-            ++tree;
-            span = span_of<kRows, kTile>(p, tree);
-        }
-        s.tree = tree;
-        s.span = span;
-        const int pair = static_cast<int>(quotient(at, span.tiles));
-        s.head = pair / span.blocks;
-        s.block = pair - s.head * span.blocks;
-        s.from = static_cast<int>(at - static_cast<long long>(pair) * span.tiles);
-        s.to = static_cast<int>(min(static_cast<long long>(span.tiles), s.from + (end - next)));
-        s.begin = next - s.from;
-        next += s.to - s.from;
-        at += s.to - s.from;
+        at = next - found[1];
+        span = span_of<C>(p, tree);
         return true;
     }
+    __device__ bool take(const TreeParams& p, Piece& s) {
+        while (next < end) {
+            while (at >= cost_of(p, span)) {
+                at -= cost_of(p, span);
+                ++tree;
+                span = span_of<C>(p, tree);
+            }
+            const int cost = span.tiles + C::kCost, pair = static_cast<int>(quotient(at, cost));
+            const int from = static_cast<int>(at - static_cast<long long>(pair) * cost);
+            const int to = static_cast<int>(min(static_cast<long long>(cost), from + (end - next)));
+            s.begin = next - from;
+            next += to - from;
+            at += to - from;
+            if (to <= C::kCost) continue;  // none of its tiles
+            s.tree = tree;
+            s.span = span;
+            s.head = pair / span.blocks;
+            s.block = pair - s.head * span.blocks;
+            s.from = max(0, from - C::kCost);
+            s.to = to - C::kCost;
+            return true;
+        }
+        return false;
+    }
+    // The CTA with the block's last tile.
+    __device__ int last_of(const Piece& s) const { return line.owner(s.begin + s.span.tiles + C::kCost - 1); }
 };
 
 // Who sees whom in a tree: depth of each node (-1: its chain of parents is not valid, and it sees nothing), and of its
@@ -273,12 +287,12 @@ template <>
 __device__ __forceinline__ void store_out<__nv_bfloat16>(__nv_bfloat16* to, float v) { *to = __float2bfloat16_rn(v); }
 
 // Zeros for the queries of trees that are not valid.
-template <typename T, int kRows, int kTile, int kThreads>
+template <typename T, typename C, int kThreads>
 __device__ __forceinline__ void write_zeros(const TreeParams& p) {
     const int d = p.a.head_dim;
     const long long values = static_cast<long long>(p.a.heads) * p.a.group * d;
     for (int i = blockIdx.x; i < p.trees.n; i += gridDim.x) {
-        const Span s = span_of<kRows, kTile>(p, i);
+        const Span s = span_of<C>(p, i);
         if (s.tiles > 0) continue;
         for (int j = 0; j < s.nodes; ++j)
             for (long long u = threadIdx.x; u < values; u += kThreads)
@@ -286,64 +300,76 @@ __device__ __forceinline__ void write_zeros(const TreeParams& p) {
     }
 }
 
-// Partial results: o[rows][D], m[rows], l[rows]. The first part of a block is in its CTA's slot 1, the others in their
+// The workspace: a note of each CTA, the block that it is the first to have a part of and not the last (tree -1: none);
+// then partial results, o[rows][D], m[rows], l[rows]. The first part of a block is in its CTA's slot 1, the others in their
 // CTAs' slots 0, so that the end of one block and the start of the next do not meet.
+struct Note {
+    int tree, head, block, last;
+};
 __host__ __device__ constexpr size_t slot_floats(int rows, int d) { return static_cast<size_t>(rows) * (d + 2); }
-template <int kRows, int D>
-__device__ __forceinline__ float* slot_of(const TreeParams& p, int worker, bool first) {
-    return p.a.ws + slot_floats(kRows, D) * (2 * static_cast<size_t>(worker) + (first ? 1 : 0));
+__host__ __device__ constexpr size_t workspace_floats(int ctas, int rows, int d) { return ctas * (sizeof(Note) / 4 + 2 * slot_floats(rows, d)); }
+template <typename C, int D>
+__device__ __forceinline__ float* slot_of(const TreeParams& p, int ctas, int worker, bool first) {
+    return p.a.ws + ctas * (sizeof(Note) / 4) + slot_floats(C::kRows, D) * (2 * static_cast<size_t>(worker) + (first ? 1 : 0));
 }
+__device__ __forceinline__ void take_note(const TreeParams& p, const Note& n) { reinterpret_cast<Note*>(p.a.ws)[blockIdx.x] = n; }
 
-// CTA (b - 1, slice) joins a slice of the rows of the block that boundary b is the first to cut.
-template <typename T, int D, int kRows, int kTile>
-__global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ TreeParams p, int ctas) {
-    constexpr int kThreads = 128, kQuads = D / 4, kAt = kThreads / kQuads;  // rows at a time
-    __shared__ long long sums[kThreads / 32], found[2];
+// CTA (b, slice) joins a slice of the rows of the block that CTA b has the first part of. A thread adds up four values of
+// every part, four parts at a time so that the loads do not wait for one another.
+template <typename T, int D, typename C>
+__global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ TreeParams p) {
+    constexpr int kThreads = 128, kQuads = D / 4, kAt = kThreads / kQuads, kAhead = 4;  // rows at a time; parts
+    constexpr int kRows = C::kRows;
     after_previous();
     let_next_start();
-    Dealer<kRows, kTile, kThreads> deal;
-    const int b = blockIdx.x + 1;
-    if (!deal.start(p, b, ctas, sums, found)) return;
-    const long long x = deal.next;
-    Piece s;
-    deal.take(p, s);
-    if (s.begin == x || s.begin < deal.line.bound(b - 1)) return;  // no cut, or an earlier boundary's
-    const int last = deal.line.owner(s.begin + s.span.tiles - 1), quad = threadIdx.x % kQuads;
-    const int row = blockIdx.y * kAt + threadIdx.x / kQuads, all = s.block * kRows + row;
-    if (threadIdx.x >= kAt * kQuads || row >= kRows || all >= s.span.nodes * p.a.group) return;
+    const Note n = reinterpret_cast<const Note*>(p.a.ws)[blockIdx.x];
+    if (n.tree < 0) return;
+    const int first = p.trees.starts[n.tree], nodes = p.trees.starts[n.tree + 1] - first, quad = threadIdx.x % kQuads;
+    const int row = blockIdx.y * kAt + threadIdx.x / kQuads, all = n.block * kRows + row;
+    if (threadIdx.x >= kAt * kQuads || row >= kRows || all >= nodes * p.a.group || 4 * quad >= p.a.head_dim) return;
     float m = kLowest, l = 0.0f;
     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int w = b - 1; w <= last; ++w) {
-        const float* slot = slot_of<kRows, D>(p, w, w == b - 1);
-        const float mw = __ldcg(slot + kRows * D + row), lw = __ldcg(slot + kRows * D + kRows + row);
-        const float4 ow = __ldcg(reinterpret_cast<const float4*>(slot + row * D) + quad);
-        const float top = fmaxf(m, mw), f = exp2_approx(m - top), g = exp2_approx(mw - top);
-        l = fmaf(g, lw, l * f);
-        o = make_float4(fmaf(g, ow.x, o.x * f), fmaf(g, ow.y, o.y * f), fmaf(g, ow.z, o.z * f), fmaf(g, ow.w, o.w * f));
-        m = top;
+    const int b = blockIdx.x;
+    for (int w = b; w <= n.last; w += kAhead) {
+        float mw[kAhead], lw[kAhead];
+        float4 ow[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const float* slot = slot_of<C, D>(p, gridDim.x, min(w + k, n.last), w + k == b);
+            mw[k] = w + k <= n.last ? __ldcg(slot + kRows * D + row) : kLowest;
+            lw[k] = w + k <= n.last ? __ldcg(slot + kRows * D + kRows + row) : 0.0f;
+            ow[k] = w + k <= n.last ? __ldcg(reinterpret_cast<const float4*>(slot + row * D) + quad) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const float top = fmaxf(m, mw[k]), f = exp2_approx(m - top), g = exp2_approx(mw[k] - top);
+            l = fmaf(g, lw[k], l * f);
+            o = make_float4(fmaf(g, ow[k].x, o.x * f), fmaf(g, ow[k].y, o.y * f), fmaf(g, ow[k].z, o.z * f), fmaf(g, ow[k].w, o.w * f));
+            m = top;
+        }
     }
-    if (4 * quad >= p.a.head_dim) return;
     const float inverse = l > 0.0f ? 1.0f / l : 0.0f;
     const int node = all / p.a.group, h = all - node * p.a.group;
-    T* out = reinterpret_cast<T*>(p.a.out) + (s.span.first + node) * p.a.out_row + (s.head * p.a.group + h) * p.a.out_head + 4 * quad;
+    T* out = reinterpret_cast<T*>(p.a.out) + (first + node) * p.a.out_row + (n.head * p.a.group + h) * p.a.out_head + 4 * quad;
     store_out(out, o.x * inverse);
     store_out(out + 1, o.y * inverse);
     store_out(out + 2, o.z * inverse);
     store_out(out + 3, o.w * inverse);
 }
 
-template <typename T, int D, int kRows, int kTile>
-cudaError_t launch_join(const TreeParams& p, int ctas, int slices, cudaStream_t s) {
+template <typename T, int D, typename C>
+cudaError_t launch_join(const TreeParams& p, int ctas, cudaStream_t s) {
+    constexpr int kAt = 128 / (D / 4);
     cudaLaunchConfig_t c = {};
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
-    c.gridDim = dim3(ctas - 1, slices);
+    c.gridDim = dim3(ctas, (C::kRows + kAt - 1) / kAt);
     c.blockDim = dim3(128);
     c.stream = s;
     c.attrs = &attr;
     c.numAttrs = 1;
-    return cudaLaunchKernelEx(&c, join_kernel<T, D, kRows, kTile>, p, ctas);
+    return cudaLaunchKernelEx(&c, join_kernel<T, D, C>, p);
 }
 
 }  // namespace

@@ -1,20 +1,19 @@
 // jb_tree_bf16.cu -- jb_attend_tree on the tensor cores, for bf16 caches.
 //
 // A block of 128 rows (node, query head of the key head) is one tile of tcgen05.mma, and its row's keys and values pass by
-// it once, 128 (heads of up to 128) or 64 positions at a time:
+// it once, 64 positions at a time:
 //   S = Q K^T (fp32, tensor memory), P = exp(S - m), O = O + P V (fp32, tensor memory)
 // with the maximum m of the softmax kept as it was until a row exceeds it by 2^8; only then is O multiplied. Weights enter
 // the second product as two bf16 numbers, 16 bits of them.
 //
-// Roles of a CTA, one on an SM: a warp copies keys and values (TMA, boxes of a page's tokens, any page size and layout)
-// into swizzled tiles; two warps copy queries and look after values that some rows do not see; one thread issues the
-// products; eight warps take scores from tensor memory and put weights in their place, so that of three score tiles one is
-// being multiplied, one worked on and one its values' operand. A row has two threads, each with half of a tile's positions
-// and half of the sums; they exchange the maximum.
+// Roles of a CTA, two on an SM (one with heads of more than 128): a warp copies keys and values (TMA, boxes of a page's
+// tokens, any page size and layout) into swizzled tiles; two warps copy queries and look after values that some rows do not
+// see; a warp issues the products; four warps, a thread a row, take scores from tensor memory and put weights in their place.
+// The two CTAs' waits fill one another.
 //
-// Loops are kept short, not unrolled: a warp that runs alone through code that is longer than its instruction cache waits
-// for instructions (64 positions of a thread unrolled: 8000 cycles a tile). Nor is cp.async for keys and values: a warp
-// issued one in 170 cycles, 10000 for a tile's.
+// Loops are kept short: a warp that runs alone through code that is longer than its instruction cache waits for
+// instructions (128 positions of a thread unrolled: 8000 cycles for as many positions). Nor is cp.async for keys and
+// values: a warp issued one in 170 cycles, 10000 for 128 positions.
 #include <atomic>
 #include <numeric>
 
@@ -30,25 +29,27 @@ namespace {
 using T = __nv_bfloat16;
 
 constexpr unsigned kAll = 0xFFFFFFFFu;
-constexpr int kRows = 128;
-constexpr int kSoftmaxWarps = 8, kHelpWarps = 2;
+constexpr int kRows = 128, kTile = 64;
+using C = Cut<kRows, kTile, 2>;
+constexpr int kSoftmaxWarps = 4, kHelpWarps = 2;
 constexpr int kThreads = 32 * (kSoftmaxWarps + 2 + kHelpWarps);
 constexpr int kHelpThreads = 32 * kHelpWarps;
-constexpr int kScoreTiles = 3;
-constexpr uint32_t kColumns = 512;   // of tensor memory
+constexpr int kScoreTiles = 2;
 constexpr float kSlack = 8.0f;       // how far a row may exceed its maximum before sums are scaled, in powers of two
+using Deal = Dealer<C, kThreads>;
 
 // What a score goes through on its way to the softmax.
 enum Scores { kPlain, kCapped, kBiased };  // a positive scale alone; a cap; a bias, with or without a cap, or any scale
 
 template <int D>
 struct Shape {
-    static constexpr int kTile = D == 256 ? 64 : 128;
+    static constexpr int kCtas = D == 256 ? 1 : 2;     // on an SM
     static constexpr int kSlots = D == 64 ? 8 : 4;
-    static constexpr int kQueries = D == 256 ? 1 : 2;  // blocks of queries that there is room for
+    static constexpr int kQueries = D == 64 ? 2 : 1;   // blocks of queries that there is room for
     static constexpr uint32_t kTileBytes = kTile * D * 2, kQueryBytes = kRows * D * 2;
     static constexpr uint32_t kPanel = kTile * 128, kQueryPanel = kRows * 128;  // 64 elements of all rows
     static constexpr uint32_t kSums = kScoreTiles * kTile;                      // column of O
+    static constexpr uint32_t kColumns = D == 256 ? 512 : 256;                  // of tensor memory
     static constexpr int kShared = 1024 + kQueries * kQueryBytes + kSlots * kTileBytes;
     static_assert(kSums + D <= kColumns && kSlots % 2 == 0);  // even: values are always in odd slots
 };
@@ -65,7 +66,6 @@ struct Control {
     int failed;
     int not_finite;          // a value that some rows see and others do not was not finite, in some tile so far
     unsigned missing[8];     // groups of a tile whose page is missing; copies are at most five tiles ahead of the softmax
-    float high[2][2][kRows]; // maxima of tiles, by the tile's parity and the half of its positions
 };
 
 // Whether some of the positions [t, t + n) are seen by some nodes and not by others.
@@ -82,9 +82,9 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 // Keys and values of the blocks' tiles, in the order in which they are needed. Lane i copies box i of a tile: `box` groups of
 // 64 elements.
 template <int D>
-__device__ void copy_role(const TcParams& tc, Dealer<kRows, Shape<D>::kTile, kThreads> deal, Control& c, uint32_t ring) {
+__device__ void copy_role(const TcParams& tc, Deal deal, Control& c, uint32_t ring) {
     using S = Shape<D>;
-    constexpr int kGroups = S::kTile / kGroup, kPanels = D / 64;
+    constexpr int kGroups = kTile / kGroup, kPanels = D / 64;
     const TreeParams& p = tc.t;
     const int lane = threadIdx.x & 31, panel = lane % kPanels, group = lane / kPanels * tc.box;  // group: of the tile
     const bool mine = group < kGroups && 64 * panel < p.a.head_dim;
@@ -129,7 +129,7 @@ __device__ void copy_role(const TcParams& tc, Dealer<kRows, Shape<D>::kTile, kTh
                 if (lane == 0) {
                     barrier_arrive_bytes(shared_address(&c.full[slot]), bytes);
                     if (kind == 1) {
-                        if (edge_of(p, s.span, tile * S::kTile, S::kTile)) barrier_arrive(shared_address(&c.edges[edges++ % 8]));
+                        if (edge_of(p, s.span, tile * kTile, kTile)) barrier_arrive(shared_address(&c.edges[edges++ % 8]));
                         else barrier_arrive_count(shared_address(&c.clean[slot]), kHelpWarps);
                     }
                 }
@@ -178,9 +178,9 @@ __device__ bool clean_values(uint32_t tile, int lo, int hi) {
     const int u = threadIdx.x - 32 * (kSoftmaxWarps + 2);
     bool bad = false;
 #pragma unroll 2
-    for (int i = u; i < S::kTile * (D / 8); i += kHelpThreads) {
+    for (int i = u; i < kTile * (D / 8); i += kHelpThreads) {
         const uint32_t at = tile + i * 16;
-        const int row = i / 8 % S::kTile;
+        const int row = i / 8 % kTile;
         uint32_t w[4], any = 0;
         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
         const bool inside = row >= lo && row < hi;
@@ -197,7 +197,7 @@ __device__ bool clean_values(uint32_t tile, int lo, int hi) {
 }
 
 template <int D>
-__device__ void help_role(const TreeParams& p, Dealer<kRows, Shape<D>::kTile, kThreads> deal, Control& c, uint32_t queries, uint32_t ring) {
+__device__ void help_role(const TreeParams& p, Deal deal, Control& c, uint32_t queries, uint32_t ring) {
     using S = Shape<D>;
     const int lane = threadIdx.x & 31;
     uint32_t blocks = 0, tiles = 0, edges = 0;
@@ -221,12 +221,12 @@ __device__ void help_role(const TreeParams& p, Dealer<kRows, Shape<D>::kTile, kT
         more = deal.take(p, next);
         if (S::kQueries > 1 && more && !block(next)) return;
         for (int tile = s.span.first_tile + s.from; tile < s.span.first_tile + s.to; ++tile, ++tiles) {
-            if (!edge_of(p, s.span, tile * S::kTile, S::kTile)) continue;
+            if (!edge_of(p, s.span, tile * kTile, kTile)) continue;
             const uint32_t i = 2 * tiles + 1, slot = i % S::kSlots, e = edges++;
             // first that its copy has begun: the slot's own phase may be any before that
             if (!__all_sync(kAll, barrier_wait(shared_address(&c.edges[e % 8]), e / 8 & 1, &c.failed))) return;
             if (!__all_sync(kAll, barrier_wait(shared_address(&c.full[slot]), i / S::kSlots & 1, &c.failed))) return;
-            if (clean_values<D>(ring + slot * S::kTileBytes, s.span.lo - tile * S::kTile, s.span.len - tile * S::kTile))
+            if (clean_values<D>(ring + slot * S::kTileBytes, s.span.lo - tile * kTile, s.span.len - tile * kTile))
                 *static_cast<volatile int*>(&c.not_finite) = 1;
             tell(&c.clean[slot]);
         }
@@ -237,133 +237,175 @@ __device__ void help_role(const TreeParams& p, Dealer<kRows, Shape<D>::kTile, kT
 }
 
 template <int D>
-__device__ void product_role(const TreeParams& p, Dealer<kRows, Shape<D>::kTile, kThreads> deal, Control& c, uint32_t queries, uint32_t ring) {
+__device__ void product_role(const TreeParams& p, Deal deal, Control& c, uint32_t queries, uint32_t ring) {
     using S = Shape<D>;
-    constexpr int kTile = S::kTile;
     const int steps = (p.a.head_dim + 15) / 16;
-    constexpr uint32_t kScores = product_descriptor(kTile, false);
+    constexpr uint32_t scores = product_descriptor(kTile, false);
     const uint32_t values = product_descriptor(16 * steps, true);
     const uint32_t tmem = c.tmem;
     uint32_t tiles = 0, blocks = 0;  // so far
+    // The whole warp runs this and one lane issues: operands are then the warp's, which products want them to be.
+    const auto wait = [&](unsigned long long* bar, uint32_t parity) {
+        const bool ok = __all_sync(kAll, barrier_wait(shared_address(bar), parity, &c.failed));
+        tc_fence_after();
+        return ok;
+    };
     const auto scores_of = [&](uint32_t tile, bool last) {
         const uint32_t i = 2 * tile, b = blocks % S::kQueries;
-        if (!barrier_wait(shared_address(&c.full[i % S::kSlots]), i / S::kSlots & 1, &c.failed)) return false;
-        tc_fence_after();
-        const uint32_t k = ring + i % S::kSlots * S::kTileBytes, q = queries + b * S::kQueryBytes;
-#pragma unroll 2
-        for (int e = 0; e < steps; ++e)
-            tc_product(tmem + tile % kScoreTiles * kTile, tile_descriptor(q + e / 4 * S::kQueryPanel + e % 4 * 32, 16),
-                       tile_descriptor(k + e / 4 * S::kPanel + e % 4 * 32, 16), kScores, e > 0);
-        tc_commit(shared_address(&c.empty[i % S::kSlots]));
-        tc_commit(shared_address(&c.scores[tile % kScoreTiles]));
-        if (last) tc_commit(shared_address(&c.queries_read[b]));
+        if (!wait(&c.full[i % S::kSlots], i / S::kSlots & 1)) return false;
+        const uint32_t k = tile_descriptor(ring + i % S::kSlots * S::kTileBytes, 16), q = tile_descriptor(queries + b * S::kQueryBytes, 16);
+        const uint32_t to = tmem + tile % kScoreTiles * kTile;
+        if (elected()) {
+#pragma unroll
+            for (int e = 0; e < D / 16; ++e)
+                if (e < steps)
+                    tc_product(to, q + ((e / 4 * S::kQueryPanel + e % 4 * 32) >> 4), k + ((e / 4 * S::kPanel + e % 4 * 32) >> 4), scores, e > 0);
+            tc_commit(shared_address(&c.empty[i % S::kSlots]));
+            tc_commit(shared_address(&c.scores[tile % kScoreTiles]));
+            if (last) tc_commit(shared_address(&c.queries_read[b]));
+        }
+        __syncwarp();
         return true;
     };
     Piece s;
     for (; deal.take(p, s); ++blocks) {
         const uint32_t n = s.to - s.from;
-        if (!barrier_wait(shared_address(&c.queries[blocks % S::kQueries]), blocks / S::kQueries & 1, &c.failed)) return;
-        tc_fence_after();
+        if (!wait(&c.queries[blocks % S::kQueries], blocks / S::kQueries & 1)) return;
         if (!scores_of(tiles, n == 1)) return;
         if (n > 1 && !scores_of(tiles + 1, n == 2)) return;
         for (uint32_t j = 0; j < n; ++j, ++tiles) {
             const uint32_t i = 2 * tiles + 1, buffer = tiles % kScoreTiles;
-            if (!barrier_wait(shared_address(&c.weights[buffer]), tiles / kScoreTiles & 1, &c.failed)) return;
-            if (!barrier_wait(shared_address(&c.full[i % S::kSlots]), i / S::kSlots & 1, &c.failed)) return;
-            if (!barrier_wait(shared_address(&c.clean[i % S::kSlots]), i / S::kSlots & 1, &c.failed)) return;
-            tc_fence_after();
-            const uint32_t v = ring + i % S::kSlots * S::kTileBytes, w = tmem + buffer * kTile;
-#pragma unroll 1
-            for (int half = 0; half < 2; ++half)  // the weights' upper and lower bits
-#pragma unroll 2
-                for (int e = 0; e < kTile / 16; ++e)
-                    tc_product_from_tmem(tmem + S::kSums, w + e / 2 * 32 + half * 16 + e % 2 * 8, tile_descriptor(v + e * 2048, S::kPanel), values,
-                                         j > 0 || half > 0 || e > 0);
-            tc_commit(shared_address(&c.empty[i % S::kSlots]));
-            tc_commit(shared_address(&c.sums));
-            if (j + 2 < n && !scores_of(tiles + 2, j + 3 == n)) return;
+            if (!wait(&c.weights[buffer], tiles / kScoreTiles & 1)) return;
+            if (!wait(&c.full[i % S::kSlots], i / S::kSlots & 1)) return;
+            if (!wait(&c.clean[i % S::kSlots], i / S::kSlots & 1)) return;
+            const uint32_t v = tile_descriptor(ring + i % S::kSlots * S::kTileBytes, S::kPanel), w = tmem + buffer * kTile;
+            if (elected()) {
+#pragma unroll
+                for (int half = 0; half < 2; ++half)  // the weights' upper and lower bits
+#pragma unroll
+                    for (int e = 0; e < kTile / 16; ++e)
+                        tc_product_from_tmem(tmem + S::kSums, w + e / 2 * 32 + half * 16 + e % 2 * 8, v + (e * 2048 >> 4), values, half > 0 || e > 0 || j > 0);
+                tc_commit(shared_address(&c.empty[i % S::kSlots]));
+                tc_commit(shared_address(&c.sums));
+            }
+            __syncwarp();
+            if (j + 2 < n) {  // where this tile's weights were
+                if (!wait(&c.sums, tiles & 1) || !scores_of(tiles + 2, j + 3 == n)) return;
+            }
         }
     }
 }
 
-// A barrier of `threads` threads, true if x is in one of them.
-template <int kThreadsHere>
-__device__ __forceinline__ bool any_of(uint32_t id, bool x) {
+// A barrier of the softmax warps, true if x is in one of their threads.
+__device__ __forceinline__ bool any_of(bool x) {
     uint32_t any;
-    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.or.pred p, %2, %3, q;\n selp.u32 %0, 1, 0, p;\n}"
-                 : "=r"(any) : "r"(static_cast<uint32_t>(x)), "r"(id), "n"(kThreadsHere) : "memory");
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.or.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(any) : "r"(static_cast<uint32_t>(x)), "n"(32 * kSoftmaxWarps) : "memory");
     return any != 0;
 }
-__device__ __forceinline__ void pair_barrier(uint32_t id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
+
+// Adds to o, 32 elements of a row's sums from element e on, the values that were taken out and that the row sees.
+__device__ __noinline__ void put_back(const TreeParams& p, const Piece& s, int depth, const unsigned* mask, int e, uint32_t* o) {
+    const int* table = p.pages.table + static_cast<size_t>(s.span.row) * p.pages.row_pages;
+    for (int tile = s.span.first_tile + s.from; tile < s.span.first_tile + s.to; ++tile) {
+        if (!edge_of(p, s.span, tile * kTile, kTile)) continue;
+        for (int k = 0; k < kTile; k += 32)
+            for (unsigned seen = seen_of(p, s.span, depth, mask, tile * kTile + k); seen != 0; seen &= seen - 1) {
+                const int t = tile * kTile + k + __ffs(seen) - 1, page = table[t / p.pages.page_tokens];
+                if (page < 0 || page >= p.pages.n_pages) continue;
+                const T* v = reinterpret_cast<const T*>(p.a.v) + page * p.a.page_stride + s.head * p.a.head_stride + t % p.pages.page_tokens * p.a.token_stride + e;
+                for (int i = 0; i < 32 && e + i < p.a.head_dim; ++i) {
+                    const float x = __bfloat162float(v[i]);
+                    if (!isfinite(x)) o[i] = __float_as_uint(__uint_as_float(o[i]) + x);
+                }
+            }
+    }
+}
 
 template <int D, Scores kScores>
-__device__ void softmax_role(const TreeParams& p, Dealer<kRows, Shape<D>::kTile, kThreads> deal, Control& c, Nodes& nodes) {
+__device__ void softmax_role(const TreeParams& p, Deal deal, Control& c, Nodes& nodes) {
     using S = Shape<D>;
-    constexpr int kTile = S::kTile, kMine = kTile / 2;  // positions of a thread
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = warp >> 2, row = threadIdx.x & 127, d = p.a.head_dim;
-    const uint32_t pair = 2 + (warp & 3);  // barrier of the two warps with the same rows
-    const uint32_t tmem = c.tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = threadIdx.x, d = p.a.head_dim;
+    const uint32_t tmem = c.tmem + (static_cast<uint32_t>(32 * warp) << 16);
     const float by = kScores == kPlain ? p.a.scale * kLog2e : 1.0f;
     uint32_t tiles = 0;
     int tree = -1;
     bool ok = true;  // a wait that gives up leaves the loops as they are: other warps may wait for this one
     Piece s;
+    Note cut = {-1, 0, 0, 0};
     while (deal.take(p, s)) {
-        if (s.tree != tree)
-            fill_nodes<32 * kSoftmaxWarps>(p, s.span, nodes, threadIdx.x, [](bool x) { return any_of<32 * kSoftmaxWarps>(1, x); });
+        if (s.tree != tree) fill_nodes<32 * kSoftmaxWarps>(p, s.span, nodes, threadIdx.x, any_of);
         tree = s.tree;
         const int rows = s.span.nodes * p.a.group, all = s.block * kRows + row;
-        const bool real = all < rows, idle = s.block * kRows + 32 * (warp & 3) >= rows;  // idle: none of the warp's rows is real
+        const bool real = all < rows, idle = s.block * kRows + 32 * warp >= rows;  // idle: none of the warp's rows is real
         const int node = real ? all / p.a.group : 0, h = real ? all - node * p.a.group : 0, depth = real ? nodes.depth[node] : -1;
         const float slope = kScores == kBiased && real && p.a.slopes != nullptr ? p.a.slopes[s.head * p.a.group + h] * kLog2e : 0.0f;
         float m = kLowest, offset = 0.0f, l = 0.0f;  // offset: what is subtracted from scores, in powers of two; 0 before one is seen
         for (int tile = s.span.first_tile + s.from; tile < s.span.first_tile + s.to; ++tile, ++tiles) {
-            const int t0 = tile * kTile + half * kMine;
-            const uint32_t buffer = tiles % kScoreTiles, at = tmem + buffer * kTile + half * kMine;
+            const int t0 = tile * kTile;
+            const uint32_t buffer = tiles % kScoreTiles, at = tmem + buffer * kTile;
             ok = barrier_wait(shared_address(&c.scores[buffer]), tiles / kScoreTiles & 1, &c.failed) && ok;
             tc_fence_after();
             if (!idle) {
-                const unsigned missing = *static_cast<volatile unsigned*>(&c.missing[tiles % 8]) >> (half * kMine / kGroup);
-                const bool edge = missing != 0 || edge_of(p, s.span, tile * kTile, kTile);
-                float high = kLowest;
-                if (kScores == kPlain && !edge) {
+                const unsigned missing = *static_cast<volatile unsigned*>(&c.missing[tiles % 8]);
+                const bool edge = missing != 0 || edge_of(p, s.span, t0, kTile);
+                if (kScores != kPlain) {  // scores are put back as the softmax takes them
 #pragma unroll 1
-                    for (int k = 0; k < kMine; k += 32) {
-                        uint32_t raw[32];
-                        tmem_load32(at + k, raw);
-                        tc_wait_loads();
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) high = fmaxf(high, __uint_as_float(raw[e]));
-                    }
-                } else {
-#pragma unroll 1
-                    for (int k = 0; k < kMine; k += 16) {
+                    for (int k = 0; k < kTile; k += 16) {
                         uint32_t raw[16];
                         tmem_load16(at + k, raw);
-                        unsigned seen = edge && !(missing >> (k / kGroup) & 1u) ? seen_of(p, s.span, depth, nodes.mask[node], t0 + k) : edge ? 0 : kAll;
                         tc_wait_loads();
+                        if constexpr (kScores == kCapped) {
+                            float most = 0.0f;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            float x = __uint_as_float(raw[e]);
-                            const bool sees = seen >> e & 1u;
-                            if constexpr (kScores == kCapped) x = capped(p, x);
-                            if constexpr (kScores == kBiased) {
+                            for (int e = 0; e < 16; ++e) most = fmaxf(most, fabsf(__uint_as_float(raw[e])));
+                            if (__all_sync(kAll, most * fabsf(p.cap_in) < kSmallCap)) {
+#pragma unroll
+                                for (int e = 0; e < 16; e += 2) {
+                                    const float2 x = capped_small(p, make_float2(__uint_as_float(raw[e]), __uint_as_float(raw[e + 1])));
+                                    raw[e] = __float_as_uint(x.x);
+                                    raw[e + 1] = __float_as_uint(x.y);
+                                }
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) raw[e] = __float_as_uint(capped(p, __uint_as_float(raw[e])));
+                            }
+                        } else {
+                            const unsigned seen = edge ? seen_of(p, s.span, depth, nodes.mask[node], t0 + k) : kAll;
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
                                 const int t = t0 + k + e;
                                 int back = t - s.span.base - depth;
-                                if (edge && sees && t >= s.span.base) back = nodes.depth[t - s.span.base] - depth;
-                                x = score<true>(p, x, slope, back);
+                                if (t >= s.span.base && (seen >> e & 1u)) back = nodes.depth[t - s.span.base] - depth;
+                                raw[e] = __float_as_uint(score<true>(p, __uint_as_float(raw[e]), slope, back));
                             }
-                            if (!sees) x = -INFINITY;
-                            raw[e] = __float_as_uint(x);
-                            high = fmaxf(high, x);
                         }
                         tmem_store16(at + k, raw);
                     }
                     tc_wait_stores();
                 }
-                c.high[tiles & 1][half][row] = high;
-                pair_barrier(pair);
-                high = fmaxf(high, c.high[tiles & 1][half ^ 1][row]);
+                uint32_t raw[kTile];
+#pragma unroll
+                for (int k = 0; k < kTile; k += 32) tmem_load32(at + k, raw + k);
+                tc_wait_loads();
+                if (edge) {
+#pragma unroll
+                    for (int k = 0; k < kTile; k += 32) {
+                        unsigned seen = seen_of(p, s.span, depth, nodes.mask[node], t0 + k);
+                        if (missing >> (k / kGroup) & 1u) seen &= 0xFFFF0000u;
+                        if (missing >> (k / kGroup + 1) & 1u) seen &= 0x0000FFFFu;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (!(seen >> e & 1u)) raw[k + e] = __float_as_uint(-INFINITY);
+                    }
+                }
+                float tops[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) tops[k] = __uint_as_float(raw[k]);
+#pragma unroll
+                for (int k = 8; k < kTile; ++k) tops[k % 8] = fmaxf(tops[k % 8], __uint_as_float(raw[k]));
+                float high = fmaxf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), fmaxf(fmaxf(tops[4], tops[5]), fmaxf(tops[6], tops[7])));
+                high = fmaxf(high, kLowest);
                 const bool rises = high > m && (m == kLowest || (high - m) * by > kSlack);
                 if (__any_sync(kAll, rises)) {
                     float k = 1.0f;
@@ -378,26 +420,24 @@ __device__ void softmax_role(const TreeParams& p, Dealer<kRows, Shape<D>::kTile,
                         ok = barrier_wait(shared_address(&c.sums), (tiles - 1) & 1, &c.failed) && ok;
                         tc_fence_after();
 #pragma unroll 1
-                        for (int e = half * (D / 2); e < (half + 1) * (D / 2); e += 32) {
-                            uint32_t o[32];
-                            tmem_load32(tmem + S::kSums + e, o);
+                        for (int e = 0; e < D; e += 16) {
+                            uint32_t o[16];
+                            tmem_load16(tmem + S::kSums + e, o);
                             tc_wait_loads();
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * k);
-                            tmem_store32(tmem + S::kSums + e, o);
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * k);
+                            tmem_store16(tmem + S::kSums + e, o);
                         }
                     }
                 }
                 float2 part[2] = {};
                 const float2 by2 = make_float2(by, by), less = make_float2(-offset, -offset);
-#pragma unroll 1
-                for (int k = 0; k < kMine; k += 32) {
-                    uint32_t raw[32], w[32];  // upper bits of 32 weights, then lower bits
-                    tmem_load32(at + k, raw);
-                    tc_wait_loads();
+#pragma unroll
+                for (int k = 0; k < kTile; k += 32) {
+                    uint32_t w[32];  // upper bits of 32 weights, then lower bits
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        float2 x = __ffma2_rn(make_float2(__uint_as_float(raw[2 * e]), __uint_as_float(raw[2 * e + 1])), by2, less);
+                        float2 x = __ffma2_rn(make_float2(__uint_as_float(raw[k + 2 * e]), __uint_as_float(raw[k + 2 * e + 1])), by2, less);
                         x.x = exp2_approx(x.x);
                         x.y = exp2_approx(x.y);
                         part[e & 1] = __fadd2_rn(part[e & 1], x);
@@ -410,25 +450,20 @@ __device__ void softmax_role(const TreeParams& p, Dealer<kRows, Shape<D>::kTile,
                 l += (part[0].x + part[0].y) + (part[1].x + part[1].y);
                 tc_wait_stores();
             }
-            // The product of the tile before this one is done before this one's may start: so its weights' place is free
-            // for the scores after next, and no wait is two phases of its barrier away from what it waits for.
+            // The product of the tile before this one is done before this one's may start: so no wait is two phases of
+            // its barrier away from what it waits for.
             if (tiles > 0) ok = barrier_wait(shared_address(&c.sums), (tiles - 1) & 1, &c.failed) && ok;
             tc_fence_before();
             __syncwarp();
             if (lane == 0) barrier_arrive(shared_address(&c.weights[buffer]));
         }
-        if (!idle) {  // the row's sum of weights; this tile's place of maxima was last read a tile ago
-            c.high[tiles & 1][half][row] = l;
-            pair_barrier(pair);
-            l += c.high[tiles & 1][half ^ 1][row];
-            pair_barrier(pair);
-        }
+        const bool whole = s.from == 0 && s.to == s.span.tiles;
+        if (s.from == 0 && !whole) cut = {s.tree, s.head, s.block, deal.last_of(s)};
         ok = barrier_wait(shared_address(&c.sums), (tiles - 1) & 1, &c.failed) && ok;
         tc_fence_after();
         if (idle) continue;
-        const bool whole = s.from == 0 && s.to == s.span.tiles;
-        float* slot = slot_of<kRows, D>(p, blockIdx.x, s.from == 0);
-        if (!whole && real && half == 0) {
+        float* slot = slot_of<C, D>(p, gridDim.x, blockIdx.x, s.from == 0);
+        if (!whole && real) {
             slot[kRows * D + row] = m == kLowest || depth < 0 ? kLowest : offset;
             slot[kRows * D + kRows + row] = depth < 0 ? 0.0f : l;
         }
@@ -436,28 +471,18 @@ __device__ void softmax_role(const TreeParams& p, Dealer<kRows, Shape<D>::kTile,
         const bool mend = *static_cast<volatile int*>(&c.not_finite) != 0;
         T* out = reinterpret_cast<T*>(p.a.out) + (s.span.first + node) * p.a.out_row + (s.head * p.a.group + h) * p.a.out_head;
 #pragma unroll 1
-        for (int e = half * (D / 2); e < (half + 1) * (D / 2); e += 32) {
+        for (int e = 0; e < D; e += 32) {
             uint32_t o[32];
             tmem_load32(tmem + S::kSums + e, o);
             tc_wait_loads();  // every lane's loads, also of lanes whose row is not real
             if (!real || e >= d) continue;
-            if (mend) {  // values that were taken out
-                const int* table = p.pages.table + static_cast<size_t>(s.span.row) * p.pages.row_pages;
-                for (int tile = s.span.first_tile + s.from; tile < s.span.first_tile + s.to; ++tile) {
-                    if (!edge_of(p, s.span, tile * kTile, kTile)) continue;
-                    for (int k = 0; k < kTile; k += 32)
-                        for (unsigned seen = seen_of(p, s.span, depth, nodes.mask[node], tile * kTile + k); seen != 0; seen &= seen - 1) {
-                            const int t = tile * kTile + k + __ffs(seen) - 1, page = table[t / p.pages.page_tokens];
-                            if (page < 0 || page >= p.pages.n_pages) continue;
-                            const T* v = reinterpret_cast<const T*>(p.a.v) + page * p.a.page_stride + s.head * p.a.head_stride + t % p.pages.page_tokens * p.a.token_stride + e;
+            if (mend) {
+                uint32_t copy[32];
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) {
-                                if (e + i >= d) continue;
-                                const float x = __bfloat162float(v[i]);
-                                if (!isfinite(x)) o[i] = __float_as_uint(__uint_as_float(o[i]) + x);
-                            }
-                        }
-                }
+                for (int i = 0; i < 32; ++i) copy[i] = o[i];
+                put_back(p, s, depth, nodes.mask[node], e, copy);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = copy[i];
             }
 #pragma unroll
             for (int i = 0; i < 32; i += 8) {
@@ -474,10 +499,11 @@ __device__ void softmax_role(const TreeParams& p, Dealer<kRows, Shape<D>::kTile,
         }
         tc_fence_before();
     }
+    if (threadIdx.x == 0) take_note(p, cut);
 }
 
 template <int D, Scores kScores>
-__global__ void __launch_bounds__(kThreads, 1) tree_bf16_kernel(const __grid_constant__ TcParams tc) {
+__global__ void __launch_bounds__(kThreads, Shape<D>::kCtas) tree_bf16_kernel(const __grid_constant__ TcParams tc) {
     using S = Shape<D>;
     const TreeParams& p = tc.t;
     extern __shared__ char dynamic[];
@@ -506,19 +532,19 @@ __global__ void __launch_bounds__(kThreads, 1) tree_bf16_kernel(const __grid_con
         c.failed = c.not_finite = 0;
         barriers_initialized();
     }
-    if (warp == kSoftmaxWarps) tmem_alloc(shared_address(&c.tmem), kColumns);
+    if (warp == kSoftmaxWarps) tmem_alloc(shared_address(&c.tmem), S::kColumns);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     after_previous();
     let_next_start();
-    Dealer<kRows, S::kTile, kThreads> deal;
+    Deal deal;
     if (deal.start(p, blockIdx.x, gridDim.x, sums, found)) {
         if (warp < kSoftmaxWarps) {
             softmax_role<D, kScores>(p, deal, c, nodes);
         } else if (warp == kSoftmaxWarps) {
+            product_role<D>(p, deal, c, queries, ring);
             if ((threadIdx.x & 31) == 0) {
-                product_role<D>(p, deal, c, queries, ring);
                 if (*static_cast<volatile int*>(&c.failed)) {  // what is under way ends before tensor memory is given back
                     int late = 0;
                     tc_commit(shared_address(&c.drained));
@@ -531,18 +557,20 @@ __global__ void __launch_bounds__(kThreads, 1) tree_bf16_kernel(const __grid_con
         } else {
             help_role<D>(p, deal, c, queries, ring);
         }
+    } else if (threadIdx.x == 0) {
+        take_note(p, {-1, 0, 0, 0});
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == kSoftmaxWarps) tmem_free(c.tmem, kColumns);
-    write_zeros<T, kRows, S::kTile, kThreads>(p);
+    if (warp == kSoftmaxWarps) tmem_free(c.tmem, S::kColumns);
+    write_zeros<T, C, kThreads>(p);
 }
 
 // SMs of a device, asked for once, and the kernel's share of shared memory set.
 constexpr int kDevices = 64;
 template <auto kKernel>
-cudaError_t resident(int shared, int& ctas) {
+cudaError_t resident(int shared, int each, int most, int& ctas) {
     static std::atomic<int> known[kDevices];
     int device = 0, sms = 0;
     cudaError_t e = cudaGetDevice(&device);
@@ -552,10 +580,13 @@ cudaError_t resident(int shared, int& ctas) {
     e = cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
     if (e != cudaSuccess) return e;
-    ctas = sms < kMaxTcCtas ? sms : kMaxTcCtas;
+    ctas = sms * each < most ? sms * each : most;
     if (device < kDevices) known[device].store(ctas, std::memory_order_relaxed);
     return cudaSuccess;
 }
+
+template <int D>
+constexpr int max_ctas() { return 160 * Shape<D>::kCtas; }
 
 using Encode = decltype(&cuTensorMapEncodeTiled);
 
@@ -590,17 +621,16 @@ cudaError_t describe(CUtensorMap& map, const TreeParams& p, const char* pool, in
 
 template <int D, Scores kScores>
 cudaError_t launch_scores(const TreeParams& p, cudaStream_t s) {
-    constexpr int slices = kRows / (128 / (D / 4));
     int ctas = 0;
-    cudaError_t e = resident<tree_bf16_kernel<D, kScores>>(Shape<D>::kShared, ctas);
+    cudaError_t e = resident<tree_bf16_kernel<D, kScores>>(Shape<D>::kShared, Shape<D>::kCtas, max_ctas<D>(), ctas);
     if (e != cudaSuccess) return e;
     TcParams tc;
     tc.t = p;
-    tc.box = std::gcd(p.page_groups, Shape<D>::kTile / kGroup);
+    tc.box = std::gcd(p.page_groups, kTile / kGroup);
     e = describe(tc.keys, p, p.a.k, tc.box);
     if (e == cudaSuccess) e = describe(tc.values, p, p.a.v, tc.box);
     if (e == cudaSuccess) e = launch(tree_bf16_kernel<D, kScores>, ctas, kThreads, Shape<D>::kShared, 0, s, tc);
-    return e != cudaSuccess || ctas == 1 ? e : launch_join<T, D, kRows, Shape<D>::kTile>(p, ctas, slices, s);
+    return e != cudaSuccess || ctas == 1 ? e : launch_join<T, D, C>(p, ctas, s);
 }
 
 template <int D>
@@ -612,7 +642,10 @@ cudaError_t launch_d(const TreeParams& p, cudaStream_t s) {
 }  // namespace
 
 uint64_t tree_workspace_bf16(int head_dim) {
-    return sizeof(float) * 2ull * kMaxTcCtas * slot_floats(kRows, head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256);
+    const size_t floats = head_dim <= 64    ? workspace_floats(max_ctas<64>(), kRows, 64)
+                          : head_dim <= 128 ? workspace_floats(max_ctas<128>(), kRows, 128)
+                                            : workspace_floats(max_ctas<256>(), kRows, 256);
+    return sizeof(float) * floats;
 }
 
 cudaError_t launch_tree_bf16(const TreeParams& p, cudaStream_t s) {
