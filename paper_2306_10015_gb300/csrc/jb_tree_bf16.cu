@@ -284,7 +284,7 @@ __device__ void product_role(const TreeParams& p, Deal deal, Control& c, uint32_
                 for (int half = 0; half < 2; ++half)  // the weights' upper and lower bits
 #pragma unroll
                     for (int e = 0; e < kTile / 16; ++e)
-                        tc_product_from_tmem(tmem + S::kSums, w + e / 2 * 32 + half * 16 + e % 2 * 8, v + (e * 2048 >> 4), values, half > 0 || e > 0 || j > 0);
+                        tc_product_from_tmem(tmem + S::kSums, w + e * 16 + half * 8, v + (e * 2048 >> 4), values, half > 0 || e > 0 || j > 0);
                 tc_commit(shared_address(&c.empty[i % S::kSlots]));
                 tc_commit(shared_address(&c.sums));
             }
@@ -349,11 +349,12 @@ __device__ void softmax_role(const TreeParams& p, Deal deal, Control& c, Nodes& 
             if (!idle) {
                 const unsigned missing = *static_cast<volatile unsigned*>(&c.missing[tiles % 8]);
                 const bool edge = missing != 0 || edge_of(p, s.span, t0, kTile);
-                if (kScores != kPlain) {  // scores are put back as the softmax takes them
+                if (kScores != kPlain || edge) {  // scores are put back as the softmax takes them
 #pragma unroll 1
                     for (int k = 0; k < kTile; k += 16) {
                         uint32_t raw[16];
                         tmem_load16(at + k, raw);
+                        const unsigned seen = !edge ? kAll : missing >> (k / kGroup) & 1u ? 0u : seen_of(p, s.span, depth, nodes.mask[node], t0 + k);
                         tc_wait_loads();
                         if constexpr (kScores == kCapped) {
                             float most = 0.0f;
@@ -370,8 +371,8 @@ __device__ void softmax_role(const TreeParams& p, Deal deal, Control& c, Nodes& 
 #pragma unroll
                                 for (int e = 0; e < 16; ++e) raw[e] = __float_as_uint(capped(p, __uint_as_float(raw[e])));
                             }
-                        } else {
-                            const unsigned seen = edge ? seen_of(p, s.span, depth, nodes.mask[node], t0 + k) : kAll;
+                        }
+                        if constexpr (kScores == kBiased) {
 #pragma unroll
                             for (int e = 0; e < 16; ++e) {
                                 const int t = t0 + k + e;
@@ -380,32 +381,27 @@ __device__ void softmax_role(const TreeParams& p, Deal deal, Control& c, Nodes& 
                                 raw[e] = __float_as_uint(score<true>(p, __uint_as_float(raw[e]), slope, back));
                             }
                         }
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (!(seen >> e & 1u)) raw[e] = __float_as_uint(-INFINITY);
                         tmem_store16(at + k, raw);
                     }
                     tc_wait_stores();
                 }
-                uint32_t raw[kTile];
+                float high;
+                {
+                    uint32_t raw[kTile];
 #pragma unroll
-                for (int k = 0; k < kTile; k += 32) tmem_load32(at + k, raw + k);
-                tc_wait_loads();
-                if (edge) {
+                    for (int k = 0; k < kTile; k += 32) tmem_load32(at + k, raw + k);
+                    tc_wait_loads();
+                    float tops[8];
 #pragma unroll
-                    for (int k = 0; k < kTile; k += 32) {
-                        unsigned seen = seen_of(p, s.span, depth, nodes.mask[node], t0 + k);
-                        if (missing >> (k / kGroup) & 1u) seen &= 0xFFFF0000u;
-                        if (missing >> (k / kGroup + 1) & 1u) seen &= 0x0000FFFFu;
+                    for (int k = 0; k < 8; ++k) tops[k] = __uint_as_float(raw[k]);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (!(seen >> e & 1u)) raw[k + e] = __float_as_uint(-INFINITY);
-                    }
+                    for (int k = 8; k < kTile; ++k) tops[k % 8] = fmaxf(tops[k % 8], __uint_as_float(raw[k]));
+                    high = fmaxf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), fmaxf(fmaxf(tops[4], tops[5]), fmaxf(tops[6], tops[7])));
+                    high = fmaxf(high, kLowest);
                 }
-                float tops[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) tops[k] = __uint_as_float(raw[k]);
-#pragma unroll
-                for (int k = 8; k < kTile; ++k) tops[k % 8] = fmaxf(tops[k % 8], __uint_as_float(raw[k]));
-                float high = fmaxf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), fmaxf(fmaxf(tops[4], tops[5]), fmaxf(tops[6], tops[7])));
-                high = fmaxf(high, kLowest);
                 const bool rises = high > m && (m == kLowest || (high - m) * by > kSlack);
                 if (__any_sync(kAll, rises)) {
                     float k = 1.0f;
@@ -432,20 +428,24 @@ __device__ void softmax_role(const TreeParams& p, Deal deal, Control& c, Nodes& 
                 }
                 float2 part[2] = {};
                 const float2 by2 = make_float2(by, by), less = make_float2(-offset, -offset);
+                uint32_t raw[16];
+                tmem_load16(at, raw);
+#pragma unroll 1
+                for (int k = 0; k < kTile; k += 16) {
+                    uint32_t w[16];  // upper bits of 16 weights, then lower bits
+                    tc_wait_loads();
 #pragma unroll
-                for (int k = 0; k < kTile; k += 32) {
-                    uint32_t w[32];  // upper bits of 32 weights, then lower bits
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        float2 x = __ffma2_rn(make_float2(__uint_as_float(raw[k + 2 * e]), __uint_as_float(raw[k + 2 * e + 1])), by2, less);
+                    for (int e = 0; e < 8; ++e) {
+                        float2 x = __ffma2_rn(make_float2(__uint_as_float(raw[2 * e]), __uint_as_float(raw[2 * e + 1])), by2, less);
                         x.x = exp2_approx(x.x);
                         x.y = exp2_approx(x.y);
                         part[e & 1] = __fadd2_rn(part[e & 1], x);
                         w[e] = pack_bf16(x.x, x.y);
                         const float2 rest = __fadd2_rn(x, make_float2(-__uint_as_float(w[e] << 16), -__uint_as_float(w[e] & 0xFFFF0000u)));
-                        w[16 + e] = pack_bf16(rest.x, rest.y);
+                        w[8 + e] = pack_bf16(rest.x, rest.y);
                     }
-                    tmem_store32(at + k, w);
+                    if (k + 16 < kTile) tmem_load16(at + k + 16, raw);
+                    tmem_store16(at + k, w);
                 }
                 l += (part[0].x + part[0].y) + (part[1].x + part[1].y);
                 tc_wait_stores();
