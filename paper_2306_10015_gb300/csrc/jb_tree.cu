@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(kThreads) tree_kernel(const __grid_constant__ 
                 *reinterpret_cast<float4*>(&sh.k[u / kQuads][e]) = k;
                 *reinterpret_cast<float4*>(&sh.v[u / kQuads][e]) = v;
             }
-            unsigned seen = seen_of(p, s.span, depth, sh.nodes.mask[node], t0);
+            unsigned seen = seen_of(p, s.span, sh.nodes, node, depth, t0);
 #pragma unroll
             for (int g = 0; g < kTile; g += kGroup) {  // a missing page is not seen
                 const int page = t0 + g < s.span.len ? table[(t0 + g) / p.pages.page_tokens] : -1;

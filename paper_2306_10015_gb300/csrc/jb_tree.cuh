@@ -199,7 +199,7 @@ struct Dealer {
 // Who sees whom in a tree: depth of each node (-1: its chain of parents is not valid, and it sees nothing), and of its
 // ancestors and itself those within the window, as bits.
 struct Nodes {
-    unsigned mask[kMaxNodes][kMaskWords];
+    unsigned mask[kMaskWords][kMaxNodes];
     int depth[kMaxNodes];
     short jump[kMaxNodes];
 };
@@ -209,6 +209,7 @@ struct Nodes {
 template <int kThreads, typename Any>
 __device__ __forceinline__ void fill_nodes(const TreeParams& p, const Span& s, Nodes& t, int rank, Any any) {
     constexpr int kBad = 1 << 20, kEach = (kMaxNodes + kThreads - 1) / kThreads;
+    const int words = (s.nodes + 31) / 32;
     bool more = false;
     any(false);  // nobody reads the last tree's any more
     for (int j = rank; j < s.nodes; j += kThreads) {
@@ -216,7 +217,7 @@ __device__ __forceinline__ void fill_nodes(const TreeParams& p, const Span& s, N
         const bool inner = up >= 0 && up < j;
         t.jump[j] = static_cast<short>(inner ? up : -1);
         t.depth[j] = inner ? 1 : up == -1 ? 0 : kBad;
-        for (int w = 0; w < kMaskWords; ++w) t.mask[j][w] = w == j >> 5 ? 1u << (j & 31) : 0;
+        for (int w = 0; w < kMaskWords; ++w) t.mask[w][j] = w == j >> 5 ? 1u << (j & 31) : 0;
         more = more || inner;
     }
     while (any(more)) {  // at most 8 rounds: a chain has at most 255 steps
@@ -229,7 +230,9 @@ __device__ __forceinline__ void fill_nodes(const TreeParams& p, const Span& s, N
             if (up < 0) continue;
             depth[e] = min(t.depth[j] + t.depth[up], kBad);
             jump[e] = t.jump[up];
-            for (int w = 0; w < kMaskWords; ++w) mask[e][w] = t.mask[j][w] | t.mask[up][w];
+#pragma unroll
+            for (int w = 0; w < kMaskWords; ++w)
+                if (w < words) mask[e][w] = t.mask[w][j] | t.mask[w][up];
         }
         any(false);
         more = false;
@@ -239,7 +242,9 @@ __device__ __forceinline__ void fill_nodes(const TreeParams& p, const Span& s, N
             if (j >= s.nodes || t.jump[j] < 0) continue;
             t.depth[j] = depth[e];
             t.jump[j] = static_cast<short>(jump[e]);
-            for (int w = 0; w < kMaskWords; ++w) t.mask[j][w] = mask[e][w];
+#pragma unroll
+            for (int w = 0; w < kMaskWords; ++w)
+                if (w < words) t.mask[w][j] = mask[e][w];
             more = more || jump[e] >= 0;
         }
     }
@@ -249,9 +254,9 @@ __device__ __forceinline__ void fill_nodes(const TreeParams& p, const Span& s, N
         if (valid && from < 0) continue;
         for (int w = 0; w < kMaskWords; ++w) {
             unsigned keep = 0;
-            for (unsigned m = valid ? t.mask[j][w] : 0; m != 0; m &= m - 1)
+            for (unsigned m = valid ? t.mask[w][j] : 0; m != 0; m &= m - 1)
                 if (t.depth[32 * w + __ffs(m) - 1] > from) keep |= m & -m;
-            t.mask[j][w] = keep;
+            t.mask[w][j] = keep;
         }
     }
     any(false);
@@ -267,16 +272,16 @@ __device__ __forceinline__ unsigned between(int t, int lo, int hi) {
     return (b == 32 ? 0xFFFFFFFFu : (1u << b) - 1u) & ~((1u << a) - 1u);
 }
 
-// Which of the 32 positions from t on a node of this depth and mask sees.
-__device__ __forceinline__ unsigned seen_of(const TreeParams& p, const Span& s, int depth, const unsigned* mask, int t) {
+// Which of the 32 positions from t on a node of this depth sees.
+__device__ __forceinline__ unsigned seen_of(const TreeParams& p, const Span& s, const Nodes& nodes, int node, int depth, int t) {
     if (depth < 0) return 0;
     const int lo = p.a.window > 0 ? max(0, min(s.base, s.base + depth - p.a.window + 1)) : 0;
     unsigned bits = between(t, lo, s.base);
     const int off = t - s.base;
     if (off <= -32 || off >= kMaxNodes) return bits;
-    if (off < 0) return bits | mask[0] << -off;
+    if (off < 0) return bits | nodes.mask[0][node] << -off;
     const int w = off >> 5;
-    return bits | __funnelshift_r(mask[w], w + 1 < kMaskWords ? mask[w + 1] : 0u, off & 31);
+    return bits | __funnelshift_r(nodes.mask[w][node], w + 1 < kMaskWords ? nodes.mask[w + 1][node] : 0u, off & 31);
 }
 
 template <typename T>

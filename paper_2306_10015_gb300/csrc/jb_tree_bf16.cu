@@ -305,12 +305,12 @@ __device__ __forceinline__ bool any_of(bool x) {
 }
 
 // Adds to o, 32 elements of a row's sums from element e on, the values that were taken out and that the row sees.
-__device__ __noinline__ void put_back(const TreeParams& p, const Piece& s, int depth, const unsigned* mask, int e, uint32_t* o) {
+__device__ __noinline__ void put_back(const TreeParams& p, const Piece& s, const Nodes& nodes, int node, int depth, int e, uint32_t* o) {
     const int* table = p.pages.table + static_cast<size_t>(s.span.row) * p.pages.row_pages;
     for (int tile = s.span.first_tile + s.from; tile < s.span.first_tile + s.to; ++tile) {
         if (!edge_of(p, s.span, tile * kTile, kTile)) continue;
         for (int k = 0; k < kTile; k += 32)
-            for (unsigned seen = seen_of(p, s.span, depth, mask, tile * kTile + k); seen != 0; seen &= seen - 1) {
+            for (unsigned seen = seen_of(p, s.span, nodes, node, depth, tile * kTile + k); seen != 0; seen &= seen - 1) {
                 const int t = tile * kTile + k + __ffs(seen) - 1, page = table[t / p.pages.page_tokens];
                 if (page < 0 || page >= p.pages.n_pages) continue;
                 const T* v = reinterpret_cast<const T*>(p.a.v) + page * p.a.page_stride + s.head * p.a.head_stride + t % p.pages.page_tokens * p.a.token_stride + e;
@@ -349,12 +349,23 @@ __device__ void softmax_role(const TreeParams& p, Deal deal, Control& c, Nodes& 
             if (!idle) {
                 const unsigned missing = *static_cast<volatile unsigned*>(&c.missing[tiles % 8]);
                 const bool edge = missing != 0 || edge_of(p, s.span, t0, kTile);
+                float tops[4] = {kLowest, kLowest, kLowest, kLowest};
                 if (kScores != kPlain || edge) {  // scores are put back as the softmax takes them
+                    unsigned seen[2] = {kAll, kAll};
+                    if (edge) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            seen[i] = seen_of(p, s.span, nodes, node, depth, t0 + 32 * i);
+                            if (missing >> (2 * i) & 1u) seen[i] &= 0xFFFF0000u;
+                            if (missing >> (2 * i + 1) & 1u) seen[i] &= 0x0000FFFFu;
+                        }
+                    }
+                    uint32_t raw[16];
+                    tmem_load16(at, raw);
 #pragma unroll 1
                     for (int k = 0; k < kTile; k += 16) {
-                        uint32_t raw[16];
-                        tmem_load16(at + k, raw);
-                        const unsigned seen = !edge ? kAll : missing >> (k / kGroup) & 1u ? 0u : seen_of(p, s.span, depth, nodes.mask[node], t0 + k);
+                        const unsigned sees = seen[k >> 5] >> (k & 16);
+                        uint32_t x[16];
                         tc_wait_loads();
                         if constexpr (kScores == kCapped) {
                             float most = 0.0f;
@@ -363,45 +374,44 @@ __device__ void softmax_role(const TreeParams& p, Deal deal, Control& c, Nodes& 
                             if (__all_sync(kAll, most * fabsf(p.cap_in) < kSmallCap)) {
 #pragma unroll
                                 for (int e = 0; e < 16; e += 2) {
-                                    const float2 x = capped_small(p, make_float2(__uint_as_float(raw[e]), __uint_as_float(raw[e + 1])));
-                                    raw[e] = __float_as_uint(x.x);
-                                    raw[e + 1] = __float_as_uint(x.y);
+                                    const float2 y = capped_small(p, make_float2(__uint_as_float(raw[e]), __uint_as_float(raw[e + 1])));
+                                    x[e] = __float_as_uint(y.x);
+                                    x[e + 1] = __float_as_uint(y.y);
                                 }
                             } else {
 #pragma unroll
-                                for (int e = 0; e < 16; ++e) raw[e] = __float_as_uint(capped(p, __uint_as_float(raw[e])));
+                                for (int e = 0; e < 16; ++e) x[e] = __float_as_uint(capped(p, __uint_as_float(raw[e])));
                             }
-                        }
-                        if constexpr (kScores == kBiased) {
+                        } else if constexpr (kScores == kBiased) {
 #pragma unroll
                             for (int e = 0; e < 16; ++e) {
                                 const int t = t0 + k + e;
                                 int back = t - s.span.base - depth;
-                                if (t >= s.span.base && (seen >> e & 1u)) back = nodes.depth[t - s.span.base] - depth;
-                                raw[e] = __float_as_uint(score<true>(p, __uint_as_float(raw[e]), slope, back));
+                                if (t >= s.span.base && (sees >> e & 1u)) back = nodes.depth[t - s.span.base] - depth;
+                                x[e] = __float_as_uint(score<true>(p, __uint_as_float(raw[e]), slope, back));
                             }
-                        }
+                        } else {
 #pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            if (!(seen >> e & 1u)) raw[e] = __float_as_uint(-INFINITY);
-                        tmem_store16(at + k, raw);
+                            for (int e = 0; e < 16; ++e) x[e] = raw[e];
+                        }
+                        if (k + 16 < kTile) tmem_load16(at + k + 16, raw);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            if (!(sees >> e & 1u)) x[e] = __float_as_uint(-INFINITY);
+                            tops[e % 4] = fmaxf(tops[e % 4], __uint_as_float(x[e]));
+                        }
+                        tmem_store16(at + k, x);
                     }
                     tc_wait_stores();
-                }
-                float high;
-                {
+                } else {
                     uint32_t raw[kTile];
 #pragma unroll
                     for (int k = 0; k < kTile; k += 32) tmem_load32(at + k, raw + k);
                     tc_wait_loads();
-                    float tops[8];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) tops[k] = __uint_as_float(raw[k]);
-#pragma unroll
-                    for (int k = 8; k < kTile; ++k) tops[k % 8] = fmaxf(tops[k % 8], __uint_as_float(raw[k]));
-                    high = fmaxf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), fmaxf(fmaxf(tops[4], tops[5]), fmaxf(tops[6], tops[7])));
-                    high = fmaxf(high, kLowest);
+                    for (int k = 0; k < kTile; ++k) tops[k % 4] = fmaxf(tops[k % 4], __uint_as_float(raw[k]));
                 }
+                const float high = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
                 const bool rises = high > m && (m == kLowest || (high - m) * by > kSlack);
                 if (__any_sync(kAll, rises)) {
                     float k = 1.0f;
@@ -480,7 +490,7 @@ __device__ void softmax_role(const TreeParams& p, Deal deal, Control& c, Nodes& 
                 uint32_t copy[32];
 #pragma unroll
                 for (int i = 0; i < 32; ++i) copy[i] = o[i];
-                put_back(p, s, depth, nodes.mask[node], e, copy);
+                put_back(p, s, nodes, node, depth, e, copy);
 #pragma unroll
                 for (int i = 0; i < 32; ++i) o[i] = copy[i];
             }
