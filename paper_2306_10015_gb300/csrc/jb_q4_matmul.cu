@@ -1,6 +1,26 @@
 // jb_q4_matmul.cu -- products of a few rows with a matrix of 4-bit weights (the format of jb_perturb_q4):
 //   y[i][o] = sum_k x[i][k] level[code[o][k]] scale[o][k / 64] + bias[o]
+//
+// The weights are read once, 4.5 bits each, and that bounds it while turning codes into numbers keeps up: a byte is a pair
+// of codes, and a table in shared memory with a copy for each lane (no bank conflicts) has the pair's two levels as two fp16,
+// which is how mma.m16n8k16 takes them. So 16 rows of the matrix by 64 columns, a block each, are 16 table reads a lane and
+// four products with up to 8 rows of x; tokens are the product's columns.
+//
+// Numbers. fp16 has 11 bits: a level is off by at most 2^-12, beside the 2^-9 of a bf16 result. bf16 inputs fit fp16 with
+// all their bits once they are scaled by a power of two, chosen for each row and 512 columns so that the largest is near
+// 2^15 (what is 2^-28 of it or smaller loses bits, 2^-40 of it is lost). fp32: levels and inputs are two fp16 each, 22 bits
+// and more; the inputs' two parts are two columns of the product, and a table read is two words (the product of two lower
+// parts, 2^-24, is left out). A block's sum is fp32 and
+// meets its scale once; sums over blocks, warps and CTAs are fp32, in an order that does not depend on the launch's timing.
+//
+// A CTA of 16 warps has a slice of the columns, whose inputs it keeps in shared memory, and takes tiles of 16 rows: warps
+// split the slice, and their sums are joined in shared memory. Where the inputs of all columns do not fit, a cluster of CTAs
+// has a slice each and their sums are joined through distributed shared memory.
+#include <atomic>
+
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 
 #include "jb_draft.h"
 #include "jb_internal.h"
@@ -9,54 +29,399 @@
 namespace jb {
 namespace {
 
-constexpr int kMatThreads = 256;
+namespace cg = cooperative_groups;
+
+constexpr int kMatWarps = 16, kMatThreads = 32 * kMatWarps;
+constexpr int kScaled = 512;        // columns that share a power of two
+constexpr int kPad = 8;             // halves between rows of inputs: reads of 8 rows meet no bank twice
+constexpr int kRed = 20;            // floats from column to column of a tile's sums, for the same reason
+constexpr int kMostColumns = 64;    // of the product at a time
+constexpr float kLevelScale = 1024.0f;  // of fp32's levels, so that their lower parts are normal numbers
 
 struct Params {
     Q4Matmul m;
     float levels[16];
+    int first, rows;     // rows of x in this pass
+    int columns;         // of the product: rows, or twice as many
+    int slice;           // columns of a CTA's slice
+    int ways, at_once;   // warps that split a slice; tiles of 16 rows that a CTA takes at a time
+    int kept;            // tiles whose sums a CTA keeps until the cluster joins them
 };
 
-__device__ __forceinline__ float value(const float* p) { return *p; }
-__device__ __forceinline__ float value(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+// Shared memory, in bytes: table, powers of two, inputs, warps' sums, kept sums.
+struct Layout {
+    int powers, inputs, sums, kept, all;
+};
+__host__ __device__ inline int round16(int x) { return (x + 15) & ~15; }
+__host__ __device__ inline Layout layout_of(bool f32, int columns, int slice, int out_columns, int kept) {
+    Layout l;
+    l.powers = f32 ? 65536 : 32768;
+    l.inputs = l.powers + round16((slice + kScaled - 1) / kScaled * ((columns + 7) / 8 * 8) * 4);
+    l.sums = l.inputs + round16(columns * (slice + kPad) * 2);
+    l.kept = l.sums + 2 * kMatWarps * out_columns * kRed * 4;
+    l.all = l.kept + kept * out_columns * 16 * 4;
+    return l;
+}
 
-// A warp takes a row of the matrix, a lane 16 codes of it at a time, against 8 rows of x.
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t halves(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// 16 inputs of a row in fp32.
+__device__ __forceinline__ void read16(const float* from, float (&x)[16]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float4 v = reinterpret_cast<const float4*>(from)[i];
+        x[4 * i] = v.x, x[4 * i + 1] = v.y, x[4 * i + 2] = v.z, x[4 * i + 3] = v.w;
+    }
+}
+__device__ __forceinline__ void read16(const __nv_bfloat16* from, float (&x)[16]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint4 v = reinterpret_cast<const uint4*>(from)[i];
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x[8 * i + 2 * e] = __uint_as_float(w[e] << 16);
+            x[8 * i + 2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+        }
+    }
+}
+
+// The slice's inputs as the product takes them, and their powers of two. A warp takes 512 columns of a row.
 template <typename T>
-__global__ void __launch_bounds__(kMatThreads) q4_matmul_kernel(const __grid_constant__ Params p) {
-    __shared__ float levels[16];
-    const Q4Matmul& m = p.m;
-    if (threadIdx.x < 16) levels[threadIdx.x] = p.levels[threadIdx.x];
-    after_previous();
-    let_next_start();
-    __syncthreads();
-    const int o = blockIdx.x * (kMatThreads / 32) + static_cast<int>(threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (o >= m.out) return;
-    const T* x = static_cast<const T*>(m.x);
-    for (int first = 0; first < m.n; first += 8) {
-        float sum[8] = {};
-        for (int k = 16 * lane; k < m.in; k += 512) {
-            const uint64_t at = static_cast<uint64_t>(o) * m.in + k;
-            const uint64_t codes = *reinterpret_cast<const uint64_t*>(m.codes + at / 2);
-            float w[16];
+__device__ void stage(const Params& p, const Layout& l, char* shared, int from) {
+    constexpr bool kF32 = sizeof(T) == 4;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, groups = (p.slice + kScaled - 1) / kScaled, padded = (p.columns + 7) / 8 * 8;
+    float* powers = reinterpret_cast<float*>(shared + l.powers);
+    __half* inputs = reinterpret_cast<__half*>(shared + l.inputs);
+    const T* x = static_cast<const T*>(p.m.x);
+    const int here = min(p.slice, p.m.in - from);
+    for (int u = warp; u < p.rows * groups; u += kMatWarps) {
+        const int row = u / groups, group = u - row * groups, k = group * kScaled + 16 * lane;
+        float v[16];
+        if (k < here) {
+            read16(x + (p.first + row) * p.m.x_row + from + k, v);
+        } else {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) w[e] = levels[codes >> (4 * e) & 15];
-            const float scale = m.scale[at / 64];
-            for (int i = 0; i < 8 && first + i < m.n; ++i) {
-                float part = 0.0f;
-                const T* row = x + (first + i) * m.x_row + k;
+            for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+        }
+        float most = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) part = fmaf(w[e], value(row + e), part);
-                sum[i] = fmaf(part, scale, sum[i]);
+        for (int i = 0; i < 16; ++i) most = fmaxf(most, isfinite(v[i]) ? fabsf(v[i]) : 0.0f);
+#pragma unroll
+        for (int d = 16; d > 0; d /= 2) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
+        // most in [2^e, 2^(e+1)) becomes [2^14, 2^15); powers of two that fp32 has with their inverses
+        const int e = most > 0.0f ? min(max(static_cast<int>(__float_as_uint(most) >> 23) - 127 - 14, -126), 126) : 0;
+        const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23), up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+        if (lane == 0) {
+            if (kF32) {
+                powers[group * padded + 2 * row] = powers[group * padded + 2 * row + 1] = up * (1.0f / kLevelScale);
+            } else {
+                powers[group * padded + row] = up;
             }
         }
+        if (k >= p.slice) continue;
+        uint32_t w[8], r[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            for (int u = 16; u > 0; u /= 2) sum[i] += __shfl_xor_sync(0xFFFFFFFFu, sum[i], u);
-            if (lane != 0 || first + i >= m.n) continue;
-            if (m.bias != nullptr) sum[i] += value(static_cast<const T*>(m.bias) + o);
-            T* y = static_cast<T*>(m.y) + (first + i) * m.y_row + o;
-            if constexpr (sizeof(T) == 4) *y = sum[i];
-            else *y = __float2bfloat16_rn(sum[i]);
+            const float a = v[2 * i] * down, b = v[2 * i + 1] * down;
+            w[i] = halves(a, b);
+            if (kF32) {  // what is not finite is all lower part: the lower parts of levels, which may be 0, do not meet it
+                w[i] = halves(isfinite(a) ? a : 0.0f, isfinite(b) ? b : 0.0f);
+                const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+                r[i] = halves(a - h.x, b - h.y);
+            }
         }
+        __half* to = inputs + (kF32 ? 2 * row : row) * (p.slice + kPad) + k;
+        reinterpret_cast<uint4*>(to)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4*>(to)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+        if (kF32) {
+            to += p.slice + kPad;
+            reinterpret_cast<uint4*>(to)[0] = make_uint4(r[0], r[1], r[2], r[3]);
+            reinterpret_cast<uint4*>(to)[1] = make_uint4(r[4], r[5], r[6], r[7]);
+        }
+    }
+}
+
+// Codes of a block of rows r and r + 8 that a lane takes (16 columns each), and the block's scales.
+struct Codes {
+    uint2 low, high;
+    float low_scale, high_scale;
+};
+
+// kTiles: columns of the product / 8.
+template <typename T, int kTiles>
+__global__ void __launch_bounds__(kMatThreads, 1) q4_matmul_kernel(const __grid_constant__ Params p) {
+    constexpr bool kF32 = sizeof(T) == 4;
+    constexpr int kAhead = kTiles <= 2 ? 6 : 4;                  // blocks whose codes are under way
+    constexpr int kOut = kF32 ? 4 : 8;                           // results of a product's 8 columns
+    extern __shared__ __align__(16) char shared[];
+    const Q4Matmul& m = p.m;
+    const Layout l = layout_of(kF32, p.columns, p.slice, kTiles * kOut, p.kept);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, t = lane & 3;
+    {   // the table: entry of byte b for lane i at (32 b + i) words
+        __shared__ uint32_t pairs[256][kF32 ? 2 : 1];
+        if (threadIdx.x < 256) {
+            const float a = p.levels[threadIdx.x & 15] * (kF32 ? kLevelScale : 1.0f), b = p.levels[threadIdx.x >> 4] * (kF32 ? kLevelScale : 1.0f);
+            const uint32_t w = halves(a, b);
+            pairs[threadIdx.x][0] = w;
+            if (kF32) {
+                const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&w));
+                pairs[threadIdx.x][kF32 ? 1 : 0] = halves(a - h.x, b - h.y);
+            }
+        }
+        __syncthreads();
+        constexpr int kQuads = kF32 ? 16 : 8;  // 16-byte pieces of an entry
+        for (int i = threadIdx.x; i < 256 * kQuads; i += kMatThreads) {
+            const uint32_t w = pairs[i / kQuads][0], v = kF32 ? pairs[i / kQuads][kF32 ? 1 : 0] : w;
+            reinterpret_cast<uint4*>(shared)[i] = make_uint4(w, v, w, v);
+        }
+    }
+    const cg::cluster_group cluster = cg::this_cluster();
+    const int rank = cluster.block_rank(), ranks = cluster.num_blocks();
+    const int from = rank * p.slice, blocks = max(0, min(p.slice, m.in - from)) / 64;
+    after_previous();
+    let_next_start();
+    stage<T>(p, l, shared, from);
+    __syncthreads();
+
+    const int tiles = (m.out + 15) / 16, way = warp % p.ways, mine = warp / p.ways;
+    const int stride = gridDim.x / ranks * p.at_once, first_tile = blockIdx.x / ranks * p.at_once;
+    const int each = (p.slice / 64 + p.ways - 1) / p.ways;               // blocks of a tile for a warp, some of them past its end
+    const int rounds = (tiles - first_tile + stride - 1) / stride;       // the same for all warps of the cluster
+    const int total = rounds * each;
+    const auto fetch = [&](int round, int j) {
+        Codes c;
+        const int tile = first_tile + round * stride + mine, block = way + p.ways * j;
+        const int low = min(tile * 16 + r, m.out - 1), high = min(tile * 16 + r + 8, m.out - 1);
+        const int at = min(block, max(blocks - 1, 0));
+        const uint64_t k = from + 64 * static_cast<uint64_t>(at);
+        if (round < rounds && blocks > 0) {
+            const uint64_t a = static_cast<uint64_t>(low) * m.in + k, b = static_cast<uint64_t>(high) * m.in + k;
+            c.low = __ldcs(reinterpret_cast<const uint2*>(m.codes + a / 2) + t);
+            c.high = __ldcs(reinterpret_cast<const uint2*>(m.codes + b / 2) + t);
+            c.low_scale = __ldcs(m.scale + a / 64);
+            c.high_scale = __ldcs(m.scale + b / 64);
+        }
+        return c;
+    };
+    const char* table = shared + lane * (kF32 ? 8 : 4);
+    const float* powers = reinterpret_cast<const float*>(shared + l.powers);
+    const __half* inputs = reinterpret_cast<const __half*>(shared + l.inputs) + r * (p.slice + kPad) + 16 * t;
+    float* sums = reinterpret_cast<float*>(shared + l.sums);
+    float* kept = reinterpret_cast<float*>(shared + l.kept);
+    const int padded = (p.columns + 7) / 8 * 8, results = kF32 ? p.columns / 2 : p.columns;
+    const T* bias = static_cast<const T*>(m.bias);
+    T* y = static_cast<T*>(m.y) + p.first * m.y_row;
+    const auto store = [&](int tile, int column, int row, float v) {
+        const int o = tile * 16 + row;
+        if (o >= m.out) return;
+        if constexpr (kF32) {
+            if (bias != nullptr) v += bias[o];
+            y[column * m.y_row + o] = v;
+        } else {
+            if (bias != nullptr) v += __bfloat162float(bias[o]);
+            y[column * m.y_row + o] = __float2bfloat16_rn(v);
+        }
+    };
+
+    Codes ring[kAhead];
+    int ahead_round = 0, ahead_j = 0;
+    const auto next = [&]() {
+        const Codes c = fetch(ahead_round, ahead_j);
+        if (++ahead_j == each) {
+            ahead_j = 0;
+            ++ahead_round;
+        }
+        return c;
+    };
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) ring[u] = next();
+    float acc[kTiles][4];
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
+    int round = 0, j = 0, held = 0;  // held: rounds whose sums are kept
+    for (int item = 0; item < total; item += kAhead) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (item + u >= total) break;
+            const int block = way + p.ways * j;
+            if (block < blocks) {
+                const Codes& c = ring[u];
+                const uint32_t codes[4] = {c.low.x, c.low.y, c.high.x, c.high.y};
+                float part[kTiles][4];
+#pragma unroll
+                for (int n = 0; n < kTiles; ++n) part[n][0] = part[n][1] = part[n][2] = part[n][3] = 0.0f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {  // 8 columns of a lane's 16
+                    uint32_t upper[2][4], lower[2][4];  // of two products
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {       // bytes
+                        constexpr int kShift = kF32 ? 8 : 7;
+#pragma unroll
+                        for (int g = 0; g < 2; ++g) {   // rows r and r + 8
+                            const uint32_t w = codes[2 * g + h];
+                            const uint32_t at = (8 * e >= kShift ? w >> (8 * e - kShift) : w << kShift) & (255u << kShift);
+                            if constexpr (kF32) {
+                                const uint2 v = *reinterpret_cast<const uint2*>(table + at);
+                                upper[e / 2][g + e % 2 * 2] = v.x;
+                                lower[e / 2][g + e % 2 * 2] = v.y;
+                            } else {
+                                upper[e / 2][g + e % 2 * 2] = *reinterpret_cast<const uint32_t*>(table + at);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int n = 0; n < kTiles; ++n) {
+                        uint4 b = make_uint4(0, 0, 0, 0);
+                        if (8 * n + r < p.columns) b = *reinterpret_cast<const uint4*>(inputs + 8 * n * (p.slice + kPad) + block * 64 + 8 * h);
+                        mma(part[n], upper[0], b.x, b.y);
+                        mma(part[n], upper[1], b.z, b.w);
+                        if constexpr (kF32) {  // lower parts of levels with upper parts of inputs
+                            if (r & 1) b = make_uint4(0, 0, 0, 0);
+                            mma(part[n], lower[0], b.x, b.y);
+                            mma(part[n], lower[1], b.z, b.w);
+                        }
+                    }
+                }
+                const float* power = powers + block * 64 / kScaled * padded + 2 * t;
+#pragma unroll
+                for (int n = 0; n < kTiles; ++n) {
+                    const float2 f = *reinterpret_cast<const float2*>(power + 8 * n);
+                    acc[n][0] = fmaf(part[n][0], c.low_scale * f.x, acc[n][0]);
+                    acc[n][1] = fmaf(part[n][1], c.low_scale * f.y, acc[n][1]);
+                    acc[n][2] = fmaf(part[n][2], c.high_scale * f.x, acc[n][2]);
+                    acc[n][3] = fmaf(part[n][3], c.high_scale * f.y, acc[n][3]);
+                }
+            }
+            ring[u] = next();
+            if (++j < each) continue;
+            // the tile's sums: each warp's, then all of them in the order of the ways
+            j = 0;
+            float* here = sums + (round & 1) * (kMatWarps * kTiles * kOut * kRed) + warp * (kTiles * kOut * kRed);
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n) {
+                if constexpr (kF32) {
+                    here[(4 * n + t) * kRed + r] = acc[n][0] + acc[n][1];
+                    here[(4 * n + t) * kRed + r + 8] = acc[n][2] + acc[n][3];
+                } else {
+                    here[(8 * n + 2 * t) * kRed + r] = acc[n][0];
+                    here[(8 * n + 2 * t + 1) * kRed + r] = acc[n][1];
+                    here[(8 * n + 2 * t) * kRed + r + 8] = acc[n][2];
+                    here[(8 * n + 2 * t + 1) * kRed + r + 8] = acc[n][3];
+                }
+                acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
+            }
+            if (p.ways == 1) __syncwarp();
+            else asm volatile("bar.sync %0, %1;" ::"r"(1 + mine), "r"(32 * p.ways) : "memory");
+            const int tile = first_tile + round * stride + mine;
+            const float* parts = sums + (round & 1) * (kMatWarps * kTiles * kOut * kRed) + mine * p.ways * (kTiles * kOut * kRed);
+            for (int i = 32 * way + lane; i < results * 16; i += 32 * p.ways) {
+                const int column = i >> 4, row = i & 15;
+                float v = 0.0f;
+                for (int w = 0; w < p.ways; ++w) v += parts[w * (kTiles * kOut * kRed) + column * kRed + row];
+                if (ranks > 1) kept[((held * p.at_once + mine) * kTiles * kOut + column) * 16 + row] = v;
+                else store(tile, column, row, v);
+            }
+            ++round;
+            if (ranks == 1 || (++held * p.at_once < p.kept && round < rounds)) continue;
+            cluster.sync();
+            const int values = held * p.at_once * results * 16;
+            for (int i = rank * kMatThreads + static_cast<int>(threadIdx.x); i < values; i += ranks * kMatThreads) {
+                const int row = i & 15, column = (i >> 4) % results, k = (i >> 4) / results;
+                const int at = (k * kTiles * kOut + column) * 16 + row;
+                float v = 0.0f;
+                for (int w = 0; w < ranks; ++w) v += *cluster.map_shared_rank(kept + at, w);
+                store(first_tile + (round - held + k / p.at_once) * stride + k % p.at_once, column, row, v);
+            }
+            cluster.sync();  // until every CTA's memory has been read
+            held = 0;
+        }
+    }
+}
+
+constexpr int kMostShared = 227 * 1024 - 2560;  // of a CTA, beside the table's source
+
+// Clusters of so many CTAs that run at once, asked for once (a cluster's CTAs share a part of the GPU, whose number of SMs
+// need not be a multiple of theirs), and the kernel's share of shared memory set.
+constexpr int kMatDevices = 64;
+template <auto kKernel>
+cudaError_t resident(int ranks, int& clusters) {
+    static std::atomic<int> known[kMatDevices][4];
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const int which = ranks == 1 ? 0 : ranks == 2 ? 1 : ranks == 4 ? 2 : 3;
+    clusters = device < kMatDevices ? known[device][which].load(std::memory_order_relaxed) : 0;
+    if (clusters > 0) return cudaSuccess;
+    e = cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
+    if (e != cudaSuccess) return e;
+    cudaLaunchAttribute a;
+    a.id = cudaLaunchAttributeClusterDimension;
+    a.val.clusterDim.x = ranks;
+    a.val.clusterDim.y = a.val.clusterDim.z = 1;
+    cudaLaunchConfig_t c = {};
+    c.gridDim = dim3(ranks);
+    c.blockDim = dim3(kMatThreads);
+    c.dynamicSmemBytes = kMostShared;
+    c.attrs = &a;
+    c.numAttrs = 1;
+    e = cudaOccupancyMaxActiveClusters(&clusters, kKernel, &c);
+    if (e != cudaSuccess) return e;
+    if (clusters < 1) return cudaErrorInvalidConfiguration;
+    if (device < kMatDevices) known[device][which].store(clusters, std::memory_order_relaxed);
+    return cudaSuccess;
+}
+
+template <typename T, int kTiles>
+cudaError_t launch_tiles(Params p, int ranks, cudaStream_t s) {
+    int clusters = 0;
+    const cudaError_t e = resident<q4_matmul_kernel<T, kTiles>>(ranks, clusters);
+    if (e != cudaSuccess) return e;
+    constexpr int kOut = sizeof(T) == 4 ? 4 : 8;
+    const int tiles = (p.m.out + 15) / 16, blocks = p.slice / 64;
+    // How many warps split a slice: what leaves the fewest of them waiting, for one another's blocks and for the last tiles
+    double best = 0.0;
+    for (int ways = kMatWarps; ways >= 1; ways /= 2) {
+        const int at_once = kMatWarps / ways, each = (blocks + ways - 1) / ways, rounds = (tiles + at_once * clusters - 1) / (at_once * clusters);
+        const double busy = static_cast<double>(blocks) / (static_cast<double>(each) * ways) * tiles / (static_cast<double>(rounds) * at_once * clusters);
+        if (busy <= best * 1.02) continue;
+        best = busy;
+        p.ways = ways;
+        p.at_once = at_once;
+    }
+    const int used = (tiles + p.at_once - 1) / p.at_once < clusters ? (tiles + p.at_once - 1) / p.at_once : clusters;
+    const int rounds = (tiles + p.at_once * used - 1) / (p.at_once * used);
+    p.kept = 0;
+    if (ranks > 1) {
+        const int room = (kMostShared - layout_of(sizeof(T) == 4, p.columns, p.slice, kTiles * kOut, 0).all) / (kTiles * kOut * 16 * 4);
+        const int want = rounds * p.at_once, fits = room / p.at_once * p.at_once;
+        p.kept = want < fits ? want : fits;
+        if (p.kept < p.at_once) return cudaErrorInvalidConfiguration;
+    }
+    const int shared = layout_of(sizeof(T) == 4, p.columns, p.slice, kTiles * kOut, p.kept).all;
+    return launch(q4_matmul_kernel<T, kTiles>, used * ranks, kMatThreads, shared, ranks, s, p);
+}
+
+template <typename T>
+cudaError_t launch_rows(const Params& p, int ranks, cudaStream_t s) {
+    switch ((p.columns + 7) / 8) {
+        case 1: return launch_tiles<T, 1>(p, ranks, s);
+        case 2: return launch_tiles<T, 2>(p, ranks, s);
+        case 3: return launch_tiles<T, 3>(p, ranks, s);
+        case 4: return launch_tiles<T, 4>(p, ranks, s);
+        case 5: return launch_tiles<T, 5>(p, ranks, s);
+        case 6: return launch_tiles<T, 6>(p, ranks, s);
+        case 7: return launch_tiles<T, 7>(p, ranks, s);
+        default: return launch_tiles<T, 8>(p, ranks, s);
     }
 }
 
@@ -66,8 +431,27 @@ cudaError_t launch_q4_matmul(const Q4Matmul& m, cudaStream_t s) {
     Params p;
     p.m = m;
     q4_levels_host(p.levels);
-    const unsigned ctas = (m.out + kMatThreads / 32 - 1) / (kMatThreads / 32);
-    return m.bf16 ? launch(q4_matmul_kernel<__nv_bfloat16>, ctas, kMatThreads, 0, 0, s, p) : launch(q4_matmul_kernel<float>, ctas, kMatThreads, 0, 0, s, p);
+    const int each = m.bf16 ? 1 : 2;  // columns of the product for a row of x
+    // The fewest CTAs that hold a slice each of the inputs of the rows at hand, sums of 12 tiles of a cluster beside them;
+    // fewer rows at a time where eight do not
+    int rows = m.n < kMostColumns / each ? m.n : kMostColumns / each, ranks = 1;
+    const auto fits = [&](int n, int c) {
+        const int columns = n * each, tiles = (columns + 7) / 8, out = tiles * (m.bf16 ? 8 : 4);
+        return layout_of(!m.bf16, columns, ((m.in / 64 + c - 1) / c) * 64, out, c > 1 ? 16 : 0).all <= kMostShared;
+    };
+    for (;; rows = (rows + 1) / 2) {
+        ranks = 1;
+        while (ranks < 8 && !fits(rows, ranks)) ranks *= 2;
+        if (fits(rows, ranks) || rows == 1) break;
+    }
+    p.slice = ((m.in / 64 + ranks - 1) / ranks) * 64;
+    for (p.first = 0; p.first < m.n; p.first += rows) {
+        p.rows = m.n - p.first < rows ? m.n - p.first : rows;
+        p.columns = p.rows * each;
+        const cudaError_t e = m.bf16 ? launch_rows<__nv_bfloat16>(p, ranks, s) : launch_rows<float>(p, ranks, s);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
 }
 
 }  // namespace jb
