@@ -15,8 +15,11 @@
 //
 // A CTA of 16 warps has a slice of the columns, whose inputs it keeps in shared memory, and takes tiles of 16 rows: warps
 // split the slice, and their sums are joined in shared memory. Where the inputs of all columns do not fit, a cluster of CTAs
-// has a slice each and their sums are joined through distributed shared memory.
+// has a slice each and their sums are joined through distributed shared memory. A warp copies its codes and scales ahead
+// (cp.async) to a ring of its own: loads to registers are waited for all together, and with six blocks ahead that left
+// 8 KB under way on an SM (one row times 20480 x 5120: 47 us).
 #include <atomic>
+#include <type_traits>
 
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
@@ -48,18 +51,33 @@ struct Params {
     int kept;            // tiles whose sums a CTA keeps until the cluster joins them
 };
 
-// Shared memory, in bytes: table, powers of two, inputs, warps' sums, kept sums.
+// What a kernel for so many columns of the product / 8 is made of.
+template <typename T, int kTiles>
+struct Shape {
+    static constexpr bool kF32 = sizeof(T) == 4;
+    static constexpr int kOut = (kF32 ? 4 : 8) * kTiles;        // results of a row of the matrix
+    static constexpr int kAhead = kTiles == 1 ? 8 : 4;          // blocks whose codes are copied ahead
+    static constexpr int kBuffers = kTiles <= 2 ? 2 : 1;        // of the warps' sums
+    // From byte to byte in the table: with 256 bytes the byte and the lane's place are put together by one permutation,
+    // with 128 by a shift and a selection, for less memory.
+    static constexpr int kShift = kF32 || kTiles == 1 ? 8 : 7;
+};
+constexpr int kStage = 512 + 64;  // a block's codes and scales
+
+// Shared memory, in bytes: table, rings, powers of two, inputs, warps' sums, kept sums.
 struct Layout {
-    int powers, inputs, sums, kept, all;
+    int rings, powers, inputs, sums, kept, all;
 };
 __host__ __device__ inline int round16(int x) { return (x + 15) & ~15; }
-__host__ __device__ inline Layout layout_of(bool f32, int columns, int slice, int out_columns, int kept) {
+template <typename S>
+__host__ __device__ inline Layout layout_of(int columns, int slice, int kept) {
     Layout l;
-    l.powers = f32 ? 65536 : 32768;
+    l.rings = 256 << S::kShift;
+    l.powers = l.rings + kMatWarps * S::kAhead * kStage;
     l.inputs = l.powers + round16((slice + kScaled - 1) / kScaled * ((columns + 7) / 8 * 8) * 4);
     l.sums = l.inputs + round16(columns * (slice + kPad) * 2);
-    l.kept = l.sums + 2 * kMatWarps * out_columns * kRed * 4;
-    l.all = l.kept + kept * out_columns * 16 * 4;
+    l.kept = l.sums + S::kBuffers * kMatWarps * S::kOut * kRed * 4;
+    l.all = l.kept + kept * S::kOut * 16 * 4;
     return l;
 }
 
@@ -151,23 +169,20 @@ __device__ void stage(const Params& p, const Layout& l, char* shared, int from) 
     }
 }
 
-// Codes of a block of rows r and r + 8 that a lane takes (16 columns each), and the block's scales.
-struct Codes {
-    uint2 low, high;
-    float low_scale, high_scale;
-};
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
+__device__ __forceinline__ void copy8(uint32_t to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory"); }
+__device__ __forceinline__ void copy4(uint32_t to, const void* from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory"); }
 
 // kTiles: columns of the product / 8.
 template <typename T, int kTiles>
 __global__ void __launch_bounds__(kMatThreads, 1) q4_matmul_kernel(const __grid_constant__ Params p) {
-    constexpr bool kF32 = sizeof(T) == 4;
-    constexpr int kAhead = kTiles <= 2 ? 6 : 4;                  // blocks whose codes are under way
-    constexpr int kOut = kF32 ? 4 : 8;                           // results of a product's 8 columns
-    extern __shared__ __align__(16) char shared[];
+    using S = Shape<T, kTiles>;
+    constexpr bool kF32 = S::kF32;
+    extern __shared__ __align__(256) char shared[];
     const Q4Matmul& m = p.m;
-    const Layout l = layout_of(kF32, p.columns, p.slice, kTiles * kOut, p.kept);
+    const Layout l = layout_of<S>(p.columns, p.slice, p.kept);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, t = lane & 3;
-    {   // the table: entry of byte b for lane i at (32 b + i) words
+    {   // the table: the entry of a byte, with a copy for each lane
         __shared__ uint32_t pairs[256][kF32 ? 2 : 1];
         if (threadIdx.x < 256) {
             const float a = p.levels[threadIdx.x & 15] * (kF32 ? kLevelScale : 1.0f), b = p.levels[threadIdx.x >> 4] * (kF32 ? kLevelScale : 1.0f);
@@ -182,7 +197,7 @@ __global__ void __launch_bounds__(kMatThreads, 1) q4_matmul_kernel(const __grid_
         constexpr int kQuads = kF32 ? 16 : 8;  // 16-byte pieces of an entry
         for (int i = threadIdx.x; i < 256 * kQuads; i += kMatThreads) {
             const uint32_t w = pairs[i / kQuads][0], v = kF32 ? pairs[i / kQuads][kF32 ? 1 : 0] : w;
-            reinterpret_cast<uint4*>(shared)[i] = make_uint4(w, v, w, v);
+            *reinterpret_cast<uint4*>(shared + (i / kQuads << S::kShift) + i % kQuads * 16) = make_uint4(w, v, w, v);
         }
     }
     const cg::cluster_group cluster = cg::this_cluster();
@@ -198,22 +213,41 @@ __global__ void __launch_bounds__(kMatThreads, 1) q4_matmul_kernel(const __grid_
     const int each = (p.slice / 64 + p.ways - 1) / p.ways;               // blocks of a tile for a warp, some of them past its end
     const int rounds = (tiles - first_tile + stride - 1) / stride;       // the same for all warps of the cluster
     const int total = rounds * each;
-    const auto fetch = [&](int round, int j) {
-        Codes c;
-        const int tile = first_tile + round * stride + mine, block = way + p.ways * j;
-        const int low = min(tile * 16 + r, m.out - 1), high = min(tile * 16 + r + 8, m.out - 1);
-        const int at = min(block, max(blocks - 1, 0));
-        const uint64_t k = from + 64 * static_cast<uint64_t>(at);
-        if (round < rounds && blocks > 0) {
-            const uint64_t a = static_cast<uint64_t>(low) * m.in + k, b = static_cast<uint64_t>(high) * m.in + k;
-            c.low = __ldcs(reinterpret_cast<const uint2*>(m.codes + a / 2) + t);
-            c.high = __ldcs(reinterpret_cast<const uint2*>(m.codes + b / 2) + t);
-            c.low_scale = __ldcs(m.scale + a / 64);
-            c.high_scale = __ldcs(m.scale + b / 64);
+    // copies: lane i half of row i / 2's codes of the block, lanes below 16 row i's scale
+    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(shared)) + l.rings + warp * (S::kAhead * kStage);
+    const uint32_t code_to = ring + lane * 16, scale_to = ring + 512 + lane * 4;
+    const uint8_t* code_from = nullptr;
+    const float* scale_from = nullptr;
+    const bool whole = reinterpret_cast<uint64_t>(m.codes) % 16 == 0;
+    int ahead_round = 0, ahead_j = 0;
+    const auto ask = [&](int stage) {
+        if (ahead_round < rounds) {
+            const int block = way + p.ways * ahead_j;
+            if (ahead_j == 0) {
+                const int row = (first_tile + ahead_round * stride + mine) * 16;
+                code_from = m.codes + (static_cast<uint64_t>(min(row + (lane >> 1), m.out - 1)) * m.in + from + 64 * block) / 2 + 16 * (lane & 1);
+                scale_from = m.scale + (static_cast<uint64_t>(min(row + (lane & 15), m.out - 1)) * m.in + from) / 64 + block;
+            }
+            if (block < blocks) {
+                if (whole) {
+                    copy16(code_to + stage * kStage, code_from);
+                } else {
+                    copy8(code_to + stage * kStage, code_from);
+                    copy8(code_to + stage * kStage + 8, code_from + 8);
+                }
+                if (lane < 16) copy4(scale_to + stage * kStage, scale_from);
+            }
+            code_from += 32 * p.ways;
+            scale_from += p.ways;
+            if (++ahead_j == each) {
+                ahead_j = 0;
+                ++ahead_round;
+            }
         }
-        return c;
+        asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    const char* table = shared + lane * (kF32 ? 8 : 4);
+    const uint32_t place = lane * (kF32 ? 8 : 4);  // of the lane's copy in an entry
+    const char* staged = shared + l.rings + warp * (S::kAhead * kStage);
     const float* powers = reinterpret_cast<const float*>(shared + l.powers);
     const __half* inputs = reinterpret_cast<const __half*>(shared + l.inputs) + r * (p.slice + kPad) + 16 * t;
     float* sums = reinterpret_cast<float*>(shared + l.sums);
@@ -233,118 +267,118 @@ __global__ void __launch_bounds__(kMatThreads, 1) q4_matmul_kernel(const __grid_
         }
     };
 
-    Codes ring[kAhead];
-    int ahead_round = 0, ahead_j = 0;
-    const auto next = [&]() {
-        const Codes c = fetch(ahead_round, ahead_j);
-        if (++ahead_j == each) {
-            ahead_j = 0;
-            ++ahead_round;
-        }
-        return c;
-    };
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) ring[u] = next();
+    for (int u = 0; u < S::kAhead; ++u) ask(u);
     float acc[kTiles][4];
 #pragma unroll
     for (int n = 0; n < kTiles; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
     int round = 0, j = 0, held = 0;  // held: rounds whose sums are kept
-    for (int item = 0; item < total; item += kAhead) {
+    int stage_now = 0;
+    for (int item = 0; item < total; ++item) {
+        const int block = way + p.ways * j;
+        asm volatile("cp.async.wait_group %0;" ::"n"(S::kAhead - 1) : "memory");
+        __syncwarp();
+        if (block < blocks) {
+            const char* stage = staged + stage_now * kStage;
+            const uint2 low = *reinterpret_cast<const uint2*>(stage + r * 32 + t * 8), high = *reinterpret_cast<const uint2*>(stage + (r + 8) * 32 + t * 8);
+            const float low_scale = *reinterpret_cast<const float*>(stage + 512 + r * 4), high_scale = *reinterpret_cast<const float*>(stage + 512 + (r + 8) * 4);
+            const uint32_t codes[4] = {low.x, low.y, high.x, high.y};
+            float part[kTiles][4];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (item + u >= total) break;
-            const int block = way + p.ways * j;
-            if (block < blocks) {
-                const Codes& c = ring[u];
-                const uint32_t codes[4] = {c.low.x, c.low.y, c.high.x, c.high.y};
-                float part[kTiles][4];
+            for (int n = 0; n < kTiles; ++n) part[n][0] = part[n][1] = part[n][2] = part[n][3] = 0.0f;
 #pragma unroll
-                for (int n = 0; n < kTiles; ++n) part[n][0] = part[n][1] = part[n][2] = part[n][3] = 0.0f;
+            for (int h = 0; h < 2; ++h) {  // 8 columns of a lane's 16
+                uint32_t upper[2][4], lower[2][4];  // of two products
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {  // 8 columns of a lane's 16
-                    uint32_t upper[2][4], lower[2][4];  // of two products
+                for (int e = 0; e < 4; ++e) {       // bytes
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {       // bytes
-                        constexpr int kShift = kF32 ? 8 : 7;
-#pragma unroll
-                        for (int g = 0; g < 2; ++g) {   // rows r and r + 8
-                            const uint32_t w = codes[2 * g + h];
-                            const uint32_t at = (8 * e >= kShift ? w >> (8 * e - kShift) : w << kShift) & (255u << kShift);
-                            if constexpr (kF32) {
-                                const uint2 v = *reinterpret_cast<const uint2*>(table + at);
-                                upper[e / 2][g + e % 2 * 2] = v.x;
-                                lower[e / 2][g + e % 2 * 2] = v.y;
-                            } else {
-                                upper[e / 2][g + e % 2 * 2] = *reinterpret_cast<const uint32_t*>(table + at);
-                            }
-                        }
-                    }
-#pragma unroll
-                    for (int n = 0; n < kTiles; ++n) {
-                        uint4 b = make_uint4(0, 0, 0, 0);
-                        if (8 * n + r < p.columns) b = *reinterpret_cast<const uint4*>(inputs + 8 * n * (p.slice + kPad) + block * 64 + 8 * h);
-                        mma(part[n], upper[0], b.x, b.y);
-                        mma(part[n], upper[1], b.z, b.w);
-                        if constexpr (kF32) {  // lower parts of levels with upper parts of inputs
-                            if (r & 1) b = make_uint4(0, 0, 0, 0);
-                            mma(part[n], lower[0], b.x, b.y);
-                            mma(part[n], lower[1], b.z, b.w);
+                    for (int g = 0; g < 2; ++g) {   // rows r and r + 8
+                        const uint32_t w = codes[2 * g + h];
+                        uint32_t at;
+                        if constexpr (S::kShift == 8) at = __byte_perm(w, place, 0x5504 | e << 4);  // place, byte e, 0, 0
+                        else at = ((8 * e >= 7 ? w >> (8 * e - 7) : w << 7) & (255u << 7)) | place;
+                        if constexpr (kF32) {
+                            const uint2 v = *reinterpret_cast<const uint2*>(shared + at);
+                            upper[e / 2][g + e % 2 * 2] = v.x;
+                            lower[e / 2][g + e % 2 * 2] = v.y;
+                        } else {
+                            upper[e / 2][g + e % 2 * 2] = *reinterpret_cast<const uint32_t*>(shared + at);
                         }
                     }
                 }
-                const float* power = powers + block * 64 / kScaled * padded + 2 * t;
 #pragma unroll
                 for (int n = 0; n < kTiles; ++n) {
-                    const float2 f = *reinterpret_cast<const float2*>(power + 8 * n);
-                    acc[n][0] = fmaf(part[n][0], c.low_scale * f.x, acc[n][0]);
-                    acc[n][1] = fmaf(part[n][1], c.low_scale * f.y, acc[n][1]);
-                    acc[n][2] = fmaf(part[n][2], c.high_scale * f.x, acc[n][2]);
-                    acc[n][3] = fmaf(part[n][3], c.high_scale * f.y, acc[n][3]);
+                    uint4 b = make_uint4(0, 0, 0, 0);
+                    if (8 * n + r < p.columns) b = *reinterpret_cast<const uint4*>(inputs + 8 * n * (p.slice + kPad) + block * 64 + 8 * h);
+                    mma(part[n], upper[0], b.x, b.y);
+                    mma(part[n], upper[1], b.z, b.w);
+                    if constexpr (kF32) {  // lower parts of levels with upper parts of inputs
+                        if (r & 1) b = make_uint4(0, 0, 0, 0);
+                        mma(part[n], lower[0], b.x, b.y);
+                        mma(part[n], lower[1], b.z, b.w);
+                    }
                 }
             }
-            ring[u] = next();
-            if (++j < each) continue;
-            // the tile's sums: each warp's, then all of them in the order of the ways
-            j = 0;
-            float* here = sums + (round & 1) * (kMatWarps * kTiles * kOut * kRed) + warp * (kTiles * kOut * kRed);
+            const float* power = powers + block * 64 / kScaled * padded + 2 * t;
 #pragma unroll
             for (int n = 0; n < kTiles; ++n) {
-                if constexpr (kF32) {
-                    here[(4 * n + t) * kRed + r] = acc[n][0] + acc[n][1];
-                    here[(4 * n + t) * kRed + r + 8] = acc[n][2] + acc[n][3];
-                } else {
-                    here[(8 * n + 2 * t) * kRed + r] = acc[n][0];
-                    here[(8 * n + 2 * t + 1) * kRed + r] = acc[n][1];
-                    here[(8 * n + 2 * t) * kRed + r + 8] = acc[n][2];
-                    here[(8 * n + 2 * t + 1) * kRed + r + 8] = acc[n][3];
-                }
-                acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
+                const float2 f = *reinterpret_cast<const float2*>(power + 8 * n);
+                acc[n][0] = fmaf(part[n][0], low_scale * f.x, acc[n][0]);
+                acc[n][1] = fmaf(part[n][1], low_scale * f.y, acc[n][1]);
+                acc[n][2] = fmaf(part[n][2], high_scale * f.x, acc[n][2]);
+                acc[n][3] = fmaf(part[n][3], high_scale * f.y, acc[n][3]);
             }
+        }
+        __syncwarp();
+        ask(stage_now);
+        stage_now = stage_now == S::kAhead - 1 ? 0 : stage_now + 1;
+        if (++j < each) continue;
+        // the tile's sums: each warp's, then all of them in the order of the ways
+        j = 0;
+        constexpr int kWarp = S::kOut * kRed;
+        float* buffer = sums + (S::kBuffers == 2 ? round & 1 : 0) * (kMatWarps * kWarp);
+        float* here = buffer + warp * kWarp;
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n) {
+            if constexpr (kF32) {
+                here[(4 * n + t) * kRed + r] = acc[n][0] + acc[n][1];
+                here[(4 * n + t) * kRed + r + 8] = acc[n][2] + acc[n][3];
+            } else {
+                here[(8 * n + 2 * t) * kRed + r] = acc[n][0];
+                here[(8 * n + 2 * t + 1) * kRed + r] = acc[n][1];
+                here[(8 * n + 2 * t) * kRed + r + 8] = acc[n][2];
+                here[(8 * n + 2 * t + 1) * kRed + r + 8] = acc[n][3];
+            }
+            acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
+        }
+        const auto together = [&]() {  // the warps of a tile
             if (p.ways == 1) __syncwarp();
             else asm volatile("bar.sync %0, %1;" ::"r"(1 + mine), "r"(32 * p.ways) : "memory");
-            const int tile = first_tile + round * stride + mine;
-            const float* parts = sums + (round & 1) * (kMatWarps * kTiles * kOut * kRed) + mine * p.ways * (kTiles * kOut * kRed);
-            for (int i = 32 * way + lane; i < results * 16; i += 32 * p.ways) {
-                const int column = i >> 4, row = i & 15;
-                float v = 0.0f;
-                for (int w = 0; w < p.ways; ++w) v += parts[w * (kTiles * kOut * kRed) + column * kRed + row];
-                if (ranks > 1) kept[((held * p.at_once + mine) * kTiles * kOut + column) * 16 + row] = v;
-                else store(tile, column, row, v);
-            }
-            ++round;
-            if (ranks == 1 || (++held * p.at_once < p.kept && round < rounds)) continue;
-            cluster.sync();
-            const int values = held * p.at_once * results * 16;
-            for (int i = rank * kMatThreads + static_cast<int>(threadIdx.x); i < values; i += ranks * kMatThreads) {
-                const int row = i & 15, column = (i >> 4) % results, k = (i >> 4) / results;
-                const int at = (k * kTiles * kOut + column) * 16 + row;
-                float v = 0.0f;
-                for (int w = 0; w < ranks; ++w) v += *cluster.map_shared_rank(kept + at, w);
-                store(first_tile + (round - held + k / p.at_once) * stride + k % p.at_once, column, row, v);
-            }
-            cluster.sync();  // until every CTA's memory has been read
-            held = 0;
+        };
+        together();
+        const int tile = first_tile + round * stride + mine;
+        const float* parts = buffer + mine * p.ways * kWarp;
+        for (int i = 32 * way + lane; i < results * 16; i += 32 * p.ways) {
+            const int column = i >> 4, row = i & 15;
+            float v = 0.0f;
+            for (int w = 0; w < p.ways; ++w) v += parts[w * kWarp + column * kRed + row];
+            if (ranks > 1) kept[((held * p.at_once + mine) * S::kOut + column) * 16 + row] = v;
+            else store(tile, column, row, v);
         }
+        if constexpr (S::kBuffers == 1) together();
+        ++round;
+        if (ranks == 1 || (++held * p.at_once < p.kept && round < rounds)) continue;
+        cluster.sync();
+        const int values = held * p.at_once * results * 16;
+        for (int i = rank * kMatThreads + static_cast<int>(threadIdx.x); i < values; i += ranks * kMatThreads) {
+            const int row = i & 15, column = (i >> 4) % results, k = (i >> 4) / results;
+            const int at = (k * S::kOut + column) * 16 + row;
+            float v = 0.0f;
+            for (int w = 0; w < ranks; ++w) v += *cluster.map_shared_rank(kept + at, w);
+            store(first_tile + (round - held + k / p.at_once) * stride + k % p.at_once, column, row, v);
+        }
+        cluster.sync();  // until every CTA's memory has been read
+        held = 0;
     }
 }
 
@@ -386,7 +420,7 @@ cudaError_t launch_tiles(Params p, int ranks, cudaStream_t s) {
     int clusters = 0;
     const cudaError_t e = resident<q4_matmul_kernel<T, kTiles>>(ranks, clusters);
     if (e != cudaSuccess) return e;
-    constexpr int kOut = sizeof(T) == 4 ? 4 : 8;
+    using S = Shape<T, kTiles>;
     const int tiles = (p.m.out + 15) / 16, blocks = p.slice / 64;
     // How many warps split a slice: what leaves the fewest of them waiting, for one another's blocks and for the last tiles
     double best = 0.0;
@@ -402,27 +436,54 @@ cudaError_t launch_tiles(Params p, int ranks, cudaStream_t s) {
     const int rounds = (tiles + p.at_once * used - 1) / (p.at_once * used);
     p.kept = 0;
     if (ranks > 1) {
-        const int room = (kMostShared - layout_of(sizeof(T) == 4, p.columns, p.slice, kTiles * kOut, 0).all) / (kTiles * kOut * 16 * 4);
+        const int room = (kMostShared - layout_of<S>(p.columns, p.slice, 0).all) / (S::kOut * 16 * 4);
         const int want = rounds * p.at_once, fits = room / p.at_once * p.at_once;
         p.kept = want < fits ? want : fits;
         if (p.kept < p.at_once) return cudaErrorInvalidConfiguration;
     }
-    const int shared = layout_of(sizeof(T) == 4, p.columns, p.slice, kTiles * kOut, p.kept).all;
+    const int shared = layout_of<S>(p.columns, p.slice, p.kept).all;
     return launch(q4_matmul_kernel<T, kTiles>, used * ranks, kMatThreads, shared, ranks, s, p);
 }
 
-template <typename T>
-cudaError_t launch_rows(const Params& p, int ranks, cudaStream_t s) {
-    switch ((p.columns + 7) / 8) {
-        case 1: return launch_tiles<T, 1>(p, ranks, s);
-        case 2: return launch_tiles<T, 2>(p, ranks, s);
-        case 3: return launch_tiles<T, 3>(p, ranks, s);
-        case 4: return launch_tiles<T, 4>(p, ranks, s);
-        case 5: return launch_tiles<T, 5>(p, ranks, s);
-        case 6: return launch_tiles<T, 6>(p, ranks, s);
-        case 7: return launch_tiles<T, 7>(p, ranks, s);
-        default: return launch_tiles<T, 8>(p, ranks, s);
+// Calls f with the number of the product's columns / 8 as a constant.
+template <typename F>
+auto with_tiles(int columns, F f) {
+    switch ((columns + 7) / 8) {
+        case 1: return f(std::integral_constant<int, 1>());
+        case 2: return f(std::integral_constant<int, 2>());
+        case 3: return f(std::integral_constant<int, 3>());
+        case 4: return f(std::integral_constant<int, 4>());
+        case 5: return f(std::integral_constant<int, 5>());
+        case 6: return f(std::integral_constant<int, 6>());
+        case 7: return f(std::integral_constant<int, 7>());
+        default: return f(std::integral_constant<int, 8>());
     }
+}
+
+template <typename T>
+cudaError_t launch_t(Params p, cudaStream_t s) {
+    const Q4Matmul& m = p.m;
+    const int each = sizeof(T) == 2 ? 1 : 2;  // columns of the product for a row of x
+    // The fewest CTAs that hold a slice each of the inputs of the rows at hand and sums of 16 tiles beside them; fewer rows
+    // at a time where eight do not
+    const auto fits = [&](int rows, int ranks) {
+        const int slice = (m.in / 64 + ranks - 1) / ranks * 64;
+        return with_tiles(rows * each, [&](auto tiles) { return layout_of<Shape<T, tiles.value>>(rows * each, slice, ranks > 1 ? 16 : 0).all <= kMostShared; });
+    };
+    int rows = m.n < kMostColumns / each ? m.n : kMostColumns / each, ranks = 1;
+    for (;; rows = (rows + 1) / 2) {
+        ranks = 1;
+        while (ranks < 8 && !fits(rows, ranks)) ranks *= 2;
+        if (fits(rows, ranks) || rows == 1) break;
+    }
+    p.slice = (m.in / 64 + ranks - 1) / ranks * 64;
+    for (p.first = 0; p.first < m.n; p.first += rows) {
+        p.rows = m.n - p.first < rows ? m.n - p.first : rows;
+        p.columns = p.rows * each;
+        const cudaError_t e = with_tiles(p.columns, [&](auto tiles) { return launch_tiles<T, tiles.value>(p, ranks, s); });
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
 }
 
 }  // namespace
@@ -431,27 +492,7 @@ cudaError_t launch_q4_matmul(const Q4Matmul& m, cudaStream_t s) {
     Params p;
     p.m = m;
     q4_levels_host(p.levels);
-    const int each = m.bf16 ? 1 : 2;  // columns of the product for a row of x
-    // The fewest CTAs that hold a slice each of the inputs of the rows at hand, sums of 12 tiles of a cluster beside them;
-    // fewer rows at a time where eight do not
-    int rows = m.n < kMostColumns / each ? m.n : kMostColumns / each, ranks = 1;
-    const auto fits = [&](int n, int c) {
-        const int columns = n * each, tiles = (columns + 7) / 8, out = tiles * (m.bf16 ? 8 : 4);
-        return layout_of(!m.bf16, columns, ((m.in / 64 + c - 1) / c) * 64, out, c > 1 ? 16 : 0).all <= kMostShared;
-    };
-    for (;; rows = (rows + 1) / 2) {
-        ranks = 1;
-        while (ranks < 8 && !fits(rows, ranks)) ranks *= 2;
-        if (fits(rows, ranks) || rows == 1) break;
-    }
-    p.slice = ((m.in / 64 + ranks - 1) / ranks) * 64;
-    for (p.first = 0; p.first < m.n; p.first += rows) {
-        p.rows = m.n - p.first < rows ? m.n - p.first : rows;
-        p.columns = p.rows * each;
-        const cudaError_t e = m.bf16 ? launch_rows<__nv_bfloat16>(p, ranks, s) : launch_rows<float>(p, ranks, s);
-        if (e != cudaSuccess) return e;
-    }
-    return cudaSuccess;
+    return m.bf16 ? launch_t<__nv_bfloat16>(p, s) : launch_t<float>(p, s);
 }
 
 }  // namespace jb
