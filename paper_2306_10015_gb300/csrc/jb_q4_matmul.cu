@@ -7,8 +7,8 @@
 // four products with up to 8 rows of x; tokens are the product's columns.
 //
 // Numbers. fp16 has 11 bits: a level is off by at most 2^-12, beside the 2^-9 of a bf16 result. bf16 inputs fit fp16 with
-// all their bits once they are scaled by a power of two, chosen for each row and 512 columns so that the largest is near
-// 2^15 (what is 2^-28 of it or smaller loses bits, 2^-40 of it is lost). fp32: levels and inputs are two fp16 each, 22 bits
+// all their bits once they are scaled by a power of two, chosen for each row (of a CTA's slice of the columns) so that the
+// largest is near 2^15 (what is 2^-28 of it or smaller loses bits, 2^-40 of it is lost). fp32: levels and inputs are two fp16 each, 22 bits
 // and more; the inputs' two parts are two columns of the product, and a table read is two words (the product of two lower
 // parts, 2^-24, is left out). A block's sum is fp32 and
 // meets its scale once; sums over blocks, warps and CTAs are fp32, in an order that does not depend on the launch's timing.
@@ -17,7 +17,8 @@
 // split the slice, and their sums are joined in shared memory. Where the inputs of all columns do not fit, a cluster of CTAs
 // has a slice each and their sums are joined through distributed shared memory. A warp copies its codes and scales ahead
 // (cp.async) to a ring of its own: loads to registers are waited for all together, and with six blocks ahead that left
-// 8 KB under way on an SM (one row times 20480 x 5120: 47 us).
+// 8 KB under way on an SM (one row times 20480 x 5120: 47 us). It takes two or four blocks of a row at a time, because each
+// line that a copy touches takes a turn of the pipe that serves shared memory, too, as a table read does (one block: 28 us).
 #include <atomic>
 #include <type_traits>
 
@@ -35,7 +36,7 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kMatWarps = 16, kMatThreads = 32 * kMatWarps;
-constexpr int kScaled = 512;        // columns that share a power of two
+constexpr int kUnit = 512;          // columns of a row that a warp converts at a time
 constexpr int kPad = 8;             // halves between rows of inputs: reads of 8 rows meet no bank twice
 constexpr int kRed = 20;            // floats from column to column of a tile's sums, for the same reason
 constexpr int kMostColumns = 64;    // of the product at a time
@@ -48,6 +49,7 @@ struct Params {
     int columns;         // of the product: rows, or twice as many
     int slice;           // columns of a CTA's slice
     int ways, at_once;   // warps that split a slice; tiles of 16 rows that a CTA takes at a time
+    int slots;           // rounds of tiles whose warps' sums are joined at a time
     int kept;            // tiles whose sums a CTA keeps until the cluster joins them
 };
 
@@ -55,29 +57,28 @@ struct Params {
 template <typename T, int kTiles>
 struct Shape {
     static constexpr bool kF32 = sizeof(T) == 4;
-    static constexpr int kOut = (kF32 ? 4 : 8) * kTiles;        // results of a row of the matrix
-    static constexpr int kAhead = kTiles == 1 ? 8 : 4;          // blocks whose codes are copied ahead
-    static constexpr int kBuffers = kTiles <= 2 ? 2 : 1;        // of the warps' sums
+    static constexpr int kSpan = kTiles == 1 ? 4 : 2;           // neighbouring blocks of a row that a warp takes
+    static constexpr int kAhead = 2;                            // of them copied ahead
+    static constexpr int kPitch = kSpan * 32 + 32;              // bytes from row to row: reads of 8 rows meet no bank twice
+    static constexpr int kStage = 16 * kPitch + kSpan * 64;     // codes, and scales by block and row
     // From byte to byte in the table: with 256 bytes the byte and the lane's place are put together by one permutation,
     // with 128 by a shift and a selection, for less memory.
     static constexpr int kShift = kF32 || kTiles == 1 ? 8 : 7;
 };
-constexpr int kStage = 512 + 64;  // a block's codes and scales
-
-// Shared memory, in bytes: table, rings, powers of two, inputs, warps' sums, kept sums.
+// Shared memory, in bytes: table, rings, powers of two and rows' maxima, inputs, warps' sums, kept sums.
 struct Layout {
     int rings, powers, inputs, sums, kept, all;
 };
 __host__ __device__ inline int round16(int x) { return (x + 15) & ~15; }
 template <typename S>
-__host__ __device__ inline Layout layout_of(int columns, int slice, int kept) {
+__host__ __device__ inline Layout layout_of(int rows, int columns, int slice, int slots, int kept) {
     Layout l;
     l.rings = 256 << S::kShift;
-    l.powers = l.rings + kMatWarps * S::kAhead * kStage;
-    l.inputs = l.powers + round16((slice + kScaled - 1) / kScaled * ((columns + 7) / 8 * 8) * 4);
+    l.powers = l.rings + kMatWarps * S::kAhead * S::kStage;
+    l.inputs = l.powers + 2 * kMostColumns * 4;
     l.sums = l.inputs + round16(columns * (slice + kPad) * 2);
-    l.kept = l.sums + S::kBuffers * kMatWarps * S::kOut * kRed * 4;
-    l.all = l.kept + kept * S::kOut * 16 * 4;
+    l.kept = l.sums + slots * kMatWarps * rows * kRed * 4;
+    l.all = l.kept + kept * rows * 16 * 4;
     return l;
 }
 
@@ -113,39 +114,44 @@ __device__ __forceinline__ void read16(const __nv_bfloat16* from, float (&x)[16]
     }
 }
 
-// The slice's inputs as the product takes them, and their powers of two. A warp takes 512 columns of a row.
+// The slice's inputs as the product takes them, and their powers of two. A warp takes 512 columns of a row at a time; what
+// it has read for the row's maximum it keeps, if that is one unit.
 template <typename T>
 __device__ void stage(const Params& p, const Layout& l, char* shared, int from) {
     constexpr bool kF32 = sizeof(T) == 4;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, groups = (p.slice + kScaled - 1) / kScaled, padded = (p.columns + 7) / 8 * 8;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, groups = (p.slice + kUnit - 1) / kUnit, units = p.rows * groups;
     float* powers = reinterpret_cast<float*>(shared + l.powers);
+    int* most_of = reinterpret_cast<int*>(powers + kMostColumns);
     __half* inputs = reinterpret_cast<__half*>(shared + l.inputs);
     const T* x = static_cast<const T*>(p.m.x);
     const int here = min(p.slice, p.m.in - from);
-    for (int u = warp; u < p.rows * groups; u += kMatWarps) {
-        const int row = u / groups, group = u - row * groups, k = group * kScaled + 16 * lane;
-        float v[16];
+    float v[16];
+    const auto read = [&](int row, int k) {
         if (k < here) {
             read16(x + (p.first + row) * p.m.x_row + from + k, v);
         } else {
 #pragma unroll
             for (int i = 0; i < 16; ++i) v[i] = 0.0f;
         }
+    };
+    for (int u = warp; u < units; u += kMatWarps) {
+        const int row = u / groups;
+        read(row, (u - row * groups) * kUnit + 16 * lane);
         float most = 0.0f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) most = fmaxf(most, isfinite(v[i]) ? fabsf(v[i]) : 0.0f);
 #pragma unroll
         for (int d = 16; d > 0; d /= 2) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
+        if (lane == 0) atomicMax(&most_of[row], __float_as_int(most));  // not negative: ordered as integers are
+    }
+    __syncthreads();
+    for (int u = warp; u < units; u += kMatWarps) {
+        const int row = u / groups, k = (u - row * groups) * kUnit + 16 * lane;
+        if (units > kMatWarps) read(row, k);
         // most in [2^e, 2^(e+1)) becomes [2^14, 2^15); powers of two that fp32 has with their inverses
-        const int e = most > 0.0f ? min(max(static_cast<int>(__float_as_uint(most) >> 23) - 127 - 14, -126), 126) : 0;
-        const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23), up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
-        if (lane == 0) {
-            if (kF32) {
-                powers[group * padded + 2 * row] = powers[group * padded + 2 * row + 1] = up * (1.0f / kLevelScale);
-            } else {
-                powers[group * padded + row] = up;
-            }
-        }
+        const int most = most_of[row], e = most > 0 ? min(max((most >> 23) - 127 - 14, -126), 126) : 0;
+        const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+        if (lane == 0) powers[row] = __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * (kF32 ? 1.0f / kLevelScale : 1.0f);
         if (k >= p.slice) continue;
         uint32_t w[8], r[8];
 #pragma unroll
@@ -180,7 +186,7 @@ __global__ void __launch_bounds__(kMatThreads, 1) q4_matmul_kernel(const __grid_
     constexpr bool kF32 = S::kF32;
     extern __shared__ __align__(256) char shared[];
     const Q4Matmul& m = p.m;
-    const Layout l = layout_of<S>(p.columns, p.slice, p.kept);
+    const Layout l = layout_of<S>(p.rows, p.columns, p.slice, p.slots, p.kept);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, t = lane & 3;
     {   // the table: the entry of a byte, with a copy for each lane
         __shared__ uint32_t pairs[256][kF32 ? 2 : 1];
@@ -200,45 +206,47 @@ __global__ void __launch_bounds__(kMatThreads, 1) q4_matmul_kernel(const __grid_
             *reinterpret_cast<uint4*>(shared + (i / kQuads << S::kShift) + i % kQuads * 16) = make_uint4(w, v, w, v);
         }
     }
+    int* most_of = reinterpret_cast<int*>(shared + l.powers) + kMostColumns;
+    if (threadIdx.x < kMostColumns) most_of[threadIdx.x] = 0;
+    __syncthreads();
     const cg::cluster_group cluster = cg::this_cluster();
     const int rank = cluster.block_rank(), ranks = cluster.num_blocks();
     const int from = rank * p.slice, blocks = max(0, min(p.slice, m.in - from)) / 64;
+    const int tiles = (m.out + 15) / 16, way = warp % p.ways, mine = warp / p.ways;  // the last warps may have nothing to do
+    const int stride = gridDim.x / ranks * p.at_once, first_tile = blockIdx.x / ranks * p.at_once;
+    const int spans = (p.slice / 64 + S::kSpan - 1) / S::kSpan, each = (spans + p.ways - 1) / p.ways;  // of a slice; for a warp
+    const int rounds = (tiles - first_tile + stride - 1) / stride;  // the same for all warps of the cluster
     after_previous();
     let_next_start();
-    stage<T>(p, l, shared, from);
-    __syncthreads();
 
-    const int tiles = (m.out + 15) / 16, way = warp % p.ways, mine = warp / p.ways;
-    const int stride = gridDim.x / ranks * p.at_once, first_tile = blockIdx.x / ranks * p.at_once;
-    const int each = (p.slice / 64 + p.ways - 1) / p.ways;               // blocks of a tile for a warp, some of them past its end
-    const int rounds = (tiles - first_tile + stride - 1) / stride;       // the same for all warps of the cluster
-    const int total = rounds * each;
-    // copies: lane i half of row i / 2's codes of the block, lanes below 16 row i's scale
-    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(shared)) + l.rings + warp * (S::kAhead * kStage);
-    const uint32_t code_to = ring + lane * 16, scale_to = ring + 512 + lane * 4;
-    const uint8_t* code_from = nullptr;
-    const float* scale_from = nullptr;
-    const bool whole = reinterpret_cast<uint64_t>(m.codes) % 16 == 0;
+    // A span's copies: 16 bytes a lane, of 32 / (2 kSpan) rows at a time; 4 bytes a lane of scales.
+    constexpr int kSpan = S::kSpan, kLanes = 2 * kSpan, kRows = 32 / kLanes, kScaleRows = 32 / kSpan;
+    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(shared)) + l.rings + warp * (S::kAhead * S::kStage);
+    const uint32_t code_to = ring + lane / kLanes * S::kPitch + lane % kLanes * 16, scale_to = ring + 16 * S::kPitch + lane % kSpan * 64 + lane / kSpan * 4;
+    const bool whole = reinterpret_cast<uint64_t>(m.codes) % 16 == 0, idle = mine >= p.at_once;
     int ahead_round = 0, ahead_j = 0;
     const auto ask = [&](int stage) {
-        if (ahead_round < rounds) {
-            const int block = way + p.ways * ahead_j;
-            if (ahead_j == 0) {
-                const int row = (first_tile + ahead_round * stride + mine) * 16;
-                code_from = m.codes + (static_cast<uint64_t>(min(row + (lane >> 1), m.out - 1)) * m.in + from + 64 * block) / 2 + 16 * (lane & 1);
-                scale_from = m.scale + (static_cast<uint64_t>(min(row + (lane & 15), m.out - 1)) * m.in + from) / 64 + block;
-            }
-            if (block < blocks) {
-                if (whole) {
-                    copy16(code_to + stage * kStage, code_from);
-                } else {
-                    copy8(code_to + stage * kStage, code_from);
-                    copy8(code_to + stage * kStage + 8, code_from + 8);
+        if (ahead_round < rounds && !idle) {
+            const int row = (first_tile + ahead_round * stride + mine) * 16, block = (way + p.ways * ahead_j) * kSpan;
+            const uint64_t column = from + 64ull * block;
+            if (block + lane % kLanes / 2 < blocks) {
+                const uint32_t to = code_to + stage * S::kStage;
+#pragma unroll
+                for (int k = 0; k < 16; k += kRows) {
+                    const uint8_t* codes = m.codes + (static_cast<uint64_t>(min(row + k + lane / kLanes, m.out - 1)) * m.in + column) / 2 + lane % kLanes * 16;
+                    if (whole) {
+                        copy16(to + k * S::kPitch, codes);
+                    } else {
+                        copy8(to + k * S::kPitch, codes);
+                        copy8(to + k * S::kPitch + 8, codes + 8);
+                    }
                 }
-                if (lane < 16) copy4(scale_to + stage * kStage, scale_from);
             }
-            code_from += 32 * p.ways;
-            scale_from += p.ways;
+            if (block + lane % kSpan < blocks) {
+#pragma unroll
+                for (int k = 0; k < 16; k += kScaleRows)
+                    copy4(scale_to + stage * S::kStage + k * 4, m.scale + (static_cast<uint64_t>(min(row + k + lane / kSpan, m.out - 1)) * m.in + column) / 64 + lane % kSpan);
+            }
             if (++ahead_j == each) {
                 ahead_j = 0;
                 ++ahead_round;
@@ -247,12 +255,12 @@ __global__ void __launch_bounds__(kMatThreads, 1) q4_matmul_kernel(const __grid_
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
     const uint32_t place = lane * (kF32 ? 8 : 4);  // of the lane's copy in an entry
-    const char* staged = shared + l.rings + warp * (S::kAhead * kStage);
+    const char* staged = shared + l.rings + warp * (S::kAhead * S::kStage);
     const float* powers = reinterpret_cast<const float*>(shared + l.powers);
-    const __half* inputs = reinterpret_cast<const __half*>(shared + l.inputs) + r * (p.slice + kPad) + 16 * t;
+    const uint32_t inputs = static_cast<uint32_t>(__cvta_generic_to_shared(shared)) + l.inputs + (r * (p.slice + kPad) + 16 * t) * 2;
+    const uint32_t real = 8 * (kTiles - 1) + r < p.columns;  // this lane's column of the product's last 8
     float* sums = reinterpret_cast<float*>(shared + l.sums);
     float* kept = reinterpret_cast<float*>(shared + l.kept);
-    const int padded = (p.columns + 7) / 8 * 8, results = kF32 ? p.columns / 2 : p.columns;
     const T* bias = static_cast<const T*>(m.bias);
     T* y = static_cast<T*>(m.y) + p.first * m.y_row;
     const auto store = [&](int tile, int column, int row, float v) {
@@ -269,112 +277,149 @@ __global__ void __launch_bounds__(kMatThreads, 1) q4_matmul_kernel(const __grid_
 
 #pragma unroll
     for (int u = 0; u < S::kAhead; ++u) ask(u);
+    stage<T>(p, l, shared, from);
+    __syncthreads();
     float acc[kTiles][4];
 #pragma unroll
     for (int n = 0; n < kTiles; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
-    int round = 0, j = 0, held = 0;  // held: rounds whose sums are kept
-    int stage_now = 0;
-    for (int item = 0; item < total; ++item) {
-        const int block = way + p.ways * j;
-        asm volatile("cp.async.wait_group %0;" ::"n"(S::kAhead - 1) : "memory");
-        __syncwarp();
-        if (block < blocks) {
-            const char* stage = staged + stage_now * kStage;
-            const uint2 low = *reinterpret_cast<const uint2*>(stage + r * 32 + t * 8), high = *reinterpret_cast<const uint2*>(stage + (r + 8) * 32 + t * 8);
-            const float low_scale = *reinterpret_cast<const float*>(stage + 512 + r * 4), high_scale = *reinterpret_cast<const float*>(stage + 512 + (r + 8) * 4);
-            const uint32_t codes[4] = {low.x, low.y, high.x, high.y};
-            float part[kTiles][4];
+    // kCount blocks of a span from its block `first` on, whose codes have arrived
+    const auto work = [&](const char* stage, int span, int first, auto count) {
+        constexpr int kCount = decltype(count)::value;
+        float part[kCount][kTiles][4], scale[kCount][2];
+        uint32_t codes[kCount][4];
 #pragma unroll
-            for (int n = 0; n < kTiles; ++n) part[n][0] = part[n][1] = part[n][2] = part[n][3] = 0.0f;
+        for (int c = 0; c < kCount; ++c) {
+            const char* at = stage + (first + c) * 32 + t * 8;
+            const uint2 low = *reinterpret_cast<const uint2*>(at + r * S::kPitch), high = *reinterpret_cast<const uint2*>(at + (r + 8) * S::kPitch);
+            codes[c][0] = low.x, codes[c][1] = low.y, codes[c][2] = high.x, codes[c][3] = high.y;
+            const float* scales = reinterpret_cast<const float*>(stage + 16 * S::kPitch) + (first + c) * 16 + r;
+            scale[c][0] = scales[0];
+            scale[c][1] = scales[8];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {  // 8 columns of a lane's 16
-                uint32_t upper[2][4], lower[2][4];  // of two products
+            for (int n = 0; n < kTiles; ++n) part[c][n][0] = part[c][n][1] = part[c][n][2] = part[c][n][3] = 0.0f;
+        }
+        const uint32_t in = inputs + (span * kSpan + first) * 128;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {  // 8 columns of a lane's 16
+            uint32_t upper[kCount][2][4], lower[kCount][2][4];  // of two products
+#pragma unroll
+            for (int c = 0; c < kCount; ++c)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {       // bytes
 #pragma unroll
                     for (int g = 0; g < 2; ++g) {   // rows r and r + 8
-                        const uint32_t w = codes[2 * g + h];
+                        const uint32_t w = codes[c][2 * g + h];
                         uint32_t at;
                         if constexpr (S::kShift == 8) at = __byte_perm(w, place, 0x5504 | e << 4);  // place, byte e, 0, 0
                         else at = ((8 * e >= 7 ? w >> (8 * e - 7) : w << 7) & (255u << 7)) | place;
                         if constexpr (kF32) {
                             const uint2 v = *reinterpret_cast<const uint2*>(shared + at);
-                            upper[e / 2][g + e % 2 * 2] = v.x;
-                            lower[e / 2][g + e % 2 * 2] = v.y;
+                            upper[c][e / 2][g + e % 2 * 2] = v.x;
+                            lower[c][e / 2][g + e % 2 * 2] = v.y;
                         } else {
-                            upper[e / 2][g + e % 2 * 2] = *reinterpret_cast<const uint32_t*>(shared + at);
+                            upper[c][e / 2][g + e % 2 * 2] = *reinterpret_cast<const uint32_t*>(shared + at);
                         }
                     }
                 }
 #pragma unroll
-                for (int n = 0; n < kTiles; ++n) {
-                    uint4 b = make_uint4(0, 0, 0, 0);
-                    if (8 * n + r < p.columns) b = *reinterpret_cast<const uint4*>(inputs + 8 * n * (p.slice + kPad) + block * 64 + 8 * h);
-                    mma(part[n], upper[0], b.x, b.y);
-                    mma(part[n], upper[1], b.z, b.w);
+            for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+                for (int c = 0; c < kCount; ++c) {
+                    uint4 b = make_uint4(0, 0, 0, 0);  // the last columns may not be real
+                    asm volatile(
+                        "{\n .reg .pred p;\n setp.ne.u32 p, %5, 0;\n @p ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];\n}"
+                        : "+r"(b.x), "+r"(b.y), "+r"(b.z), "+r"(b.w)
+                        : "r"(in + 16 * n * (p.slice + kPad) + c * 128 + 16 * h), "r"(n == kTiles - 1 ? real : 1u));
+                    mma(part[c][n], upper[c][0], b.x, b.y);
+                    mma(part[c][n], upper[c][1], b.z, b.w);
                     if constexpr (kF32) {  // lower parts of levels with upper parts of inputs
                         if (r & 1) b = make_uint4(0, 0, 0, 0);
-                        mma(part[n], lower[0], b.x, b.y);
-                        mma(part[n], lower[1], b.z, b.w);
+                        mma(part[c][n], lower[c][0], b.x, b.y);
+                        mma(part[c][n], lower[c][1], b.z, b.w);
                     }
                 }
+        }
+#pragma unroll
+        for (int c = 0; c < kCount; ++c)
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[n][i] = fmaf(part[c][n][i], scale[c][i / 2], acc[n][i]);
+    };
+    using One = std::integral_constant<int, 1>;
+    using Two = std::integral_constant<int, 2>;
+    const int kWarp = p.rows * kRed;  // floats of a warp's sums
+    const auto together = [&]() {     // the warps of a tile
+        if (p.ways == 1) __syncwarp();
+        else asm volatile("bar.sync %0, %1;" ::"r"(1 + mine), "r"(32 * p.ways) : "memory");
+    };
+    int stage_now = 0, slot = 0, held = 0;  // held: rounds whose sums are kept
+    for (int round = 0; round < rounds;) {
+        if (!idle) {
+#pragma unroll 1
+            for (int j = 0; j < each; ++j) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(S::kAhead - 1) : "memory");
+                __syncwarp();
+                const int span = way + p.ways * j, here = min(kSpan, blocks - span * kSpan);
+                const char* stage = staged + stage_now * S::kStage;
+                int first = 0;
+                if constexpr (kTiles <= 2) {  // two blocks at a time: their reads and products do not wait for one another
+#pragma unroll 1
+                    for (; first + 1 < here; first += 2) work(stage, span, first, Two());
+                }
+#pragma unroll 1
+                for (; first < here; ++first) work(stage, span, first, One());
+                __syncwarp();
+                ask(stage_now);
+                stage_now = stage_now == S::kAhead - 1 ? 0 : stage_now + 1;
             }
-            const float* power = powers + block * 64 / kScaled * padded + 2 * t;
+            float* here = sums + (slot * kMatWarps + warp) * kWarp;
 #pragma unroll
             for (int n = 0; n < kTiles; ++n) {
-                const float2 f = *reinterpret_cast<const float2*>(power + 8 * n);
-                acc[n][0] = fmaf(part[n][0], low_scale * f.x, acc[n][0]);
-                acc[n][1] = fmaf(part[n][1], low_scale * f.y, acc[n][1]);
-                acc[n][2] = fmaf(part[n][2], high_scale * f.x, acc[n][2]);
-                acc[n][3] = fmaf(part[n][3], high_scale * f.y, acc[n][3]);
+                if constexpr (kF32) {
+                    if (4 * n + t < p.rows) {
+                        here[(4 * n + t) * kRed + r] = acc[n][0] + acc[n][1];
+                        here[(4 * n + t) * kRed + r + 8] = acc[n][2] + acc[n][3];
+                    }
+                } else {
+                    if (8 * n + 2 * t < p.rows) {
+                        here[(8 * n + 2 * t) * kRed + r] = acc[n][0];
+                        here[(8 * n + 2 * t) * kRed + r + 8] = acc[n][2];
+                    }
+                    if (8 * n + 2 * t + 1 < p.rows) {
+                        here[(8 * n + 2 * t + 1) * kRed + r] = acc[n][1];
+                        here[(8 * n + 2 * t + 1) * kRed + r + 8] = acc[n][3];
+                    }
+                }
+                acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
             }
         }
-        __syncwarp();
-        ask(stage_now);
-        stage_now = stage_now == S::kAhead - 1 ? 0 : stage_now + 1;
-        if (++j < each) continue;
-        // the tile's sums: each warp's, then all of them in the order of the ways
-        j = 0;
-        constexpr int kWarp = S::kOut * kRed;
-        float* buffer = sums + (S::kBuffers == 2 ? round & 1 : 0) * (kMatWarps * kWarp);
-        float* here = buffer + warp * kWarp;
-#pragma unroll
-        for (int n = 0; n < kTiles; ++n) {
-            if constexpr (kF32) {
-                here[(4 * n + t) * kRed + r] = acc[n][0] + acc[n][1];
-                here[(4 * n + t) * kRed + r + 8] = acc[n][2] + acc[n][3];
-            } else {
-                here[(8 * n + 2 * t) * kRed + r] = acc[n][0];
-                here[(8 * n + 2 * t + 1) * kRed + r] = acc[n][1];
-                here[(8 * n + 2 * t) * kRed + r + 8] = acc[n][2];
-                here[(8 * n + 2 * t + 1) * kRed + r + 8] = acc[n][3];
-            }
-            acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
-        }
-        const auto together = [&]() {  // the warps of a tile
-            if (p.ways == 1) __syncwarp();
-            else asm volatile("bar.sync %0, %1;" ::"r"(1 + mine), "r"(32 * p.ways) : "memory");
-        };
-        together();
-        const int tile = first_tile + round * stride + mine;
-        const float* parts = buffer + mine * p.ways * kWarp;
-        for (int i = 32 * way + lane; i < results * 16; i += 32 * p.ways) {
-            const int column = i >> 4, row = i & 15;
-            float v = 0.0f;
-            for (int w = 0; w < p.ways; ++w) v += parts[w * kWarp + column * kRed + row];
-            if (ranks > 1) kept[((held * p.at_once + mine) * S::kOut + column) * 16 + row] = v;
-            else store(tile, column, row, v);
-        }
-        if constexpr (S::kBuffers == 1) together();
         ++round;
-        if (ranks == 1 || (++held * p.at_once < p.kept && round < rounds)) continue;
+        if (++slot < p.slots && round < rounds) continue;
+        // the sums of `slot` rounds' tiles: all warps' in the order of the ways
+        if (!idle) {
+            together();
+            for (int i = 32 * way + lane; i < slot * p.rows * 16; i += 32 * p.ways) {
+                const int k = i / (p.rows * 16), column = i / 16 - k * p.rows, row = i & 15;
+                const float* parts = sums + (k * kMatWarps + mine * p.ways) * kWarp + column * kRed + row;
+                float v = 0.0f;
+#pragma unroll 4
+                for (int w = 0; w < p.ways; ++w) v += parts[w * kWarp];
+                v *= powers[column];
+                if (ranks > 1) kept[(((held + k) * p.at_once + mine) * p.rows + column) * 16 + row] = v;
+                else store(first_tile + (round - slot + k) * stride + mine, column, row, v);
+            }
+            together();
+        }
+        held += slot;
+        slot = 0;
+        if (ranks == 1 || ((held + p.slots) * p.at_once <= p.kept && round < rounds)) continue;
         cluster.sync();
-        const int values = held * p.at_once * results * 16;
+        const int values = held * p.at_once * p.rows * 16;
         for (int i = rank * kMatThreads + static_cast<int>(threadIdx.x); i < values; i += ranks * kMatThreads) {
-            const int row = i & 15, column = (i >> 4) % results, k = (i >> 4) / results;
-            const int at = (k * S::kOut + column) * 16 + row;
+            const int row = i & 15, column = (i >> 4) % p.rows, k = (i >> 4) / p.rows;
             float v = 0.0f;
-            for (int w = 0; w < ranks; ++w) v += *cluster.map_shared_rank(kept + at, w);
+            for (int w = 0; w < ranks; ++w) v += *cluster.map_shared_rank(kept + i, w);
             store(first_tile + (round - held + k / p.at_once) * stride + k % p.at_once, column, row, v);
         }
         cluster.sync();  // until every CTA's memory has been read
@@ -422,26 +467,33 @@ cudaError_t launch_tiles(Params p, int ranks, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     using S = Shape<T, kTiles>;
     const int tiles = (p.m.out + 15) / 16, blocks = p.slice / 64;
-    // How many warps split a slice: what leaves the fewest of them waiting, for one another's blocks and for the last tiles
+    // How many warps split a slice: what leaves the fewest of them waiting, for one another's spans, for the last tiles and
+    // for want of a tile (three warps of 16 without one cost less than a tile in three of a round)
+    const int spans = (blocks + S::kSpan - 1) / S::kSpan;
     double best = 0.0;
-    for (int ways = kMatWarps; ways >= 1; ways /= 2) {
-        const int at_once = kMatWarps / ways, each = (blocks + ways - 1) / ways, rounds = (tiles + at_once * clusters - 1) / (at_once * clusters);
-        const double busy = static_cast<double>(blocks) / (static_cast<double>(each) * ways) * tiles / (static_cast<double>(rounds) * at_once * clusters);
-        if (busy <= best * 1.02) continue;
+    for (int ways = kMatWarps; ways >= 1; --ways) {
+        const int at_once = kMatWarps / ways, each = (spans + ways - 1) / ways, rounds = (tiles + at_once * clusters - 1) / (at_once * clusters);
+        const double busy = static_cast<double>(spans) / (static_cast<double>(each) * ways) * tiles / (static_cast<double>(rounds) * at_once * clusters) *
+                            (0.5 + 0.5 * ways * at_once / kMatWarps);
+        if (busy <= best * 1.01) continue;
         best = busy;
         p.ways = ways;
         p.at_once = at_once;
     }
     const int used = (tiles + p.at_once - 1) / p.at_once < clusters ? (tiles + p.at_once - 1) / p.at_once : clusters;
     const int rounds = (tiles + p.at_once * used - 1) / (p.at_once * used);
+    // sums of as many rounds as there is room for are joined at a time, and kept until the cluster joins them
+    const int room = kMostShared - layout_of<S>(p.rows, p.columns, p.slice, 0, 0).all, round_bytes = kMatWarps * p.rows * kRed * 4;
+    const int tile_bytes = ranks > 1 ? p.rows * 16 * 4 : 0;
+    p.slots = rounds;
+    while (p.slots > 1 && p.slots * (round_bytes + p.at_once * tile_bytes) > (room < 48 * 1024 ? room : 48 * 1024)) --p.slots;
     p.kept = 0;
     if (ranks > 1) {
-        const int room = (kMostShared - layout_of<S>(p.columns, p.slice, 0).all) / (S::kOut * 16 * 4);
-        const int want = rounds * p.at_once, fits = room / p.at_once * p.at_once;
-        p.kept = want < fits ? want : fits;
-        if (p.kept < p.at_once) return cudaErrorInvalidConfiguration;
+        const int most = (room - p.slots * round_bytes) / tile_bytes, want = (rounds + p.slots - 1) / p.slots * p.slots * p.at_once;
+        p.kept = want < most ? want : most;
+        if (p.kept < p.slots * p.at_once) return cudaErrorInvalidConfiguration;
     }
-    const int shared = layout_of<S>(p.columns, p.slice, p.kept).all;
+    const int shared = layout_of<S>(p.rows, p.columns, p.slice, p.slots, p.kept).all;
     return launch(q4_matmul_kernel<T, kTiles>, used * ranks, kMatThreads, shared, ranks, s, p);
 }
 
@@ -468,7 +520,7 @@ cudaError_t launch_t(Params p, cudaStream_t s) {
     // at a time where eight do not
     const auto fits = [&](int rows, int ranks) {
         const int slice = (m.in / 64 + ranks - 1) / ranks * 64;
-        return with_tiles(rows * each, [&](auto tiles) { return layout_of<Shape<T, tiles.value>>(rows * each, slice, ranks > 1 ? 16 : 0).all <= kMostShared; });
+        return with_tiles(rows * each, [&](auto tiles) { return layout_of<Shape<T, tiles.value>>(rows, rows * each, slice, 1, ranks > 1 ? kMatWarps : 0).all <= kMostShared; });
     };
     int rows = m.n < kMostColumns / each ? m.n : kMostColumns / each, ranks = 1;
     for (;; rows = (rows + 1) / 2) {
