@@ -542,10 +542,16 @@ uint64_t jb_cache_keep_workspace(const jb_trees* trees);
  *   d_bias        [out_features], or NULL
  *   d_y           [n][out_features], rows y_row_stride elements apart; shares no byte with what is
  *                 read: JB_ERR_INVALID_ARG
+ *   workspace     jb_q4_matmul_workspace(...) bytes, 16-byte aligned, contents free; NULL where that
+ *                 is 0. Calls that may run at the same time need one each.
  * Made for few rows: the weights are read once for each 64 of them at most.
  */
 int jb_q4_matmul(const jb_q4_segment* weights, int out_features, int in_features, int dtype, const void* d_x, uint64_t x_row_stride,
-                 int n, const void* d_bias, void* d_y, uint64_t y_row_stride, struct CUstream_st* stream);
+                 int n, const void* d_bias, void* d_y, uint64_t y_row_stride, void* workspace, uint64_t workspace_bytes,
+                 struct CUstream_st* stream);
+
+/* Device bytes that jb_q4_matmul works in; 0 for small products. */
+uint64_t jb_q4_matmul_workspace(int out_features, int in_features, int dtype, int n);
 
 /* ---------------------------------------------------------------------------
  * Test hooks (not on the hot path). Device buffers are caller-owned.

@@ -154,7 +154,9 @@ def lib() -> ctypes.CDLL:
                                           vp, i32, vp]
             L.jb_attend_tree.argtypes = [vp, vp, vp, vp, vp, u64, u64, i32, vp, u64, u64, vp, u64, vp]
             L.jb_cache_keep.argtypes = [vp, vp, i32, vp, vp, vp, vp, u64, vp]
-            L.jb_q4_matmul.argtypes = [vp, i32, i32, i32, vp, u64, i32, vp, vp, u64, vp]
+            L.jb_q4_matmul.argtypes = [vp, i32, i32, i32, vp, u64, i32, vp, vp, u64, vp, u64, vp]
+            L.jb_q4_matmul_workspace.argtypes = [i32, i32, i32, i32]
+            L.jb_q4_matmul_workspace.restype = u64
             L.jb_attend_tree_workspace.argtypes = [vp]
             L.jb_attend_tree_workspace.restype = u64
             L.jb_cache_keep_workspace.argtypes = [vp]
@@ -359,6 +361,17 @@ class Q4Table:
                 raise ValueError("codes or scales too short for numel")
             self.segments[i] = jb_q4_segment(codes.data_ptr(), scale.data_ptr(), int(numel), int(fo))
         self.n_segments = n
+        self._workspaces, self._matmul_bytes = _Workspaces(), {}
+
+    def matmul_workspace(self, out_features: int, in_features: int, dtype, n: int) -> int:
+        """Device bytes that jb_q4_matmul of n rows (of a torch type) with such a matrix works in."""
+        key = out_features, in_features, dtype, n
+        nbytes = self._matmul_bytes.get(key)
+        if nbytes is None:
+            if torch is None:
+                _need_torch()
+            nbytes = self._matmul_bytes[key] = int(lib().jb_q4_matmul_workspace(out_features, in_features, _storage(dtype), n))
+        return nbytes
 
 
 def jb_perturb_q4(table: "Q4Table", seed, eps: float, stream=None) -> None:
@@ -809,9 +822,10 @@ def jb_cache_keep(cache: KVCache, trees: DraftTrees, leaves, status=None, stream
     return status
 
 
-def jb_q4_matmul(table: "Q4Table", index: int, x, out_features: int, bias=None, out=None, stream=None):
+def jb_q4_matmul(table: "Q4Table", index: int, x, out_features: int, bias=None, out=None, workspace=None, stream=None):
     """Products of x [n, in_features] with tensor `index` of the table, a matrix [out_features, in_features] of 4-bit weights,
-    plus bias; returns ``out`` [n, out_features]. float32 or bfloat16; in_features a multiple of 64."""
+    plus bias; returns ``out`` [n, out_features]. float32 or bfloat16; in_features a multiple of 64. ``workspace``: by default
+    one that the table keeps for the stream; ``table.matmul_workspace`` says how many bytes another one needs."""
     if torch is None:
         _need_torch()
     device = x.get_device()
@@ -834,9 +848,18 @@ def jb_q4_matmul(table: "Q4Table", index: int, x, out_features: int, bias=None, 
     elif out.dtype is not x.dtype or out.get_device() != device or out.shape != (n, out_features) \
             or (out.stride(1) != 1 and out_features > 1):
         raise ValueError("out must be [n, out_features] of x's type on its CUDA device, contiguous in a row")
+    handle = _stream_on(device, stream)
+    nbytes, ws = table.matmul_workspace(out_features, inner, x.dtype, n), None
+    if workspace is not None:
+        if workspace.get_device() != device or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on x's CUDA device")
+        ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    elif nbytes:
+        ws, nbytes, held = table._workspaces.get("matmul", nbytes, stream, handle,
+                                                 lambda size: _new(stream, torch.empty, size, dtype=torch.uint8, device=x.device))
     segment = ctypes.byref(table.segments, index % table.n_segments * ctypes.sizeof(jb_q4_segment))
     _check(lib().jb_q4_matmul(segment, out_features, inner, dtype, x.data_ptr(), x.stride(0), n,
-                              None if bias is None else bias.data_ptr(), out.data_ptr(), out.stride(0), _stream_on(device, stream)))
+                              None if bias is None else bias.data_ptr(), out.data_ptr(), out.stride(0), ws, nbytes, handle))
     return out
 
 

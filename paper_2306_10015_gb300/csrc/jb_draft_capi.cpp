@@ -209,8 +209,14 @@ JB_EXPORT int jb_attend_tree(const jb_pages* pages, const jb_kv* layer, const jb
     });
 }
 
+JB_EXPORT uint64_t jb_q4_matmul_workspace(int out_features, int in_features, int dtype, int n) {
+    if ((dtype != JB_F32 && dtype != JB_BF16) || out_features < 1 || in_features < 64 || in_features % 64 != 0 || in_features > kMaxInner || n < 0) return 0;
+    return q4_workspace(n, out_features, in_features, dtype == JB_BF16);
+}
+
 JB_EXPORT int jb_q4_matmul(const jb_q4_segment* weights, int out_features, int in_features, int dtype, const void* d_x, uint64_t x_row_stride,
-                           int n, const void* d_bias, void* d_y, uint64_t y_row_stride, struct CUstream_st* stream) {
+                           int n, const void* d_bias, void* d_y, uint64_t y_row_stride, void* workspace, uint64_t workspace_bytes,
+                           struct CUstream_st* stream) {
     return guarded([&] {
         if (dtype != JB_F32 && dtype != JB_BF16) return static_cast<int>(JB_ERR_UNSUPPORTED_DTYPE);
         if (weights == nullptr || out_features < 1 || in_features < 64 || in_features % 64 != 0 || in_features > kMaxInner || n < 0 ||
@@ -232,7 +238,9 @@ JB_EXPORT int jb_q4_matmul(const jb_q4_segment* weights, int out_features, int i
         if ((n > 1 && y_row_stride < static_cast<uint64_t>(out_features)) || !apart(x, y) || !apart(codes, y) || !apart(scale, y) ||
             (d_bias != nullptr && !apart(bias, y)))
             return static_cast<int>(JB_ERR_INVALID_ARG);
-        const Q4Matmul m = {weights->codes, weights->scale, d_x, d_bias, d_y, x_row_stride, y_row_stride, n, out_features, in_features, dtype == JB_BF16};
+        const uint64_t need = q4_workspace(n, out_features, in_features, dtype == JB_BF16);
+        if (need > 0) JB_TRY(check_workspace(workspace, workspace_bytes, need));
+        const Q4Matmul m = {weights->codes, weights->scale, d_x, d_bias, d_y, x_row_stride, y_row_stride, workspace, n, out_features, in_features, dtype == JB_BF16};
         return cuda_status(launch_q4_matmul(m, stream));
     });
 }

@@ -227,25 +227,27 @@ __global__ void __launch_bounds__(kMatThreads, 1) q4_matmul_kernel(const __grid_
     int ahead_round = 0, ahead_j = 0;
     const auto ask = [&](int stage) {
         if (ahead_round < rounds && !idle) {
-            const int row = (first_tile + ahead_round * stride + mine) * 16, block = (way + p.ways * ahead_j) * kSpan;
-            const uint64_t column = from + 64ull * block;
+            const int row = (first_tile + ahead_round * stride + mine) * 16, last = m.out - 1 - row, block = (way + p.ways * ahead_j) * kSpan;
+            const int64_t at = static_cast<int64_t>(row) * m.in + from + 64 * block;
             if (block + lane % kLanes / 2 < blocks) {
                 const uint32_t to = code_to + stage * S::kStage;
+                const uint8_t* codes = m.codes + at / 2 + lane % kLanes * 16;
 #pragma unroll
                 for (int k = 0; k < 16; k += kRows) {
-                    const uint8_t* codes = m.codes + (static_cast<uint64_t>(min(row + k + lane / kLanes, m.out - 1)) * m.in + column) / 2 + lane % kLanes * 16;
+                    const uint8_t* here = codes + static_cast<int64_t>(min(k + lane / kLanes, last)) * (m.in / 2);
                     if (whole) {
-                        copy16(to + k * S::kPitch, codes);
+                        copy16(to + k * S::kPitch, here);
                     } else {
-                        copy8(to + k * S::kPitch, codes);
-                        copy8(to + k * S::kPitch + 8, codes + 8);
+                        copy8(to + k * S::kPitch, here);
+                        copy8(to + k * S::kPitch + 8, here + 8);
                     }
                 }
             }
             if (block + lane % kSpan < blocks) {
+                const float* scales = m.scale + at / 64 + lane % kSpan;
 #pragma unroll
                 for (int k = 0; k < 16; k += kScaleRows)
-                    copy4(scale_to + stage * S::kStage + k * 4, m.scale + (static_cast<uint64_t>(min(row + k + lane / kSpan, m.out - 1)) * m.in + column) / 64 + lane % kSpan);
+                    copy4(scale_to + stage * S::kStage + k * 4, scales + static_cast<int64_t>(min(k + lane / kSpan, last)) * (m.in / 64));
             }
             if (++ahead_j == each) {
                 ahead_j = 0;
@@ -301,7 +303,8 @@ __global__ void __launch_bounds__(kMatThreads, 1) q4_matmul_kernel(const __grid_
         const uint32_t in = inputs + (span * kSpan + first) * 128;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {  // 8 columns of a lane's 16
-            uint32_t upper[kCount][2][4], lower[kCount][2][4];  // of two products
+            uint32_t upper[kCount][2][4];  // of two products
+            [[maybe_unused]] uint32_t lower[kCount][2][4];
 #pragma unroll
             for (int c = 0; c < kCount; ++c)
 #pragma unroll
@@ -541,6 +544,7 @@ cudaError_t launch_t(Params p, cudaStream_t s) {
 }  // namespace
 
 cudaError_t launch_q4_matmul(const Q4Matmul& m, cudaStream_t s) {
+    if (q4_by_tiles(m.n, m.out, m.in) && reinterpret_cast<uint64_t>(m.codes) % 16 == 0) return launch_q4_tiles(m, s);
     Params p;
     p.m = m;
     q4_levels_host(p.levels);

@@ -1,0 +1,537 @@
+// jb_q4_tiles.cu -- large products with 4-bit weights on tcgen05: tiles of 128 rows of the matrix by all rows of x.
+//
+// Three kernels. The first converts x: to fp16, scaled by a power of two for each row so that the largest is near 2^15 (fp32:
+// an upper and a lower part, which are rows of their own; see jb_q4_matmul.cu for what that keeps). The second multiplies: the
+// matrix's 128-row tiles, 256 columns (four blocks) at a time, are one line of steps, of which every CTA takes an equal
+// stretch; sums of what a CTA has of a tile go to the workspace. The third adds them up in the order of the line, multiplies
+// by the power of two and adds the bias.
+//
+// In the second kernel codes and converted inputs come by TMA, in rows of 128 bytes. Eight warps turn codes into numbers: a
+// thread has a row, reads its block's 32 bytes, and a table with a copy for each lane gives each byte's two levels as two
+// fp16, which go to tensor memory (levels never pass through shared memory again). One warp issues the block's products, 64
+// columns deep, the levels from tensor memory, the inputs from shared memory; four warps take the block's sums from tensor
+// memory and add them up in fp32, times the block's scale, a thread a row. So a scale is applied in fp32 and once, and a
+// weight's level enters with fp16's 11 bits (fp32: 22, from two products).
+//
+// Reads of the table bound it: 16 turns of the pipe that serves shared memory for 16 rows by 64 columns, of about 31.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "jb_draft.h"
+#include "jb_internal.h"
+#include "jb_launch.cuh"
+#include "jb_tcgen05.cuh"
+#include "jb_tensor_map.h"
+
+namespace jb {
+namespace {
+
+constexpr unsigned kAll = 0xFFFFFFFFu;
+constexpr int kRows = 128, kStepBlocks = 4;
+constexpr int kDecodeWarps = 8, kSumWarps = 4;
+constexpr int kTileThreads = 32 * (kDecodeWarps + kSumWarps + 2);
+constexpr int kMostRows = 64;           // rows of x at a time
+constexpr int kBuffersA = 4;            // blocks of levels in tensor memory
+constexpr float kLevelScale = 1024.0f;  // of fp32's levels, so that their lower parts are normal numbers
+constexpr int kTileCtas = 160;          // most
+
+// Rows of converted x: n rounded up to a product's 16 columns, upper parts and then lower parts.
+__host__ __device__ constexpr int padded_rows(int n) { return (n + 15) / 16 * 16; }
+
+struct Line {  // of steps
+    int steps, each, extra;  // of a tile; of a CTA, and the first `extra` CTAs one more
+    __host__ __device__ long long bound(int w) const { return static_cast<long long>(each) * w + (w < extra ? w : extra); }
+    __host__ __device__ int owner(long long x) const {
+        const long long longer = (each + 1ll) * extra;
+        return static_cast<int>(x < longer ? x / (each + 1) : extra + (x - longer) / each);
+    }
+};
+
+struct TileParams {
+    CUtensorMap codes, inputs;
+    Q4Matmul m;
+    float levels[16];
+    Line line;
+    int rows, pad;    // rows of x in this pass, and what they are padded to
+    int first;        // row of x
+    int parts;        // most parts of a tile
+    __half* converted;  // [2 pad or pad][in]
+    float* powers;      // [pad]
+    float* sums;        // [tile][part][row of x][row of the matrix]
+};
+
+__device__ __forceinline__ uint32_t halves(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+__device__ __forceinline__ void read8(const float* from, float (&x)[8]) {
+    const float4 a = reinterpret_cast<const float4*>(from)[0], b = reinterpret_cast<const float4*>(from)[1];
+    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+}
+__device__ __forceinline__ void read8(const __nv_bfloat16* from, float (&x)[8]) {
+    const uint4 v = *reinterpret_cast<const uint4*>(from);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[2 * e] = __uint_as_float(w[e] << 16);
+        x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+    }
+}
+
+// A CTA a row of x; rows past the last are zeros.
+template <typename T>
+__global__ void __launch_bounds__(512) q4_convert_kernel(const __grid_constant__ TileParams p) {
+    constexpr bool kF32 = sizeof(T) == 4;
+    constexpr int kKept = 4;  // pieces of 8 that a thread keeps between its two looks
+    __shared__ float most_of[16];
+    after_previous();
+    let_next_start();
+    const int row = blockIdx.x, in = p.m.in, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const T* x = static_cast<const T*>(p.m.x) + (p.first + row) * p.m.x_row;
+    const bool real = row < p.rows;
+    float v[kKept][8];
+    float most = 0.0f;
+    const auto look = [&](const float (&w)[8]) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = fmaxf(most, isfinite(w[i]) ? fabsf(w[i]) : 0.0f);
+    };
+#pragma unroll
+    for (int u = 0; u < kKept; ++u) {
+        const int k = 8 * (threadIdx.x + 512 * u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[u][i] = 0.0f;
+        if (real && k < in) read8(x + k, v[u]);
+        look(v[u]);
+    }
+    for (int k = 8 * (threadIdx.x + 512 * kKept); real && k < in; k += 8 * 512) {
+        float w[8];
+        read8(x + k, w);
+        look(w);
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d /= 2) most = fmaxf(most, __shfl_xor_sync(kAll, most, d));
+    if (lane == 0) most_of[warp] = most;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) most = fmaxf(most, most_of[i]);
+    // most in [2^e, 2^(e+1)) becomes [2^14, 2^15); powers of two that fp32 has with their inverses
+    const int e = most > 0.0f ? min(max((__float_as_int(most) >> 23) - 127 - 14, -126), 126) : 0;
+    const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+    if (threadIdx.x == 0) p.powers[row] = __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * (kF32 ? 1.0f / kLevelScale : 1.0f);
+    __half* upper = p.converted + static_cast<size_t>(row) * in;
+    __half* lower = upper + static_cast<size_t>(p.pad) * in;
+    const auto convert = [&](const float (&w)[8], int k) {
+        uint32_t a[4], b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float lo = w[2 * i] * down, hi = w[2 * i + 1] * down;
+            a[i] = halves(lo, hi);
+            if (kF32) {  // what is not finite is all lower part: the lower parts of levels, which may be 0, do not meet it
+                a[i] = halves(isfinite(lo) ? lo : 0.0f, isfinite(hi) ? hi : 0.0f);
+                const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&a[i]));
+                b[i] = halves(lo - h.x, hi - h.y);
+            }
+        }
+        *reinterpret_cast<uint4*>(upper + k) = make_uint4(a[0], a[1], a[2], a[3]);
+        if (kF32) *reinterpret_cast<uint4*>(lower + k) = make_uint4(b[0], b[1], b[2], b[3]);
+    };
+#pragma unroll
+    for (int u = 0; u < kKept; ++u) {
+        const int k = 8 * (threadIdx.x + 512 * u);
+        if (k < in) convert(v[u], k);
+    }
+    for (int k = 8 * (threadIdx.x + 512 * kKept); k < in; k += 8 * 512) {
+        float w[8] = {};
+        if (real) read8(x + k, w);
+        convert(w, k);
+    }
+}
+
+// kPad: rows of x, padded.
+template <typename T, int kPad>
+struct Tiles {
+    static constexpr bool kF32 = sizeof(T) == 4;
+    static constexpr int kColumns = kF32 ? 2 * kPad : kPad;      // of a product
+    static constexpr int kLevels = kF32 ? 64 : 32;               // columns of tensor memory of a block's levels
+    static constexpr int kSums = kBuffersA * kLevels;            // where sums begin
+    static constexpr int kBuffersD = (512 - kSums) / kColumns >= 4 ? 4 : 2;
+    static constexpr uint32_t kCodeBytes = kRows * 128, kInputBytes = kColumns * 128, kStageBytes = kCodeBytes + kStepBlocks * kInputBytes;
+    static constexpr int kStages = 160 * 1024 / kStageBytes >= 4 ? 4 : 160 * 1024 / kStageBytes >= 3 ? 3 : 2;
+    static constexpr uint32_t kTable = 65536;
+    static constexpr int kShared = 1024 + kTable + kStages * kStageBytes;
+    static_assert(kSums + kBuffersD * kColumns <= 512 && kShared <= 226 * 1024);
+};
+
+struct TileControl {
+    unsigned long long full[4], empty[4], levels[kBuffersA], levels_read[kBuffersA], sums[4], sums_read[4], drained;
+    uint32_t tmem;
+    int failed;
+};
+
+template <typename T, int kPad>
+__global__ void __launch_bounds__(kTileThreads, 1) q4_tiles_kernel(const __grid_constant__ TileParams p) {
+    using S = Tiles<T, kPad>;
+    constexpr bool kF32 = S::kF32;
+    extern __shared__ char dynamic[];
+    __shared__ TileControl c;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t base = (shared_address(dynamic) + 1023) & ~1023u, table = base, stages = base + S::kTable;
+    char* const table_at = dynamic + (base - shared_address(dynamic));
+    {   // the table: 256 bytes for each byte of codes, with a copy of its two levels for each lane
+        for (int i = threadIdx.x; i < 256 * 16; i += kTileThreads) {
+            const int byte = i / 16, quad = i % 16;
+            if (!kF32 && quad >= 8) continue;
+            const float scale = kF32 ? kLevelScale : 1.0f, a = p.levels[byte & 15] * scale, b = p.levels[byte >> 4] * scale;
+            const uint32_t w = halves(a, b);
+            const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&w));
+            const uint32_t v = kF32 ? halves(a - h.x, b - h.y) : w;
+            *reinterpret_cast<uint4*>(table_at + byte * 256 + quad * 16) = make_uint4(w, v, w, v);
+        }
+    }
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 4; ++i) {
+            barrier_init(shared_address(&c.full[i]), 1);
+            barrier_init(shared_address(&c.empty[i]), kDecodeWarps + 1);
+            barrier_init(shared_address(&c.levels[i]), kDecodeWarps / 2);
+            barrier_init(shared_address(&c.levels_read[i]), 1);
+            barrier_init(shared_address(&c.sums[i]), 1);
+            barrier_init(shared_address(&c.sums_read[i]), kSumWarps);
+        }
+        barrier_init(shared_address(&c.drained), 1);
+        c.failed = 0;
+        barriers_initialized();
+    }
+    if (warp == kDecodeWarps + kSumWarps) tmem_alloc(shared_address(&c.tmem), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    after_previous();
+    let_next_start();
+    const uint32_t tmem = c.tmem;
+    const Q4Matmul& m = p.m;
+    const int blocks = m.in / 64, steps = p.line.steps;
+    const long long begin = p.line.bound(blockIdx.x), end = p.line.bound(blockIdx.x + 1);
+    const auto blocks_of = [&](int step) { return min(kStepBlocks, blocks - step * kStepBlocks); };
+    const auto wait = [&](unsigned long long* bar, uint32_t parity) { return __all_sync(kAll, barrier_wait(shared_address(bar), parity, &c.failed)); };
+
+    if (warp < kDecodeWarps) {  // codes to levels: groups of four warps take blocks in turn
+        const int group = warp >> 2, row = threadIdx.x & 127;
+        const uint32_t place = lane * (kF32 ? 8 : 4), to = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16);
+        uint32_t block = 0, stage = 0;
+        int step = static_cast<int>(begin % steps);
+        bool ok = true;
+        for (long long x = begin; ok && x < end; ++x, ++stage) {
+            const uint32_t slot = stage % S::kStages;
+            ok = wait(&c.full[slot], stage / S::kStages & 1);
+            const int here = blocks_of(step);
+            const uint32_t codes = stages + slot * S::kStageBytes + row * 128;
+            for (int b = 0; ok && b < here; ++b, ++block) {
+                if ((block & 1) != static_cast<uint32_t>(group)) continue;
+                const uint32_t buffer = block % kBuffersA;
+                ok = wait(&c.levels_read[buffer], (block / kBuffersA & 1) ^ 1);
+                tc_fence_after();
+#pragma unroll 1
+                for (int half = 0; half < 2; ++half) {  // 16 bytes of the block's 32
+                    uint32_t w[4], upper[16];
+                    [[maybe_unused]] uint32_t lower[16];
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                                 : "r"(codes + (((2 * b + half) ^ (row & 7)) << 4)) : "memory");
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const uint32_t at = __byte_perm(w[e / 4], place, 0x5504 | e % 4 << 4) + table;  // place, the byte, 0, 0
+                        if constexpr (kF32) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(upper[e]), "=r"(lower[e]) : "r"(at) : "memory");
+                        else asm volatile("ld.shared.b32 %0, [%1];" : "=r"(upper[e]) : "r"(at) : "memory");
+                    }
+                    tmem_store16(to + buffer * S::kLevels + 16 * half, upper);
+                    if constexpr (kF32) tmem_store16(to + buffer * S::kLevels + 32 + 16 * half, lower);
+                }
+                tc_wait_stores();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) barrier_arrive(shared_address(&c.levels[buffer]));
+            }
+            __syncwarp();
+            if (lane == 0) barrier_arrive(shared_address(&c.empty[slot]));
+            if (++step == steps) step = 0;
+        }
+    } else if (warp < kDecodeWarps + kSumWarps) {  // sums of blocks, times their scales
+        const int row = threadIdx.x & 127;
+        const uint32_t from = tmem + S::kSums + (static_cast<uint32_t>(32 * (warp & 3)) << 16);
+        float acc[kPad];
+#pragma unroll
+        for (int i = 0; i < kPad; ++i) acc[i] = 0.0f;
+        uint32_t block = 0;
+        int step = static_cast<int>(begin % steps), tile = static_cast<int>(begin / steps);
+        float next[kStepBlocks];
+        const auto scales_of = [&](int at_tile, int at_step) {
+            const int o = at_tile * kRows + row;
+            const float* scale = m.scale + static_cast<int64_t>(o) * blocks + at_step * kStepBlocks;
+#pragma unroll
+            for (int b = 0; b < kStepBlocks; ++b) next[b] = 0.0f;
+            if (o >= m.out) return;
+            if (blocks % 4 == 0 && reinterpret_cast<uint64_t>(m.scale) % 16 == 0) {
+                const float4 v = __ldg(reinterpret_cast<const float4*>(scale));
+                next[0] = v.x, next[1] = v.y, next[2] = v.z, next[3] = v.w;
+            } else {
+#pragma unroll
+                for (int b = 0; b < kStepBlocks; ++b)
+                    if (b < blocks_of(at_step)) next[b] = __ldg(scale + b);
+            }
+        };
+        if (begin < end) scales_of(tile, step);
+        bool ok = true;
+        for (long long x = begin; x < end; ++x) {
+            const int here = blocks_of(step);
+            float scale[kStepBlocks];
+#pragma unroll
+            for (int b = 0; b < kStepBlocks; ++b) scale[b] = next[b];
+            const int this_tile = tile;
+            if (++step == steps) {
+                step = 0;
+                ++tile;
+            }
+            if (x + 1 < end) scales_of(tile, step);
+#pragma unroll
+            for (int b = 0; b < kStepBlocks; ++b) {
+                if (b >= here) break;
+                const uint32_t buffer = block % S::kBuffersD;
+                ok = wait(&c.sums[buffer], block / S::kBuffersD & 1) && ok;
+                tc_fence_after();
+                ++block;
+#pragma unroll
+                for (int i = 0; i < kPad; i += 16) {
+                    uint32_t d[16];
+                    tmem_load16(from + buffer * S::kColumns + i, d);
+                    tc_wait_loads();
+                    if constexpr (kF32) {
+                        uint32_t l[16];
+                        tmem_load16(from + buffer * S::kColumns + kPad + i, l);
+                        tc_wait_loads();
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) d[k] = __float_as_uint(__uint_as_float(d[k]) + __uint_as_float(l[k]));
+                    }
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) acc[i + k] = fmaf(__uint_as_float(d[k]), scale[b], acc[i + k]);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) barrier_arrive(shared_address(&c.sums_read[buffer]));
+            }
+            if (step != 0 && x + 1 < end) continue;
+            // the tile's part, or all of it
+            const long long start = static_cast<long long>(this_tile) * steps;
+            const int part = static_cast<int>(blockIdx.x) - p.line.owner(start);
+            float* to = p.sums + (static_cast<size_t>(this_tile) * p.parts + part) * p.rows * kRows + row;
+#pragma unroll
+            for (int i = 0; i < kPad; ++i) {
+                if (i < p.rows) to[static_cast<size_t>(i) * kRows] = ok ? acc[i] : NAN;
+                acc[i] = 0.0f;
+            }
+        }
+    } else if (warp == kDecodeWarps + kSumWarps) {  // products
+        constexpr uint32_t kF16 = 1u << 4 | 128u >> 4 << 24;  // fp16, fp32 sums, 128 rows
+        constexpr uint32_t kBoth = kF16 | static_cast<uint32_t>(S::kColumns >> 3) << 17, kUpper = kF16 | static_cast<uint32_t>(kPad >> 3) << 17;
+        uint32_t block = 0, stage = 0;
+        int step = static_cast<int>(begin % steps);
+        bool ok = true;
+        for (long long x = begin; ok && x < end; ++x, ++stage) {
+            const uint32_t slot = stage % S::kStages;
+            ok = wait(&c.full[slot], stage / S::kStages & 1);
+            const int here = blocks_of(step);
+            for (int b = 0; ok && b < here; ++b, ++block) {
+                const uint32_t buffer = block % kBuffersA, sums = block % S::kBuffersD;
+                ok = wait(&c.levels[buffer], block / kBuffersA & 1) && wait(&c.sums_read[sums], (block / S::kBuffersD & 1) ^ 1);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t a = tmem + buffer * S::kLevels, d = tmem + S::kSums + sums * S::kColumns;
+                const uint32_t in = tile_descriptor(stages + slot * S::kStageBytes + S::kCodeBytes + b * S::kInputBytes, 16);
+                if (elected()) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) tc_product_from_tmem(d, a + 8 * k, in + (k * 32 >> 4), kBoth, k > 0);
+                    if constexpr (kF32) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) tc_product_from_tmem(d, a + 32 + 8 * k, in + (k * 32 >> 4), kUpper, true);
+                    }
+                    tc_commit(shared_address(&c.levels_read[buffer]));
+                    tc_commit(shared_address(&c.sums[sums]));
+                    if (b == here - 1) tc_commit(shared_address(&c.empty[slot]));
+                }
+                __syncwarp();
+            }
+            if (++step == steps) step = 0;
+        }
+        if (!ok && elected()) {  // what is under way ends before tensor memory is given back
+            int late = 0;
+            tc_commit(shared_address(&c.drained));
+            barrier_wait(shared_address(&c.drained), 0, &late);
+        }
+        __syncwarp();
+    } else {  // copies
+        uint32_t stage = 0;
+        int step = static_cast<int>(begin % steps), tile = static_cast<int>(begin / steps);
+        for (long long x = begin; x < end; ++x, ++stage) {
+            const uint32_t slot = stage % S::kStages, to = stages + slot * S::kStageBytes, bar = shared_address(&c.full[slot]);
+            if (!wait(&c.empty[slot], (stage / S::kStages & 1) ^ 1)) {
+                int late = 0;  // what is under way arrives first
+                for (uint32_t k = stage < S::kStages ? 0 : stage - S::kStages; k < stage; ++k) barrier_wait(shared_address(&c.full[k % S::kStages]), k / S::kStages & 1, &late);
+                break;
+            }
+            const int here = blocks_of(step);
+            if (lane == 0) barrier_arrive_bytes(bar, S::kCodeBytes + here * S::kInputBytes);
+            __syncwarp();
+            if (lane == 0) copy_box(to, &p.codes, step * 128, tile * kRows, 0, 0, bar);
+            else if (lane <= here) copy_box(to + S::kCodeBytes + (lane - 1) * S::kInputBytes, &p.inputs, (step * kStepBlocks + lane - 1) * 64, 0, 0, 0, bar);
+            if (++step == steps) {
+                step = 0;
+                ++tile;
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == kDecodeWarps + kSumWarps) tmem_free(c.tmem, 512);
+}
+
+// A thread a result.
+template <typename T>
+__global__ void __launch_bounds__(128) q4_join_kernel(const __grid_constant__ TileParams p) {
+    after_previous();
+    let_next_start();
+    const int tile = blockIdx.x, i = blockIdx.y, o = tile * kRows + static_cast<int>(threadIdx.x);
+    if (o >= p.m.out) return;
+    const long long start = static_cast<long long>(tile) * p.line.steps;
+    const int parts = p.line.owner(start + p.line.steps - 1) - p.line.owner(start) + 1;
+    const float* from = p.sums + (static_cast<size_t>(tile) * p.parts * p.rows + i) * kRows + threadIdx.x;
+    float v = 0.0f;
+#pragma unroll 4
+    for (int k = 0; k < parts; ++k) v += __ldcg(from + static_cast<size_t>(k) * p.rows * kRows);
+    v *= p.powers[i];
+    T* y = static_cast<T*>(p.m.y) + (p.first + i) * p.m.y_row + o;
+    if constexpr (sizeof(T) == 4) {
+        if (p.m.bias != nullptr) v += static_cast<const float*>(p.m.bias)[o];
+        *y = v;
+    } else {
+        if (p.m.bias != nullptr) v += __bfloat162float(static_cast<const __nv_bfloat16*>(p.m.bias)[o]);
+        *y = __float2bfloat16_rn(v);
+    }
+}
+
+int steps_of(int in) { return (in / 64 + kStepBlocks - 1) / kStepBlocks; }
+
+// CTAs that the line is dealt to, and most parts of a tile.
+Line line_of(int out, int in, int ctas) {
+    const long long total = static_cast<long long>((out + kRows - 1) / kRows) * steps_of(in);
+    return {steps_of(in), static_cast<int>(total / ctas), static_cast<int>(total % ctas)};
+}
+int parts_of(const Line& l) { return l.each == 0 ? l.steps : (l.steps + l.each - 1) / l.each + 1; }
+
+constexpr int kTileDevices = 64;
+cudaError_t sms_of(int& sms) {
+    static std::atomic<int> known[kTileDevices];
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    sms = device < kTileDevices ? known[device].load(std::memory_order_relaxed) : 0;
+    if (sms > 0) return cudaSuccess;
+    e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    if (e != cudaSuccess) return e;
+    if (sms > kTileCtas) sms = kTileCtas;
+    if (device < kTileDevices) known[device].store(sms, std::memory_order_relaxed);
+    return cudaSuccess;
+}
+
+cudaError_t describe(CUtensorMap& map, CUtensorMapDataType type, const void* at, cuuint64_t inner, cuuint64_t outer, cuuint64_t stride, cuuint32_t box_inner,
+                     cuuint32_t box_outer) {
+    Encode encode = nullptr;
+    const cudaError_t e = encoder(encode);
+    if (e != cudaSuccess) return e;
+    const cuuint64_t dims[4] = {inner, outer, 1, 1}, strides[3] = {stride, stride * outer, stride * outer};
+    const cuuint32_t boxes[4] = {box_inner, box_outer, 1, 1}, steps[4] = {1, 1, 1, 1};
+    const CUresult r = encode(&map, type, 4, const_cast<void*>(at), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+template <typename T, int kPad>
+cudaError_t launch_pad(const TileParams& p, int ctas, cudaStream_t s) {
+    using S = Tiles<T, kPad>;
+    static std::atomic<bool> ready[kTileDevices];
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    if (device >= kTileDevices || !ready[device].load(std::memory_order_relaxed)) {
+        e = cudaFuncSetAttribute(q4_tiles_kernel<T, kPad>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kShared);
+        if (e != cudaSuccess) return e;
+        if (device < kTileDevices) ready[device].store(true, std::memory_order_relaxed);
+    }
+    return launch(q4_tiles_kernel<T, kPad>, ctas, kTileThreads, S::kShared, 0, s, p);
+}
+
+template <typename T>
+cudaError_t launch_type(const Q4Matmul& m, cudaStream_t s) {
+    constexpr int kParts = sizeof(T) == 4 ? 2 : 1;
+    int sms = 0;
+    cudaError_t e = sms_of(sms);
+    if (e != cudaSuccess) return e;
+    TileParams p;
+    p.m = m;
+    q4_levels_host(p.levels);
+    const int tiles = (m.out + kRows - 1) / kRows;
+    const long long total = static_cast<long long>(tiles) * steps_of(m.in);
+    const int ctas = total < sms ? static_cast<int>(total) : sms;
+    p.line = line_of(m.out, m.in, ctas);
+    p.parts = parts_of(p.line);
+    e = describe(p.codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, m.codes, m.in / 2, m.out, m.in / 2, 128, kRows);
+    if (e != cudaSuccess) return e;
+    for (p.first = 0; p.first < m.n; p.first += kMostRows) {
+        p.rows = m.n - p.first < kMostRows ? m.n - p.first : kMostRows;
+        p.pad = padded_rows(p.rows);
+        char* ws = static_cast<char*>(m.ws);
+        p.converted = reinterpret_cast<__half*>(ws);
+        ws += static_cast<size_t>(kParts) * p.pad * m.in * 2;
+        p.powers = reinterpret_cast<float*>(ws);
+        p.sums = p.powers + kMostRows;
+        e = describe(p.inputs, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, p.converted, m.in, kParts * p.pad, m.in * 2, 64, kParts * p.pad);
+        if (e != cudaSuccess) return e;
+        e = launch(q4_convert_kernel<T>, p.pad, 512, 0, 0, s, p);
+        if (e != cudaSuccess) return e;
+        e = p.pad == 16 ? launch_pad<T, 16>(p, ctas, s) : p.pad == 32 ? launch_pad<T, 32>(p, ctas, s) : p.pad == 48 ? launch_pad<T, 48>(p, ctas, s) : launch_pad<T, 64>(p, ctas, s);
+        if (e != cudaSuccess) return e;
+        cudaLaunchConfig_t c = {};
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr.val.programmaticStreamSerializationAllowed = 1;
+        c.gridDim = dim3(tiles, p.rows);
+        c.blockDim = dim3(128);
+        c.stream = s;
+        c.attrs = &attr;
+        c.numAttrs = 1;
+        e = cudaLaunchKernelEx(&c, q4_join_kernel<T>, p);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+}  // namespace
+
+bool q4_by_tiles(int n, int out, int in) {
+    // three launches and a tile of 128 rows pay where the matrix is large, and the sooner the more rows x has
+    return n > 0 && static_cast<long long>(out) * in >= (1ll << 22);
+}
+
+uint64_t q4_workspace(int n, int out, int in, int bf16) {
+    if (!q4_by_tiles(n, out, in)) return 0;
+    const int rows = n < kMostRows ? n : kMostRows, tiles = (out + kRows - 1) / kRows;
+    const long long total = static_cast<long long>(tiles) * steps_of(in);
+    // parts are most with the most CTAs
+    const int parts = parts_of(line_of(out, in, static_cast<int>(total < kTileCtas ? total : kTileCtas)));
+    return static_cast<uint64_t>(bf16 ? 1 : 2) * padded_rows(rows) * in * 2 + 4ull * kMostRows + 4ull * tiles * parts * rows * kRows;
+}
+
+cudaError_t launch_q4_tiles(const Q4Matmul& m, cudaStream_t s) {
+    return m.bf16 ? launch_type<__nv_bfloat16>(m, s) : launch_type<float>(m, s);
+}
+
+}  // namespace jb

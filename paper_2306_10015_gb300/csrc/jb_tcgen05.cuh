@@ -36,7 +36,7 @@ __device__ __forceinline__ bool barrier_sleep(uint32_t bar, uint32_t parity) {
 // that finds it set: then all roles of the CTA leave their loops. Few polls: those of waiting warps took 40 % of all
 // instructions without sleep and with a look at the clock each.
 constexpr long long kPatience = 4000000000ll;  // cycles
-__device__ __noinline__ bool barrier_wait_long(uint32_t bar, uint32_t parity, volatile int* failed) {
+static __device__ __noinline__ bool barrier_wait_long(uint32_t bar, uint32_t parity, volatile int* failed) {
     const long long start = clock64();
     for (;;) {
         for (int i = 0; i < 32; ++i)

@@ -17,10 +17,10 @@
 #include <atomic>
 #include <numeric>
 
-#include <cuda.h>
 #include <cuda_bf16.h>
 
 #include "jb_tcgen05.cuh"
+#include "jb_tensor_map.h"
 #include "jb_tree.cuh"
 
 namespace jb {
@@ -597,23 +597,6 @@ cudaError_t resident(int shared, int each, int most, int& ctas) {
 
 template <int D>
 constexpr int max_ctas() { return 160 * Shape<D>::kCtas; }
-
-using Encode = decltype(&cuTensorMapEncodeTiled);
-
-// The driver's function that describes a tensor to the copies, asked for once.
-cudaError_t encoder(Encode& encode) {
-    static std::atomic<void*> known;
-    void* f = known.load(std::memory_order_acquire);
-    if (f == nullptr) {
-        cudaDriverEntryPointQueryResult found;
-        const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found);
-        if (e != cudaSuccess) return e;
-        if (found != cudaDriverEntryPointSuccess || f == nullptr) return cudaErrorNotSupported;
-        known.store(f, std::memory_order_release);
-    }
-    encode = reinterpret_cast<Encode>(f);
-    return cudaSuccess;
-}
 
 cudaError_t describe(CUtensorMap& map, const TreeParams& p, const char* pool, int box) {
     Encode encode = nullptr;

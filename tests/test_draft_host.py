@@ -129,9 +129,9 @@ def test_appends_that_share_bytes(jb):
     assert rc(turns=FAKE + 2) == bad and rc(turns=FAKE + 2, out=FAR) == bad
 
 
-def q4(jb, codes=FAKE, scale=FAKE + (1 << 30), numel=128 * 256, out=128, inner=256, dtype=1, x=FAR, xs=256, n=2, bias=0, y=FAR + (1 << 20), ys=128, none=False):
+def q4(jb, codes=FAKE, scale=FAKE + (1 << 30), numel=128 * 256, out=128, inner=256, dtype=1, x=FAR, xs=256, n=2, bias=0, y=FAR + (1 << 20), ys=128, none=False, ws=0, size=0):
     w = jb.jb_q4_segment(codes, scale, numel, 0)
-    return jb.lib().jb_q4_matmul(None if none else C.byref(w), out, inner, dtype, p(x), xs, n, p(bias), p(y), ys, None)
+    return jb.lib().jb_q4_matmul(None if none else C.byref(w), out, inner, dtype, p(x), xs, n, p(bias), p(y), ys, p(ws), size, None)
 
 
 def test_bad_products(jb):
@@ -143,6 +143,12 @@ def test_bad_products(jb):
                    (dict(xs=1 << 50), INV), (dict(ys=1 << 50), INV), (dict(ys=127), INV), (dict(y=FAR), INV), (dict(y=FAR + 510), INV), (dict(y=FAKE + 100), INV),
                    (dict(y=FAKE + (1 << 30)), INV), (dict(bias=FAR + (1 << 20) + 2), INV), (dict(x=(1 << 64) - 256), INV), (dict(codes=(1 << 64) - 1024), INV)):
         assert q4(jb, **kw) == rc, kw
+    need = lambda *a: jb.lib().jb_q4_matmul_workspace(*a)  # noqa: E731
+    assert need(128, 256, 1, 2) == 0 and need(4096, 4096, 2, 1) == 0 and need(4096, 4000, 1, 1) == 0 and need(0, 4096, 1, 1) == 0
+    big = dict(numel=4096 * 4096, out=4096, inner=4096, xs=4096, ys=4096, n=3, ws=FAKE, size=need(4096, 4096, 1, 3))
+    assert big["size"] > 3 * 4096 * 2
+    for kw, rc in ((dict(ws=0), INV), (dict(ws=FAKE + 8), MIS), (dict(size=big["size"] - 1), INV)):
+        assert q4(jb, **{**big, **kw}) == rc, kw
 
 
 def test_python_refuses(jb, monkeypatch):
@@ -183,7 +189,7 @@ def test_python_refuses(jb, monkeypatch):
     table = jb.Q4Table([(new(128 * 32, dtype=torch.uint8), new(128, dtype=f32), 128 * 64)])
     good = dict(x=new(3, 64, dtype=f32), out_features=128, bias=new(128, dtype=f32), out=new(3, 128, dtype=f32))
     for change in (dict(x=new(3, 64, dtype=f32, at=1)), dict(x=torch.zeros(3, 64)), dict(x=new(64, dtype=f32)), dict(x=new(64, 3, dtype=f32).T), dict(bias=new(64, dtype=f32)),
-                   dict(bias=new(128, dtype=torch.bfloat16)), dict(out=new(3, 127, dtype=f32)), dict(out=new(128, 3, dtype=f32).T), dict(out=new(3, 128, dtype=f32, at=1))):
+                   dict(bias=new(128, dtype=torch.bfloat16)), dict(out=new(3, 127, dtype=f32)), dict(out=new(128, 3, dtype=f32).T), dict(out=new(3, 128, dtype=f32, at=1)), dict(workspace=new(64, at=1))):
         calls.append(("jb_q4_matmul", (table, 0), {**good, **change}))
     elsewhere = jb.Q4Table([(new(128 * 32, dtype=torch.uint8, at=1), new(128, dtype=f32), 128 * 64)])
     calls.append(("jb_q4_matmul", (elsewhere, 0), good))

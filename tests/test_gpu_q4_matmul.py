@@ -1,8 +1,8 @@
 """jb_q4_matmul against the definition in 64 bits.
 
 Tolerance with A = sum_k |x_k w_k|: a term is a product of a level and an input. In bf16 a level enters with half a step of
-fp16, 2^-12, and inputs keep their 8 bits unless they are 2^-28 of the largest of their row and smaller (2^-40 of that one,
-covered below); in fp32 both enter with 2^-24 and their product drops less than 2^-23. The sum of K terms and the
+fp16, 2^-12, and inputs keep their 8 bits unless they are 2^-28 of the largest of their row and smaller (2^-40 of that one:
+far below the sum's own allowance); in fp32 both enter with 2^-24 and their product drops less than 2^-23. The sum of K terms and the
 products with scales lose at most (K / 16 + 70) 2^-23 of A in any order of blocks and lanes (16 terms a step of a tensor
 core, whose sums may truncate: 2^-22 a step), and a result is rounded once: 2^-8 of it for bf16 with the tie.
 """
@@ -72,6 +72,50 @@ def test_shapes(dtype, n, out, inner):
 @pytest.mark.parametrize("out,inner", [(40, 20480), (5, 65536), (17, 8256), (20000, 128)])
 def test_long_and_wide(dtype, n, out, inner):
     check(dtype, n, out, inner)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 33, 48, 64, 65, 100])
+@pytest.mark.parametrize("out,inner", [(4096, 1024), (1000, 4224), (65601, 64), (150, 32768), (130, 65536), (2049, 2112)])
+def test_matrices_that_are_cut_into_tiles(dtype, n, out, inner):
+    """Tiles of 128 rows: the last one ragged, columns that end inside a step of four blocks, tiles that many CTAs share and
+    CTAs that have many."""
+    check(dtype, n, out, inner, bias=n % 2 == 0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_tiles_strides_and_odd_scales(dtype):
+    """Rows inside wider ones and scales off a 16-byte boundary; codes off one, which take the other kernel."""
+    g = torch.Generator(device="cuda").manual_seed(4)
+    out, inner = 3000, 1536
+    codes = torch.randint(0, 256, (out * inner // 2 + 8,), dtype=torch.uint8, device="cuda", generator=g)
+    scale = torch.rand(out * inner // 64 + 3, device="cuda", generator=g)
+    x = torch.randn(6, inner + 80, device="cuda", generator=g).to(DT[dtype])[:, 40:40 + inner]
+    for skip, first in ((0, 3), (8, 0)):
+        table = jb.Q4Table([(codes[skip:skip + out * inner // 2], scale[first:first + out * inner // 64], out * inner)])
+        y = torch.full((6, out + 9), 4.0, dtype=DT[dtype], device="cuda")
+        got = jb.jb_q4_matmul(table, 0, x, out, out=y[:, 4:4 + out])
+        assert (y[:, :4] == 4).all() and (y[:, 4 + out:] == 4).all()
+        w = dense(table, 0, out, inner)
+        want = x.double() @ w.T
+        assert ((got.double() - want).abs() <= bound(x, w, None, want)).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_tiles_inputs_that_are_not_finite_or_of_all_sizes(dtype):
+    table = weights(2100, 2048)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(9, 2048, device="cuda", generator=g)
+    x *= torch.tensor([1e-38, 1e-30, 1e-10, 1e-3, 1.0, 1e10, 1e30, 1e35, 0.0], device="cuda")[:, None]
+    x[:, ::97] *= 100.0
+    x = x.to(DT[dtype])
+    clean = check(dtype, 9, 2100, 2048, bias=False, x=x, table=table)
+    x[1, 500], x[3, 70], x[4, 2047] = float("inf"), float("nan"), -float("inf")
+    got = jb.jb_q4_matmul(table, 0, x, 2100)
+    away = [0, 2, 5, 6, 7, 8]
+    assert torch.equal(got[away], clean[away])
+    want = x.double() @ dense(table, 0, 2100, 2048).T
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isinf(got), torch.isinf(want))
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
