@@ -13,7 +13,9 @@
 // memory and add them up in fp32, times the block's scale, a thread a row. So a scale is applied in fp32 and once, and a
 // weight's level enters with fp16's 11 bits (fp32: 22, from two products).
 //
-// Reads of the table bound it: 16 turns of the pipe that serves shared memory for 16 rows by 64 columns, of about 31.
+// Blocks pass from role to role in pairs: with one at a time the waits and commits of the warp that issues products, 160
+// cycles a block, bounded it (33 us for one row times 20480 x 5120). The pipe that serves shared memory would: 16 rows by 64
+// columns take 16 turns of it for the table and about 15 others.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -30,8 +32,8 @@ constexpr unsigned kAll = 0xFFFFFFFFu;
 constexpr int kRows = 128, kStepBlocks = 4;
 constexpr int kDecodeWarps = 8, kSumWarps = 4;
 constexpr int kTileThreads = 32 * (kDecodeWarps + kSumWarps + 2);
-constexpr int kMostRows = 64;           // rows of x at a time
-constexpr int kBuffersA = 4;            // blocks of levels in tensor memory
+template <typename T>
+constexpr int kMostRows = sizeof(T) == 4 ? 32 : 64;  // rows of x at a time
 constexpr float kLevelScale = 1024.0f;  // of fp32's levels, so that their lower parts are normal numbers
 constexpr int kTileCtas = 160;          // most
 
@@ -154,17 +156,18 @@ struct Tiles {
     static constexpr bool kF32 = sizeof(T) == 4;
     static constexpr int kColumns = kF32 ? 2 * kPad : kPad;      // of a product
     static constexpr int kLevels = kF32 ? 64 : 32;               // columns of tensor memory of a block's levels
-    static constexpr int kSums = kBuffersA * kLevels;            // where sums begin
-    static constexpr int kBuffersD = (512 - kSums) / kColumns >= 4 ? 4 : 2;
+    static constexpr int kBuffersA = kF32 ? 2 : 4;               // pairs of blocks whose levels are there
+    static constexpr int kSums = kBuffersA * 2 * kLevels;        // where sums begin
+    static constexpr int kBuffersD = (512 - kSums) / (2 * kColumns) >= 4 ? 4 : 2;
     static constexpr uint32_t kCodeBytes = kRows * 128, kInputBytes = kColumns * 128, kStageBytes = kCodeBytes + kStepBlocks * kInputBytes;
     static constexpr int kStages = 160 * 1024 / kStageBytes >= 4 ? 4 : 160 * 1024 / kStageBytes >= 3 ? 3 : 2;
     static constexpr uint32_t kTable = 65536;
     static constexpr int kShared = 1024 + kTable + kStages * kStageBytes;
-    static_assert(kSums + kBuffersD * kColumns <= 512 && kShared <= 226 * 1024);
+    static_assert(kSums + kBuffersD * 2 * kColumns <= 512 && kShared <= 226 * 1024);
 };
 
 struct TileControl {
-    unsigned long long full[4], empty[4], levels[kBuffersA], levels_read[kBuffersA], sums[4], sums_read[4], drained;
+    unsigned long long full[4], empty[4], levels[4], levels_read[4], sums[4], sums_read[4], drained;
     uint32_t tmem;
     int failed;
 };
@@ -215,10 +218,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tiles_kernel(const __grid_
     const auto blocks_of = [&](int step) { return min(kStepBlocks, blocks - step * kStepBlocks); };
     const auto wait = [&](unsigned long long* bar, uint32_t parity) { return __all_sync(kAll, barrier_wait(shared_address(bar), parity, &c.failed)); };
 
-    if (warp < kDecodeWarps) {  // codes to levels: groups of four warps take blocks in turn
+    if (warp < kDecodeWarps) {  // codes to levels: groups of four warps take pairs of blocks in turn
         const int group = warp >> 2, row = threadIdx.x & 127;
         const uint32_t place = lane * (kF32 ? 8 : 4), to = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16);
-        uint32_t block = 0, stage = 0;
+        uint32_t pair = 0, stage = 0;
         int step = static_cast<int>(begin % steps);
         bool ok = true;
         for (long long x = begin; ok && x < end; ++x, ++stage) {
@@ -226,25 +229,28 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tiles_kernel(const __grid_
             ok = wait(&c.full[slot], stage / S::kStages & 1);
             const int here = blocks_of(step);
             const uint32_t codes = stages + slot * S::kStageBytes + row * 128;
-            for (int b = 0; ok && b < here; ++b, ++block) {
-                if ((block & 1) != static_cast<uint32_t>(group)) continue;
-                const uint32_t buffer = block % kBuffersA;
-                ok = wait(&c.levels_read[buffer], (block / kBuffersA & 1) ^ 1);
+            for (int first = 0; ok && first < here; first += 2, ++pair) {
+                if ((pair & 1) != static_cast<uint32_t>(group)) continue;
+                const uint32_t buffer = pair % S::kBuffersA;
+                ok = wait(&c.levels_read[buffer], (pair / S::kBuffersA & 1) ^ 1);
                 tc_fence_after();
 #pragma unroll 1
-                for (int half = 0; half < 2; ++half) {  // 16 bytes of the block's 32
-                    uint32_t w[4], upper[16];
-                    [[maybe_unused]] uint32_t lower[16];
-                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                                 : "r"(codes + (((2 * b + half) ^ (row & 7)) << 4)) : "memory");
+                for (int b = first; b < min(first + 2, here); ++b) {
+                    uint32_t w[8], upper[32];
+                    [[maybe_unused]] uint32_t lower[32];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
+                    for (int half = 0; half < 2; ++half)  // 16 bytes of the block's 32
+                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[4 * half]), "=r"(w[4 * half + 1]), "=r"(w[4 * half + 2]), "=r"(w[4 * half + 3])
+                                     : "r"(codes + (((2 * b + half) ^ (row & 7)) << 4)));
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
                         const uint32_t at = __byte_perm(w[e / 4], place, 0x5504 | e % 4 << 4) + table;  // place, the byte, 0, 0
-                        if constexpr (kF32) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(upper[e]), "=r"(lower[e]) : "r"(at) : "memory");
-                        else asm volatile("ld.shared.b32 %0, [%1];" : "=r"(upper[e]) : "r"(at) : "memory");
+                        if constexpr (kF32) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(upper[e]), "=r"(lower[e]) : "r"(at));
+                        else asm volatile("ld.shared.b32 %0, [%1];" : "=r"(upper[e]) : "r"(at));
                     }
-                    tmem_store16(to + buffer * S::kLevels + 16 * half, upper);
-                    if constexpr (kF32) tmem_store16(to + buffer * S::kLevels + 32 + 16 * half, lower);
+                    const uint32_t there = to + (2 * buffer + (b & 1)) * S::kLevels;
+                    tmem_store32(there, upper);
+                    if constexpr (kF32) tmem_store32(there + 32, lower);
                 }
                 tc_wait_stores();
                 tc_fence_before();
@@ -261,7 +267,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tiles_kernel(const __grid_
         float acc[kPad];
 #pragma unroll
         for (int i = 0; i < kPad; ++i) acc[i] = 0.0f;
-        uint32_t block = 0;
+        uint32_t pair = 0;
         int step = static_cast<int>(begin % steps), tile = static_cast<int>(begin / steps);
         float next[kStepBlocks];
         const auto scales_of = [&](int at_tile, int at_step) {
@@ -293,26 +299,34 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tiles_kernel(const __grid_
             }
             if (x + 1 < end) scales_of(tile, step);
 #pragma unroll
-            for (int b = 0; b < kStepBlocks; ++b) {
-                if (b >= here) break;
-                const uint32_t buffer = block % S::kBuffersD;
-                ok = wait(&c.sums[buffer], block / S::kBuffersD & 1) && ok;
+            for (int first = 0; first < kStepBlocks; first += 2) {
+                if (first >= here) break;
+                const uint32_t buffer = pair % S::kBuffersD, at = from + buffer * 2 * S::kColumns;
+                ok = wait(&c.sums[buffer], pair / S::kBuffersD & 1) && ok;
                 tc_fence_after();
-                ++block;
+                ++pair;
+                const bool two = first + 1 < here;
 #pragma unroll
                 for (int i = 0; i < kPad; i += 16) {
-                    uint32_t d[16];
-                    tmem_load16(from + buffer * S::kColumns + i, d);
-                    tc_wait_loads();
+                    uint32_t d[2][16];
+                    [[maybe_unused]] uint32_t l[2][16];
+                    tmem_load16(at + i, d[0]);
+                    tmem_load16(at + S::kColumns + i, d[1]);
                     if constexpr (kF32) {
-                        uint32_t l[16];
-                        tmem_load16(from + buffer * S::kColumns + kPad + i, l);
-                        tc_wait_loads();
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) d[k] = __float_as_uint(__uint_as_float(d[k]) + __uint_as_float(l[k]));
+                        tmem_load16(at + kPad + i, l[0]);
+                        tmem_load16(at + S::kColumns + kPad + i, l[1]);
                     }
+                    tc_wait_loads();
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) acc[i + k] = fmaf(__uint_as_float(d[k]), scale[b], acc[i + k]);
+                    for (int b = 0; b < 2; ++b) {
+                        if (b == 1 && !two) continue;  // what an earlier pair left there
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            float v = __uint_as_float(d[b][k]);
+                            if constexpr (kF32) v += __uint_as_float(l[b][k]);
+                            acc[i + k] = fmaf(v, scale[first + b], acc[i + k]);
+                        }
+                    }
                 }
                 tc_fence_before();
                 __syncwarp();
@@ -332,30 +346,37 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tiles_kernel(const __grid_
     } else if (warp == kDecodeWarps + kSumWarps) {  // products
         constexpr uint32_t kF16 = 1u << 4 | 128u >> 4 << 24;  // fp16, fp32 sums, 128 rows
         constexpr uint32_t kBoth = kF16 | static_cast<uint32_t>(S::kColumns >> 3) << 17, kUpper = kF16 | static_cast<uint32_t>(kPad >> 3) << 17;
-        uint32_t block = 0, stage = 0;
+        uint32_t pair = 0, stage = 0;
         int step = static_cast<int>(begin % steps);
         bool ok = true;
         for (long long x = begin; ok && x < end; ++x, ++stage) {
             const uint32_t slot = stage % S::kStages;
             ok = wait(&c.full[slot], stage / S::kStages & 1);
             const int here = blocks_of(step);
-            for (int b = 0; ok && b < here; ++b, ++block) {
-                const uint32_t buffer = block % kBuffersA, sums = block % S::kBuffersD;
-                ok = wait(&c.levels[buffer], block / kBuffersA & 1) && wait(&c.sums_read[sums], (block / S::kBuffersD & 1) ^ 1);
+            for (int first = 0; ok && first < here; first += 2, ++pair) {
+                const uint32_t buffer = pair % S::kBuffersA, sums = pair % S::kBuffersD;
+                ok = wait(&c.sums_read[sums], (pair / S::kBuffersD & 1) ^ 1) && wait(&c.levels[buffer], pair / S::kBuffersA & 1);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t a = tmem + buffer * S::kLevels, d = tmem + S::kSums + sums * S::kColumns;
-                const uint32_t in = tile_descriptor(stages + slot * S::kStageBytes + S::kCodeBytes + b * S::kInputBytes, 16);
+                const uint32_t in = tile_descriptor(stages + slot * S::kStageBytes + S::kCodeBytes + first * S::kInputBytes, 16);
+                const uint32_t a = tmem + buffer * 2 * S::kLevels, d = tmem + S::kSums + sums * 2 * S::kColumns;
+                const bool two = first + 1 < here;
                 if (elected()) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) tc_product_from_tmem(d, a + 8 * k, in + (k * 32 >> 4), kBoth, k > 0);
-                    if constexpr (kF32) {
+                    for (int b = 0; b < 2; ++b) {
+                        if (b == 1 && !two) continue;
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) tc_product_from_tmem(d, a + 32 + 8 * k, in + (k * 32 >> 4), kUpper, true);
+                        for (int k = 0; k < 4; ++k)
+                            tc_product_from_tmem(d + b * S::kColumns, a + b * S::kLevels + 8 * k, in + ((b * S::kInputBytes + k * 32) >> 4), kBoth, k > 0);
+                        if constexpr (kF32) {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                tc_product_from_tmem(d + b * S::kColumns, a + b * S::kLevels + 32 + 8 * k, in + ((b * S::kInputBytes + k * 32) >> 4), kUpper, true);
+                        }
                     }
                     tc_commit(shared_address(&c.levels_read[buffer]));
                     tc_commit(shared_address(&c.sums[sums]));
-                    if (b == here - 1) tc_commit(shared_address(&c.empty[slot]));
+                    if (first + 2 >= here) tc_commit(shared_address(&c.empty[slot]));
                 }
                 __syncwarp();
             }
@@ -485,19 +506,21 @@ cudaError_t launch_type(const Q4Matmul& m, cudaStream_t s) {
     p.parts = parts_of(p.line);
     e = describe(p.codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, m.codes, m.in / 2, m.out, m.in / 2, 128, kRows);
     if (e != cudaSuccess) return e;
-    for (p.first = 0; p.first < m.n; p.first += kMostRows) {
-        p.rows = m.n - p.first < kMostRows ? m.n - p.first : kMostRows;
+    for (p.first = 0; p.first < m.n; p.first += kMostRows<T>) {
+        p.rows = m.n - p.first < kMostRows<T> ? m.n - p.first : kMostRows<T>;
         p.pad = padded_rows(p.rows);
         char* ws = static_cast<char*>(m.ws);
         p.converted = reinterpret_cast<__half*>(ws);
         ws += static_cast<size_t>(kParts) * p.pad * m.in * 2;
         p.powers = reinterpret_cast<float*>(ws);
-        p.sums = p.powers + kMostRows;
+        p.sums = p.powers + kMostRows<__nv_bfloat16>;
         e = describe(p.inputs, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, p.converted, m.in, kParts * p.pad, m.in * 2, 64, kParts * p.pad);
         if (e != cudaSuccess) return e;
         e = launch(q4_convert_kernel<T>, p.pad, 512, 0, 0, s, p);
         if (e != cudaSuccess) return e;
-        e = p.pad == 16 ? launch_pad<T, 16>(p, ctas, s) : p.pad == 32 ? launch_pad<T, 32>(p, ctas, s) : p.pad == 48 ? launch_pad<T, 48>(p, ctas, s) : launch_pad<T, 64>(p, ctas, s);
+        if (p.pad == 16) e = launch_pad<T, 16>(p, ctas, s);
+        else if (p.pad == 32) e = launch_pad<T, 32>(p, ctas, s);
+        else if constexpr (kMostRows<T> == 64) e = p.pad == 48 ? launch_pad<T, 48>(p, ctas, s) : launch_pad<T, 64>(p, ctas, s);
         if (e != cudaSuccess) return e;
         cudaLaunchConfig_t c = {};
         cudaLaunchAttribute attr;
@@ -523,11 +546,11 @@ bool q4_by_tiles(int n, int out, int in) {
 
 uint64_t q4_workspace(int n, int out, int in, int bf16) {
     if (!q4_by_tiles(n, out, in)) return 0;
-    const int rows = n < kMostRows ? n : kMostRows, tiles = (out + kRows - 1) / kRows;
+    const int most = bf16 ? kMostRows<__nv_bfloat16> : kMostRows<float>, rows = n < most ? n : most, tiles = (out + kRows - 1) / kRows;
     const long long total = static_cast<long long>(tiles) * steps_of(in);
     // parts are most with the most CTAs
     const int parts = parts_of(line_of(out, in, static_cast<int>(total < kTileCtas ? total : kTileCtas)));
-    return static_cast<uint64_t>(bf16 ? 1 : 2) * padded_rows(rows) * in * 2 + 4ull * kMostRows + 4ull * tiles * parts * rows * kRows;
+    return static_cast<uint64_t>(bf16 ? 1 : 2) * padded_rows(rows) * in * 2 + 4ull * kMostRows<__nv_bfloat16> + 4ull * tiles * parts * rows * kRows;
 }
 
 cudaError_t launch_q4_tiles(const Q4Matmul& m, cudaStream_t s) {
