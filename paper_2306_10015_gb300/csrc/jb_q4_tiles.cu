@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tiles_kernel(const __grid_
     constexpr bool kF32 = S::kF32;
     extern __shared__ char dynamic[];
     __shared__ TileControl c;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = same(static_cast<int>(threadIdx.x) >> 5), lane = threadIdx.x & 31;
     const uint32_t base = (shared_address(dynamic) + 1023) & ~1023u, table = base, stages = base + S::kTable;
     char* const table_at = dynamic + (base - shared_address(dynamic));
     {   // the table: 256 bytes for each byte of codes, with a copy of its two levels for each lane
@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tiles_kernel(const __grid_
     tc_fence_after();
     after_previous();
     let_next_start();
-    const uint32_t tmem = c.tmem;
+    const uint32_t tmem = same(c.tmem);
     const Q4Matmul& m = p.m;
     const int blocks = m.in / 64, steps = p.line.steps;
     const long long begin = p.line.bound(blockIdx.x), end = p.line.bound(blockIdx.x + 1);
@@ -234,23 +234,33 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tiles_kernel(const __grid_
                 const uint32_t buffer = pair % S::kBuffersA;
                 ok = wait(&c.levels_read[buffer], (pair / S::kBuffersA & 1) ^ 1);
                 tc_fence_after();
+                // all reads of the pair under way together (fp32: of a block; a second block that is not there is decoded too)
+                constexpr int kTogether = kF32 ? 1 : 2;
 #pragma unroll 1
-                for (int b = first; b < min(first + 2, here); ++b) {
-                    uint32_t w[8], upper[32];
+                for (int b0 = 0; b0 < 2; b0 += kTogether) {
+                    uint32_t w[kTogether][8], upper[kTogether][32];
                     [[maybe_unused]] uint32_t lower[32];
 #pragma unroll
-                    for (int half = 0; half < 2; ++half)  // 16 bytes of the block's 32
-                        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[4 * half]), "=r"(w[4 * half + 1]), "=r"(w[4 * half + 2]), "=r"(w[4 * half + 3])
-                                     : "r"(codes + (((2 * b + half) ^ (row & 7)) << 4)));
+                    for (int b = 0; b < kTogether; ++b)
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const uint32_t at = __byte_perm(w[e / 4], place, 0x5504 | e % 4 << 4) + table;  // place, the byte, 0, 0
-                        if constexpr (kF32) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(upper[e]), "=r"(lower[e]) : "r"(at));
-                        else asm volatile("ld.shared.b32 %0, [%1];" : "=r"(upper[e]) : "r"(at));
+                        for (int half = 0; half < 2; ++half)  // 16 bytes of a block's 32
+                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                         : "=r"(w[b][4 * half]), "=r"(w[b][4 * half + 1]), "=r"(w[b][4 * half + 2]), "=r"(w[b][4 * half + 3])
+                                         : "r"(codes + (((2 * (first + b0 + b) + half) ^ (row & 7)) << 4)));
+#pragma unroll
+                    for (int b = 0; b < kTogether; ++b)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            const uint32_t at = __byte_perm(w[b][e / 4], place, 0x5504 | e % 4 << 4) + table;  // place, the byte, 0, 0
+                            if constexpr (kF32) asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(upper[b][e]), "=r"(lower[e]) : "r"(at));
+                            else asm volatile("ld.shared.b32 %0, [%1];" : "=r"(upper[b][e]) : "r"(at));
+                        }
+#pragma unroll
+                    for (int b = 0; b < kTogether; ++b) {
+                        const uint32_t there = to + (2 * buffer + b0 + b) * S::kLevels;
+                        tmem_store32(there, upper[b]);
+                        if constexpr (kF32) tmem_store32(there + 32, lower);
                     }
-                    const uint32_t there = to + (2 * buffer + (b & 1)) * S::kLevels;
-                    tmem_store32(there, upper);
-                    if constexpr (kF32) tmem_store32(there + 32, lower);
                 }
                 tc_wait_stores();
                 tc_fence_before();

@@ -242,7 +242,7 @@ __device__ void product_role(const TreeParams& p, Deal deal, Control& c, uint32_
     const int steps = (p.a.head_dim + 15) / 16;
     constexpr uint32_t scores = product_descriptor(kTile, false);
     const uint32_t values = product_descriptor(16 * steps, true);
-    const uint32_t tmem = c.tmem;
+    const uint32_t tmem = same(c.tmem);
     uint32_t tiles = 0, blocks = 0;  // so far
     // The whole warp runs this and one lane issues: operands are then the warp's, which products want them to be.
     const auto wait = [&](unsigned long long* bar, uint32_t parity) {
@@ -268,8 +268,8 @@ __device__ void product_role(const TreeParams& p, Deal deal, Control& c, uint32_
         return true;
     };
     Piece s;
-    for (; deal.take(p, s); ++blocks) {
-        const uint32_t n = s.to - s.from;
+    for (; same(static_cast<int>(deal.take(p, s))) != 0; ++blocks) {
+        const uint32_t n = same(s.to - s.from);
         if (!wait(&c.queries[blocks % S::kQueries], blocks / S::kQueries & 1)) return;
         if (!scores_of(tiles, n == 1)) return;
         if (n > 1 && !scores_of(tiles + 1, n == 2)) return;
@@ -520,7 +520,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kCtas) tree_bf16_kernel(co
     __shared__ Control c;
     __shared__ Nodes nodes;
     __shared__ long long sums[kThreads / 32], found[2];
-    const int warp = threadIdx.x >> 5;
+    const int warp = same(static_cast<int>(threadIdx.x) >> 5);
     const uint32_t queries = (shared_address(dynamic) + 1023) & ~1023u, ring = queries + S::kQueries * S::kQueryBytes;
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kSlots; ++i) {
