@@ -849,14 +849,15 @@ def jb_q4_matmul(table: "Q4Table", index: int, x, out_features: int, bias=None, 
             or (out.stride(1) != 1 and out_features > 1):
         raise ValueError("out must be [n, out_features] of x's type on its CUDA device, contiguous in a row")
     handle = _stream_on(device, stream)
-    nbytes, ws = table.matmul_workspace(out_features, inner, x.dtype, n), None
     if workspace is not None:
         if workspace.get_device() != device or not workspace.is_contiguous():
             raise ValueError("workspace must be a contiguous tensor on x's CUDA device")
         ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    elif nbytes:
-        ws, nbytes, held = table._workspaces.get("matmul", nbytes, stream, handle,
-                                                 lambda size: _new(stream, torch.empty, size, dtype=torch.uint8, device=x.device))
+    else:
+        ws, nbytes = None, table.matmul_workspace(out_features, inner, x.dtype, n)
+        if nbytes:
+            ws, nbytes, held = table._workspaces.get("matmul", nbytes, stream, handle, lambda size: _new(
+                stream, torch.empty, size, dtype=torch.uint8, device=x.device))
     segment = ctypes.byref(table.segments, index % table.n_segments * ctypes.sizeof(jb_q4_segment))
     _check(lib().jb_q4_matmul(segment, out_features, inner, dtype, x.data_ptr(), x.stride(0), n,
                               None if bias is None else bias.data_ptr(), out.data_ptr(), out.stride(0), ws, nbytes, handle))

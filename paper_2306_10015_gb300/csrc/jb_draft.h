@@ -68,7 +68,7 @@ struct Q4Matmul {
     int n, out, in, bf16;
 };
 // Large products, by tcgen05: whether one is, its workspace and its launch.
-bool q4_by_tiles(int n, int out, int in);
+bool q4_by_tiles(int n, int out, int in, int bf16);
 uint64_t q4_workspace(int n, int out, int in, int bf16);
 cudaError_t launch_q4_tiles(const Q4Matmul& m, cudaStream_t s);
 cudaError_t launch_q4_matmul(const Q4Matmul& m, cudaStream_t s);

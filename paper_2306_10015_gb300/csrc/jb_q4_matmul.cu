@@ -1,4 +1,5 @@
-// jb_q4_matmul.cu -- products of a few rows with a matrix of 4-bit weights (the format of jb_perturb_q4):
+// jb_q4_matmul.cu -- products of very few rows, or with small matrices, of 4-bit weights (the format of jb_perturb_q4; the
+// others are in jb_q4_tiles.cu):
 //   y[i][o] = sum_k x[i][k] level[code[o][k]] scale[o][k / 64] + bias[o]
 //
 // The weights are read once, 4.5 bits each, and that bounds it while turning codes into numbers keeps up: a byte is a pair
@@ -520,11 +521,12 @@ cudaError_t launch_t(Params p, cudaStream_t s) {
     const Q4Matmul& m = p.m;
     const int each = sizeof(T) == 2 ? 1 : 2;  // columns of the product for a row of x
     // The fewest CTAs that hold a slice each of the inputs of the rows at hand and sums of 16 tiles beside them; fewer rows
-    // at a time where eight do not
-    const auto fits = [&](int rows, int ranks) {
+    // at a time where eight do not, or where they do not hold the last rows (few columns come with a larger table)
+    const auto fit = [&](int rows, int ranks) {
         const int slice = (m.in / 64 + ranks - 1) / ranks * 64;
         return with_tiles(rows * each, [&](auto tiles) { return layout_of<Shape<T, tiles.value>>(rows, rows * each, slice, 1, ranks > 1 ? kMatWarps : 0).all <= kMostShared; });
     };
+    const auto fits = [&](int rows, int ranks) { return fit(rows, ranks) && (m.n % rows == 0 || fit(m.n % rows, ranks)); };
     int rows = m.n < kMostColumns / each ? m.n : kMostColumns / each, ranks = 1;
     for (;; rows = (rows + 1) / 2) {
         ranks = 1;
@@ -544,7 +546,7 @@ cudaError_t launch_t(Params p, cudaStream_t s) {
 }  // namespace
 
 cudaError_t launch_q4_matmul(const Q4Matmul& m, cudaStream_t s) {
-    if (q4_by_tiles(m.n, m.out, m.in) && reinterpret_cast<uint64_t>(m.codes) % 16 == 0) return launch_q4_tiles(m, s);
+    if (q4_by_tiles(m.n, m.out, m.in, m.bf16) && reinterpret_cast<uint64_t>(m.codes) % 16 == 0) return launch_q4_tiles(m, s);
     Params p;
     p.m = m;
     q4_levels_host(p.levels);

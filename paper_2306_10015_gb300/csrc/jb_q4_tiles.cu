@@ -549,13 +549,20 @@ cudaError_t launch_type(const Q4Matmul& m, cudaStream_t s) {
 
 }  // namespace
 
-bool q4_by_tiles(int n, int out, int in) {
-    // three launches and a tile of 128 rows pay where the matrix is large, and the sooner the more rows x has
-    return n > 0 && static_cast<long long>(out) * in >= (1ll << 22);
+bool q4_by_tiles(int n, int out, int in, int bf16) {
+    // Three launches pay from some columns of the product on, the fewer the larger the matrix is and the longer its rows are
+    // (a CTA of the other kernel holds so much input). Measured with bf16, the other kernel and this one in us: 20480 x 5120,
+    // 7 rows 24.8 and 24.2, 32 rows 102 and 27; 5120 x 20480, 1 row 26.6 and 23.8, 2 rows 24.0 and 23.9;
+    // 4096 x 4096, 8 rows 9.1 and 10.5, 9 rows 11.5 and 10.5; 2048 x 2048, 16 rows 7.4 and 7.6, 24 rows 9.7 and 8.6;
+    // 1024 x 1024, 16 rows 4.4 and 6.6, 32 rows 7.0 and 6.9, 64 rows 13.8 and 7.7.
+    const long long size = static_cast<long long>(out) * in, columns = static_cast<long long>(n) * (bf16 ? 1 : 2);
+    if (size >= 1ll << 26) return columns >= 8 || columns * in > 40000;
+    if (size >= 1ll << 24) return columns > 8;
+    return columns >= (size >= 1ll << 22 ? 24 : 32) && size >= 1ll << 19;
 }
 
 uint64_t q4_workspace(int n, int out, int in, int bf16) {
-    if (!q4_by_tiles(n, out, in)) return 0;
+    if (!q4_by_tiles(n, out, in, bf16)) return 0;
     const int most = bf16 ? kMostRows<__nv_bfloat16> : kMostRows<float>, rows = n < most ? n : most, tiles = (out + kRows - 1) / kRows;
     const long long total = static_cast<long long>(tiles) * steps_of(in);
     // parts are most with the most CTAs

@@ -145,8 +145,8 @@ def test_bad_products(jb):
         assert q4(jb, **kw) == rc, kw
     need = lambda *a: jb.lib().jb_q4_matmul_workspace(*a)  # noqa: E731
     assert need(128, 256, 1, 2) == 0 and need(4096, 4096, 2, 1) == 0 and need(4096, 4000, 1, 1) == 0 and need(0, 4096, 1, 1) == 0
-    big = dict(numel=4096 * 4096, out=4096, inner=4096, xs=4096, ys=4096, n=3, ws=FAKE, size=need(4096, 4096, 1, 3))
-    assert big["size"] > 3 * 4096 * 2
+    big = dict(numel=4096 * 4096, out=4096, inner=4096, xs=4096, ys=4096, n=9, ws=FAKE, size=need(4096, 4096, 1, 9))
+    assert big["size"] > 9 * 4096 * 2
     for kw, rc in ((dict(ws=0), INV), (dict(ws=FAKE + 8), MIS), (dict(size=big["size"] - 1), INV)):
         assert q4(jb, **{**big, **kw}) == rc, kw
 

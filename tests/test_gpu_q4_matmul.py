@@ -75,8 +75,17 @@ def test_long_and_wide(dtype, n, out, inner):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("inner", [8192, 13312, 20480, 32768, 65536])
+def test_long_rows_that_are_taken_some_at_a_time(dtype, inner):
+    """The last rows are fewer than those before them, whatever the number."""
+    table = weights(19, inner)
+    for n in range(1, 72):
+        check(dtype, n, 19, inner, bias=n % 2 == 0, table=table)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 33, 48, 64, 65, 100])
-@pytest.mark.parametrize("out,inner", [(4096, 1024), (1000, 4224), (65601, 64), (150, 32768), (130, 65536), (2049, 2112)])
+@pytest.mark.parametrize("out,inner", [(4096, 1024), (1000, 4224), (65601, 64), (150, 32768), (130, 65536), (2049, 2112), (777, 704)])
 def test_matrices_that_are_cut_into_tiles(dtype, n, out, inner):
     """Tiles of 128 rows: the last one ragged, columns that end inside a step of four blocks, tiles that many CTAs share and
     CTAs that have many."""
@@ -84,16 +93,27 @@ def test_matrices_that_are_cut_into_tiles(dtype, n, out, inner):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_tiles_strides_and_odd_scales(dtype):
+@pytest.mark.parametrize("out,inner,ns", [(4100, 4160, (4, 5, 8, 9, 12)), (10001, 6720, (1, 3, 4, 5, 7, 8, 11)),
+                                          (1050, 65536, (1, 2, 3))])
+def test_large_matrices_and_few_rows(dtype, out, inner, ns):
+    """On both sides of the sizes at which the tiles begin to pay."""
+    table = weights(out, inner)
+    for n in ns:
+        check(dtype, n, out, inner, bias=n % 2 == 0, table=table)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [6, 27])
+def test_tiles_strides_and_odd_scales(dtype, n):
     """Rows inside wider ones and scales off a 16-byte boundary; codes off one, which take the other kernel."""
     g = torch.Generator(device="cuda").manual_seed(4)
     out, inner = 3000, 1536
     codes = torch.randint(0, 256, (out * inner // 2 + 8,), dtype=torch.uint8, device="cuda", generator=g)
     scale = torch.rand(out * inner // 64 + 3, device="cuda", generator=g)
-    x = torch.randn(6, inner + 80, device="cuda", generator=g).to(DT[dtype])[:, 40:40 + inner]
+    x = torch.randn(n, inner + 80, device="cuda", generator=g).to(DT[dtype])[:, 40:40 + inner]
     for skip, first in ((0, 3), (8, 0)):
         table = jb.Q4Table([(codes[skip:skip + out * inner // 2], scale[first:first + out * inner // 64], out * inner)])
-        y = torch.full((6, out + 9), 4.0, dtype=DT[dtype], device="cuda")
+        y = torch.full((n, out + 9), 4.0, dtype=DT[dtype], device="cuda")
         got = jb.jb_q4_matmul(table, 0, x, out, out=y[:, 4:4 + out])
         assert (y[:, :4] == 4).all() and (y[:, 4 + out:] == 4).all()
         w = dense(table, 0, out, inner)
@@ -102,17 +122,18 @@ def test_tiles_strides_and_odd_scales(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_tiles_inputs_that_are_not_finite_or_of_all_sizes(dtype):
+@pytest.mark.parametrize("times", [1, 3])
+def test_tiles_inputs_that_are_not_finite_or_of_all_sizes(dtype, times):
     table = weights(2100, 2048)
     g = torch.Generator(device="cuda").manual_seed(3)
     x = torch.randn(9, 2048, device="cuda", generator=g)
     x *= torch.tensor([1e-38, 1e-30, 1e-10, 1e-3, 1.0, 1e10, 1e30, 1e35, 0.0], device="cuda")[:, None]
     x[:, ::97] *= 100.0
-    x = x.to(DT[dtype])
-    clean = check(dtype, 9, 2100, 2048, bias=False, x=x, table=table)
+    x = x.to(DT[dtype]).repeat(times, 1)
+    clean = check(dtype, 9 * times, 2100, 2048, bias=False, x=x, table=table)
     x[1, 500], x[3, 70], x[4, 2047] = float("inf"), float("nan"), -float("inf")
     got = jb.jb_q4_matmul(table, 0, x, 2100)
-    away = [0, 2, 5, 6, 7, 8]
+    away = [i for i in range(9 * times) if i not in (1, 3, 4)]
     assert torch.equal(got[away], clean[away])
     want = x.double() @ dense(table, 0, 2100, 2048).T
     assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isinf(got), torch.isinf(want))
