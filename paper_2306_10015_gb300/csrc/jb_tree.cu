@@ -41,7 +41,7 @@ __global__ void __launch_bounds__(kThreads) tree_kernel(const __grid_constant__ 
     const bool work = deal.start(p, blockIdx.x, gridDim.x, sh.sums, sh.found);
     int tree = -1;
     Piece s;
-    Note cut = {-1, 0, 0, 0};
+    Note cut = {};
     while (work && deal.take(p, s)) {
         if (s.tree != tree) fill_nodes<kThreads>(p, s.span, sh.nodes, threadIdx.x, [](bool x) { return __syncthreads_or(x); });
         tree = s.tree;
@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(kThreads) tree_kernel(const __grid_constant__ 
         }
         const bool whole = s.from == 0 && s.to == s.span.tiles;
         float* slot = slot_of<C, D>(p, gridDim.x, blockIdx.x, s.from == 0);
-        if (s.from == 0 && !whole) cut = {s.tree, s.head, s.block, deal.last_of(s)};
+        if (s.from == 0 && !whole) cut = {s.span.first, s.head, s.block, deal.last_of(s), s.span.nodes * p.a.group, {}};
         __syncthreads();
         if (c == 0) {
             sh.factor[r] = l > 0.0f ? 1.0f / l : 0.0f;

@@ -305,11 +305,12 @@ __device__ __forceinline__ void write_zeros(const TreeParams& p) {
     }
 }
 
-// The workspace: a note of each CTA, the block that it is the first to have a part of and not the last (tree -1: none);
-// then partial results, o[rows][D], m[rows], l[rows]. The first part of a block is in its CTA's slot 1, the others in their
+// The workspace: a note of each CTA, the block that it is the first to have a part of and not the last (rows 0: none); then
+// partial results, o[rows][D], m[rows], l[rows]. The first part of a block is in its CTA's slot 1, the others in their
 // CTAs' slots 0, so that the end of one block and the start of the next do not meet.
 struct Note {
-    int tree, head, block, last;
+    int first, head, block, last, rows;  // first: node of the tree; last: CTA with the block's end; rows: of the tree
+    int pad[3];                          // slots begin on 16 bytes
 };
 __host__ __device__ constexpr size_t slot_floats(int rows, int d) { return static_cast<size_t>(rows) * (d + 2); }
 __host__ __device__ constexpr size_t workspace_floats(int ctas, int rows, int d) { return ctas * (sizeof(Note) / 4 + 2 * slot_floats(rows, d)); }
@@ -320,57 +321,58 @@ __device__ __forceinline__ float* slot_of(const TreeParams& p, int ctas, int wor
 __device__ __forceinline__ void take_note(const TreeParams& p, const Note& n) { reinterpret_cast<Note*>(p.a.ws)[blockIdx.x] = n; }
 
 // CTA (b, slice) joins a slice of the rows of the block that CTA b has the first part of. A thread adds up four values of
-// every part, four parts at a time so that the loads do not wait for one another.
+// every part, four parts at a time so that the loads do not wait for one another. A few CTAs of many threads on each SM: it
+// is the chain of reads, note, sums, maxima, that takes the time, and CTAs that come in several rounds repeat it (304 blocks
+// of 128 rows by 32 slices of four rows: 12 us, by slices of kSlice @JOIN@).
+constexpr int kJoinThreads = 256, kSlice = 32;
 template <typename T, int D, typename C>
-__global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ TreeParams p) {
-    constexpr int kThreads = 128, kQuads = D / 4, kAt = kThreads / kQuads, kAhead = 4;  // rows at a time; parts
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ TreeParams p) {
+    constexpr int kQuads = D / 4, kAt = kJoinThreads / kQuads, kAhead = 4;  // rows at a time; parts
     constexpr int kRows = C::kRows;
     after_previous();
     let_next_start();
     const Note n = reinterpret_cast<const Note*>(p.a.ws)[blockIdx.x];
-    if (n.tree < 0) return;
-    const int first = p.trees.starts[n.tree], nodes = p.trees.starts[n.tree + 1] - first, quad = threadIdx.x % kQuads;
-    const int row = blockIdx.y * kAt + threadIdx.x / kQuads, all = n.block * kRows + row;
-    if (threadIdx.x >= kAt * kQuads || row >= kRows || all >= nodes * p.a.group || 4 * quad >= p.a.head_dim) return;
-    float m = kLowest, l = 0.0f;
-    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    const int b = blockIdx.x;
-    for (int w = b; w <= n.last; w += kAhead) {
-        float mw[kAhead], lw[kAhead];
-        float4 ow[kAhead];
+    const int quad = threadIdx.x % kQuads, b = blockIdx.x, end = min(min(kRows, n.rows - n.block * kRows), (static_cast<int>(blockIdx.y) + 1) * kSlice);
+    if (4 * quad >= p.a.head_dim) return;
+    for (int row = blockIdx.y * kSlice + threadIdx.x / kQuads; row < end; row += kAt) {
+        float m = kLowest, l = 0.0f;
+        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int w = b; w <= n.last; w += kAhead) {
+            float mw[kAhead], lw[kAhead];
+            float4 ow[kAhead];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const float* slot = slot_of<C, D>(p, gridDim.x, min(w + k, n.last), w + k == b);
-            mw[k] = w + k <= n.last ? __ldcg(slot + kRows * D + row) : kLowest;
-            lw[k] = w + k <= n.last ? __ldcg(slot + kRows * D + kRows + row) : 0.0f;
-            ow[k] = w + k <= n.last ? __ldcg(reinterpret_cast<const float4*>(slot + row * D) + quad) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        }
+            for (int k = 0; k < kAhead; ++k) {
+                const float* slot = slot_of<C, D>(p, gridDim.x, min(w + k, n.last), w + k == b);
+                mw[k] = w + k <= n.last ? __ldcg(slot + kRows * D + row) : kLowest;
+                lw[k] = w + k <= n.last ? __ldcg(slot + kRows * D + kRows + row) : 0.0f;
+                ow[k] = w + k <= n.last ? __ldcg(reinterpret_cast<const float4*>(slot + row * D) + quad) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            }
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const float top = fmaxf(m, mw[k]), f = exp2_approx(m - top), g = exp2_approx(mw[k] - top);
-            l = fmaf(g, lw[k], l * f);
-            o = make_float4(fmaf(g, ow[k].x, o.x * f), fmaf(g, ow[k].y, o.y * f), fmaf(g, ow[k].z, o.z * f), fmaf(g, ow[k].w, o.w * f));
-            m = top;
+            for (int k = 0; k < kAhead; ++k) {
+                const float top = fmaxf(m, mw[k]), f = exp2_approx(m - top), g = exp2_approx(mw[k] - top);
+                l = fmaf(g, lw[k], l * f);
+                o = make_float4(fmaf(g, ow[k].x, o.x * f), fmaf(g, ow[k].y, o.y * f), fmaf(g, ow[k].z, o.z * f), fmaf(g, ow[k].w, o.w * f));
+                m = top;
+            }
         }
+        const float inverse = l > 0.0f ? 1.0f / l : 0.0f;
+        const int all = n.block * kRows + row, node = all / p.a.group, h = all - node * p.a.group;
+        T* out = reinterpret_cast<T*>(p.a.out) + (n.first + node) * p.a.out_row + (n.head * p.a.group + h) * p.a.out_head + 4 * quad;
+        store_out(out, o.x * inverse);
+        store_out(out + 1, o.y * inverse);
+        store_out(out + 2, o.z * inverse);
+        store_out(out + 3, o.w * inverse);
     }
-    const float inverse = l > 0.0f ? 1.0f / l : 0.0f;
-    const int node = all / p.a.group, h = all - node * p.a.group;
-    T* out = reinterpret_cast<T*>(p.a.out) + (first + node) * p.a.out_row + (n.head * p.a.group + h) * p.a.out_head + 4 * quad;
-    store_out(out, o.x * inverse);
-    store_out(out + 1, o.y * inverse);
-    store_out(out + 2, o.z * inverse);
-    store_out(out + 3, o.w * inverse);
 }
 
 template <typename T, int D, typename C>
 cudaError_t launch_join(const TreeParams& p, int ctas, cudaStream_t s) {
-    constexpr int kAt = 128 / (D / 4);
     cudaLaunchConfig_t c = {};
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
-    c.gridDim = dim3(ctas, (C::kRows + kAt - 1) / kAt);
-    c.blockDim = dim3(128);
+    c.gridDim = dim3(ctas, (C::kRows + kSlice - 1) / kSlice);
+    c.blockDim = dim3(kJoinThreads);
     c.stream = s;
     c.attrs = &attr;
     c.numAttrs = 1;

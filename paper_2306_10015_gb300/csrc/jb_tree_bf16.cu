@@ -332,7 +332,7 @@ __device__ void softmax_role(const TreeParams& p, Deal deal, Control& c, Nodes& 
     int tree = -1;
     bool ok = true;  // a wait that gives up leaves the loops as they are: other warps may wait for this one
     Piece s;
-    Note cut = {-1, 0, 0, 0};
+    Note cut = {};
     while (deal.take(p, s)) {
         if (s.tree != tree) fill_nodes<32 * kSoftmaxWarps>(p, s.span, nodes, threadIdx.x, any_of);
         tree = s.tree;
@@ -468,7 +468,7 @@ __device__ void softmax_role(const TreeParams& p, Deal deal, Control& c, Nodes& 
             if (lane == 0) barrier_arrive(shared_address(&c.weights[buffer]));
         }
         const bool whole = s.from == 0 && s.to == s.span.tiles;
-        if (s.from == 0 && !whole) cut = {s.tree, s.head, s.block, deal.last_of(s)};
+        if (s.from == 0 && !whole) cut = {s.span.first, s.head, s.block, deal.last_of(s), rows, {}};
         ok = barrier_wait(shared_address(&c.sums), (tiles - 1) & 1, &c.failed) && ok;
         tc_fence_after();
         if (idle) continue;
@@ -568,7 +568,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kCtas) tree_bf16_kernel(co
             help_role<D>(p, deal, c, queries, ring);
         }
     } else if (threadIdx.x == 0) {
-        take_note(p, {-1, 0, 0, 0});
+        take_note(p, {});
     }
     tc_fence_before();
     __syncthreads();
