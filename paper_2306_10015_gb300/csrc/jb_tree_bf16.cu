@@ -57,7 +57,9 @@ struct Shape {
 struct TcParams {
     TreeParams t;
     CUtensorMap keys, values;  // [pages][heads][tokens][elements]
+    CUtensorMap queries;       // [nodes][heads][query heads of one][elements]
     int box;                   // groups of a box, which lie in one page
+    int query_box;             // whether a block of queries is a box, too: whole nodes; else threads copy them
 };
 
 struct Control {
@@ -82,14 +84,22 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 // Keys and values of the blocks' tiles, in the order in which they are needed. Lane i copies box i of a tile: `box` groups of
 // 64 elements.
 template <int D>
-__device__ void copy_role(const TcParams& tc, Deal deal, Control& c, uint32_t ring) {
+__device__ void copy_role(const TcParams& tc, Deal deal, Control& c, uint32_t queries, uint32_t ring) {
     using S = Shape<D>;
     constexpr int kGroups = kTile / kGroup, kPanels = D / 64;
     const TreeParams& p = tc.t;
     const int lane = threadIdx.x & 31, panel = lane % kPanels, group = lane / kPanels * tc.box;  // group: of the tile
     const bool mine = group < kGroups && 64 * panel < p.a.head_dim;
     const uint32_t box_bytes = tc.box * kGroup * 128;
-    uint32_t copies = 0, tiles = 0, edges = 0;
+    uint32_t copies = 0, tiles = 0, edges = 0, blocks = 0;
+    const auto give_up = [&] {  // what is under way arrives first
+        int late = 0;
+        for (uint32_t k = copies < S::kSlots ? 0 : copies - S::kSlots; k < copies; ++k)
+            barrier_wait(shared_address(&c.full[k % S::kSlots]), k / S::kSlots & 1, &late);
+        if (tc.query_box)
+            for (uint32_t k = blocks < S::kQueries ? 0 : blocks - S::kQueries; k < blocks; ++k)
+                barrier_wait(shared_address(&c.queries[k % S::kQueries]), k / S::kQueries & 1, &late);
+    };
     Piece s;
     while (deal.take(p, s)) {
         const int* table = p.pages.table + static_cast<size_t>(s.span.row) * p.pages.row_pages;
@@ -111,12 +121,8 @@ __device__ void copy_role(const TcParams& tc, Deal deal, Control& c, uint32_t ri
             const uint32_t bytes = __popc(boxes) * box_bytes;
 #pragma unroll 1
             for (int kind = 0; kind < 2; ++kind) {
-                const uint32_t i = copies++, slot = i % S::kSlots, at = ring + slot * S::kTileBytes;
-                if (!__all_sync(kAll, barrier_wait(shared_address(&c.empty[slot]), (i / S::kSlots & 1) ^ 1, &c.failed))) {
-                    int late = 0;  // what is under way arrives first
-                    for (uint32_t k = i < S::kSlots ? 0 : i - S::kSlots; k < i; ++k) barrier_wait(shared_address(&c.full[k % S::kSlots]), k / S::kSlots & 1, &late);
-                    return;
-                }
+                const uint32_t i = copies, slot = i % S::kSlots, at = ring + slot * S::kTileBytes;
+                if (!__all_sync(kAll, barrier_wait(shared_address(&c.empty[slot]), (i / S::kSlots & 1) ^ 1, &c.failed))) return give_up();
                 if (kind == 1 && missing != 0) {  // what tiles before left there is no number to meet a weight of zero
                     for (int g = 0; g < kGroups; ++g)
                         if (missing >> g & 1u)
@@ -135,6 +141,16 @@ __device__ void copy_role(const TcParams& tc, Deal deal, Control& c, uint32_t ri
                 }
                 __syncwarp();
                 if (real) copy_box(at + panel * S::kPanel + group * (kGroup * 128), kind == 0 ? &tc.keys : &tc.values, 64 * panel, y, s.head, w, shared_address(&c.full[slot]));
+                ++copies;
+                if (tc.query_box && kind == 0 && tile == s.span.first_tile + s.from) {
+                    const uint32_t b = blocks % S::kQueries, to = queries + b * S::kQueryBytes;
+                    if (!__all_sync(kAll, barrier_wait(shared_address(&c.queries_read[b]), (blocks / S::kQueries & 1) ^ 1, &c.failed))) return give_up();
+                    if (lane == 0) barrier_arrive_bytes(shared_address(&c.queries[b]), (p.a.head_dim + 63) / 64 * S::kQueryPanel);
+                    __syncwarp();
+                    if (lane < kPanels && 64 * lane < p.a.head_dim)
+                        copy_box(to + lane * S::kQueryPanel, &tc.queries, 64 * lane, 0, s.head, s.span.first + s.block * (kRows / p.a.group), shared_address(&c.queries[b]));
+                    ++blocks;
+                }
             }
         }
     }
@@ -197,8 +213,9 @@ __device__ bool clean_values(uint32_t tile, int lo, int hi) {
 }
 
 template <int D>
-__device__ void help_role(const TreeParams& p, Deal deal, Control& c, uint32_t queries, uint32_t ring) {
+__device__ void help_role(const TcParams& tc, Deal deal, Control& c, uint32_t queries, uint32_t ring) {
     using S = Shape<D>;
+    const TreeParams& p = tc.t;
     const int lane = threadIdx.x & 31;
     uint32_t blocks = 0, tiles = 0, edges = 0;
     const auto tell = [&](unsigned long long* bar) {
@@ -207,6 +224,7 @@ __device__ void help_role(const TreeParams& p, Deal deal, Control& c, uint32_t q
         if (lane == 0) barrier_arrive(shared_address(bar));
     };
     const auto block = [&](const Piece& s) {
+        if (tc.query_box) return true;
         const uint32_t b = blocks % S::kQueries;
         if (!__all_sync(kAll, barrier_wait(shared_address(&c.queries_read[b]), (blocks / S::kQueries & 1) ^ 1, &c.failed))) return false;
         ++blocks;
@@ -224,7 +242,7 @@ __device__ void help_role(const TreeParams& p, Deal deal, Control& c, uint32_t q
             if (!edge_of(p, s.span, tile * kTile, kTile)) continue;
             const uint32_t i = 2 * tiles + 1, slot = i % S::kSlots, e = edges++;
             // first that its copy has begun: the slot's own phase may be any before that
-            if (!__all_sync(kAll, barrier_wait(shared_address(&c.edges[e % 8]), e / 8 & 1, &c.failed))) return;
+            if (!__all_sync(kAll, barrier_wait_idle(shared_address(&c.edges[e % 8]), e / 8 & 1, &c.failed))) return;
             if (!__all_sync(kAll, barrier_wait(shared_address(&c.full[slot]), i / S::kSlots & 1, &c.failed))) return;
             if (clean_values<D>(ring + slot * S::kTileBytes, s.span.lo - tile * kTile, s.span.len - tile * kTile))
                 *static_cast<volatile int*>(&c.not_finite) = 1;
@@ -395,11 +413,13 @@ __device__ void softmax_role(const TreeParams& p, Deal deal, Control& c, Nodes& 
                             for (int e = 0; e < 16; ++e) x[e] = raw[e];
                         }
                         if (k + 16 < kTile) tmem_load16(at + k + 16, raw);
+                        if (edge) {
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            if (!(sees >> e & 1u)) x[e] = __float_as_uint(-INFINITY);
-                            tops[e % 4] = fmaxf(tops[e % 4], __uint_as_float(x[e]));
+                            for (int e = 0; e < 16; ++e)
+                                if (!(sees >> e & 1u)) x[e] = __float_as_uint(-INFINITY);
                         }
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) tops[e % 4] = fmaxf(tops[e % 4], __uint_as_float(x[e]));
                         tmem_store16(at + k, x);
                     }
                     tc_wait_stores();
@@ -534,7 +554,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kCtas) tree_bf16_kernel(co
             barrier_init(shared_address(&c.weights[i]), kSoftmaxWarps);
         }
         for (int i = 0; i < S::kQueries; ++i) {
-            barrier_init(shared_address(&c.queries[i]), kHelpWarps);
+            barrier_init(shared_address(&c.queries[i]), tc.query_box ? 1 : kHelpWarps);
             barrier_init(shared_address(&c.queries_read[i]), 1);
         }
         barrier_init(shared_address(&c.sums), 1);
@@ -563,9 +583,9 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kCtas) tree_bf16_kernel(co
             }
             __syncwarp();
         } else if (warp == kSoftmaxWarps + 1) {
-            copy_role<D>(tc, deal, c, ring);
+            copy_role<D>(tc, deal, c, queries, ring);
         } else {
-            help_role<D>(p, deal, c, queries, ring);
+            help_role<D>(tc, deal, c, queries, ring);
         }
     } else if (threadIdx.x == 0) {
         take_note(p, {});
@@ -598,18 +618,29 @@ cudaError_t resident(int shared, int each, int most, int& ctas) {
 template <int D>
 constexpr int max_ctas() { return 160 * Shape<D>::kCtas; }
 
-cudaError_t describe(CUtensorMap& map, const TreeParams& p, const char* pool, int box) {
-    Encode encode = nullptr;
-    const cudaError_t e = encoder(encode);
-    if (e != cudaSuccess) return e;
+bool encoded(Encode encode, CUtensorMap& map, const void* from, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* boxes) {
+    const cuuint32_t steps[4] = {1, 1, 1, 1};
+    return encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(from), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+cudaError_t describe(Encode encode, CUtensorMap& map, const TreeParams& p, const char* pool, int box) {
     const cuuint64_t page = static_cast<cuuint64_t>(p.a.heads) * p.a.head_dim * p.pages.page_tokens;
     const cuuint64_t dims[4] = {static_cast<cuuint64_t>(p.a.head_dim), static_cast<cuuint64_t>(p.pages.page_tokens), static_cast<cuuint64_t>(p.a.heads),
                                 static_cast<cuuint64_t>(p.pages.n_pages)};
     const cuuint64_t strides[3] = {p.a.token_stride * sizeof(T), p.a.head_stride * sizeof(T), (p.pages.n_pages > 1 ? p.a.page_stride : page) * sizeof(T)};
-    const cuuint32_t boxes[4] = {64, static_cast<cuuint32_t>(box * kGroup), 1, 1}, steps[4] = {1, 1, 1, 1};
-    const CUresult r = encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<char*>(pool), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+    const cuuint32_t boxes[4] = {64, static_cast<cuuint32_t>(box * kGroup), 1, 1};
+    return encoded(encode, map, pool, dims, strides, boxes) ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+// Queries in blocks of whole nodes: false where a block is none, or strides are none of a box.
+bool describe_queries(Encode encode, CUtensorMap& map, const TreeParams& p) {
+    if (kRows % p.a.group != 0) return false;
+    const cuuint64_t dims[4] = {static_cast<cuuint64_t>(p.a.head_dim), static_cast<cuuint64_t>(p.a.group), static_cast<cuuint64_t>(p.a.heads),
+                                static_cast<cuuint64_t>(p.trees.n_nodes)};
+    const cuuint64_t strides[3] = {p.a.q_head * sizeof(T), p.a.q_head * p.a.group * sizeof(T), p.a.q_row * sizeof(T)};
+    const cuuint32_t boxes[4] = {64, static_cast<cuuint32_t>(p.a.group), 1, static_cast<cuuint32_t>(kRows / p.a.group)};
+    return encoded(encode, map, p.a.q, dims, strides, boxes);
 }
 
 template <int D, Scores kScores>
@@ -620,8 +651,11 @@ cudaError_t launch_scores(const TreeParams& p, cudaStream_t s) {
     TcParams tc;
     tc.t = p;
     tc.box = std::gcd(p.page_groups, kTile / kGroup);
-    e = describe(tc.keys, p, p.a.k, tc.box);
-    if (e == cudaSuccess) e = describe(tc.values, p, p.a.v, tc.box);
+    Encode encode = nullptr;
+    e = encoder(encode);
+    if (e == cudaSuccess) e = describe(encode, tc.keys, p, p.a.k, tc.box);
+    if (e == cudaSuccess) e = describe(encode, tc.values, p, p.a.v, tc.box);
+    if (e == cudaSuccess) tc.query_box = describe_queries(encode, tc.queries, p);
     if (e == cudaSuccess) e = launch(tree_bf16_kernel<D, kScores>, ctas, kThreads, Shape<D>::kShared, 0, s, tc);
     return e != cudaSuccess || ctas == 1 ? e : launch_join<T, D, C>(p, ctas, s);
 }
