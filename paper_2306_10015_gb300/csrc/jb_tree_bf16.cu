@@ -340,18 +340,32 @@ __device__ __noinline__ void put_back(const TreeParams& p, const Piece& s, const
     }
 }
 
+// What the softmax's warps work on, held for all of them in shared memory: their registers are for scores.
+struct Work {
+    Deal deal;
+    Piece piece;
+    int more;
+};
+
 template <int D, Scores kScores>
-__device__ void softmax_role(const TreeParams& p, Deal deal, Control& c, Nodes& nodes) {
+__device__ void softmax_role(const TreeParams& p, Control& c, Work& work, Nodes& nodes) {
     using S = Shape<D>;
+    // Whether a tile's scores stay in registers from one pass to the next. Where a cap is put on them between the passes that
+    // pays (729 -> 630 us for three rows of 58000 tokens), and without one a short loop that takes them from tensor memory
+    // twice does (78 us and not 84 for 24 ragged rows).
+    constexpr bool kHeld = kScores == kCapped;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = threadIdx.x, d = p.a.head_dim;
     const uint32_t tmem = c.tmem + (static_cast<uint32_t>(32 * warp) << 16);
     const float by = kScores == kPlain ? p.a.scale * kLog2e : 1.0f;
     uint32_t tiles = 0;
     int tree = -1;
     bool ok = true;  // a wait that gives up leaves the loops as they are: other warps may wait for this one
-    Piece s;
-    Note cut = {};
-    while (deal.take(p, s)) {
+    const Piece& s = work.piece;
+    for (;;) {
+        any_of(false);  // nobody reads the last piece any more
+        if (threadIdx.x == 0) work.more = work.deal.take(p, work.piece);
+        any_of(false);
+        if (work.more == 0) break;
         if (s.tree != tree) fill_nodes<32 * kSoftmaxWarps>(p, s.span, nodes, threadIdx.x, any_of);
         tree = s.tree;
         const int rows = s.span.nodes * p.a.group, all = s.block * kRows + row;
@@ -368,59 +382,80 @@ __device__ void softmax_role(const TreeParams& p, Deal deal, Control& c, Nodes& 
                 const unsigned missing = *static_cast<volatile unsigned*>(&c.missing[tiles % 8]);
                 const bool edge = missing != 0 || edge_of(p, s.span, t0, kTile);
                 float tops[4] = {kLowest, kLowest, kLowest, kLowest};
-                if (kScores != kPlain || edge) {  // scores are put back as the softmax takes them
-                    unsigned seen[2] = {kAll, kAll};
+                const auto seen_at = [&](int i) {  // of 32 positions
+                    unsigned seen = seen_of(p, s.span, nodes, node, depth, t0 + 32 * i);
+                    if (missing >> (2 * i) & 1u) seen &= 0xFFFF0000u;
+                    if (missing >> (2 * i + 1) & 1u) seen &= 0x0000FFFFu;
+                    return seen;
+                };
+                uint32_t x[kHeld ? kTile : 1];
+                if constexpr (kHeld) {
+#pragma unroll
+                    for (int k = 0; k < kTile; k += 32) tmem_load32(at + k, x + k);
+                    tc_wait_loads();
+                    float most[2] = {};
+#pragma unroll
+                    for (int k = 0; k < kTile; ++k) most[k & 1] = fmaxf(most[k & 1], fabsf(__uint_as_float(x[k])));
+                    if (__all_sync(kAll, fmaxf(most[0], most[1]) * fabsf(p.cap_in) < kSmallCap)) {
+#pragma unroll
+                        for (int k = 0; k < kTile; k += 2) {
+                            const float2 y = capped_small(p, make_float2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])));
+                            x[k] = __float_as_uint(y.x);
+                            x[k + 1] = __float_as_uint(y.y);
+                        }
+                    } else {
+#pragma unroll 1
+                        for (int k = 0; k < kTile; k += 16) {
+                            uint32_t raw[16];
+                            tmem_load16(at + k, raw);
+                            tc_wait_loads();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) raw[e] = __float_as_uint(capped(p, __uint_as_float(raw[e])));
+                            tmem_store16(at + k, raw);
+                        }
+                        tc_wait_stores();
+#pragma unroll
+                        for (int k = 0; k < kTile; k += 32) tmem_load32(at + k, x + k);
+                        tc_wait_loads();
+                    }
                     if (edge) {
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            seen[i] = seen_of(p, s.span, nodes, node, depth, t0 + 32 * i);
-                            if (missing >> (2 * i) & 1u) seen[i] &= 0xFFFF0000u;
-                            if (missing >> (2 * i + 1) & 1u) seen[i] &= 0x0000FFFFu;
+                            const unsigned seen = seen_at(i);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (!(seen >> e & 1u)) x[32 * i + e] = __float_as_uint(-INFINITY);
                         }
                     }
+#pragma unroll
+                    for (int k = 0; k < kTile; ++k) tops[k % 4] = fmaxf(tops[k % 4], __uint_as_float(x[k]));
+                } else if (kScores == kBiased || edge) {  // scores are put back as the softmax takes them
+                    unsigned seen[2] = {kAll, kAll};
+                    if (edge) seen[0] = seen_at(0), seen[1] = seen_at(1);
                     uint32_t raw[16];
                     tmem_load16(at, raw);
 #pragma unroll 1
                     for (int k = 0; k < kTile; k += 16) {
                         const unsigned sees = seen[k >> 5] >> (k & 16);
-                        uint32_t x[16];
+                        uint32_t y[16];
                         tc_wait_loads();
-                        if constexpr (kScores == kCapped) {
-                            float most = 0.0f;
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) most = fmaxf(most, fabsf(__uint_as_float(raw[e])));
-                            if (__all_sync(kAll, most * fabsf(p.cap_in) < kSmallCap)) {
-#pragma unroll
-                                for (int e = 0; e < 16; e += 2) {
-                                    const float2 y = capped_small(p, make_float2(__uint_as_float(raw[e]), __uint_as_float(raw[e + 1])));
-                                    x[e] = __float_as_uint(y.x);
-                                    x[e + 1] = __float_as_uint(y.y);
-                                }
-                            } else {
-#pragma unroll
-                                for (int e = 0; e < 16; ++e) x[e] = __float_as_uint(capped(p, __uint_as_float(raw[e])));
-                            }
-                        } else if constexpr (kScores == kBiased) {
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) {
+                        for (int e = 0; e < 16; ++e) {
+                            y[e] = raw[e];
+                            if constexpr (kScores == kBiased) {
                                 const int t = t0 + k + e;
                                 int back = t - s.span.base - depth;
                                 if (t >= s.span.base && (sees >> e & 1u)) back = nodes.depth[t - s.span.base] - depth;
-                                x[e] = __float_as_uint(score<true>(p, __uint_as_float(raw[e]), slope, back));
+                                y[e] = __float_as_uint(score<true>(p, __uint_as_float(raw[e]), slope, back));
                             }
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) x[e] = raw[e];
                         }
                         if (k + 16 < kTile) tmem_load16(at + k + 16, raw);
-                        if (edge) {
 #pragma unroll
-                            for (int e = 0; e < 16; ++e)
-                                if (!(sees >> e & 1u)) x[e] = __float_as_uint(-INFINITY);
+                        for (int e = 0; e < 16; ++e) {
+                            if (!(sees >> e & 1u)) y[e] = __float_as_uint(-INFINITY);
+                            tops[e % 4] = fmaxf(tops[e % 4], __uint_as_float(y[e]));
                         }
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) tops[e % 4] = fmaxf(tops[e % 4], __uint_as_float(x[e]));
-                        tmem_store16(at + k, x);
+                        tmem_store16(at + k, y);
                     }
                     tc_wait_stores();
                 } else {
@@ -458,24 +493,36 @@ __device__ void softmax_role(const TreeParams& p, Deal deal, Control& c, Nodes& 
                 }
                 float2 part[2] = {};
                 const float2 by2 = make_float2(by, by), less = make_float2(-offset, -offset);
-                uint32_t raw[16];
-                tmem_load16(at, raw);
-#pragma unroll 1
-                for (int k = 0; k < kTile; k += 16) {
-                    uint32_t w[16];  // upper bits of 16 weights, then lower bits
-                    tc_wait_loads();
+                // 16 scores to the upper bits of their weights, then the lower ones
+                const auto weights_of = [&](const uint32_t* score, uint32_t to) {
+                    uint32_t w[16];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        float2 x = __ffma2_rn(make_float2(__uint_as_float(raw[2 * e]), __uint_as_float(raw[2 * e + 1])), by2, less);
-                        x.x = exp2_approx(x.x);
-                        x.y = exp2_approx(x.y);
-                        part[e & 1] = __fadd2_rn(part[e & 1], x);
-                        w[e] = pack_bf16(x.x, x.y);
-                        const float2 rest = __fadd2_rn(x, make_float2(-__uint_as_float(w[e] << 16), -__uint_as_float(w[e] & 0xFFFF0000u)));
+                        float2 y = __ffma2_rn(make_float2(__uint_as_float(score[2 * e]), __uint_as_float(score[2 * e + 1])), by2, less);
+                        y.x = exp2_approx(y.x);
+                        y.y = exp2_approx(y.y);
+                        part[e & 1] = __fadd2_rn(part[e & 1], y);
+                        w[e] = pack_bf16(y.x, y.y);
+                        const float2 rest = __fadd2_rn(y, make_float2(-__uint_as_float(w[e] << 16), -__uint_as_float(w[e] & 0xFFFF0000u)));
                         w[8 + e] = pack_bf16(rest.x, rest.y);
                     }
-                    if (k + 16 < kTile) tmem_load16(at + k + 16, raw);
-                    tmem_store16(at + k, w);
+                    tmem_store16(to, w);
+                };
+                if constexpr (kHeld) {
+#pragma unroll
+                    for (int k = 0; k < kTile; k += 16) weights_of(x + k, at + k);
+                } else {
+                    uint32_t raw[16];
+                    tmem_load16(at, raw);
+#pragma unroll 1
+                    for (int k = 0; k < kTile; k += 16) {
+                        uint32_t now[16];
+                        tc_wait_loads();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) now[e] = raw[e];
+                        if (k + 16 < kTile) tmem_load16(at + k + 16, raw);
+                        weights_of(now, at + k);
+                    }
                 }
                 l += (part[0].x + part[0].y) + (part[1].x + part[1].y);
                 tc_wait_stores();
@@ -488,7 +535,7 @@ __device__ void softmax_role(const TreeParams& p, Deal deal, Control& c, Nodes& 
             if (lane == 0) barrier_arrive(shared_address(&c.weights[buffer]));
         }
         const bool whole = s.from == 0 && s.to == s.span.tiles;
-        if (s.from == 0 && !whole) cut = {s.span.first, s.head, s.block, deal.last_of(s), rows, {}};
+        if (threadIdx.x == 0 && s.from == 0 && !whole) take_note(p, {s.span.first, s.head, s.block, work.deal.last_of(s), rows, {}});
         ok = barrier_wait(shared_address(&c.sums), (tiles - 1) & 1, &c.failed) && ok;
         tc_fence_after();
         if (idle) continue;
@@ -529,7 +576,6 @@ __device__ void softmax_role(const TreeParams& p, Deal deal, Control& c, Nodes& 
         }
         tc_fence_before();
     }
-    if (threadIdx.x == 0) take_note(p, cut);
 }
 
 template <int D, Scores kScores>
@@ -539,6 +585,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kCtas) tree_bf16_kernel(co
     extern __shared__ char dynamic[];
     __shared__ Control c;
     __shared__ Nodes nodes;
+    __shared__ Work work;
     __shared__ long long sums[kThreads / 32], found[2];
     const int warp = same(static_cast<int>(threadIdx.x) >> 5);
     const uint32_t queries = (shared_address(dynamic) + 1023) & ~1023u, ring = queries + S::kQueries * S::kQueryBytes;
@@ -571,7 +618,11 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kCtas) tree_bf16_kernel(co
     Deal deal;
     if (deal.start(p, blockIdx.x, gridDim.x, sums, found)) {
         if (warp < kSoftmaxWarps) {
-            softmax_role<D, kScores>(p, deal, c, nodes);
+            if (threadIdx.x == 0) {
+                take_note(p, {});
+                work.deal = deal;
+            }
+            softmax_role<D, kScores>(p, c, work, nodes);
         } else if (warp == kSoftmaxWarps) {
             product_role<D>(p, deal, c, queries, ring);
             if ((threadIdx.x & 31) == 0) {
