@@ -14,6 +14,7 @@
 // Loops are kept short: a warp that runs alone through code that is longer than its instruction cache waits for
 // instructions (128 positions of a thread unrolled: 8000 cycles for as many positions). Nor is cp.async for keys and
 // values: a warp issued one in 170 cycles, 10000 for 128 positions.
+#include <algorithm>
 #include <atomic>
 #include <numeric>
 
@@ -29,29 +30,36 @@ namespace {
 using T = __nv_bfloat16;
 
 constexpr unsigned kAll = 0xFFFFFFFFu;
-constexpr int kRows = 128, kTile = 64;
-using C = Cut<kRows, kTile, 2>;
-constexpr int kSoftmaxWarps = 4, kHelpWarps = 2;
-constexpr int kThreads = 32 * (kSoftmaxWarps + 2 + kHelpWarps);
-constexpr int kHelpThreads = 32 * kHelpWarps;
+constexpr int kRows = 128, kTile = 64;  // of a product's tile
+constexpr int kHelpWarps = 2, kHelpThreads = 32 * kHelpWarps;
 constexpr int kScoreTiles = 2;
 constexpr float kSlack = 8.0f;       // how far a row may exceed its maximum before sums are scaled, in powers of two
-using Deal = Dealer<C, kThreads>;
 
 // What a score goes through on its way to the softmax.
 enum Scores { kPlain, kCapped, kBiased };  // a positive scale alone; a cap; a bias, with or without a cap, or any scale
 
-template <int D>
+// Heads of up to D elements, blocks of kGroups x 128 rows.
+template <int D, int kGroups>
 struct Shape {
-    static constexpr int kCtas = D == 256 ? 1 : 2;     // on an SM
-    static constexpr int kSlots = D == 64 ? 8 : 4;
+    static_assert(kGroups == 1 || D <= 128);
+    static constexpr int kBlock = kGroups * kRows;
+    using C = Cut<kBlock, kTile, 2>;
+    static constexpr int kSoftmaxWarps = 4 * kGroups, kThreads = 32 * (kSoftmaxWarps + 2 + kHelpWarps);
+    using Deal = Dealer<C, kThreads>;
+    static constexpr int kCtas = D == 256 || kGroups == 2 ? 1 : 2;     // on an SM
+    static constexpr int kSlots = D == 64 || kGroups == 2 ? 8 : 4;
     static constexpr int kQueries = D == 64 ? 2 : 1;   // blocks of queries that there is room for
-    static constexpr uint32_t kTileBytes = kTile * D * 2, kQueryBytes = kRows * D * 2;
+    static constexpr uint32_t kTileBytes = kTile * D * 2, kQueryBytes = kRows * D * 2;  // of a group
     static constexpr uint32_t kPanel = kTile * 128, kQueryPanel = kRows * 128;  // 64 elements of all rows
-    static constexpr uint32_t kSums = kScoreTiles * kTile;                      // column of O
-    static constexpr uint32_t kColumns = D == 256 ? 512 : 256;                  // of tensor memory
-    static constexpr int kShared = 1024 + kQueries * kQueryBytes + kSlots * kTileBytes;
-    static_assert(kSums + D <= kColumns && kSlots % 2 == 0);  // even: values are always in odd slots
+    static constexpr uint32_t kSums = kScoreTiles * kTile;                      // column of a group's O
+    static constexpr uint32_t kGroupColumns = D == 256 ? 512 : 256, kColumns = kGroups * kGroupColumns;  // of tensor memory
+    static constexpr int kGroupsOf = kGroups;
+    static __device__ __forceinline__ int groups_of(const TreeParams& p, const Piece& s) {  // of the block that have rows
+        return kGroups == 1 || s.span.nodes * p.a.group - s.block * kBlock <= kRows ? 1 : 2;
+    }
+    static __device__ __forceinline__ uint32_t query_of(uint32_t block, uint32_t group) { return (block * kGroups + group) * kQueryBytes; }
+    static constexpr int kShared = 1024 + kQueries * kGroups * kQueryBytes + kSlots * kTileBytes;
+    static_assert(kSums + D <= kGroupColumns && kColumns <= 512 && kSlots % 2 == 0);  // even: values are always in odd slots
 };
 
 struct TcParams {
@@ -63,7 +71,8 @@ struct TcParams {
 };
 
 struct Control {
-    unsigned long long full[8], clean[8], empty[8], edges[8], scores[kScoreTiles], weights[kScoreTiles], queries[2], queries_read[2], sums, drained;
+    unsigned long long full[8], clean[8], empty[8], edges[8], queries[2], queries_read[2], drained;
+    unsigned long long scores[2][kScoreTiles], weights[2][kScoreTiles], sums[2];  // of each group of rows
     uint32_t tmem;
     int failed;
     int not_finite;          // a value that some rows see and others do not was not finite, in some tile so far
@@ -83,9 +92,8 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 
 // Keys and values of the blocks' tiles, in the order in which they are needed. Lane i copies box i of a tile: `box` groups of
 // 64 elements.
-template <int D>
-__device__ void copy_role(const TcParams& tc, Deal deal, Control& c, uint32_t queries, uint32_t ring) {
-    using S = Shape<D>;
+template <typename S, int D>
+__device__ void copy_role(const TcParams& tc, typename S::Deal deal, Control& c, uint32_t queries, uint32_t ring) {
     constexpr int kGroups = kTile / kGroup, kPanels = D / 64;
     const TreeParams& p = tc.t;
     const int lane = threadIdx.x & 31, panel = lane % kPanels, group = lane / kPanels * tc.box;  // group: of the tile
@@ -143,12 +151,14 @@ __device__ void copy_role(const TcParams& tc, Deal deal, Control& c, uint32_t qu
                 if (real) copy_box(at + panel * S::kPanel + group * (kGroup * 128), kind == 0 ? &tc.keys : &tc.values, 64 * panel, y, s.head, w, shared_address(&c.full[slot]));
                 ++copies;
                 if (tc.query_box && kind == 0 && tile == s.span.first_tile + s.from) {
-                    const uint32_t b = blocks % S::kQueries, to = queries + b * S::kQueryBytes;
+                    const uint32_t b = blocks % S::kQueries;
                     if (!__all_sync(kAll, barrier_wait(shared_address(&c.queries_read[b]), (blocks / S::kQueries & 1) ^ 1, &c.failed))) return give_up();
-                    if (lane == 0) barrier_arrive_bytes(shared_address(&c.queries[b]), (p.a.head_dim + 63) / 64 * S::kQueryPanel);
+                    const int groups = S::groups_of(p, s), g = lane / kPanels, x = 64 * (lane % kPanels);
+                    if (lane == 0) barrier_arrive_bytes(shared_address(&c.queries[b]), groups * ((p.a.head_dim + 63) / 64) * S::kQueryPanel);
                     __syncwarp();
-                    if (lane < kPanels && 64 * lane < p.a.head_dim)
-                        copy_box(to + lane * S::kQueryPanel, &tc.queries, 64 * lane, 0, s.head, s.span.first + s.block * (kRows / p.a.group), shared_address(&c.queries[b]));
+                    if (g < groups && x < p.a.head_dim)
+                        copy_box(queries + S::query_of(b, g) + x / 64 * S::kQueryPanel, &tc.queries, x, 0, s.head,
+                                 s.span.first + (s.block * S::kGroupsOf + g) * (kRows / p.a.group), shared_address(&c.queries[b]));
                     ++blocks;
                 }
             }
@@ -156,14 +166,13 @@ __device__ void copy_role(const TcParams& tc, Deal deal, Control& c, uint32_t qu
     }
 }
 
-// Queries of the block, by all helpers. Rows that are not real stay what they were: their results go nowhere.
-template <int D>
-__device__ void copy_queries(const TreeParams& p, const Piece& s, uint32_t to) {
-    using S = Shape<D>;
+// 128 rows of queries from row `first` of the tree's on, by all helpers. Rows that are not real stay what they were: their results go nowhere.
+template <typename S, int D>
+__device__ void copy_queries(const TreeParams& p, const Piece& s, int first, uint32_t to) {
     constexpr int kPieces = D / 8, kStep = kHelpThreads / kPieces;
-    const int u = threadIdx.x - 32 * (kSoftmaxWarps + 2), piece = u % kPieces, row0 = u / kPieces, rows = s.span.nodes * p.a.group;
-    const int rows_here = min(kRows, rows - s.block * kRows);
-    int all = s.block * kRows + row0, node = all / p.a.group, h = all - node * p.a.group;
+    const int u = threadIdx.x - 32 * (S::kSoftmaxWarps + 2), piece = u % kPieces, row0 = u / kPieces, rows = s.span.nodes * p.a.group;
+    const int rows_here = min(kRows, rows - first);
+    int all = first + row0, node = all / p.a.group, h = all - node * p.a.group;
     const T* from = reinterpret_cast<const T*>(p.a.q) + s.span.first * p.a.q_row + static_cast<uint64_t>(s.head) * p.a.group * p.a.q_head + 8 * piece;
     const bool held = 8 * piece < p.a.head_dim;
     constexpr int kAhead = 8;
@@ -188,10 +197,9 @@ __device__ void copy_queries(const TreeParams& p, const Piece& s, uint32_t to) {
 
 // A value that is not finite must not meet a weight of zero: it is taken out here and added at the end to the rows that see
 // it. So are the rows outside [lo, hi), which nobody sees. True if there was one inside.
-template <int D>
+template <typename S, int D>
 __device__ bool clean_values(uint32_t tile, int lo, int hi) {
-    using S = Shape<D>;
-    const int u = threadIdx.x - 32 * (kSoftmaxWarps + 2);
+    const int u = threadIdx.x - 32 * (S::kSoftmaxWarps + 2);
     bool bad = false;
 #pragma unroll 2
     for (int i = u; i < kTile * (D / 8); i += kHelpThreads) {
@@ -212,9 +220,8 @@ __device__ bool clean_values(uint32_t tile, int lo, int hi) {
     return bad;
 }
 
-template <int D>
-__device__ void help_role(const TcParams& tc, Deal deal, Control& c, uint32_t queries, uint32_t ring) {
-    using S = Shape<D>;
+template <typename S, int D>
+__device__ void help_role(const TcParams& tc, typename S::Deal deal, Control& c, uint32_t queries, uint32_t ring) {
     const TreeParams& p = tc.t;
     const int lane = threadIdx.x & 31;
     uint32_t blocks = 0, tiles = 0, edges = 0;
@@ -228,7 +235,7 @@ __device__ void help_role(const TcParams& tc, Deal deal, Control& c, uint32_t qu
         const uint32_t b = blocks % S::kQueries;
         if (!__all_sync(kAll, barrier_wait(shared_address(&c.queries_read[b]), (blocks / S::kQueries & 1) ^ 1, &c.failed))) return false;
         ++blocks;
-        copy_queries<D>(p, s, queries + b * S::kQueryBytes);
+        for (int g = 0; g < S::groups_of(p, s); ++g) copy_queries<S, D>(p, s, s.block * S::kBlock + g * kRows, queries + S::query_of(b, g));
         tell(&c.queries[b]);
         return true;
     };
@@ -244,7 +251,7 @@ __device__ void help_role(const TcParams& tc, Deal deal, Control& c, uint32_t qu
             // first that its copy has begun: the slot's own phase may be any before that
             if (!__all_sync(kAll, barrier_wait_idle(shared_address(&c.edges[e % 8]), e / 8 & 1, &c.failed))) return;
             if (!__all_sync(kAll, barrier_wait(shared_address(&c.full[slot]), i / S::kSlots & 1, &c.failed))) return;
-            if (clean_values<D>(ring + slot * S::kTileBytes, s.span.lo - tile * kTile, s.span.len - tile * kTile))
+            if (clean_values<S, D>(ring + slot * S::kTileBytes, s.span.lo - tile * kTile, s.span.len - tile * kTile))
                 *static_cast<volatile int*>(&c.not_finite) = 1;
             tell(&c.clean[slot]);
         }
@@ -254,67 +261,82 @@ __device__ void help_role(const TcParams& tc, Deal deal, Control& c, uint32_t qu
     }
 }
 
-template <int D>
-__device__ void product_role(const TreeParams& p, Deal deal, Control& c, uint32_t queries, uint32_t ring) {
-    using S = Shape<D>;
+template <typename S, int D>
+__device__ void product_role(const TreeParams& p, typename S::Deal deal, Control& c, uint32_t queries, uint32_t ring) {
     const int steps = (p.a.head_dim + 15) / 16;
     constexpr uint32_t scores = product_descriptor(kTile, false);
     const uint32_t values = product_descriptor(16 * steps, true);
     const uint32_t tmem = same(c.tmem);
-    uint32_t tiles = 0, blocks = 0;  // so far
+    uint32_t tiles = 0, blocks = 0, second = 0;  // so far; second: tiles that the second group had no rows for
     // The whole warp runs this and one lane issues: operands are then the warp's, which products want them to be.
     const auto wait = [&](unsigned long long* bar, uint32_t parity) {
         const bool ok = __all_sync(kAll, barrier_wait(shared_address(bar), parity, &c.failed));
         tc_fence_after();
         return ok;
     };
-    const auto scores_of = [&](uint32_t tile, bool last) {
-        const uint32_t i = 2 * tile, b = blocks % S::kQueries;
-        if (!wait(&c.full[i % S::kSlots], i / S::kSlots & 1)) return false;
-        const uint32_t k = tile_descriptor(ring + i % S::kSlots * S::kTileBytes, 16), q = tile_descriptor(queries + b * S::kQueryBytes, 16);
-        const uint32_t to = tmem + tile % kScoreTiles * kTile;
-        if (elected()) {
-#pragma unroll
-            for (int e = 0; e < D / 16; ++e)
-                if (e < steps)
-                    tc_product(to, q + ((e / 4 * S::kQueryPanel + e % 4 * 32) >> 4), k + ((e / 4 * S::kPanel + e % 4 * 32) >> 4), scores, e > 0);
-            tc_commit(shared_address(&c.empty[i % S::kSlots]));
-            tc_commit(shared_address(&c.scores[tile % kScoreTiles]));
-            if (last) tc_commit(shared_address(&c.queries_read[b]));
-        }
-        __syncwarp();
-        return true;
-    };
     Piece s;
     for (; same(static_cast<int>(deal.take(p, s))) != 0; ++blocks) {
-        const uint32_t n = same(s.to - s.from);
-        if (!wait(&c.queries[blocks % S::kQueries], blocks / S::kQueries & 1)) return;
-        if (!scores_of(tiles, n == 1)) return;
-        if (n > 1 && !scores_of(tiles + 1, n == 2)) return;
+        const uint32_t n = same(s.to - s.from), b = blocks % S::kQueries;
+        const int groups = same(S::groups_of(p, s));
+        // A tile's scores take the place of the weights of two tiles before, whose product has to be done. That of a block's
+        // first tile is, for the weights after them were given later than it ended.
+        const auto scores_of = [&](uint32_t tile, bool first, bool last) {
+            const uint32_t i = 2 * tile;
+            if (!wait(&c.full[i % S::kSlots], i / S::kSlots & 1)) return false;
+            const uint32_t k = tile_descriptor(ring + i % S::kSlots * S::kTileBytes, 16);
+#pragma unroll
+            for (int g = 0; g < S::kGroupsOf; ++g) {
+                if (g >= groups) break;
+                const uint32_t mine = tile - (g == 1 ? second : 0), to = tmem + g * S::kGroupColumns + mine % kScoreTiles * kTile;
+                if (!first && mine > 1 && !wait(&c.sums[g], mine & 1)) return false;
+                const uint32_t q = tile_descriptor(queries + S::query_of(b, g), 16);
+                if (elected()) {
+#pragma unroll
+                    for (int e = 0; e < D / 16; ++e)
+                        if (e < steps)
+                            tc_product(to, q + ((e / 4 * S::kQueryPanel + e % 4 * 32) >> 4), k + ((e / 4 * S::kPanel + e % 4 * 32) >> 4), scores, e > 0);
+                    tc_commit(shared_address(&c.scores[g][mine % kScoreTiles]));
+                    if (g + 1 == groups) {
+                        tc_commit(shared_address(&c.empty[i % S::kSlots]));
+                        if (last) tc_commit(shared_address(&c.queries_read[b]));
+                    }
+                }
+                __syncwarp();
+            }
+            return true;
+        };
+        if (!wait(&c.queries[b], blocks / S::kQueries & 1)) return;
+        if (!scores_of(tiles, true, n == 1)) return;
+        if (n > 1 && !scores_of(tiles + 1, false, n == 2)) return;
         for (uint32_t j = 0; j < n; ++j, ++tiles) {
-            const uint32_t i = 2 * tiles + 1, buffer = tiles % kScoreTiles;
-            if (!wait(&c.weights[buffer], tiles / kScoreTiles & 1)) return;
+            const uint32_t i = 2 * tiles + 1;
             if (!wait(&c.full[i % S::kSlots], i / S::kSlots & 1)) return;
             if (!wait(&c.clean[i % S::kSlots], i / S::kSlots & 1)) return;
-            const uint32_t v = tile_descriptor(ring + i % S::kSlots * S::kTileBytes, S::kPanel), w = tmem + buffer * kTile;
-            if (elected()) {
+            const uint32_t v = tile_descriptor(ring + i % S::kSlots * S::kTileBytes, S::kPanel);
 #pragma unroll
-                for (int half = 0; half < 2; ++half)  // the weights' upper and lower bits
+            for (int g = 0; g < S::kGroupsOf; ++g) {
+                if (g >= groups) break;
+                const uint32_t mine = tiles - (g == 1 ? second : 0), buffer = mine % kScoreTiles, at = tmem + g * S::kGroupColumns, w = at + buffer * kTile;
+                if (!wait(&c.weights[g][buffer], mine / kScoreTiles & 1)) return;
+                if (elected()) {
 #pragma unroll
-                    for (int e = 0; e < kTile / 16; ++e)
-                        tc_product_from_tmem(tmem + S::kSums, w + e * 16 + half * 8, v + (e * 2048 >> 4), values, half > 0 || e > 0 || j > 0);
-                tc_commit(shared_address(&c.empty[i % S::kSlots]));
-                tc_commit(shared_address(&c.sums));
+                    for (int half = 0; half < 2; ++half)  // the weights' upper and lower bits
+#pragma unroll
+                        for (int e = 0; e < kTile / 16; ++e)
+                            tc_product_from_tmem(at + S::kSums, w + e * 16 + half * 8, v + (e * 2048 >> 4), values, half > 0 || e > 0 || j > 0);
+                    tc_commit(shared_address(&c.sums[g]));
+                    if (g + 1 == groups) tc_commit(shared_address(&c.empty[i % S::kSlots]));
+                }
+                __syncwarp();
             }
-            __syncwarp();
-            if (j + 2 < n) {  // where this tile's weights were
-                if (!wait(&c.sums, tiles & 1) || !scores_of(tiles + 2, j + 3 == n)) return;
-            }
+            if (j + 2 < n && !scores_of(tiles + 2, false, j + 3 == n)) return;
         }
+        if (groups < S::kGroupsOf) second += n;
     }
 }
 
 // A barrier of the softmax warps, true if x is in one of their threads.
+template <int kSoftmaxWarps>
 __device__ __forceinline__ bool any_of(bool x) {
     uint32_t any;
     asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.or.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}"
@@ -341,42 +363,48 @@ __device__ __noinline__ void put_back(const TreeParams& p, const Piece& s, const
 }
 
 // What the softmax's warps work on, held for all of them in shared memory: their registers are for scores.
+template <typename Deal>
 struct Work {
     Deal deal;
     Piece piece;
     int more;
 };
 
-template <int D, Scores kScores>
-__device__ void softmax_role(const TreeParams& p, Control& c, Work& work, Nodes& nodes) {
-    using S = Shape<D>;
+template <typename S, int D, Scores kScores>
+__device__ void softmax_role(const TreeParams& p, Control& c, Work<typename S::Deal>& work, Nodes& nodes) {
+    using C = typename S::C;
     // Whether a tile's scores stay in registers from one pass to the next. Where a cap is put on them between the passes that
     // pays (729 -> 630 us for three rows of 58000 tokens), and without one a short loop that takes them from tensor memory
     // twice does (78 us and not 84 for 24 ragged rows).
     constexpr bool kHeld = kScores == kCapped;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = threadIdx.x, d = p.a.head_dim;
-    const uint32_t tmem = c.tmem + (static_cast<uint32_t>(32 * warp) << 16);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = warp / 4, row = threadIdx.x, d = p.a.head_dim;
+    const uint32_t tmem = c.tmem + g * S::kGroupColumns + (static_cast<uint32_t>(32 * (warp % 4)) << 16);
     const float by = kScores == kPlain ? p.a.scale * kLog2e : 1.0f;
-    uint32_t tiles = 0;
+    uint32_t tiles = 0, mine = 0;  // so far; mine: of those that the group has rows for
     int tree = -1;
     bool ok = true;  // a wait that gives up leaves the loops as they are: other warps may wait for this one
     const Piece& s = work.piece;
     for (;;) {
-        any_of(false);  // nobody reads the last piece any more
+        any_of<S::kSoftmaxWarps>(false);  // nobody reads the last piece any more
         if (threadIdx.x == 0) work.more = work.deal.take(p, work.piece);
-        any_of(false);
+        any_of<S::kSoftmaxWarps>(false);
         if (work.more == 0) break;
-        if (s.tree != tree) fill_nodes<32 * kSoftmaxWarps>(p, s.span, nodes, threadIdx.x, any_of);
+        if (s.tree != tree) fill_nodes<32 * S::kSoftmaxWarps>(p, s.span, nodes, threadIdx.x, any_of<S::kSoftmaxWarps>);
         tree = s.tree;
-        const int rows = s.span.nodes * p.a.group, all = s.block * kRows + row;
-        const bool real = all < rows, idle = s.block * kRows + 32 * warp >= rows;  // idle: none of the warp's rows is real
+        const int rows = s.span.nodes * p.a.group, all = s.block * S::kBlock + row;
+        if (threadIdx.x == 0 && s.from == 0 && s.to != s.span.tiles) take_note(p, {s.span.first, s.head, s.block, work.deal.last_of(s), rows, {}});
+        if (g >= S::groups_of(p, s)) {
+            tiles += s.to - s.from;
+            continue;
+        }
+        const bool real = all < rows, idle = s.block * S::kBlock + 32 * warp >= rows;  // idle: none of the warp's rows is real
         const int node = real ? all / p.a.group : 0, h = real ? all - node * p.a.group : 0, depth = real ? nodes.depth[node] : -1;
         const float slope = kScores == kBiased && real && p.a.slopes != nullptr ? p.a.slopes[s.head * p.a.group + h] * kLog2e : 0.0f;
         float m = kLowest, offset = 0.0f, l = 0.0f;  // offset: what is subtracted from scores, in powers of two; 0 before one is seen
-        for (int tile = s.span.first_tile + s.from; tile < s.span.first_tile + s.to; ++tile, ++tiles) {
+        for (int tile = s.span.first_tile + s.from; tile < s.span.first_tile + s.to; ++tile, ++tiles, ++mine) {
             const int t0 = tile * kTile;
-            const uint32_t buffer = tiles % kScoreTiles, at = tmem + buffer * kTile;
-            ok = barrier_wait(shared_address(&c.scores[buffer]), tiles / kScoreTiles & 1, &c.failed) && ok;
+            const uint32_t buffer = mine % kScoreTiles, at = tmem + buffer * kTile;
+            ok = barrier_wait(shared_address(&c.scores[g][buffer]), mine / kScoreTiles & 1, &c.failed) && ok;
             tc_fence_after();
             if (!idle) {
                 const unsigned missing = *static_cast<volatile unsigned*>(&c.missing[tiles % 8]);
@@ -478,7 +506,7 @@ __device__ void softmax_role(const TreeParams& p, Control& c, Work& work, Nodes&
                         l *= k;
                     }
                     if (tile != s.span.first_tile + s.from) {
-                        ok = barrier_wait(shared_address(&c.sums), (tiles - 1) & 1, &c.failed) && ok;
+                        ok = barrier_wait(shared_address(&c.sums[g]), (mine - 1) & 1, &c.failed) && ok;
                         tc_fence_after();
 #pragma unroll 1
                         for (int e = 0; e < D; e += 16) {
@@ -529,20 +557,19 @@ __device__ void softmax_role(const TreeParams& p, Control& c, Work& work, Nodes&
             }
             // The product of the tile before this one is done before this one's may start: so no wait is two phases of
             // its barrier away from what it waits for.
-            if (tiles > 0) ok = barrier_wait(shared_address(&c.sums), (tiles - 1) & 1, &c.failed) && ok;
+            if (mine > 0) ok = barrier_wait(shared_address(&c.sums[g]), (mine - 1) & 1, &c.failed) && ok;
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) barrier_arrive(shared_address(&c.weights[buffer]));
+            if (lane == 0) barrier_arrive(shared_address(&c.weights[g][buffer]));
         }
         const bool whole = s.from == 0 && s.to == s.span.tiles;
-        if (threadIdx.x == 0 && s.from == 0 && !whole) take_note(p, {s.span.first, s.head, s.block, work.deal.last_of(s), rows, {}});
-        ok = barrier_wait(shared_address(&c.sums), (tiles - 1) & 1, &c.failed) && ok;
+        ok = barrier_wait(shared_address(&c.sums[g]), (mine - 1) & 1, &c.failed) && ok;
         tc_fence_after();
         if (idle) continue;
         float* slot = slot_of<C, D>(p, gridDim.x, blockIdx.x, s.from == 0);
         if (!whole && real) {
-            slot[kRows * D + row] = m == kLowest || depth < 0 ? kLowest : offset;
-            slot[kRows * D + kRows + row] = depth < 0 ? 0.0f : l;
+            slot[S::kBlock * D + row] = m == kLowest || depth < 0 ? kLowest : offset;
+            slot[S::kBlock * D + S::kBlock + row] = depth < 0 ? 0.0f : l;
         }
         const float inverse = l > 0.0f ? 1.0f / l : 0.0f;
         const bool mend = *static_cast<volatile int*>(&c.not_finite) != 0;
@@ -578,17 +605,18 @@ __device__ void softmax_role(const TreeParams& p, Control& c, Work& work, Nodes&
     }
 }
 
-template <int D, Scores kScores>
-__global__ void __launch_bounds__(kThreads, Shape<D>::kCtas) tree_bf16_kernel(const __grid_constant__ TcParams tc) {
-    using S = Shape<D>;
+template <int D, int kGroups, Scores kScores>
+__global__ void __launch_bounds__(Shape<D, kGroups>::kThreads, Shape<D, kGroups>::kCtas) tree_bf16_kernel(const __grid_constant__ TcParams tc) {
+    using S = Shape<D, kGroups>;
+    constexpr int kThreads = S::kThreads, kSoftmaxWarps = S::kSoftmaxWarps;
     const TreeParams& p = tc.t;
     extern __shared__ char dynamic[];
     __shared__ Control c;
     __shared__ Nodes nodes;
-    __shared__ Work work;
+    __shared__ Work<typename S::Deal> work;
     __shared__ long long sums[kThreads / 32], found[2];
     const int warp = same(static_cast<int>(threadIdx.x) >> 5);
-    const uint32_t queries = (shared_address(dynamic) + 1023) & ~1023u, ring = queries + S::kQueries * S::kQueryBytes;
+    const uint32_t queries = (shared_address(dynamic) + 1023) & ~1023u, ring = queries + S::kQueries * kGroups * S::kQueryBytes;
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kSlots; ++i) {
             barrier_init(shared_address(&c.full[i]), 1);
@@ -596,15 +624,17 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kCtas) tree_bf16_kernel(co
             barrier_init(shared_address(&c.empty[i]), 1);
         }
         for (int i = 0; i < 8; ++i) barrier_init(shared_address(&c.edges[i]), 1);
-        for (int i = 0; i < kScoreTiles; ++i) {
-            barrier_init(shared_address(&c.scores[i]), 1);
-            barrier_init(shared_address(&c.weights[i]), kSoftmaxWarps);
+        for (int g = 0; g < kGroups; ++g) {
+            for (int i = 0; i < kScoreTiles; ++i) {
+                barrier_init(shared_address(&c.scores[g][i]), 1);
+                barrier_init(shared_address(&c.weights[g][i]), 4);
+            }
+            barrier_init(shared_address(&c.sums[g]), 1);
         }
         for (int i = 0; i < S::kQueries; ++i) {
             barrier_init(shared_address(&c.queries[i]), tc.query_box ? 1 : kHelpWarps);
             barrier_init(shared_address(&c.queries_read[i]), 1);
         }
-        barrier_init(shared_address(&c.sums), 1);
         barrier_init(shared_address(&c.drained), 1);
         c.failed = c.not_finite = 0;
         barriers_initialized();
@@ -615,16 +645,16 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kCtas) tree_bf16_kernel(co
     tc_fence_after();
     after_previous();
     let_next_start();
-    Deal deal;
+    typename S::Deal deal;
     if (deal.start(p, blockIdx.x, gridDim.x, sums, found)) {
         if (warp < kSoftmaxWarps) {
             if (threadIdx.x == 0) {
                 take_note(p, {});
                 work.deal = deal;
             }
-            softmax_role<D, kScores>(p, c, work, nodes);
+            softmax_role<S, D, kScores>(p, c, work, nodes);
         } else if (warp == kSoftmaxWarps) {
-            product_role<D>(p, deal, c, queries, ring);
+            product_role<S, D>(p, deal, c, queries, ring);
             if ((threadIdx.x & 31) == 0) {
                 if (*static_cast<volatile int*>(&c.failed)) {  // what is under way ends before tensor memory is given back
                     int late = 0;
@@ -634,9 +664,9 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kCtas) tree_bf16_kernel(co
             }
             __syncwarp();
         } else if (warp == kSoftmaxWarps + 1) {
-            copy_role<D>(tc, deal, c, queries, ring);
+            copy_role<S, D>(tc, deal, c, queries, ring);
         } else {
-            help_role<D>(tc, deal, c, queries, ring);
+            help_role<S, D>(tc, deal, c, queries, ring);
         }
     } else if (threadIdx.x == 0) {
         take_note(p, {});
@@ -645,7 +675,7 @@ __global__ void __launch_bounds__(kThreads, Shape<D>::kCtas) tree_bf16_kernel(co
     __syncthreads();
     tc_fence_after();
     if (warp == kSoftmaxWarps) tmem_free(c.tmem, S::kColumns);
-    write_zeros<T, C, kThreads>(p);
+    write_zeros<T, typename S::C, kThreads>(p);
 }
 
 // SMs of a device, asked for once, and the kernel's share of shared memory set.
@@ -666,8 +696,8 @@ cudaError_t resident(int shared, int each, int most, int& ctas) {
     return cudaSuccess;
 }
 
-template <int D>
-constexpr int max_ctas() { return 160 * Shape<D>::kCtas; }
+template <int D, int kGroups>
+constexpr int max_ctas() { return 160 * Shape<D, kGroups>::kCtas; }
 
 bool encoded(Encode encode, CUtensorMap& map, const void* from, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* boxes) {
     const cuuint32_t steps[4] = {1, 1, 1, 1};
@@ -694,10 +724,11 @@ bool describe_queries(Encode encode, CUtensorMap& map, const TreeParams& p) {
     return encoded(encode, map, p.a.q, dims, strides, boxes);
 }
 
-template <int D, Scores kScores>
+template <int D, int kGroups, Scores kScores>
 cudaError_t launch_scores(const TreeParams& p, cudaStream_t s) {
+    using S = Shape<D, kGroups>;
     int ctas = 0;
-    cudaError_t e = resident<tree_bf16_kernel<D, kScores>>(Shape<D>::kShared, Shape<D>::kCtas, max_ctas<D>(), ctas);
+    cudaError_t e = resident<tree_bf16_kernel<D, kGroups, kScores>>(S::kShared, S::kCtas, max_ctas<D, kGroups>(), ctas);
     if (e != cudaSuccess) return e;
     TcParams tc;
     tc.t = p;
@@ -707,22 +738,32 @@ cudaError_t launch_scores(const TreeParams& p, cudaStream_t s) {
     if (e == cudaSuccess) e = describe(encode, tc.keys, p, p.a.k, tc.box);
     if (e == cudaSuccess) e = describe(encode, tc.values, p, p.a.v, tc.box);
     if (e == cudaSuccess) tc.query_box = describe_queries(encode, tc.queries, p);
-    if (e == cudaSuccess) e = launch(tree_bf16_kernel<D, kScores>, ctas, kThreads, Shape<D>::kShared, 0, s, tc);
-    return e != cudaSuccess || ctas == 1 ? e : launch_join<T, D, C>(p, ctas, s);
+    if (e == cudaSuccess) e = launch(tree_bf16_kernel<D, kGroups, kScores>, ctas, S::kThreads, S::kShared, 0, s, tc);
+    return e != cudaSuccess || ctas == 1 ? e : launch_join<T, D, typename S::C>(p, ctas, s);
+}
+
+template <int D, int kGroups>
+cudaError_t launch_groups(const TreeParams& p, cudaStream_t s) {
+    if (p.a.slopes != nullptr || (p.a.softcap == 0.0f && !(p.a.scale > 0.0f))) return launch_scores<D, kGroups, kBiased>(p, s);
+    return p.a.softcap > 0.0f ? launch_scores<D, kGroups, kCapped>(p, s) : launch_scores<D, kGroups, kPlain>(p, s);
 }
 
 template <int D>
 cudaError_t launch_d(const TreeParams& p, cudaStream_t s) {
-    if (p.a.slopes != nullptr || (p.a.softcap == 0.0f && !(p.a.scale > 0.0f))) return launch_scores<D, kBiased>(p, s);
-    return p.a.softcap > 0.0f ? launch_scores<D, kCapped>(p, s) : launch_scores<D, kPlain>(p, s);
+    if constexpr (D <= 128)
+        if (static_cast<long long>(p.trees.n_nodes) * p.a.group > static_cast<long long>(kRows) * p.trees.n) return launch_groups<D, 2>(p, s);
+    return launch_groups<D, 1>(p, s);
 }
+
+template <int D, int kGroups>
+constexpr size_t floats_of() { return workspace_floats(max_ctas<D, kGroups>(), Shape<D, kGroups>::kBlock, D); }
 
 }  // namespace
 
 uint64_t tree_workspace_bf16(int head_dim) {
-    const size_t floats = head_dim <= 64    ? workspace_floats(max_ctas<64>(), kRows, 64)
-                          : head_dim <= 128 ? workspace_floats(max_ctas<128>(), kRows, 128)
-                                            : workspace_floats(max_ctas<256>(), kRows, 256);
+    const size_t floats = head_dim <= 64    ? std::max(floats_of<64, 1>(), floats_of<64, 2>())
+                          : head_dim <= 128 ? std::max(floats_of<128, 1>(), floats_of<128, 2>())
+                                            : floats_of<256, 1>();
     return sizeof(float) * floats;
 }
 
