@@ -31,7 +31,6 @@ using T = __nv_bfloat16;
 
 constexpr unsigned kAll = 0xFFFFFFFFu;
 constexpr int kRows = 128, kTile = 64;  // of a product's tile
-constexpr int kHelpWarps = 2, kHelpThreads = 32 * kHelpWarps;
 constexpr int kScoreTiles = 2;
 constexpr float kSlack = 8.0f;       // how far a row may exceed its maximum before sums are scaled, in powers of two
 
@@ -44,7 +43,9 @@ struct Shape {
     static_assert(kGroups == 1 || D <= 128);
     static constexpr int kBlock = kGroups * kRows;
     using C = Cut<kBlock, kTile, 2>;
-    static constexpr int kSoftmaxWarps = 4 * kGroups, kThreads = 32 * (kSoftmaxWarps + 2 + kHelpWarps);
+    // Warps: of the softmax, one for each group's products, one that copies, the helpers.
+    static constexpr int kSoftmaxWarps = 4 * kGroups, kHelpWarps = 3 - kGroups, kHelpThreads = 32 * kHelpWarps;
+    static constexpr int kCopyWarp = kSoftmaxWarps + kGroups, kFirstHelper = 32 * (kCopyWarp + 1), kThreads = kFirstHelper + kHelpThreads;
     using Deal = Dealer<C, kThreads>;
     static constexpr int kCtas = D == 256 || kGroups == 2 ? 1 : 2;     // on an SM
     static constexpr int kSlots = D == 64 || kGroups == 2 ? 8 : 4;
@@ -71,7 +72,7 @@ struct TcParams {
 };
 
 struct Control {
-    unsigned long long full[8], clean[8], empty[8], edges[8], queries[2], queries_read[2], drained;
+    unsigned long long full[8], clean[8], empty[8], edges[8], queries[2], queries_read[2], drained[2];
     unsigned long long scores[2][kScoreTiles], weights[2][kScoreTiles], sums[2];  // of each group of rows
     uint32_t tmem;
     int failed;
@@ -144,7 +145,7 @@ __device__ void copy_role(const TcParams& tc, typename S::Deal deal, Control& c,
                     barrier_arrive_bytes(shared_address(&c.full[slot]), bytes);
                     if (kind == 1) {
                         if (edge_of(p, s.span, tile * kTile, kTile)) barrier_arrive(shared_address(&c.edges[edges++ % 8]));
-                        else barrier_arrive_count(shared_address(&c.clean[slot]), kHelpWarps);
+                        else barrier_arrive_count(shared_address(&c.clean[slot]), S::kHelpWarps);
                     }
                 }
                 __syncwarp();
@@ -169,8 +170,8 @@ __device__ void copy_role(const TcParams& tc, typename S::Deal deal, Control& c,
 // 128 rows of queries from row `first` of the tree's on, by all helpers. Rows that are not real stay what they were: their results go nowhere.
 template <typename S, int D>
 __device__ void copy_queries(const TreeParams& p, const Piece& s, int first, uint32_t to) {
-    constexpr int kPieces = D / 8, kStep = kHelpThreads / kPieces;
-    const int u = threadIdx.x - 32 * (S::kSoftmaxWarps + 2), piece = u % kPieces, row0 = u / kPieces, rows = s.span.nodes * p.a.group;
+    constexpr int kPieces = D / 8, kStep = S::kHelpThreads / kPieces;
+    const int u = threadIdx.x - S::kFirstHelper, piece = u % kPieces, row0 = u / kPieces, rows = s.span.nodes * p.a.group;
     const int rows_here = min(kRows, rows - first);
     int all = first + row0, node = all / p.a.group, h = all - node * p.a.group;
     const T* from = reinterpret_cast<const T*>(p.a.q) + s.span.first * p.a.q_row + static_cast<uint64_t>(s.head) * p.a.group * p.a.q_head + 8 * piece;
@@ -199,23 +200,34 @@ __device__ void copy_queries(const TreeParams& p, const Piece& s, int first, uin
 // it. So are the rows outside [lo, hi), which nobody sees. True if there was one inside.
 template <typename S, int D>
 __device__ bool clean_values(uint32_t tile, int lo, int hi) {
-    const int u = threadIdx.x - 32 * (S::kSoftmaxWarps + 2);
+    const int u = threadIdx.x - S::kFirstHelper;
+    constexpr int kAhead = S::kHelpWarps == 1 ? 8 : 2;
+    static_assert(kTile * (D / 8) % (kAhead * S::kHelpThreads) == 0);
     bool bad = false;
-#pragma unroll 2
-    for (int i = u; i < kTile * (D / 8); i += kHelpThreads) {
-        const uint32_t at = tile + i * 16;
-        const int row = i / 8 % kTile;
-        uint32_t w[4], any = 0;
-        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
-        const bool inside = row >= lo && row < hi;
+#pragma unroll 1
+    for (int i = u; i < kTile * (D / 8); i += kAhead * S::kHelpThreads) {
+        uint32_t w[kAhead][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t mask = ((w[e] & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((w[e] & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
-            any |= mask;
-            w[e] = inside ? w[e] & ~mask : 0;
+        for (int k = 0; k < kAhead; ++k)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(w[k][0]), "=r"(w[k][1]), "=r"(w[k][2]), "=r"(w[k][3]) : "r"(tile + (i + k * S::kHelpThreads) * 16) : "memory");
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int at = i + k * S::kHelpThreads, row = at / 8 % kTile;
+            const bool inside = row >= lo && row < hi;
+            uint32_t any = 0;  // an exponent of ones carries over into the sign's place
+#pragma unroll
+            for (int e = 0; e < 4; ++e) any |= (w[k][e] & 0x7F807F80u) + 0x00800080u;
+            any &= 0x80008000u;
+            if (any == 0 && inside) continue;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t mask = ((w[k][e] & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((w[k][e] & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+                w[k][e] = inside ? w[k][e] & ~mask : 0;
+            }
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(tile + at * 16), "r"(w[k][0]), "r"(w[k][1]), "r"(w[k][2]), "r"(w[k][3]) : "memory");
+            bad = bad || inside;
         }
-        if (any != 0 || !inside) asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
-        bad = bad || (any != 0 && inside);
     }
     return bad;
 }
@@ -261,77 +273,83 @@ __device__ void help_role(const TcParams& tc, typename S::Deal deal, Control& c,
     }
 }
 
+// Products of group g's rows.
 template <typename S, int D>
-__device__ void product_role(const TreeParams& p, typename S::Deal deal, Control& c, uint32_t queries, uint32_t ring) {
+__device__ void product_role(const TreeParams& p, typename S::Deal deal, Control& c, int g, uint32_t queries, uint32_t ring) {
     const int steps = (p.a.head_dim + 15) / 16;
     constexpr uint32_t scores = product_descriptor(kTile, false);
+    constexpr bool kDeep = S::kSlots >= 8;
     const uint32_t values = product_descriptor(16 * steps, true);
-    const uint32_t tmem = same(c.tmem);
-    uint32_t tiles = 0, blocks = 0, second = 0;  // so far; second: tiles that the second group had no rows for
+    const uint32_t tmem = same(c.tmem) + g * S::kGroupColumns;
+    uint32_t tiles = 0, mine = 0;  // so far; mine: of those that the group has rows for
     // The whole warp runs this and one lane issues: operands are then the warp's, which products want them to be.
     const auto wait = [&](unsigned long long* bar, uint32_t parity) {
         const bool ok = __all_sync(kAll, barrier_wait(shared_address(bar), parity, &c.failed));
         tc_fence_after();
         return ok;
     };
+    const auto came = [&](uint32_t copy) { return wait(&c.full[copy % S::kSlots], copy / S::kSlots & 1); };
     Piece s;
-    for (; same(static_cast<int>(deal.take(p, s))) != 0; ++blocks) {
+    for (uint32_t blocks = 0; same(static_cast<int>(deal.take(p, s))) != 0; ++blocks) {
         const uint32_t n = same(s.to - s.from), b = blocks % S::kQueries;
-        const int groups = same(S::groups_of(p, s));
+        if (!wait(&c.queries[b], blocks / S::kQueries & 1)) return;
+        if (g >= same(S::groups_of(p, s))) {  // nothing to do, which the copies have to know
+            for (uint32_t copy = 2 * tiles; copy < 2 * (tiles + n); ++copy) {
+                if (!came(copy)) return;
+                if (elected()) barrier_arrive(shared_address(&c.empty[copy % S::kSlots]));
+                __syncwarp();
+            }
+            if (elected()) barrier_arrive(shared_address(&c.queries_read[b]));
+            __syncwarp();
+            tiles += n;
+            continue;
+        }
+        const uint32_t q = tile_descriptor(queries + S::query_of(b, g), 16);
+        const auto scores_of = [&](uint32_t tile, bool last) {  // of the block's tile
+            const uint32_t slot = 2 * (tiles + tile) % S::kSlots, k = tile_descriptor(ring + slot * S::kTileBytes, 16), buffer = (mine + tile) % kScoreTiles;
+            if (elected()) {
+#pragma unroll
+                for (int e = 0; e < D / 16; ++e)
+                    if (e < steps)
+                        tc_product(tmem + buffer * kTile, q + ((e / 4 * S::kQueryPanel + e % 4 * 32) >> 4), k + ((e / 4 * S::kPanel + e % 4 * 32) >> 4), scores, e > 0);
+                tc_commit(shared_address(&c.empty[slot]));
+                tc_commit(shared_address(&c.scores[g][buffer]));
+                if (last) tc_commit(shared_address(&c.queries_read[b]));
+            }
+            __syncwarp();
+        };
         // A tile's scores take the place of the weights of two tiles before, whose product has to be done. That of a block's
         // first tile is, for the weights after them were given later than it ended.
-        const auto scores_of = [&](uint32_t tile, bool first, bool last) {
-            const uint32_t i = 2 * tile;
-            if (!wait(&c.full[i % S::kSlots], i / S::kSlots & 1)) return false;
-            const uint32_t k = tile_descriptor(ring + i % S::kSlots * S::kTileBytes, 16);
-#pragma unroll
-            for (int g = 0; g < S::kGroupsOf; ++g) {
-                if (g >= groups) break;
-                const uint32_t mine = tile - (g == 1 ? second : 0), to = tmem + g * S::kGroupColumns + mine % kScoreTiles * kTile;
-                if (!first && mine > 1 && !wait(&c.sums[g], mine & 1)) return false;
-                const uint32_t q = tile_descriptor(queries + S::query_of(b, g), 16);
-                if (elected()) {
-#pragma unroll
-                    for (int e = 0; e < D / 16; ++e)
-                        if (e < steps)
-                            tc_product(to, q + ((e / 4 * S::kQueryPanel + e % 4 * 32) >> 4), k + ((e / 4 * S::kPanel + e % 4 * 32) >> 4), scores, e > 0);
-                    tc_commit(shared_address(&c.scores[g][mine % kScoreTiles]));
-                    if (g + 1 == groups) {
-                        tc_commit(shared_address(&c.empty[i % S::kSlots]));
-                        if (last) tc_commit(shared_address(&c.queries_read[b]));
-                    }
-                }
-                __syncwarp();
-            }
-            return true;
-        };
-        if (!wait(&c.queries[b], blocks / S::kQueries & 1)) return;
-        if (!scores_of(tiles, true, n == 1)) return;
-        if (n > 1 && !scores_of(tiles + 1, false, n == 2)) return;
-        for (uint32_t j = 0; j < n; ++j, ++tiles) {
-            const uint32_t i = 2 * tiles + 1;
-            if (!wait(&c.full[i % S::kSlots], i / S::kSlots & 1)) return;
-            if (!wait(&c.clean[i % S::kSlots], i / S::kSlots & 1)) return;
-            const uint32_t v = tile_descriptor(ring + i % S::kSlots * S::kTileBytes, S::kPanel);
-#pragma unroll
-            for (int g = 0; g < S::kGroupsOf; ++g) {
-                if (g >= groups) break;
-                const uint32_t mine = tiles - (g == 1 ? second : 0), buffer = mine % kScoreTiles, at = tmem + g * S::kGroupColumns, w = at + buffer * kTile;
-                if (!wait(&c.weights[g][buffer], mine / kScoreTiles & 1)) return;
-                if (elected()) {
-#pragma unroll
-                    for (int half = 0; half < 2; ++half)  // the weights' upper and lower bits
-#pragma unroll
-                        for (int e = 0; e < kTile / 16; ++e)
-                            tc_product_from_tmem(at + S::kSums, w + e * 16 + half * 8, v + (e * 2048 >> 4), values, half > 0 || e > 0 || j > 0);
-                    tc_commit(shared_address(&c.sums[g]));
-                    if (g + 1 == groups) tc_commit(shared_address(&c.empty[i % S::kSlots]));
-                }
-                __syncwarp();
-            }
-            if (j + 2 < n && !scores_of(tiles + 2, false, j + 3 == n)) return;
+        if (!came(2 * tiles)) return;
+        scores_of(0, n == 1);
+        if (n > 1) {
+            if (!came(2 * (tiles + 1)) || (mine > 0 && !wait(&c.sums[g], (mine - 1) & 1))) return;
+            scores_of(1, n == 2);
         }
-        if (groups < S::kGroupsOf) second += n;
+        for (uint32_t j = 0; j < n; ++j) {
+            const uint32_t i = 2 * (tiles + j) + 1, slot = i % S::kSlots, turn = mine + j, buffer = turn % kScoreTiles;
+            // What has come by now is looked at before the weights, from which on every look counts; with few slots keys have not
+            if (!came(i) || !wait(&c.clean[slot], i / S::kSlots & 1)) return;
+            if (kDeep && j + 2 < n && !came(i + 3)) return;
+            if (!wait(&c.weights[g][buffer], turn / kScoreTiles & 1)) return;
+            const uint32_t v = tile_descriptor(ring + slot * S::kTileBytes, S::kPanel), w = tmem + buffer * kTile;
+            if (elected()) {
+#pragma unroll
+                for (int half = 0; half < 2; ++half)  // the weights' upper and lower bits
+#pragma unroll
+                    for (int e = 0; e < kTile / 16; ++e)
+                        tc_product_from_tmem(tmem + S::kSums, w + e * 16 + half * 8, v + (e * 2048 >> 4), values, half > 0 || e > 0 || j > 0);
+                tc_commit(shared_address(&c.empty[slot]));
+                tc_commit(shared_address(&c.sums[g]));
+            }
+            __syncwarp();
+            if (j + 2 < n) {
+                if ((!kDeep && !came(i + 3)) || !wait(&c.sums[g], turn & 1)) return;
+                scores_of(j + 2, j + 3 == n);
+            }
+        }
+        tiles += n;
+        mine += n;
     }
 }
 
@@ -620,8 +638,8 @@ __global__ void __launch_bounds__(Shape<D, kGroups>::kThreads, Shape<D, kGroups>
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kSlots; ++i) {
             barrier_init(shared_address(&c.full[i]), 1);
-            barrier_init(shared_address(&c.clean[i]), kHelpWarps);
-            barrier_init(shared_address(&c.empty[i]), 1);
+            barrier_init(shared_address(&c.clean[i]), S::kHelpWarps);
+            barrier_init(shared_address(&c.empty[i]), kGroups);
         }
         for (int i = 0; i < 8; ++i) barrier_init(shared_address(&c.edges[i]), 1);
         for (int g = 0; g < kGroups; ++g) {
@@ -630,12 +648,12 @@ __global__ void __launch_bounds__(Shape<D, kGroups>::kThreads, Shape<D, kGroups>
                 barrier_init(shared_address(&c.weights[g][i]), 4);
             }
             barrier_init(shared_address(&c.sums[g]), 1);
+            barrier_init(shared_address(&c.drained[g]), 1);
         }
         for (int i = 0; i < S::kQueries; ++i) {
-            barrier_init(shared_address(&c.queries[i]), tc.query_box ? 1 : kHelpWarps);
-            barrier_init(shared_address(&c.queries_read[i]), 1);
+            barrier_init(shared_address(&c.queries[i]), tc.query_box ? 1 : S::kHelpWarps);
+            barrier_init(shared_address(&c.queries_read[i]), kGroups);
         }
-        barrier_init(shared_address(&c.drained), 1);
         c.failed = c.not_finite = 0;
         barriers_initialized();
     }
@@ -653,17 +671,18 @@ __global__ void __launch_bounds__(Shape<D, kGroups>::kThreads, Shape<D, kGroups>
                 work.deal = deal;
             }
             softmax_role<S, D, kScores>(p, c, work, nodes);
-        } else if (warp == kSoftmaxWarps) {
-            product_role<S, D>(p, deal, c, queries, ring);
+        } else if (warp < S::kCopyWarp) {
+            const int g = warp - kSoftmaxWarps;
+            product_role<S, D>(p, deal, c, g, queries, ring);
             if ((threadIdx.x & 31) == 0) {
                 if (*static_cast<volatile int*>(&c.failed)) {  // what is under way ends before tensor memory is given back
                     int late = 0;
-                    tc_commit(shared_address(&c.drained));
-                    barrier_wait(shared_address(&c.drained), 0, &late);
+                    tc_commit(shared_address(&c.drained[g]));
+                    barrier_wait(shared_address(&c.drained[g]), 0, &late);
                 }
             }
             __syncwarp();
-        } else if (warp == kSoftmaxWarps + 1) {
+        } else if (warp == S::kCopyWarp) {
             copy_role<S, D>(tc, deal, c, queries, ring);
         } else {
             help_role<S, D>(tc, deal, c, queries, ring);
