@@ -499,7 +499,8 @@ int jb_cache_append(const jb_pages* pages, const jb_kv* layer, const jb_rotation
  * A node whose chain of parents is not valid (an index not below its own, or below -1) gets
  * zeros, and so do the nodes of a tree whose row is out of range, holds fewer tokens than the
  * tree, or that has more than 256 nodes. Queries of no tree are left as they are.
- * Accuracy, missing pages, infinite scores and what unseen places hold: as jb_attend.
+ * Accuracy, missing pages, infinite scores and what unseen places hold: as jb_attend; bf16
+ * weights meet values with 16 bits.
  *   q_heads    a multiple of the layer's heads
  *   strides    in elements, multiples of 16 bytes; pointers 16-byte aligned. Outputs share bytes
  *              neither with one another nor with queries: JB_ERR_INVALID_ARG
@@ -533,10 +534,13 @@ uint64_t jb_cache_keep_workspace(const jb_trees* trees);
  * jb_q4_matmul -- products of n rows with a matrix of 4-bit weights, as they are between two
  * calls of jb_perturb_q4: y_i[o] = sum_k x_i[k] level[code] scale + bias[o], the weight of
  * output o and input k being element o in_features + k of the tensor.
- *   weights       numel = out_features in_features; its flat_offset is not looked at
+ *   weights       numel = out_features in_features, its codes 8-byte aligned (16-byte: large
+ *                 products are faster); its flat_offset is not looked at
+ *   out_features  at most 2^30
  *   in_features   a multiple of 64 (a block's scale belongs to one output), at most 65536
  *   dtype         JB_F32 or JB_BF16, of x, bias and y alike; sums are fp32. Levels enter bf16
- *                 products with 11 bits and fp32 products with 24, and so does x (bf16: all its bits)
+ *                 products with 11 bits and fp32 products with 22; x with all its bits or 22, but
+ *                 nothing finer than 2^-40 of the largest element of its row
  *   d_x           [n][in_features], 16-byte aligned, rows x_row_stride elements apart (a multiple
  *                 of 16 bytes)
  *   d_bias        [out_features], or NULL

@@ -12,6 +12,7 @@ namespace jb {
 
 constexpr int kMaxNodes = 256;           // drafted tokens of a tree
 constexpr int kMaxInner = 65536;         // columns of a matrix of 4-bit weights
+constexpr int kMaxOutputs = 1 << 30;     // its rows
 constexpr int kMaxAppendVecs = 1 << 20;  // 16-byte vectors of a token's queries and keys
 
 struct Append {

@@ -321,9 +321,9 @@ __device__ __forceinline__ float* slot_of(const TreeParams& p, int ctas, int wor
 __device__ __forceinline__ void take_note(const TreeParams& p, const Note& n) { reinterpret_cast<Note*>(p.a.ws)[blockIdx.x] = n; }
 
 // CTA (b, slice) joins a slice of the rows of the block that CTA b has the first part of. A thread adds up four values of
-// every part, four parts at a time so that the loads do not wait for one another. A few CTAs of many threads on each SM: it
-// is the chain of reads, note, sums, maxima, that takes the time, and CTAs that come in several rounds repeat it (304 blocks
-// of 128 rows by 32 slices of four rows: 12 us, by slices of kSlice @JOIN@).
+// every part, four parts at a time so that the loads do not wait for one another. A few CTAs of many threads on each SM: a
+// chain of reads (note, maxima and sums, values) is what takes the time where a block has few parts, and CTAs that come in
+// several rounds repeat it.
 constexpr int kJoinThreads = 256, kSlice = 32;
 template <typename T, int D, typename C>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ TreeParams p) {

@@ -138,13 +138,14 @@ def test_bad_products(jb):
     assert q4(jb, n=0, x=0, y=0, codes=0) == 0
     for kw, rc in ((dict(dtype=2), DTYPE), (dict(none=True), INV), (dict(out=0), INV), (dict(inner=0), INV), (dict(inner=32, numel=128 * 32), INV),
                    (dict(inner=250), INV), (dict(inner=65600, numel=128 * 65600), INV), (dict(n=-1), INV), (dict(numel=128 * 256 - 1), INV), (dict(out=127), INV),
-                   (dict(codes=0), INV), (dict(scale=0), INV), (dict(x=0), INV), (dict(y=0), INV), (dict(codes=FAKE + 4), MIS), (dict(scale=FAKE + 2), MIS),
+                   (dict(out=(1 << 30) + 1, inner=64, numel=64 * ((1 << 30) + 1), ys=(1 << 30) + 1), INV), (dict(codes=0), INV), (dict(scale=0), INV), (dict(x=0), INV), (dict(y=0), INV), (dict(codes=FAKE + 4), MIS), (dict(scale=FAKE + 2), MIS),
                    (dict(x=FAR + 8), MIS), (dict(xs=260), MIS), (dict(y=FAR + 1), MIS), (dict(bias=FAKE + 1), MIS), (dict(dtype=0, y=FAR + 2), MIS),
                    (dict(xs=1 << 50), INV), (dict(ys=1 << 50), INV), (dict(ys=127), INV), (dict(y=FAR), INV), (dict(y=FAR + 510), INV), (dict(y=FAKE + 100), INV),
                    (dict(y=FAKE + (1 << 30)), INV), (dict(bias=FAR + (1 << 20) + 2), INV), (dict(x=(1 << 64) - 256), INV), (dict(codes=(1 << 64) - 1024), INV)):
         assert q4(jb, **kw) == rc, kw
     need = lambda *a: jb.lib().jb_q4_matmul_workspace(*a)  # noqa: E731
     assert need(128, 256, 1, 2) == 0 and need(4096, 4096, 2, 1) == 0 and need(4096, 4000, 1, 1) == 0 and need(0, 4096, 1, 1) == 0
+    assert need((1 << 30) + 1, 64, 1, 1) == 0
     big = dict(numel=4096 * 4096, out=4096, inner=4096, xs=4096, ys=4096, n=9, ws=FAKE, size=need(4096, 4096, 1, 9))
     assert big["size"] > 9 * 4096 * 2
     for kw, rc in ((dict(ws=0), INV), (dict(ws=FAKE + 8), MIS), (dict(size=big["size"] - 1), INV)):

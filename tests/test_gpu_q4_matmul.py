@@ -200,10 +200,11 @@ def test_strides_outputs_and_later_tensors(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_repeatable_streams_and_graphs(dtype):
+@pytest.mark.parametrize("n", [12, 40])
+def test_repeatable_streams_and_graphs(dtype, n):
     table = weights(3000, 2048)
-    x = torch.randn(12, 2048, device="cuda").to(DT[dtype])
-    want = check(dtype, 12, 3000, 2048, bias=False, x=x, table=table)
+    x = torch.randn(n, 2048, device="cuda").to(DT[dtype])
+    want = check(dtype, n, 3000, 2048, bias=False, x=x, table=table)
     stream = torch.cuda.Stream()
     stream.wait_stream(torch.cuda.current_stream())
     a, b = jb.jb_q4_matmul(table, 0, x, 3000), jb.jb_q4_matmul(table, 0, x, 3000, stream=stream)
@@ -231,9 +232,37 @@ def test_between_two_perturbations():
         assert ((got.double() - want).abs() <= bound(x, w, None, want)).all()
 
 
-def test_large_matrices():
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_calls_side_by_side(dtype):
+    """Two streams and two captured graphs of one table, which keeps or makes a workspace for each of them."""
+    table = weights(8192, 4096)
+    x = [torch.randn(n, 4096, device="cuda").to(DT[dtype]) for n in (33, 20)]
+    want = [jb.jb_q4_matmul(table, 0, v, 8192) for v in x]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got, graphs, out = [[], []], [], []
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(jb.jb_q4_matmul(table, 0, x[i], 8192))
+    torch.cuda.synchronize()
+    for i, s in enumerate(streams):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            out.append([jb.jb_q4_matmul(table, 0, x[i], 8192) for _ in range(10)])
+        graphs.append(graph)
+    torch.cuda.synchronize()
+    for s, graph in zip(streams, graphs):
+        with torch.cuda.stream(s):
+            graph.replay()
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(y, want[i]) for y in got[i] + out[i])
+
+
+@pytest.mark.parametrize("out,inner,n", [(33000, 65536, 2), (140000, 16384, 1)])
+def test_large_matrices(out, inner, n):
     """More than 2^31 weights: offsets past 32 bits."""
-    out, inner = 33000, 65536
     codes = torch.zeros(out * inner // 2, dtype=torch.uint8, device="cuda")
     scale = torch.zeros(out * inner // 64, device="cuda")
     g = torch.Generator(device="cuda").manual_seed(1)
@@ -242,7 +271,7 @@ def test_large_matrices():
     scale[-tail // 64:] = torch.rand(tail // 64, device="cuda", generator=g)
     table = jb.Q4Table([(codes, scale, out * inner)])
     for dtype in ("f32", "bf16"):
-        x = torch.randn(2, inner, device="cuda", generator=g).to(DT[dtype])
+        x = torch.randn(n, inner, device="cuda", generator=g).to(DT[dtype])
         got = jb.jb_q4_matmul(table, 0, x, out)
         w = dense(jb.Q4Table([(codes[-tail // 2:], scale[-tail // 64:], tail)]), 0, 40, inner)
         want = x.double() @ w.T
