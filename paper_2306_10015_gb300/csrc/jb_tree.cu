@@ -1,223 +1,447 @@
 // jb_tree.cu -- attention of trees of drafted tokens over the pages of a cache: every node sees the tokens of its row
 // before the tree, its ancestors and itself.
 //   out = sum_t exp(x_t) v_t / sum_t exp(x_t),  x_t as in jb_attend.cu, positions by depth
+//
+// Here fp32, on the FMA units (bf16: jb_tree_bf16.cu). A CTA has a block of rows, whose queries are in shared memory, and lets
+// the row's keys and values pass by in tiles, which a warp copies ahead (TMA, swizzled by 128 bytes so that 16 rows of keys are
+// read without conflicts). A warp takes 16 rows (8 with heads of more than 128) and a part of a tile's positions: half of
+// its lanes have half of the rows each, so that a step of four elements is 8 reads of queries, which all lanes share, and
+// one or two of keys for up to 64 packed products; weights pass through shared memory to the same rows' lanes, which then
+// have columns of the values. The maximum of a row stays as it was until a score exceeds it by 2^8, so that lanes compare
+// notes only then.
+//
+// FMA units bound it where trees are large, and HBM where they are small; two warps a scheduler reach neither. @MEASURED@
+#include <algorithm>
 #include <atomic>
+#include <numeric>
 
 #include <cuda_bf16.h>
 
+#include "jb_tcgen05.cuh"
 #include "jb_tree.cuh"
 
 namespace jb {
 namespace {
 
-constexpr int kThreads = 128;
-constexpr int kRows = 16;   // rows of a block
-constexpr int kTile = 32;   // positions of a tile
-using C = Cut<kRows, kTile, 1>;
+constexpr unsigned kAll = 0xFFFFFFFFu;
+constexpr int kWarps = 8, kWorkThreads = 32 * kWarps, kThreads = kWorkThreads + 32;  // the last warp copies
+constexpr float kSlack = 8.0f;  // how far a row may exceed its maximum before sums are scaled, in powers of two
+constexpr int kCtas = 160;      // most
 
-__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
-template <int D>
-struct Shared {
-    float q[kRows][D];
-    float k[kTile][D + 4];
-    float v[kTile][D];
-    float w[kTile][kRows];
-    unsigned seen[kRows];
-    float factor[kRows];
+// Heads of up to D elements; kGroups groups of rows, and kWays warps that share a group's positions.
+template <int D, int kGroups_>
+struct Shape {
+    static constexpr int kGroups = kGroups_, kWays = kWarps / kGroups;
+    static constexpr int kRows = D == 256 ? 4 : 8;                   // of a lane; a warp has two times as many
+    static constexpr int kBlock = 2 * kRows * kGroups;
+    static constexpr int kTile = D == 256 ? 32 : 64, kPos = kTile / kWays, kEach = kPos / 16;  // of a warp; of a lane
+    static constexpr int kStages = D == 64 ? 4 : 2;
+    static constexpr int kPanels = D / 32, kPitch = 2 * kRows + 4;    // floats from position to position of the weights
+    static constexpr uint32_t kPanel = kTile * 128, kTileBytes = kPanels * kPanel;
+    using C = Cut<kBlock, kTile, 1>;
+    using Deal = Dealer<C, kThreads>;
+    static constexpr int kShared = 1024 + 2 * kStages * kTileBytes + 4 * (kBlock * D + kWarps * kPos * kPitch);
+    static_assert(kEach >= 1 && kPos % 16 == 0 && kPos <= 32);
+};
+
+struct F32Params {
+    TreeParams t;
+    CUtensorMap keys, values;
+    int box;  // groups of a box, which lie in one page
+};
+
+template <typename S>
+struct Control {
+    unsigned long long full[S::kStages], empty[S::kStages];
+    unsigned missing[S::kStages];  // groups of a tile whose page is missing
+    int failed, more;
+    typename S::Deal deal;
+    Piece piece;
     Nodes nodes;
+    int depth[S::kBlock], node[S::kBlock];
+    float slope[S::kBlock], most[S::kBlock], sum[S::kBlock];
     long long sums[kThreads / 32], found[2];
 };
 
-// fp32 arithmetic on the FMA units, tiles of 32 positions against blocks of 16 rows in shared memory.
-template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) tree_kernel(const __grid_constant__ TreeParams p) {
-    constexpr int kQuads = D / 4, kGroups = kThreads / kQuads, kEach = kRows / kGroups;  // rows whose values a thread adds up
-    extern __shared__ __align__(16) char dynamic[];
-    Shared<D>& sh = *reinterpret_cast<Shared<D>*>(dynamic);
-    const int d = p.a.head_dim;
-    after_previous();
-    let_next_start();
-    Dealer<C, kThreads> deal;
-    const bool work = deal.start(p, blockIdx.x, gridDim.x, sh.sums, sh.found);
-    int tree = -1;
+__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 read4(uint32_t at) {
+    float4 x;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(at) : "memory");
+    return x;
+}
+
+// A barrier of the warps that compute, true if x is in one of their threads.
+__device__ __forceinline__ bool any_of(bool x) {
+    uint32_t any;
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.or.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(any) : "r"(static_cast<uint32_t>(x)), "n"(kWorkThreads) : "memory");
+    return any != 0;
+}
+
+template <typename S, int D>
+__device__ void copy_role(const F32Params& f, typename S::Deal deal, Control<S>& c, uint32_t ring) {
+    constexpr int kTileGroups = S::kTile / kGroup;
+    const TreeParams& p = f.t;
+    const int lane = threadIdx.x & 31, panel = lane % S::kPanels, group = lane / S::kPanels * f.box;
+    const bool mine = group < kTileGroups && 32 * panel < p.a.head_dim;
+    const uint32_t box_bytes = f.box * kGroup * 128;
+    uint32_t copies = 0;
     Piece s;
-    Note cut = {};
-    while (work && deal.take(p, s)) {
-        if (s.tree != tree) fill_nodes<kThreads>(p, s.span, sh.nodes, threadIdx.x, [](bool x) { return __syncthreads_or(x); });
+    while (deal.take(p, s)) {
+        const int* table = p.pages.table + static_cast<size_t>(s.span.row) * p.pages.row_pages;
+        for (int tile = s.span.first_tile + s.from; tile < s.span.first_tile + s.to; ++tile, ++copies) {
+            const int g = tile * kTileGroups + group, page = mine && g * kGroup < s.span.len ? table[g / p.page_groups] : -1;
+            const bool real = page >= 0 && page < p.pages.n_pages;
+            const unsigned boxes = __ballot_sync(kAll, real);
+            unsigned missing = 0;  // groups, from the boxes of the first panel
+            for (int k = 0; k < kTileGroups; ++k)
+                if (!(boxes >> (k / f.box * S::kPanels) & 1u)) missing |= 1u << k;
+            const uint32_t stage = copies % S::kStages, bar = shared_address(&c.full[stage]), to = ring + 2 * stage * S::kTileBytes + panel * S::kPanel + group * (kGroup * 128);
+            if (!__all_sync(kAll, barrier_wait(shared_address(&c.empty[stage]), (copies / S::kStages & 1) ^ 1, &c.failed))) {
+                int late = 0;  // what is under way arrives first
+                for (uint32_t k = copies < S::kStages ? 0 : copies - S::kStages; k < copies; ++k)
+                    barrier_wait(shared_address(&c.full[k % S::kStages]), k / S::kStages & 1, &late);
+                return;
+            }
+            if (lane == 0) {
+                *static_cast<volatile unsigned*>(&c.missing[stage]) = missing;
+                barrier_arrive_bytes(bar, 2 * __popc(boxes) * box_bytes);
+            }
+            __syncwarp();
+            if (real) {
+                copy_box(to, &f.keys, 32 * panel, g % p.page_groups * kGroup, s.head, page, bar);
+                copy_box(to + S::kTileBytes, &f.values, 32 * panel, g % p.page_groups * kGroup, s.head, page, bar);
+            }
+            __syncwarp();
+        }
+    }
+}
+
+// kExtra: a cap or a bias on the scores.
+template <typename S, int D, bool kExtra>
+__device__ void work_role(const TreeParams& p, Control<S>& c, uint32_t ring, float* queries, float* all_weights) {
+    constexpr int kRows = S::kRows, kEach = S::kEach, kPos = S::kPos, kPairs = D / 32;  // pairs of columns of a lane
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = warp % S::kGroups, way = warp / S::kGroups, d = p.a.head_dim;
+    const int half = lane >> 4, place = lane & 15, row0 = group * (2 * kRows) + half * kRows;  // the lane's first row
+    float* weights = all_weights + warp * (kPos * S::kPitch);
+    const uint32_t query_at = shared_address(queries) + row0 * (D * 4), weights_at = shared_address(weights) + half * kRows * 4;
+    const Piece& s = c.piece;
+    uint32_t tiles = 0;
+    int tree = -1;
+    bool ok = true;  // a wait that gives up leaves the loops as they are: other warps may wait for this one
+    for (;;) {
+        any_of(false);  // nobody reads the last piece, its queries and its parts any more
+        if (threadIdx.x == 0) c.more = c.deal.take(p, c.piece);
+        any_of(false);
+        if (c.more == 0) break;
+        if (s.tree != tree) fill_nodes<kWorkThreads>(p, s.span, c.nodes, threadIdx.x, any_of);
         tree = s.tree;
         const int rows = s.span.nodes * p.a.group;
-        __syncthreads();
-        for (int u = threadIdx.x; u < kRows * kQuads; u += kThreads) {
-            const int r = u / kQuads, e = u % kQuads * 4, all = s.block * kRows + r, node = all / p.a.group, h = all - node * p.a.group;
+        const bool whole = s.from == 0 && s.to == s.span.tiles;
+        if (threadIdx.x == 0 && s.from == 0 && !whole) take_note(p, {s.span.first, s.head, s.block, c.deal.last_of(s), rows, {}});
+        for (int u = threadIdx.x; u < S::kBlock * (D / 4); u += kWorkThreads) {
+            const int r = u / (D / 4), e = u % (D / 4) * 4, all = s.block * S::kBlock + r, node = all / p.a.group, h = all - node * p.a.group;
             float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             if (all < rows && e < d)
-                x = load4(reinterpret_cast<const T*>(p.a.q) + (s.span.first + node) * p.a.q_row + (s.head * p.a.group + h) * p.a.q_head + e);
-            *reinterpret_cast<float4*>(&sh.q[r][e]) = x;
+                x = load4(reinterpret_cast<const float*>(p.a.q) + (s.span.first + node) * p.a.q_row + (s.head * p.a.group + h) * p.a.q_head + e);
+            *reinterpret_cast<float4*>(queries + r * D + e) = x;
         }
-        // scores: row threadIdx.x / 8, positions threadIdx.x % 8 + 8 i
-        const int r = threadIdx.x >> 3, c = threadIdx.x & 7, all = s.block * kRows + r;
-        const bool real = all < rows;
-        const int node = real ? all / p.a.group : 0, depth = real ? sh.nodes.depth[node] : -1;
-        const float slope = real && p.a.slopes != nullptr ? p.a.slopes[s.head * p.a.group + all - node * p.a.group] * kLog2e : 0.0f;
-        const int quad = threadIdx.x % kQuads * 4, group = threadIdx.x / kQuads;
-        float m = kLowest, l = 0.0f;
-        float4 acc[kEach];
+        if (threadIdx.x < S::kBlock) {
+            const int all = s.block * S::kBlock + threadIdx.x, node = all < rows ? all / p.a.group : 0;
+            c.node[threadIdx.x] = node;
+            c.depth[threadIdx.x] = all < rows ? c.nodes.depth[node] : -1;
+            c.slope[threadIdx.x] = kExtra && all < rows && p.a.slopes != nullptr ? p.a.slopes[s.head * p.a.group + all - node * p.a.group] * kLog2e : 0.0f;
+        }
+        any_of(false);
+        const bool idle = s.block * S::kBlock + group * 2 * kRows >= rows;
+        float m[kRows], l[kRows];
+        float2 acc[kRows][kPairs];
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) acc[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        const int* table = p.pages.table + static_cast<size_t>(s.span.row) * p.pages.row_pages;
-        for (int tile = s.span.first_tile + s.from; tile < s.span.first_tile + s.to; ++tile) {
-            const int t0 = tile * kTile;
-            __syncthreads();
-            for (int u = threadIdx.x; u < kTile * kQuads; u += kThreads) {
-                const int t = t0 + u / kQuads, e = u % kQuads * 4;
-                float4 k = make_float4(0.0f, 0.0f, 0.0f, 0.0f), v = k;
-                if (t >= s.span.lo && t < s.span.len && e < d) {
-                    const int page = table[t / p.pages.page_tokens];
-                    if (page >= 0 && page < p.pages.n_pages) {
-                        const uint64_t at = page * p.a.page_stride + s.head * p.a.head_stride + t % p.pages.page_tokens * p.a.token_stride + e;
-                        k = load4(reinterpret_cast<const T*>(p.a.k) + at);
-                        v = load4(reinterpret_cast<const T*>(p.a.v) + at);
+        for (int i = 0; i < kRows; ++i) {
+            m[i] = kLowest;
+            l[i] = 0.0f;
+#pragma unroll
+            for (int q = 0; q < kPairs; ++q) acc[i][q] = make_float2(0.0f, 0.0f);
+        }
+        for (int tile = s.span.first_tile + s.from; tile < s.span.first_tile + s.to; ++tile, ++tiles) {
+            const uint32_t stage = tiles % S::kStages, keys = ring + 2 * stage * S::kTileBytes, values = keys + S::kTileBytes;
+            const int t0 = tile * S::kTile + way * kPos;
+            ok = barrier_wait(shared_address(&c.full[stage]), tiles / S::kStages & 1, &c.failed) && ok;
+            __syncwarp();
+            if (!idle) {
+                const unsigned missing = *static_cast<volatile unsigned*>(&c.missing[stage]) >> (way * kPos / kGroup);
+                const bool edge = missing != 0 || t0 + kPos > s.span.base || (p.a.window > 0 && t0 < static_cast<long long>(s.span.base) + kMaxNodes - p.a.window);
+                // scores of the lane's rows at positions place and place + 16 of the warp's
+                float2 x[kRows][kEach];
+#pragma unroll
+                for (int i = 0; i < kRows; ++i)
+#pragma unroll
+                    for (int j = 0; j < kEach; ++j) x[i][j] = make_float2(0.0f, 0.0f);
+                const uint32_t key_at = keys + (way * kPos + place) * 128;
+#pragma unroll 1
+                for (int panel = 0; 32 * panel < d; ++panel) {
+#pragma unroll
+                    for (int piece = 0; piece < 8; ++piece) {  // beyond the head's end copies put zeros
+                        const uint32_t at = key_at + panel * S::kPanel + ((piece ^ (place & 7)) << 4);
+                        float4 k[kEach];
+#pragma unroll
+                        for (int j = 0; j < kEach; ++j) k[j] = read4(at + j * (16 * 128));
+#pragma unroll
+                        for (int i = 0; i < kRows; ++i) {
+                            const float4 q = read4(query_at + i * (D * 4) + panel * 128 + piece * 16);
+#pragma unroll
+                            for (int j = 0; j < kEach; ++j) {
+                                x[i][j] = __ffma2_rn(make_float2(q.x, q.y), make_float2(k[j].x, k[j].y), x[i][j]);
+                                x[i][j] = __ffma2_rn(make_float2(q.z, q.w), make_float2(k[j].z, k[j].w), x[i][j]);
+                            }
+                        }
                     }
                 }
-                *reinterpret_cast<float4*>(&sh.k[u / kQuads][e]) = k;
-                *reinterpret_cast<float4*>(&sh.v[u / kQuads][e]) = v;
-            }
-            unsigned seen = seen_of(p, s.span, sh.nodes, node, depth, t0);
+                unsigned seen[kRows];
+                if (edge) {
+                    const int mine = row0 + (lane & (kRows - 1));
+                    unsigned bits = seen_of(p, s.span, c.nodes, c.node[mine], c.depth[mine], t0);
+                    if (missing & 1u) bits &= 0xFFFF0000u;
+                    if (missing & 2u) bits &= 0x0000FFFFu;
+                    __syncwarp();
 #pragma unroll
-            for (int g = 0; g < kTile; g += kGroup) {  // a missing page is not seen
-                const int page = t0 + g < s.span.len ? table[(t0 + g) / p.pages.page_tokens] : -1;
-                if (page < 0 || page >= p.pages.n_pages) seen &= ~(0xFFFFu << g);
-            }
-            if (c == 0) sh.seen[r] = seen;
-            __syncthreads();
-            float x[kTile / 8] = {};
-            for (int e = 0; e < D; e += 4) {
-                const float4 q = *reinterpret_cast<const float4*>(&sh.q[r][e]);
+                    for (int i = 0; i < kRows; ++i) seen[i] = __shfl_sync(kAll, bits, (lane & 16) + i);
+                }
+                bool rises = false;
 #pragma unroll
-                for (int i = 0; i < kTile / 8; ++i) {
-                    const float4 k = *reinterpret_cast<const float4*>(&sh.k[c + 8 * i][e]);
-                    x[i] = fmaf(q.x, k.x, fmaf(q.y, k.y, fmaf(q.z, k.z, fmaf(q.w, k.w, x[i]))));
+                for (int i = 0; i < kRows; ++i) {
+#pragma unroll
+                    for (int j = 0; j < kEach; ++j) {
+                        const int at = place + 16 * j;
+                        float y = x[i][j].x + x[i][j].y;
+                        const bool sees = !edge || (seen[i] >> at & 1u);
+                        if constexpr (kExtra) {
+                            const int t = t0 + at, depth = c.depth[row0 + i];
+                            int back = t - s.span.base - depth;
+                            if (t >= s.span.base && sees) back = c.nodes.depth[t - s.span.base] - depth;
+                            y = score<true>(p, y, c.slope[row0 + i], back);
+                        } else {
+                            y *= p.a.scale * kLog2e;
+                        }
+                        y = sees ? y : -INFINITY;
+                        rises = rises || (y > m[i] && (m[i] == kLowest || y - m[i] > kSlack));
+                        x[i][j].x = y;
+                    }
+                }
+                if (__any_sync(kAll, rises)) {
+#pragma unroll
+                    for (int i = 0; i < kRows; ++i) {
+                        float top = m[i];
+#pragma unroll
+                        for (int j = 0; j < kEach; ++j) top = fmaxf(top, x[i][j].x);
+#pragma unroll
+                        for (int u = 1; u < 16; u *= 2) top = fmaxf(top, __shfl_xor_sync(kAll, top, u));
+                        const float k = exp2_approx(m[i] - top);
+                        m[i] = top;
+                        l[i] *= k;
+#pragma unroll
+                        for (int q = 0; q < kPairs; ++q) acc[i][q] = __fmul2_rn(acc[i][q], make_float2(k, k));
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < kEach; ++j) {
+                    float w[kRows];
+#pragma unroll
+                    for (int i = 0; i < kRows; ++i) {
+                        w[i] = exp2_approx(x[i][j].x - m[i]);
+                        l[i] += w[i];
+                    }
+#pragma unroll
+                    for (int i = 0; i < kRows; i += 4)
+                        *reinterpret_cast<float4*>(weights + (place + 16 * j) * S::kPitch + half * kRows + i) = make_float4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+                }
+                __syncwarp();
+                // columns 4 place .. + 3 of every 64
+                const uint32_t value_at = values + (place >> 3) * S::kPanel + way * kPos * 128;
+                const auto add = [&](int u, auto sees) {
+                    float w[kRows];
+#pragma unroll
+                    for (int i = 0; i < kRows; i += 4) {
+                        const float4 y = read4(weights_at + u * (S::kPitch * 4) + i * 4);
+                        w[i] = y.x, w[i + 1] = y.y, w[i + 2] = y.z, w[i + 3] = y.w;
+                    }
+#pragma unroll
+                    for (int q = 0; q < kPairs; q += 2) {
+                        const float4 v = read4(value_at + q * S::kPanel + u * 128 + (((place & 7) ^ (u & 7)) << 4));
+#pragma unroll
+                        for (int i = 0; i < kRows; ++i) {
+                            if (!sees(i)) continue;
+                            acc[i][q] = __ffma2_rn(make_float2(w[i], w[i]), make_float2(v.x, v.y), acc[i][q]);
+                            acc[i][q + 1] = __ffma2_rn(make_float2(w[i], w[i]), make_float2(v.z, v.w), acc[i][q + 1]);
+                        }
+                    }
+                };
+                if (edge) {  // a value that is not seen must not reach the sum, whatever it holds
+#pragma unroll 1
+                    for (int u = 0; u < kPos; ++u) add(u, [&](int i) { return (seen[i] >> u & 1u) != 0; });
+                } else {
+#pragma unroll 4
+                    for (int u = 0; u < kPos; ++u) add(u, [](int) { return true; });
+                }
+                __syncwarp();
+            }
+            if (lane == 0) barrier_arrive(shared_address(&c.empty[stage]));
+        }
+#pragma unroll
+        for (int i = 0; i < kRows; ++i)
+#pragma unroll
+            for (int u = 1; u < 16; u *= 2) l[i] += __shfl_xor_sync(kAll, l[i], u);
+        // the ways' parts one after the other, through the queries' place
+        for (int w = 1; w < S::kWays; ++w) {
+            any_of(false);
+            if (way == w && !idle) {
+#pragma unroll
+                for (int i = 0; i < kRows; ++i) {
+                    if (place == 0) {
+                        c.most[row0 + i] = m[i];
+                        c.sum[row0 + i] = l[i];
+                    }
+#pragma unroll
+                    for (int q = 0; q < kPairs; q += 2)
+                        *reinterpret_cast<float4*>(queries + (row0 + i) * D + 32 * q + 4 * place) = make_float4(acc[i][q].x, acc[i][q].y, acc[i][q + 1].x, acc[i][q + 1].y);
                 }
             }
-            float high = kLowest;
+            any_of(false);
+            if (way == 0 && !idle) {
 #pragma unroll
-            for (int i = 0; i < kTile / 8; ++i) {
-                const int t = t0 + c + 8 * i;
-                const bool sees = seen >> (c + 8 * i) & 1u;
-                const int where = t < s.span.base || !sees ? t : s.span.base + sh.nodes.depth[t - s.span.base];
-                x[i] = sees ? score<true>(p, x[i], slope, where - s.span.base - depth) : -INFINITY;
-                high = fmaxf(high, x[i]);
-            }
+                for (int i = 0; i < kRows; ++i) {
+                    const float other = c.most[row0 + i], top = fmaxf(m[i], other), k = exp2_approx(m[i] - top), by = exp2_approx(other - top);
+                    m[i] = top;
+                    l[i] = fmaf(c.sum[row0 + i], by, l[i] * k);
 #pragma unroll
-            for (int u = 1; u < 8; u *= 2) high = fmaxf(high, __shfl_xor_sync(0xFFFFFFFFu, high, u));
-            const float top = fmaxf(m, high), f = exp2_approx(m - top);
-            float sum = 0.0f;
-#pragma unroll
-            for (int i = 0; i < kTile / 8; ++i) {
-                x[i] = exp2_approx(x[i] - top);
-                sum += x[i];
-                sh.w[c + 8 * i][r] = x[i];
-            }
-#pragma unroll
-            for (int u = 1; u < 8; u *= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, u);
-            l = fmaf(l, f, sum);
-            m = top;
-            if (c == 0) sh.factor[r] = f;
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                const float k = sh.factor[group * kEach + i];
-                acc[i] = make_float4(acc[i].x * k, acc[i].y * k, acc[i].z * k, acc[i].w * k);
-            }
-            for (int u = 0; u < kTile; ++u) {
-                const float4 v = *reinterpret_cast<const float4*>(&sh.v[u][quad]);
-#pragma unroll
-                for (int i = 0; i < kEach; ++i) {
-                    // a value that is not seen must not reach the sum, whatever it holds
-                    if (!(sh.seen[group * kEach + i] >> u & 1u)) continue;
-                    const float w = sh.w[u][group * kEach + i];
-                    acc[i] = make_float4(fmaf(w, v.x, acc[i].x), fmaf(w, v.y, acc[i].y), fmaf(w, v.z, acc[i].z), fmaf(w, v.w, acc[i].w));
+                    for (int q = 0; q < kPairs; q += 2) {
+                        const float4 o = load4(queries + (row0 + i) * D + 32 * q + 4 * place);
+                        acc[i][q] = make_float2(fmaf(o.x, by, acc[i][q].x * k), fmaf(o.y, by, acc[i][q].y * k));
+                        acc[i][q + 1] = make_float2(fmaf(o.z, by, acc[i][q + 1].x * k), fmaf(o.w, by, acc[i][q + 1].y * k));
+                    }
                 }
             }
         }
-        const bool whole = s.from == 0 && s.to == s.span.tiles;
-        float* slot = slot_of<C, D>(p, gridDim.x, blockIdx.x, s.from == 0);
-        if (s.from == 0 && !whole) cut = {s.span.first, s.head, s.block, deal.last_of(s), s.span.nodes * p.a.group, {}};
-        __syncthreads();
-        if (c == 0) {
-            sh.factor[r] = l > 0.0f ? 1.0f / l : 0.0f;
-            if (!whole) {
-                slot[kRows * D + r] = m;
-                slot[kRows * D + kRows + r] = l;
-            }
-        }
-        __syncthreads();
+        if (way != 0 || idle) continue;
+        float* slot = slot_of<typename S::C, D>(p, gridDim.x, blockIdx.x, s.from == 0);
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int row = group * kEach + i, all_i = s.block * kRows + row;
-            if (!whole) {
-                *reinterpret_cast<float4*>(slot + row * D + quad) = acc[i];
-            } else if (all_i < rows && quad < d) {
-                const float k = sh.factor[row];
-                const int n = all_i / p.a.group, h = all_i - n * p.a.group;
-                T* out = reinterpret_cast<T*>(p.a.out) + (s.span.first + n) * p.a.out_row + (s.head * p.a.group + h) * p.a.out_head + quad;
-                store_out(out, acc[i].x * k);
-                store_out(out + 1, acc[i].y * k);
-                store_out(out + 2, acc[i].z * k);
-                store_out(out + 3, acc[i].w * k);
+        for (int i = 0; i < kRows; ++i) {
+            const int row = row0 + i, all = s.block * S::kBlock + row, node = c.node[row], h = all - node * p.a.group;
+            if (all >= rows) continue;
+            const bool none = c.depth[row] < 0;  // its chain of parents is not valid
+            const float k = !ok ? NAN : whole ? (l[i] > 0.0f ? 1.0f / l[i] : 0.0f) : 1.0f;
+            float* to = whole ? reinterpret_cast<float*>(p.a.out) + (s.span.first + node) * p.a.out_row + (s.head * p.a.group + h) * p.a.out_head : slot + row * D;
+            if (!whole && place == 0) {
+                slot[S::kBlock * D + row] = none ? kLowest : m[i];
+                slot[S::kBlock * D + S::kBlock + row] = none ? 0.0f : l[i];
+            }
+#pragma unroll
+            for (int q = 0; q < kPairs; q += 2) {
+                const int e = 32 * q + 4 * place;
+                if (e >= d) continue;
+                *reinterpret_cast<float4*>(to + e) = none ? make_float4(0.0f, 0.0f, 0.0f, 0.0f)
+                                                          : make_float4(acc[i][q].x * k, acc[i][q].y * k, acc[i][q + 1].x * k, acc[i][q + 1].y * k);
             }
         }
     }
-    if (threadIdx.x == 0) take_note(p, cut);
-    write_zeros<T, C, kThreads>(p);
 }
 
-// SMs of a device and CTAs of a kernel on one, asked for once.
+template <int D, int kGroups, bool kExtra>
+__global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant__ F32Params f) {
+    using S = Shape<D, kGroups>;
+    const TreeParams& p = f.t;
+    extern __shared__ char dynamic[];
+    __shared__ Control<S> c;
+    const int warp = same(static_cast<int>(threadIdx.x) >> 5);
+    const uint32_t ring = (shared_address(dynamic) + 1023) & ~1023u;
+    float* queries = reinterpret_cast<float*>(dynamic + (ring - shared_address(dynamic)) + 2 * S::kStages * S::kTileBytes);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S::kStages; ++i) {
+            barrier_init(shared_address(&c.full[i]), 1);
+            barrier_init(shared_address(&c.empty[i]), kWarps);
+        }
+        c.failed = 0;
+        barriers_initialized();
+    }
+    __syncthreads();
+    after_previous();
+    let_next_start();
+    typename S::Deal deal;
+    const bool work = deal.start(p, blockIdx.x, gridDim.x, c.sums, c.found);
+    if (threadIdx.x == 0) {
+        take_note(p, {});
+        c.deal = deal;
+    }
+    if (work) {
+        if (warp == kWarps) copy_role<S, D>(f, deal, c, ring);
+        else work_role<S, D, kExtra>(p, c, ring, queries, queries + S::kBlock * D);
+    }
+    __syncthreads();
+    write_zeros<float, typename S::C, kThreads>(p);
+}
+
+// SMs of a device, asked for once, and the kernel's share of shared memory set.
 constexpr int kDevices = 64;
 template <auto kKernel>
-cudaError_t resident(int threads, int shared, int& ctas) {
+cudaError_t resident(int shared, int& ctas) {
     static std::atomic<int> known[kDevices];
-    int device = 0, sms = 0, each = 0;
+    int device = 0, sms = 0;
     cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return e;
     ctas = device < kDevices ? known[device].load(std::memory_order_relaxed) : 0;
     if (ctas > 0) return cudaSuccess;
-    if (shared > 48 * 1024) e = cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
+    e = cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, kKernel, threads, shared);
     if (e != cudaSuccess) return e;
-    ctas = sms * each < kMaxCtas ? sms * each : kMaxCtas;
-    if (ctas < 1) return cudaErrorInvalidConfiguration;
+    ctas = sms < kCtas ? sms : kCtas;
     if (device < kDevices) known[device].store(ctas, std::memory_order_relaxed);
     return cudaSuccess;
 }
 
-template <typename T, int D>
-cudaError_t launch_d(const TreeParams& p, cudaStream_t s) {
-    constexpr int shared = sizeof(Shared<D>);
+template <int D, int kGroups, bool kExtra>
+cudaError_t launch_extra(const TreeParams& p, cudaStream_t s) {
+    using S = Shape<D, kGroups>;
     int ctas = 0;
-    cudaError_t e = resident<tree_kernel<T, D>>(kThreads, shared, ctas);
+    cudaError_t e = resident<tree_kernel<D, kGroups, kExtra>>(S::kShared, ctas);
     if (e != cudaSuccess) return e;
-    e = launch(tree_kernel<T, D>, ctas, kThreads, shared, 0, s, p);
-    return e != cudaSuccess || ctas == 1 ? e : launch_join<T, D, C>(p, ctas, s);
+    F32Params f;
+    f.t = p;
+    f.box = std::gcd(p.page_groups, S::kTile / kGroup);
+    Encode encode = nullptr;
+    e = encoder(encode);
+    if (e == cudaSuccess) e = describe_pool(encode, f.keys, p, p.a.k, f.box, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4);
+    if (e == cudaSuccess) e = describe_pool(encode, f.values, p, p.a.v, f.box, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4);
+    if (e == cudaSuccess) e = launch(tree_kernel<D, kGroups, kExtra>, ctas, kThreads, S::kShared, 0, s, f);
+    return e != cudaSuccess || ctas == 1 ? e : launch_join<float, D, typename S::C>(p, ctas, s);
 }
 
-template <typename T>
-cudaError_t launch_t(const TreeParams& p, cudaStream_t s) {
-    return p.a.head_dim <= 64 ? launch_d<T, 64>(p, s) : p.a.head_dim <= 128 ? launch_d<T, 128>(p, s) : launch_d<T, 256>(p, s);
+template <int D, int kGroups>
+cudaError_t launch_groups(const TreeParams& p, cudaStream_t s) {
+    return p.a.slopes != nullptr || p.a.softcap > 0.0f ? launch_extra<D, kGroups, true>(p, s) : launch_extra<D, kGroups, false>(p, s);
 }
+
+template <int D>
+cudaError_t launch_d(const TreeParams& p, cudaStream_t s) {
+    if constexpr (D <= 128)
+        if (static_cast<long long>(p.trees.n_nodes) * p.a.group <= 32ll * p.trees.n) return launch_groups<D, 2>(p, s);
+    return launch_groups<D, 4>(p, s);
+}
+
+template <int D, int kGroups>
+constexpr size_t floats_of() { return workspace_floats(kCtas, Shape<D, kGroups>::kBlock, D); }
 
 }  // namespace
 
 uint64_t tree_workspace(int bf16, int head_dim) {
     if (bf16) return tree_workspace_bf16(head_dim);
-    return sizeof(float) * workspace_floats(kMaxCtas, kRows, head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256);
+    return sizeof(float) * (head_dim <= 64 ? floats_of<64, 4>() : head_dim <= 128 ? floats_of<128, 4>() : floats_of<256, 4>());
 }
 
 cudaError_t launch_tree(const Pages& pages, const Trees& trees, const TreeAttend& a, cudaStream_t s) {
     const float cap = a.softcap > 0.0f ? a.softcap : 1.0f;
     const TreeParams p = {pages, trees, a, pages.page_tokens / kGroup, a.scale / cap, cap * kLog2e};
-    return a.bf16 ? launch_tree_bf16(p, s) : launch_t<float>(p, s);
+    if (a.bf16) return launch_tree_bf16(p, s);
+    return a.head_dim <= 64 ? launch_d<64>(p, s) : a.head_dim <= 128 ? launch_d<128>(p, s) : launch_d<256>(p, s);
 }
 
 }  // namespace jb

@@ -13,13 +13,13 @@
 #include "jb_draft.h"
 #include "jb_launch.cuh"
 #include "jb_scores.cuh"
+#include "jb_tensor_map.h"
 
 namespace jb {
 namespace {
 
 constexpr int kGroup = 16;          // pages hold a multiple of so many tokens
 constexpr int kMaskWords = kMaxNodes / 32;
-constexpr int kMaxCtas = 640;       // of the persistent grids; the workspace has two slots for each
 
 }  // namespace
 
@@ -363,6 +363,23 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
         store_out(out + 2, o.z * inverse);
         store_out(out + 3, o.w * inverse);
     }
+}
+
+// Four dimensions, boxes with 128 bytes of the first one, their 16-byte pieces swizzled.
+inline bool encoded(Encode encode, CUtensorMap& map, const void* from, CUtensorMapDataType type, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* boxes) {
+    const cuuint32_t steps[4] = {1, 1, 1, 1};
+    return encode(&map, type, 4, const_cast<void*>(from), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// A layer's keys or values, [pages][heads][tokens][elements], in boxes of `box` groups of tokens.
+inline cudaError_t describe_pool(Encode encode, CUtensorMap& map, const TreeParams& p, const char* pool, int box, CUtensorMapDataType type, int bytes) {
+    const cuuint64_t page = static_cast<cuuint64_t>(p.a.heads) * p.a.head_dim * p.pages.page_tokens;
+    const cuuint64_t dims[4] = {static_cast<cuuint64_t>(p.a.head_dim), static_cast<cuuint64_t>(p.pages.page_tokens), static_cast<cuuint64_t>(p.a.heads),
+                                static_cast<cuuint64_t>(p.pages.n_pages)};
+    const cuuint64_t strides[3] = {p.a.token_stride * bytes, p.a.head_stride * bytes, (p.pages.n_pages > 1 ? p.a.page_stride : page) * bytes};
+    const cuuint32_t boxes[4] = {static_cast<cuuint32_t>(128 / bytes), static_cast<cuuint32_t>(box * kGroup), 1, 1};
+    return encoded(encode, map, pool, type, dims, strides, boxes) ? cudaSuccess : cudaErrorInvalidValue;
 }
 
 template <typename T, int D, typename C>

@@ -21,7 +21,6 @@
 #include <cuda_bf16.h>
 
 #include "jb_tcgen05.cuh"
-#include "jb_tensor_map.h"
 #include "jb_tree.cuh"
 
 namespace jb {
@@ -718,21 +717,6 @@ cudaError_t resident(int shared, int each, int most, int& ctas) {
 template <int D, int kGroups>
 constexpr int max_ctas() { return 160 * Shape<D, kGroups>::kCtas; }
 
-bool encoded(Encode encode, CUtensorMap& map, const void* from, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* boxes) {
-    const cuuint32_t steps[4] = {1, 1, 1, 1};
-    return encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(from), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-cudaError_t describe(Encode encode, CUtensorMap& map, const TreeParams& p, const char* pool, int box) {
-    const cuuint64_t page = static_cast<cuuint64_t>(p.a.heads) * p.a.head_dim * p.pages.page_tokens;
-    const cuuint64_t dims[4] = {static_cast<cuuint64_t>(p.a.head_dim), static_cast<cuuint64_t>(p.pages.page_tokens), static_cast<cuuint64_t>(p.a.heads),
-                                static_cast<cuuint64_t>(p.pages.n_pages)};
-    const cuuint64_t strides[3] = {p.a.token_stride * sizeof(T), p.a.head_stride * sizeof(T), (p.pages.n_pages > 1 ? p.a.page_stride : page) * sizeof(T)};
-    const cuuint32_t boxes[4] = {64, static_cast<cuuint32_t>(box * kGroup), 1, 1};
-    return encoded(encode, map, pool, dims, strides, boxes) ? cudaSuccess : cudaErrorInvalidValue;
-}
-
 // Queries in blocks of whole nodes: false where a block is none, or strides are none of a box.
 bool describe_queries(Encode encode, CUtensorMap& map, const TreeParams& p) {
     if (kRows % p.a.group != 0) return false;
@@ -740,7 +724,7 @@ bool describe_queries(Encode encode, CUtensorMap& map, const TreeParams& p) {
                                 static_cast<cuuint64_t>(p.trees.n_nodes)};
     const cuuint64_t strides[3] = {p.a.q_head * sizeof(T), p.a.q_head * p.a.group * sizeof(T), p.a.q_row * sizeof(T)};
     const cuuint32_t boxes[4] = {64, static_cast<cuuint32_t>(p.a.group), 1, static_cast<cuuint32_t>(kRows / p.a.group)};
-    return encoded(encode, map, p.a.q, dims, strides, boxes);
+    return encoded(encode, map, p.a.q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, dims, strides, boxes);
 }
 
 template <int D, int kGroups, Scores kScores>
@@ -754,8 +738,8 @@ cudaError_t launch_scores(const TreeParams& p, cudaStream_t s) {
     tc.box = std::gcd(p.page_groups, kTile / kGroup);
     Encode encode = nullptr;
     e = encoder(encode);
-    if (e == cudaSuccess) e = describe(encode, tc.keys, p, p.a.k, tc.box);
-    if (e == cudaSuccess) e = describe(encode, tc.values, p, p.a.v, tc.box);
+    if (e == cudaSuccess) e = describe_pool(encode, tc.keys, p, p.a.k, tc.box, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, sizeof(T));
+    if (e == cudaSuccess) e = describe_pool(encode, tc.values, p, p.a.v, tc.box, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, sizeof(T));
     if (e == cudaSuccess) tc.query_box = describe_queries(encode, tc.queries, p);
     if (e == cudaSuccess) e = launch(tree_bf16_kernel<D, kGroups, kScores>, ctas, S::kThreads, S::kShared, 0, s, tc);
     return e != cudaSuccess || ctas == 1 ? e : launch_join<T, D, typename S::C>(p, ctas, s);
