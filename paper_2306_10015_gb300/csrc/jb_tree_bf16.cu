@@ -1,19 +1,28 @@
 // jb_tree_bf16.cu -- jb_attend_tree on the tensor cores, for bf16 caches.
 //
-// A block of 128 rows (node, query head of the key head) is one tile of tcgen05.mma, and its row's keys and values pass by
+// A group of 128 rows (node, query head of the key head) is one tile of tcgen05.mma, and its row's keys and values pass by
 // it once, 64 positions at a time:
 //   S = Q K^T (fp32, tensor memory), P = exp(S - m), O = O + P V (fp32, tensor memory)
 // with the maximum m of the softmax kept as it was until a row exceeds it by 2^8; only then is O multiplied. Weights enter
 // the second product as two bf16 numbers, 16 bits of them.
 //
-// Roles of a CTA, two on an SM (one with heads of more than 128): a warp copies keys and values (TMA, boxes of a page's
-// tokens, any page size and layout) into swizzled tiles; two warps copy queries and look after values that some rows do not
-// see; a warp issues the products; four warps, a thread a row, take scores from tensor memory and put weights in their place.
-// The two CTAs' waits fill one another.
+// A block is one group, with two CTAs on an SM (one with heads of more than 128), or, for large trees, two groups in a CTA with
+// an SM to itself, which share the tiles of keys and values and twice as many of them ahead. Roles: a warp copies keys and values
+// (TMA, boxes of a page's tokens, any page size and layout) into swizzled tiles, and queries where a group is whole nodes; one
+// or two warps look after values that some rows do not see, and copy queries otherwise; a warp for each group issues its
+// products; four warps for each group, a thread a row, take scores from tensor memory and put weights in their place.
+//
+// What bounds it. Large trees: the softmax's warps, two on a scheduler. Three rows of 58000 tokens, 64 nodes by 8 query heads,
+// 8 key heads of 128, capped: 554 us, issue slots 55 % used, packed fp32 units half, tensor pipes 45 % (one group a block:
+// 643 us; without the cap 1.8 times as many tiles a second). 16 chains of 255 behind 400 to 1800 tokens, 40 heads of 128: 201 us,
+// 24 % of the tensor pipes' rate; starts and ends of blocks, whose products wait for queries, are a fifth of it. Small trees: memory
+// latency. 24 rows of 65 to 2000 tokens, up to 33 nodes, 32 heads of 128: 74 us for 36 us of bytes; the tiles that fit beside
+// the queries are two ahead.
 //
 // Loops are kept short: a warp that runs alone through code that is longer than its instruction cache waits for
 // instructions (128 positions of a thread unrolled: 8000 cycles for as many positions). Nor is cp.async for keys and
-// values: a warp issued one in 170 cycles, 10000 for 128 positions.
+// values: a warp issued one in 170 cycles, 10000 for 128 positions. Eight warps for a group's softmax, two threads a row, were
+// no faster (757 and 741 us for the long rows): what they gain in waits they lose in registers and barriers.
 #include <algorithm>
 #include <atomic>
 #include <numeric>
@@ -391,7 +400,7 @@ template <typename S, int D, Scores kScores>
 __device__ void softmax_role(const TreeParams& p, Control& c, Work<typename S::Deal>& work, Nodes& nodes) {
     using C = typename S::C;
     // Whether a tile's scores stay in registers from one pass to the next. Where a cap is put on them between the passes that
-    // pays (729 -> 630 us for three rows of 58000 tokens), and without one a short loop that takes them from tensor memory
+    // pays (729 -> 636 us for three rows of 58000 tokens), and without one a short loop that takes them from tensor memory
     // twice does (78 us and not 84 for 24 ragged rows).
     constexpr bool kHeld = kScores == kCapped;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = warp / 4, row = threadIdx.x, d = p.a.head_dim;
@@ -753,6 +762,8 @@ cudaError_t launch_groups(const TreeParams& p, cudaStream_t s) {
 
 template <int D>
 cudaError_t launch_d(const TreeParams& p, cudaStream_t s) {
+    // Two groups where trees have more than one's rows on average. Measured with 16 rows of 400 to 1800 tokens, 40 heads of 128,
+    // one group and two in us: chains of 127 105 and 145, of 129 164 and 154, of 192 182 and 171, of 256 201 and 198.
     if constexpr (D <= 128)
         if (static_cast<long long>(p.trees.n_nodes) * p.a.group > static_cast<long long>(kRows) * p.trees.n) return launch_groups<D, 2>(p, s);
     return launch_groups<D, 1>(p, s);
