@@ -384,7 +384,7 @@ typedef struct {
  *   out = sum_t exp(x_t) v_t / sum_t exp(x_t)
  * A new token's query comes with the position that its key was written to; the tokens
  * of a prompt are queries of one row with consecutive positions, each of which reads the
- * row for itself: long prompts are slow. A query that sees
+ * row for itself: long prompts are slow (jb_attend_tree takes them 256 tokens at a time). A query that sees
  * nothing (position -1, or a row or position out of range) gets zeros; a position whose
  * page is missing is not seen, nor is one whose score is -inf. What a page holds past the
  * last position seen has no effect, NaN included. Results are bitwise repeatable.

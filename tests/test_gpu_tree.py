@@ -378,3 +378,64 @@ def test_scores_far_apart(dtype):
             page, slot = int(cache.pages.table[r, t // 16]), t % 16
             cache.keys[0][page, 0, slot] = (t if r == 0 else 1005 - t) / 64.0
     check(cache, 0, q, range(2), trees, scale=0.5)
+
+
+LARGE = [bush(200, 3, 2), chain(5), wide(129), bush(256, 1), chain(140), [-1]]   # more than 128 rows a tree on average
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("group,d,page,layout", [(1, 64, 16, "hnd"), (1, 128, 48, "nhd"), (3, 80, 32, "hnd"), (2, 128, 16, "hnd"), (1, 256, 16, "nhd")])
+def test_blocks_of_large_trees(dtype, group, d, page, layout):
+    """Blocks that are full, half empty and of one row, some of which have no rows for the second half of a block."""
+    cache, q = case(dtype, [150, 64, 1, 0, 333, 40], LARGE, 2, group, d, page, layout)
+    check(cache, 0, q, range(6), LARGE)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("window,softcap,bias", [(3, 0.0, False), (100, 20.0, False), (0, 3.0, False), (0, 0.0, True), (130, 5.0, True)])
+def test_large_trees_with_windows_caps_and_biases(dtype, window, softcap, bias):
+    cache, _ = case(dtype, [150, 64, 1, 0, 333, 40], LARGE, 2, 2, 64, 16)
+    q = query(sum(map(len, LARGE)), 4, 64, dtype, std=4.0)
+    slopes = 2.0 ** -torch.arange(1, 5, device="cuda").float() if bias else None
+    check(cache, 0, q, range(6), LARGE, window=window, softcap=softcap, slopes=slopes)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_trees_with_gaps(dtype):
+    """Missing pages, invalid chains and rows, and values that are not finite in nodes that few see."""
+    trees = [list(t) for t in LARGE]
+    trees[0][150], trees[4][77] = 151, -2
+    cache, q = case(dtype, [150, 64, 1, 0, 333, 40], trees, 2, 1, 128, 16)
+    cache.pages.table[0, 4] = -1
+    cache.pages.table[3, 9] = -1
+    cache.pages.table[4, 3:5] = -1
+    rows = [0, 1, 2, 3, 4, 9]
+    clean = check(cache, 0, q, rows, trees, out=torch.full_like(q, math.nan))
+    base, first = 64, len(trees[0])                     # the chain of five: its last node alone sees itself
+    cache.values[0][int(cache.pages.table[1, (base + 4) // 16]), :, (base + 4) % 16] = math.inf
+    got = jb.jb_attend_tree(cache, 0, q, draft(rows, trees))
+    same = [j for j in range(len(q)) if j != first + 4]
+    assert torch.equal(got[same], clean[same]) and not torch.isfinite(got[first + 4]).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("group", [1, 3, 8])
+def test_large_trees_queries_in_wider_rows(dtype, group):
+    """Queries of part of a row's heads, outputs likewise, several streams, one cache."""
+    trees = [bush(180), chain(130), bush(250, 2)]
+    cache, _ = case(dtype, [70, 200, 9], trees, 2, group, 128, 16)
+    n = sum(map(len, trees))
+    wide_q = query(n, 2 * group + 3, 128, dtype)
+    q = wide_q[:, 2:2 + 2 * group]
+    want = check(cache, 0, q.contiguous(), range(3), trees)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(4):
+        for s in streams:
+            with torch.cuda.stream(s):
+                out = torch.full((n, 2 * group + 1, 128), 7.0, dtype=q.dtype, device="cuda")
+                jb.jb_attend_tree(cache, 0, q, draft(range(3), trees), out=out[:, 1:])
+                got.append(out)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o[:, 1:], want) and (o[:, 0] == 7).all() for o in got)
