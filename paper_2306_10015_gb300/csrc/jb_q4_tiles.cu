@@ -169,7 +169,7 @@ struct Tiles {
 };
 
 struct TileControl {
-    unsigned long long full[4], empty[4], levels[4], levels_read[4], sums[4], sums_read[4], drained;
+    unsigned long long full[4], inputs[4], empty[4], levels[4], levels_read[4], sums[4], sums_read[4], drained;
     uint32_t tmem;
     int failed;
 };
@@ -197,6 +197,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tiles_kernel(const __grid_
     if (threadIdx.x == 0) {
         for (int i = 0; i < 4; ++i) {
             barrier_init(shared_address(&c.full[i]), 1);
+            barrier_init(shared_address(&c.inputs[i]), 1);
             barrier_init(shared_address(&c.empty[i]), kDecodeWarps + 1);
             barrier_init(shared_address(&c.levels[i]), kDecodeWarps / 2);
             barrier_init(shared_address(&c.levels_read[i]), 1);
@@ -211,7 +212,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tiles_kernel(const __grid_
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    after_previous();
+    // Only what the kernel before this one writes waits for its end: that one starts this one when all before itself are done.
     let_next_start();
     const uint32_t tmem = same(c.tmem);
     const Q4Matmul& m = p.m;
@@ -363,7 +364,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tiles_kernel(const __grid_
         bool ok = true;
         for (long long x = begin; ok && x < end; ++x, ++stage) {
             const uint32_t slot = stage % S::kStages;
-            ok = wait(&c.full[slot], stage / S::kStages & 1);
+            ok = wait(&c.inputs[slot], stage / S::kStages & 1);
             const int here = blocks_of(step);
             for (int first = 0; ok && first < here; first += 2, ++pair) {
                 const uint32_t buffer = pair % S::kBuffersA, sums = pair % S::kBuffersD;
@@ -400,25 +401,40 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tiles_kernel(const __grid_
             barrier_wait(shared_address(&c.drained), 0, &late);
         }
         __syncwarp();
-    } else {  // copies
+    } else {  // copies; codes of the first stages go ahead of the inputs, which another kernel may still be converting
+        const uint32_t all = static_cast<uint32_t>(end - begin);
+        const int from_step = static_cast<int>(begin % steps), from_tile = static_cast<int>(begin / steps);
+        uint32_t asked = 0;
+        int code_step = from_step, code_tile = from_tile;
+        const auto codes = [&] {
+            const uint32_t slot = asked++ % S::kStages, bar = shared_address(&c.full[slot]);
+            if (lane == 0) {
+                barrier_arrive_bytes(bar, S::kCodeBytes);
+                copy_box(stages + slot * S::kStageBytes, &p.codes, code_step * 128, code_tile * kRows, 0, 0, bar);
+            }
+            if (++code_step == steps) {
+                code_step = 0;
+                ++code_tile;
+            }
+        };
+        while (asked < all && asked < S::kStages) codes();
+        if (all > 0) after_previous();
+        int step = from_step;
         uint32_t stage = 0;
-        int step = static_cast<int>(begin % steps), tile = static_cast<int>(begin / steps);
-        for (long long x = begin; x < end; ++x, ++stage) {
-            const uint32_t slot = stage % S::kStages, to = stages + slot * S::kStageBytes, bar = shared_address(&c.full[slot]);
-            if (!wait(&c.empty[slot], (stage / S::kStages & 1) ^ 1)) {
-                int late = 0;  // what is under way arrives first
-                for (uint32_t k = stage < S::kStages ? 0 : stage - S::kStages; k < stage; ++k) barrier_wait(shared_address(&c.full[k % S::kStages]), k / S::kStages & 1, &late);
-                break;
-            }
+        for (; stage < all; ++stage) {
+            const uint32_t slot = stage % S::kStages, to = stages + slot * S::kStageBytes + S::kCodeBytes, bar = shared_address(&c.inputs[slot]);
+            if (!wait(&c.empty[slot], (stage / S::kStages & 1) ^ 1)) break;
+            if (asked == stage) codes();
             const int here = blocks_of(step);
-            if (lane == 0) barrier_arrive_bytes(bar, S::kCodeBytes + here * S::kInputBytes);
+            if (lane == 0) barrier_arrive_bytes(bar, here * S::kInputBytes);
             __syncwarp();
-            if (lane == 0) copy_box(to, &p.codes, step * 128, tile * kRows, 0, 0, bar);
-            else if (lane <= here) copy_box(to + S::kCodeBytes + (lane - 1) * S::kInputBytes, &p.inputs, (step * kStepBlocks + lane - 1) * 64, 0, 0, 0, bar);
-            if (++step == steps) {
-                step = 0;
-                ++tile;
-            }
+            if (lane < here) copy_box(to + lane * S::kInputBytes, &p.inputs, (step * kStepBlocks + lane) * 64, 0, 0, 0, bar);
+            if (++step == steps) step = 0;
+        }
+        if (stage < all) {  // what is under way arrives first
+            int late = 0;
+            for (uint32_t k = asked < S::kStages ? 0 : asked - S::kStages; k < asked; ++k) barrier_wait(shared_address(&c.full[k % S::kStages]), k / S::kStages & 1, &late);
+            for (uint32_t k = stage < S::kStages ? 0 : stage - S::kStages; k < stage; ++k) barrier_wait(shared_address(&c.inputs[k % S::kStages]), k / S::kStages & 1, &late);
         }
     }
     tc_fence_before();
