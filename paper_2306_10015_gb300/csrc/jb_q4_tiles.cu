@@ -16,8 +16,8 @@
 // Blocks pass from role to role in pairs: with one at a time the waits and commits of the warp that issues products, 160
 // cycles a block, bounded it (33 us for one row times 20480 x 5120). Now products do, 64 to 75 cycles each whatever the rows of
 // x are (a tile of 128 rows with levels from tensor memory), and beside them the pipe that serves shared memory: 16 rows by 64
-// columns take 16 turns of it for the table and about 15 others. 17 bf16 rows times 5120 x 20480: 24 us and 4 us of the two
-// kernels around it that do not hide, for 8.9 us of bytes; 64 rows times 20480 x 5120 36 us.
+// columns take 16 turns of it for the table and about 15 others. 17 bf16 rows times 5120 x 20480: 27.6 us, 4 of
+// them the two kernels around it, for 8.9 us of bytes; 64 rows times 20480 x 5120 36 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

@@ -13,10 +13,10 @@
 // products; four warps for each group, a thread a row, take scores from tensor memory and put weights in their place.
 //
 // What bounds it. Large trees: the softmax's warps, two on a scheduler. Three rows of 58000 tokens, 64 nodes by 8 query heads,
-// 8 key heads of 128, capped: 554 us, issue slots 55 % used, packed fp32 units half, tensor pipes 45 % (one group a block:
-// 643 us). 16 chains of 255 behind 400 to 1800 tokens, 40 heads of 128: 201 us, 24 % of the rate of plain products; a block has
+// 8 key heads of 128, capped: 549 us, issue slots 55 % used, packed fp32 units half, tensor pipes 45 % (one group a block:
+// 643 us). 16 chains of 255 behind 400 to 1800 tokens, 40 heads of 128: 198 us, 24 % of the rate of plain products; a block has
 // a dozen to three dozen tiles, and its first scores wait for its queries. Small trees: memory latency. 24 rows of 65 to 2000
-// tokens, up to 33 nodes, 32 heads of 128: 74 us for 36 us of bytes; the tiles that fit beside the queries are two ahead.
+// tokens, up to 33 nodes, 32 heads of 128: 70 us for 36 us of bytes; the tiles that fit beside the queries are two ahead.
 //
 // Loops are kept short: a warp that runs alone through code that is longer than its instruction cache waits for
 // instructions (128 positions of a thread unrolled: 8000 cycles for as many positions). Nor is cp.async for keys and
