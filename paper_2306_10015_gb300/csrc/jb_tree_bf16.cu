@@ -725,9 +725,9 @@ cudaError_t resident(int shared, int each, int most, int& ctas) {
 template <int D, int kGroups>
 constexpr int max_ctas() { return 160 * Shape<D, kGroups>::kCtas; }
 
-// Queries in blocks of whole nodes: false where a block is none, or strides are none of a box.
+// Queries in blocks of whole nodes: false where a block is none, or strides are none of a box (one query for all nodes, say).
 bool describe_queries(Encode encode, CUtensorMap& map, const TreeParams& p) {
-    if (kRows % p.a.group != 0) return false;
+    if (kRows % p.a.group != 0 || p.a.q_head == 0 || p.a.q_row == 0) return false;
     const cuuint64_t dims[4] = {static_cast<cuuint64_t>(p.a.head_dim), static_cast<cuuint64_t>(p.a.group), static_cast<cuuint64_t>(p.a.heads),
                                 static_cast<cuuint64_t>(p.trees.n_nodes)};
     const cuuint64_t strides[3] = {p.a.q_head * sizeof(T), p.a.q_head * p.a.group * sizeof(T), p.a.q_row * sizeof(T)};

@@ -439,3 +439,14 @@ def test_large_trees_queries_in_wider_rows(dtype, group):
                 got.append(out)
     torch.cuda.synchronize()
     assert all(torch.equal(o[:, 1:], want) and (o[:, 0] == 7).all() for o in got)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tree", [bush(20), bush(200)], ids=["small", "large"])
+def test_broadcast_and_transposed_queries(dtype, tree):
+    """One query for all nodes, one for all heads, and heads before nodes."""
+    n = len(tree)
+    cache, q = case(dtype, [90], [tree], 2, 2, 128, 16)
+    for view in (q[:1].expand(n, 4, 128), q[:, :1].expand(n, 4, 128), query(n * 4, 1, 128, dtype).view(4, n, 128).transpose(0, 1)):
+        want = check(cache, 0, view.contiguous(), [0], [tree])
+        assert torch.equal(jb.jb_attend_tree(cache, 0, view, draft([0], [tree])), want)
