@@ -431,11 +431,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tiles_kernel(const __grid_
             if (lane < here) copy_box(to + lane * S::kInputBytes, &p.inputs, (step * kStepBlocks + lane) * 64, 0, 0, 0, bar);
             if (++step == steps) step = 0;
         }
-        if (stage < all) {  // what is under way arrives first
-            int late = 0;
-            for (uint32_t k = asked < S::kStages ? 0 : asked - S::kStages; k < asked; ++k) barrier_wait(shared_address(&c.full[k % S::kStages]), k / S::kStages & 1, &late);
-            for (uint32_t k = stage < S::kStages ? 0 : stage - S::kStages; k < stage; ++k) barrier_wait(shared_address(&c.inputs[k % S::kStages]), k / S::kStages & 1, &late);
-        }
+        // what is under way arrives before the role ends, whatever became of the others
+        int late = 0;
+        for (uint32_t k = asked < S::kStages ? 0 : asked - S::kStages; k < asked; ++k) barrier_wait(shared_address(&c.full[k % S::kStages]), k / S::kStages & 1, &late);
+        for (uint32_t k = stage < S::kStages ? 0 : stage - S::kStages; k < stage; ++k) barrier_wait(shared_address(&c.inputs[k % S::kStages]), k / S::kStages & 1, &late);
     }
     tc_fence_before();
     __syncthreads();

@@ -86,6 +86,11 @@ __device__ void copy_role(const F32Params& f, typename S::Deal deal, Control<S>&
     const bool mine = group < kTileGroups && 32 * panel < p.a.head_dim;
     const uint32_t box_bytes = f.box * kGroup * 128;
     uint32_t copies = 0;
+    const auto last = [&] {  // what is under way arrives before the role ends, whatever became of the others
+        int late = 0;
+        for (uint32_t k = copies < S::kStages ? 0 : copies - S::kStages; k < copies; ++k)
+            barrier_wait(shared_address(&c.full[k % S::kStages]), k / S::kStages & 1, &late);
+    };
     Piece s;
     while (deal.take(p, s)) {
         const int* table = p.pages.table + static_cast<size_t>(s.span.row) * p.pages.row_pages;
@@ -97,12 +102,7 @@ __device__ void copy_role(const F32Params& f, typename S::Deal deal, Control<S>&
             for (int k = 0; k < kTileGroups; ++k)
                 if (!(boxes >> (k / f.box * S::kPanels) & 1u)) missing |= 1u << k;
             const uint32_t stage = copies % S::kStages, bar = shared_address(&c.full[stage]), to = ring + 2 * stage * S::kTileBytes + panel * S::kPanel + group * (kGroup * 128);
-            if (!__all_sync(kAll, barrier_wait(shared_address(&c.empty[stage]), (copies / S::kStages & 1) ^ 1, &c.failed))) {
-                int late = 0;  // what is under way arrives first
-                for (uint32_t k = copies < S::kStages ? 0 : copies - S::kStages; k < copies; ++k)
-                    barrier_wait(shared_address(&c.full[k % S::kStages]), k / S::kStages & 1, &late);
-                return;
-            }
+            if (!__all_sync(kAll, barrier_wait(shared_address(&c.empty[stage]), (copies / S::kStages & 1) ^ 1, &c.failed))) return last();
             if (lane == 0) {
                 *static_cast<volatile unsigned*>(&c.missing[stage]) = missing;
                 barrier_arrive_bytes(bar, 2 * __popc(boxes) * box_bytes);
@@ -115,6 +115,7 @@ __device__ void copy_role(const F32Params& f, typename S::Deal deal, Control<S>&
             __syncwarp();
         }
     }
+    last();
 }
 
 // kExtra: a cap or a bias on the scores.

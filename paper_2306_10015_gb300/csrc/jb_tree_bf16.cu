@@ -108,7 +108,7 @@ __device__ void copy_role(const TcParams& tc, typename S::Deal deal, Control& c,
     const bool mine = group < kGroups && 64 * panel < p.a.head_dim;
     const uint32_t box_bytes = tc.box * kGroup * 128;
     uint32_t copies = 0, tiles = 0, edges = 0, blocks = 0;
-    const auto give_up = [&] {  // what is under way arrives first
+    const auto last = [&] {  // what is under way arrives before the role ends, whatever became of the others
         int late = 0;
         for (uint32_t k = copies < S::kSlots ? 0 : copies - S::kSlots; k < copies; ++k)
             barrier_wait(shared_address(&c.full[k % S::kSlots]), k / S::kSlots & 1, &late);
@@ -138,7 +138,7 @@ __device__ void copy_role(const TcParams& tc, typename S::Deal deal, Control& c,
 #pragma unroll 1
             for (int kind = 0; kind < 2; ++kind) {
                 const uint32_t i = copies, slot = i % S::kSlots, at = ring + slot * S::kTileBytes;
-                if (!__all_sync(kAll, barrier_wait(shared_address(&c.empty[slot]), (i / S::kSlots & 1) ^ 1, &c.failed))) return give_up();
+                if (!__all_sync(kAll, barrier_wait(shared_address(&c.empty[slot]), (i / S::kSlots & 1) ^ 1, &c.failed))) return last();
                 if (kind == 1 && missing != 0) {  // what tiles before left there is no number to meet a weight of zero
                     for (int g = 0; g < kGroups; ++g)
                         if (missing >> g & 1u)
@@ -160,7 +160,7 @@ __device__ void copy_role(const TcParams& tc, typename S::Deal deal, Control& c,
                 ++copies;
                 if (tc.query_box && kind == 0 && tile == s.span.first_tile + s.from) {
                     const uint32_t b = blocks % S::kQueries;
-                    if (!__all_sync(kAll, barrier_wait(shared_address(&c.queries_read[b]), (blocks / S::kQueries & 1) ^ 1, &c.failed))) return give_up();
+                    if (!__all_sync(kAll, barrier_wait(shared_address(&c.queries_read[b]), (blocks / S::kQueries & 1) ^ 1, &c.failed))) return last();
                     const int groups = S::groups_of(p, s), g = lane / kPanels, x = 64 * (lane % kPanels);
                     if (lane == 0) barrier_arrive_bytes(shared_address(&c.queries[b]), groups * ((p.a.head_dim + 63) / 64) * S::kQueryPanel);
                     __syncwarp();
@@ -172,6 +172,7 @@ __device__ void copy_role(const TcParams& tc, typename S::Deal deal, Control& c,
             }
         }
     }
+    last();
 }
 
 // 128 rows of queries from row `first` of the tree's on, by all helpers. Rows that are not real stay what they were: their results go nowhere.
