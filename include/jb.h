@@ -313,6 +313,10 @@ typedef struct {
     int32_t by_token;
 } jb_kv;
 
+/* Host threads: a call from here on may be several launches. No other call with the same workspace or the same page table may
+ * be made until it returns, also not on its stream, where the other's launches would come between its own. Calls that follow
+ * one another on one stream can share a workspace. */
+
 /*
  * jb_cache_reserve -- room for new tokens: lens[d_rows[i]] += d_tokens[i], with free
  * pages taken for it, the lowest ids first, in the order of the list (i, then the

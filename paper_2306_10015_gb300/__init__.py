@@ -26,8 +26,8 @@ and, for scores that are not losses, what writing an answer with the perturbed m
   their positions' rotation (``Rotation``), attended to at once, and one path of them kept
 * ``jb_q4_matmul``  products with the 4-bit weights that ``jb_perturb_q4`` perturbs
 
-Their tensors are on one device, the current one. No gradients flow through any call here: results
-of tensors that require them carry none.
+Their tensors are on one device, the current one. Calls of several host threads on one ``PageTable`` or one ``Q4Table``
+are enqueued one after the other. No gradients flow through any call here: results of tensors that require them carry none.
 
 There is no CPU fallback: if ``libjb.so`` is missing, loading it raises.
 """
@@ -361,7 +361,7 @@ class Q4Table:
                 raise ValueError("codes or scales too short for numel")
             self.segments[i] = jb_q4_segment(codes.data_ptr(), scale.data_ptr(), int(numel), int(fo))
         self.n_segments = n
-        self._workspaces, self._matmul_bytes = _Workspaces(), {}
+        self._workspaces, self._matmul_bytes, self._lock = _Workspaces(), {}, threading.Lock()
 
     def matmul_workspace(self, out_features: int, in_features: int, dtype, n: int) -> int:
         """Device bytes that jb_q4_matmul of n rows (of a torch type) with such a matrix works in."""
@@ -376,8 +376,9 @@ class Q4Table:
 
 def jb_perturb_q4(table: "Q4Table", seed, eps: float, stream=None) -> None:
     """4-bit weights: dequantize, add eps z(seed), quantize again, in place."""
-    _check(lib().jb_perturb_q4(table.segments, table.n_segments, _seed(seed), float(eps),
-                               _stream(stream)))
+    with table._lock:
+        _check(lib().jb_perturb_q4(table.segments, table.n_segments, _seed(seed), float(eps),
+                                   _stream(stream)))
 
 
 def jb_q4_levels() -> np.ndarray:
@@ -409,6 +410,10 @@ def _need_torch():
     torch = module
 
 
+# A call is one launch or several, over a workspace that is kept for the stream and over the tables of the pages. Launches
+# of another host thread's call must not come between them (its stream may be the same one, and the interpreter is free
+# during a call), so calls on one PageTable, and calls on one Q4Table, are enqueued one at a time: its _lock.
+#
 # The tensors of a call are on one device, and that is the current one: a kernel of another device would take their
 # addresses for its own memory's. `device` is the number of the cache's or, of jb_sample, of the logits'.
 
@@ -464,7 +469,7 @@ class PageTable:
         self.struct = jb_pages(table.data_ptr(), lens.data_ptr(), refs.data_ptr(), table.shape[0],
                                table.shape[1], refs.shape[0], self.page_tokens)
         self.ref = ctypes.byref(self.struct)
-        self._bytes = {}
+        self._bytes, self._lock = {}, threading.Lock()
 
     def workspace(self, n: int) -> int:
         """Device bytes that jb_cache_fork of n pairs works in, or jb_cache_compact (n = 0)."""
@@ -595,7 +600,8 @@ def jb_cache_reserve(cache, rows, tokens, status=None, stream=None):
     device = getattr(pages, "device", None)
     pr, pt, n = _two_lists(rows, tokens, "rows and tokens", device)
     status = _status_of(status, pages, stream)
-    _check(lib().jb_cache_reserve(pages.ref, pr, pt, n, status.data_ptr(), _stream_on(device, stream)))
+    with pages._lock:
+        _check(lib().jb_cache_reserve(pages.ref, pr, pt, n, status.data_ptr(), _stream_on(device, stream)))
     return status
 
 
@@ -604,7 +610,8 @@ def jb_cache_free(cache, rows, stream=None) -> None:
     pages = getattr(cache, "pages", cache)
     device = getattr(pages, "device", None)
     pr, n = _list32(rows, "rows", device)
-    _check(lib().jb_cache_free(pages.ref, pr, n, _stream_on(device, stream)))
+    with pages._lock:
+        _check(lib().jb_cache_free(pages.ref, pr, n, _stream_on(device, stream)))
 
 
 def jb_cache_fork(cache: KVCache, parents, children, status=None, stream=None):
@@ -614,8 +621,9 @@ def jb_cache_fork(cache: KVCache, parents, children, status=None, stream=None):
     pp, pc, n = _two_lists(parents, children, "parents and children", cache.device)
     status = _status_of(status, pages, stream)
     handle = _stream_on(cache.device, stream)
-    ws, nbytes, held = cache._pages_workspace(n, stream, handle)
-    _check(lib().jb_cache_fork(pages.ref, cache.layers, cache.n_layers, pp, pc, n, status.data_ptr(), ws, nbytes, handle))
+    with pages._lock:
+        ws, nbytes, held = cache._pages_workspace(n, stream, handle)
+        _check(lib().jb_cache_fork(pages.ref, cache.layers, cache.n_layers, pp, pc, n, status.data_ptr(), ws, nbytes, handle))
     return status
 
 
@@ -624,8 +632,9 @@ def jb_cache_compact(cache: KVCache, status=None, stream=None):
     pages = cache.pages
     status = _status_of(status, pages, stream)
     handle = _stream_on(cache.device, stream)
-    ws, nbytes, held = cache._pages_workspace(0, stream, handle)
-    _check(lib().jb_cache_compact(pages.ref, cache.layers, cache.n_layers, status.data_ptr(), ws, nbytes, handle))
+    with pages._lock:
+        ws, nbytes, held = cache._pages_workspace(0, stream, handle)
+        _check(lib().jb_cache_compact(pages.ref, cache.layers, cache.n_layers, status.data_ptr(), ws, nbytes, handle))
     return status
 
 
@@ -646,8 +655,9 @@ def jb_cache_write(cache: KVCache, layer: int, k, v, rows, pos, stream=None) -> 
     pr, pp, n = _two_lists(rows, pos, "rows and positions", cache.device)
     ka, kb = _heads_of(k, cache.heads, cache, n, "new keys")
     va, vb = _heads_of(v, cache.heads, cache, n, "new values")
-    _check(lib().jb_cache_write(cache.pages.ref, cache.layer_refs[layer], k.data_ptr(), ka, kb, v.data_ptr(), va, vb,
-                                pr, pp, n, _stream_on(cache.device, stream)))
+    with cache.pages._lock:
+        _check(lib().jb_cache_write(cache.pages.ref, cache.layer_refs[layer], k.data_ptr(), ka, kb, v.data_ptr(), va, vb,
+                                    pr, pp, n, _stream_on(cache.device, stream)))
 
 
 def jb_attend(cache: KVCache, layer: int, q, rows, pos, out=None, scale: Optional[float] = None,
@@ -669,16 +679,17 @@ def jb_attend(cache: KVCache, layer: int, q, rows, pos, out=None, scale: Optiona
                                or slopes.shape != (heads,) or not slopes.is_contiguous()):
         raise ValueError("slopes must be a contiguous float32 tensor on the cache's CUDA device, one per query head")
     handle = _stream_on(cache.device, stream)
-    if workspace is None:
-        ws, nbytes, held = cache._attend_workspace(heads, stream, handle)
-    else:
-        if workspace.get_device() != cache.device or not workspace.is_contiguous():
-            raise ValueError("workspace must be a contiguous tensor on the cache's CUDA device")
-        ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    if workspace is not None and (workspace.get_device() != cache.device or not workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous tensor on the cache's CUDA device")
     scores = jb_scores(cache.head_dim ** -0.5 if scale is None else scale, softcap, window,
                        None if slopes is None else slopes.data_ptr())
-    _check(lib().jb_attend(cache.pages.ref, cache.layer_refs[layer], ctypes.byref(scores), q.data_ptr(), qa, qb, heads,
-                           pr, pp, n, out.data_ptr(), oa, ob, ws, nbytes, handle))
+    with cache.pages._lock:
+        if workspace is None:
+            ws, nbytes, held = cache._attend_workspace(heads, stream, handle)
+        else:
+            ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        _check(lib().jb_attend(cache.pages.ref, cache.layer_refs[layer], ctypes.byref(scores), q.data_ptr(), qa, qb, heads,
+                               pr, pp, n, out.data_ptr(), oa, ob, ws, nbytes, handle))
     return out
 
 
@@ -766,8 +777,9 @@ def jb_cache_append(cache: KVCache, layer: int, q, k, v, rows, pos, rotation: Ro
             q_out = _new(stream, torch.empty, (n, heads, cache.head_dim), dtype=q.dtype, device=q.device)
         oa, ob = _heads_of(q_out, heads, cache, n, "turned queries")
         pq, po = q.data_ptr(), q_out.data_ptr()
-    _check(lib().jb_cache_append(cache.pages.ref, cache.layer_refs[layer], rotation.ref, pq, qa, qb, heads, po, oa, ob,
-                                 k.data_ptr(), ka, kb, v.data_ptr(), va, vb, pr, pp, pt, n, _stream_on(device, stream)))
+    with cache.pages._lock:
+        _check(lib().jb_cache_append(cache.pages.ref, cache.layer_refs[layer], rotation.ref, pq, qa, qb, heads, po, oa, ob,
+                                     k.data_ptr(), ka, kb, v.data_ptr(), va, vb, pr, pp, pt, n, _stream_on(device, stream)))
     return q_out
 
 
@@ -793,16 +805,17 @@ def jb_attend_tree(cache: KVCache, layer: int, q, trees: DraftTrees, out=None, s
                                or slopes.shape != (heads,) or not slopes.is_contiguous()):
         raise ValueError("slopes must be a contiguous float32 tensor on the cache's CUDA device, one per query head")
     handle = _stream_on(cache.device, stream)
-    if workspace is None:
-        ws, nbytes, held = cache._plain_workspace("tree", cache._tree_workspace_bytes(), stream, handle)
-    else:
-        if workspace.get_device() != cache.device or not workspace.is_contiguous():
-            raise ValueError("workspace must be a contiguous tensor on the cache's CUDA device")
-        ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    if workspace is not None and (workspace.get_device() != cache.device or not workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous tensor on the cache's CUDA device")
     scores = jb_scores(cache.head_dim ** -0.5 if scale is None else scale, softcap, window,
                        None if slopes is None else slopes.data_ptr())
-    _check(lib().jb_attend_tree(cache.pages.ref, cache.layer_refs[layer], ctypes.byref(scores), trees.ref, q.data_ptr(), qa, qb,
-                                heads, out.data_ptr(), oa, ob, ws, nbytes, handle))
+    with cache.pages._lock:
+        if workspace is None:
+            ws, nbytes, held = cache._plain_workspace("tree", cache._tree_workspace_bytes(), stream, handle)
+        else:
+            ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        _check(lib().jb_attend_tree(cache.pages.ref, cache.layer_refs[layer], ctypes.byref(scores), trees.ref, q.data_ptr(), qa, qb,
+                                    heads, out.data_ptr(), oa, ob, ws, nbytes, handle))
     return out
 
 
@@ -818,8 +831,9 @@ def jb_cache_keep(cache: KVCache, trees: DraftTrees, leaves, status=None, stream
     status = _status_of(status, pages, stream)
     handle = _stream_on(cache.device, stream)
     nbytes = max(16, int(lib().jb_cache_keep_workspace(trees.ref)))
-    ws, nbytes, held = cache._plain_workspace("keep", nbytes, stream, handle)
-    _check(lib().jb_cache_keep(pages.ref, cache.layers, cache.n_layers, trees.ref, pl, status.data_ptr(), ws, nbytes, handle))
+    with pages._lock:
+        ws, nbytes, held = cache._plain_workspace("keep", nbytes, stream, handle)
+        _check(lib().jb_cache_keep(pages.ref, cache.layers, cache.n_layers, trees.ref, pl, status.data_ptr(), ws, nbytes, handle))
     return status
 
 
@@ -850,18 +864,19 @@ def jb_q4_matmul(table: "Q4Table", index: int, x, out_features: int, bias=None, 
             or (out.stride(1) != 1 and out_features > 1):
         raise ValueError("out must be [n, out_features] of x's type on its CUDA device, contiguous in a row")
     handle = _stream_on(device, stream)
-    if workspace is not None:
-        if workspace.get_device() != device or not workspace.is_contiguous():
-            raise ValueError("workspace must be a contiguous tensor on x's CUDA device")
-        ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    else:
-        ws, nbytes = None, table.matmul_workspace(out_features, inner, x.dtype, n)
-        if nbytes:
-            ws, nbytes, held = table._workspaces.get("matmul", nbytes, stream, handle, lambda size: _new(
-                stream, torch.empty, size, dtype=torch.uint8, device=x.device))
+    if workspace is not None and (workspace.get_device() != device or not workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous tensor on x's CUDA device")
     segment = ctypes.byref(table.segments, index % table.n_segments * ctypes.sizeof(jb_q4_segment))
-    _check(lib().jb_q4_matmul(segment, out_features, inner, dtype, x.data_ptr(), x.stride(0), n,
-                              None if bias is None else bias.data_ptr(), out.data_ptr(), out.stride(0), ws, nbytes, handle))
+    with table._lock:
+        if workspace is not None:
+            ws, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        else:
+            ws, nbytes = None, table.matmul_workspace(out_features, inner, x.dtype, n)
+            if nbytes:
+                ws, nbytes, held = table._workspaces.get("matmul", nbytes, stream, handle, lambda size: _new(
+                    stream, torch.empty, size, dtype=torch.uint8, device=x.device))
+        _check(lib().jb_q4_matmul(segment, out_features, inner, dtype, x.data_ptr(), x.stride(0), n,
+                                  None if bias is None else bias.data_ptr(), out.data_ptr(), out.stride(0), ws, nbytes, handle))
     return out
 
 
