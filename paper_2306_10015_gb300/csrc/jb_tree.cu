@@ -171,7 +171,7 @@ __device__ void work_role(const TreeParams& p, Control<S>& c, uint32_t ring, flo
             __syncwarp();
             if (!idle) {
                 const unsigned missing = *static_cast<volatile unsigned*>(&c.missing[stage]) >> (way * kPos / kGroup);
-                const bool edge = missing != 0 || t0 + kPos > s.span.base || (p.a.window > 0 && t0 < static_cast<long long>(s.span.base) + kMaxNodes - p.a.window);
+                const bool edge = missing != 0 || s.span.base - t0 < kPos || (p.a.window > 0 && t0 < static_cast<long long>(s.span.base) + kMaxNodes - p.a.window);
                 // scores of the lane's rows at positions place and place + 16 of the warp's
                 float2 x[kRows][kEach];
 #pragma unroll

@@ -87,9 +87,9 @@ struct Control {
     unsigned missing[8];     // groups of a tile whose page is missing; copies are at most five tiles ahead of the softmax
 };
 
-// Whether some of the positions [t, t + n) are seen by some nodes and not by others.
+// Whether some of the positions [t, t + n) are seen by some nodes and not by others. t + n itself may leave 31 bits.
 __device__ __forceinline__ bool edge_of(const TreeParams& p, const Span& s, int t, int n) {
-    return t + n > s.base || (p.a.window > 0 && t < static_cast<long long>(s.base) + kMaxNodes - p.a.window);
+    return s.base - t < n || (p.a.window > 0 && t < static_cast<long long>(s.base) + kMaxNodes - p.a.window);
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {

@@ -450,3 +450,28 @@ def test_broadcast_and_transposed_queries(dtype, tree):
     for view in (q[:1].expand(n, 4, 128), q[:, :1].expand(n, 4, 128), query(n * 4, 1, 128, dtype).view(4, n, 128).transpose(0, 1)):
         want = check(cache, 0, view.contiguous(), [0], [tree])
         assert torch.equal(jb.jb_attend_tree(cache, 0, view, draft([0], [tree])), want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("length", [(1 << 31) - 16, (1 << 31) - 20, (1 << 31) - 49])
+def test_rows_that_end_at_2_to_the_31(dtype, length):
+    """A window over the last tokens of the longest row: the tile of the last ones ends where positions leave 31 bits. Pages
+    further back are missing, places without a token and siblings' values hold NaN."""
+    tree, window, page = [-1, 0, 0, 1, 1, 0, 5], 300, 16
+    tokens = 400                                                          # that there are pages for
+    row_pages, first = (1 << 27) - 1, -(-length // page) - tokens // page
+    shift = first * page                                                  # the same tokens as a short row
+    small, q = case(dtype, [length - shift - len(tree)], [tree], 2, 1, 64, page)
+    pages = jb.PageTable.empty(1, row_pages, small.pages.refs.shape[0], page)
+    n = int((small.pages.table[0] >= 0).sum())
+    pages.table[0, first:first + n] = small.pages.table[0, :n]
+    pages.refs.copy_(small.pages.refs)
+    pages.lens.fill_(length)
+    cache = jb.KVCache(pages, small.keys, small.values)
+    want, tol = reference(small, 0, q, [0], [tree], window=window)
+    got = jb.jb_attend_tree(cache, 0, q, draft([0], [tree]), window=window)
+    assert torch.isfinite(got).all() and ((got.double() - want).abs() <= tol).all()
+    leaf = length - shift - 1                                             # the last node: itself alone sees it
+    small.values[0][int(small.pages.table[0, leaf // page]), :, leaf % page] = math.nan
+    hurt = jb.jb_attend_tree(cache, 0, q, draft([0], [tree]), window=window)
+    assert torch.equal(hurt[:-1], got[:-1]) and torch.isnan(hurt[-1]).all()
