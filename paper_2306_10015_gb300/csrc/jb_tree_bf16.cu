@@ -426,7 +426,9 @@ __device__ void softmax_role(const TreeParams& p, Control& c, Work<typename S::D
         const bool real = all < rows, idle = s.block * S::kBlock + 32 * warp >= rows;  // idle: none of the warp's rows is real
         const int node = real ? all / p.a.group : 0, h = real ? all - node * p.a.group : 0, depth = real ? nodes.depth[node] : -1;
         const float slope = kScores == kBiased && real && p.a.slopes != nullptr ? p.a.slopes[s.head * p.a.group + h] * kLog2e : 0.0f;
-        float m = kLowest, offset = 0.0f, l = 0.0f;  // offset: what is subtracted from scores, in powers of two; 0 before one is seen
+        // m: the largest score, in kPlain before the scale, which may bring anything finite into range; after it what is not
+        // above kLowest counts as infinite. offset: what is subtracted from scores, in powers of two; 0 before one is seen
+        float m = -INFINITY, offset = 0.0f, l = 0.0f;
         for (int tile = s.span.first_tile + s.from; tile < s.span.first_tile + s.to; ++tile, ++tiles, ++mine) {
             const int t0 = tile * kTile;
             const uint32_t buffer = mine % kScoreTiles, at = tmem + buffer * kTile;
@@ -435,7 +437,7 @@ __device__ void softmax_role(const TreeParams& p, Control& c, Work<typename S::D
             if (!idle) {
                 const unsigned missing = *static_cast<volatile unsigned*>(&c.missing[tiles % 8]);
                 const bool edge = missing != 0 || edge_of(p, s.span, t0, kTile);
-                float tops[4] = {kLowest, kLowest, kLowest, kLowest};
+                float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                 const auto seen_at = [&](int i) {  // of 32 positions
                     unsigned seen = seen_of(p, s.span, nodes, node, depth, t0 + 32 * i);
                     if (missing >> (2 * i) & 1u) seen &= 0xFFFF0000u;
@@ -521,12 +523,12 @@ __device__ void softmax_role(const TreeParams& p, Control& c, Work<typename S::D
                     for (int k = 0; k < kTile; ++k) tops[k % 4] = fmaxf(tops[k % 4], __uint_as_float(raw[k]));
                 }
                 const float high = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-                const bool rises = high > m && (m == kLowest || (high - m) * by > kSlack);
+                const float top = high * by;
+                const bool rises = high > m && top > kLowest && (m == -INFINITY || (high - m) * by > kSlack);
                 if (__any_sync(kAll, rises)) {
                     float k = 1.0f;
                     if (rises) {
-                        const float top = high * by;
-                        k = m == kLowest ? 0.0f : exp2_approx(offset - top);
+                        k = m == -INFINITY ? 0.0f : exp2_approx(offset - top);
                         m = high;
                         offset = top;
                         l *= k;
@@ -594,7 +596,7 @@ __device__ void softmax_role(const TreeParams& p, Control& c, Work<typename S::D
         if (idle) continue;
         float* slot = slot_of<C, D>(p, gridDim.x, blockIdx.x, s.from == 0);
         if (!whole && real) {
-            slot[S::kBlock * D + row] = m == kLowest || depth < 0 ? kLowest : offset;
+            slot[S::kBlock * D + row] = m == -INFINITY || depth < 0 ? kLowest : offset;
             slot[S::kBlock * D + S::kBlock + row] = depth < 0 ? 0.0f : l;
         }
         const float inverse = l > 0.0f ? 1.0f / l : 0.0f;

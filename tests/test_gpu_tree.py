@@ -475,3 +475,36 @@ def test_rows_that_end_at_2_to_the_31(dtype, length):
     small.values[0][int(small.pages.table[0, leaf // page]), :, leaf % page] = math.nan
     hurt = jb.jb_attend_tree(cache, 0, q, draft([0], [tree]), window=window)
     assert torch.equal(hurt[:-1], got[:-1]) and torch.isnan(hurt[-1]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_products_under_a_small_scale(dtype):
+    """Products of -3.1e38 by a scale of 2^-120 are scores of -232, as good as any others."""
+    trees = [chain(3), chain(1)]
+    cache, _ = case(dtype, [70, 0], trees, 1, 1, 64, 16, spare=0)
+    q = torch.full((4, 1, 64), 2.0**61, dtype=DT[dtype], device="cuda")
+    cache.keys[0].copy_(torch.where(torch.isnan(cache.keys[0]), cache.keys[0], torch.full_like(cache.keys[0], -1.8125 * 2.0**60)))
+    check(cache, 0, q, range(2), trees, scale=2.0**-120)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [1.0, 4.0])
+def test_scores_beyond_2e38_count_as_infinite(dtype, scale):
+    """Products of -3.0e38 leave fp32 with the factor that makes powers of two of exponentials: those positions are not seen, and a
+    node that sees no others gets zeros, as single queries have it."""
+    trees = [chain(3), chain(2)]
+    cache, _ = case(dtype, [130, 20], trees, 1, 1, 64, 16, spare=0)
+    q = torch.full((5, 1, 64), 2.0**61, dtype=DT[dtype], device="cuda")
+    key = torch.where(torch.isnan(cache.keys[0]), cache.keys[0], torch.full_like(cache.keys[0], -1.75 * 2.0**60))
+    for t in range(0, 133, 3):
+        key[int(cache.pages.table[0, t // 16]), :, t % 16] = 0.0
+    cache.keys[0].copy_(key)
+    got = jb.jb_attend_tree(cache, 0, q, draft(range(2), trees), scale=scale)
+    one = jb.jb_attend(cache, 0, q, i32([0, 0, 0, 1, 1]), i32([130, 131, 132, 20, 21]), scale=scale)
+    assert (got[3:] == 0).all() and (one[3:] == 0).all()
+    for j in range(3):
+        place = torch.arange(0, 131 + j, 3)
+        ids = cache.pages.table[0].cpu()[place // 16].long()
+        want = cache.values[0][ids.cuda(), 0, (place % 16).cuda()].double().mean(0)
+        tol = 2.0**-20 + (2.0**-16 + 2.0**-8 * want.abs() if dtype == "bf16" else 0)
+        assert ((got[j, 0].double() - want).abs() <= tol).all() and ((one[j, 0].double() - want).abs() <= tol).all()
