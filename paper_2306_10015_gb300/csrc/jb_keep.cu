@@ -18,7 +18,8 @@ namespace {
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWarps = kPlanThreads / 32;
 
-__device__ __forceinline__ int pages_of(int tokens, int page_tokens) { return (tokens + page_tokens - 1) / page_tokens; }
+// Without the end of the last page, which may lie past 2^31 - 1.
+__device__ __forceinline__ int pages_of(int tokens, int page_tokens) { return tokens / page_tokens + (tokens % page_tokens != 0); }
 
 // Workspace: header; count[n], moves of each tree; from[n_nodes] and to[n_nodes] as (page, place in it), a tree's moves
 // at its nodes' places in the list.

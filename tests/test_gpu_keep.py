@@ -152,3 +152,22 @@ def test_many_layers_and_a_graph():
         graph.replay()
         assert status.item() == want == 0
         both.same()
+
+
+def test_a_row_that_ends_at_2_to_the_31():
+    """Its last pages are there, of 48 tokens, so that the row's end is less than a page from where positions leave 31 bits."""
+    page, n_pages, heads, d = 48, 16, 2, 8
+    row_pages = ((1 << 31) - 1) // page
+    pages = jb.PageTable.empty(1, row_pages, n_pages, page)
+    length, nodes = row_pages * page - 3, 200
+    pages.table[0, row_pages - 8:] = torch.arange(8, dtype=torch.int32, device="cuda")
+    pages.refs[:8] = 1
+    pages.lens.fill_(length)
+    k, v = (torch.randn(n_pages, heads, page, d, device="cuda") for _ in range(2))
+    cache = jb.KVCache(pages, [k], [v])
+    assert jb.jb_cache_keep(cache, draft([0], [chain(nodes)]), i32([9])).item() == 0
+    kept = length - nodes + 10
+    left = -(-kept // page) - (row_pages - 8)                             # of the eight pages
+    assert pages.lens.tolist() == [kept] and 0 < left < 8
+    assert pages.table[0, row_pages - 8:].tolist() == list(range(left)) + [-1] * (8 - left)
+    assert pages.refs[:8].tolist() == [1] * left + [0] * (8 - left)
