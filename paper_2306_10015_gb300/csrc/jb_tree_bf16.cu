@@ -205,15 +205,17 @@ __device__ void copy_queries(const TreeParams& p, const Piece& s, int first, uin
 }
 
 // A value that is not finite must not meet a weight of zero: it is taken out here and added at the end to the rows that see
-// it. So are the rows outside [lo, hi), which nobody sees. True if there was one inside.
-template <typename S, int D>
-__device__ bool clean_values(uint32_t tile, int lo, int hi) {
-    const int u = threadIdx.x - S::kFirstHelper;
+// it. So are the rows outside [lo, hi), which nobody sees. True if there was one inside. Panels that heads of `d` elements do not
+// reach are not copied and hold anything: a pattern found there sent every later block of the CTA through put_back (8 chains of
+// 255, 4 heads of 192: 2930 us, with zeros there 54).
+template <typename S>
+__device__ bool clean_values(uint32_t tile, int d, int lo, int hi) {
+    const int u = threadIdx.x - S::kFirstHelper, pieces = (d + 63) / 64 * (kTile * 8);
     constexpr int kAhead = S::kHelpWarps == 1 ? 8 : 2;
-    static_assert(kTile * (D / 8) % (kAhead * S::kHelpThreads) == 0);
+    static_assert(kTile * 8 % (kAhead * S::kHelpThreads) == 0);
     bool bad = false;
 #pragma unroll 1
-    for (int i = u; i < kTile * (D / 8); i += kAhead * S::kHelpThreads) {
+    for (int i = u; i < pieces; i += kAhead * S::kHelpThreads) {
         uint32_t w[kAhead][4];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
@@ -271,7 +273,7 @@ __device__ void help_role(const TcParams& tc, typename S::Deal deal, Control& c,
             // first that its copy has begun: the slot's own phase may be any before that
             if (!__all_sync(kAll, barrier_wait_idle(shared_address(&c.edges[e % 8]), e / 8 & 1, &c.failed))) return;
             if (!__all_sync(kAll, barrier_wait(shared_address(&c.full[slot]), i / S::kSlots & 1, &c.failed))) return;
-            if (clean_values<S, D>(ring + slot * S::kTileBytes, s.span.lo - tile * kTile, s.span.len - tile * kTile))
+            if (clean_values<S>(ring + slot * S::kTileBytes, p.a.head_dim, s.span.lo - tile * kTile, s.span.len - tile * kTile))
                 *static_cast<volatile int*>(&c.not_finite) = 1;
             tell(&c.clean[slot]);
         }

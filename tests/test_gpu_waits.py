@@ -1,0 +1,46 @@
+"""What a kernel before them left in shared memory, and values that are not finite, say nothing of the time of others."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+import torch
+
+import paper_2306_10015_gb300 as jb
+from paper_2306_10015_gb300 import build
+from test_gpu_tree import case, chain, check, draft
+
+pytestmark = pytest.mark.gpu
+HERE = os.path.dirname(os.path.abspath(__file__))
+
+
+@pytest.fixture(scope="module")
+def helper():
+    src, out_dir = os.path.join(HERE, "helpers", "waits.cu"), os.path.join(HERE, "_build")
+    os.makedirs(out_dir, exist_ok=True)
+    so = os.path.join(out_dir, "libwaits.so")
+    subprocess.run([build.nvcc(), *build.ARCH, "-O2", "-std=c++17", "-I", build.CSRC, "-shared", "-Xcompiler", "-fPIC", src, "-o", so], check=True)
+    lib = ctypes.CDLL(so)
+    lib.unserved_wait.argtypes = [ctypes.c_void_p]
+    lib.fill_shared.argtypes = [ctypes.c_uint32]
+    return lib
+
+
+def test_heads_of_192_do_not_depend_on_what_shared_memory_held(helper):
+    """Only three of the four panels of a tile are copied for them; the fourth may hold anything."""
+    trees = [chain(255)] * 8
+    cache, q = case("bf16", [100] * 8, trees, 4, 1, 192, 16)
+    want = check(cache, 0, q, range(8), trees)
+    t, out = draft(range(8), trees), torch.empty_like(q)
+    times = {}
+    for _ in range(6):
+        for pattern in (0, 0x7FC07FC0):
+            assert helper.fill_shared(pattern) == 0
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            jb.jb_attend_tree(cache, 0, q, t, out=out)
+            b.record()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want)
+            times[pattern] = min(times.get(pattern, 1e9), a.elapsed_time(b))
+    assert times[0x7FC07FC0] <= 1.3 * times[0], times
