@@ -83,7 +83,9 @@ struct Control {
     unsigned long long scores[2][kScoreTiles], weights[2][kScoreTiles], sums[2];  // of each group of rows
     uint32_t tmem;
     int failed;
-    int not_finite;          // a value that some rows see and others do not was not finite, in some tile so far
+    // Block b's place b % 8 is b + 1 if a value in it that some rows see and others do not was not finite. A block has a tile at
+    // least, and helpers are at most five tiles ahead of the softmax, as copies are.
+    uint32_t not_finite[8];
     unsigned missing[8];     // groups of a tile whose page is missing; copies are at most five tiles ahead of the softmax
 };
 
@@ -246,7 +248,7 @@ template <typename S, int D>
 __device__ void help_role(const TcParams& tc, typename S::Deal deal, Control& c, uint32_t queries, uint32_t ring) {
     const TreeParams& p = tc.t;
     const int lane = threadIdx.x & 31;
-    uint32_t blocks = 0, tiles = 0, edges = 0;
+    uint32_t blocks = 0, done = 0, tiles = 0, edges = 0;
     const auto tell = [&](unsigned long long* bar) {
         shared_to_async_proxy();
         __syncwarp();
@@ -274,9 +276,10 @@ __device__ void help_role(const TcParams& tc, typename S::Deal deal, Control& c,
             if (!__all_sync(kAll, barrier_wait_idle(shared_address(&c.edges[e % 8]), e / 8 & 1, &c.failed))) return;
             if (!__all_sync(kAll, barrier_wait(shared_address(&c.full[slot]), i / S::kSlots & 1, &c.failed))) return;
             if (clean_values<S>(ring + slot * S::kTileBytes, p.a.head_dim, s.span.lo - tile * kTile, s.span.len - tile * kTile))
-                *static_cast<volatile int*>(&c.not_finite) = 1;
+                *static_cast<volatile uint32_t*>(&c.not_finite[done % 8]) = done + 1;
             tell(&c.clean[slot]);
         }
+        ++done;
         // with room for one block of queries the next can come only when this one has been read to its end
         if (S::kQueries == 1 && more && !block(next)) return;
         s = next;
@@ -408,7 +411,7 @@ __device__ void softmax_role(const TreeParams& p, Control& c, Work<typename S::D
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = warp / 4, row = threadIdx.x, d = p.a.head_dim;
     const uint32_t tmem = c.tmem + g * S::kGroupColumns + (static_cast<uint32_t>(32 * (warp % 4)) << 16);
     const float by = kScores == kPlain ? p.a.scale * kLog2e : 1.0f;
-    uint32_t tiles = 0, mine = 0;  // so far; mine: of those that the group has rows for
+    uint32_t blocks = 0, tiles = 0, mine = 0;  // so far, the block at hand among them; mine: of tiles that the group has rows for
     int tree = -1;
     bool ok = true;  // a wait that gives up leaves the loops as they are: other warps may wait for this one
     const Piece& s = work.piece;
@@ -417,6 +420,7 @@ __device__ void softmax_role(const TreeParams& p, Control& c, Work<typename S::D
         if (threadIdx.x == 0) work.more = work.deal.take(p, work.piece);
         any_of<S::kSoftmaxWarps>(false);
         if (work.more == 0) break;
+        ++blocks;
         if (s.tree != tree) fill_nodes<32 * S::kSoftmaxWarps>(p, s.span, nodes, threadIdx.x, any_of<S::kSoftmaxWarps>);
         tree = s.tree;
         const int rows = s.span.nodes * p.a.group, all = s.block * S::kBlock + row;
@@ -602,7 +606,7 @@ __device__ void softmax_role(const TreeParams& p, Control& c, Work<typename S::D
             slot[S::kBlock * D + S::kBlock + row] = depth < 0 ? 0.0f : l;
         }
         const float inverse = l > 0.0f ? 1.0f / l : 0.0f;
-        const bool mend = *static_cast<volatile int*>(&c.not_finite) != 0;
+        const bool mend = *static_cast<volatile uint32_t*>(&c.not_finite[(blocks - 1) % 8]) == blocks;
         T* out = reinterpret_cast<T*>(p.a.out) + (s.span.first + node) * p.a.out_row + (s.head * p.a.group + h) * p.a.out_head;
 #pragma unroll 1
         for (int e = 0; e < D; e += 32) {
@@ -653,7 +657,10 @@ __global__ void __launch_bounds__(Shape<D, kGroups>::kThreads, Shape<D, kGroups>
             barrier_init(shared_address(&c.clean[i]), S::kHelpWarps);
             barrier_init(shared_address(&c.empty[i]), kGroups);
         }
-        for (int i = 0; i < 8; ++i) barrier_init(shared_address(&c.edges[i]), 1);
+        for (int i = 0; i < 8; ++i) {
+            barrier_init(shared_address(&c.edges[i]), 1);
+            c.not_finite[i] = 0;
+        }
         for (int g = 0; g < kGroups; ++g) {
             for (int i = 0; i < kScoreTiles; ++i) {
                 barrier_init(shared_address(&c.scores[g][i]), 1);
@@ -666,7 +673,7 @@ __global__ void __launch_bounds__(Shape<D, kGroups>::kThreads, Shape<D, kGroups>
             barrier_init(shared_address(&c.queries[i]), tc.query_box ? 1 : S::kHelpWarps);
             barrier_init(shared_address(&c.queries_read[i]), kGroups);
         }
-        c.failed = c.not_finite = 0;
+        c.failed = 0;
         barriers_initialized();
     }
     if (warp == kSoftmaxWarps) tmem_alloc(shared_address(&c.tmem), S::kColumns);

@@ -508,3 +508,22 @@ def test_scores_beyond_2e38_count_as_infinite(dtype, scale):
         want = cache.values[0][ids.cuda(), 0, (place % 16).cuda()].double().mean(0)
         tol = 2.0**-20 + (2.0**-16 + 2.0**-8 * want.abs() if dtype == "bf16" else 0)
         assert ((got[j, 0].double() - want).abs() <= tol).all() and ((one[j, 0].double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_many_blocks_some_with_values_that_are_not_finite(bad):
+    """A CTA works on block after block: what it has to mend in one says nothing of the others."""
+    n, heads = 400, 8
+    trees = [bush(3 + i % 5, i) for i in range(n)]
+    cache, q = case("bf16", [(7 * i) % 50 for i in range(n)], trees, heads, 1, 64, 16)
+    clean = check(cache, 0, q, range(n), trees)
+    table, lens, first, own = cache.pages.table.cpu(), cache.pages.lens.tolist(), 0, []
+    for i, tree in enumerate(trees):
+        if i % 7 == 0:                                                    # the tree's last node, which nobody follows
+            t = lens[i] - 1
+            cache.values[0][int(table[i, t // 16]), :, t % 16] = bad
+            own.append(first + len(tree) - 1)
+        first += len(tree)
+    got = jb.jb_attend_tree(cache, 0, q, draft(range(n), trees))
+    others = sorted(set(range(first)) - set(own))
+    assert torch.equal(got[others], clean[others]) and not torch.isfinite(got[own]).any()

@@ -44,3 +44,24 @@ def test_heads_of_192_do_not_depend_on_what_shared_memory_held(helper):
             assert torch.equal(out, want)
             times[pattern] = min(times.get(pattern, 1e9), a.elapsed_time(b))
     assert times[0x7FC07FC0] <= 1.3 * times[0], times
+
+
+def test_a_value_that_is_not_finite_slows_its_own_block_alone():
+    """In the first head of the first tree or in the last of the last: the CTA with the first block has others after it."""
+    n, heads = 120, 8
+    trees = [chain(200)] * n
+    cache, q = case("bf16", [60] * n, trees, heads, 1, 64, 16)
+    t, out, times, values = draft(range(n), trees), torch.empty_like(q), {}, cache.values[0].clone()
+    for _ in range(6):
+        for tree, head in ((0, 0), (n - 1, heads - 1)):
+            cache.values[0].copy_(values)
+            cache.values[0][int(cache.pages.table[tree, 259 // 16]), head, 259 % 16] = float("nan")   # the last node
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            jb.jb_attend_tree(cache, 0, q, t, out=out)
+            b.record()
+            torch.cuda.synchronize()
+            last = 200 * tree + 199
+            assert torch.isnan(out[last]).all(1).nonzero().tolist() == [[head]] and torch.isfinite(out[:last]).all() and torch.isfinite(out[last + 1:]).all()
+            times[tree] = min(times.get(tree, 1e9), a.elapsed_time(b))
+    assert times[0] <= 1.5 * times[n - 1], times
