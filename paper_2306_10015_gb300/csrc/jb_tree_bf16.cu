@@ -210,9 +210,9 @@ __device__ void copy_queries(const TreeParams& p, const Piece& s, int first, uin
 // it. So are the rows outside [lo, hi), which nobody sees. True if there was one inside. Panels that heads of `d` elements do not
 // reach are not copied and hold anything: a pattern found there sent every later block of the CTA through put_back (8 chains of
 // 255, 4 heads of 192: 2930 us, with zeros there 54).
-template <typename S>
+template <typename S, int D>
 __device__ bool clean_values(uint32_t tile, int d, int lo, int hi) {
-    const int u = threadIdx.x - S::kFirstHelper, pieces = (d + 63) / 64 * (kTile * 8);
+    const int u = threadIdx.x - S::kFirstHelper, pieces = (D == 256 ? (d + 63) / 64 : D / 64) * (kTile * 8);
     constexpr int kAhead = S::kHelpWarps == 1 ? 8 : 2;
     static_assert(kTile * 8 % (kAhead * S::kHelpThreads) == 0);
     bool bad = false;
@@ -275,7 +275,7 @@ __device__ void help_role(const TcParams& tc, typename S::Deal deal, Control& c,
             // first that its copy has begun: the slot's own phase may be any before that
             if (!__all_sync(kAll, barrier_wait_idle(shared_address(&c.edges[e % 8]), e / 8 & 1, &c.failed))) return;
             if (!__all_sync(kAll, barrier_wait(shared_address(&c.full[slot]), i / S::kSlots & 1, &c.failed))) return;
-            if (clean_values<S>(ring + slot * S::kTileBytes, p.a.head_dim, s.span.lo - tile * kTile, s.span.len - tile * kTile))
+            if (clean_values<S, D>(ring + slot * S::kTileBytes, p.a.head_dim, s.span.lo - tile * kTile, s.span.len - tile * kTile))
                 *static_cast<volatile uint32_t*>(&c.not_finite[done % 8]) = done + 1;
             tell(&c.clean[slot]);
         }
@@ -399,6 +399,7 @@ struct Work {
     Deal deal;
     Piece piece;
     int more;
+    uint32_t blocks;  // so far, the piece's among them
 };
 
 template <typename S, int D, Scores kScores>
@@ -411,16 +412,18 @@ __device__ void softmax_role(const TreeParams& p, Control& c, Work<typename S::D
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = warp / 4, row = threadIdx.x, d = p.a.head_dim;
     const uint32_t tmem = c.tmem + g * S::kGroupColumns + (static_cast<uint32_t>(32 * (warp % 4)) << 16);
     const float by = kScores == kPlain ? p.a.scale * kLog2e : 1.0f;
-    uint32_t blocks = 0, tiles = 0, mine = 0;  // so far, the block at hand among them; mine: of tiles that the group has rows for
+    uint32_t tiles = 0, mine = 0;  // so far; mine: of those that the group has rows for
     int tree = -1;
     bool ok = true;  // a wait that gives up leaves the loops as they are: other warps may wait for this one
     const Piece& s = work.piece;
     for (;;) {
         any_of<S::kSoftmaxWarps>(false);  // nobody reads the last piece any more
-        if (threadIdx.x == 0) work.more = work.deal.take(p, work.piece);
+        if (threadIdx.x == 0) {
+            work.more = work.deal.take(p, work.piece);
+            ++work.blocks;
+        }
         any_of<S::kSoftmaxWarps>(false);
         if (work.more == 0) break;
-        ++blocks;
         if (s.tree != tree) fill_nodes<32 * S::kSoftmaxWarps>(p, s.span, nodes, threadIdx.x, any_of<S::kSoftmaxWarps>);
         tree = s.tree;
         const int rows = s.span.nodes * p.a.group, all = s.block * S::kBlock + row;
@@ -606,6 +609,7 @@ __device__ void softmax_role(const TreeParams& p, Control& c, Work<typename S::D
             slot[S::kBlock * D + S::kBlock + row] = depth < 0 ? 0.0f : l;
         }
         const float inverse = l > 0.0f ? 1.0f / l : 0.0f;
+        const uint32_t blocks = work.blocks;
         const bool mend = *static_cast<volatile uint32_t*>(&c.not_finite[(blocks - 1) % 8]) == blocks;
         T* out = reinterpret_cast<T*>(p.a.out) + (s.span.first + node) * p.a.out_row + (s.head * p.a.group + h) * p.a.out_head;
 #pragma unroll 1
@@ -688,6 +692,7 @@ __global__ void __launch_bounds__(Shape<D, kGroups>::kThreads, Shape<D, kGroups>
             if (threadIdx.x == 0) {
                 take_note(p, {});
                 work.deal = deal;
+                work.blocks = 0;
             }
             softmax_role<S, D, kScores>(p, c, work, nodes);
         } else if (warp < S::kCopyWarp) {
