@@ -24,7 +24,7 @@ __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
         : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
 }
-// The same, but the thread may sleep for about a millisecond before it says no.
+// The same, but the thread may sleep for up to about a millisecond before it says no.
 __device__ __forceinline__ bool barrier_sleep(uint32_t bar, uint32_t parity) {
     uint32_t done;
     asm volatile(
@@ -32,16 +32,17 @@ __device__ __forceinline__ bool barrier_sleep(uint32_t bar, uint32_t parity) {
         : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
 }
-// Waits for the phase of this parity to end. A wait of over about two seconds gives up and sets *failed, and so does one
-// that finds it set: then all roles of the CTA leave their loops. Few polls: those of waiting warps took 40 % of all
-// instructions without sleep and with a look at the clock each.
+// Waits for the phase of this parity to end. A wait of over about two seconds gives up and sets *failed, and one that finds it
+// set gives up after a look: then the roles of the CTA leave their loops, or go through the rest of them, a look a wait, where
+// other warps need their part in a barrier. Few polls: those of waiting warps took 40 % of all instructions without sleep and
+// with a look at the clock each.
 constexpr long long kPatience = 4000000000ll;  // cycles
 static __device__ __noinline__ bool barrier_wait_long(uint32_t bar, uint32_t parity, volatile int* failed) {
     const long long start = clock64();
     for (;;) {
+        if (*failed) return false;
         for (int i = 0; i < 32; ++i)
             if (barrier_sleep(bar, parity)) return true;
-        if (*failed) return false;
         if (clock64() - start > kPatience) {
             *failed = 1;
             return false;

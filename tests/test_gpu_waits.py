@@ -1,4 +1,4 @@
-"""What a kernel before them left in shared memory, and values that are not finite, say nothing of the time of others."""
+"""Waits that run out, and what a kernel before them left in shared memory or values that are not finite do to the time of others."""
 import ctypes
 import os
 import subprocess
@@ -65,3 +65,13 @@ def test_a_value_that_is_not_finite_slows_its_own_block_alone():
             assert torch.isnan(out[last]).all(1).nonzero().tolist() == [[head]] and torch.isfinite(out[:last]).all() and torch.isfinite(out[last + 1:]).all()
             times[tree] = min(times.get(tree, 1e9), a.elapsed_time(b))
     assert times[0] <= 1.5 * times[n - 1], times
+
+
+def test_a_wait_that_nobody_serves_gives_up_and_later_ones_do_not_wait(helper):
+    """The limit is 4e9 cycles, looked at after every 32 looks at the barrier. After it a wait is one look and no more."""
+    out = torch.zeros(6, dtype=torch.int64, device="cuda")
+    assert helper.unserved_wait(out.data_ptr()) == 0
+    first, failed, cycles, look, later, second = out.tolist()
+    assert (first, failed, second) == (0, 1, 0)
+    assert 4e9 < cycles < 4e9 + 40 * look + 10_000, (cycles, look)
+    assert later <= 3 * look + 2000, f"{later} cycles after the limit, {look} a look"
