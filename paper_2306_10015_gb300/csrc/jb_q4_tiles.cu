@@ -395,12 +395,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tiles_kernel(const __grid_
             }
             if (++step == steps) step = 0;
         }
-        if (!ok && elected()) {  // what is under way ends before tensor memory is given back
-            int late = 0;
-            tc_commit(shared_address(&c.drained));
-            barrier_wait(shared_address(&c.drained), 0, &late);
-        }
-        __syncwarp();
+        if (!ok) tc_drain(shared_address(&c.drained));  // what is under way ends before tensor memory is given back
     } else {  // copies; codes of the first stages go ahead of the inputs, which another kernel may still be converting
         const uint32_t all = static_cast<uint32_t>(end - begin);
         const int from_step = static_cast<int>(begin % steps), from_tile = static_cast<int>(begin / steps);

@@ -114,6 +114,17 @@ __device__ __forceinline__ void tc_wait_stores() { __syncwarp(); asm volatile("t
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
+// Waits for all products that the warp has issued, which a commit knows of in the lane that issued them: the elected one, the same
+// at each time. The whole warp; a barrier with one arrival that nothing else uses.
+__device__ __forceinline__ void tc_drain(uint32_t bar) {
+    __syncwarp();
+    if (elected()) {
+        int late = 0;
+        tc_commit(bar);
+        barrier_wait(bar, 0, &late);
+    }
+    __syncwarp();
+}
 
 // A tile in shared memory with rows of 128 bytes, 16-byte pieces of row r at (piece ^ r % 8), 1024-byte aligned: the lower
 // word of its descriptor, to which bytes / 16 can be added; the upper word is the same for all. `leading`: bytes from one

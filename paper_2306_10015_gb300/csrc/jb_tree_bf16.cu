@@ -698,14 +698,8 @@ __global__ void __launch_bounds__(Shape<D, kGroups>::kThreads, Shape<D, kGroups>
         } else if (warp < S::kCopyWarp) {
             const int g = warp - kSoftmaxWarps;
             product_role<S, D>(p, deal, c, g, queries, ring);
-            if ((threadIdx.x & 31) == 0) {
-                if (*static_cast<volatile int*>(&c.failed)) {  // what is under way ends before tensor memory is given back
-                    int late = 0;
-                    tc_commit(shared_address(&c.drained[g]));
-                    barrier_wait(shared_address(&c.drained[g]), 0, &late);
-                }
-            }
-            __syncwarp();
+            // what is under way ends before tensor memory is given back
+            if (__any_sync(kAll, *static_cast<volatile int*>(&c.failed) != 0)) tc_drain(shared_address(&c.drained[g]));
         } else if (warp == S::kCopyWarp) {
             copy_role<S, D>(tc, deal, c, queries, ring);
         } else {

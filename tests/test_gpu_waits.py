@@ -22,6 +22,7 @@ def helper():
     subprocess.run([build.nvcc(), *build.ARCH, "-O2", "-std=c++17", "-I", build.CSRC, "-shared", "-Xcompiler", "-fPIC", src, "-o", so], check=True)
     lib = ctypes.CDLL(so)
     lib.unserved_wait.argtypes = [ctypes.c_void_p]
+    lib.drained_products.argtypes = [ctypes.c_void_p]
     lib.fill_shared.argtypes = [ctypes.c_uint32]
     return lib
 
@@ -75,3 +76,11 @@ def test_a_wait_that_nobody_serves_gives_up_and_later_ones_do_not_wait(helper):
     assert (first, failed, second) == (0, 1, 0)
     assert 4e9 < cycles < 4e9 + 40 * look + 10_000, (cycles, look)
     assert later <= 3 * look + 2000, f"{later} cycles after the limit, {look} a look"
+
+
+def test_products_are_done_when_they_are_waited_for_at_the_end(helper):
+    out = torch.zeros(32, device="cuda")
+    for _ in range(50):
+        out.zero_()
+        assert helper.drained_products(out.data_ptr()) == 0
+        assert (out == 64 * 64).all()
