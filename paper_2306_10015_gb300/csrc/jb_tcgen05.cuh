@@ -17,14 +17,7 @@ __device__ __forceinline__ void barriers_initialized() { asm volatile("fence.mba
 __device__ __forceinline__ void barrier_arrive(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
-    uint32_t done;
-    asm volatile(
-        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-        : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-    return done != 0;
-}
-// The same, but the thread may sleep for up to about a millisecond before it says no.
+// Whether the phase of this parity has ended; the thread may sleep for up to about a millisecond before it says no.
 __device__ __forceinline__ bool barrier_sleep(uint32_t bar, uint32_t parity) {
     uint32_t done;
     asm volatile(
