@@ -370,6 +370,8 @@ class Q4Table:
         if nbytes is None:
             if torch is None:
                 _need_torch()
+            if len(self._matmul_bytes) >= 1024:  # numbers of rows may be any
+                self._matmul_bytes.clear()
             nbytes = self._matmul_bytes[key] = int(lib().jb_q4_matmul_workspace(out_features, in_features, _storage(dtype), n))
         return nbytes
 

@@ -216,3 +216,14 @@ def test_steps_are_the_frequencies(jb):
     turns = jb.Rotation.steps_of(f).view(np.uint64).astype(np.float64) / 2.0**64
     want = np.mod(f / (2 * np.pi), 1.0)
     assert np.abs(turns - want).max() <= 2.0**-53
+
+
+def test_sizes_of_workspaces_do_not_pile_up(jb):
+    """A server's numbers of rows are many; what is remembered of them is not."""
+    import torch
+    new = lambda *shape, dtype: on_device(0, torch.zeros(shape, dtype=dtype))[0]  # noqa: E731
+    table = jb.Q4Table([(new(128 * 32, dtype=torch.uint8), new(128, dtype=torch.float32), 128 * 64)])
+    want = [int(jb.lib().jb_q4_matmul_workspace(4096, 4096, 1, n)) for n in range(1, 3000)]
+    assert [table.matmul_workspace(4096, 4096, torch.bfloat16, n) for n in range(1, 3000)] == want and max(want) > 0
+    assert len(table._matmul_bytes) <= 1024
+    assert table.matmul_workspace(4096, 4096, torch.bfloat16, 9) == want[8]
