@@ -543,7 +543,7 @@ uint64_t jb_cache_keep_workspace(const jb_trees* trees);
  *   out_features  at most 2^30
  *   in_features   a multiple of 64 (a block's scale belongs to one output), at most 65536
  *   dtype         JB_F32 or JB_BF16, of x, bias and y alike; sums are fp32. Levels enter bf16
- *                 products with 11 bits and fp32 products with 22; x with all its bits or 22, but
+ *                 products off by at most 1.6e-4 of themselves and fp32 products with 22 bits; x with all its bits or 22, but
  *                 nothing finer than 2^-40 of the largest element of its row
  *   d_x           [n][in_features], 16-byte aligned, rows x_row_stride elements apart (a multiple
  *                 of 16 bytes)

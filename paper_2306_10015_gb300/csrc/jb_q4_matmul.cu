@@ -7,7 +7,7 @@
 // which is how mma.m16n8k16 takes them. So 16 rows of the matrix by 64 columns, a block each, are 16 table reads a lane and
 // four products with up to 8 rows of x; tokens are the product's columns.
 //
-// Numbers. fp16 has 11 bits: a level is off by at most 2^-12, beside the 2^-9 of a bf16 result. bf16 inputs fit fp16 with
+// Numbers. fp16 has 11 bits: a level is off by at most 1.6e-4 of itself (see kLevelScale), beside the 2^-9 of a bf16 result. bf16 inputs fit fp16 with
 // all their bits once they are scaled by a power of two, chosen for each row (of a CTA's slice of the columns) so that the
 // largest is near 2^15 (what is 2^-28 of it or smaller loses bits, 2^-40 of it is lost). fp32: levels and inputs are two fp16 each, 22 bits
 // and more; the inputs' two parts are two columns of the product, and a table read is two words (the product of two lower
@@ -42,7 +42,6 @@ constexpr int kUnit = 512;          // columns of a row that a warp converts at 
 constexpr int kPad = 8;             // halves between rows of inputs: reads of 8 rows meet no bank twice
 constexpr int kRed = 20;            // floats from column to column of a tile's sums, for the same reason
 constexpr int kMostColumns = 64;    // of the product at a time
-constexpr float kLevelScale = 1024.0f;  // of fp32's levels, so that their lower parts are normal numbers
 
 struct Params {
     Q4Matmul m;
@@ -153,7 +152,7 @@ __device__ void stage(const Params& p, const Layout& l, char* shared, int from) 
         // most in [2^e, 2^(e+1)) becomes [2^14, 2^15); powers of two that fp32 has with their inverses
         const int most = most_of[row], e = most > 0 ? min(max((most >> 23) - 127 - 14, -126), 126) : 0;
         const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-        if (lane == 0) powers[row] = __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * (kF32 ? 1.0f / kLevelScale : 1.0f);
+        if (lane == 0) powers[row] = __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * (1.0f / kLevelScale<kF32>);
         if (k >= p.slice) continue;
         uint32_t w[8], r[8];
 #pragma unroll
@@ -193,7 +192,7 @@ __global__ void __launch_bounds__(kMatThreads, 1) q4_matmul_kernel(const __grid_
     {   // the table: the entry of a byte, with a copy for each lane
         __shared__ uint32_t pairs[256][kF32 ? 2 : 1];
         if (threadIdx.x < 256) {
-            const float a = p.levels[threadIdx.x & 15] * (kF32 ? kLevelScale : 1.0f), b = p.levels[threadIdx.x >> 4] * (kF32 ? kLevelScale : 1.0f);
+            const float a = p.levels[threadIdx.x & 15] * kLevelScale<kF32>, b = p.levels[threadIdx.x >> 4] * kLevelScale<kF32>;
             const uint32_t w = halves(a, b);
             pairs[threadIdx.x][0] = w;
             if (kF32) {

@@ -36,7 +36,6 @@ constexpr int kDecodeWarps = 8, kSumWarps = 4;
 constexpr int kTileThreads = 32 * (kDecodeWarps + kSumWarps + 2);
 template <typename T>
 constexpr int kMostRows = sizeof(T) == 4 ? 32 : 64;  // rows of x at a time
-constexpr float kLevelScale = 1024.0f;  // of fp32's levels, so that their lower parts are normal numbers
 constexpr int kTileCtas = 160;          // most
 
 // Rows of converted x: n rounded up to a product's 16 columns, upper parts and then lower parts.
@@ -122,7 +121,7 @@ __global__ void __launch_bounds__(512) q4_convert_kernel(const __grid_constant__
     // most in [2^e, 2^(e+1)) becomes [2^14, 2^15); powers of two that fp32 has with their inverses
     const int e = most > 0.0f ? min(max((__float_as_int(most) >> 23) - 127 - 14, -126), 126) : 0;
     const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-    if (threadIdx.x == 0) p.powers[row] = __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * (kF32 ? 1.0f / kLevelScale : 1.0f);
+    if (threadIdx.x == 0) p.powers[row] = __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * (1.0f / kLevelScale<kF32>);
     __half* upper = p.converted + static_cast<size_t>(row) * in;
     __half* lower = upper + static_cast<size_t>(p.pad) * in;
     const auto convert = [&](const float (&w)[8], int k) {
@@ -187,7 +186,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) q4_tiles_kernel(const __grid_
         for (int i = threadIdx.x; i < 256 * 16; i += kTileThreads) {
             const int byte = i / 16, quad = i % 16;
             if (!kF32 && quad >= 8) continue;
-            const float scale = kF32 ? kLevelScale : 1.0f, a = p.levels[byte & 15] * scale, b = p.levels[byte >> 4] * scale;
+            const float a = p.levels[byte & 15] * kLevelScale<kF32>, b = p.levels[byte >> 4] * kLevelScale<kF32>;
             const uint32_t w = halves(a, b);
             const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&w));
             const uint32_t v = kF32 ? halves(a - h.x, b - h.y) : w;

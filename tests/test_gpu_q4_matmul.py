@@ -277,3 +277,33 @@ def test_large_matrices(out, inner, n):
         want = x.double() @ w.T
         assert (got[:, :-40] == 0).all()
         assert ((got[:, -40:].double() - want).abs() <= bound(x, w, None, want)).all()
+
+
+# A matrix whose column k has the code k % 16 in all rows, scales of 1: a product with few inputs that are not zero tells
+# how well each level is held, whatever the type of the result.
+def columns_of_codes(out, inner):
+    codes = torch.arange(inner, dtype=torch.uint8, device="cuda") & 15
+    return jb.Q4Table([((codes[0::2] | codes[1::2] << 4).repeat(out), torch.ones(out * inner // 64, device="cuda"), out * inner)])
+
+
+KERNELS = [(130, 704, 5), (777, 704, 64), (150, 4160, 64), (130, 65536, 33), (19, 65536, 7)]  # few rows; tiles; tiles; tiles; long
+
+
+@pytest.mark.parametrize("out,inner,n", KERNELS)
+def test_levels_enter_bf16_products_within_2_to_the_minus_12(out, inner, n):
+    """An input of 1 at a code and one at the level -1 that takes away what bf16 has of the code's level: what is left is small
+    and tells the level's own error, at most 2^-12 of it. The sum has two terms, 3 roundings of 2^-22 of 2, and the result is
+    rounded once, half a step of bf16."""
+    table = columns_of_codes(out, inner)
+    level = torch.from_numpy(jb.jb_q4_levels()).cuda()
+    assert level[0] == -1.0
+    for block in (0, 1, inner // 128, inner // 64 - 1):
+        for first in range(0, 16, n):
+            x = torch.zeros(n, inner, dtype=torch.bfloat16, device="cuda")
+            at = torch.arange(first, min(first + n, 16), device="cuda")
+            x[at - first, 64 * block + 16 + at] = 1.0
+            x[at - first, 64 * block + 32] = level[at].bfloat16()
+            got = jb.jb_q4_matmul(table, 0, x, out)[:len(at)].double()
+            want = (level[at].double() - level[at].bfloat16().double())[:, None].expand_as(got)
+            tol = 2.0**-12 * level[at].double().abs()[:, None] + 3 * 2.0**-22 * 2 + 2.0**-8 * want.abs() + 1e-38
+            assert ((got - want).abs() <= tol).all(), ((got - want).abs() / tol).amax().item()
