@@ -307,3 +307,77 @@ def test_levels_enter_bf16_products_within_2_to_the_minus_12(out, inner, n):
             want = (level[at].double() - level[at].bfloat16().double())[:, None].expand_as(got)
             tol = 2.0**-12 * level[at].double().abs()[:, None] + 3 * 2.0**-22 * 2 + 2.0**-8 * want.abs() + 1e-38
             assert ((got - want).abs() <= tol).all(), ((got - want).abs() / tol).amax().item()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("out,inner,n", KERNELS)
+@pytest.mark.parametrize("width", [1, 64])
+def test_blocks_by_themselves(dtype, out, inner, n, width):
+    """Inputs that are zero but for one column, or one block of 64, at the first, second, middle and last blocks: the allowance is
+    that block's alone. With A = sum |x w|: fp32 levels and inputs are two fp16 numbers each, off by at most 2^-22, and the
+    product of two lower parts, 2^-22, is left out; sums take a step for 16 terms, eight of them, each off by at most 2^-22; one
+    more for scales and powers of two. bf16: levels 2^-12, four steps, the result half a step with the tie."""
+    table, g = weights(out, inner, 3), torch.Generator(device="cuda").manual_seed(inner + n)
+    w = dense(table, 0, out, inner)
+    for block in (0, 1, inner // 128, inner // 64 - 1):
+        k = 64 * block + (0 if width == 64 else 37)
+        x = torch.zeros(n, inner, device="cuda")
+        x[:, k:k + width] = torch.randn(n, width, device="cuda", generator=g)
+        x = x.to(DT[dtype])
+        got = jb.jb_q4_matmul(table, 0, x, out).double()
+        want = x[:, k:k + width].double() @ w[:, k:k + width].T
+        a = x[:, k:k + width].double().abs() @ w[:, k:k + width].abs().T
+        tol = a * 12 * 2.0**-22 if dtype == "f32" else a * (2.0**-12 + 5 * 2.0**-22) + 2.0**-8 * want.abs()
+        assert ((got - want).abs() <= tol + 1e-38).all(), (block, ((got - want).abs() / (tol + 1e-38)).amax().item())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_every_level_in_tiles(dtype):
+    """Each code in each place of a block and both blocks of a pair, on the kernel that cuts matrices into tiles."""
+    out, inner = 2049, 320
+    table = weights(out, inner, 5)
+    w = dense(table, 0, out, inner)
+    for first in range(0, inner, 64):
+        x = torch.zeros(64, inner, device="cuda", dtype=DT[dtype])
+        at = torch.arange(64, device="cuda")
+        x[at, first + at] = 1.5
+        got = jb.jb_q4_matmul(table, 0, x, out).double()
+        want = 1.5 * w[:, first:first + 64].T
+        assert ((got - want).abs() <= want.abs() * (2.0**-8 + 2.0**-12 if dtype == "bf16" else 4 * 2.0**-22)).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [24, 40, 100])
+def test_tiles_read_weights_that_were_written_just_before(dtype, n):
+    """Codes and scales change on the stream directly before each product, by the perturbation and by copies, eagerly and in a
+    graph; the kernel reads them ahead of its inputs."""
+    out, inner = 2100, 2048
+    table = weights(out, inner)
+    x = torch.randn(n, inner, device="cuda").to(DT[dtype])
+    codes, scale, _ = table.tensors[0]
+    steps = []
+    for seed in (11, 12, 13):
+        other = weights(out, inner, seed).tensors[0]
+        steps.append(lambda other=other: (codes.copy_(other[0]), scale.copy_(other[1])))
+        steps.append(lambda: jb.jb_perturb_q4(table, (5, 1, 0), 1e-2))
+    def wanted(got):
+        w = dense(table, 0, out, inner)
+        want = x.double() @ w.T
+        assert ((got.double() - want).abs() <= bound(x, w, None, want)).all()
+    torch.cuda.synchronize()
+    for step in steps:
+        step()
+        wanted(jb.jb_q4_matmul(table, 0, x, out))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    y = torch.empty(len(steps), n, out, dtype=DT[dtype], device="cuda")
+    with torch.cuda.graph(graph):
+        for i, step in enumerate(steps):
+            step()
+            jb.jb_q4_matmul(table, 0, x, out, out=y[i])
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    for i, step in enumerate(steps):
+        step()
+        assert torch.equal(jb.jb_q4_matmul(table, 0, x, out), y[i])
