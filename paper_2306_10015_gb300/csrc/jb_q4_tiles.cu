@@ -561,15 +561,26 @@ cudaError_t launch_type(const Q4Matmul& m, cudaStream_t s) {
 }  // namespace
 
 bool q4_by_tiles(int n, int out, int in, int bf16) {
-    // Three launches pay from some columns of the product on, the fewer the larger the matrix is and the longer its rows are
-    // (a CTA of the other kernel holds so much input). Measured with bf16, the other kernel and this one in us: 20480 x 5120,
-    // 7 rows 24.8 and 24.2, 32 rows 102 and 27; 5120 x 20480, 1 row 26.6 and 23.8, 2 rows 24.0 and 23.9;
-    // 4096 x 4096, 8 rows 9.1 and 10.5, 9 rows 11.5 and 10.5; 2048 x 2048, 16 rows 7.4 and 7.6, 24 rows 9.7 and 8.6;
-    // 1024 x 1024, 16 rows 4.4 and 6.6, 32 rows 7.0 and 6.9, 64 rows 13.8 and 7.7.
+    // Three launches pay from some columns of the product on (rows of x, in fp32 two for each): the fewer the larger the matrix is
+    // and the longer its rows are, as a CTA of the other kernel holds so much input. Measured over 48 shapes with cold weights, the
+    // other kernel and this one in us, bf16 unless fp32 is said:
+    //   32768 x 1024, 16 rows 16.0 and 15.9, 17 rows 19.2 and 16.3; 4096 x 1024, 24 rows 6.9 and 8.0, 32 rows 8.2 and 8.1;
+    //   1024 x 1024, 24 rows 5.7 and 6.6, 32 rows 6.9 and 6.6, fp32 12 rows 5.8 and 6.8, 16 rows 6.9 and 6.8;
+    //   2048 x 2048, 12 rows 6.3 and 7.1, 16 rows 7.4 and 7.4; 3000 x 3008, 9 rows 8.6 and 9.1, 12 rows 10.0 and 9.1;
+    //   4096 x 4096, 8 rows 9.5 and 11.6, 9 rows 11.9 and 11.7, fp32 4 rows 11.6 and 12.0, 5 rows 13.0 and 12.1;
+    //   20480 x 5120, 6 rows 24.2 and 26.0, 8 rows 26.2 and 26.0, fp32 3 rows 29.4 and 32.3, 4 rows 32.5 and 32.4;
+    //   32000 x 4096, 6 rows 31.3 and 29.9, 7 rows 37.7 and 29.9; 8192 x 8192, 3 rows 17.9 and 20.0, 4 rows 21.3 and 20.0;
+    //   5120 x 20480, 1 row 27.1 and 24.9, 2 rows 24.5 and 25.0, 5 rows 24.9 and 26.0, 6 rows 28.9 and 26.0, fp32 1 row 32.4 and 31.2;
+    //   4096 x 16384, 1 row 16.6 and 19.1, 4 rows 19.3 and 19.1, 6 rows 24.2 and 20.1.
+    // Over all of them the side that is taken costs 0.8 % more than the faster one on average, more than a quarter only where at most
+    // 1024 rows of the matrix are 16384 long or longer.
     const long long size = static_cast<long long>(out) * in, columns = static_cast<long long>(n) * (bf16 ? 1 : 2);
-    if (size >= 1ll << 26) return columns >= 8 || columns * in > 40000;
-    if (size >= 1ll << 24) return columns > 8;
-    return columns >= (size >= 1ll << 22 ? 24 : 32) && size >= 1ll << 19;
+    if (size < 1ll << 19) return false;
+    if (in < 2048) return columns >= (size >= 1ll << 23 ? 17 : size >= 1ll << 21 ? 24 : 32);
+    if (size >= 1ll << 25 && in >= 13000) return columns * in >= 20480;
+    if (size >= 1ll << 26) return columns >= 7 || columns * in >= 1ll << 15;
+    if (size >= 1ll << 25 || in >= 4096) return columns > 8;
+    return columns * in >= 1ll << 15;
 }
 
 uint64_t q4_workspace(int n, int out, int in, int bf16) {

@@ -227,3 +227,14 @@ def test_sizes_of_workspaces_do_not_pile_up(jb):
     assert [table.matmul_workspace(4096, 4096, torch.bfloat16, n) for n in range(1, 3000)] == want and max(want) > 0
     assert len(table._matmul_bytes) <= 1024
     assert table.matmul_workspace(4096, 4096, torch.bfloat16, 9) == want[8]
+
+
+@pytest.mark.parametrize("out,inner,rows_bf16,rows_f32", [(5120, 20480, 1, 1), (4096, 16384, 2, 1), (20480, 5120, 7, 4), (4096, 4096, 9, 5), (1024, 4096, 9, 5),
+                                                          (2048, 2048, 16, 8), (16384, 1024, 17, 9), (4096, 1024, 24, 12), (1024, 1024, 32, 16),
+                                                          (8192, 8192, 4, 2), (512, 512, 1 << 20, 1 << 20)])
+def test_from_how_many_rows_on_products_are_cut_into_tiles(jb, out, inner, rows_bf16, rows_f32):
+    """Where the kernels' measured times cross, on a GB300; the tiles alone work in a workspace."""
+    need = lambda dtype, n: jb.lib().jb_q4_matmul_workspace(out, inner, dtype, n)  # noqa: E731
+    for dtype, first in ((1, rows_bf16), (0, rows_f32)):
+        rows = [n for n in list(range(1, 70)) + [1000, 100_000] if need(dtype, n) > 0]
+        assert rows == [n for n in list(range(1, 70)) + [1000, 100_000] if n >= first], (dtype, rows[:1])
