@@ -207,7 +207,7 @@ cudaError_t launch_append(const Pages& pages, const Append& a, cudaStream_t s) {
     p.magic = magic_of(p.units);
     p.vec_magic = magic_of(p.vecs);
     // a token's heads are shared out while that fills the GPU
-    const uint32_t most = ((a.q_heads + a.heads) * p.units + kThreads - 1) / kThreads, want = (152 * 8 + a.n - 1) / a.n;
+    const uint32_t most = ((a.q_heads + a.heads) * p.units + kThreads - 1) / kThreads, want = (152u * 8 + a.n - 1) / a.n;
     const dim3 grid(a.n, most < want ? most : want);
     cudaLaunchConfig_t c = {};
     cudaLaunchAttribute attr;

@@ -149,3 +149,18 @@ def test_a_graph_and_another_stream():
         stream.synchronize()
         at = lambda t: cache.keys[0][cache.pages.table[0, t // 16].long(), :, t % 16]  # noqa: E731
         assert torch.equal(out, again) and torch.equal(at(p), at(p + 1))
+
+
+def test_as_many_tokens_as_a_list_can_have():
+    """2^31 - 1 of them, of which the last one alone has a place; keys and values are one token's, again and again."""
+    n = (1 << 31) - 1
+    cache = make("bf16", [5], 2, 64, 16, fill=9.0)
+    where = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    where[-1] = 0
+    k, v = (torch.randn(1, 2, 64, device="cuda").bfloat16() for _ in range(2))
+    before = [x.clone() for x in (cache.keys[0], cache.values[0])]
+    none = jb.Rotation(torch.zeros(32, dtype=torch.int64, device="cuda"))
+    jb.jb_cache_append(cache, 0, None, k.expand(n, 2, 64), v.expand(n, 2, 64), where, where, none)
+    page = int(cache.pages.table[0, 0])
+    before[0][page, :, 0], before[1][page, :, 0] = k[0], v[0]
+    assert torch.equal(cache.keys[0], before[0]) and torch.equal(cache.values[0], before[1])
