@@ -547,6 +547,7 @@ uint64_t jb_cache_keep_workspace(const jb_trees* trees);
  *                 nothing finer than 2^-40 of the largest element of its row
  *   d_x           [n][in_features], 16-byte aligned, rows x_row_stride elements apart (a multiple
  *                 of 16 bytes)
+ *   n             at most 2^30
  *   d_bias        [out_features], or NULL
  *   d_y           [n][out_features], rows y_row_stride elements apart; shares no byte with what is
  *                 read: JB_ERR_INVALID_ARG

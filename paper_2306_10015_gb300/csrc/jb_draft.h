@@ -13,6 +13,7 @@ namespace jb {
 constexpr int kMaxNodes = 256;           // drafted tokens of a tree
 constexpr int kMaxInner = 65536;         // columns of a matrix of 4-bit weights
 constexpr int kMaxOutputs = 1 << 30;     // its rows
+constexpr int kMaxMatmulRows = 1 << 30;  // rows that it is multiplied with: passes over them end below 2^31
 constexpr int kMaxAppendVecs = 1 << 20;  // 16-byte vectors of a token's queries and keys
 
 struct Append {

@@ -210,7 +210,7 @@ JB_EXPORT int jb_attend_tree(const jb_pages* pages, const jb_kv* layer, const jb
 }
 
 JB_EXPORT uint64_t jb_q4_matmul_workspace(int out_features, int in_features, int dtype, int n) {
-    if ((dtype != JB_F32 && dtype != JB_BF16) || out_features < 1 || out_features > kMaxOutputs || in_features < 64 || in_features % 64 != 0 || in_features > kMaxInner || n < 0) return 0;
+    if ((dtype != JB_F32 && dtype != JB_BF16) || out_features < 1 || out_features > kMaxOutputs || in_features < 64 || in_features % 64 != 0 || in_features > kMaxInner || n < 0 || n > kMaxMatmulRows) return 0;
     return q4_workspace(n, out_features, in_features, dtype == JB_BF16);
 }
 
@@ -219,7 +219,7 @@ JB_EXPORT int jb_q4_matmul(const jb_q4_segment* weights, int out_features, int i
                            struct CUstream_st* stream) {
     return guarded([&] {
         if (dtype != JB_F32 && dtype != JB_BF16) return static_cast<int>(JB_ERR_UNSUPPORTED_DTYPE);
-        if (weights == nullptr || out_features < 1 || out_features > kMaxOutputs || in_features < 64 || in_features % 64 != 0 || in_features > kMaxInner || n < 0 ||
+        if (weights == nullptr || out_features < 1 || out_features > kMaxOutputs || in_features < 64 || in_features % 64 != 0 || in_features > kMaxInner || n < 0 || n > kMaxMatmulRows ||
             x_row_stride > (1ull << 48) || y_row_stride > (1ull << 48))
             return static_cast<int>(JB_ERR_INVALID_ARG);
         if (weights->numel != static_cast<uint64_t>(out_features) * in_features) return static_cast<int>(JB_ERR_INVALID_ARG);

@@ -238,3 +238,14 @@ def test_from_how_many_rows_on_products_are_cut_into_tiles(jb, out, inner, rows_
     for dtype, first in ((1, rows_bf16), (0, rows_f32)):
         rows = [n for n in list(range(1, 70)) + [1000, 100_000] if need(dtype, n) > 0]
         assert rows == [n for n in list(range(1, 70)) + [1000, 100_000] if n >= first], (dtype, rows[:1])
+
+
+def test_products_of_more_rows_than_2_to_the_30(jb):
+    """Passes over the rows count them in 31 bits, beyond the last of which there is no room."""
+    most = 1 << 30
+    for dtype in (0, 1):
+        for n in (most + 1, (1 << 31) - 1):
+            assert q4(jb, n=n, dtype=dtype, xs=0, out=1, numel=256, ys=1) == INV
+            assert jb.lib().jb_q4_matmul_workspace(4096, 4096, dtype, n) == 0
+        assert q4(jb, n=most, dtype=dtype, xs=0, out=1, numel=256, ys=1, bias=FAKE + 1) == MIS   # a misaligned bias ends it, not its rows
+        assert jb.lib().jb_q4_matmul_workspace(4096, 4096, dtype, most) > 0
