@@ -23,7 +23,7 @@ ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["jb_kernels.cu", "jb_q4.cu", "jb_attend.cu", "jb_pages.cu", "jb_sample.cu", "jb_capi.cpp",
            "jb_answer_capi.cpp", "jb_append.cu", "jb_keep.cu", "jb_tree.cu", "jb_tree_bf16.cu", "jb_q4_matmul.cu", "jb_q4_tiles.cu", "jb_draft_capi.cpp"]
 HEADERS = ["jb_rng.cuh", "jb_internal.h", "jb_offgrid.h", "jb_answer.h", "jb_host.h", "jb_launch.cuh",
-           "jb_check.h", "jb_draft.h", "jb_scores.cuh", "jb_tree.cuh", "jb_tcgen05.cuh", "jb_tensor_map.h"]
+           "jb_check.h", "jb_draft.h", "jb_scores.cuh", "jb_tree.cuh", "jb_tcgen05.cuh", "jb_tensor_map.h", "jb_q4_halves.cuh"]
 
 
 def nvcc() -> str:

@@ -209,20 +209,12 @@ cudaError_t launch_append(const Pages& pages, const Append& a, cudaStream_t s) {
     // a token's heads are shared out while that fills the GPU
     const uint32_t most = ((a.q_heads + a.heads) * p.units + kThreads - 1) / kThreads, want = (152u * 8 + a.n - 1) / a.n;
     const dim3 grid(a.n, most < want ? most : want);
-    cudaLaunchConfig_t c = {};
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    c.gridDim = grid;
-    c.blockDim = dim3(kThreads);
-    c.stream = s;
-    c.attrs = &attr;
-    c.numAttrs = 1;
+    const auto start = [&](auto kernel) { return launch(kernel, grid, kThreads, 0, 0, s, p); };
     using B = __nv_bfloat16;
     switch (pairing) {
-        case kNext: return a.bf16 ? cudaLaunchKernelEx(&c, append_kernel<B, kNext>, p) : cudaLaunchKernelEx(&c, append_kernel<float, kNext>, p);
-        case kHalves: return a.bf16 ? cudaLaunchKernelEx(&c, append_kernel<B, kHalves>, p) : cudaLaunchKernelEx(&c, append_kernel<float, kHalves>, p);
-        default: return a.bf16 ? cudaLaunchKernelEx(&c, append_kernel<B, kOddHalves>, p) : cudaLaunchKernelEx(&c, append_kernel<float, kOddHalves>, p);
+        case kNext: return a.bf16 ? start(append_kernel<B, kNext>) : start(append_kernel<float, kNext>);
+        case kHalves: return a.bf16 ? start(append_kernel<B, kHalves>) : start(append_kernel<float, kHalves>);
+        default: return a.bf16 ? start(append_kernel<B, kOddHalves>) : start(append_kernel<float, kOddHalves>);
     }
 }
 

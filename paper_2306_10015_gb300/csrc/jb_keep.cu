@@ -147,16 +147,7 @@ cudaError_t launch_keep_plan(const Pages& p, const Trees& t, const int* leaves, 
 
 cudaError_t launch_keep_move(const Pages& p, const Trees& t, const Pools& pools, const int* ws, cudaStream_t s) {
     const int parts = static_cast<int>((static_cast<uint64_t>(pools.slabs) * pools.row_vecs + kMoveThreads - 1) / kMoveThreads);
-    cudaLaunchConfig_t c = {};
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    c.gridDim = dim3(static_cast<unsigned>(t.n) * parts, pools.n);
-    c.blockDim = dim3(kMoveThreads);
-    c.stream = s;
-    c.attrs = &attr;
-    c.numAttrs = 1;
-    return cudaLaunchKernelEx(&c, keep_move_kernel, p, t, pools, parts, ws);
+    return launch(keep_move_kernel, dim3(static_cast<unsigned>(t.n) * parts, pools.n), kMoveThreads, 0, 0, s, p, t, pools, parts, ws);
 }
 
 }  // namespace jb

@@ -13,7 +13,7 @@ __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.
 
 // Enqueues a kernel on clusters of `cluster` CTAs (0: none).
 template <typename... Params, typename... Args>
-cudaError_t launch(void (*kernel)(Params...), unsigned grid, unsigned block, size_t shared, unsigned cluster, cudaStream_t s,
+cudaError_t launch(void (*kernel)(Params...), dim3 grid, unsigned block, size_t shared, unsigned cluster, cudaStream_t s,
                    const Args&... args) {
     cudaLaunchAttribute a[2];
     a[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -22,7 +22,7 @@ cudaError_t launch(void (*kernel)(Params...), unsigned grid, unsigned block, siz
     a[1].val.clusterDim.x = cluster;
     a[1].val.clusterDim.y = a[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t c = {};
-    c.gridDim = dim3(grid);
+    c.gridDim = grid;
     c.blockDim = dim3(block);
     c.dynamicSmemBytes = shared;
     c.stream = s;

@@ -513,16 +513,7 @@ cudaError_t launch_compact_move(const Pages& p, const Pools& pools, bool table, 
 
 cudaError_t launch_write(const Pages& p, const Write& w, cudaStream_t s) {
     const unsigned vecs = w.heads * w.head_vecs, parts = (vecs + 32 * kVecs - 1) / (32 * kVecs);
-    cudaLaunchConfig_t c = {};
-    cudaLaunchAttribute a;
-    a.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    a.val.programmaticStreamSerializationAllowed = 1;
-    c.gridDim = dim3((w.n + 7u) / 8u, 2 * parts);
-    c.blockDim = dim3(256);
-    c.stream = s;
-    c.attrs = &a;
-    c.numAttrs = 1;
-    return cudaLaunchKernelEx(&c, write_kernel, p, w);
+    return launch(write_kernel, dim3((w.n + 7u) / 8u, 2 * parts), 256, 0, 0, s, p, w);
 }
 
 }  // namespace jb

@@ -31,6 +31,7 @@
 #include "jb_draft.h"
 #include "jb_internal.h"
 #include "jb_launch.cuh"
+#include "jb_q4_halves.cuh"
 
 namespace jb {
 namespace {
@@ -89,11 +90,6 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-__device__ __forceinline__ uint32_t halves(float lo, float hi) {
-    const __half2 h = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
-
 // 16 inputs of a row in fp32.
 __device__ __forceinline__ void read16(const float* from, float (&x)[16]) {
 #pragma unroll
@@ -149,22 +145,13 @@ __device__ void stage(const Params& p, const Layout& l, char* shared, int from) 
     for (int u = warp; u < units; u += kMatWarps) {
         const int row = u / groups, k = (u - row * groups) * kUnit + 16 * lane;
         if (units > kMatWarps) read(row, k);
-        // most in [2^e, 2^(e+1)) becomes [2^14, 2^15); powers of two that fp32 has with their inverses
-        const int most = most_of[row], e = most > 0 ? min(max((most >> 23) - 127 - 14, -126), 126) : 0;
-        const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-        if (lane == 0) powers[row] = __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * (1.0f / kLevelScale<kF32>);
+        const int e = exponent_of(__int_as_float(most_of[row]));
+        const float down = scaled_down(e);
+        if (lane == 0) powers[row] = scaled_up<kF32>(e);
         if (k >= p.slice) continue;
         uint32_t w[8], r[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float a = v[2 * i] * down, b = v[2 * i + 1] * down;
-            w[i] = halves(a, b);
-            if (kF32) {  // what is not finite is all lower part: the lower parts of levels, which may be 0, do not meet it
-                w[i] = halves(isfinite(a) ? a : 0.0f, isfinite(b) ? b : 0.0f);
-                const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-                r[i] = halves(a - h.x, b - h.y);
-            }
-        }
+        for (int i = 0; i < 8; ++i) split<kF32>(v[2 * i] * down, v[2 * i + 1] * down, w[i], r[i]);
         __half* to = inputs + (kF32 ? 2 * row : row) * (p.slice + kPad) + k;
         reinterpret_cast<uint4*>(to)[0] = make_uint4(w[0], w[1], w[2], w[3]);
         reinterpret_cast<uint4*>(to)[1] = make_uint4(w[4], w[5], w[6], w[7]);

@@ -24,6 +24,7 @@
 #include "jb_draft.h"
 #include "jb_internal.h"
 #include "jb_launch.cuh"
+#include "jb_q4_halves.cuh"
 #include "jb_tcgen05.cuh"
 #include "jb_tensor_map.h"
 
@@ -62,11 +63,6 @@ struct TileParams {
     float* powers;      // [pad]
     float* sums;        // [tile][part][row of x][row of the matrix]
 };
-
-__device__ __forceinline__ uint32_t halves(float lo, float hi) {
-    const __half2 h = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
 
 __device__ __forceinline__ void read8(const float* from, float (&x)[8]) {
     const float4 a = reinterpret_cast<const float4*>(from)[0], b = reinterpret_cast<const float4*>(from)[1];
@@ -118,24 +114,15 @@ __global__ void __launch_bounds__(512) q4_convert_kernel(const __grid_constant__
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 16; ++i) most = fmaxf(most, most_of[i]);
-    // most in [2^e, 2^(e+1)) becomes [2^14, 2^15); powers of two that fp32 has with their inverses
-    const int e = most > 0.0f ? min(max((__float_as_int(most) >> 23) - 127 - 14, -126), 126) : 0;
-    const float down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-    if (threadIdx.x == 0) p.powers[row] = __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * (1.0f / kLevelScale<kF32>);
+    const int e = exponent_of(most);
+    const float down = scaled_down(e);
+    if (threadIdx.x == 0) p.powers[row] = scaled_up<kF32>(e);
     __half* upper = p.converted + static_cast<size_t>(row) * in;
     __half* lower = upper + static_cast<size_t>(p.pad) * in;
     const auto convert = [&](const float (&w)[8], int k) {
         uint32_t a[4], b[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float lo = w[2 * i] * down, hi = w[2 * i + 1] * down;
-            a[i] = halves(lo, hi);
-            if (kF32) {  // what is not finite is all lower part: the lower parts of levels, which may be 0, do not meet it
-                a[i] = halves(isfinite(lo) ? lo : 0.0f, isfinite(hi) ? hi : 0.0f);
-                const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&a[i]));
-                b[i] = halves(lo - h.x, hi - h.y);
-            }
-        }
+        for (int i = 0; i < 4; ++i) split<kF32>(w[2 * i] * down, w[2 * i + 1] * down, a[i], b[i]);
         *reinterpret_cast<uint4*>(upper + k) = make_uint4(a[0], a[1], a[2], a[3]);
         if (kF32) *reinterpret_cast<uint4*>(lower + k) = make_uint4(b[0], b[1], b[2], b[3]);
     };
@@ -543,16 +530,7 @@ cudaError_t launch_type(const Q4Matmul& m, cudaStream_t s) {
         else if (p.pad == 32) e = launch_pad<T, 32>(p, ctas, s);
         else if constexpr (kMostRows<T> == 64) e = p.pad == 48 ? launch_pad<T, 48>(p, ctas, s) : launch_pad<T, 64>(p, ctas, s);
         if (e != cudaSuccess) return e;
-        cudaLaunchConfig_t c = {};
-        cudaLaunchAttribute attr;
-        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr.val.programmaticStreamSerializationAllowed = 1;
-        c.gridDim = dim3(tiles, p.rows);
-        c.blockDim = dim3(128);
-        c.stream = s;
-        c.attrs = &attr;
-        c.numAttrs = 1;
-        e = cudaLaunchKernelEx(&c, q4_join_kernel<T>, p);
+        e = launch(q4_join_kernel<T>, dim3(tiles, p.rows), 128, 0, 0, s, p);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;

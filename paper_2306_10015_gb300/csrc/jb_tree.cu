@@ -15,7 +15,6 @@
 // nodes: 160 us for 72 us of bytes; up to 33 nodes: 253 us). Two warps a scheduler reach neither: each waits for its own
 // reads of shared memory and copies of two tiles ahead are all that fits. With 16 rows a warp and the same parts small trees
 // took 1.3 to 2.3 times as long, large ones 0.95 to 1.15 times.
-#include <atomic>
 #include <numeric>
 
 #include <cuda_bf16.h>
@@ -381,29 +380,11 @@ __global__ void __launch_bounds__(kThreads, Shape<D, kGroups>::kCtas) tree_kerne
     write_zeros<float, typename S::C, kThreads>(p);
 }
 
-// SMs of a device, asked for once, and the kernel's share of shared memory set.
-constexpr int kDevices = 64;
-template <auto kKernel>
-cudaError_t resident(int shared, int each, int& ctas) {
-    static std::atomic<int> known[kDevices];
-    int device = 0, sms = 0;
-    cudaError_t e = cudaGetDevice(&device);
-    if (e != cudaSuccess) return e;
-    ctas = device < kDevices ? known[device].load(std::memory_order_relaxed) : 0;
-    if (ctas > 0) return cudaSuccess;
-    e = cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
-    if (e != cudaSuccess) return e;
-    ctas = each * (sms < kSms ? sms : kSms);
-    if (device < kDevices) known[device].store(ctas, std::memory_order_relaxed);
-    return cudaSuccess;
-}
-
 template <int D, int kGroups, bool kExtra>
 cudaError_t launch_extra(const TreeParams& p, cudaStream_t s) {
     using S = Shape<D, kGroups>;
     int ctas = 0;
-    cudaError_t e = resident<tree_kernel<D, kGroups, kExtra>>(S::kShared, S::kCtas, ctas);
+    cudaError_t e = resident<tree_kernel<D, kGroups, kExtra>>(S::kShared, S::kCtas, kSms * S::kCtas, ctas);
     if (e != cudaSuccess) return e;
     F32Params f;
     f.t = p;

@@ -7,6 +7,8 @@
 // values, maximum, sum) in the workspace, which join_kernel adds up in the order of the line: results do not depend on
 // which CTA was first.
 #pragma once
+#include <atomic>
+
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -382,17 +384,26 @@ inline cudaError_t describe_pool(Encode encode, CUtensorMap& map, const TreePara
 
 template <typename T, int D, typename C>
 cudaError_t launch_join(const TreeParams& p, int ctas, cudaStream_t s) {
-    cudaLaunchConfig_t c = {};
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
     constexpr int kAt = kJoinThreads / (D / 4);
-    c.gridDim = dim3(ctas, (C::kRows + kAt - 1) / kAt);
-    c.blockDim = dim3(kJoinThreads);
-    c.stream = s;
-    c.attrs = &attr;
-    c.numAttrs = 1;
-    return cudaLaunchKernelEx(&c, join_kernel<T, D, C>, p);
+    return launch(join_kernel<T, D, C>, dim3(ctas, (C::kRows + kAt - 1) / kAt), kJoinThreads, 0, 0, s, p);
+}
+
+// CTAs of a kernel, `each` on an SM and `most` at most: the device's SMs are asked for once, and the kernel's share of shared memory set.
+constexpr int kDevices = 64;
+template <auto kKernel>
+cudaError_t resident(int shared, int each, int most, int& ctas) {
+    static std::atomic<int> known[kDevices];
+    int device = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    ctas = device < kDevices ? known[device].load(std::memory_order_relaxed) : 0;
+    if (ctas > 0) return cudaSuccess;
+    e = cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    if (e != cudaSuccess) return e;
+    ctas = sms * each < most ? sms * each : most;
+    if (device < kDevices) known[device].store(ctas, std::memory_order_relaxed);
+    return cudaSuccess;
 }
 
 }  // namespace

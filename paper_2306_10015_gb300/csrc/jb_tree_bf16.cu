@@ -23,7 +23,6 @@
 // values: a warp issued one in 170 cycles, 10000 for 128 positions. Eight warps for a group's softmax, two threads a row, were
 // no faster (757 and 741 us for the long rows): what they gain in waits they lose in registers and barriers.
 #include <algorithm>
-#include <atomic>
 #include <numeric>
 
 #include <cuda_bf16.h>
@@ -713,24 +712,6 @@ __global__ void __launch_bounds__(Shape<D, kGroups>::kThreads, Shape<D, kGroups>
     tc_fence_after();
     if (warp == kSoftmaxWarps) tmem_free(c.tmem, S::kColumns);
     write_zeros<T, typename S::C, kThreads>(p);
-}
-
-// SMs of a device, asked for once, and the kernel's share of shared memory set.
-constexpr int kDevices = 64;
-template <auto kKernel>
-cudaError_t resident(int shared, int each, int most, int& ctas) {
-    static std::atomic<int> known[kDevices];
-    int device = 0, sms = 0;
-    cudaError_t e = cudaGetDevice(&device);
-    if (e != cudaSuccess) return e;
-    ctas = device < kDevices ? known[device].load(std::memory_order_relaxed) : 0;
-    if (ctas > 0) return cudaSuccess;
-    e = cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
-    if (e != cudaSuccess) return e;
-    ctas = sms * each < most ? sms * each : most;
-    if (device < kDevices) known[device].store(ctas, std::memory_order_relaxed);
-    return cudaSuccess;
 }
 
 template <int D, int kGroups>
