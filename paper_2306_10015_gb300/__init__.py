@@ -361,7 +361,7 @@ class Q4Table:
                 raise ValueError("codes or scales too short for numel")
             self.segments[i] = jb_q4_segment(codes.data_ptr(), scale.data_ptr(), int(numel), int(fo))
         self.n_segments = n
-        self._workspaces, self._matmul_bytes, self._lock = _Workspaces(), {}, threading.Lock()
+        self._workspaces, self._matmul_bytes, self._lock = _Workspaces(), {}, threading.RLock()
 
     def matmul_workspace(self, out_features: int, in_features: int, dtype, n: int) -> int:
         """Device bytes that jb_q4_matmul of n rows (of a torch type) with such a matrix works in."""
@@ -414,7 +414,8 @@ def _need_torch():
 
 # A call is one launch or several, over a workspace that is kept for the stream and over the tables of the pages. Launches
 # of another host thread's call must not come between them (its stream may be the same one, and the interpreter is free
-# during a call), so calls on one PageTable, and calls on one Q4Table, are enqueued one at a time: its _lock.
+# during a call), so calls on one PageTable, and calls on one Q4Table, are enqueued one at a time: its _lock. A thread may take it again, for
+# a finalizer that runs where a call asks for memory.
 #
 # The tensors of a call are on one device, and that is the current one: a kernel of another device would take their
 # addresses for its own memory's. `device` is the number of the cache's or, of jb_sample, of the logits'.
@@ -471,7 +472,7 @@ class PageTable:
         self.struct = jb_pages(table.data_ptr(), lens.data_ptr(), refs.data_ptr(), table.shape[0],
                                table.shape[1], refs.shape[0], self.page_tokens)
         self.ref = ctypes.byref(self.struct)
-        self._bytes, self._lock = {}, threading.Lock()
+        self._bytes, self._lock = {}, threading.RLock()
 
     def workspace(self, n: int) -> int:
         """Device bytes that jb_cache_fork of n pairs works in, or jb_cache_compact (n = 0)."""

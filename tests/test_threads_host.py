@@ -106,3 +106,20 @@ def test_a_call_that_fails_leaves_the_others_free(slow, jb):  # noqa: F811
             call()
     all_at_once([of_cache[1], of_table[1]])
     assert library.calls == 6
+
+
+def test_a_finalizer_may_call_while_its_thread_is_in_a_call(slow, jb, monkeypatch):  # noqa: F811
+    """The collector runs where memory is asked for, and with it whatever frees the rows of an answer that nobody holds."""
+    library, (of_cache, of_table, _) = slow
+    seen = []
+
+    def new(stream, make, *args, **kw):
+        if not seen and make is not __import__("torch").cuda.is_current_stream_capturing:
+            seen.append(1)
+            of_cache[4]()                                                 # jb_cache_free, of the same pages
+        return make(*args, **kw)
+    monkeypatch.setattr(jb, "_new", new)
+    t = threading.Thread(target=of_cache[0], daemon=True)                 # jb_attend_tree, which makes its workspace
+    t.start()
+    t.join(10)
+    assert not t.is_alive() and seen and library.calls == 2
